@@ -418,6 +418,25 @@ rwkvq_status rwkvq_gemm_prefill_grouped(const rwkvq_prefill_op* ops, int n_ops, 
                                         void* stream);
 
 /*
+ * Eight-bit floating point (e4m3) with one scale per block of 128 columns, beside the two packed formats: for what does not suit three bits.
+ * rwkvq_fp8_quantize: x_dev[rows][cols] (F32, F16 or BF16, x_row elements from row to row) to codes_dev[rows][cols] (one byte each).  A group is
+ *      128 columns of one row (block_rows 1: activations) or of 128 rows (block_rows 128: weights); the last may be smaller.
+ *      scale_dev[ceil(rows / block_rows)][rwkvq_fp8_scale_pitch(cols)]: byte g of a row is e + 127 of group g, whose scale 2^e is the smallest power of
+ *      two (e >= -126) with max|x| <= 448 * 2^e, or 1 where all are zero; bytes behind the last group are written or left and never mean
+ *      anything.  A code is x * 2^-e rounded to nearest even.  NaN and infinities become NaN codes and do not count for the scale.
+ * rwkvq_gemm_fp8: Y[t][i] = sum_k x_hat[t][k] * w_hat[i][k] over such codes, w with block_rows 128 ([oc][ic]), x with block_rows 1 ([M][ic]),
+ *      accumulated in fp32 on the tensor cores; 1 <= M.  Y_dev: F32, F16 or BF16, y_row >= oc elements from row to row.  A scale byte of 255 gives NaN.
+ *      A device-side wait that ran out shows in rwkvq_device_status (ETIMEOUT).
+ * All pointers 16-byte aligned (x_row too), nothing overlaps; asynchronous on `stream`, no workspace.
+ * Errors: EINVAL, ESHAPE (cols or ic not a multiple of 16), EALIGN, EUNSUPPORTED (more than 2^30 groups or tiles), ECUDA.
+ */
+size_t rwkvq_fp8_scale_pitch(int cols);
+rwkvq_status rwkvq_fp8_quantize(const void* x_dev, int dtype, int rows, int cols, long long x_row, int block_rows,
+                                void* codes_dev, void* scale_dev, void* stream);
+rwkvq_status rwkvq_gemm_fp8(const void* w_codes_dev, const void* w_scale_dev, int oc, int ic, const void* x_codes_dev,
+                            const void* x_scale_dev, int M, void* Y_dev, int y_dtype, long long y_row, void* stream);
+
+/*
  * Decode the packed matrix to out_dev[oc][ic]: F32 = the exact value s*(q-z) (two IEEE fp32
  * operations: subtract, then multiply) or the fp16 codebook entry; BF16 = that value rounded to
  * nearest even.  Uses the same device unpack routines as the products (test surface for

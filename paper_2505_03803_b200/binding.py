@@ -87,6 +87,7 @@ EXPORTS = [
     "rwkvq_proxy_segments_workspace_bytes", "rwkvq_proxy_segments", "rwkvq_tau_for_fraction", "rwkvq_tau_largest_gap", "rwkvq_quant_error_workspace_bytes", "rwkvq_quant_error",
     "rwkvq_desc_for", "rwkvq_quantize_workspace_bytes", "rwkvq_quantize_dev", "rwkvq_calib_representative",
     "rwkvq_quantize_dev_async", "rwkvq_quantize_dev_lost", "rwkvq_quantize_check",
+    "rwkvq_fp8_scale_pitch", "rwkvq_fp8_quantize", "rwkvq_gemm_fp8",
 ]
 
 _lib = None
@@ -170,6 +171,12 @@ def lib() -> C.CDLL:
         L.rwkvq_quantize_dev_async.argtypes = L.rwkvq_quantize_dev.argtypes
         L.rwkvq_quantize_dev_lost.argtypes = [vp, i32, i32, C.POINTER(QuantCfg), vp, vp, sz, vp, sz, C.c_uint32, C.c_uint32, vp]
         L.rwkvq_quantize_check.argtypes = [vp, vp]
+    if hasattr(L, "rwkvq_gemm_fp8"):
+        i64 = C.c_longlong
+        L.rwkvq_fp8_scale_pitch.argtypes = [i32]
+        L.rwkvq_fp8_scale_pitch.restype = sz
+        L.rwkvq_fp8_quantize.argtypes = [vp, i32, i32, i32, i64, i32, vp, vp, vp]
+        L.rwkvq_gemm_fp8.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, i64, vp]
     _lib = L
     return L
 
@@ -653,3 +660,75 @@ def rwkvq_calib_representative(samples, pct: float, rep=None, rep_sq=None, strea
     S, n = samples.shape
     _check(lib().rwkvq_calib_representative(_dev_ptr(samples), S, n, float(pct), _dev_ptr(rep), _dev_ptr(rep_sq),
                                             _stream_ptr(stream)), "rwkvq_calib_representative")
+
+
+def _refuse(where: str, why: str):
+    e = RwkvqError(1, where)
+    e.args = (f"{e.args[0]}: {why}",)
+    raise e
+
+
+_DTYPES = None
+
+
+def _dtype_of(t) -> int:
+    """RWKVQ_F32 / F16 / BF16 of a tensor, -1 for another type."""
+    global _DTYPES
+    if _DTYPES is None:
+        m = _torch or _load_torch()
+        _DTYPES = {m.float32: RWKVQ_F32, m.float16: RWKVQ_F16, m.bfloat16: RWKVQ_BF16}
+    return _DTYPES.get(t.dtype, -1)
+
+
+def _check_device(where: str, *tensors):
+    """All on the current CUDA device: the library launches there."""
+    t = _torch or _load_torch()
+    here = t.cuda.current_device() if t.cuda.is_available() else -1
+    for x in tensors:
+        if x is not None and (not x.is_cuda or x.get_device() != here):
+            _refuse(where, f"a tensor is on {x.device}, the current device is cuda:{here}")
+
+
+def _bytes_of(where: str, x, rows: int, cols: int, what: str):
+    if x.element_size() != 1 or x.dim() != 2 or x.shape[0] != rows or x.shape[1] != cols or not x.is_contiguous():
+        _refuse(where, f"{what} has to be contiguous, of one-byte elements, [{rows}, {cols}]")
+
+
+def rwkvq_fp8_scale_pitch(cols: int) -> int:
+    """Bytes of a row of scales for `cols` columns."""
+    return int(lib().rwkvq_fp8_scale_pitch(cols))
+
+
+def rwkvq_fp8_quantize(x, codes, scale, block_rows: int, stream=None):
+    """rwkvq_fp8_quantize: x float32 / float16 / bfloat16 [rows, cols] (rows may be strided), codes float8_e4m3fn or uint8 [rows, cols],
+    scale uint8 [ceil(rows / block_rows), rwkvq_fp8_scale_pitch(cols)]."""
+    where = "rwkvq_fp8_quantize"
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        _refuse(where, "x has to be two-dimensional with columns side by side")
+    rows, cols = x.shape
+    if block_rows not in (1, 128):
+        _refuse(where, "block_rows is 1 or 128")
+    _check_device(where, x, codes, scale)
+    _bytes_of(where, codes, rows, cols, "codes")
+    _bytes_of(where, scale, (rows + block_rows - 1) // block_rows, rwkvq_fp8_scale_pitch(cols), "scale")
+    _check(lib().rwkvq_fp8_quantize(x.data_ptr(), _dtype_of(x), rows, cols, x.stride(0) if rows > 1 else cols, block_rows, codes.data_ptr(),
+                                    scale.data_ptr(), _stream_ptr(stream)), where)
+
+
+def rwkvq_gemm_fp8(w_codes, w_scale, x_codes, x_scale, Y, stream=None):
+    """rwkvq_gemm_fp8: codes and scales of rwkvq_fp8_quantize, w [oc, ic] with block_rows 128, x [M, ic] with block_rows 1; Y float32,
+    float16 or bfloat16 [M, oc], whose rows may be strided."""
+    where = "rwkvq_gemm_fp8"
+    if w_codes.dim() != 2 or x_codes.dim() != 2 or Y.dim() != 2:
+        _refuse(where, "codes and Y have to be two-dimensional")
+    (oc, ic), M = w_codes.shape, x_codes.shape[0]
+    _check_device(where, w_codes, w_scale, x_codes, x_scale, Y)
+    pitch = rwkvq_fp8_scale_pitch(ic)
+    _bytes_of(where, w_codes, oc, ic, "w_codes")
+    _bytes_of(where, x_codes, M, ic, "x_codes")
+    _bytes_of(where, w_scale, (oc + 127) // 128, pitch, "w_scale")
+    _bytes_of(where, x_scale, M, pitch, "x_scale")
+    if tuple(Y.shape) != (M, oc) or (oc > 1 and Y.stride(1) != 1):
+        _refuse(where, f"Y has to be [{M}, {oc}] with columns side by side")
+    _check(lib().rwkvq_gemm_fp8(w_codes.data_ptr(), w_scale.data_ptr(), oc, ic, x_codes.data_ptr(), x_scale.data_ptr(), M, Y.data_ptr(), _dtype_of(Y),
+                                Y.stride(0) if M > 1 else oc, _stream_ptr(stream)), where)

@@ -1,0 +1,431 @@
+// Eight-bit floating point (e4m3) with one power-of-two scale per block of 128 columns: the quantizer and the product.
+//
+// Scale of a group (128 columns of one row for activations, of 128 rows for weights): the smallest 2^e with max|x| <= 448 * 2^e (448 = 1.75 * 2^8 is
+// the largest e4m3 number).  A power of two, so that scaling rounds nothing: a code is x * 2^-e rounded once, and a product of two
+// scales is exact.  It is stored as the eight-bit exponent e + 127, the form that the block-scaled tensor-core instruction applies itself, which
+// leaves no scaling to the CUDA cores.  (Scales of 32 bits would use up to twice the range of the format, which buys a floating-point
+// code nothing but its few subnormals, and cost a pass of every partial sum of 128 columns through registers.)
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "../../include/rwkvq.h"
+#include "host_util.h"
+#include "tc5.cuh"
+
+namespace rwkvq {
+
+int* device_status_ptr();  // api_misc.cu
+
+namespace f8 {
+
+using namespace tc5;
+
+// ---- quantizer --------------------------------------------------------------------------------------------
+__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
+  const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+__device__ __forceinline__ float2 unpack2(uint32_t v, __half) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+__device__ __forceinline__ float2 unpack2(uint32_t v, __nv_bfloat16) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v)); }
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
+  const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const float2 v = unpack2(w[i], T()); f[2 * i] = v.x; f[2 * i + 1] = v.y; }
+}
+constexpr uint32_t kInfBits = 0x7F800000u;
+// Bits of the largest finite magnitude (as unsigned integers they sort like the numbers).
+__device__ __forceinline__ uint32_t amax8(const float (&f)[8]) {
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { const uint32_t b = __float_as_uint(f[i]) & 0x7FFFFFFFu; a = max(a, b < kInfBits ? b : 0u); }
+  return a;
+}
+// The scale's exponent + 127 from those bits: x = m * 2^(E - 127) with m <= 1.75 fits 448 * 2^(E - 127 - 8), a larger m needs one more.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
+  if (amax == 0u) return 127u;
+  const int e = (int)(amax >> 23) - 8 + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return (uint32_t)max(e, 1);
+}
+__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }     // 1 <= byte <= 247
+// Infinities become NaN codes (the conversion alone would saturate them).
+__device__ __forceinline__ uint2 encode8(const float (&f)[8], float inv) {
+  uint32_t h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float v[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float x = f[2 * i + j];
+      v[j] = (__float_as_uint(x) & 0x7FFFFFFFu) < kInfBits ? x * inv : __uint_as_float(0x7FFFFFFFu);
+    }
+    uint16_t c;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(v[1]), "f"(v[0]));
+    h[i] = c;
+  }
+  return make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+}
+
+// Rows: a warp takes 256 columns per 16-byte load (16 lanes a group), four loads under way, and writes the eight scales together.
+constexpr int kRowWarps = 8, kRowChunks = 4, kRowCols = kRowChunks * 256;
+template <typename T>
+__global__ void __launch_bounds__(kRowWarps * 32) fp8_rows_kernel(const T* __restrict__ x, long long x_row, int rows, int cols, int pieces,
+                                                                 uint8_t* __restrict__ codes, uint8_t* __restrict__ scale, int pitch) {
+  const long long unit = (long long)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  const long long row = unit / pieces;
+  if (row >= rows) return;
+  const int c0 = (int)(unit % pieces) * kRowCols + lane * 8;
+  float f[kRowChunks][8];
+#pragma unroll
+  for (int j = 0; j < kRowChunks; ++j) {
+    if (c0 + j * 256 < cols) load8(x + row * x_row + c0 + j * 256, f[j]);
+    else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[j][i] = 0.f;
+    }
+  }
+  uint32_t lo = 0, hi = 0;
+#pragma unroll
+  for (int j = 0; j < kRowChunks; ++j) {
+    uint32_t a = amax8(f[j]);
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, d));
+    const uint32_t b = scale_byte(a);
+    const uint32_t two = b | __shfl_down_sync(0xFFFFFFFFu, b, 16) << 8;
+    if (j < 2) lo |= two << (16 * j);
+    else hi |= two << (16 * (j - 2));
+    if (c0 + j * 256 < cols) *reinterpret_cast<uint2*>(codes + row * cols + c0 + j * 256) = encode8(f[j], inverse_scale(b));
+  }
+  // the pitch is a multiple of 16, and a piece of columns begins inside it
+  if (lane == 0) *reinterpret_cast<uint2*>(scale + row * pitch + (c0 >> 7)) = make_uint2(lo, hi);
+}
+
+// Blocks of 128 x 128: one thread block each, its elements in registers between the maximum and the codes.
+constexpr int kBlockThreads = 256;
+template <typename T>
+__global__ void __launch_bounds__(kBlockThreads) fp8_blocks_kernel(const T* __restrict__ x, long long x_row, int rows, int cols, int groups,
+                                                                  uint8_t* __restrict__ codes, uint8_t* __restrict__ scale, int pitch) {
+  __shared__ uint32_t most[kBlockThreads / 32];
+  const int g = (int)(blockIdx.x % (unsigned)groups), rb = (int)(blockIdx.x / (unsigned)groups);
+  const int c = g * 128 + (threadIdx.x & 15) * 8;
+  const long long r0 = (long long)rb * 128 + (threadIdx.x >> 4);
+  constexpr int kSteps = 128 / (kBlockThreads / 16);
+  float f[kSteps][8];
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const long long r = r0 + i * (kBlockThreads / 16);
+    if (r < rows && c < cols) load8(x + r * x_row + c, f[i]);
+    else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[i][k] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) a = max(a, amax8(f[i]));
+  a = __reduce_max_sync(0xFFFFFFFFu, a);
+  if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = a;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kBlockThreads / 32; ++i) a = max(a, most[i]);
+  const uint32_t b = scale_byte(a);
+  const float inv = inverse_scale(b);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const long long r = r0 + i * (kBlockThreads / 16);
+    if (r < rows && c < cols) *reinterpret_cast<uint2*>(codes + r * cols + c) = encode8(f[i], inv);
+  }
+  if (threadIdx.x == 0) scale[(size_t)rb * pitch + g] = (uint8_t)b;
+}
+
+int blocks_of(int n) { return n / 128 + (n % 128 != 0); }
+size_t scale_pitch(int cols) { return round_up_sz((size_t)blocks_of(cols), 16); }
+
+template <typename T>
+cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int block_rows, void* codes, void* scale, int pitch, cudaStream_t s) {
+  if (block_rows == 1) {
+    const int pieces = cols / kRowCols + (cols % kRowCols != 0);
+    const long long blocks = ((long long)rows * pieces + kRowWarps - 1) / kRowWarps;
+    fp8_rows_kernel<T><<<(unsigned)blocks, kRowWarps * 32, 0, s>>>(static_cast<const T*>(x), x_row, rows, cols, pieces, static_cast<uint8_t*>(codes),
+                                                                  static_cast<uint8_t*>(scale), pitch);
+  } else {
+    const int groups = blocks_of(cols);
+    const long long blocks = (long long)blocks_of(rows) * groups;
+    fp8_blocks_kernel<T><<<(unsigned)blocks, kBlockThreads, 0, s>>>(static_cast<const T*>(x), x_row, rows, cols, groups, static_cast<uint8_t*>(codes),
+                                                                   static_cast<uint8_t*>(scale), pitch);
+  }
+  return cudaGetLastError();
+}
+
+// ---- product ----------------------------------------------------------------------------------------------
+// Y[t][i] = sum_g 2^(ex[t][g] + ew[i / 128][g]) sum_{k in group g} x[t][k] w[i][k].  Weights are the 128-row operand (a tile's rows are
+// one block of scales), tokens the other one, NT of them, so that a lane of an accumulator is an output channel and a warp writes 32
+// consecutive outputs of one token.  Roles of the eight warps of a CTA: (0) tensor-map copies of 128-column stages, (1) tensor-core
+// instructions, (2) scales, (3) tensor memory, (4-7) epilogue.  Two accumulators, so that a tile's epilogue runs under the next tile's sums.
+// Scales: four groups' bytes of a row are the word that the instruction picks its byte from; warp 2 deals the words of 512 columns out in the order
+// of the copy to tensor memory (32 lanes x 16 bytes, row r in line r % 32, word r / 32), where they lie once per 32-lane quarter.
+constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 8, kSfSlots = 2, kThreads = 256;
+constexpr uint32_t kWBytes = kRows * kStageCols, kSfBytes = 512 + 1024, kSfCols = 16, kCtrlBytes = 512;
+constexpr uint32_t kMaxSmemBytes = 232448;
+
+struct GemmArgs {
+  CUtensorMap wmap, xmap;
+  const uint8_t* w_scale;
+  const uint8_t* x_scale;
+  void* Y;
+  long long y_row;
+  int oc, M, groups, pitch, NT, MT, tiles, stages, y_dtype;
+  uint32_t tmem_cols;
+  int* status;
+};
+
+struct Ctrl {
+  uint64_t full[kMaxStages], empty[kMaxStages];
+  uint64_t sffull[kSfSlots], sfempty[kSfSlots];
+  uint64_t accfull[2], accempty[2];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+static_assert(sizeof(Ctrl) <= kCtrlBytes, "control block");
+
+// Shared-memory descriptor of 32 lines of 16 bytes without a swizzle: eight lines are 128 bytes.
+__device__ __forceinline__ uint64_t smem_desc_lines(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(128u >> 4) << 32 | (uint64_t)1 << 46;
+}
+// e4m3 x e4m3 -> fp32 with eight-bit exponents as scales, one per 32 columns, both operands K-major; `id`: the byte of the scale words.
+__device__ __forceinline__ uint32_t idesc_mx(int M, int N, uint32_t id) {
+  return id << 4 | (uint32_t)(N >> 3) << 17 | 1u << 23 | (uint32_t)(M >> 7) << 27 | id << 29;
+}
+// 32 lines of scales to four columns of tensor memory, once per quarter of the lanes.
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n @q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n}" ::"r"(tmem), "l"(desc) : "memory");
+}
+// One stage: four instructions of 32 columns and the commit that frees it.
+__device__ __forceinline__ void mma_stage(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate,
+                                          uint32_t bar) {
+  asm volatile(
+      "{\n .reg .pred q, p, one;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      " elect.sync _|q, 0xffffffff;\n setp.ne.b32 p, %6, 0;\n setp.eq.b32 one, 0, 0;\n"
+      " add.u64 a1, %1, 2;\n add.u64 a2, %1, 4;\n add.u64 a3, %1, 6;\n add.u64 b1, %2, 2;\n add.u64 b2, %2, 4;\n add.u64 b3, %2, 6;\n"
+      " @q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n"
+      " @q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a1, b1, %3, [%4], [%5], one;\n"
+      " @q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a2, b2, %3, [%4], [%5], one;\n"
+      " @q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a3, b3, %3, [%4], [%5], one;\n"
+      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%7];\n}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(bar) : "memory");
+}
+
+template <typename T> __device__ __forceinline__ T to_out(float f);
+template <> __device__ __forceinline__ float to_out<float>(float f) { return f; }
+template <> __device__ __forceinline__ __half to_out<__half>(float f) { return __float2half_rn(f); }
+template <> __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float f) { return __float2bfloat16_rn(f); }
+
+template <typename T>
+__device__ __forceinline__ void store_tile(const GemmArgs& a, uint32_t tmem, int row, int t0, int nt) {
+  T* y = static_cast<T*>(a.Y) + (long long)t0 * a.y_row + row;
+  for (int c = 0; c < nt; c += 32) {
+    uint32_t r[32];
+    tmem_ld32_issue(tmem + (uint32_t)c, r);
+    tmem_ld_wait(r);
+    if (row < a.oc) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (c + j < nt) y[(c + j) * a.y_row] = to_out<T>(__uint_as_float(r[j]));
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
+  const uint32_t stage_bytes = kWBytes + (uint32_t)a.NT * kStageCols;
+  uint8_t* sf = smem + (uint32_t)a.stages * stage_bytes;
+  Ctrl* ctrl = reinterpret_cast<Ctrl*>(sf + kSfSlots * kSfBytes);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abortp = &ctrl->abort_flag;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kMaxStages; ++i) { mbar_init(&ctrl->full[i], 1); mbar_init(&ctrl->empty[i], 1); }
+    for (int i = 0; i < kSfSlots; ++i) { mbar_init(&ctrl->sffull[i], 32); mbar_init(&ctrl->sfempty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&ctrl->accfull[i], 1); mbar_init(&ctrl->accempty[i], 128); }
+    ctrl->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 3) tmem_alloc(&ctrl->tmem_base, a.tmem_cols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctrl->tmem_base;
+  const int n_k = a.groups;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int st = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+        const int mt = t % a.MT, rb = t / a.MT;
+        for (int k = 0; k < n_k; ++k) {
+          if (!mbar_wait(&ctrl->empty[st], ph ^ 1u, abortp, a.status)) { ok = false; break; }
+          uint8_t* w = smem + (uint32_t)st * stage_bytes;
+          mbar_arrive_expect_tx(&ctrl->full[st], stage_bytes);
+          tensor_g2s(w, &a.wmap, k * kStageCols, rb * kRows, &ctrl->full[st]);
+          tensor_g2s(w + kWBytes, &a.xmap, k * kStageCols, mt * a.NT, &ctrl->full[st]);
+          if (++st == a.stages) { st = 0; ph ^= 1u; }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    int st = 0, sl = 0;
+    uint32_t ph = 0, sph = 0, acc = 0, aph = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+      if (!mbar_wait(&ctrl->accempty[acc], aph ^ 1u, abortp, a.status)) break;
+      tc_fence_after();
+      const uint32_t d = tmem + acc * (uint32_t)a.NT;
+      for (int k = 0; k < n_k; ++k) {
+        const uint32_t sfa = tmem + a.tmem_cols - (uint32_t)(kSfSlots - sl) * kSfCols, sfb = sfa + 4;
+        if ((k & 3) == 0) {
+          if (!mbar_wait(&ctrl->sffull[sl], sph, abortp, a.status)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t src = smem_u32(sf + sl * kSfBytes);
+          copy_scales(sfa, smem_desc_lines(src));
+          copy_scales(sfb, smem_desc_lines(src + 512));
+          if (a.NT > 128) copy_scales(sfb + 4, smem_desc_lines(src + 1024));
+        }
+        if (!mbar_wait(&ctrl->full[st], ph, abortp, a.status)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t w = smem_u32(smem + (uint32_t)st * stage_bytes);
+        mma_stage(d, smem_desc_sw128(w), smem_desc_sw128(w + kWBytes), idesc_mx(kRows, a.NT, (uint32_t)(k & 3)), sfa, sfb, k != 0, smem_u32(&ctrl->empty[st]));
+        if (++st == a.stages) { st = 0; ph ^= 1u; }
+        if ((k & 3) == 3 || k + 1 == n_k) {
+          umma_commit(&ctrl->sfempty[sl]);
+          if (++sl == kSfSlots) { sl = 0; sph ^= 1u; }
+        }
+      }
+      if (!ok) break;
+      umma_commit(&ctrl->accfull[acc]);
+      acc ^= 1u;
+      if (acc == 0) aph ^= 1u;
+    }
+  } else if (warp == 2) {
+    int sl = 0;
+    uint32_t sph = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+      const int mt = t % a.MT, rb = t / a.MT;
+      const uint8_t* ws = a.w_scale + (size_t)rb * a.pitch;
+      for (int k = 0; k < n_k; k += 4) {
+        const uint32_t ww = *reinterpret_cast<const uint32_t*>(ws + k);
+        uint32_t xw[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int r = j * 32 + lane, tok = mt * a.NT + r;
+          xw[j] = r < a.NT && tok < a.M ? *reinterpret_cast<const uint32_t*>(a.x_scale + (size_t)tok * a.pitch + k) : 0x7F7F7F7Fu;
+        }
+        if (!mbar_wait(&ctrl->sfempty[sl], sph ^ 1u, abortp, a.status)) { ok = false; break; }
+        uint4* dst = reinterpret_cast<uint4*>(sf + sl * kSfBytes) + lane;
+        dst[0] = make_uint4(ww, ww, ww, ww);
+        dst[32] = make_uint4(xw[0], xw[1], xw[2], xw[3]);
+        dst[64] = make_uint4(xw[4], xw[5], xw[6], xw[7]);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(&ctrl->sffull[sl]);
+        if (++sl == kSfSlots) { sl = 0; sph ^= 1u; }
+      }
+    }
+  } else if (warp >= 4) {
+    uint32_t acc = 0, aph = 0;
+    for (int t = blockIdx.x; t < a.tiles; t += gridDim.x) {
+      const int mt = t % a.MT, rb = t / a.MT, t0 = mt * a.NT;
+      if (!mbar_wait(&ctrl->accfull[acc], aph, abortp, a.status)) break;
+      tc_fence_after();
+      const uint32_t src = tmem + acc * (uint32_t)a.NT + ((uint32_t)(warp - 4) << 21);
+      const int row = rb * kRows + (warp - 4) * 32 + lane, nt = min(a.NT, a.M - t0);
+      if (a.y_dtype == RWKVQ_F32) store_tile<float>(a, src, row, t0, nt);
+      else if (a.y_dtype == RWKVQ_F16) store_tile<__half>(a, src, row, t0, nt);
+      else store_tile<__nv_bfloat16>(a, src, row, t0, nt);
+      tc_fence_before();
+      mbar_arrive(&ctrl->accempty[acc]);
+      acc ^= 1u;
+      if (acc == 0) aph ^= 1u;
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 3) tmem_dealloc(tmem, a.tmem_cols);
+}
+
+// codes[rows][cols] as boxes of 128 columns x box_rows rows in the 128-byte swizzle.
+bool encode_codes(CUtensorMap* map, const void* codes, int rows, int cols, int box_rows) {
+  EncodeTiledFn fn = encode_tiled();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)cols};
+  const cuuint32_t box[2] = {(cuuint32_t)kStageCols, (cuuint32_t)box_rows}, step[2] = {1u, 1u};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int element_size(int dtype) { return dtype == RWKVQ_F32 ? 4 : dtype == RWKVQ_F16 || dtype == RWKVQ_BF16 ? 2 : 0; }
+
+}  // namespace f8
+}  // namespace rwkvq
+
+using namespace rwkvq;
+
+extern "C" {
+
+size_t rwkvq_fp8_scale_pitch(int cols) { return cols > 0 ? f8::scale_pitch(cols) : 0; }
+
+rwkvq_status rwkvq_fp8_quantize(const void* x, int dtype, int rows, int cols, long long x_row, int block_rows, void* codes, void* scale, void* stream) {
+  const int es = f8::element_size(dtype);
+  if (!x || !codes || !scale || es == 0 || rows <= 0 || cols <= 0 || (block_rows != 1 && block_rows != 128)) return RWKVQ_EINVAL;
+  if (cols % 16) return RWKVQ_ESHAPE;
+  if (x_row < cols) return RWKVQ_EINVAL;
+  if (!aligned16(x) || (x_row * es) % 16 || !aligned16(codes) || !aligned16(scale)) return RWKVQ_EALIGN;
+  if ((long long)rows * f8::blocks_of(cols) > (1ll << 30)) return RWKVQ_EUNSUPPORTED;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int pitch = (int)f8::scale_pitch(cols);
+  if (dtype == RWKVQ_F32) return cuda_status(f8::quantize<float>(x, x_row, rows, cols, block_rows, codes, scale, pitch, s));
+  if (dtype == RWKVQ_F16) return cuda_status(f8::quantize<__half>(x, x_row, rows, cols, block_rows, codes, scale, pitch, s));
+  return cuda_status(f8::quantize<__nv_bfloat16>(x, x_row, rows, cols, block_rows, codes, scale, pitch, s));
+}
+
+rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, int ic, const void* x_codes, const void* x_scale, int M, void* Y, int y_dtype,
+                            long long y_row, void* stream) {
+  if (!w_codes || !w_scale || !x_codes || !x_scale || !Y || oc <= 0 || ic <= 0 || M <= 0 || f8::element_size(y_dtype) == 0 || y_row < oc) return RWKVQ_EINVAL;
+  if (ic % 16) return RWKVQ_ESHAPE;
+  if (!aligned16(w_codes) || !aligned16(w_scale) || !aligned16(x_codes) || !aligned16(x_scale) || !aligned16(Y)) return RWKVQ_EALIGN;
+  f8::GemmArgs a;
+  memset(&a, 0, sizeof(a));
+  a.w_scale = static_cast<const uint8_t*>(w_scale); a.x_scale = static_cast<const uint8_t*>(x_scale);
+  a.Y = Y; a.y_row = y_row; a.oc = oc; a.M = M; a.y_dtype = y_dtype;
+  a.groups = f8::blocks_of(ic); a.pitch = (int)f8::scale_pitch(ic);
+  a.MT = (int)(((long long)M + f8::kMaxTokens - 1) / f8::kMaxTokens);
+  a.NT = (int)((((long long)M + a.MT - 1) / a.MT + 15) / 16 * 16);
+  const long long tiles = (long long)f8::blocks_of(oc) * a.MT;
+  if (tiles > (1ll << 30)) return RWKVQ_EUNSUPPORTED;
+  a.tiles = (int)tiles;
+  a.status = device_status_ptr();
+  if (!a.status) return RWKVQ_ECUDA;
+  a.tmem_cols = 32;
+  while (a.tmem_cols < (uint32_t)a.NT * 2u + f8::kSfSlots * f8::kSfCols) a.tmem_cols *= 2;
+  if (!f8::encode_codes(&a.wmap, w_codes, oc, ic, f8::kRows) || !f8::encode_codes(&a.xmap, x_codes, M, ic, a.NT)) return RWKVQ_ECUDA;
+  const uint32_t fixed = 1024 + f8::kSfSlots * f8::kSfBytes + f8::kCtrlBytes, stage = f8::kWBytes + (uint32_t)a.NT * f8::kStageCols;
+  a.stages = (int)std::min<uint32_t>(f8::kMaxStages, (f8::kMaxSmemBytes - fixed) / stage);
+  static SmemOptIn opt_in;
+  const cudaError_t e = opt_in((const void*)f8::fp8_gemm_kernel, (int)f8::kMaxSmemBytes);
+  if (e != cudaSuccess) return cuda_status(e);
+  f8::fp8_gemm_kernel<<<(unsigned)std::min<int>(a.tiles, sm_count()), f8::kThreads, fixed + (uint32_t)a.stages * stage, static_cast<cudaStream_t>(stream)>>>(a);
+  return cuda_status(cudaGetLastError());
+}
+
+}  // extern "C"

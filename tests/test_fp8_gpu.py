@@ -1,0 +1,255 @@
+"""Eight-bit floating point (rwkvq_fp8_quantize, rwkvq_gemm_fp8) against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_03803_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF_ULP = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+def e4m3_table():
+    """Values of the 256 codes: sign, four exponent bits (bias 7), three mantissa bits; 0x7F and 0xFF are NaN."""
+    c = np.arange(256)
+    e, m = (c >> 3) & 15, c & 7
+    v = np.where(e == 0, m * 2.0 ** -9, (8 + m) * 2.0 ** (e - 10.0))
+    v = np.where((c & 127) == 127, np.nan, v)
+    return np.where(c & 128, -v, v)
+
+
+TABLE = e4m3_table()
+
+
+def encode_exact(x):
+    """Nearest code, ties to the even one, of numbers of magnitude at most 448; NaN and infinities to 0x7F."""
+    pos = TABLE[:127]
+    a = np.abs(np.where(np.isfinite(x), x, 0.0))
+    hi = np.clip(np.searchsorted(pos, a), 0, 126)
+    lo = np.maximum(hi - 1, 0)
+    dl, dh = a - pos[lo], pos[hi] - a
+    code = np.where(dl < dh, lo, np.where(dh < dl, hi, np.where(lo % 2 == 0, lo, hi)))
+    code = code | np.where(np.signbit(x), 128, 0)
+    return np.where(np.isfinite(x), code, 127).astype(np.uint8)
+
+
+def quantize_exact(x, block):
+    """(codes, scale bytes [.., groups]) by the definition: the smallest e >= -126 with max|x| <= 448 * 2^e."""
+    rows, cols = x.shape
+    rb, groups = -(-rows // block), -(-cols // 128)
+    codes, bytes_ = np.zeros((rows, cols), np.uint8), np.zeros((rb, groups), np.uint8)
+    for i in range(rb):
+        for g in range(groups):
+            part = x[i * block:(i + 1) * block, g * 128:(g + 1) * 128]
+            top = np.abs(np.where(np.isfinite(part), part, 0.0)).max()
+            e = 0
+            if top > 0:
+                e = -126
+                while top > 448.0 * 2.0 ** e:
+                    e += 1
+            codes[i * block:(i + 1) * block, g * 128:(g + 1) * 128] = encode_exact(part * 2.0 ** -e)
+            bytes_[i, g] = e + 127
+    return codes, bytes_
+
+
+def run_quantize(x, block):
+    rows, cols = x.shape
+    codes = torch.full((rows, cols), 0xAA, dtype=torch.uint8, device="cuda")
+    scale = torch.full((-(-rows // block), B.rwkvq_fp8_scale_pitch(cols)), 0xAA, dtype=torch.uint8, device="cuda")
+    B.rwkvq_fp8_quantize(x, codes, scale, block)
+    torch.cuda.synchronize()
+    return codes.cpu().numpy(), scale.cpu().numpy()[:, :-(-cols // 128)]
+
+
+def check_quantize(x, block):
+    codes, scale = run_quantize(x, block)
+    ref_codes, ref_scale = quantize_exact(x.double().cpu().numpy(), block)
+    np.testing.assert_array_equal(scale, ref_scale)
+    # NaN codes may carry either sign
+    same = (codes == ref_codes) | (((codes & 127) == 127) & ((ref_codes & 127) == 127))
+    assert same.all(), np.argwhere(~same)[:5]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("shape", [(1, 16), (1, 128), (3, 144), (127, 1040), (129, 272), (130, 2064), (257, 128)])
+def test_quantize_equals_the_definition(dtype, block, shape):
+    g = torch.Generator().manual_seed(shape[0] * 7 + shape[1])
+    x = torch.randn(shape, generator=g) * torch.exp(3.0 * torch.randn((shape[0], 1), generator=g))
+    check_quantize(x.to(TYPES[dtype]).cuda(), block)
+
+
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize_borders(block):
+    # powers of two and 448 * 2^e with their neighbours, zeros, the ends of the range, subnormals
+    one = np.float32(448.0)
+    tops = [0.0, 2.0 ** -149, 2.0 ** -130, 2.0 ** -126, 448.0 * 2.0 ** -126, 1.0, 1.75, float(np.nextafter(np.float32(1.75), np.float32(2))), float(one),
+            float(np.nextafter(one, np.float32(1e9))), float(np.nextafter(one, np.float32(0))), 2.0 ** 127, float(np.finfo(np.float32).max)]
+    for top in tops:
+        x = torch.linspace(-1.0, 1.0, 256).reshape(2, 128).double() * top
+        x[0, 5] = top
+        x[1, 7] = -top
+        check_quantize(x.float().cuda(), block)
+
+
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize_ties_go_to_even(block):
+    # every midpoint of two neighbouring codes, at scale 1 (a 448 in each group)
+    mids = (TABLE[:126] + TABLE[1:127]) / 2
+    x = torch.zeros((2, 128))
+    x[0, :126] = torch.from_numpy(mids).float()
+    x[1, :126] = -x[0, :126]
+    x[:, 126] = 448.0
+    check_quantize(x.cuda(), block)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize_nonfinite(dtype, block):
+    x = torch.randn((130, 272), generator=torch.Generator().manual_seed(3))
+    x[0, 3], x[1, 100], x[2, 130], x[129, 271] = float("nan"), float("inf"), -float("inf"), float("nan")
+    x[5, :128] = float("inf")           # nothing finite in a row's group
+    check_quantize(x.to(TYPES[dtype]).cuda(), block)
+
+
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize_strided_rows(block):
+    wide = torch.randn((70, 640), device="cuda").bfloat16()
+    x = wide[:, 128:128 + 272]
+    assert not x.is_contiguous()
+    check_quantize(x, block)
+
+
+# ---- product ------------------------------------------------------------------------------------------------
+def random_codes(gen, rows, cols):
+    """Random finite codes."""
+    c = gen.integers(0, 256, (rows, cols)).astype(np.uint8)
+    return np.where((c & 127) == 127, 0x3A, c).astype(np.uint8)
+
+
+def random_scales(gen, rows, cols, lo, hi):
+    s = np.full((rows, B.rwkvq_fp8_scale_pitch(cols)), 255, np.uint8)         # bytes behind the last group would show as NaN
+    s[:, :-(-cols // 128)] = gen.integers(lo, hi, (rows, -(-cols // 128)))
+    return s
+
+
+def values(codes, scale, block):
+    rows, cols = codes.shape
+    s = 2.0 ** (scale.astype(np.float64) - 127.0)
+    s = np.repeat(np.repeat(s, block, 0)[:rows], 128, 1)[:, :cols]
+    return TABLE[codes] * s
+
+
+def product_inputs(seed, M, oc, ic, lo=120, hi=134):
+    gen = np.random.default_rng(seed)
+    return (random_codes(gen, oc, ic), random_scales(gen, -(-oc // 128), ic, lo, hi), random_codes(gen, M, ic), random_scales(gen, M, ic, lo, hi))
+
+
+def check_product(y, dtype, wc, ws, xc, xs):
+    w, x = values(wc, ws, 128), values(xc, xs, 1)
+    ref, mag = x @ w.T, np.abs(x) @ np.abs(w).T
+    # a product of two codes is exact in fp32; at most ic / 32 + 32 additions (instructions of 32 columns, and the sum inside one), each off by at
+    # most the last place of a running sum that is never more than the sum of the magnitudes; then the output's rounding
+    tol = (wc.shape[1] / 32 + 32) * 2.0 ** -23 * mag + HALF_ULP[dtype] * np.abs(ref)
+    if dtype == "f16":
+        tol = tol + 2.0 ** -25                       # half a step of its subnormals
+    got = y.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    err = np.abs(got - ref)
+    assert (err <= tol).all(), f"max err/tol {np.max(err / np.maximum(tol, 1e-300))} at {np.argwhere(err > tol)[:4]}"
+
+
+SHAPES = [(1, 64, 16), (1, 128, 128), (1, 4096, 512), (2, 128, 1024), (3, 130, 144), (8, 1, 272), (16, 384, 4096), (17, 256, 640), (33, 129, 2064),
+          (77, 1000, 1152), (130, 640, 1536), (240, 128, 256), (241, 300, 528), (500, 777, 2064), (1000, 1536, 1024)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_product_against_64_bits(shape, dtype):
+    M, oc, ic = shape
+    # fp16 outputs stay in range: 448 * 448 * sqrt(ic) * scales
+    wc, ws, xc, xs = product_inputs(M + oc + ic, M, oc, ic, *((114, 121) if dtype == "f16" else (120, 134)))
+    dev = [torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)]
+    y = torch.full((M, oc), float("nan"), dtype=TYPES[dtype], device="cuda")
+    B.rwkvq_gemm_fp8(*dev, y)
+    torch.cuda.synchronize()
+    assert B.rwkvq_device_status() == 0
+    check_product(y, dtype, wc, ws, xc, xs)
+    again = torch.full_like(y, float("nan"))
+    B.rwkvq_gemm_fp8(*dev, again)
+    assert torch.equal(y, again)
+
+
+def test_product_every_scale_has_its_place():
+    # one non-zero code in each operand at a time would be slow; instead every (row, group) has its own scale and all codes are 1 (0x38): sums of powers of two
+    M, oc, ic = 200, 300, 1664
+    gen = np.random.default_rng(5)
+    wc, xc = np.full((oc, ic), 0x38, np.uint8), np.full((M, ic), 0x38, np.uint8)
+    ws, xs = random_scales(gen, 3, ic, 124, 131), random_scales(gen, M, ic, 124, 131)
+    y = torch.empty((M, oc), device="cuda")
+    B.rwkvq_gemm_fp8(*[torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)], y)
+    ref = values(xc, xs, 1) @ values(wc, ws, 128).T
+    assert np.array_equal(y.double().cpu().numpy(), ref)         # exact: small whole multiples of 2^-6
+
+
+def test_product_scales_at_the_ends_of_their_range():
+    wc, ws, xc, xs = product_inputs(9, 5, 130, 256)
+    ws[:, :2], xs[:, :2] = [1, 254], [254, 1]        # 2^-126 * 2^127 in either order
+    y = torch.empty((5, 130), device="cuda")
+    B.rwkvq_gemm_fp8(*[torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)], y)
+    check_product(y, "f32", wc, ws, xc, xs)
+
+
+@pytest.mark.parametrize("M", [2, 40])
+def test_product_strided_output_leaves_the_rest(M):
+    wc, ws, xc, xs = product_inputs(11, M, 200, 384)
+    wide = torch.full((M + 2, 3, 200), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.rwkvq_gemm_fp8(*[torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)], wide[:M, 1])
+    check_product(wide[:M, 1], "bf16", wc, ws, xc, xs)
+    assert (wide[:, 0] == 7).all() and (wide[:, 2] == 7).all() and (wide[M:] == 7).all()
+
+
+def test_product_nan_stays_in_its_row():
+    wc, ws, xc, xs = product_inputs(12, 20, 256, 512)
+    xc[3, 100] = 0x7F
+    y = torch.empty((20, 256), device="cuda")
+    B.rwkvq_gemm_fp8(*[torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)], y)
+    nan = torch.isnan(y).cpu().numpy()
+    assert nan[3].all() and not np.delete(nan, 3, 0).any()
+
+
+def test_quantize_then_product():
+    # codes and scales as one entry point leaves them and the other reads them
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((50, 1040), generator=g, device="cuda").bfloat16()
+    w = (torch.randn((260, 1040), generator=g, device="cuda") * 0.02).half()
+    pitch = B.rwkvq_fp8_scale_pitch(1040)
+    xc, wc = torch.empty((50, 1040), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty((260, 1040), dtype=torch.float8_e4m3fn, device="cuda")
+    xs, ws = torch.empty((50, pitch), dtype=torch.uint8, device="cuda"), torch.empty((3, pitch), dtype=torch.uint8, device="cuda")
+    y = torch.empty((50, 260), device="cuda")
+    B.rwkvq_fp8_quantize(x, xc, xs, 1)
+    B.rwkvq_fp8_quantize(w, wc, ws, 128)
+    B.rwkvq_gemm_fp8(wc, ws, xc, xs, y)
+    check_product(y, "f32", *[t.view(torch.uint8).cpu().numpy() for t in (wc, ws, xc, xs)])
+
+
+def test_product_captured_and_on_another_stream():
+    wc, ws, xc, xs = product_inputs(13, 30, 512, 1024)
+    dev = [torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)]
+    y = torch.zeros((30, 512), device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    B.rwkvq_gemm_fp8(*dev, y, stream=s)
+    s.synchronize()
+    first = y.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.rwkvq_gemm_fp8(*dev, y)
+    for _ in range(3):
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, first)
+    check_product(y, "f32", wc, ws, xc, xs)
