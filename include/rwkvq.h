@@ -437,6 +437,43 @@ rwkvq_status rwkvq_gemm_fp8(const void* w_codes_dev, const void* w_scale_dev, in
                             const void* x_scale_dev, int M, void* Y_dev, int y_dtype, long long y_row, void* stream);
 
 /*
+ * Linear attention with decaying state, what an RWKV-6-shaped block has between its R, K, V and O projections: for each sequence and head, with
+ * S [n keys][n values], token after token
+ *     out_t[j] = sum_i r_t[i] * (S[i][j] + u[i] * k_t[i] * v_t[j]);    S[i][j] = exp(logw_t[i]) * S[i][j] + k_t[i] * v_t[j].
+ * (The step's RWKVQ_IN_WKV is the per-channel recurrence of Eq. 23.)  Prompts, ragged batches and single tokens through one call; sums, decays and
+ * states in fp32.
+ *  r, k, v, out: [tokens][heads][n] of `dtype` (F32, F16, BF16), n 64 or 128; *_row elements from row to row, so that they may lie side by side.
+ *  logw: logarithms of the decays, <= 0, -inf = forget, of decay_dtype (F32 or `dtype`): [tokens][heads][n], or [tokens][heads] with decay_per_head;
+ *      logw_row = 0: the same for all tokens.  u: [heads][n] fp32, NULL = ones.
+ *  seq_start: [n_seq + 1] rows where the sequences begin, rising, device memory (NULL: n_seq is 1 and has all rows).  A sequence may be empty; rows in front
+ *      of the first and behind the last are not touched.
+ *  state, state_out: [n_slots][heads][n][n] fp32 (keys, values), the same buffer (updated in place) or two that do not overlap.  slots: [n_seq]
+ *      which of them belongs to each sequence (NULL: sequence i has state i), device memory; -1: begins with zeros, is not kept.  state NULL: all begin with
+ *      zeros; state_out NULL: none is kept.  States of no sequence are not touched.
+ * Rows of seq_start out of order, a slot that does not exist, or that an earlier sequence of the call has: that sequence is left out (outputs and
+ * state as they were) and rwkvq_device_status reports EINVAL.
+ * workspace_dev: rwkvq_linattn_workspace_bytes() bytes, 16-byte aligned, contents irrelevant, not shared by calls in flight at the same time.
+ * Pointers (and rows of r, k, v, out, and of logw without decay_per_head) 16-byte aligned; out overlaps no input.  Asynchronous on `stream`.
+ * Errors: EINVAL, EALIGN, EUNSUPPORTED (another n, more than 65535 sequences), ENOMEM (workspace too small), ECUDA.
+ */
+typedef struct {
+  const void* r;
+  const void* k;
+  const void* v;
+  const void* logw;
+  const float* u;
+  void* out;
+  const float* state;
+  float* state_out;
+  const int32_t* seq_start;
+  const int32_t* slots;
+  int64_t r_row, k_row, v_row, logw_row, out_row;
+  int32_t tokens, n_seq, heads, n, n_slots, dtype, decay_dtype, decay_per_head;
+} rwkvq_linattn_args;
+size_t rwkvq_linattn_workspace_bytes(int tokens, int n_seq, int heads, int n);
+rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
  * Decode the packed matrix to out_dev[oc][ic]: F32 = the exact value s*(q-z) (two IEEE fp32
  * operations: subtract, then multiply) or the fp16 codebook entry; BF16 = that value rounded to
  * nearest even.  Uses the same device unpack routines as the products (test surface for
@@ -526,8 +563,8 @@ rwkvq_status rwkvq_quant_error(const void* w_fp16_dev, const rwkvq_desc* W_desc,
                                double* sse_host, void* workspace_dev, size_t workspace_bytes,
                                void* stream);
 
-/* Device status word of the last launches on this device: RWKVQ_OK, or ETIMEOUT if a bounded
- * wait inside a kernel gave up.  Synchronizes `stream`; clears the word. */
+/* Device status word of the last launches on this device: RWKVQ_OK, ETIMEOUT if a bounded
+ * wait inside a kernel gave up, or EINVAL (rwkvq_linattn's lists).  Synchronizes `stream`; clears the word. */
 rwkvq_status rwkvq_device_status(void* stream);
 const char* rwkvq_status_str(rwkvq_status s);
 /* Text of the last CUDA error seen by this thread's library calls ("" if none). */

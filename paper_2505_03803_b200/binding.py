@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -87,7 +88,7 @@ EXPORTS = [
     "rwkvq_proxy_segments_workspace_bytes", "rwkvq_proxy_segments", "rwkvq_tau_for_fraction", "rwkvq_tau_largest_gap", "rwkvq_quant_error_workspace_bytes", "rwkvq_quant_error",
     "rwkvq_desc_for", "rwkvq_quantize_workspace_bytes", "rwkvq_quantize_dev", "rwkvq_calib_representative",
     "rwkvq_quantize_dev_async", "rwkvq_quantize_dev_lost", "rwkvq_quantize_check",
-    "rwkvq_fp8_scale_pitch", "rwkvq_fp8_quantize", "rwkvq_gemm_fp8",
+    "rwkvq_fp8_scale_pitch", "rwkvq_fp8_quantize", "rwkvq_gemm_fp8", "rwkvq_linattn_workspace_bytes", "rwkvq_linattn",
 ]
 
 _lib = None
@@ -177,6 +178,10 @@ def lib() -> C.CDLL:
         L.rwkvq_fp8_scale_pitch.restype = sz
         L.rwkvq_fp8_quantize.argtypes = [vp, i32, i32, i32, i64, i32, vp, vp, vp]
         L.rwkvq_gemm_fp8.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, i64, vp]
+    if hasattr(L, "rwkvq_linattn"):
+        L.rwkvq_linattn_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.rwkvq_linattn_workspace_bytes.restype = sz
+        L.rwkvq_linattn.argtypes = [C.c_char_p, vp, sz, vp]
     _lib = L
     return L
 
@@ -732,3 +737,54 @@ def rwkvq_gemm_fp8(w_codes, w_scale, x_codes, x_scale, Y, stream=None):
         _refuse(where, f"Y has to be [{M}, {oc}] with columns side by side")
     _check(lib().rwkvq_gemm_fp8(w_codes.data_ptr(), w_scale.data_ptr(), oc, ic, x_codes.data_ptr(), x_scale.data_ptr(), M, Y.data_ptr(), _dtype_of(Y),
                                 Y.stride(0) if M > 1 else oc, _stream_ptr(stream)), where)
+
+
+_LINATTN_ARGS = struct.Struct("@10P5q8i")          # rwkvq_linattn_args; packed at a third of what filling a ctypes structure costs
+
+
+def rwkvq_linattn_workspace_bytes(tokens: int, n_seq: int, heads: int, n: int) -> int:
+    return int(lib().rwkvq_linattn_workspace_bytes(tokens, n_seq, heads, n))
+
+
+def rwkvq_linattn(r, k, v, logw, u, out, state, state_out=None, seq_start=None, slots=None, workspace=None, stream=None):
+    """rwkvq_linattn: r, k, v, out [tokens, heads, n] of one type (float32, float16, bfloat16; rows may be strided), logw [tokens, heads, n] or
+    [tokens, heads] of that type or float32 (expanded along tokens: the same decays for all), u float32 [heads, n] or None, state float32
+    [slots, heads, n, n] (None: zeros), updated in place unless state_out is another buffer, seq_start int32 [n_seq + 1], slots int32 [n_seq],
+    workspace uint8."""
+    where = "rwkvq_linattn"
+    t = _torch or _load_torch()
+    if r.dim() != 3:
+        _refuse(where, "r has to be [tokens, heads, n]")
+    tokens, heads, n = r.shape
+    dt = _dtype_of(r)
+    if state_out is None:
+        state_out = state
+    _check_device(where, r, k, v, logw, u, out, state, state_out, seq_start, slots, workspace)
+    for name, x in (("r", r), ("k", k), ("v", v), ("out", out)):
+        if x.shape != r.shape or x.dtype is not r.dtype or (tokens > 0 and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != n))):
+            _refuse(where, f"{name} has to be [{tokens}, {heads}, {n}] of {r.dtype} with heads side by side")
+    per_head = logw.dim() == 2
+    if logw.shape != (r.shape[:2] if per_head else r.shape) or (logw.dtype is not r.dtype and logw.dtype is not t.float32):
+        _refuse(where, "logw has to be [tokens, heads, n] or [tokens, heads] of r's type or float32")
+    if tokens > 0 and ((heads > 1 and logw.stride(1) != (1 if per_head else n)) or (not per_head and logw.stride(2) != 1)):
+        _refuse(where, "logw has to have its heads side by side")
+    n_seq, n_slots = 1, 0
+    if seq_start is not None:
+        n_seq = seq_start.numel() - 1
+        if seq_start.dtype is not t.int32 or not seq_start.is_contiguous():
+            _refuse(where, "seq_start has to be int32, contiguous")
+    if slots is not None and (slots.dtype is not t.int32 or slots.numel() != n_seq or not slots.is_contiguous()):
+        _refuse(where, f"slots has to be int32 [{n_seq}], contiguous")
+    for x in (state, state_out):
+        if x is None:
+            continue
+        if x.dtype is not t.float32 or x.dim() != 4 or tuple(x.shape[1:]) != (heads, n, n) or not x.is_contiguous() or (n_slots and x.shape[0] != n_slots):
+            _refuse(where, f"states have to be float32 [slots, {heads}, {n}, {n}], contiguous, as many before as after")
+        n_slots = x.shape[0]
+    if u is not None and (u.dtype is not t.float32 or tuple(u.shape) != (heads, n) or not u.is_contiguous()):
+        _refuse(where, f"u has to be float32 [{heads}, {n}], contiguous")
+    rows = (r.stride(0), k.stride(0), v.stride(0), logw.stride(0), out.stride(0)) if tokens > 1 else (0, 0, 0, 0, 0)
+    args = _LINATTN_ARGS.pack(*(0 if x is None else x.data_ptr() for x in (r, k, v, logw, u, out, state, state_out, seq_start, slots)), *rows,
+                              tokens, n_seq, heads, n, n_slots, dt, _dtype_of(logw), 1 if per_head else 0)
+    _check(lib().rwkvq_linattn(args, None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
+                               _stream_ptr(stream)), where)
