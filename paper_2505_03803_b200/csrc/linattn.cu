@@ -19,9 +19,16 @@ int* device_status_ptr();  // api_misc.cu
 
 namespace la {
 
+// A sequence as the lists' checks leave it: rows [start, end), its state's slot (-1: none), or rows [0, 0) where it is left out.
+struct Entry { int start, end, slot, unused; };
+
 struct Args {
   rwkvq_linattn_args a;
   int* status;
+  int limit;                // the token kernel takes sequences of at most so many rows, the chunk kernels the others
+  int block_rows, blocks;   // rows of a block of the chunk kernels
+  Entry* entries;           // [n_seq], written by the token kernel; nullptr: one sequence, all rows, slot 0
+  float* block_states;      // [blocks][heads]: the state a block's last piece adds up, the one its sequence began with, the piece's decays
 };
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
@@ -65,10 +72,12 @@ __global__ void __launch_bounds__(kTokenThreads) linattn_token_kernel(const __gr
     bad = bad || slot < -1 || slot >= a.n_slots;
     for (int j = tid; j < seq; j += kTokenThreads) bad = bad || (slot >= 0 && a.slots[j] == slot);      // a state belongs to one sequence of a call
   }
-  if (__syncthreads_or(bad)) {
-    if (tid == 0) atomicExch(p.status, (int)RWKVQ_EINVAL);
-    return;
+  bad = __syncthreads_or(bad);
+  if (tid == 0 && h == 0 && v0 == 0) {
+    if (bad) atomicExch(p.status, (int)RWKVQ_EINVAL);
+    if (p.entries) p.entries[seq] = bad ? Entry{0, 0, -1, 0} : Entry{start, end, slot, 0};
   }
+  if (bad || end - start > p.limit) return;
   const size_t at = (((size_t)max(slot, 0) * a.heads + h) * N + kg * R) * N + v0 + col;
   float4 S[R];
 #pragma unroll
@@ -112,12 +121,509 @@ __global__ void __launch_bounds__(kTokenThreads) linattn_token_kernel(const __gr
   }
 }
 
-template <typename T>
-cudaError_t launch(const Args& p, cudaStream_t s) {
-  const dim3 grid((unsigned)p.a.heads, (unsigned)p.a.n_seq, (unsigned)(p.a.n / kCols));
-  if (p.a.n == 64) linattn_token_kernel<T, 64><<<grid, kTokenThreads, 0, s>>>(p);
-  else linattn_token_kernel<T, 128><<<grid, kTokenThreads, 0, s>>>(p);
+// ---- chunks -------------------------------------------------------------------------------------------------
+// Sixteen tokens at a time.  With P_t, Q_s the products of the decays from the chunk's beginning to t and from behind s to its end, D all of them:
+//   out_t = (r_t P_t) S + sum_{s <= t} A[t][s] v_s,   S <- D S + sum_s (k_s Q_s) v_s^T,
+//   A[t][s] = sum_i r_t k_s prod_{s < x < t} w_x  (s < t),  sum_i r_t u k_t  (s = t).
+// Nothing is divided by a decay: products of decays may underflow to the zero that they mean.  The 8 x 8 block of A below the diagonal is a product of
+// (r_t P'_t) and (k_s Q'_s), P' and Q' from and to the chunk's middle; the two triangles are added up in fp32 with a running product along t.
+//
+// The products run on mma.sync.m16n8k16 with operands of several bf16 terms (hi + lo + ...), whose exponents reach as far as fp32's: r P and S with two
+// (2^-17 of each; the output is rounded to 2^-9 or 2^-12), k Q with three (all 24 bits: it goes into the fp32 state), v with as many as it has
+// (bf16 one, fp16 two); fp32 inputs take three of everything.  mma.sync and not tcgen05: S stays in registers from chunk to chunk as the accumulator of
+// S^T, in the layout in which the next product takes it as its operand; through tensor memory it would have to be read, split and written every 16 tokens.
+//
+// A block of N / 16 warps has one head; warp w the value columns 16 w to 16 w + 15, so that warps share r P, k Q and A but no sums.
+// Rows are cut into blocks of block_rows, dealt out over the SMs: first (kStateOnly) the state that each block's last piece adds up from zero (or from its
+// sequence's own), where the sequence goes on behind the block; then all blocks at once, each beginning with what those before it left.
+
+template <typename T> struct Terms;
+template <> struct Terms<__nv_bfloat16> { static constexpr int R = 2, V = 1; };
+template <> struct Terms<__half> { static constexpr int R = 2, V = 2; };
+template <> struct Terms<float> { static constexpr int R = 3, V = 3; };
+constexpr int kChunk = 16, kHalf = 8, K3 = 3;
+
+template <typename T, int N>
+struct Shape {
+  static constexpr int kThreads = 2 * N, kTiles = N / 8, kSteps = N / 16;
+  static constexpr int R = Terms<T>::R, V = Terms<T>::V;
+  static constexpr int kPitch = (N + 8) * 2;                      // bytes of a row of terms: an odd number of 16 bytes, no conflicts for ldmatrix
+  static constexpr int kRawPitch = N * (int)sizeof(T) + 16, kDecayPitch = N * 4 + 16;
+  static constexpr int kTerm = kChunk * kPitch, kHalfTerm = kHalf * kPitch, kRaw = kChunk * kRawPitch;
+  // a raw stage: r, k, v, logarithms of decays
+  static constexpr int kStage = 3 * kRaw + kChunk * kDecayPitch;
+  static constexpr int oRt = 2 * kStage, oKt = oRt + R * kTerm, oRp = oKt + K3 * kTerm, oKp = oRp + R * kHalfTerm, oVt = oKp + R * kHalfTerm;
+  static constexpr int oW = oVt + (V > 1 ? V * kTerm : 0), oD = oW + kChunk * (N + 4) * 4, oA = oD + N * 4, oU = oA + (N / 64) * 2 * 64 * 4;
+  static constexpr int kBytes = oU + N * 4;
+  static constexpr int kStateFloats = N * N, kBlockFloats = 2 * N * N + N;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cp_async16(void* dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// (x, y) as n bf16 terms, x in the low half: each term is what the ones before it leave, rounded.
+template <int n>
+__device__ __forceinline__ void split(float x, float y, uint32_t (&t)[n]) {
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    t[i] = *reinterpret_cast<const uint32_t*>(&h);
+    if (i + 1 < n) { x -= __uint_as_float(t[i] << 16); y -= __uint_as_float(t[i] & 0xFFFF0000u); }
+  }
+}
+template <int n>
+__device__ __forceinline__ void store_split(uint8_t* at, int term_bytes, float x, float y) {
+  uint32_t t[n];
+  split<n>(x, y, t);
+#pragma unroll
+  for (int i = 0; i < n; ++i) *reinterpret_cast<uint32_t*>(at + i * term_bytes) = t[i];
+}
+__device__ __forceinline__ float2 load2(const float* p) { return *reinterpret_cast<const float2*>(p); }
+__device__ __forceinline__ float2 load2(const __half* p) { return __half22float2(*reinterpret_cast<const __half2*>(p)); }
+__device__ __forceinline__ float2 load2(const __nv_bfloat16* p) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p)); }
+
+template <typename T, int N, bool kStateOnly>
+struct Worker {
+  using Sh = Shape<T, N>;
+  const Args& p;
+  uint8_t* sm;
+  int h, warp, lane, tid;
+  float S[Sh::kTiles][4];      // S^T: values 16 warp + lane / 4 (+ 8: the last two), keys 8 j + 2 (lane % 4) and the next
+  float2 total;                // kStateOnly: sums of the logarithms of the decays of this thread's channels
+
+  __device__ __forceinline__ Worker(const Args& p_, uint8_t* sm_) : p(p_), sm(sm_), h(blockIdx.y), warp(threadIdx.x >> 5), lane(threadIdx.x & 31), tid(threadIdx.x) {}
+
+  // Rows t0 .. t0 + 15 into a raw stage; zeros (no decay, nothing to add) behind `end`.
+  __device__ __forceinline__ void fetch(int stage, int t0, int end) {
+    const rwkvq_linattn_args& a = p.a;
+    uint8_t* st = sm + stage * Sh::kStage;
+    constexpr int kPieces = N * (int)sizeof(T) / 16;
+    for (int i = tid; i < kChunk * kPieces; i += Sh::kThreads) {
+      const int t = i / kPieces, c = i % kPieces, row = t0 + t;
+      const bool there = row < end;
+      const long long at = there ? row : t0, off = ((long long)h * N * (int)sizeof(T)) + c * 16;
+      uint8_t* dst = st + t * Sh::kRawPitch + c * 16;
+      if (!kStateOnly) cp_async16(dst, static_cast<const uint8_t*>(a.r) + at * a.r_row * (int)sizeof(T) + off, there);
+      cp_async16(dst + Sh::kRaw, static_cast<const uint8_t*>(a.k) + at * a.k_row * (int)sizeof(T) + off, there);
+      cp_async16(dst + 2 * Sh::kRaw, static_cast<const uint8_t*>(a.v) + at * a.v_row * (int)sizeof(T) + off, there);
+    }
+    uint8_t* lw = st + 3 * Sh::kRaw;
+    if (a.decay_per_head) {
+      if (tid < kChunk) reinterpret_cast<float*>(lw)[tid] = t0 + tid < end ? log_decay<T>(a, t0 + tid, h, 0) : 0.f;
+    } else {
+      const int ws = a.decay_dtype == RWKVQ_F32 ? 4 : (int)sizeof(T), pieces = N * ws / 16;
+      for (int i = tid; i < kChunk * pieces; i += Sh::kThreads) {
+        const int t = i / pieces, c = i % pieces, row = t0 + t;
+        const bool there = row < end;
+        cp_async16(lw + t * Sh::kDecayPitch + c * 16,
+                   static_cast<const uint8_t*>(a.logw) + ((there ? row : t0) * a.logw_row + (long long)h * N) * ws + c * 16, there);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+
+  __device__ __forceinline__ float2 decay2(const uint8_t* lw, int t, int c) const {
+    if (p.a.decay_per_head) { const float v = reinterpret_cast<const float*>(lw)[t]; return make_float2(v, v); }
+    const uint8_t* row = lw + t * Sh::kDecayPitch;
+    return p.a.decay_dtype == RWKVQ_F32 ? load2(reinterpret_cast<const float*>(row) + c) : load2(reinterpret_cast<const T*>(row) + c);
+  }
+
+  // A stage's operands.  Warps of a group of four take: r of the first eight tokens, r of the last, k of the last, k of the first; a lane two channels.
+  __device__ __forceinline__ void operands(int stage) {
+    const uint8_t* st = sm + stage * Sh::kStage;
+    const uint8_t* lw = st + 3 * Sh::kRaw;
+    const int role = warp & 3, c = (warp >> 2) * 64 + lane * 2;
+    auto raw = [&](int which, int t) { return load2(reinterpret_cast<const T*>(st + which * Sh::kRaw + t * Sh::kRawPitch) + c); };
+    auto w_at = [&](int t) { return reinterpret_cast<float2*>(sm + Sh::oW + (t * (N + 4) + c) * 4); };
+    if (role == 0) {
+      if (!kStateOnly) {
+        float2 q = make_float2(1.f, 1.f);
+#pragma unroll
+        for (int t = 0; t < kHalf; ++t) {
+          const float2 l = decay2(lw, t, c), w = make_float2(__expf(l.x), __expf(l.y)), r = raw(0, t);
+          *w_at(t) = w;
+          store_split<Sh::R>(sm + Sh::oRt + t * Sh::kPitch + c * 2, Sh::kTerm, r.x * q.x, r.y * q.y);
+          q.x *= w.x; q.y *= w.y;
+        }
+      }
+    } else if (role == 1) {
+      float2 s = make_float2(0.f, 0.f), q = make_float2(1.f, 1.f);
+#pragma unroll
+      for (int t = 0; t < kHalf; ++t) { const float2 l = decay2(lw, t, c); s.x += l.x; s.y += l.y; }
+      const float2 d1 = make_float2(__expf(s.x), __expf(s.y));
+#pragma unroll
+      for (int t = kHalf; t < kChunk; ++t) {
+        const float2 l = decay2(lw, t, c);
+        s.x += l.x; s.y += l.y;
+        if (!kStateOnly) {
+          const float2 w = make_float2(__expf(l.x), __expf(l.y)), r = raw(0, t);
+          *w_at(t) = w;
+          const float2 m = make_float2(r.x * q.x, r.y * q.y);
+          store_split<Sh::R>(sm + Sh::oRp + (t - kHalf) * Sh::kPitch + c * 2, Sh::kHalfTerm, m.x, m.y);
+          store_split<Sh::R>(sm + Sh::oRt + t * Sh::kPitch + c * 2, Sh::kTerm, m.x * d1.x, m.y * d1.y);
+          q.x *= w.x; q.y *= w.y;
+        }
+      }
+      // the state's decay, over and over the same where decays do not change: the accurate exponential of the sum
+      *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(s.x), expf(s.y));
+      if (kStateOnly) { total.x += s.x; total.y += s.y; }
+    } else if (role == 2) {
+      float2 q = make_float2(1.f, 1.f);
+#pragma unroll
+      for (int t = kChunk - 1; t >= kHalf; --t) {
+        const float2 l = decay2(lw, t, c), k = raw(1, t);
+        store_split<K3>(sm + Sh::oKt + t * Sh::kPitch + c * 2, Sh::kTerm, k.x * q.x, k.y * q.y);
+        q.x *= __expf(l.x); q.y *= __expf(l.y);
+      }
+    } else {
+      float2 s = make_float2(0.f, 0.f), q = make_float2(1.f, 1.f);
+#pragma unroll
+      for (int t = kHalf; t < kChunk; ++t) { const float2 l = decay2(lw, t, c); s.x += l.x; s.y += l.y; }
+      const float2 d2 = make_float2(__expf(s.x), __expf(s.y));
+#pragma unroll
+      for (int t = kHalf - 1; t >= 0; --t) {
+        const float2 l = decay2(lw, t, c), k = raw(1, t), m = make_float2(k.x * q.x, k.y * q.y);
+        if (!kStateOnly) store_split<Sh::R>(sm + Sh::oKp + t * Sh::kPitch + c * 2, Sh::kHalfTerm, m.x, m.y);
+        store_split<K3>(sm + Sh::oKt + t * Sh::kPitch + c * 2, Sh::kTerm, m.x * d2.x, m.y * d2.y);
+        q.x *= __expf(l.x); q.y *= __expf(l.y);
+      }
+    }
+    if (Sh::V > 1 && (role & 1) == 0) {       // the warps with less to do
+      const int t0 = role == 0 ? 0 : kHalf;
+#pragma unroll
+      for (int t = 0; t < kHalf; ++t) {
+        const float2 v = raw(2, t0 + t);
+        store_split<Sh::V>(sm + Sh::oVt + (t0 + t) * Sh::kPitch + c * 2, Sh::kTerm, v.x, v.y);
+      }
+    }
+  }
+
+  // The triangles of A: lanes 0-15 tokens 0-7, the others tokens 8-15, four channels each.  Warp w of a group of four takes columns s = w and 7 - w,
+  // together seven entries below the diagonal (and the two on it), whatever w.
+  __device__ __forceinline__ void triangles(int stage) {
+    const uint8_t* st = sm + stage * Sh::kStage;
+    const int w = warp & 3, t0 = (lane >> 4) * kHalf, c = (warp >> 2) * 64 + (lane & 15) * 4, first = 7 - w;
+    auto four = [&](int which, int t) {
+      const T* at = reinterpret_cast<const T*>(st + which * Sh::kRaw + (t0 + t) * Sh::kRawPitch) + c;
+      const float2 a = load2(at), b = load2(at + 2);
+      return make_float4(a.x, a.y, b.x, b.y);
+    };
+    float4 x = four(1, w);
+    const float4 x2 = four(1, first), u = *reinterpret_cast<const float4*>(sm + Sh::oU + c * 4);
+    float v[8], last;
+    {
+      const float4 r = four(0, w), r2 = four(0, first);
+      v[7] = r.x * u.x * x.x + r.y * u.y * x.y + r.z * u.z * x.z + r.w * u.w * x.w;
+      last = r2.x * u.x * x2.x + r2.y * u.y * x2.y + r2.z * u.z * x2.z + r2.w * u.w * x2.w;
+    }
+#pragma unroll
+    for (int j = 0; j < 7; ++j) {
+      if (j == first) x = x2;
+      const int t = j < first ? w + 1 + j : j + 1;
+      const float4 r = four(0, t), wt = *reinterpret_cast<const float4*>(sm + Sh::oW + ((t0 + t) * (N + 4) + c) * 4);
+      v[j] = r.x * x.x + r.y * x.y + r.z * x.z + r.w * x.w;
+      x.x *= wt.x; x.y *= wt.y; x.z *= wt.z; x.w *= wt.w;
+    }
+    // eight sums over sixteen lanes: each step halves the values a lane carries
+#pragma unroll
+    for (int d = 8, n = 4; d > 1; d >>= 1, n >>= 1) {
+      const bool up = (lane & d) != 0;
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const float keep = up ? v[i + n] : v[i], send = up ? v[i] : v[i + n];
+        v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, d);
+      }
+    }
+    v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], 1);
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) last += __shfl_xor_sync(0xFFFFFFFFu, last, d);
+    float* A = reinterpret_cast<float*>(sm + Sh::oA) + (warp >> 2) * 128 + (lane >> 4) * 64;
+    if ((lane & 1) == 0) {
+      const int j = ((lane >> 3) & 1) * 4 + ((lane >> 2) & 1) * 2 + ((lane >> 1) & 1);
+      const int s = j == 7 ? w : j < first ? w : first, t = j == 7 ? w : j < first ? w + 1 + j : j + 1;
+      A[t * 8 + s] = v[0];
+    }
+    if ((lane & 15) == 1) A[first * 8 + first] = last;
+  }
+
+  // Chunks of rows [t, end), t + 16, ...
+  __device__ __forceinline__ void rows(int begin, int end) {
+    const rwkvq_linattn_args& a = p.a;
+    const int n = (end - begin + kChunk - 1) / kChunk, g = lane >> 2, q = lane & 3;
+    fetch(0, begin, end);
+    if (n > 1) fetch(1, begin + kChunk, end);
+    if (n > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    operands(0);
+    __syncthreads();
+    for (int i = 0; i < n; ++i) {
+      const int t0 = begin + i * kChunk;
+      float o[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, mid[4] = {0.f, 0.f, 0.f, 0.f};
+      if (!kStateOnly) {
+        triangles(i & 1);
+        const uint32_t rt = smem_u32(sm + Sh::oRt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
+        // rows of r P' (lanes 0-15) and of k Q' (16-31), the first eight keys and the next
+        const uint32_t half = smem_u32(sm + (lane < 16 ? Sh::oRp : Sh::oKp)) + (lane & 7) * Sh::kPitch + ((lane >> 3) & 1) * 16;
+#pragma unroll
+        for (int k = 0; k < Sh::kSteps; ++k) {
+          uint32_t x[Sh::R][4], y[Sh::R][4], b[2][2][Sh::R];
+#pragma unroll
+          for (int e = 0; e < Sh::R; ++e) {
+            ldsm4(rt + e * Sh::kTerm + k * 32, x[e]);
+            ldsm4(half + e * Sh::kHalfTerm + k * 32, y[e]);
+          }
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) split<Sh::R>(S[2 * k + m][2 * nb], S[2 * k + m][2 * nb + 1], b[nb][m]);
+#pragma unroll
+          for (int e = 0; e < Sh::R; ++e)
+#pragma unroll
+            for (int f = 0; f < Sh::R - e; ++f) {
+              mma(o[0], x[e], b[0][0][f], b[0][1][f]);
+              mma(o[1], x[e], b[1][0][f], b[1][1][f]);
+              const uint32_t low[4] = {0u, y[e][0], 0u, y[e][1]};
+              mma(mid, low, y[f][2], y[f][3]);
+            }
+        }
+      }
+      // values of the chunk's tokens: an operand of both products that follow
+      uint32_t v[Sh::V][4];
+      {
+        const int row = (lane & 7) + (lane >> 4) * 8, col = warp * 16 + ((lane >> 3) & 1) * 8;
+        const uint32_t at = Sh::V > 1 ? smem_u32(sm + Sh::oVt) + row * Sh::kPitch + col * 2
+                                      : smem_u32(sm + (i & 1) * Sh::kStage + 2 * Sh::kRaw) + row * Sh::kRawPitch + col * 2;
+#pragma unroll
+        for (int e = 0; e < Sh::V; ++e) ldsm4t(at + e * Sh::kTerm, v[e]);
+      }
+#pragma unroll
+      for (int j = 0; j < Sh::kTiles; ++j) {
+        const float2 d = *reinterpret_cast<const float2*>(sm + Sh::oD + (j * 8 + q * 2) * 4);
+        S[j][0] *= d.x; S[j][1] *= d.y; S[j][2] *= d.x; S[j][3] *= d.y;
+      }
+      {
+        const uint32_t kt = smem_u32(sm + Sh::oKt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
+#pragma unroll
+        for (int f = 0; f < K3; ++f)
+#pragma unroll
+          for (int k = 0; k < Sh::kSteps; ++k) {
+            uint32_t b[4];
+            ldsm4t(kt + f * Sh::kTerm + k * 32, b);
+#pragma unroll
+            for (int e = 0; e < Sh::V && e + f < K3; ++e) {
+              mma(S[2 * k], v[e], b[0], b[1]);
+              mma(S[2 * k + 1], v[e], b[2], b[3]);
+            }
+          }
+      }
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncthreads();
+      if (i + 2 < n) fetch(i & 1, t0 + 2 * kChunk, end);
+      if (!kStateOnly) {
+        const float* A = reinterpret_cast<const float*>(sm + Sh::oA) + g * 8 + q * 2;
+        float2 up = *reinterpret_cast<const float2*>(A), dn = *reinterpret_cast<const float2*>(A + 64);
+#pragma unroll
+        for (int x = 1; x < N / 64; ++x) {
+          const float2 up2 = *reinterpret_cast<const float2*>(A + x * 128), dn2 = *reinterpret_cast<const float2*>(A + x * 128 + 64);
+          up.x += up2.x; up.y += up2.y; dn.x += dn2.x; dn.y += dn2.y;
+        }
+        uint32_t a0[Sh::R], a1[Sh::R], a3[Sh::R];
+        split<Sh::R>(up.x, up.y, a0);
+        split<Sh::R>(mid[2], mid[3], a1);
+        split<Sh::R>(dn.x, dn.y, a3);
+#pragma unroll
+        for (int e = 0; e < Sh::R; ++e) {
+          const uint32_t x[4] = {a0[e], a1[e], 0u, a3[e]};
+#pragma unroll
+          for (int f = 0; f < Sh::V && e + f < Sh::R; ++f) {
+            mma(o[0], x, v[f][0], v[f][2]);
+            mma(o[1], x, v[f][1], v[f][3]);
+          }
+        }
+        T* out = static_cast<T*>(a.out) + (long long)h * N + warp * 16 + q * 2;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const int row = t0 + g + 8 * m;
+          if (row < end) {
+#pragma unroll
+            for (int nb = 0; nb < 2; ++nb) {
+              T* at = out + row * a.out_row + nb * 8;
+              if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(at) = make_float2(o[nb][2 * m], o[nb][2 * m + 1]);
+              else {
+                const T pair[2] = {from_f32<T>(o[nb][2 * m]), from_f32<T>(o[nb][2 * m + 1])};
+                *reinterpret_cast<uint32_t*>(at) = *reinterpret_cast<const uint32_t*>(pair);
+              }
+            }
+          }
+        }
+      }
+      if (i + 1 < n) operands((i + 1) & 1);
+      __syncthreads();
+    }
+  }
+
+  // States in the caller's layout [key][value].
+  __device__ __forceinline__ void load_state(int slot) {
+    const float* s = p.a.state && slot >= 0 ? p.a.state + ((size_t)slot * p.a.heads + h) * Sh::kStateFloats + warp * 16 + (lane >> 2) : nullptr;
+#pragma unroll
+    for (int j = 0; j < Sh::kTiles; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[j][e] = s ? __ldg(s + (j * 8 + (lane & 3) * 2 + (e & 1)) * N + (e >> 1) * 8) : 0.f;
+  }
+  __device__ __forceinline__ void store_state(int slot) {
+    float* s = p.a.state_out + ((size_t)slot * p.a.heads + h) * Sh::kStateFloats + warp * 16 + (lane >> 2);
+#pragma unroll
+    for (int j = 0; j < Sh::kTiles; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[(j * 8 + (lane & 3) * 2 + (e & 1)) * N + (e >> 1) * 8] = S[j][e];
+  }
+  // States in the workspace: as the registers hold them.  which: 0 what the block's last piece comes to, 1 what its sequence began with.
+  __device__ __forceinline__ float* block_state(int block, int which) const {
+    return p.block_states + ((size_t)block * p.a.heads + h) * Sh::kBlockFloats + which * Sh::kStateFloats;
+  }
+  __device__ __forceinline__ void keep(float* to) const {
+#pragma unroll
+    for (int j = 0; j < Sh::kTiles; ++j)
+      reinterpret_cast<float4*>(to)[(warp * Sh::kTiles + j) * 32 + lane] = make_float4(S[j][0], S[j][1], S[j][2], S[j][3]);
+  }
+  __device__ __forceinline__ float4 kept(const float* from, int j) const { return reinterpret_cast<const float4*>(from)[(warp * Sh::kTiles + j) * 32 + lane]; }
+};
+
+// The next sequence from `from` on that has rows in [row0, row1) and is longer than the limit; n_seq: none.  Called by the whole block.
+__device__ __forceinline__ int next_sequence(const Args& p, int from, int row0, int row1, int* word) {
+  if (threadIdx.x == 0) *word = p.a.n_seq;
+  __syncthreads();
+  int found = p.a.n_seq;
+  for (int i = from + (int)threadIdx.x; i < p.a.n_seq; i += (int)blockDim.x) {
+    const Entry e = p.entries[i];
+    if (e.end - e.start > p.limit && e.end > row0 && e.start < row1) { found = i; break; }
+  }
+  found = __reduce_min_sync(0xFFFFFFFFu, found);
+  if ((threadIdx.x & 31) == 0) atomicMin(word, found);
+  __syncthreads();
+  found = *word;
+  __syncthreads();
+  return found;
+}
+
+template <typename T, int N, bool kStateOnly>
+__global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? 4 : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
+  using Sh = Shape<T, N>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int word;
+  Worker<T, N, kStateOnly> w(p, smem);
+  const int block = blockIdx.x, row0 = block * p.block_rows, row1 = min(row0 + p.block_rows, p.a.tokens);
+  if (!kStateOnly) {
+    for (int i = threadIdx.x; i < (N / 64) * 128; i += Sh::kThreads) reinterpret_cast<float*>(smem + Sh::oA)[i] = 0.f;       // above the diagonals it stays zero
+    for (int i = threadIdx.x; i < N; i += Sh::kThreads) reinterpret_cast<float*>(smem + Sh::oU)[i] = p.a.u ? p.a.u[w.h * N + i] : 1.f;
+  }
+  for (int seq = 0;; ++seq) {
+    Entry e = {0, p.a.tokens, 0, 0};
+    if (p.entries) {
+      seq = next_sequence(p, seq, row0, row1, &word);
+      if (seq >= p.a.n_seq) return;
+      e = p.entries[seq];
+    } else if (seq > 0) {
+      return;
+    }
+    const int begin = max(e.start, row0), end = min(e.end, row1);
+    if (kStateOnly) {
+      if (e.end <= row1) continue;
+      if (e.start >= row0) {
+        w.load_state(e.slot);
+        w.keep(w.block_state(block, 1));       // for the pass that follows: by then the last of its blocks may have written the new state over it
+      } else {
+#pragma unroll
+        for (int j = 0; j < Sh::kTiles; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w.S[j][i] = 0.f;
+      }
+      w.total = make_float2(0.f, 0.f);
+      w.rows(begin, end);
+      w.keep(w.block_state(block, 0));
+      if ((w.warp & 3) == 1)
+        *reinterpret_cast<float2*>(w.block_state(block, 2) + (w.warp >> 2) * 64 + w.lane * 2) = make_float2(expf(w.total.x), expf(w.total.y));
+      return;
+    }
+    if (e.start < row0 || e.end > row1) {
+      // from the workspace: what the sequence began with, or what the blocks before this one make of it
+      const int b0 = e.start >= row0 ? block : e.start / p.block_rows;
+      const float* from = w.block_state(b0, e.start >= row0 ? 1 : 0);
+#pragma unroll
+      for (int j = 0; j < Sh::kTiles; ++j) { const float4 x = w.kept(from, j); w.S[j][0] = x.x; w.S[j][1] = x.y; w.S[j][2] = x.z; w.S[j][3] = x.w; }
+      for (int b = b0 + 1; b < block; ++b) {
+        const float* add = w.block_state(b, 0);
+        const float* decay = w.block_state(b, 2) + (w.lane & 3) * 2;
+#pragma unroll
+        for (int j = 0; j < Sh::kTiles; ++j) {
+          const float4 x = w.kept(add, j);
+          const float2 d = *reinterpret_cast<const float2*>(decay + j * 8);
+          w.S[j][0] = fmaf(w.S[j][0], d.x, x.x); w.S[j][1] = fmaf(w.S[j][1], d.y, x.y);
+          w.S[j][2] = fmaf(w.S[j][2], d.x, x.z); w.S[j][3] = fmaf(w.S[j][3], d.y, x.w);
+        }
+      }
+    } else {
+      w.load_state(e.slot);
+    }
+    w.rows(begin, end);
+    if (e.end <= row1 && p.a.state_out && e.slot >= 0) w.store_state(e.slot);
+  }
+}
+
+// Rows of a block and how many blocks.  A block's warps work on one head; about four thread blocks fit an SM.
+struct Plan { int block_rows, blocks, limit; size_t entries_bytes, bytes; };
+constexpr int kShortest = 8;
+Plan plan_of(int tokens, int n_seq, int heads, int n) {
+  Plan l = {0, 0, 0x7FFFFFFF, 0, 0};
+  if (tokens <= std::max<long long>(kShortest, 2ll * n_seq)) return l;        // all by the token kernel
+  const long long most = std::max<long long>(1, (long long)sm_count() * (n == 64 ? 4 : 1) / heads);
+  const long long rows = std::max<long long>(64, ((tokens + most - 1) / most + kChunk - 1) / kChunk * kChunk);
+  l.block_rows = (int)std::min<long long>(rows, 1 << 30);
+  l.blocks = (int)((tokens + (long long)l.block_rows - 1) / l.block_rows);
+  l.limit = kShortest;
+  l.entries_bytes = round_up_sz((size_t)n_seq * sizeof(Entry), 256);
+  // as much as any fewer tokens could ask for
+  const long long bound = std::min<long long>(most, (tokens + 63ll) / 64);
+  l.bytes = l.entries_bytes + (bound > 1 ? (size_t)bound * heads * (2 * n * n + n) * 4 : 0);
+  return l;
+}
+
+template <typename T, int N>
+cudaError_t launch_n(Args& p, const Plan& l, cudaStream_t s) {
+  if (l.blocks == 0 || p.entries) {
+    linattn_token_kernel<T, N><<<dim3((unsigned)p.a.heads, (unsigned)p.a.n_seq, N / kCols), kTokenThreads, 0, s>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess || l.blocks == 0) return e;
+  }
+  using Sh = Shape<T, N>;
+  static SmemOptIn opt_state, opt_all;
+  cudaError_t e = opt_all((const void*)linattn_chunk_kernel<T, N, false>, Sh::kBytes);
+  if (e == cudaSuccess && l.blocks > 1) {
+    e = opt_state((const void*)linattn_chunk_kernel<T, N, true>, Sh::kBytes);
+    if (e == cudaSuccess) {
+      linattn_chunk_kernel<T, N, true><<<dim3((unsigned)l.blocks - 1, (unsigned)p.a.heads), Sh::kThreads, Sh::kBytes, s>>>(p);
+      e = cudaGetLastError();
+    }
+  }
+  if (e != cudaSuccess) return e;
+  linattn_chunk_kernel<T, N, false><<<dim3((unsigned)l.blocks, (unsigned)p.a.heads), Sh::kThreads, Sh::kBytes, s>>>(p);
   return cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch(Args& p, const Plan& l, cudaStream_t s) {
+  return p.a.n == 64 ? launch_n<T, 64>(p, l, s) : launch_n<T, 128>(p, l, s);
 }
 
 }  // namespace la
@@ -128,8 +634,8 @@ using namespace rwkvq;
 extern "C" {
 
 size_t rwkvq_linattn_workspace_bytes(int tokens, int n_seq, int heads, int n) {
-  (void)tokens; (void)n_seq; (void)heads; (void)n;
-  return 0;
+  if (tokens < 0 || n_seq <= 0 || heads <= 0 || (n != 64 && n != 128)) return 0;
+  return la::plan_of(tokens, n_seq, heads, n).bytes;
 }
 
 rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace, size_t workspace_bytes, void* stream) {
@@ -141,7 +647,7 @@ rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace, size
   if (es == 0 || (a.decay_dtype != RWKVQ_F32 && a.decay_dtype != a.dtype)) return RWKVQ_EINVAL;
   if (a.tokens < 0 || a.n_seq <= 0 || a.heads <= 0 || a.n <= 0 || a.n_slots < 0) return RWKVQ_EINVAL;
   if (a.n != 64 && a.n != 128) return RWKVQ_EUNSUPPORTED;
-  if (a.n_seq > 65535 || (long long)a.heads * a.n > (1ll << 24)) return RWKVQ_EUNSUPPORTED;
+  if (a.n_seq > 65535 || a.heads > 65535 || a.tokens > (1 << 30)) return RWKVQ_EUNSUPPORTED;
   if (a.tokens > 0 && (!a.r || !a.k || !a.v || !a.logw || !a.out)) return RWKVQ_EINVAL;
   if (a.tokens > 0 && (a.out == a.r || a.out == a.k || a.out == a.v || a.out == a.logw)) return RWKVQ_EINVAL;
   if (!a.seq_start && a.n_seq != 1) return RWKVQ_EINVAL;
@@ -161,13 +667,18 @@ rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace, size
     const size_t bytes = (size_t)a.n_slots * a.heads * a.n * a.n * 4;
     if (x < y + bytes && y < x + bytes) return RWKVQ_EINVAL;
   }
-  (void)workspace; (void)workspace_bytes;
+  const la::Plan l = la::plan_of(a.tokens, a.n_seq, a.heads, a.n);
+  if (l.bytes > 0 && (!workspace || workspace_bytes < l.bytes)) return RWKVQ_ENOMEM;
+  if (!aligned16(workspace)) return RWKVQ_EALIGN;
+  p.limit = l.limit; p.block_rows = l.block_rows; p.blocks = l.blocks;
+  p.entries = l.blocks > 0 && (a.seq_start || a.slots) ? static_cast<la::Entry*>(workspace) : nullptr;
+  p.block_states = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + l.entries_bytes);
   p.status = device_status_ptr();
   if (!p.status) return RWKVQ_ECUDA;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (a.dtype == RWKVQ_F32) return cuda_status(la::launch<float>(p, s));
-  if (a.dtype == RWKVQ_F16) return cuda_status(la::launch<__half>(p, s));
-  return cuda_status(la::launch<__nv_bfloat16>(p, s));
+  if (a.dtype == RWKVQ_F32) return cuda_status(la::launch<float>(p, l, s));
+  if (a.dtype == RWKVQ_F16) return cuda_status(la::launch<__half>(p, l, s));
+  return cuda_status(la::launch<__nv_bfloat16>(p, l, s));
 }
 
 }  // extern "C"

@@ -14,9 +14,9 @@ GOOD = dict(r=P, k=P + 65536, v=P + 131072, logw=P + 196608, u=P, out=P + 262144
             k_row=128, v_row=128, logw_row=128, out_row=128, tokens=8, n_seq=2, heads=2, n=64, n_slots=4, dtype=2, decay_dtype=0, decay_per_head=0)
 
 
-def status(**kw):
+def status(ws_at=P + (1 << 21), ws_bytes=1 << 20, **kw):
     a = dict(GOOD, **kw)
-    return B.lib().rwkvq_linattn(B._LINATTN_ARGS.pack(*(a[f] for f in FIELDS)), P + (1 << 21), kw.pop("ws", 1 << 20), None)
+    return B.lib().rwkvq_linattn(B._LINATTN_ARGS.pack(*(a[f] for f in FIELDS)), ws_at, ws_bytes, None)
 
 
 @pytest.mark.parametrize("kw,want", [
@@ -24,7 +24,7 @@ def status(**kw):
     (dict(out=P), EINVAL), (dict(out=P + 65536), EINVAL), (dict(out=P + 131072), EINVAL), (dict(out=P + 196608), EINVAL),
     (dict(dtype=3), EINVAL), (dict(dtype=-1), EINVAL), (dict(decay_dtype=1), EINVAL), (dict(decay_dtype=3), EINVAL), (dict(tokens=-1), EINVAL),
     (dict(n_seq=0), EINVAL), (dict(heads=0), EINVAL), (dict(n=0), EINVAL), (dict(n_slots=-1), EINVAL), (dict(n=32), EUNSUPPORTED), (dict(n=256), EUNSUPPORTED),
-    (dict(n_seq=65536), EUNSUPPORTED), (dict(heads=1 << 20), EUNSUPPORTED), (dict(seq_start=0), EINVAL), (dict(slots=0, n_slots=1), EINVAL),
+    (dict(n_seq=65536), EUNSUPPORTED), (dict(heads=65536), EUNSUPPORTED), (dict(tokens=(1 << 30) + 1), EUNSUPPORTED), (dict(tokens=5000, r_row=0), EINVAL), (dict(seq_start=0), EINVAL), (dict(slots=0, n_slots=1), EINVAL),
     (dict(n_slots=0), EINVAL), (dict(state=0, state_out=0), EINVAL), (dict(r_row=120), EINVAL), (dict(k_row=0), EINVAL), (dict(v_row=64), EINVAL),
     (dict(out_row=127), EINVAL), (dict(logw_row=64), EINVAL), (dict(decay_per_head=1, logw_row=1), EINVAL), (dict(r_row=132), EALIGN),
     (dict(logw_row=130), EALIGN), (dict(r=P + 8), EALIGN), (dict(k=P + 65538), EALIGN), (dict(v=P + 131076), EALIGN), (dict(out=P + 262146), EALIGN),
@@ -46,3 +46,17 @@ def test_binding_refuses():
     assert e.value.status == EINVAL
     with pytest.raises(B.RwkvqError):
         B.rwkvq_linattn(x[0][0], *x[1:4], None, x[4], None)
+
+
+def test_workspace():
+    size = B.rwkvq_linattn_workspace_bytes
+    assert size(1, 1, 4, 64) == size(64, 64, 4, 64) == size(100, 1, 4, 32) == size(-1, 1, 4, 64) == size(5, 0, 4, 64) == 0
+    for heads, n in ((1, 64), (32, 64), (64, 64), (300, 64), (5, 128)):
+        last = 0
+        for tokens in list(range(9, 700, 7)) + [1000, 2048, 4100, 9999, 70001]:
+            assert size(tokens, 1, heads, n) >= last, (tokens, heads, n)
+            last = size(tokens, 1, heads, n)
+    need = size(5000, 2, 2, 64)
+    assert need > 0
+    assert status(tokens=5000, ws_bytes=need - 1) == ENOMEM and status(tokens=5000, ws_at=0, ws_bytes=need) == ENOMEM
+    assert status(tokens=5000, ws_at=P + (1 << 21) + 4, ws_bytes=need) == EALIGN
