@@ -673,30 +673,23 @@ def _refuse(where: str, why: str):
     raise e
 
 
-_DTYPES = None
+_DTYPES = {}          # torch's types -> RWKVQ_F32 / F16 / BF16; filled when torch is loaded
 
 
-def _dtype_of(t) -> int:
-    """RWKVQ_F32 / F16 / BF16 of a tensor, -1 for another type."""
-    global _DTYPES
-    if _DTYPES is None:
-        m = _torch or _load_torch()
-        _DTYPES = {m.float32: RWKVQ_F32, m.float16: RWKVQ_F16, m.bfloat16: RWKVQ_BF16}
-    return _DTYPES.get(t.dtype, -1)
-
-
-def _check_device(where: str, *tensors):
-    """All on the current CUDA device: the library launches there."""
+def _dtypes():
     t = _torch or _load_torch()
-    here = t.cuda.current_device() if t.cuda.is_available() else -1
-    for x in tensors:
-        if x is not None and (not x.is_cuda or x.get_device() != here):
-            _refuse(where, f"a tensor is on {x.device}, the current device is cuda:{here}")
+    _DTYPES.update({t.float32: RWKVQ_F32, t.float16: RWKVQ_F16, t.bfloat16: RWKVQ_BF16})
+    return _DTYPES
 
 
-def _bytes_of(where: str, x, rows: int, cols: int, what: str):
-    if x.element_size() != 1 or x.dim() != 2 or x.shape[0] != rows or x.shape[1] != cols or not x.is_contiguous():
-        _refuse(where, f"{what} has to be contiguous, of one-byte elements, [{rows}, {cols}]")
+def _here() -> int:
+    """Index of the current CUDA device, on which the library launches (-2 before CUDA is up)."""
+    t = _torch or _load_torch()
+    return t._C._cuda_getDevice() if t.cuda.is_initialized() else -2
+
+
+def _elsewhere(where: str, x, here: int):
+    _refuse(where, f"a tensor is on {x.device}, the current device is {'not in use yet' if here < 0 else f'cuda:{here}'}")
 
 
 def rwkvq_fp8_scale_pitch(cols: int) -> int:
@@ -704,39 +697,62 @@ def rwkvq_fp8_scale_pitch(cols: int) -> int:
     return int(lib().rwkvq_fp8_scale_pitch(cols))
 
 
+# The checks of the three functions below ask a tensor for as little as they can: every attribute costs 60 to 200 ns, and the calls are short.
+def _check_bytes(where: str, x, shape, what: str, here: int):
+    if x.get_device() != here:
+        _elsewhere(where, x, here)
+    if x.shape != shape or x.element_size() != 1 or not x.is_contiguous():
+        _refuse(where, f"{what} has to be contiguous, of one-byte elements, {list(shape)}")
+
+
 def rwkvq_fp8_quantize(x, codes, scale, block_rows: int, stream=None):
     """rwkvq_fp8_quantize: x float32 / float16 / bfloat16 [rows, cols] (rows may be strided), codes float8_e4m3fn or uint8 [rows, cols],
     scale uint8 [ceil(rows / block_rows), rwkvq_fp8_scale_pitch(cols)]."""
     where = "rwkvq_fp8_quantize"
-    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
-        _refuse(where, "x has to be two-dimensional with columns side by side")
-    rows, cols = x.shape
-    if block_rows not in (1, 128):
+    shape = x.shape
+    if len(shape) != 2:
+        _refuse(where, "x has to be two-dimensional")
+    rows, cols = shape
+    x_row, one = x.stride()
+    if one != 1 and cols > 1:
+        _refuse(where, "x has to have its columns side by side")
+    if block_rows != 1 and block_rows != 128:
         _refuse(where, "block_rows is 1 or 128")
-    _check_device(where, x, codes, scale)
-    _bytes_of(where, codes, rows, cols, "codes")
-    _bytes_of(where, scale, (rows + block_rows - 1) // block_rows, rwkvq_fp8_scale_pitch(cols), "scale")
-    _check(lib().rwkvq_fp8_quantize(x.data_ptr(), _dtype_of(x), rows, cols, x.stride(0) if rows > 1 else cols, block_rows, codes.data_ptr(),
-                                    scale.data_ptr(), _stream_ptr(stream)), where)
+    here = _here()
+    if x.get_device() != here:
+        _elsewhere(where, x, here)
+    _check_bytes(where, codes, shape, "codes", here)
+    _check_bytes(where, scale, ((rows + block_rows - 1) // block_rows, (cols + 2047) // 2048 * 16), "scale", here)
+    status = (_lib or lib()).rwkvq_fp8_quantize(x.data_ptr(), (_DTYPES or _dtypes()).get(x.dtype, -1), rows, cols, x_row if rows > 1 else cols, block_rows,
+                                                codes.data_ptr(), scale.data_ptr(), _stream_ptr(stream))
+    if status:
+        _check(status, where)
 
 
 def rwkvq_gemm_fp8(w_codes, w_scale, x_codes, x_scale, Y, stream=None):
     """rwkvq_gemm_fp8: codes and scales of rwkvq_fp8_quantize, w [oc, ic] with block_rows 128, x [M, ic] with block_rows 1; Y float32,
     float16 or bfloat16 [M, oc], whose rows may be strided."""
     where = "rwkvq_gemm_fp8"
-    if w_codes.dim() != 2 or x_codes.dim() != 2 or Y.dim() != 2:
+    w_shape, y_shape = w_codes.shape, Y.shape
+    if len(w_shape) != 2 or len(y_shape) != 2:
         _refuse(where, "codes and Y have to be two-dimensional")
-    (oc, ic), M = w_codes.shape, x_codes.shape[0]
-    _check_device(where, w_codes, w_scale, x_codes, x_scale, Y)
-    pitch = rwkvq_fp8_scale_pitch(ic)
-    _bytes_of(where, w_codes, oc, ic, "w_codes")
-    _bytes_of(where, x_codes, M, ic, "x_codes")
-    _bytes_of(where, w_scale, (oc + 127) // 128, pitch, "w_scale")
-    _bytes_of(where, x_scale, M, pitch, "x_scale")
-    if tuple(Y.shape) != (M, oc) or (oc > 1 and Y.stride(1) != 1):
+    oc, ic = w_shape
+    M = y_shape[0]
+    y_row, one = Y.stride()
+    here = _here()
+    pitch = (ic + 2047) // 2048 * 16
+    _check_bytes(where, w_codes, w_shape, "w_codes", here)
+    _check_bytes(where, x_codes, (M, ic), "x_codes", here)
+    _check_bytes(where, w_scale, ((oc + 127) // 128, pitch), "w_scale", here)
+    _check_bytes(where, x_scale, (M, pitch), "x_scale", here)
+    if y_shape[1] != oc or (one != 1 and oc > 1):
         _refuse(where, f"Y has to be [{M}, {oc}] with columns side by side")
-    _check(lib().rwkvq_gemm_fp8(w_codes.data_ptr(), w_scale.data_ptr(), oc, ic, x_codes.data_ptr(), x_scale.data_ptr(), M, Y.data_ptr(), _dtype_of(Y),
-                                Y.stride(0) if M > 1 else oc, _stream_ptr(stream)), where)
+    if Y.get_device() != here:
+        _elsewhere(where, Y, here)
+    status = (_lib or lib()).rwkvq_gemm_fp8(w_codes.data_ptr(), w_scale.data_ptr(), oc, ic, x_codes.data_ptr(), x_scale.data_ptr(), M, Y.data_ptr(),
+                                            (_DTYPES or _dtypes()).get(Y.dtype, -1), y_row if M > 1 else oc, _stream_ptr(stream))
+    if status:
+        _check(status, where)
 
 
 _LINATTN_ARGS = struct.Struct("@10P5q8i")          # rwkvq_linattn_args; packed at a third of what filling a ctypes structure costs
@@ -753,38 +769,60 @@ def rwkvq_linattn(r, k, v, logw, u, out, state, state_out=None, seq_start=None, 
     workspace uint8."""
     where = "rwkvq_linattn"
     t = _torch or _load_torch()
-    if r.dim() != 3:
+    shape, dtype, here = r.shape, r.dtype, _here()
+    if len(shape) != 3:
         _refuse(where, "r has to be [tokens, heads, n]")
-    tokens, heads, n = r.shape
-    dt = _dtype_of(r)
-    if state_out is None:
-        state_out = state
-    _check_device(where, r, k, v, logw, u, out, state, state_out, seq_start, slots, workspace)
-    for name, x in (("r", r), ("k", k), ("v", v), ("out", out)):
-        if x.shape != r.shape or x.dtype is not r.dtype or (tokens > 0 and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != n))):
-            _refuse(where, f"{name} has to be [{tokens}, {heads}, {n}] of {r.dtype} with heads side by side")
-    per_head = logw.dim() == 2
-    if logw.shape != (r.shape[:2] if per_head else r.shape) or (logw.dtype is not r.dtype and logw.dtype is not t.float32):
+    tokens, heads, n = shape
+    rows = []
+    for x in (r, k, v, out):
+        if x.get_device() != here:
+            _elsewhere(where, x, here)
+        row, head, one = x.stride() if x.dim() == 3 else (0, 0, 0)
+        if x.dtype is not dtype or x.shape != shape or (tokens and (one != 1 or (head != n and heads > 1))):
+            _refuse(where, f"r, k, v and out have to be [{tokens}, {heads}, {n}] of {dtype} with heads side by side")
+        rows.append(row if tokens > 1 else 0)
+    w_shape, w_stride, w_dtype = logw.shape, logw.stride(), logw.dtype
+    if logw.get_device() != here:
+        _elsewhere(where, logw, here)
+    per_head = len(w_shape) == 2
+    if w_shape != (shape[:2] if per_head else shape) or (w_dtype is not dtype and w_dtype is not t.float32):
         _refuse(where, "logw has to be [tokens, heads, n] or [tokens, heads] of r's type or float32")
-    if tokens > 0 and ((heads > 1 and logw.stride(1) != (1 if per_head else n)) or (not per_head and logw.stride(2) != 1)):
+    if tokens and ((w_stride[1] != (1 if per_head else n) and heads > 1) or (not per_head and w_stride[2] != 1)):
         _refuse(where, "logw has to have its heads side by side")
     n_seq, n_slots = 1, 0
     if seq_start is not None:
         n_seq = seq_start.numel() - 1
+        if seq_start.get_device() != here:
+            _elsewhere(where, seq_start, here)
         if seq_start.dtype is not t.int32 or not seq_start.is_contiguous():
             _refuse(where, "seq_start has to be int32, contiguous")
-    if slots is not None and (slots.dtype is not t.int32 or slots.numel() != n_seq or not slots.is_contiguous()):
-        _refuse(where, f"slots has to be int32 [{n_seq}], contiguous")
-    for x in (state, state_out):
+    if slots is not None:
+        if slots.get_device() != here:
+            _elsewhere(where, slots, here)
+        if slots.dtype is not t.int32 or slots.numel() != n_seq or not slots.is_contiguous():
+            _refuse(where, f"slots has to be int32 [{n_seq}], contiguous")
+    for x in (state,) if state_out is None or state_out is state else (state, state_out):
         if x is None:
             continue
-        if x.dtype is not t.float32 or x.dim() != 4 or tuple(x.shape[1:]) != (heads, n, n) or not x.is_contiguous() or (n_slots and x.shape[0] != n_slots):
+        if x.get_device() != here:
+            _elsewhere(where, x, here)
+        s_shape = x.shape
+        if x.dtype is not t.float32 or s_shape[1:] != (heads, n, n) or not x.is_contiguous() or (n_slots and s_shape[0] != n_slots):
             _refuse(where, f"states have to be float32 [slots, {heads}, {n}, {n}], contiguous, as many before as after")
-        n_slots = x.shape[0]
-    if u is not None and (u.dtype is not t.float32 or tuple(u.shape) != (heads, n) or not u.is_contiguous()):
-        _refuse(where, f"u has to be float32 [{heads}, {n}], contiguous")
-    rows = (r.stride(0), k.stride(0), v.stride(0), logw.stride(0), out.stride(0)) if tokens > 1 else (0, 0, 0, 0, 0)
-    args = _LINATTN_ARGS.pack(*(0 if x is None else x.data_ptr() for x in (r, k, v, logw, u, out, state, state_out, seq_start, slots)), *rows,
-                              tokens, n_seq, heads, n, n_slots, dt, _dtype_of(logw), 1 if per_head else 0)
-    _check(lib().rwkvq_linattn(args, None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
-                               _stream_ptr(stream)), where)
+        n_slots = s_shape[0]
+    if u is not None:
+        if u.get_device() != here:
+            _elsewhere(where, u, here)
+        if u.dtype is not t.float32 or u.shape != (heads, n) or not u.is_contiguous():
+            _refuse(where, f"u has to be float32 [{heads}, {n}], contiguous")
+    if workspace is not None and workspace.get_device() != here:
+        _elsewhere(where, workspace, here)
+    types = _DTYPES or _dtypes()
+    at = 0 if state is None else state.data_ptr()
+    args = _LINATTN_ARGS.pack(r.data_ptr(), k.data_ptr(), v.data_ptr(), logw.data_ptr(), 0 if u is None else u.data_ptr(), out.data_ptr(), at,
+                              at if state_out is None else state_out.data_ptr(), 0 if seq_start is None else seq_start.data_ptr(),
+                              0 if slots is None else slots.data_ptr(), rows[0], rows[1], rows[2], w_stride[0] if tokens > 1 else 0, rows[3],
+                              tokens, n_seq, heads, n, n_slots, types.get(dtype, -1), types.get(w_dtype, -1), per_head)
+    status = (_lib or lib()).rwkvq_linattn(args, *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)), _stream_ptr(stream))
+    if status:
+        _check(status, where)
