@@ -172,71 +172,112 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// Two fp32 numbers side by side: one instruction multiplies, adds or subtracts both.
+typedef unsigned long long pair;
+__device__ __forceinline__ pair pair_of(float x, float y) {
+  pair v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+  return v;
+}
+__device__ __forceinline__ float2 both(pair v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+__device__ __forceinline__ pair mul2(pair a, pair b) { pair d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ pair add2(pair a, pair b) { pair d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ pair fma2(pair a, pair b, pair c) { pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ pair exp2_(pair l) { const float2 f = both(l); return pair_of(__expf(f.x), __expf(f.y)); }
+__device__ __forceinline__ pair ones() { return pair_of(1.f, 1.f); }
+__device__ __forceinline__ pair load2(const float* p) { return *reinterpret_cast<const pair*>(p); }
+__device__ __forceinline__ pair widen(uint32_t v, __half) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v)); return pair_of(f.x, f.y); }
+__device__ __forceinline__ pair widen(uint32_t v, __nv_bfloat16) { return pair_of(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
+template <typename T> __device__ __forceinline__ pair load2(const T* p) { return widen(*reinterpret_cast<const uint32_t*>(p), T()); }
+// Four numbers.
+__device__ __forceinline__ void load4(const float* p, pair (&v)[2]) { const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(p); v[0] = q.x; v[1] = q.y; }
+template <typename T> __device__ __forceinline__ void load4(const T* p, pair (&v)[2]) {
+  const uint2 q = *reinterpret_cast<const uint2*>(p);
+  v[0] = widen(q.x, T()); v[1] = widen(q.y, T());
+}
 // (x, y) as n bf16 terms, x in the low half: each term is what the ones before it leave, rounded.
 template <int n>
-__device__ __forceinline__ void split(float x, float y, uint32_t (&t)[n]) {
+__device__ __forceinline__ void split(pair v, uint32_t (&t)[n]) {
 #pragma unroll
   for (int i = 0; i < n; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    const float2 f = both(v);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
     t[i] = *reinterpret_cast<const uint32_t*>(&h);
-    if (i + 1 < n) { x -= __uint_as_float(t[i] << 16); y -= __uint_as_float(t[i] & 0xFFFF0000u); }
+    if (i + 1 < n) v = fma2(widen(t[i], __nv_bfloat16()), pair_of(-1.f, -1.f), v);
   }
 }
 template <int n>
-__device__ __forceinline__ void store_split(uint8_t* at, int term_bytes, float x, float y) {
+__device__ __forceinline__ void store_split(uint8_t* at, int term_bytes, pair v) {
   uint32_t t[n];
-  split<n>(x, y, t);
+  split<n>(v, t);
 #pragma unroll
   for (int i = 0; i < n; ++i) *reinterpret_cast<uint32_t*>(at + i * term_bytes) = t[i];
 }
-__device__ __forceinline__ float2 load2(const float* p) { return *reinterpret_cast<const float2*>(p); }
-__device__ __forceinline__ float2 load2(const __half* p) { return __half22float2(*reinterpret_cast<const __half2*>(p)); }
-__device__ __forceinline__ float2 load2(const __nv_bfloat16* p) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p)); }
+// Where the logarithms of decays come from.
+enum { DECAY_F32 = 0, DECAY_SAME = 1, DECAY_HEAD = 2 };
 
-template <typename T, int N, bool kStateOnly>
+template <typename T, int N, int kDecay, bool kStateOnly>
 struct Worker {
   using Sh = Shape<T, N>;
   const Args& p;
   uint8_t* sm;
   int h, warp, lane, tid;
   float S[Sh::kTiles][4];      // S^T: values 16 warp + lane / 4 (+ 8: the last two), keys 8 j + 2 (lane % 4) and the next
-  float2 total;                // kStateOnly: sums of the logarithms of the decays of this thread's channels
+  pair total;                  // kStateOnly: sums of the logarithms of the decays of this thread's channels
+  // This thread's pieces of 16 bytes of the next chunk to fetch, and bytes from row to row.
+  static constexpr int kPieces = N * (int)sizeof(T) / 16, kRowsAtOnce = Sh::kThreads / kPieces;
+  static constexpr int kDecaySize = kDecay == DECAY_F32 ? 4 : (int)sizeof(T), kDecayPieces = N * kDecaySize / 16, kDecayRowsAtOnce = Sh::kThreads / kDecayPieces;
+  const uint8_t *rp, *kp, *vp, *lp;
 
   __device__ __forceinline__ Worker(const Args& p_, uint8_t* sm_) : p(p_), sm(sm_), h(blockIdx.y), warp(threadIdx.x >> 5), lane(threadIdx.x & 31), tid(threadIdx.x) {}
 
-  // Rows t0 .. t0 + 15 into a raw stage; zeros (no decay, nothing to add) behind `end`.
-  __device__ __forceinline__ void fetch(int stage, int t0, int end) {
+  __device__ __forceinline__ void fetch_from(int t0) {
     const rwkvq_linattn_args& a = p.a;
-    uint8_t* st = sm + stage * Sh::kStage;
-    constexpr int kPieces = N * (int)sizeof(T) / 16;
-    for (int i = tid; i < kChunk * kPieces; i += Sh::kThreads) {
-      const int t = i / kPieces, c = i % kPieces, row = t0 + t;
-      const bool there = row < end;
-      const long long at = there ? row : t0, off = ((long long)h * N * (int)sizeof(T)) + c * 16;
-      uint8_t* dst = st + t * Sh::kRawPitch + c * 16;
-      if (!kStateOnly) cp_async16(dst, static_cast<const uint8_t*>(a.r) + at * a.r_row * (int)sizeof(T) + off, there);
-      cp_async16(dst + Sh::kRaw, static_cast<const uint8_t*>(a.k) + at * a.k_row * (int)sizeof(T) + off, there);
-      cp_async16(dst + 2 * Sh::kRaw, static_cast<const uint8_t*>(a.v) + at * a.v_row * (int)sizeof(T) + off, there);
+    const long long row = t0 + tid / kPieces, off = (long long)h * N * (int)sizeof(T) + tid % kPieces * 16;
+    rp = static_cast<const uint8_t*>(a.r) + row * a.r_row * (int)sizeof(T) + off;
+    kp = static_cast<const uint8_t*>(a.k) + row * a.k_row * (int)sizeof(T) + off;
+    vp = static_cast<const uint8_t*>(a.v) + row * a.v_row * (int)sizeof(T) + off;
+    if (kDecay == DECAY_HEAD) lp = static_cast<const uint8_t*>(a.logw) + ((t0 + (tid & 15)) * a.logw_row + h) * (a.decay_dtype == RWKVQ_F32 ? 4 : (int)sizeof(T));
+    else lp = static_cast<const uint8_t*>(a.logw) + ((t0 + tid / kDecayPieces) * a.logw_row + (long long)h * N) * kDecaySize + tid % kDecayPieces * 16;
+  }
+  // The next 16 rows into a raw stage, `left` of them in the sequence; zeros (no decay, nothing to add) behind.
+  __device__ __forceinline__ void fetch(int stage, int left) {
+    const rwkvq_linattn_args& a = p.a;
+    uint8_t* dst = sm + stage * Sh::kStage + tid / kPieces * Sh::kRawPitch + tid % kPieces * 16;
+    const int rb = (int)sizeof(T) * kRowsAtOnce;
+#pragma unroll
+    for (int i = 0; i < kChunk / kRowsAtOnce; ++i) {
+      const bool there = tid / kPieces + i * kRowsAtOnce < left;
+      // a row that is not there is not read: the address is one that is
+      if (!kStateOnly) cp_async16(dst + i * kRowsAtOnce * Sh::kRawPitch, there ? rp : static_cast<const uint8_t*>(a.r), there);
+      cp_async16(dst + i * kRowsAtOnce * Sh::kRawPitch + Sh::kRaw, there ? kp : static_cast<const uint8_t*>(a.k), there);
+      cp_async16(dst + i * kRowsAtOnce * Sh::kRawPitch + 2 * Sh::kRaw, there ? vp : static_cast<const uint8_t*>(a.v), there);
+      rp += a.r_row * rb; kp += a.k_row * rb; vp += a.v_row * rb;
     }
-    uint8_t* lw = st + 3 * Sh::kRaw;
-    if (a.decay_per_head) {
-      if (tid < kChunk) reinterpret_cast<float*>(lw)[tid] = t0 + tid < end ? log_decay<T>(a, t0 + tid, h, 0) : 0.f;
+    uint8_t* lw = sm + stage * Sh::kStage + 3 * Sh::kRaw;
+    if (kDecay == DECAY_HEAD) {
+      const bool f32 = a.decay_dtype == RWKVQ_F32;
+      if (tid < kChunk) reinterpret_cast<float*>(lw)[tid] = tid >= left ? 0.f : f32 ? *reinterpret_cast<const float*>(lp) : to_f32(*reinterpret_cast<const T*>(lp));
+      lp += a.logw_row * ((f32 ? 4 : (int)sizeof(T)) * kChunk);
     } else {
-      const int ws = a.decay_dtype == RWKVQ_F32 ? 4 : (int)sizeof(T), pieces = N * ws / 16;
-      for (int i = tid; i < kChunk * pieces; i += Sh::kThreads) {
-        const int t = i / pieces, c = i % pieces, row = t0 + t;
-        const bool there = row < end;
-        cp_async16(lw + t * Sh::kDecayPitch + c * 16,
-                   static_cast<const uint8_t*>(a.logw) + ((there ? row : t0) * a.logw_row + (long long)h * N) * ws + c * 16, there);
+#pragma unroll
+      for (int i = 0; i < kChunk / kDecayRowsAtOnce; ++i) {
+        const int t = tid / kDecayPieces + i * kDecayRowsAtOnce;
+        cp_async16(lw + t * Sh::kDecayPitch + tid % kDecayPieces * 16, t < left ? lp : static_cast<const uint8_t*>(a.logw), t < left);
+        lp += a.logw_row * (kDecaySize * kDecayRowsAtOnce);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
 
-  __device__ __forceinline__ float2 decay2(const uint8_t* lw, int t, int c) const {
-    if (p.a.decay_per_head) { const float v = reinterpret_cast<const float*>(lw)[t]; return make_float2(v, v); }
+  __device__ __forceinline__ pair decay2(const uint8_t* lw, int t, int c) const {
+    if (kDecay == DECAY_HEAD) { const float v = reinterpret_cast<const float*>(lw)[t]; return pair_of(v, v); }
     const uint8_t* row = lw + t * Sh::kDecayPitch;
-    return p.a.decay_dtype == RWKVQ_F32 ? load2(reinterpret_cast<const float*>(row) + c) : load2(reinterpret_cast<const T*>(row) + c);
+    return kDecay == DECAY_F32 ? load2(reinterpret_cast<const float*>(row) + c) : load2(reinterpret_cast<const T*>(row) + c);
   }
 
   // A stage's operands.  Warps of a group of four take: r of the first eight tokens, r of the last, k of the last, k of the first; a lane two channels.
@@ -245,95 +286,100 @@ struct Worker {
     const uint8_t* lw = st + 3 * Sh::kRaw;
     const int role = warp & 3, c = (warp >> 2) * 64 + lane * 2;
     auto raw = [&](int which, int t) { return load2(reinterpret_cast<const T*>(st + which * Sh::kRaw + t * Sh::kRawPitch) + c); };
-    auto w_at = [&](int t) { return reinterpret_cast<float2*>(sm + Sh::oW + (t * (N + 4) + c) * 4); };
+    auto w_at = [&](int t) { return reinterpret_cast<pair*>(sm + Sh::oW + (t * (N + 4) + c) * 4); };
     if (role == 0) {
       if (!kStateOnly) {
-        float2 q = make_float2(1.f, 1.f);
+        pair q = ones();
 #pragma unroll
         for (int t = 0; t < kHalf; ++t) {
-          const float2 l = decay2(lw, t, c), w = make_float2(__expf(l.x), __expf(l.y)), r = raw(0, t);
+          const pair w = exp2_(decay2(lw, t, c));
           *w_at(t) = w;
-          store_split<Sh::R>(sm + Sh::oRt + t * Sh::kPitch + c * 2, Sh::kTerm, r.x * q.x, r.y * q.y);
-          q.x *= w.x; q.y *= w.y;
+          store_split<Sh::R>(sm + Sh::oRt + t * Sh::kPitch + c * 2, Sh::kTerm, mul2(raw(0, t), q));
+          q = mul2(q, w);
         }
       }
     } else if (role == 1) {
-      float2 s = make_float2(0.f, 0.f), q = make_float2(1.f, 1.f);
+      pair s = decay2(lw, 0, c), q = ones();
 #pragma unroll
-      for (int t = 0; t < kHalf; ++t) { const float2 l = decay2(lw, t, c); s.x += l.x; s.y += l.y; }
-      const float2 d1 = make_float2(__expf(s.x), __expf(s.y));
+      for (int t = 1; t < kHalf; ++t) s = add2(s, decay2(lw, t, c));
+      const pair d1 = exp2_(s);
 #pragma unroll
       for (int t = kHalf; t < kChunk; ++t) {
-        const float2 l = decay2(lw, t, c);
-        s.x += l.x; s.y += l.y;
+        const pair l = decay2(lw, t, c);
+        s = add2(s, l);
         if (!kStateOnly) {
-          const float2 w = make_float2(__expf(l.x), __expf(l.y)), r = raw(0, t);
+          const pair w = exp2_(l), m = mul2(raw(0, t), q);
           *w_at(t) = w;
-          const float2 m = make_float2(r.x * q.x, r.y * q.y);
-          store_split<Sh::R>(sm + Sh::oRp + (t - kHalf) * Sh::kPitch + c * 2, Sh::kHalfTerm, m.x, m.y);
-          store_split<Sh::R>(sm + Sh::oRt + t * Sh::kPitch + c * 2, Sh::kTerm, m.x * d1.x, m.y * d1.y);
-          q.x *= w.x; q.y *= w.y;
+          store_split<Sh::R>(sm + Sh::oRp + (t - kHalf) * Sh::kPitch + c * 2, Sh::kHalfTerm, m);
+          store_split<Sh::R>(sm + Sh::oRt + t * Sh::kPitch + c * 2, Sh::kTerm, mul2(m, d1));
+          q = mul2(q, w);
         }
       }
       // the state's decay, over and over the same where decays do not change: the accurate exponential of the sum
-      *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(s.x), expf(s.y));
-      if (kStateOnly) { total.x += s.x; total.y += s.y; }
+      const float2 f = both(s);
+      *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(f.x), expf(f.y));
+      if (kStateOnly) total = add2(total, s);
     } else if (role == 2) {
-      float2 q = make_float2(1.f, 1.f);
+      pair q = ones();
 #pragma unroll
       for (int t = kChunk - 1; t >= kHalf; --t) {
-        const float2 l = decay2(lw, t, c), k = raw(1, t);
-        store_split<K3>(sm + Sh::oKt + t * Sh::kPitch + c * 2, Sh::kTerm, k.x * q.x, k.y * q.y);
-        q.x *= __expf(l.x); q.y *= __expf(l.y);
+        store_split<K3>(sm + Sh::oKt + t * Sh::kPitch + c * 2, Sh::kTerm, mul2(raw(1, t), q));
+        q = mul2(q, exp2_(decay2(lw, t, c)));
       }
     } else {
-      float2 s = make_float2(0.f, 0.f), q = make_float2(1.f, 1.f);
+      pair s = decay2(lw, kHalf, c), q = ones();
 #pragma unroll
-      for (int t = kHalf; t < kChunk; ++t) { const float2 l = decay2(lw, t, c); s.x += l.x; s.y += l.y; }
-      const float2 d2 = make_float2(__expf(s.x), __expf(s.y));
+      for (int t = kHalf + 1; t < kChunk; ++t) s = add2(s, decay2(lw, t, c));
+      const pair d2 = exp2_(s);
 #pragma unroll
       for (int t = kHalf - 1; t >= 0; --t) {
-        const float2 l = decay2(lw, t, c), k = raw(1, t), m = make_float2(k.x * q.x, k.y * q.y);
-        if (!kStateOnly) store_split<Sh::R>(sm + Sh::oKp + t * Sh::kPitch + c * 2, Sh::kHalfTerm, m.x, m.y);
-        store_split<K3>(sm + Sh::oKt + t * Sh::kPitch + c * 2, Sh::kTerm, m.x * d2.x, m.y * d2.y);
-        q.x *= __expf(l.x); q.y *= __expf(l.y);
+        const pair m = mul2(raw(1, t), q);
+        if (!kStateOnly) store_split<Sh::R>(sm + Sh::oKp + t * Sh::kPitch + c * 2, Sh::kHalfTerm, m);
+        store_split<K3>(sm + Sh::oKt + t * Sh::kPitch + c * 2, Sh::kTerm, mul2(m, d2));
+        q = mul2(q, exp2_(decay2(lw, t, c)));
       }
     }
     if (Sh::V > 1 && (role & 1) == 0) {       // the warps with less to do
       const int t0 = role == 0 ? 0 : kHalf;
 #pragma unroll
-      for (int t = 0; t < kHalf; ++t) {
-        const float2 v = raw(2, t0 + t);
-        store_split<Sh::V>(sm + Sh::oVt + (t0 + t) * Sh::kPitch + c * 2, Sh::kTerm, v.x, v.y);
-      }
+      for (int t = 0; t < kHalf; ++t) store_split<Sh::V>(sm + Sh::oVt + (t0 + t) * Sh::kPitch + c * 2, Sh::kTerm, raw(2, t0 + t));
     }
   }
 
   // The triangles of A: lanes 0-15 tokens 0-7, the others tokens 8-15, four channels each.  Warp w of a group of four takes columns s = w and 7 - w,
   // together seven entries below the diagonal (and the two on it), whatever w.
   __device__ __forceinline__ void triangles(int stage) {
-    const uint8_t* st = sm + stage * Sh::kStage;
     const int w = warp & 3, t0 = (lane >> 4) * kHalf, c = (warp >> 2) * 64 + (lane & 15) * 4, first = 7 - w;
-    auto four = [&](int which, int t) {
-      const T* at = reinterpret_cast<const T*>(st + which * Sh::kRaw + (t0 + t) * Sh::kRawPitch) + c;
-      const float2 a = load2(at), b = load2(at + 2);
-      return make_float4(a.x, a.y, b.x, b.y);
-    };
-    float4 x = four(1, w);
-    const float4 x2 = four(1, first), u = *reinterpret_cast<const float4*>(sm + Sh::oU + c * 4);
+    const uint8_t* rr = sm + stage * Sh::kStage + t0 * Sh::kRawPitch + c * (int)sizeof(T);
+    const uint8_t* ww = sm + Sh::oW + (t0 * (N + 4) + c) * 4;
+    auto row4 = [&](const uint8_t* at, int t, pair (&v)[2]) { load4(reinterpret_cast<const T*>(at + t * Sh::kRawPitch), v); };
+    auto dot = [](const pair (&a)[2], const pair (&b)[2]) { const float2 f = both(fma2(a[1], b[1], mul2(a[0], b[0]))); return f.x + f.y; };
+    pair x[2], x2[2], r[2], u[2];
     float v[8], last;
+    row4(rr + Sh::kRaw, w, x);
+    row4(rr + Sh::kRaw, first, x2);
+    load4(reinterpret_cast<const float*>(sm + Sh::oU) + c, u);
     {
-      const float4 r = four(0, w), r2 = four(0, first);
-      v[7] = r.x * u.x * x.x + r.y * u.y * x.y + r.z * u.z * x.z + r.w * u.w * x.w;
-      last = r2.x * u.x * x2.x + r2.y * u.y * x2.y + r2.z * u.z * x2.z + r2.w * u.w * x2.w;
+      pair ru[2];
+      row4(rr, w, r);
+      ru[0] = mul2(r[0], u[0]); ru[1] = mul2(r[1], u[1]);
+      v[7] = dot(ru, x);
+      row4(rr, first, r);
+      ru[0] = mul2(r[0], u[0]); ru[1] = mul2(r[1], u[1]);
+      last = dot(ru, x2);
     }
+    // j < first: t = w + 1 + j of column w, then t = j + 1 of column 7 - w; first is at least 4
+    const uint8_t *rw = rr + w * Sh::kRawPitch, *wx = ww + w * ((N + 4) * 4);
 #pragma unroll
     for (int j = 0; j < 7; ++j) {
-      if (j == first) x = x2;
-      const int t = j < first ? w + 1 + j : j + 1;
-      const float4 r = four(0, t), wt = *reinterpret_cast<const float4*>(sm + Sh::oW + ((t0 + t) * (N + 4) + c) * 4);
-      v[j] = r.x * x.x + r.y * x.y + r.z * x.z + r.w * x.w;
-      x.x *= wt.x; x.y *= wt.y; x.z *= wt.z; x.w *= wt.w;
+      if (j >= 4 && j == first) { x[0] = x2[0]; x[1] = x2[1]; rw = rr; wx = ww; }
+      pair wt[2];
+      row4(rw, j + 1, r);
+      v[j] = dot(r, x);
+      if (j < 6) {
+        load4(reinterpret_cast<const float*>(wx + (j + 1) * ((N + 4) * 4)), wt);
+        x[0] = mul2(x[0], wt[0]); x[1] = mul2(x[1], wt[1]);
+      }
     }
     // eight sums over sixteen lanes: each step halves the values a lane carries
 #pragma unroll
@@ -361,8 +407,9 @@ struct Worker {
   __device__ __forceinline__ void rows(int begin, int end) {
     const rwkvq_linattn_args& a = p.a;
     const int n = (end - begin + kChunk - 1) / kChunk, g = lane >> 2, q = lane & 3;
-    fetch(0, begin, end);
-    if (n > 1) fetch(1, begin + kChunk, end);
+    fetch_from(begin);
+    fetch(0, end - begin);
+    if (n > 1) fetch(1, end - begin - kChunk);
     if (n > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
     else asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
@@ -387,7 +434,7 @@ struct Worker {
 #pragma unroll
           for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) split<Sh::R>(S[2 * k + m][2 * nb], S[2 * k + m][2 * nb + 1], b[nb][m]);
+            for (int m = 0; m < 2; ++m) split<Sh::R>(pair_of(S[2 * k + m][2 * nb], S[2 * k + m][2 * nb + 1]), b[nb][m]);
 #pragma unroll
           for (int e = 0; e < Sh::R; ++e)
 #pragma unroll
@@ -410,8 +457,9 @@ struct Worker {
       }
 #pragma unroll
       for (int j = 0; j < Sh::kTiles; ++j) {
-        const float2 d = *reinterpret_cast<const float2*>(sm + Sh::oD + (j * 8 + q * 2) * 4);
-        S[j][0] *= d.x; S[j][1] *= d.y; S[j][2] *= d.x; S[j][3] *= d.y;
+        const pair d = *reinterpret_cast<const pair*>(sm + Sh::oD + (j * 8 + q * 2) * 4);
+        const float2 lo = both(mul2(pair_of(S[j][0], S[j][1]), d)), hi = both(mul2(pair_of(S[j][2], S[j][3]), d));
+        S[j][0] = lo.x; S[j][1] = lo.y; S[j][2] = hi.x; S[j][3] = hi.y;
       }
       {
         const uint32_t kt = smem_u32(sm + Sh::oKt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
@@ -430,7 +478,7 @@ struct Worker {
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
       __syncthreads();
-      if (i + 2 < n) fetch(i & 1, t0 + 2 * kChunk, end);
+      if (i + 2 < n) fetch(i & 1, end - t0 - 2 * kChunk);
       if (!kStateOnly) {
         const float* A = reinterpret_cast<const float*>(sm + Sh::oA) + g * 8 + q * 2;
         float2 up = *reinterpret_cast<const float2*>(A), dn = *reinterpret_cast<const float2*>(A + 64);
@@ -440,9 +488,9 @@ struct Worker {
           up.x += up2.x; up.y += up2.y; dn.x += dn2.x; dn.y += dn2.y;
         }
         uint32_t a0[Sh::R], a1[Sh::R], a3[Sh::R];
-        split<Sh::R>(up.x, up.y, a0);
-        split<Sh::R>(mid[2], mid[3], a1);
-        split<Sh::R>(dn.x, dn.y, a3);
+        split<Sh::R>(pair_of(up.x, up.y), a0);
+        split<Sh::R>(pair_of(mid[2], mid[3]), a1);
+        split<Sh::R>(pair_of(dn.x, dn.y), a3);
 #pragma unroll
         for (int e = 0; e < Sh::R; ++e) {
           const uint32_t x[4] = {a0[e], a1[e], 0u, a3[e]};
@@ -518,12 +566,12 @@ __device__ __forceinline__ int next_sequence(const Args& p, int from, int row0, 
   return found;
 }
 
-template <typename T, int N, bool kStateOnly>
+template <typename T, int N, int kDecay, bool kStateOnly>
 __global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? 4 : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
   using Sh = Shape<T, N>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int word;
-  Worker<T, N, kStateOnly> w(p, smem);
+  Worker<T, N, kDecay, kStateOnly> w(p, smem);
   const int block = blockIdx.x, row0 = block * p.block_rows, row1 = min(row0 + p.block_rows, p.a.tokens);
   if (!kStateOnly) {
     for (int i = threadIdx.x; i < (N / 64) * 128; i += Sh::kThreads) reinterpret_cast<float*>(smem + Sh::oA)[i] = 0.f;       // above the diagonals it stays zero
@@ -550,11 +598,13 @@ __global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? 4 : 1) lina
 #pragma unroll
           for (int i = 0; i < 4; ++i) w.S[j][i] = 0.f;
       }
-      w.total = make_float2(0.f, 0.f);
+      w.total = pair_of(0.f, 0.f);
       w.rows(begin, end);
       w.keep(w.block_state(block, 0));
-      if ((w.warp & 3) == 1)
-        *reinterpret_cast<float2*>(w.block_state(block, 2) + (w.warp >> 2) * 64 + w.lane * 2) = make_float2(expf(w.total.x), expf(w.total.y));
+      if ((w.warp & 3) == 1) {
+        const float2 f = both(w.total);
+        *reinterpret_cast<float2*>(w.block_state(block, 2) + (w.warp >> 2) * 64 + w.lane * 2) = make_float2(expf(f.x), expf(f.y));
+      }
       return;
     }
     if (e.start < row0 || e.end > row1) {
@@ -600,29 +650,35 @@ Plan plan_of(int tokens, int n_seq, int heads, int n) {
   return l;
 }
 
+template <typename T, int N, int kDecay>
+cudaError_t launch_chunks(const Args& p, const Plan& l, cudaStream_t s) {
+  using Sh = Shape<T, N>;
+  static SmemOptIn opt_state, opt_all;
+  cudaError_t e = opt_all((const void*)linattn_chunk_kernel<T, N, kDecay, false>, Sh::kBytes);
+  if (e == cudaSuccess && l.blocks > 1) {
+    e = opt_state((const void*)linattn_chunk_kernel<T, N, kDecay, true>, Sh::kBytes);
+    if (e == cudaSuccess) {
+      linattn_chunk_kernel<T, N, kDecay, true><<<dim3((unsigned)l.blocks - 1, (unsigned)p.a.heads), Sh::kThreads, Sh::kBytes, s>>>(p);
+      e = cudaGetLastError();
+    }
+  }
+  if (e != cudaSuccess) return e;
+  linattn_chunk_kernel<T, N, kDecay, false><<<dim3((unsigned)l.blocks, (unsigned)p.a.heads), Sh::kThreads, Sh::kBytes, s>>>(p);
+  return cudaGetLastError();
+}
 template <typename T, int N>
-cudaError_t launch_n(Args& p, const Plan& l, cudaStream_t s) {
+cudaError_t launch_n(const Args& p, const Plan& l, cudaStream_t s) {
   if (l.blocks == 0 || p.entries) {
     linattn_token_kernel<T, N><<<dim3((unsigned)p.a.heads, (unsigned)p.a.n_seq, N / kCols), kTokenThreads, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || l.blocks == 0) return e;
   }
-  using Sh = Shape<T, N>;
-  static SmemOptIn opt_state, opt_all;
-  cudaError_t e = opt_all((const void*)linattn_chunk_kernel<T, N, false>, Sh::kBytes);
-  if (e == cudaSuccess && l.blocks > 1) {
-    e = opt_state((const void*)linattn_chunk_kernel<T, N, true>, Sh::kBytes);
-    if (e == cudaSuccess) {
-      linattn_chunk_kernel<T, N, true><<<dim3((unsigned)l.blocks - 1, (unsigned)p.a.heads), Sh::kThreads, Sh::kBytes, s>>>(p);
-      e = cudaGetLastError();
-    }
-  }
-  if (e != cudaSuccess) return e;
-  linattn_chunk_kernel<T, N, false><<<dim3((unsigned)l.blocks, (unsigned)p.a.heads), Sh::kThreads, Sh::kBytes, s>>>(p);
-  return cudaGetLastError();
+  if (p.a.decay_per_head) return launch_chunks<T, N, DECAY_HEAD>(p, l, s);
+  if (sizeof(T) == 4 || p.a.decay_dtype == RWKVQ_F32) return launch_chunks<T, N, DECAY_F32>(p, l, s);
+  return launch_chunks<T, N, sizeof(T) == 4 ? DECAY_F32 : DECAY_SAME>(p, l, s);
 }
 template <typename T>
-cudaError_t launch(Args& p, const Plan& l, cudaStream_t s) {
+cudaError_t launch(const Args& p, const Plan& l, cudaStream_t s) {
   return p.a.n == 64 ? launch_n<T, 64>(p, l, s) : launch_n<T, 128>(p, l, s);
 }
 
