@@ -153,7 +153,7 @@ struct Shape {
   // a raw stage: r, k, v, logarithms of decays
   static constexpr int kStage = 3 * kRaw + kChunk * kDecayPitch;
   static constexpr int oRt = 2 * kStage, oKt = oRt + R * kTerm, oRp = oKt + K3 * kTerm, oKp = oRp + R * kHalfTerm, oVt = oKp + R * kHalfTerm;
-  static constexpr int oW = oVt + (V > 1 ? V * kTerm : 0), oD = oW + kChunk * (N + 4) * 4, oA = oD + N * 4, oU = oA + (N / 64) * 2 * 64 * 4;
+  static constexpr int oW = oVt + (V > 2 ? V * kTerm : 0), oD = oW + kChunk * (N + 4) * 4, oA = oD + N * 4, oMid = oA + (N / 64) * 2 * 64 * 4, oU = oMid + kSteps * 64 * 4;
   static constexpr int kBytes = oU + N * 4;
   static constexpr int kStateFloats = N * N, kBlockFloats = 2 * N * N + N;
 };
@@ -339,7 +339,7 @@ struct Worker {
         q = mul2(q, exp2_(decay2(lw, t, c)));
       }
     }
-    if (Sh::V > 1 && (role & 1) == 0) {       // the warps with less to do
+    if (Sh::V > 2 && (role & 1) == 0) {       // the warps with less to do
       const int t0 = role == 0 ? 0 : kHalf;
 #pragma unroll
       for (int t = 0; t < kHalf; ++t) store_split<Sh::V>(sm + Sh::oVt + (t0 + t) * Sh::kPitch + c * 2, Sh::kTerm, raw(2, t0 + t));
@@ -417,20 +417,31 @@ struct Worker {
     __syncthreads();
     for (int i = 0; i < n; ++i) {
       const int t0 = begin + i * kChunk;
-      float o[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, mid[4] = {0.f, 0.f, 0.f, 0.f};
+      float o[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
       if (!kStateOnly) {
         triangles(i & 1);
+        {
+          // the block of A below the triangles: warp w adds up sixteen keys.  Rows of r P' (lanes 0-15) and of k Q' (16-31), eight keys and the next
+          float mid[4] = {0.f, 0.f, 0.f, 0.f};
+          const uint32_t half = smem_u32(sm + (lane < 16 ? Sh::oRp : Sh::oKp)) + (lane & 7) * Sh::kPitch + ((lane >> 3) & 1) * 16 + warp * 32;
+          uint32_t y[Sh::R][4];
+#pragma unroll
+          for (int e = 0; e < Sh::R; ++e) ldsm4(half + e * Sh::kHalfTerm, y[e]);
+#pragma unroll
+          for (int e = 0; e < Sh::R; ++e)
+#pragma unroll
+            for (int f = 0; f < Sh::R - e; ++f) {
+              const uint32_t low[4] = {0u, y[e][0], 0u, y[e][1]};
+              mma(mid, low, y[f][2], y[f][3]);
+            }
+          *reinterpret_cast<float2*>(sm + Sh::oMid + (warp * 64 + g * 8 + q * 2) * 4) = make_float2(mid[2], mid[3]);
+        }
         const uint32_t rt = smem_u32(sm + Sh::oRt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
-        // rows of r P' (lanes 0-15) and of k Q' (16-31), the first eight keys and the next
-        const uint32_t half = smem_u32(sm + (lane < 16 ? Sh::oRp : Sh::oKp)) + (lane & 7) * Sh::kPitch + ((lane >> 3) & 1) * 16;
 #pragma unroll
         for (int k = 0; k < Sh::kSteps; ++k) {
-          uint32_t x[Sh::R][4], y[Sh::R][4], b[2][2][Sh::R];
+          uint32_t x[Sh::R][4], b[2][2][Sh::R];
 #pragma unroll
-          for (int e = 0; e < Sh::R; ++e) {
-            ldsm4(rt + e * Sh::kTerm + k * 32, x[e]);
-            ldsm4(half + e * Sh::kHalfTerm + k * 32, y[e]);
-          }
+          for (int e = 0; e < Sh::R; ++e) ldsm4(rt + e * Sh::kTerm + k * 32, x[e]);
 #pragma unroll
           for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -441,8 +452,6 @@ struct Worker {
             for (int f = 0; f < Sh::R - e; ++f) {
               mma(o[0], x[e], b[0][0][f], b[0][1][f]);
               mma(o[1], x[e], b[1][0][f], b[1][1][f]);
-              const uint32_t low[4] = {0u, y[e][0], 0u, y[e][1]};
-              mma(mid, low, y[f][2], y[f][3]);
             }
         }
       }
@@ -450,10 +459,24 @@ struct Worker {
       uint32_t v[Sh::V][4];
       {
         const int row = (lane & 7) + (lane >> 4) * 8, col = warp * 16 + ((lane >> 3) & 1) * 8;
-        const uint32_t at = Sh::V > 1 ? smem_u32(sm + Sh::oVt) + row * Sh::kPitch + col * 2
-                                      : smem_u32(sm + (i & 1) * Sh::kStage + 2 * Sh::kRaw) + row * Sh::kRawPitch + col * 2;
+        if constexpr (Sh::V > 2) {
+          const uint32_t at = smem_u32(sm + Sh::oVt) + row * Sh::kPitch + col * 2;
 #pragma unroll
-        for (int e = 0; e < Sh::V; ++e) ldsm4t(at + e * Sh::kTerm, v[e]);
+          for (int e = 0; e < Sh::V; ++e) ldsm4t(at + e * Sh::kTerm, v[e]);
+        } else {
+          uint32_t x[4];
+          ldsm4t(smem_u32(sm + (i & 1) * Sh::kStage + 2 * Sh::kRaw) + row * Sh::kRawPitch + col * 2, x);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if constexpr (Sh::V == 1) v[0][j] = x[j];
+            else {
+              uint32_t t[Sh::V];
+              split<Sh::V>(widen(x[j], T()), t);
+#pragma unroll
+              for (int e = 0; e < Sh::V; ++e) v[e][j] = t[e];
+            }
+          }
+        }
       }
 #pragma unroll
       for (int j = 0; j < Sh::kTiles; ++j) {
@@ -487,9 +510,12 @@ struct Worker {
           const float2 up2 = *reinterpret_cast<const float2*>(A + x * 128), dn2 = *reinterpret_cast<const float2*>(A + x * 128 + 64);
           up.x += up2.x; up.y += up2.y; dn.x += dn2.x; dn.y += dn2.y;
         }
+        pair mid = load2(reinterpret_cast<const float*>(sm + Sh::oMid) + g * 8 + q * 2);
+#pragma unroll
+        for (int x = 1; x < Sh::kSteps; ++x) mid = add2(mid, load2(reinterpret_cast<const float*>(sm + Sh::oMid) + x * 64 + g * 8 + q * 2));
         uint32_t a0[Sh::R], a1[Sh::R], a3[Sh::R];
         split<Sh::R>(pair_of(up.x, up.y), a0);
-        split<Sh::R>(pair_of(mid[2], mid[3]), a1);
+        split<Sh::R>(mid, a1);
         split<Sh::R>(pair_of(dn.x, dn.y), a3);
 #pragma unroll
         for (int e = 0; e < Sh::R; ++e) {
@@ -566,8 +592,12 @@ __device__ __forceinline__ int next_sequence(const Args& p, int from, int row0, 
   return found;
 }
 
+#ifndef LA_PER_SM
+#define LA_PER_SM 4
+#endif
+constexpr int kPerSm = LA_PER_SM;
 template <typename T, int N, int kDecay, bool kStateOnly>
-__global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? 4 : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
+__global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? kPerSm : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
   using Sh = Shape<T, N>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int word;
@@ -638,7 +668,7 @@ constexpr int kShortest = 8;
 Plan plan_of(int tokens, int n_seq, int heads, int n) {
   Plan l = {0, 0, 0x7FFFFFFF, 0, 0};
   if (tokens <= std::max<long long>(kShortest, 2ll * n_seq)) return l;        // all by the token kernel
-  const long long most = std::max<long long>(1, (long long)sm_count() * (n == 64 ? 4 : 1) / heads);
+  const long long most = std::max<long long>(1, (long long)sm_count() * (n == 64 ? kPerSm : 1) / heads);
   const long long rows = std::max<long long>(64, ((tokens + most - 1) / most + kChunk - 1) / kChunk * kChunk);
   l.block_rows = (int)std::min<long long>(rows, 1 << 30);
   l.blocks = (int)((tokens + (long long)l.block_rows - 1) / l.block_rows);
