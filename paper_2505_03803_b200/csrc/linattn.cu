@@ -163,13 +163,13 @@ __device__ __forceinline__ void cp_async16(void* dst, const void* src, bool ther
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // Two fp32 numbers side by side: one instruction multiplies, adds or subtracts both.
@@ -285,64 +285,66 @@ struct Worker {
     const uint8_t* st = sm + stage * Sh::kStage;
     const uint8_t* lw = st + 3 * Sh::kRaw;
     const int role = warp & 3, c = (warp >> 2) * 64 + lane * 2;
-    auto raw = [&](int which, int t) { return load2(reinterpret_cast<const T*>(st + which * Sh::kRaw + t * Sh::kRawPitch) + c); };
-    auto w_at = [&](int t) { return reinterpret_cast<pair*>(sm + Sh::oW + (t * (N + 4) + c) * 4); };
-    if (role == 0) {
+    // All that a role reads is read before it writes: the compiler cannot tell that what is written lies elsewhere, and would wait for each read in turn.
+    const int t0 = role == 0 || role == 3 ? 0 : kHalf;
+    pair x[kHalf], l[kHalf], w[kHalf], s = ones(), q = ones();
+    if (!kStateOnly || role >= 2) {
+#pragma unroll
+      for (int t = 0; t < kHalf; ++t)
+        x[t] = load2(reinterpret_cast<const T*>(st + (role < 2 ? 0 : Sh::kRaw) + (t0 + t) * Sh::kRawPitch) + c);
+    }
+#pragma unroll
+    for (int t = 0; t < kHalf; ++t) l[t] = decay2(lw, t0 + t, c);
+    if (role & 1) {            // the decays of the other half
+      s = decay2(lw, kHalf - t0, c);
+#pragma unroll
+      for (int t = 1; t < kHalf; ++t) s = add2(s, decay2(lw, kHalf - t0 + t, c));
+    }
+#pragma unroll
+    for (int t = 0; t < kHalf; ++t) w[t] = exp2_(l[t]);
+    uint8_t* const to = sm + t0 * Sh::kPitch + c * 2;
+    if (role < 2) {
+      if (role == 1) {
+        pair all = s;
+#pragma unroll
+        for (int t = 0; t < kHalf; ++t) all = add2(all, l[t]);
+        // the state's decay, over and over the same where decays do not change: the accurate exponential of the sum
+        const float2 f = both(all);
+        *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(f.x), expf(f.y));
+        if (kStateOnly) total = add2(total, all);
+      }
       if (!kStateOnly) {
-        pair q = ones();
+        const pair d = role == 1 ? exp2_(s) : s;
 #pragma unroll
         for (int t = 0; t < kHalf; ++t) {
-          const pair w = exp2_(decay2(lw, t, c));
-          *w_at(t) = w;
-          store_split<Sh::R>(sm + Sh::oRt + t * Sh::kPitch + c * 2, Sh::kTerm, mul2(raw(0, t), q));
-          q = mul2(q, w);
+          *reinterpret_cast<pair*>(sm + Sh::oW + ((t0 + t) * (N + 4) + c) * 4) = w[t];
+          pair m = mul2(x[t], q);
+          if (role == 1) {
+            store_split<Sh::R>(to + Sh::oRp + (t - kHalf) * Sh::kPitch, Sh::kHalfTerm, m);
+            m = mul2(m, d);
+          }
+          store_split<Sh::R>(to + Sh::oRt + t * Sh::kPitch, Sh::kTerm, m);
+          q = mul2(q, w[t]);
         }
-      }
-    } else if (role == 1) {
-      pair s = decay2(lw, 0, c), q = ones();
-#pragma unroll
-      for (int t = 1; t < kHalf; ++t) s = add2(s, decay2(lw, t, c));
-      const pair d1 = exp2_(s);
-#pragma unroll
-      for (int t = kHalf; t < kChunk; ++t) {
-        const pair l = decay2(lw, t, c);
-        s = add2(s, l);
-        if (!kStateOnly) {
-          const pair w = exp2_(l), m = mul2(raw(0, t), q);
-          *w_at(t) = w;
-          store_split<Sh::R>(sm + Sh::oRp + (t - kHalf) * Sh::kPitch + c * 2, Sh::kHalfTerm, m);
-          store_split<Sh::R>(sm + Sh::oRt + t * Sh::kPitch + c * 2, Sh::kTerm, mul2(m, d1));
-          q = mul2(q, w);
-        }
-      }
-      // the state's decay, over and over the same where decays do not change: the accurate exponential of the sum
-      const float2 f = both(s);
-      *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(f.x), expf(f.y));
-      if (kStateOnly) total = add2(total, s);
-    } else if (role == 2) {
-      pair q = ones();
-#pragma unroll
-      for (int t = kChunk - 1; t >= kHalf; --t) {
-        store_split<K3>(sm + Sh::oKt + t * Sh::kPitch + c * 2, Sh::kTerm, mul2(raw(1, t), q));
-        q = mul2(q, exp2_(decay2(lw, t, c)));
       }
     } else {
-      pair s = decay2(lw, kHalf, c), q = ones();
-#pragma unroll
-      for (int t = kHalf + 1; t < kChunk; ++t) s = add2(s, decay2(lw, t, c));
-      const pair d2 = exp2_(s);
+      const pair d = role == 3 ? exp2_(s) : s;
 #pragma unroll
       for (int t = kHalf - 1; t >= 0; --t) {
-        const pair m = mul2(raw(1, t), q);
-        if (!kStateOnly) store_split<Sh::R>(sm + Sh::oKp + t * Sh::kPitch + c * 2, Sh::kHalfTerm, m);
-        store_split<K3>(sm + Sh::oKt + t * Sh::kPitch + c * 2, Sh::kTerm, mul2(m, d2));
-        q = mul2(q, exp2_(decay2(lw, t, c)));
+        pair m = mul2(x[t], q);
+        if (role == 3) {
+          if (!kStateOnly) store_split<Sh::R>(to + Sh::oKp + t * Sh::kPitch, Sh::kHalfTerm, m);
+          m = mul2(m, d);
+        }
+        store_split<K3>(to + Sh::oKt + t * Sh::kPitch, Sh::kTerm, m);
+        q = mul2(q, w[t]);
       }
     }
     if (Sh::V > 2 && (role & 1) == 0) {       // the warps with less to do
-      const int t0 = role == 0 ? 0 : kHalf;
 #pragma unroll
-      for (int t = 0; t < kHalf; ++t) store_split<Sh::V>(sm + Sh::oVt + (t0 + t) * Sh::kPitch + c * 2, Sh::kTerm, raw(2, t0 + t));
+      for (int t = 0; t < kHalf; ++t) x[t] = load2(reinterpret_cast<const T*>(st + 2 * Sh::kRaw + (t0 + t) * Sh::kRawPitch) + c);
+#pragma unroll
+      for (int t = 0; t < kHalf; ++t) store_split<Sh::V>(to + Sh::oVt + t * Sh::kPitch, Sh::kTerm, x[t]);
     }
   }
 
