@@ -153,8 +153,7 @@ struct Shape {
   // a raw stage: r, k, v, logarithms of decays
   static constexpr int kStage = 3 * kRaw + kChunk * kDecayPitch;
   static constexpr int oRt = 2 * kStage, oKt = oRt + R * kTerm, oRp = oKt + K3 * kTerm, oKp = oRp + R * kHalfTerm, oVt = oKp + R * kHalfTerm;
-  static constexpr int oW = oVt + (V > 2 ? V * kTerm : 0), oD = oW + kChunk * (N + 4) * 4, oA = oD + N * 4, oMid = oA + (N / 64) * 2 * 64 * 4, oU = oMid + kSteps * 64 * 4;
-  static constexpr int kBytes = oU + N * 4;
+  static constexpr int oD = oVt + (V > 2 ? V * kTerm : 0), oA = oD + N * 4, kTriangles = (N / 64) * 2 * 64 * 4, oMid = oA + 2 * kTriangles, kBytes = oMid + kSteps * 64 * 4;
   static constexpr int kStateFloats = N * N, kBlockFloats = 2 * N * N + N;
 };
 
@@ -232,8 +231,16 @@ struct Worker {
   static constexpr int kPieces = N * (int)sizeof(T) / 16, kRowsAtOnce = Sh::kThreads / kPieces;
   static constexpr int kDecaySize = kDecay == DECAY_F32 ? 4 : (int)sizeof(T), kDecayPieces = N * kDecaySize / 16, kDecayRowsAtOnce = Sh::kThreads / kDecayPieces;
   const uint8_t *rp, *kp, *vp, *lp;
+  pair bonus;                  // u of this thread's channels
+  int place, place2;           // bytes into a triangle of A of the entries that this lane ends up with
 
-  __device__ __forceinline__ Worker(const Args& p_, uint8_t* sm_) : p(p_), sm(sm_), h(blockIdx.y), warp(threadIdx.x >> 5), lane(threadIdx.x & 31), tid(threadIdx.x) {}
+  __device__ __forceinline__ Worker(const Args& p_, uint8_t* sm_) : p(p_), sm(sm_), h(blockIdx.y), warp(threadIdx.x >> 5), lane(threadIdx.x & 31), tid(threadIdx.x) {
+    if (kStateOnly) return;
+    const int set = (warp & 3) < 2 ? 0 : 1, c = (warp >> 2) * 64 + lane * 2;
+    place = entry(set, lane >> 1) * 4;
+    place2 = entry(set, 16 + (lane & 1)) * 4;
+    bonus = p.a.u ? load2(p.a.u + h * N + c) : ones();
+  }
 
   __device__ __forceinline__ void fetch_from(int t0) {
     const rwkvq_linattn_args& a = p.a;
@@ -280,6 +287,40 @@ struct Worker {
     return kDecay == DECAY_F32 ? load2(reinterpret_cast<const float*>(row) + c) : load2(reinterpret_cast<const T*>(row) + c);
   }
 
+  // Entry number i of 18 of a set of columns: (t, s).  Constant where i and the set are.
+  static __device__ __forceinline__ int entry(int set, int i) {
+    constexpr int kFirst[2][4] = {{0, 3, 5, 6}, {1, 2, 4, 7}};
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int s = kFirst[set][j], len = kHalf - s;          // the diagonal first
+      if (i < n + len) return (s + i - n) * 8 + s;
+      n += len;
+    }
+    return 0;
+  }
+  // This lane's part (two channels) of the entries of a set.
+  template <int set>
+  __device__ __forceinline__ void entries(const pair (&r)[kHalf], const pair (&k)[kHalf], const pair (&w)[kHalf], float (&v)[18]) const {
+    constexpr int kFirst[2][4] = {{0, 3, 5, 6}, {1, 2, 4, 7}};
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int s = kFirst[set][j];
+      pair x = k[s];
+      {
+        const float2 f = both(mul2(mul2(r[s], bonus), x));
+        v[n++] = f.x + f.y;
+      }
+#pragma unroll
+      for (int t = s + 1; t < kHalf; ++t) {
+        const float2 f = both(mul2(r[t], x));
+        v[n++] = f.x + f.y;
+        if (t + 1 < kHalf) x = mul2(x, w[t]);
+      }
+    }
+  }
+
   // A stage's operands.  Warps of a group of four take: r of the first eight tokens, r of the last, k of the last, k of the first; a lane two channels.
   __device__ __forceinline__ void operands(int stage) {
     const uint8_t* st = sm + stage * Sh::kStage;
@@ -317,7 +358,6 @@ struct Worker {
         const pair d = role == 1 ? exp2_(s) : s;
 #pragma unroll
         for (int t = 0; t < kHalf; ++t) {
-          *reinterpret_cast<pair*>(sm + Sh::oW + ((t0 + t) * (N + 4) + c) * 4) = w[t];
           pair m = mul2(x[t], q);
           if (role == 1) {
             store_split<Sh::R>(to + Sh::oRp + (t - kHalf) * Sh::kPitch, Sh::kHalfTerm, m);
@@ -340,69 +380,46 @@ struct Worker {
         q = mul2(q, w[t]);
       }
     }
+    if (!kStateOnly) {
+      // The triangles of A: tokens 0-7 by roles 0 and 3, tokens 8-15 by 1 and 2, which have one of r and k and the decays in registers and read the other.
+      // Seven columns have entries below the diagonal, 7 - s each: the warps with r take s = 0, 3, 5, 6, those with k 1, 2, 4, fourteen entries either way,
+      // and four of the eight on the diagonal.
+      pair y[kHalf];
+#pragma unroll
+      for (int t = 0; t < kHalf; ++t)
+        y[t] = load2(reinterpret_cast<const T*>(st + (role < 2 ? Sh::kRaw : 0) + (t0 + t) * Sh::kRawPitch) + c);
+      float v[18];
+      if (role < 2) entries<0>(x, y, w, v);
+      else entries<1>(y, x, w, v);
+      // sixteen sums over the lanes, each step halves the values that a lane carries, and two more
+#pragma unroll
+      for (int d = 16, n = 8; d > 1; d >>= 1, n >>= 1) {
+        const bool up = (lane & d) != 0;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+          const float keep = up ? v[i + n] : v[i], send = up ? v[i] : v[i + n];
+          v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, d);
+        }
+      }
+      v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], 1);
+      {
+        const bool up = (lane & 1) != 0;
+        const float keep = up ? v[17] : v[16], send = up ? v[16] : v[17];
+        v[16] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, 1);
+      }
+#pragma unroll
+      for (int d = 16; d > 1; d >>= 1) v[16] += __shfl_xor_sync(0xFFFFFFFFu, v[16], d);
+      // lane 2 i holds entry i, lanes 0 and 1 the last two: where these are in A
+      uint8_t* A = sm + Sh::oA + stage * Sh::kTriangles + (warp >> 2) * 512 + (t0 >> 3) * 256;
+      if ((lane & 1) == 0) *reinterpret_cast<float*>(A + place) = v[0];
+      if (lane < 2) *reinterpret_cast<float*>(A + place2) = v[16];
+    }
     if (Sh::V > 2 && (role & 1) == 0) {       // the warps with less to do
 #pragma unroll
       for (int t = 0; t < kHalf; ++t) x[t] = load2(reinterpret_cast<const T*>(st + 2 * Sh::kRaw + (t0 + t) * Sh::kRawPitch) + c);
 #pragma unroll
       for (int t = 0; t < kHalf; ++t) store_split<Sh::V>(to + Sh::oVt + t * Sh::kPitch, Sh::kTerm, x[t]);
     }
-  }
-
-  // The triangles of A: lanes 0-15 tokens 0-7, the others tokens 8-15, four channels each.  Warp w of a group of four takes columns s = w and 7 - w,
-  // together seven entries below the diagonal (and the two on it), whatever w.
-  __device__ __forceinline__ void triangles(int stage) {
-    const int w = warp & 3, t0 = (lane >> 4) * kHalf, c = (warp >> 2) * 64 + (lane & 15) * 4, first = 7 - w;
-    const uint8_t* rr = sm + stage * Sh::kStage + t0 * Sh::kRawPitch + c * (int)sizeof(T);
-    const uint8_t* ww = sm + Sh::oW + (t0 * (N + 4) + c) * 4;
-    auto row4 = [&](const uint8_t* at, int t, pair (&v)[2]) { load4(reinterpret_cast<const T*>(at + t * Sh::kRawPitch), v); };
-    auto dot = [](const pair (&a)[2], const pair (&b)[2]) { const float2 f = both(fma2(a[1], b[1], mul2(a[0], b[0]))); return f.x + f.y; };
-    pair x[2], x2[2], r[2], u[2];
-    float v[8], last;
-    row4(rr + Sh::kRaw, w, x);
-    row4(rr + Sh::kRaw, first, x2);
-    load4(reinterpret_cast<const float*>(sm + Sh::oU) + c, u);
-    {
-      pair ru[2];
-      row4(rr, w, r);
-      ru[0] = mul2(r[0], u[0]); ru[1] = mul2(r[1], u[1]);
-      v[7] = dot(ru, x);
-      row4(rr, first, r);
-      ru[0] = mul2(r[0], u[0]); ru[1] = mul2(r[1], u[1]);
-      last = dot(ru, x2);
-    }
-    // j < first: t = w + 1 + j of column w, then t = j + 1 of column 7 - w; first is at least 4
-    const uint8_t *rw = rr + w * Sh::kRawPitch, *wx = ww + w * ((N + 4) * 4);
-#pragma unroll
-    for (int j = 0; j < 7; ++j) {
-      if (j >= 4 && j == first) { x[0] = x2[0]; x[1] = x2[1]; rw = rr; wx = ww; }
-      pair wt[2];
-      row4(rw, j + 1, r);
-      v[j] = dot(r, x);
-      if (j < 6) {
-        load4(reinterpret_cast<const float*>(wx + (j + 1) * ((N + 4) * 4)), wt);
-        x[0] = mul2(x[0], wt[0]); x[1] = mul2(x[1], wt[1]);
-      }
-    }
-    // eight sums over sixteen lanes: each step halves the values a lane carries
-#pragma unroll
-    for (int d = 8, n = 4; d > 1; d >>= 1, n >>= 1) {
-      const bool up = (lane & d) != 0;
-#pragma unroll
-      for (int i = 0; i < n; ++i) {
-        const float keep = up ? v[i + n] : v[i], send = up ? v[i] : v[i + n];
-        v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, d);
-      }
-    }
-    v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], 1);
-#pragma unroll
-    for (int d = 8; d > 0; d >>= 1) last += __shfl_xor_sync(0xFFFFFFFFu, last, d);
-    float* A = reinterpret_cast<float*>(sm + Sh::oA) + (warp >> 2) * 128 + (lane >> 4) * 64;
-    if ((lane & 1) == 0) {
-      const int j = ((lane >> 3) & 1) * 4 + ((lane >> 2) & 1) * 2 + ((lane >> 1) & 1);
-      const int s = j == 7 ? w : j < first ? w : first, t = j == 7 ? w : j < first ? w + 1 + j : j + 1;
-      A[t * 8 + s] = v[0];
-    }
-    if ((lane & 15) == 1) A[first * 8 + first] = last;
   }
 
   // Chunks of rows [t, end), t + 16, ...
@@ -421,7 +438,6 @@ struct Worker {
       const int t0 = begin + i * kChunk;
       float o[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
       if (!kStateOnly) {
-        triangles(i & 1);
         {
           // the block of A below the triangles: warp w adds up sixteen keys.  Rows of r P' (lanes 0-15) and of k Q' (16-31), eight keys and the next
           float mid[4] = {0.f, 0.f, 0.f, 0.f};
@@ -505,7 +521,7 @@ struct Worker {
       __syncthreads();
       if (i + 2 < n) fetch(i & 1, end - t0 - 2 * kChunk);
       if (!kStateOnly) {
-        const float* A = reinterpret_cast<const float*>(sm + Sh::oA) + g * 8 + q * 2;
+        const float* A = reinterpret_cast<const float*>(sm + Sh::oA + (i & 1) * Sh::kTriangles) + g * 8 + q * 2;
         float2 up = *reinterpret_cast<const float2*>(A), dn = *reinterpret_cast<const float2*>(A + 64);
 #pragma unroll
         for (int x = 1; x < N / 64; ++x) {
@@ -606,8 +622,7 @@ __global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? kPerSm : 1)
   Worker<T, N, kDecay, kStateOnly> w(p, smem);
   const int block = blockIdx.x, row0 = block * p.block_rows, row1 = min(row0 + p.block_rows, p.a.tokens);
   if (!kStateOnly) {
-    for (int i = threadIdx.x; i < (N / 64) * 128; i += Sh::kThreads) reinterpret_cast<float*>(smem + Sh::oA)[i] = 0.f;       // above the diagonals it stays zero
-    for (int i = threadIdx.x; i < N; i += Sh::kThreads) reinterpret_cast<float*>(smem + Sh::oU)[i] = p.a.u ? p.a.u[w.h * N + i] : 1.f;
+    for (int i = threadIdx.x; i < 2 * Sh::kTriangles / 4; i += Sh::kThreads) reinterpret_cast<float*>(smem + Sh::oA)[i] = 0.f;       // above the diagonals it stays zero
   }
   for (int seq = 0;; ++seq) {
     Entry e = {0, p.a.tokens, 0, 0};
