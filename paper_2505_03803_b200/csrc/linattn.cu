@@ -321,6 +321,44 @@ struct Worker {
     }
   }
 
+  // Without outputs only k Q is needed: a warp of a group of four takes four tokens (the last first, as the sums of the decays behind them are longer).
+  __device__ __forceinline__ void state_operands(int stage) {
+    constexpr int kQuarter = 4;
+    const uint8_t* st = sm + stage * Sh::kStage;
+    const uint8_t* lw = st + 3 * Sh::kRaw;
+    const int c = (warp >> 2) * 64 + lane * 2, t0 = (3 - (warp & 3)) * kQuarter;
+    pair x[kQuarter], l[kQuarter], s = pair_of(0.f, 0.f);
+#pragma unroll
+    for (int t = 0; t < kQuarter; ++t) {
+      x[t] = load2(reinterpret_cast<const T*>(st + Sh::kRaw + (t0 + t) * Sh::kRawPitch) + c);
+      l[t] = decay2(lw, t0 + t, c);
+    }
+#pragma unroll
+    for (int t = kQuarter; t < kChunk; ++t)
+      if (t >= t0 + kQuarter) s = add2(s, decay2(lw, t, c));
+    uint8_t* const to = sm + t0 * Sh::kPitch + c * 2;
+    pair v[kQuarter];
+    if (Sh::V > 2) {
+#pragma unroll
+      for (int t = 0; t < kQuarter; ++t) v[t] = load2(reinterpret_cast<const T*>(st + 2 * Sh::kRaw + (t0 + t) * Sh::kRawPitch) + c);
+    }
+    // exponentials of sums, not products of exponentials: they do not wait for one another
+#pragma unroll
+    for (int t = kQuarter - 1; t >= 0; --t) {
+      store_split<K3>(to + Sh::oKt + t * Sh::kPitch, Sh::kTerm, mul2(x[t], exp2_(s)));
+      s = add2(s, l[t]);
+    }
+    if (Sh::V > 2) {
+#pragma unroll
+      for (int t = 0; t < kQuarter; ++t) store_split<Sh::V>(to + Sh::oVt + t * Sh::kPitch, Sh::kTerm, v[t]);
+    }
+    if (t0 == 0) {
+      const float2 f = both(s);
+      *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(f.x), expf(f.y));
+      total = add2(total, s);
+    }
+  }
+
   // A stage's operands.  Warps of a group of four take: r of the first eight tokens, r of the last, k of the last, k of the first; a lane two channels.
   __device__ __forceinline__ void operands(int stage) {
     const uint8_t* st = sm + stage * Sh::kStage;
@@ -329,11 +367,9 @@ struct Worker {
     // All that a role reads is read before it writes: the compiler cannot tell that what is written lies elsewhere, and would wait for each read in turn.
     const int t0 = role == 0 || role == 3 ? 0 : kHalf;
     pair x[kHalf], l[kHalf], w[kHalf], s = ones(), q = ones();
-    if (!kStateOnly || role >= 2) {
 #pragma unroll
-      for (int t = 0; t < kHalf; ++t)
-        x[t] = load2(reinterpret_cast<const T*>(st + (role < 2 ? 0 : Sh::kRaw) + (t0 + t) * Sh::kRawPitch) + c);
-    }
+    for (int t = 0; t < kHalf; ++t)
+      x[t] = load2(reinterpret_cast<const T*>(st + (role < 2 ? 0 : Sh::kRaw) + (t0 + t) * Sh::kRawPitch) + c);
 #pragma unroll
     for (int t = 0; t < kHalf; ++t) l[t] = decay2(lw, t0 + t, c);
     if (role & 1) {            // the decays of the other half
@@ -352,20 +388,17 @@ struct Worker {
         // the state's decay, over and over the same where decays do not change: the accurate exponential of the sum
         const float2 f = both(all);
         *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(f.x), expf(f.y));
-        if (kStateOnly) total = add2(total, all);
       }
-      if (!kStateOnly) {
-        const pair d = role == 1 ? exp2_(s) : s;
+      const pair d = role == 1 ? exp2_(s) : s;
 #pragma unroll
-        for (int t = 0; t < kHalf; ++t) {
-          pair m = mul2(x[t], q);
-          if (role == 1) {
-            store_split<Sh::R>(to + Sh::oRp + (t - kHalf) * Sh::kPitch, Sh::kHalfTerm, m);
-            m = mul2(m, d);
-          }
-          store_split<Sh::R>(to + Sh::oRt + t * Sh::kPitch, Sh::kTerm, m);
-          q = mul2(q, w[t]);
+      for (int t = 0; t < kHalf; ++t) {
+        pair m = mul2(x[t], q);
+        if (role == 1) {
+          store_split<Sh::R>(to + Sh::oRp + (t - kHalf) * Sh::kPitch, Sh::kHalfTerm, m);
+          m = mul2(m, d);
         }
+        store_split<Sh::R>(to + Sh::oRt + t * Sh::kPitch, Sh::kTerm, m);
+        q = mul2(q, w[t]);
       }
     } else {
       const pair d = role == 3 ? exp2_(s) : s;
@@ -373,14 +406,14 @@ struct Worker {
       for (int t = kHalf - 1; t >= 0; --t) {
         pair m = mul2(x[t], q);
         if (role == 3) {
-          if (!kStateOnly) store_split<Sh::R>(to + Sh::oKp + t * Sh::kPitch, Sh::kHalfTerm, m);
+          store_split<Sh::R>(to + Sh::oKp + t * Sh::kPitch, Sh::kHalfTerm, m);
           m = mul2(m, d);
         }
         store_split<K3>(to + Sh::oKt + t * Sh::kPitch, Sh::kTerm, m);
         q = mul2(q, w[t]);
       }
     }
-    if (!kStateOnly) {
+    {
       // The triangles of A: tokens 0-7 by roles 0 and 3, tokens 8-15 by 1 and 2, which have one of r and k and the decays in registers and read the other.
       // Seven columns have entries below the diagonal, 7 - s each: the warps with r take s = 0, 3, 5, 6, those with k 1, 2, 4, fourteen entries either way,
       // and four of the eight on the diagonal.
@@ -422,18 +455,22 @@ struct Worker {
     }
   }
 
-  // Chunks of rows [t, end), t + 16, ...
-  __device__ __forceinline__ void rows(int begin, int end) {
-    const rwkvq_linattn_args& a = p.a;
-    const int n = (end - begin + kChunk - 1) / kChunk, g = lane >> 2, q = lane & 3;
+  // Chunks of rows [begin, end): what comes before the state is needed, and the rest.
+  __device__ __forceinline__ void first_rows(int begin, int end) {
+    const int n = (end - begin + kChunk - 1) / kChunk;
     fetch_from(begin);
     fetch(0, end - begin);
     if (n > 1) fetch(1, end - begin - kChunk);
     if (n > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
     else asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
-    operands(0);
+    if (kStateOnly) state_operands(0);
+    else operands(0);
     __syncthreads();
+  }
+  __device__ __forceinline__ void rows(int begin, int end) {
+    const rwkvq_linattn_args& a = p.a;
+    const int n = (end - begin + kChunk - 1) / kChunk, g = lane >> 2, q = lane & 3;
     for (int i = 0; i < n; ++i) {
       const int t0 = begin + i * kChunk;
       float o[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -561,7 +598,10 @@ struct Worker {
           }
         }
       }
-      if (i + 1 < n) operands((i + 1) & 1);
+      if (i + 1 < n) {
+        if (kStateOnly) state_operands((i + 1) & 1);
+        else operands((i + 1) & 1);
+      }
       __syncthreads();
     }
   }
@@ -628,13 +668,15 @@ __global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? kPerSm : 1)
     Entry e = {0, p.a.tokens, 0, 0};
     if (p.entries) {
       seq = next_sequence(p, seq, row0, row1, &word);
-      if (seq >= p.a.n_seq) return;
+      if (seq >= p.a.n_seq) break;
       e = p.entries[seq];
     } else if (seq > 0) {
-      return;
+      break;
     }
     const int begin = max(e.start, row0), end = min(e.end, row1);
     if (kStateOnly) {
+      // the blocks' pass may begin as soon as there is room for it: it waits for this one where it needs the states
+      asm volatile("griddepcontrol.launch_dependents;");
       if (e.end <= row1) continue;
       if (e.start >= row0) {
         w.load_state(e.slot);
@@ -646,20 +688,24 @@ __global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? kPerSm : 1)
           for (int i = 0; i < 4; ++i) w.S[j][i] = 0.f;
       }
       w.total = pair_of(0.f, 0.f);
+      w.first_rows(begin, end);
       w.rows(begin, end);
       w.keep(w.block_state(block, 0));
-      if ((w.warp & 3) == 1) {
+      if ((w.warp & 3) == 3) {
         const float2 f = both(w.total);
         *reinterpret_cast<float2*>(w.block_state(block, 2) + (w.warp >> 2) * 64 + w.lane * 2) = make_float2(expf(f.x), expf(f.y));
       }
       return;
     }
+    w.first_rows(begin, end);
     if (e.start < row0 || e.end > row1) {
+      asm volatile("griddepcontrol.wait;" ::: "memory");
       // from the workspace: what the sequence began with, or what the blocks before this one make of it
       const int b0 = e.start >= row0 ? block : e.start / p.block_rows;
       const float* from = w.block_state(b0, e.start >= row0 ? 1 : 0);
 #pragma unroll
       for (int j = 0; j < Sh::kTiles; ++j) { const float4 x = w.kept(from, j); w.S[j][0] = x.x; w.S[j][1] = x.y; w.S[j][2] = x.z; w.S[j][3] = x.w; }
+#pragma unroll 2
       for (int b = b0 + 1; b < block; ++b) {
         const float* add = w.block_state(b, 0);
         const float* decay = w.block_state(b, 2) + (w.lane & 3) * 2;
@@ -675,8 +721,10 @@ __global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? kPerSm : 1)
       w.load_state(e.slot);
     }
     w.rows(begin, end);
+    asm volatile("griddepcontrol.wait;" ::: "memory");      // a state may be written where the pass before read it
     if (e.end <= row1 && p.a.state_out && e.slot >= 0) w.store_state(e.slot);
   }
+  if (!kStateOnly) asm volatile("griddepcontrol.wait;" ::: "memory");      // a block without rows does not end before the pass in front of it, either
 }
 
 // Rows of a block and how many blocks.  A block's warps work on one head; about four thread blocks fit an SM.
@@ -710,8 +758,13 @@ cudaError_t launch_chunks(const Args& p, const Plan& l, cudaStream_t s) {
     }
   }
   if (e != cudaSuccess) return e;
-  linattn_chunk_kernel<T, N, kDecay, false><<<dim3((unsigned)l.blocks, (unsigned)p.a.heads), Sh::kThreads, Sh::kBytes, s>>>(p);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)l.blocks, (unsigned)p.a.heads); cfg.blockDim = dim3(Sh::kThreads); cfg.dynamicSmemBytes = Sh::kBytes; cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = l.blocks > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, linattn_chunk_kernel<T, N, kDecay, false>, p);
 }
 template <typename T, int N>
 cudaError_t launch_n(const Args& p, const Plan& l, cudaStream_t s) {
