@@ -62,17 +62,22 @@ unsigned long long context_id();
 
 // The opt-in to more than 48 KB of dynamic shared memory holds for a kernel as long as the context: it is asked for once (about 1 us of host
 // time) and not at every launch.  One object per kernel, `bytes` the same at every call.  `wide`: clusters of more than eight blocks as well.
+// kCarveOut: as much of an SM's memory as there is for shared memory, as kernels do that follow one another without a gap: an SM changes that division only when it
+// is empty, so that a kernel which asks for another one waits for the last block of the one before.
+enum SmemCarveOut { kCarveOut };
 struct SmemOptIn {
   std::atomic<unsigned long long> context[kMaxDevices];      // in which it was asked for
-  const bool wide = false;
+  const bool wide = false, carve_out = false;
   SmemOptIn() = default;
   explicit SmemOptIn(bool wide_clusters) : context{}, wide(wide_clusters) {}
+  explicit SmemOptIn(SmemCarveOut) : context{}, carve_out(true) {}
   cudaError_t operator()(const void* fn, int bytes) {
     const int dev = current_device();
     const unsigned long long id = dev >= 0 ? context_id() : 0ull;
     if (id != 0 && context[dev].load(std::memory_order_relaxed) == id) return cudaSuccess;
     cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e == cudaSuccess && wide) e = cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && carve_out) e = cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e == cudaSuccess && id != 0) context[dev].store(id, std::memory_order_relaxed);
     return e;
   }

@@ -143,17 +143,19 @@ template <> struct Terms<__half> { static constexpr int R = 2, V = 2; };
 template <> struct Terms<float> { static constexpr int R = 3, V = 3; };
 constexpr int kChunk = 16, kHalf = 8, K3 = 3;
 
-template <typename T, int N>
+template <typename T, int N, bool kStateOnly>
 struct Shape {
   static constexpr int kThreads = 2 * N, kTiles = N / 8, kSteps = N / 16;
   static constexpr int R = Terms<T>::R, V = Terms<T>::V;
   static constexpr int kPitch = (N + 8) * 2;                      // bytes of a row of terms: an odd number of 16 bytes, no conflicts for ldmatrix
   static constexpr int kRawPitch = N * (int)sizeof(T) + 16, kDecayPitch = N * 4 + 16;
   static constexpr int kTerm = kChunk * kPitch, kHalfTerm = kHalf * kPitch, kRaw = kChunk * kRawPitch;
-  // a raw stage: r, k, v, logarithms of decays
-  static constexpr int kStage = 3 * kRaw + kChunk * kDecayPitch;
-  static constexpr int oRt = 2 * kStage, oKt = oRt + R * kTerm, oRp = oKt + K3 * kTerm, oKp = oRp + R * kHalfTerm, oVt = oKp + R * kHalfTerm;
-  static constexpr int oD = oVt + (V > 2 ? V * kTerm : 0), oA = oD + N * 4, kTriangles = (N / 64) * 2 * 64 * 4, oMid = oA + 2 * kTriangles, kBytes = oMid + kSteps * 64 * 4;
+  // a raw stage: r (where there are outputs), k, v, logarithms of decays
+  static constexpr int kR = 0, kK = kStateOnly ? 0 : kRaw, kV = kK + kRaw, kL = kV + kRaw, kStage = kL + kChunk * kDecayPitch;
+  static constexpr int oKt = 2 * kStage, oD = oKt + K3 * kTerm, oVt = oD + N * 4, oRt = oVt + (V > 2 ? V * kTerm : 0);
+  // what only outputs need
+  static constexpr int oRp = oRt + R * kTerm, oKp = oRp + R * kHalfTerm, oA = oKp + R * kHalfTerm;
+  static constexpr int kTriangles = (N / 64) * 2 * 64 * 4, oMid = oA + 2 * kTriangles, kBytes = kStateOnly ? oRt : oMid + kSteps * 64 * 4;
   static constexpr int kStateFloats = N * N, kBlockFloats = 2 * N * N + N;
 };
 
@@ -186,7 +188,14 @@ __device__ __forceinline__ float2 both(pair v) {
 __device__ __forceinline__ pair mul2(pair a, pair b) { pair d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 __device__ __forceinline__ pair add2(pair a, pair b) { pair d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 __device__ __forceinline__ pair fma2(pair a, pair b, pair c) { pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
-__device__ __forceinline__ pair exp2_(pair l) { const float2 f = both(l); return pair_of(__expf(f.x), __expf(f.y)); }
+// e^l of both.  Below 2^-126 it is zero (a decay of that size leaves nothing; keeping subnormal numbers takes four more instructions each).
+__device__ __forceinline__ pair exp_both(pair l) {
+  const float2 f = both(mul2(l, pair_of(1.4426950408889634f, 1.4426950408889634f)));
+  float x, y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(f.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(f.y));
+  return pair_of(x, y);
+}
 __device__ __forceinline__ pair ones() { return pair_of(1.f, 1.f); }
 __device__ __forceinline__ pair load2(const float* p) { return *reinterpret_cast<const pair*>(p); }
 __device__ __forceinline__ pair widen(uint32_t v, __half) { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v)); return pair_of(f.x, f.y); }
@@ -221,7 +230,7 @@ enum { DECAY_F32 = 0, DECAY_SAME = 1, DECAY_HEAD = 2 };
 
 template <typename T, int N, int kDecay, bool kStateOnly>
 struct Worker {
-  using Sh = Shape<T, N>;
+  using Sh = Shape<T, N, kStateOnly>;
   const Args& p;
   uint8_t* sm;
   int h, warp, lane, tid;
@@ -261,11 +270,11 @@ struct Worker {
       const bool there = tid / kPieces + i * kRowsAtOnce < left;
       // a row that is not there is not read: the address is one that is
       if (!kStateOnly) cp_async16(dst + i * kRowsAtOnce * Sh::kRawPitch, there ? rp : static_cast<const uint8_t*>(a.r), there);
-      cp_async16(dst + i * kRowsAtOnce * Sh::kRawPitch + Sh::kRaw, there ? kp : static_cast<const uint8_t*>(a.k), there);
-      cp_async16(dst + i * kRowsAtOnce * Sh::kRawPitch + 2 * Sh::kRaw, there ? vp : static_cast<const uint8_t*>(a.v), there);
+      cp_async16(dst + i * kRowsAtOnce * Sh::kRawPitch + Sh::kK, there ? kp : static_cast<const uint8_t*>(a.k), there);
+      cp_async16(dst + i * kRowsAtOnce * Sh::kRawPitch + Sh::kV, there ? vp : static_cast<const uint8_t*>(a.v), there);
       rp += a.r_row * rb; kp += a.k_row * rb; vp += a.v_row * rb;
     }
-    uint8_t* lw = sm + stage * Sh::kStage + 3 * Sh::kRaw;
+    uint8_t* lw = sm + stage * Sh::kStage + Sh::kL;
     if (kDecay == DECAY_HEAD) {
       const bool f32 = a.decay_dtype == RWKVQ_F32;
       if (tid < kChunk) reinterpret_cast<float*>(lw)[tid] = tid >= left ? 0.f : f32 ? *reinterpret_cast<const float*>(lp) : to_f32(*reinterpret_cast<const T*>(lp));
@@ -325,12 +334,12 @@ struct Worker {
   __device__ __forceinline__ void state_operands(int stage) {
     constexpr int kQuarter = 4;
     const uint8_t* st = sm + stage * Sh::kStage;
-    const uint8_t* lw = st + 3 * Sh::kRaw;
+    const uint8_t* lw = st + Sh::kL;
     const int c = (warp >> 2) * 64 + lane * 2, t0 = (3 - (warp & 3)) * kQuarter;
     pair x[kQuarter], l[kQuarter], s = pair_of(0.f, 0.f);
 #pragma unroll
     for (int t = 0; t < kQuarter; ++t) {
-      x[t] = load2(reinterpret_cast<const T*>(st + Sh::kRaw + (t0 + t) * Sh::kRawPitch) + c);
+      x[t] = load2(reinterpret_cast<const T*>(st + Sh::kK + (t0 + t) * Sh::kRawPitch) + c);
       l[t] = decay2(lw, t0 + t, c);
     }
 #pragma unroll
@@ -340,12 +349,12 @@ struct Worker {
     pair v[kQuarter];
     if (Sh::V > 2) {
 #pragma unroll
-      for (int t = 0; t < kQuarter; ++t) v[t] = load2(reinterpret_cast<const T*>(st + 2 * Sh::kRaw + (t0 + t) * Sh::kRawPitch) + c);
+      for (int t = 0; t < kQuarter; ++t) v[t] = load2(reinterpret_cast<const T*>(st + Sh::kV + (t0 + t) * Sh::kRawPitch) + c);
     }
     // exponentials of sums, not products of exponentials: they do not wait for one another
 #pragma unroll
     for (int t = kQuarter - 1; t >= 0; --t) {
-      store_split<K3>(to + Sh::oKt + t * Sh::kPitch, Sh::kTerm, mul2(x[t], exp2_(s)));
+      store_split<K3>(to + Sh::oKt + t * Sh::kPitch, Sh::kTerm, mul2(x[t], exp_both(s)));
       s = add2(s, l[t]);
     }
     if (Sh::V > 2) {
@@ -362,14 +371,14 @@ struct Worker {
   // A stage's operands.  Warps of a group of four take: r of the first eight tokens, r of the last, k of the last, k of the first; a lane two channels.
   __device__ __forceinline__ void operands(int stage) {
     const uint8_t* st = sm + stage * Sh::kStage;
-    const uint8_t* lw = st + 3 * Sh::kRaw;
+    const uint8_t* lw = st + Sh::kL;
     const int role = warp & 3, c = (warp >> 2) * 64 + lane * 2;
     // All that a role reads is read before it writes: the compiler cannot tell that what is written lies elsewhere, and would wait for each read in turn.
     const int t0 = role == 0 || role == 3 ? 0 : kHalf;
     pair x[kHalf], l[kHalf], w[kHalf], s = ones(), q = ones();
 #pragma unroll
     for (int t = 0; t < kHalf; ++t)
-      x[t] = load2(reinterpret_cast<const T*>(st + (role < 2 ? 0 : Sh::kRaw) + (t0 + t) * Sh::kRawPitch) + c);
+      x[t] = load2(reinterpret_cast<const T*>(st + (role < 2 ? Sh::kR : Sh::kK) + (t0 + t) * Sh::kRawPitch) + c);
 #pragma unroll
     for (int t = 0; t < kHalf; ++t) l[t] = decay2(lw, t0 + t, c);
     if (role & 1) {            // the decays of the other half
@@ -378,7 +387,7 @@ struct Worker {
       for (int t = 1; t < kHalf; ++t) s = add2(s, decay2(lw, kHalf - t0 + t, c));
     }
 #pragma unroll
-    for (int t = 0; t < kHalf; ++t) w[t] = exp2_(l[t]);
+    for (int t = 0; t < kHalf; ++t) w[t] = exp_both(l[t]);
     uint8_t* const to = sm + t0 * Sh::kPitch + c * 2;
     if (role < 2) {
       if (role == 1) {
@@ -389,7 +398,7 @@ struct Worker {
         const float2 f = both(all);
         *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(f.x), expf(f.y));
       }
-      const pair d = role == 1 ? exp2_(s) : s;
+      const pair d = role == 1 ? exp_both(s) : s;
 #pragma unroll
       for (int t = 0; t < kHalf; ++t) {
         pair m = mul2(x[t], q);
@@ -401,7 +410,7 @@ struct Worker {
         q = mul2(q, w[t]);
       }
     } else {
-      const pair d = role == 3 ? exp2_(s) : s;
+      const pair d = role == 3 ? exp_both(s) : s;
 #pragma unroll
       for (int t = kHalf - 1; t >= 0; --t) {
         pair m = mul2(x[t], q);
@@ -420,7 +429,7 @@ struct Worker {
       pair y[kHalf];
 #pragma unroll
       for (int t = 0; t < kHalf; ++t)
-        y[t] = load2(reinterpret_cast<const T*>(st + (role < 2 ? Sh::kRaw : 0) + (t0 + t) * Sh::kRawPitch) + c);
+        y[t] = load2(reinterpret_cast<const T*>(st + (role < 2 ? Sh::kK : Sh::kR) + (t0 + t) * Sh::kRawPitch) + c);
       float v[18];
       if (role < 2) entries<0>(x, y, w, v);
       else entries<1>(y, x, w, v);
@@ -449,7 +458,7 @@ struct Worker {
     }
     if (Sh::V > 2 && (role & 1) == 0) {       // the warps with less to do
 #pragma unroll
-      for (int t = 0; t < kHalf; ++t) x[t] = load2(reinterpret_cast<const T*>(st + 2 * Sh::kRaw + (t0 + t) * Sh::kRawPitch) + c);
+      for (int t = 0; t < kHalf; ++t) x[t] = load2(reinterpret_cast<const T*>(st + Sh::kV + (t0 + t) * Sh::kRawPitch) + c);
 #pragma unroll
       for (int t = 0; t < kHalf; ++t) store_split<Sh::V>(to + Sh::oVt + t * Sh::kPitch, Sh::kTerm, x[t]);
     }
@@ -520,7 +529,7 @@ struct Worker {
           for (int e = 0; e < Sh::V; ++e) ldsm4t(at + e * Sh::kTerm, v[e]);
         } else {
           uint32_t x[4];
-          ldsm4t(smem_u32(sm + (i & 1) * Sh::kStage + 2 * Sh::kRaw) + row * Sh::kRawPitch + col * 2, x);
+          ldsm4t(smem_u32(sm + (i & 1) * Sh::kStage + Sh::kV) + row * Sh::kRawPitch + col * 2, x);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             if constexpr (Sh::V == 1) v[0][j] = x[j];
@@ -650,13 +659,16 @@ __device__ __forceinline__ int next_sequence(const Args& p, int from, int row0, 
   return found;
 }
 
+#ifndef LA_PER_SM1
+#define LA_PER_SM1 5
+#endif
 #ifndef LA_PER_SM
 #define LA_PER_SM 4
 #endif
 constexpr int kPerSm = LA_PER_SM;
 template <typename T, int N, int kDecay, bool kStateOnly>
-__global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? kPerSm : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
-  using Sh = Shape<T, N>;
+__global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? (kStateOnly ? LA_PER_SM1 : kPerSm) : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
+  using Sh = Shape<T, N, kStateOnly>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int word;
   Worker<T, N, kDecay, kStateOnly> w(p, smem);
@@ -747,19 +759,20 @@ Plan plan_of(int tokens, int n_seq, int heads, int n) {
 
 template <typename T, int N, int kDecay>
 cudaError_t launch_chunks(const Args& p, const Plan& l, cudaStream_t s) {
-  using Sh = Shape<T, N>;
-  static SmemOptIn opt_state, opt_all;
-  cudaError_t e = opt_all((const void*)linattn_chunk_kernel<T, N, kDecay, false>, Sh::kBytes);
+  using All = Shape<T, N, false>;
+  using States = Shape<T, N, true>;
+  static SmemOptIn opt_state(kCarveOut), opt_all(kCarveOut);
+  cudaError_t e = opt_all((const void*)linattn_chunk_kernel<T, N, kDecay, false>, All::kBytes);
   if (e == cudaSuccess && l.blocks > 1) {
-    e = opt_state((const void*)linattn_chunk_kernel<T, N, kDecay, true>, Sh::kBytes);
+    e = opt_state((const void*)linattn_chunk_kernel<T, N, kDecay, true>, States::kBytes);
     if (e == cudaSuccess) {
-      linattn_chunk_kernel<T, N, kDecay, true><<<dim3((unsigned)l.blocks - 1, (unsigned)p.a.heads), Sh::kThreads, Sh::kBytes, s>>>(p);
+      linattn_chunk_kernel<T, N, kDecay, true><<<dim3((unsigned)l.blocks - 1, (unsigned)p.a.heads), States::kThreads, States::kBytes, s>>>(p);
       e = cudaGetLastError();
     }
   }
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)l.blocks, (unsigned)p.a.heads); cfg.blockDim = dim3(Sh::kThreads); cfg.dynamicSmemBytes = Sh::kBytes; cfg.stream = s;
+  cfg.gridDim = dim3((unsigned)l.blocks, (unsigned)p.a.heads); cfg.blockDim = dim3(All::kThreads); cfg.dynamicSmemBytes = All::kBytes; cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
