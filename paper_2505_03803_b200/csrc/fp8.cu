@@ -26,22 +26,38 @@ namespace f8 {
 using namespace tc5;
 
 // ---- quantizer --------------------------------------------------------------------------------------------
-__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
-  const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
 __device__ __forceinline__ float2 unpack2(uint32_t v, __half) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 __device__ __forceinline__ float2 unpack2(uint32_t v, __nv_bfloat16) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v)); }
+// Eight elements as they lie in memory: between the maximum and the codes they wait in as few registers as that takes.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
-  const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+struct Eight {
+  static constexpr int kWords = sizeof(T) * 2;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void zero() {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { const float2 v = unpack2(w[i], T()); f[2 * i] = v.x; f[2 * i + 1] = v.y; }
-}
+    for (int i = 0; i < kWords; ++i) w[i] = 0u;
+  }
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kWords / 4; ++i) {
+      const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+      w[4 * i] = a.x; w[4 * i + 1] = a.y; w[4 * i + 2] = a.z; w[4 * i + 3] = a.w;
+    }
+  }
+  __device__ __forceinline__ void floats(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) { f[2 * i] = __uint_as_float(w[2 * i]); f[2 * i + 1] = __uint_as_float(w[2 * i + 1]); }
+      else { const float2 v = unpack2(w[i], T()); f[2 * i] = v.x; f[2 * i + 1] = v.y; }
+    }
+  }
+};
 constexpr uint32_t kInfBits = 0x7F800000u;
 // Bits of the largest finite magnitude (as unsigned integers they sort like the numbers).
-__device__ __forceinline__ uint32_t amax8(const float (&f)[8]) {
+template <typename T>
+__device__ __forceinline__ uint32_t amax8(const Eight<T>& x) {
+  float f[8];
+  x.floats(f);
   uint32_t a = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) { const uint32_t b = __float_as_uint(f[i]) & 0x7FFFFFFFu; a = max(a, b < kInfBits ? b : 0u); }
@@ -55,7 +71,10 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
 }
 __device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }     // 1 <= byte <= 247
 // Infinities become NaN codes (the conversion alone would saturate them).
-__device__ __forceinline__ uint2 encode8(const float (&f)[8], float inv) {
+template <typename T>
+__device__ __forceinline__ uint2 encode8(const Eight<T>& e, float inv) {
+  float f[8];
+  e.floats(f);
   uint32_t h[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -75,21 +94,20 @@ __device__ __forceinline__ uint2 encode8(const float (&f)[8], float inv) {
 // Rows: a warp takes 256 columns per 16-byte load (16 lanes a group), four loads under way, and writes the eight scales together.
 constexpr int kRowWarps = 8, kRowChunks = 4, kRowCols = kRowChunks * 256;
 template <typename T>
-__global__ void __launch_bounds__(kRowWarps * 32) fp8_rows_kernel(const T* __restrict__ x, long long x_row, int rows, int cols, int pieces,
-                                                                 uint8_t* __restrict__ codes, uint8_t* __restrict__ scale, int pitch) {
+__global__ void __launch_bounds__(kRowWarps * 32) fp8_rows_kernel(const T* x, long long x_row, int rows, int cols, int pieces, uint8_t* codes,
+                                                                 uint8_t* scale, int pitch) {
   const long long unit = (long long)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   const long long row = unit / pieces;
-  if (row >= rows) return;
+  if (row >= rows) { asm volatile("griddepcontrol.wait;" ::: "memory"); return; }
   const int c0 = (int)(unit % pieces) * kRowCols + lane * 8;
-  float f[kRowChunks][8];
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  Eight<T> f[kRowChunks];
 #pragma unroll
   for (int j = 0; j < kRowChunks; ++j) {
-    if (c0 + j * 256 < cols) load8(x + row * x_row + c0 + j * 256, f[j]);
-    else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[j][i] = 0.f;
-    }
+    if (c0 + j * 256 < cols) f[j].load(x + row * x_row + c0 + j * 256);
+    else f[j].zero();
   }
   uint32_t lo = 0, hi = 0;
 #pragma unroll
@@ -110,23 +128,22 @@ __global__ void __launch_bounds__(kRowWarps * 32) fp8_rows_kernel(const T* __res
 // Blocks of 128 x 128: one thread block each, its elements in registers between the maximum and the codes.
 constexpr int kBlockThreads = 256;
 template <typename T>
-__global__ void __launch_bounds__(kBlockThreads) fp8_blocks_kernel(const T* __restrict__ x, long long x_row, int rows, int cols, int groups,
-                                                                  uint8_t* __restrict__ codes, uint8_t* __restrict__ scale, int pitch) {
+__global__ void __launch_bounds__(kBlockThreads, sizeof(T) == 2 ? 5 : 3) fp8_blocks_kernel(const T* x, long long x_row, int rows, int cols, int groups, uint8_t* codes,
+                                                                  uint8_t* scale, int pitch) {
   __shared__ uint32_t most[kBlockThreads / 32];
   const int g = (int)(blockIdx.x % (unsigned)groups), rb = (int)(blockIdx.x / (unsigned)groups);
   const int c = g * 128 + (threadIdx.x & 15) * 8;
   const long long r0 = (long long)rb * 128 + (threadIdx.x >> 4);
   constexpr int kSteps = 128 / (kBlockThreads / 16);
-  float f[kSteps][8];
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  Eight<T> f[kSteps];
   uint32_t a = 0;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const long long r = r0 + i * (kBlockThreads / 16);
-    if (r < rows && c < cols) load8(x + r * x_row + c, f[i]);
-    else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) f[i][k] = 0.f;
-    }
+    if (r < rows && c < cols) f[i].load(x + r * x_row + c);
+    else f[i].zero();
   }
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) a = max(a, amax8(f[i]));
@@ -148,20 +165,31 @@ __global__ void __launch_bounds__(kBlockThreads) fp8_blocks_kernel(const T* __re
 int blocks_of(int n) { return n / 128 + (n % 128 != 0); }
 size_t scale_pitch(int cols) { return round_up_sz((size_t)blocks_of(cols), 16); }
 
+// All launches here may begin while the kernel before them ends; the kernels wait for that end before they touch memory.
+cudaLaunchConfig_t launch_config(dim3 grid, int threads, uint32_t smem, cudaStream_t s, cudaLaunchAttribute (&attr)[2]) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cfg;
+}
+
 template <typename T>
 cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int block_rows, void* codes, void* scale, int pitch, cudaStream_t s) {
+  cudaLaunchAttribute attr[2];
   if (block_rows == 1) {
     const int pieces = cols / kRowCols + (cols % kRowCols != 0);
     const long long blocks = ((long long)rows * pieces + kRowWarps - 1) / kRowWarps;
-    fp8_rows_kernel<T><<<(unsigned)blocks, kRowWarps * 32, 0, s>>>(static_cast<const T*>(x), x_row, rows, cols, pieces, static_cast<uint8_t*>(codes),
-                                                                  static_cast<uint8_t*>(scale), pitch);
-  } else {
-    const int groups = blocks_of(cols);
-    const long long blocks = (long long)blocks_of(rows) * groups;
-    fp8_blocks_kernel<T><<<(unsigned)blocks, kBlockThreads, 0, s>>>(static_cast<const T*>(x), x_row, rows, cols, groups, static_cast<uint8_t*>(codes),
-                                                                   static_cast<uint8_t*>(scale), pitch);
+    const cudaLaunchConfig_t cfg = launch_config(dim3((unsigned)blocks), kRowWarps * 32, 0, s, attr);
+    return cudaLaunchKernelEx(&cfg, fp8_rows_kernel<T>, static_cast<const T*>(x), x_row, rows, cols, pieces, static_cast<uint8_t*>(codes),
+                              static_cast<uint8_t*>(scale), pitch);
   }
-  return cudaGetLastError();
+  const int groups = blocks_of(cols);
+  const long long blocks = (long long)blocks_of(rows) * groups;
+  const cudaLaunchConfig_t cfg = launch_config(dim3((unsigned)blocks), kBlockThreads, 0, s, attr);
+  return cudaLaunchKernelEx(&cfg, fp8_blocks_kernel<T>, static_cast<const T*>(x), x_row, rows, cols, groups, static_cast<uint8_t*>(codes),
+                            static_cast<uint8_t*>(scale), pitch);
 }
 
 // ---- product ----------------------------------------------------------------------------------------------
@@ -171,7 +199,7 @@ cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int blo
 // instructions, (2) scales, (3) tensor memory, (4-7) epilogue.  Two accumulators, so that a tile's epilogue runs under the next tile's sums.
 // Scales: four groups' bytes of a row are the word that the instruction picks its byte from; warp 2 deals the words of 512 columns out in the order
 // of the copy to tensor memory (32 lanes x 16 bytes, row r in line r % 32, word r / 32), where they lie once per 32-lane quarter.
-constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 8, kSfSlots = 2, kThreads = 256;
+constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 8, kSfSlots = 2, kMaxSlices = 8, kMinStages = 4, kThreads = 256;
 constexpr uint32_t kWBytes = kRows * kStageCols, kSfBytes = 512 + 1024, kSfCols = 16, kCtrlBytes = 512;
 constexpr uint32_t kMaxSmemBytes = 232448;
 
@@ -181,7 +209,7 @@ struct GemmArgs {
   const uint8_t* x_scale;
   void* Y;
   long long y_row;
-  int oc, M, groups, pitch, NT, MT, tiles, stages, y_dtype;
+  int oc, M, groups, pitch, NT, MT, tiles, stages, slices, y_dtype;
   uint32_t tmem_cols;
   int* status;
 };
@@ -242,7 +270,34 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, uint32_t tmem, int
   }
 }
 
-__global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A cluster's sums added up in the order of the slices: each block takes its share of the tokens, two at a time.
+template <typename T>
+__device__ __forceinline__ void add_slices(const GemmArgs& a, uint8_t* smem, int slice, int tile) {
+  const int mt = tile % a.MT, t0 = mt * a.NT, nt = min(a.NT, a.M - t0), i = threadIdx.x % kRows, row = tile / a.MT * kRows + i;
+  const int c1 = nt * (slice + 1) / a.slices;
+  for (int c = nt * slice / a.slices + (int)threadIdx.x / kRows; c < c1; c += kThreads / kRows) {
+    const uint32_t at = smem_u32(smem) + (uint32_t)(c * kRows + i) * 4u;
+    float v[kMaxSlices];
+#pragma unroll
+    for (int s = 0; s < kMaxSlices; ++s) {
+      if (s < a.slices) {
+        uint32_t peer;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(at), "r"(s));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[s]) : "r"(peer) : "memory");
+      }
+    }
+    float sum = v[0];
+#pragma unroll
+    for (int s = 1; s < kMaxSlices; ++s)
+      if (s < a.slices) sum += v[s];
+    if (row < a.oc) static_cast<T*>(a.Y)[(long long)(t0 + c) * a.y_row + row] = to_out<T>(sum);
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 2) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
   const uint32_t stage_bytes = kWBytes + (uint32_t)a.NT * kStageCols;
@@ -257,26 +312,32 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
     ctrl->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // Only now: tensor memory taken while an earlier kernel still wants some would be waited for by it, and it by this one.
   if (warp == 3) tmem_alloc(&ctrl->tmem_base, a.tmem_cols);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ctrl->tmem_base;
-  const int n_k = a.groups;
+  // A cluster of `slices` blocks has one tile, each a range of its columns (whole words of scales); without slices a block goes from tile to tile.
+  const int slice = a.slices > 1 ? (int)(blockIdx.x % (unsigned)a.slices) : 0, tile0 = (int)(blockIdx.x / (unsigned)a.slices);
+  const int step = a.slices > 1 ? a.tiles : (int)gridDim.x;
+  const int words = (a.groups + 3) / 4, k0 = words * slice / a.slices * 4, n_k = min(a.groups, words * (slice + 1) / a.slices * 4) - k0;
 
   if (warp == 0) {
     if (lane == 0) {
       int st = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+      for (int t = tile0; ok && t < a.tiles; t += step) {
         const int mt = t % a.MT, rb = t / a.MT;
         for (int k = 0; k < n_k; ++k) {
           if (!mbar_wait(&ctrl->empty[st], ph ^ 1u, abortp, a.status)) { ok = false; break; }
           uint8_t* w = smem + (uint32_t)st * stage_bytes;
           mbar_arrive_expect_tx(&ctrl->full[st], stage_bytes);
-          tensor_g2s(w, &a.wmap, k * kStageCols, rb * kRows, &ctrl->full[st]);
-          tensor_g2s(w + kWBytes, &a.xmap, k * kStageCols, mt * a.NT, &ctrl->full[st]);
+          tensor_g2s(w, &a.wmap, (k0 + k) * kStageCols, rb * kRows, &ctrl->full[st]);
+          tensor_g2s(w + kWBytes, &a.xmap, (k0 + k) * kStageCols, mt * a.NT, &ctrl->full[st]);
           if (++st == a.stages) { st = 0; ph ^= 1u; }
         }
       }
@@ -286,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
     int st = 0, sl = 0;
     uint32_t ph = 0, sph = 0, acc = 0, aph = 0;
     bool ok = true;
-    for (int t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+    for (int t = tile0; ok && t < a.tiles; t += step) {
       if (!mbar_wait(&ctrl->accempty[acc], aph ^ 1u, abortp, a.status)) break;
       tc_fence_after();
       const uint32_t d = tmem + acc * (uint32_t)a.NT;
@@ -319,16 +380,16 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
     int sl = 0;
     uint32_t sph = 0;
     bool ok = true;
-    for (int t = blockIdx.x; ok && t < a.tiles; t += gridDim.x) {
+    for (int t = tile0; ok && t < a.tiles; t += step) {
       const int mt = t % a.MT, rb = t / a.MT;
       const uint8_t* ws = a.w_scale + (size_t)rb * a.pitch;
       for (int k = 0; k < n_k; k += 4) {
-        const uint32_t ww = *reinterpret_cast<const uint32_t*>(ws + k);
+        const uint32_t ww = *reinterpret_cast<const uint32_t*>(ws + k0 + k);
         uint32_t xw[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int r = j * 32 + lane, tok = mt * a.NT + r;
-          xw[j] = r < a.NT && tok < a.M ? *reinterpret_cast<const uint32_t*>(a.x_scale + (size_t)tok * a.pitch + k) : 0x7F7F7F7Fu;
+          xw[j] = r < a.NT && tok < a.M ? *reinterpret_cast<const uint32_t*>(a.x_scale + (size_t)tok * a.pitch + k0 + k) : 0x7F7F7F7Fu;
         }
         if (!mbar_wait(&ctrl->sfempty[sl], sph ^ 1u, abortp, a.status)) { ok = false; break; }
         uint4* dst = reinterpret_cast<uint4*>(sf + sl * kSfBytes) + lane;
@@ -342,13 +403,24 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
     }
   } else if (warp >= 4) {
     uint32_t acc = 0, aph = 0;
-    for (int t = blockIdx.x; t < a.tiles; t += gridDim.x) {
+    for (int t = tile0; t < a.tiles; t += step) {
       const int mt = t % a.MT, rb = t / a.MT, t0 = mt * a.NT;
       if (!mbar_wait(&ctrl->accfull[acc], aph, abortp, a.status)) break;
       tc_fence_after();
       const uint32_t src = tmem + acc * (uint32_t)a.NT + ((uint32_t)(warp - 4) << 21);
       const int row = rb * kRows + (warp - 4) * 32 + lane, nt = min(a.NT, a.M - t0);
-      if (a.y_dtype == RWKVQ_F32) store_tile<float>(a, src, row, t0, nt);
+      if (a.slices > 1) {
+        // this slice's sums, where the stages were: [token][row]
+        float* part = reinterpret_cast<float*>(smem) + (warp - 4) * 32 + lane;
+        for (int c = 0; c < nt; c += 32) {
+          uint32_t r[32];
+          tmem_ld32_issue(src + (uint32_t)c, r);
+          tmem_ld_wait(r);
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (c + j < nt) part[(c + j) * kRows] = __uint_as_float(r[j]);
+        }
+      } else if (a.y_dtype == RWKVQ_F32) store_tile<float>(a, src, row, t0, nt);
       else if (a.y_dtype == RWKVQ_F16) store_tile<__half>(a, src, row, t0, nt);
       else store_tile<__nv_bfloat16>(a, src, row, t0, nt);
       tc_fence_before();
@@ -358,6 +430,13 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
     }
   }
   __syncwarp();
+  if (a.slices > 1) {
+    cluster_sync();
+    if (a.y_dtype == RWKVQ_F32) add_slices<float>(a, smem, slice, tile0);
+    else if (a.y_dtype == RWKVQ_F16) add_slices<__half>(a, smem, slice, tile0);
+    else add_slices<__nv_bfloat16>(a, smem, slice, tile0);
+    cluster_sync();
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -374,6 +453,27 @@ bool encode_codes(CUtensorMap* map, const void* codes, int rows, int cols, int b
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles, slices and stages of a product.
+struct Plan { int NT, MT, slices, stages, per_sm; uint32_t tmem_cols, smem_bytes; };
+constexpr uint32_t kFixedBytes = 1024 + kSfSlots * kSfBytes + kCtrlBytes;
+Plan plan_of(int M, int oc, int groups) {
+  Plan l;
+  l.MT = (int)(((long long)M + kMaxTokens - 1) / kMaxTokens);
+  l.NT = (int)((((long long)M + l.MT - 1) / l.MT + 15) / 16 * 16);
+  const long long tiles = (long long)blocks_of(oc) * l.MT;
+  const int words = (groups + 3) / 4, sms = sm_count();
+  const uint32_t stage = kWBytes + (uint32_t)l.NT * kStageCols;
+  // two blocks an SM where four stages of each fit
+  l.per_sm = (kMaxSmemBytes - 2048) / 2 >= kFixedBytes + kMinStages * stage ? 2 : 1;
+  l.slices = 1;
+  while (l.slices < kMaxSlices && l.slices * 2 <= words && tiles * l.slices * 2 <= (long long)sms * l.per_sm) l.slices *= 2;
+  const uint32_t room = l.per_sm == 2 ? (kMaxSmemBytes - 2048) / 2 : kMaxSmemBytes;
+  l.stages = (int)std::min<uint32_t>(kMaxStages, (room - kFixedBytes) / stage);
+  l.smem_bytes = kFixedBytes + (uint32_t)l.stages * stage;
+  l.tmem_cols = 32;
+  while (l.tmem_cols < (uint32_t)l.NT * 2u + kSfSlots * kSfCols) l.tmem_cols *= 2;
+  return l;
+}
 int element_size(int dtype) { return dtype == RWKVQ_F32 ? 4 : dtype == RWKVQ_F16 || dtype == RWKVQ_BF16 ? 2 : 0; }
 
 }  // namespace f8
@@ -409,23 +509,25 @@ rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, in
   a.w_scale = static_cast<const uint8_t*>(w_scale); a.x_scale = static_cast<const uint8_t*>(x_scale);
   a.Y = Y; a.y_row = y_row; a.oc = oc; a.M = M; a.y_dtype = y_dtype;
   a.groups = f8::blocks_of(ic); a.pitch = (int)f8::scale_pitch(ic);
-  a.MT = (int)(((long long)M + f8::kMaxTokens - 1) / f8::kMaxTokens);
-  a.NT = (int)((((long long)M + a.MT - 1) / a.MT + 15) / 16 * 16);
-  const long long tiles = (long long)f8::blocks_of(oc) * a.MT;
-  if (tiles > (1ll << 30)) return RWKVQ_EUNSUPPORTED;
-  a.tiles = (int)tiles;
+  const f8::Plan l = f8::plan_of(M, oc, a.groups);
+  const long long tiles = (long long)f8::blocks_of(oc) * l.MT;
+  if (tiles > (1ll << 28)) return RWKVQ_EUNSUPPORTED;
+  a.NT = l.NT; a.MT = l.MT; a.slices = l.slices; a.stages = l.stages; a.tiles = (int)tiles; a.tmem_cols = l.tmem_cols;
   a.status = device_status_ptr();
   if (!a.status) return RWKVQ_ECUDA;
-  a.tmem_cols = 32;
-  while (a.tmem_cols < (uint32_t)a.NT * 2u + f8::kSfSlots * f8::kSfCols) a.tmem_cols *= 2;
   if (!f8::encode_codes(&a.wmap, w_codes, oc, ic, f8::kRows) || !f8::encode_codes(&a.xmap, x_codes, M, ic, a.NT)) return RWKVQ_ECUDA;
-  const uint32_t fixed = 1024 + f8::kSfSlots * f8::kSfBytes + f8::kCtrlBytes, stage = f8::kWBytes + (uint32_t)a.NT * f8::kStageCols;
-  a.stages = (int)std::min<uint32_t>(f8::kMaxStages, (f8::kMaxSmemBytes - fixed) / stage);
-  static SmemOptIn opt_in;
+  static SmemOptIn opt_in(kCarveOut);
   const cudaError_t e = opt_in((const void*)f8::fp8_gemm_kernel, (int)f8::kMaxSmemBytes);
   if (e != cudaSuccess) return cuda_status(e);
-  f8::fp8_gemm_kernel<<<(unsigned)std::min<int>(a.tiles, sm_count()), f8::kThreads, fixed + (uint32_t)a.stages * stage, static_cast<cudaStream_t>(stream)>>>(a);
-  return cuda_status(cudaGetLastError());
+  cudaLaunchAttribute attr[2];
+  const unsigned blocks = l.slices > 1 ? (unsigned)(a.tiles * l.slices) : (unsigned)std::min<int>(a.tiles, sm_count() * l.per_sm);
+  cudaLaunchConfig_t cfg = f8::launch_config(dim3(blocks), f8::kThreads, l.smem_bytes, static_cast<cudaStream_t>(stream), attr);
+  if (l.slices > 1) {
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)l.slices; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+  }
+  return cuda_status(cudaLaunchKernelEx(&cfg, f8::fp8_gemm_kernel, a));
 }
 
 }  // extern "C"
