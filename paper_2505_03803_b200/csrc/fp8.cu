@@ -200,7 +200,7 @@ cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int blo
 // Scales: four groups' bytes of a row are the word that the instruction picks its byte from; warp 2 deals the words of 512 columns out in the order
 // of the copy to tensor memory (32 lanes x 16 bytes, row r in line r % 32, word r / 32), where they lie once per 32-lane quarter.
 constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 8, kSfSlots = 2, kMaxSlices = 8, kMinStages = 4, kThreads = 256;
-constexpr uint32_t kWBytes = kRows * kStageCols, kSfBytes = 512 + 1024, kSfCols = 16, kCtrlBytes = 512;
+constexpr uint32_t kWBytes = kRows * kStageCols, kSfBytes = 512 + 1024, kSfCols = 16, kOutBytes = 4096, kCtrlBytes = 512;
 constexpr uint32_t kMaxSmemBytes = 232448;
 
 struct GemmArgs {
@@ -209,7 +209,7 @@ struct GemmArgs {
   const uint8_t* x_scale;
   void* Y;
   long long y_row;
-  int oc, M, groups, pitch, NT, MT, tiles, stages, slices, y_dtype;
+  int oc, M, groups, pitch, NT, MT, tiles, stages, slices, y_dtype, wide;
   uint32_t tmem_cols;
   int* status;
 };
@@ -255,17 +255,34 @@ template <> __device__ __forceinline__ float to_out<float>(float f) { return f; 
 template <> __device__ __forceinline__ __half to_out<__half>(float f) { return __float2half_rn(f); }
 template <> __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float f) { return __float2bfloat16_rn(f); }
 
+// A warp's 32 output channels of a tile's tokens.  A lane holds one channel, so that a store of it writes 32 elements of one token: through shared memory
+// (`stage`, 4 KB of the warp's own) it becomes 16 bytes a lane, several tokens a store.  `wide`: rows of Y begin on 16 bytes and all 32 channels are there.
 template <typename T>
-__device__ __forceinline__ void store_tile(const GemmArgs& a, uint32_t tmem, int row, int t0, int nt) {
-  T* y = static_cast<T*>(a.Y) + (long long)t0 * a.y_row + row;
+__device__ __forceinline__ void store_tile(const GemmArgs& a, uint32_t tmem, int row0, int t0, int nt, uint8_t* stage, int lane) {
+  constexpr int kLanes = 32 * (int)sizeof(T) / 16, kTokens = 32 / kLanes;        // lanes of a token's 32 channels, tokens of a store
+  T* y = static_cast<T*>(a.Y) + (long long)t0 * a.y_row + row0;
+  const bool wide = a.wide && row0 + 32 <= a.oc;
   for (int c = 0; c < nt; c += 32) {
     uint32_t r[32];
     tmem_ld32_issue(tmem + (uint32_t)c, r);
     tmem_ld_wait(r);
-    if (row < a.oc) {
+    if (wide) {
+      T* st = reinterpret_cast<T*>(stage) + lane;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) st[j * 32] = to_out<T>(__uint_as_float(r[j]));
+      __syncwarp();
+      T* at = y + (long long)(c + lane / kLanes) * a.y_row + lane % kLanes * (16 / (int)sizeof(T));
+#pragma unroll
+      for (int i = 0; i < 32 / kTokens; ++i) {
+        const uint4 v = *reinterpret_cast<const uint4*>(stage + i * 512 + lane * 16);
+        if (c + i * kTokens + lane / kLanes < nt) *reinterpret_cast<uint4*>(at) = v;
+        at += kTokens * a.y_row;
+      }
+      __syncwarp();
+    } else if (row0 + lane < a.oc) {
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        if (c + j < nt) y[(c + j) * a.y_row] = to_out<T>(__uint_as_float(r[j]));
+        if (c + j < nt) y[(c + j) * a.y_row + lane] = to_out<T>(__uint_as_float(r[j]));
     }
   }
 }
@@ -274,27 +291,37 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // A cluster's sums added up in the order of the slices: each block takes its share of the tokens, two at a time.
+template <typename T, int S>
+__device__ __forceinline__ void add_slices(const GemmArgs& a, uint8_t* smem, int slice, int tile) {
+  constexpr int kAtOnce = 16 / S, kStep = kThreads / kRows;      // sixteen loads from the other blocks' memories under way
+  const int mt = tile % a.MT, t0 = mt * a.NT, nt = min(a.NT, a.M - t0), i = threadIdx.x % kRows, row = tile / a.MT * kRows + i;
+  const int c1 = nt * (slice + 1) / S;
+  uint32_t from[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from[s]) : "r"(smem_u32(smem) + (uint32_t)i * 4u), "r"(s));
+  for (int c = nt * slice / S + (int)threadIdx.x / kRows; c < c1; c += kAtOnce * kStep) {
+    float v[kAtOnce][S];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const int at = min(c + j * kStep, c1 - 1);
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[j][s]) : "r"(from[s] + (uint32_t)at * (kRows * 4u)));
+      }
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      float sum = v[j][0];
+#pragma unroll
+      for (int s = 1; s < S; ++s) sum += v[j][s];
+      if (row < a.oc && c + j * kStep < c1) static_cast<T*>(a.Y)[(long long)(t0 + c + j * kStep) * a.y_row + row] = to_out<T>(sum);
+    }
+  }
+}
 template <typename T>
 __device__ __forceinline__ void add_slices(const GemmArgs& a, uint8_t* smem, int slice, int tile) {
-  const int mt = tile % a.MT, t0 = mt * a.NT, nt = min(a.NT, a.M - t0), i = threadIdx.x % kRows, row = tile / a.MT * kRows + i;
-  const int c1 = nt * (slice + 1) / a.slices;
-  for (int c = nt * slice / a.slices + (int)threadIdx.x / kRows; c < c1; c += kThreads / kRows) {
-    const uint32_t at = smem_u32(smem) + (uint32_t)(c * kRows + i) * 4u;
-    float v[kMaxSlices];
-#pragma unroll
-    for (int s = 0; s < kMaxSlices; ++s) {
-      if (s < a.slices) {
-        uint32_t peer;
-        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer) : "r"(at), "r"(s));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[s]) : "r"(peer) : "memory");
-      }
-    }
-    float sum = v[0];
-#pragma unroll
-    for (int s = 1; s < kMaxSlices; ++s)
-      if (s < a.slices) sum += v[s];
-    if (row < a.oc) static_cast<T*>(a.Y)[(long long)(t0 + c) * a.y_row + row] = to_out<T>(sum);
-  }
+  if (a.slices == 2) add_slices<T, 2>(a, smem, slice, tile);
+  else if (a.slices == 4) add_slices<T, 4>(a, smem, slice, tile);
+  else add_slices<T, 8>(a, smem, slice, tile);
 }
 
 __global__ void __launch_bounds__(kThreads, 2) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
@@ -302,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 2) fp8_gemm_kernel(const __grid_cons
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
   const uint32_t stage_bytes = kWBytes + (uint32_t)a.NT * kStageCols;
   uint8_t* sf = smem + (uint32_t)a.stages * stage_bytes;
-  Ctrl* ctrl = reinterpret_cast<Ctrl*>(sf + kSfSlots * kSfBytes);
+  Ctrl* ctrl = reinterpret_cast<Ctrl*>(sf + kSfSlots * kSfBytes + 4 * kOutBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abortp = &ctrl->abort_flag;
   if (threadIdx.x == 0) {
@@ -408,7 +435,8 @@ __global__ void __launch_bounds__(kThreads, 2) fp8_gemm_kernel(const __grid_cons
       if (!mbar_wait(&ctrl->accfull[acc], aph, abortp, a.status)) break;
       tc_fence_after();
       const uint32_t src = tmem + acc * (uint32_t)a.NT + ((uint32_t)(warp - 4) << 21);
-      const int row = rb * kRows + (warp - 4) * 32 + lane, nt = min(a.NT, a.M - t0);
+      const int row0 = rb * kRows + (warp - 4) * 32, nt = min(a.NT, a.M - t0);
+      uint8_t* out = sf + kSfSlots * kSfBytes + (warp - 4) * kOutBytes;
       if (a.slices > 1) {
         // this slice's sums, where the stages were: [token][row]
         float* part = reinterpret_cast<float*>(smem) + (warp - 4) * 32 + lane;
@@ -420,9 +448,9 @@ __global__ void __launch_bounds__(kThreads, 2) fp8_gemm_kernel(const __grid_cons
           for (int j = 0; j < 32; ++j)
             if (c + j < nt) part[(c + j) * kRows] = __uint_as_float(r[j]);
         }
-      } else if (a.y_dtype == RWKVQ_F32) store_tile<float>(a, src, row, t0, nt);
-      else if (a.y_dtype == RWKVQ_F16) store_tile<__half>(a, src, row, t0, nt);
-      else store_tile<__nv_bfloat16>(a, src, row, t0, nt);
+      } else if (a.y_dtype == RWKVQ_F32) store_tile<float>(a, src, row0, t0, nt, out, lane);
+      else if (a.y_dtype == RWKVQ_F16) store_tile<__half>(a, src, row0, t0, nt, out, lane);
+      else store_tile<__nv_bfloat16>(a, src, row0, t0, nt, out, lane);
       tc_fence_before();
       mbar_arrive(&ctrl->accempty[acc]);
       acc ^= 1u;
@@ -455,7 +483,7 @@ bool encode_codes(CUtensorMap* map, const void* codes, int rows, int cols, int b
 
 // Tiles, slices and stages of a product.
 struct Plan { int NT, MT, slices, stages, per_sm; uint32_t tmem_cols, smem_bytes; };
-constexpr uint32_t kFixedBytes = 1024 + kSfSlots * kSfBytes + kCtrlBytes;
+constexpr uint32_t kFixedBytes = 1024 + kSfSlots * kSfBytes + 4 * kOutBytes + kCtrlBytes;
 Plan plan_of(int M, int oc, int groups) {
   Plan l;
   l.MT = (int)(((long long)M + kMaxTokens - 1) / kMaxTokens);
@@ -507,7 +535,7 @@ rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, in
   f8::GemmArgs a;
   memset(&a, 0, sizeof(a));
   a.w_scale = static_cast<const uint8_t*>(w_scale); a.x_scale = static_cast<const uint8_t*>(x_scale);
-  a.Y = Y; a.y_row = y_row; a.oc = oc; a.M = M; a.y_dtype = y_dtype;
+  a.Y = Y; a.y_row = y_row; a.wide = (y_row * f8::element_size(y_dtype)) % 16 == 0; a.oc = oc; a.M = M; a.y_dtype = y_dtype;
   a.groups = f8::blocks_of(ic); a.pitch = (int)f8::scale_pitch(ic);
   const f8::Plan l = f8::plan_of(M, oc, a.groups);
   const long long tiles = (long long)f8::blocks_of(oc) * l.MT;
