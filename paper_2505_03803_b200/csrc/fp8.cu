@@ -44,6 +44,11 @@ struct Eight {
       w[4 * i] = a.x; w[4 * i + 1] = a.y; w[4 * i + 2] = a.z; w[4 * i + 3] = a.w;
     }
   }
+  // The compiler is to forget what it has made of the words: kept for a second use, that takes twice the registers.
+  __device__ __forceinline__ void forget() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) asm volatile("" : "+r"(w[i]));
+  }
   __device__ __forceinline__ void floats(float (&f)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -53,15 +58,18 @@ struct Eight {
   }
 };
 constexpr uint32_t kInfBits = 0x7F800000u;
-// Bits of the largest finite magnitude (as unsigned integers they sort like the numbers).
-template <typename T>
+// Bits of the largest magnitude (as unsigned integers they sort like the numbers); NaN does not count.  kFinite: infinities do not, either, which takes
+// four times the instructions and is asked for only where the first answer is infinity.
+template <bool kFinite, typename T>
 __device__ __forceinline__ uint32_t amax8(const Eight<T>& x) {
-  float f[8];
+  float f[8], a = 0.f;
   x.floats(f);
-  uint32_t a = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { const uint32_t b = __float_as_uint(f[i]) & 0x7FFFFFFFu; a = max(a, b < kInfBits ? b : 0u); }
-  return a;
+  for (int i = 0; i < 8; ++i) {
+    const float m = fabsf(f[i]);
+    a = fmaxf(a, !kFinite || __float_as_uint(m) < kInfBits ? m : 0.f);
+  }
+  return __float_as_uint(a);
 }
 // The scale's exponent + 127 from those bits: x = m * 2^(E - 127) with m <= 1.75 fits 448 * 2^(E - 127 - 8), a larger m needs one more.
 __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
@@ -70,8 +78,8 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
   return (uint32_t)max(e, 1);
 }
 __device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }     // 1 <= byte <= 247
-// Infinities become NaN codes (the conversion alone would saturate them).
-template <typename T>
+// kFinite: there may be infinities, which become NaN codes (the conversion alone would saturate them).
+template <bool kFinite, typename T>
 __device__ __forceinline__ uint2 encode8(const Eight<T>& e, float inv) {
   float f[8];
   e.floats(f);
@@ -82,7 +90,7 @@ __device__ __forceinline__ uint2 encode8(const Eight<T>& e, float inv) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const float x = f[2 * i + j];
-      v[j] = (__float_as_uint(x) & 0x7FFFFFFFu) < kInfBits ? x * inv : __uint_as_float(0x7FFFFFFFu);
+      v[j] = !kFinite || (__float_as_uint(x) & 0x7FFFFFFFu) < kInfBits ? x * inv : __uint_as_float(0x7FFFFFFFu);
     }
     uint16_t c;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(v[1]), "f"(v[0]));
@@ -109,55 +117,79 @@ __global__ void __launch_bounds__(kRowWarps * 32) fp8_rows_kernel(const T* x, lo
     if (c0 + j * 256 < cols) f[j].load(x + row * x_row + c0 + j * 256);
     else f[j].zero();
   }
+  uint32_t m[kRowChunks], most = 0;
+#pragma unroll
+  for (int j = 0; j < kRowChunks; ++j) { m[j] = amax8<false>(f[j]); most = max(most, m[j]); }
+  const bool infinite = __any_sync(0xFFFFFFFFu, most >= kInfBits);
+  if (infinite) {
+#pragma unroll
+    for (int j = 0; j < kRowChunks; ++j) m[j] = amax8<true>(f[j]);
+  }
   uint32_t lo = 0, hi = 0;
 #pragma unroll
   for (int j = 0; j < kRowChunks; ++j) {
-    uint32_t a = amax8(f[j]);
+    uint32_t a = m[j];
 #pragma unroll
     for (int d = 8; d > 0; d >>= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, d));
     const uint32_t b = scale_byte(a);
     const uint32_t two = b | __shfl_down_sync(0xFFFFFFFFu, b, 16) << 8;
     if (j < 2) lo |= two << (16 * j);
     else hi |= two << (16 * (j - 2));
-    if (c0 + j * 256 < cols) *reinterpret_cast<uint2*>(codes + row * cols + c0 + j * 256) = encode8(f[j], inverse_scale(b));
+    if (c0 + j * 256 < cols)
+      *reinterpret_cast<uint2*>(codes + row * cols + c0 + j * 256) = infinite ? encode8<true>(f[j], inverse_scale(b)) : encode8<false>(f[j], inverse_scale(b));
   }
   // the pitch is a multiple of 16, and a piece of columns begins inside it
   if (lane == 0) *reinterpret_cast<uint2*>(scale + row * pitch + (c0 >> 7)) = make_uint2(lo, hi);
 }
 
 // Blocks of 128 x 128: one thread block each, its elements in registers between the maximum and the codes.
-constexpr int kBlockThreads = 256;
+constexpr int kBlockThreads = 512;
 template <typename T>
-__global__ void __launch_bounds__(kBlockThreads, sizeof(T) == 2 ? 5 : 3) fp8_blocks_kernel(const T* x, long long x_row, int rows, int cols, int groups, uint8_t* codes,
+__global__ void __launch_bounds__(kBlockThreads, 2) fp8_blocks_kernel(const T* x, long long x_row, int rows, int cols, int groups, uint8_t* codes,
                                                                   uint8_t* scale, int pitch) {
   __shared__ uint32_t most[kBlockThreads / 32];
   const int g = (int)(blockIdx.x % (unsigned)groups), rb = (int)(blockIdx.x / (unsigned)groups);
   const int c = g * 128 + (threadIdx.x & 15) * 8;
   const long long r0 = (long long)rb * 128 + (threadIdx.x >> 4);
-  constexpr int kSteps = 128 / (kBlockThreads / 16);
+  constexpr int kStepRows = kBlockThreads / 16, kSteps = 128 / kStepRows;
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int left = c < cols ? (int)min(rows - r0, (long long)128) : 0;       // rows of this thread's that are there: every kStepRows-th of so many
   Eight<T> f[kSteps];
   uint32_t a = 0;
+  const T* from = x + r0 * x_row + c;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const long long r = r0 + i * (kBlockThreads / 16);
-    if (r < rows && c < cols) f[i].load(x + r * x_row + c);
+    if (i * kStepRows < left) f[i].load(from);
     else f[i].zero();
+    from += kStepRows * x_row;
   }
+  auto whole = [&](uint32_t v) {
+    v = __reduce_max_sync(0xFFFFFFFFu, v);
+    if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = v;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) a = max(a, amax8(f[i]));
-  a = __reduce_max_sync(0xFFFFFFFFu, a);
-  if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = a;
-  __syncthreads();
+    for (int i = 0; i < kBlockThreads / 32; ++i) v = max(v, most[i]);
+    return v;
+  };
 #pragma unroll
-  for (int i = 0; i < kBlockThreads / 32; ++i) a = max(a, most[i]);
+  for (int i = 0; i < kSteps; ++i) { a = max(a, amax8<false>(f[i])); f[i].forget(); }
+  a = whole(a);
+  const bool infinite = a >= kInfBits;       // the same in all threads
+  if (infinite) {
+    a = 0;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) a = max(a, amax8<true>(f[i]));
+    __syncthreads();
+    a = whole(a);
+  }
   const uint32_t b = scale_byte(a);
   const float inv = inverse_scale(b);
+  uint8_t* to = codes + r0 * cols + c;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const long long r = r0 + i * (kBlockThreads / 16);
-    if (r < rows && c < cols) *reinterpret_cast<uint2*>(codes + r * cols + c) = encode8(f[i], inv);
+    if (i * kStepRows < left) *reinterpret_cast<uint2*>(to) = infinite ? encode8<true>(f[i], inv) : encode8<false>(f[i], inv);
+    to += (size_t)kStepRows * cols;
   }
   if (threadIdx.x == 0) scale[(size_t)rb * pitch + g] = (uint8_t)b;
 }
@@ -199,7 +231,7 @@ cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int blo
 // instructions, (2) scales, (3) tensor memory, (4-7) epilogue.  Two accumulators, so that a tile's epilogue runs under the next tile's sums.
 // Scales: four groups' bytes of a row are the word that the instruction picks its byte from; warp 2 deals the words of 512 columns out in the order
 // of the copy to tensor memory (32 lanes x 16 bytes, row r in line r % 32, word r / 32), where they lie once per 32-lane quarter.
-constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 8, kSfSlots = 2, kMaxSlices = 8, kMinStages = 4, kThreads = 256;
+constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 12, kSfSlots = 2, kMaxSlices = 8, kThreads = 256;
 constexpr uint32_t kWBytes = kRows * kStageCols, kSfBytes = 512 + 1024, kSfCols = 16, kOutBytes = 4096, kCtrlBytes = 512;
 constexpr uint32_t kMaxSmemBytes = 232448;
 
@@ -324,7 +356,7 @@ __device__ __forceinline__ void add_slices(const GemmArgs& a, uint8_t* smem, int
   else add_slices<T, 8>(a, smem, slice, tile);
 }
 
-__global__ void __launch_bounds__(kThreads, 2) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
   const uint32_t stage_bytes = kWBytes + (uint32_t)a.NT * kStageCols;
@@ -481,22 +513,34 @@ bool encode_codes(CUtensorMap* map, const void* codes, int rows, int cols, int b
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Tiles, slices and stages of a product.
-struct Plan { int NT, MT, slices, stages, per_sm; uint32_t tmem_cols, smem_bytes; };
+// Tiles, slices and stages of a product: the cheapest by an estimate of an SM's cycles, fitted to 150 times of 17 products (1 to 1000 tokens, 1024 to 14336 x
+// 1024 to 14336), which it gives to within a tenth; over 16 others it is 2 % off the best choice on average, 9 % at most.  A stage takes 130 cycles and its
+// bytes at 64 a cycle, what an SM takes in, or the tensor core's 2 cycles a token where that is more; a tile's epilogue 14 a token; slices meet in 1500 and 45
+// a token (but up to 112), and their blocks have to fit side by side (clusters of eight only up to 112 blocks); nothing is faster than HBM.  More tiles of
+// fewer tokens or more slices fill SMs: 203 tokens x 7168 x 2048 10.0 us as two tiles (one: 11.7; in two slices: 12.8), 2048 x 7168 12.2 as two in four slices (one in
+// four: 14.4, four in two: 13.8), one token x 4096 x 4096 7.3 in four slices, 8.9 in two, 12.3 in one.
+struct Plan { int NT, MT, slices, stages; uint32_t tmem_cols, smem_bytes; };
 constexpr uint32_t kFixedBytes = 1024 + kSfSlots * kSfBytes + 4 * kOutBytes + kCtrlBytes;
 Plan plan_of(int M, int oc, int groups) {
-  Plan l;
-  l.MT = (int)(((long long)M + kMaxTokens - 1) / kMaxTokens);
-  l.NT = (int)((((long long)M + l.MT - 1) / l.MT + 15) / 16 * 16);
-  const long long tiles = (long long)blocks_of(oc) * l.MT;
-  const int words = (groups + 3) / 4, sms = sm_count();
+  const int words = (groups + 3) / 4, sms = sm_count(), first = (int)(((long long)M + kMaxTokens - 1) / kMaxTokens);
+  const double hbm = ((double)oc + M) * groups * 128.0 / 3300.0;
+  double best = 0.0;
+  Plan l = {};
+  for (int i = 0; i < 12; ++i) {
+    const int NT = (int)((((long long)M + first + i - 1) / (first + i) + 15) / 16 * 16), MT = (int)(((long long)M + NT - 1) / NT);
+    if (NT == l.NT) continue;
+    const long long tiles = (long long)blocks_of(oc) * MT;
+    const double stage = std::max(2.0 * NT, 130.0 + (kWBytes + NT * kStageCols) / 64.0);
+    for (int S = 1; S <= kMaxSlices && S <= words; S *= 2) {
+      if (S > 1 && tiles * S > (S == 8 ? std::min(112, sms) : sms)) break;
+      const long long waves = S > 1 ? 1 : (tiles + sms - 1) / sms;
+      const int stages = S > 1 ? (words + S - 1) / S * 4 : groups;
+      const double cost = std::max((double)waves * stages * stage, hbm) + 14.0 * NT + (S > 1 ? 1500.0 + 45.0 * std::min(NT, 112) : 0.0);
+      if (l.NT == 0 || cost < best) { best = cost; l.NT = NT; l.MT = MT; l.slices = S; }
+    }
+  }
   const uint32_t stage = kWBytes + (uint32_t)l.NT * kStageCols;
-  // two blocks an SM where four stages of each fit
-  l.per_sm = (kMaxSmemBytes - 2048) / 2 >= kFixedBytes + kMinStages * stage ? 2 : 1;
-  l.slices = 1;
-  while (l.slices < kMaxSlices && l.slices * 2 <= words && tiles * l.slices * 2 <= (long long)sms * l.per_sm) l.slices *= 2;
-  const uint32_t room = l.per_sm == 2 ? (kMaxSmemBytes - 2048) / 2 : kMaxSmemBytes;
-  l.stages = (int)std::min<uint32_t>(kMaxStages, (room - kFixedBytes) / stage);
+  l.stages = (int)std::min<uint32_t>(kMaxStages, (kMaxSmemBytes - kFixedBytes) / stage);
   l.smem_bytes = kFixedBytes + (uint32_t)l.stages * stage;
   l.tmem_cols = 32;
   while (l.tmem_cols < (uint32_t)l.NT * 2u + kSfSlots * kSfCols) l.tmem_cols *= 2;
@@ -548,7 +592,7 @@ rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, in
   const cudaError_t e = opt_in((const void*)f8::fp8_gemm_kernel, (int)f8::kMaxSmemBytes);
   if (e != cudaSuccess) return cuda_status(e);
   cudaLaunchAttribute attr[2];
-  const unsigned blocks = l.slices > 1 ? (unsigned)(a.tiles * l.slices) : (unsigned)std::min<int>(a.tiles, sm_count() * l.per_sm);
+  const unsigned blocks = l.slices > 1 ? (unsigned)(a.tiles * l.slices) : (unsigned)std::min<int>(a.tiles, sm_count());
   cudaLaunchConfig_t cfg = f8::launch_config(dim3(blocks), f8::kThreads, l.smem_bytes, static_cast<cudaStream_t>(stream), attr);
   if (l.slices > 1) {
     attr[1].id = cudaLaunchAttributeClusterDimension;
