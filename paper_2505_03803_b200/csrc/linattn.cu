@@ -26,9 +26,12 @@ struct Args {
   rwkvq_linattn_args a;
   int* status;
   int limit;                // the token kernel takes sequences of at most so many rows, the chunk kernels the others
-  int block_rows, blocks;   // rows of a block of the chunk kernels
+  // The chunk kernels' blocks: so many rows each of all heads' rows one head after the other, a head's rows `pitch` apart (more than there are, where no
+  // block is to have rows of two heads).
+  long long block_rows, pitch;
+  int blocks;
   Entry* entries;           // [n_seq], written by the token kernel; nullptr: one sequence, all rows, slot 0
-  float* block_states;      // [blocks][heads]: the state a block's last piece adds up, the one its sequence began with, the piece's decays
+  float* block_states;      // [blocks]: the state a block's last piece adds up, the one its sequence began with, the piece's decays
 };
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
@@ -151,11 +154,14 @@ struct Shape {
   static constexpr int kRawPitch = N * (int)sizeof(T) + 16, kDecayPitch = N * 4 + 16;
   static constexpr int kTerm = kChunk * kPitch, kHalfTerm = kHalf * kPitch, kRaw = kChunk * kRawPitch;
   // a raw stage: r (where there are outputs), k, v, logarithms of decays
+  static constexpr int kStages = 3;
   static constexpr int kR = 0, kK = kStateOnly ? 0 : kRaw, kV = kK + kRaw, kL = kV + kRaw, kStage = kL + kChunk * kDecayPitch;
-  static constexpr int oKt = 2 * kStage, oD = oKt + K3 * kTerm, oVt = oD + N * 4, oRt = oVt + (V > 2 ? V * kTerm : 0);
+  // a set of operands
+  static constexpr int kKt = 0, kD = kKt + K3 * kTerm, kVt = kD + N * 4, kRt = kVt + (V > 2 ? V * kTerm : 0);
   // what only outputs need
-  static constexpr int oRp = oRt + R * kTerm, oKp = oRp + R * kHalfTerm, oA = oKp + R * kHalfTerm;
-  static constexpr int kTriangles = (N / 64) * 2 * 64 * 4, oMid = oA + 2 * kTriangles, kBytes = kStateOnly ? oRt : oMid + kSteps * 64 * 4;
+  static constexpr int kRp = kRt + R * kTerm, kKp = kRp + R * kHalfTerm, kA = kKp + R * kHalfTerm, kTriangles = (N / 64) * 2 * 64 * 4;
+  static constexpr int kSet = kStateOnly ? kRt : kA + kTriangles, oSets = kStages * kStage, oMid = oSets + 2 * kSet;
+  static constexpr int kBytes = oMid + (kStateOnly ? 0 : kSteps * 64 * 4);
   static constexpr int kStateFloats = N * N, kBlockFloats = 2 * N * N + N;
 };
 
@@ -225,6 +231,11 @@ __device__ __forceinline__ void store_split(uint8_t* at, int term_bytes, pair v)
 #pragma unroll
   for (int i = 0; i < n; ++i) *reinterpret_cast<uint32_t*>(at + i * term_bytes) = t[i];
 }
+// Barriers of a block, by number (0 is __syncthreads).
+enum { kFull = 1, kEmpty = 3, kMakers = 5, kMultipliers = 6 };
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
 // Where the logarithms of decays come from.
 enum { DECAY_F32 = 0, DECAY_SAME = 1, DECAY_HEAD = 2 };
 
@@ -233,7 +244,8 @@ struct Worker {
   using Sh = Shape<T, N, kStateOnly>;
   const Args& p;
   uint8_t* sm;
-  int h, warp, lane, tid;
+  int h, warp, lane, tid;      // tid, warp: in its role
+  int count = 0, stage = 0;    // chunks so far, stage of the next one
   float S[Sh::kTiles][4];      // S^T: values 16 warp + lane / 4 (+ 8: the last two), keys 8 j + 2 (lane % 4) and the next
   pair total;                  // kStateOnly: sums of the logarithms of the decays of this thread's channels
   // This thread's pieces of 16 bytes of the next chunk to fetch, and bytes from row to row.
@@ -243,12 +255,12 @@ struct Worker {
   pair bonus;                  // u of this thread's channels
   int place, place2;           // bytes into a triangle of A of the entries that this lane ends up with
 
-  __device__ __forceinline__ Worker(const Args& p_, uint8_t* sm_) : p(p_), sm(sm_), h(blockIdx.y), warp(threadIdx.x >> 5), lane(threadIdx.x & 31), tid(threadIdx.x) {
+  __device__ __forceinline__ Worker(const Args& p_, uint8_t* sm_) : p(p_), sm(sm_), warp((threadIdx.x & (2 * N - 1)) >> 5), lane(threadIdx.x & 31),
+        tid(threadIdx.x & (2 * N - 1)) {
     if (kStateOnly) return;
-    const int set = (warp & 3) < 2 ? 0 : 1, c = (warp >> 2) * 64 + lane * 2;
+    const int set = (warp & 3) < 2 ? 0 : 1;
     place = entry(set, lane >> 1) * 4;
     place2 = entry(set, 16 + (lane & 1)) * 4;
-    bonus = p.a.u ? load2(p.a.u + h * N + c) : ones();
   }
 
   __device__ __forceinline__ void fetch_from(int t0) {
@@ -331,7 +343,7 @@ struct Worker {
   }
 
   // Without outputs only k Q is needed: a warp of a group of four takes four tokens (the last first, as the sums of the decays behind them are longer).
-  __device__ __forceinline__ void state_operands(int stage) {
+  __device__ __forceinline__ void state_operands(int stage, uint8_t* set) {
     constexpr int kQuarter = 4;
     const uint8_t* st = sm + stage * Sh::kStage;
     const uint8_t* lw = st + Sh::kL;
@@ -345,7 +357,7 @@ struct Worker {
 #pragma unroll
     for (int t = kQuarter; t < kChunk; ++t)
       if (t >= t0 + kQuarter) s = add2(s, decay2(lw, t, c));
-    uint8_t* const to = sm + t0 * Sh::kPitch + c * 2;
+    uint8_t* const to = set + t0 * Sh::kPitch + c * 2;
     pair v[kQuarter];
     if (Sh::V > 2) {
 #pragma unroll
@@ -354,22 +366,22 @@ struct Worker {
     // exponentials of sums, not products of exponentials: they do not wait for one another
 #pragma unroll
     for (int t = kQuarter - 1; t >= 0; --t) {
-      store_split<K3>(to + Sh::oKt + t * Sh::kPitch, Sh::kTerm, mul2(x[t], exp_both(s)));
+      store_split<K3>(to + Sh::kKt + t * Sh::kPitch, Sh::kTerm, mul2(x[t], exp_both(s)));
       s = add2(s, l[t]);
     }
     if (Sh::V > 2) {
 #pragma unroll
-      for (int t = 0; t < kQuarter; ++t) store_split<Sh::V>(to + Sh::oVt + t * Sh::kPitch, Sh::kTerm, v[t]);
+      for (int t = 0; t < kQuarter; ++t) store_split<Sh::V>(to + Sh::kVt + t * Sh::kPitch, Sh::kTerm, v[t]);
     }
     if (t0 == 0) {
       const float2 f = both(s);
-      *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(f.x), expf(f.y));
+      *reinterpret_cast<float2*>(set + Sh::kD + c * 4) = make_float2(expf(f.x), expf(f.y));
       total = add2(total, s);
     }
   }
 
   // A stage's operands.  Warps of a group of four take: r of the first eight tokens, r of the last, k of the last, k of the first; a lane two channels.
-  __device__ __forceinline__ void operands(int stage) {
+  __device__ __forceinline__ void operands(int stage, uint8_t* set) {
     const uint8_t* st = sm + stage * Sh::kStage;
     const uint8_t* lw = st + Sh::kL;
     const int role = warp & 3, c = (warp >> 2) * 64 + lane * 2;
@@ -388,7 +400,7 @@ struct Worker {
     }
 #pragma unroll
     for (int t = 0; t < kHalf; ++t) w[t] = exp_both(l[t]);
-    uint8_t* const to = sm + t0 * Sh::kPitch + c * 2;
+    uint8_t* const to = set + t0 * Sh::kPitch + c * 2;
     if (role < 2) {
       if (role == 1) {
         pair all = s;
@@ -396,17 +408,17 @@ struct Worker {
         for (int t = 0; t < kHalf; ++t) all = add2(all, l[t]);
         // the state's decay, over and over the same where decays do not change: the accurate exponential of the sum
         const float2 f = both(all);
-        *reinterpret_cast<float2*>(sm + Sh::oD + c * 4) = make_float2(expf(f.x), expf(f.y));
+        *reinterpret_cast<float2*>(set + Sh::kD + c * 4) = make_float2(expf(f.x), expf(f.y));
       }
       const pair d = role == 1 ? exp_both(s) : s;
 #pragma unroll
       for (int t = 0; t < kHalf; ++t) {
         pair m = mul2(x[t], q);
         if (role == 1) {
-          store_split<Sh::R>(to + Sh::oRp + (t - kHalf) * Sh::kPitch, Sh::kHalfTerm, m);
+          store_split<Sh::R>(to + Sh::kRp + (t - kHalf) * Sh::kPitch, Sh::kHalfTerm, m);
           m = mul2(m, d);
         }
-        store_split<Sh::R>(to + Sh::oRt + t * Sh::kPitch, Sh::kTerm, m);
+        store_split<Sh::R>(to + Sh::kRt + t * Sh::kPitch, Sh::kTerm, m);
         q = mul2(q, w[t]);
       }
     } else {
@@ -415,10 +427,10 @@ struct Worker {
       for (int t = kHalf - 1; t >= 0; --t) {
         pair m = mul2(x[t], q);
         if (role == 3) {
-          store_split<Sh::R>(to + Sh::oKp + t * Sh::kPitch, Sh::kHalfTerm, m);
+          store_split<Sh::R>(to + Sh::kKp + t * Sh::kPitch, Sh::kHalfTerm, m);
           m = mul2(m, d);
         }
-        store_split<K3>(to + Sh::oKt + t * Sh::kPitch, Sh::kTerm, m);
+        store_split<K3>(to + Sh::kKt + t * Sh::kPitch, Sh::kTerm, m);
         q = mul2(q, w[t]);
       }
     }
@@ -452,7 +464,7 @@ struct Worker {
 #pragma unroll
       for (int d = 16; d > 1; d >>= 1) v[16] += __shfl_xor_sync(0xFFFFFFFFu, v[16], d);
       // lane 2 i holds entry i, lanes 0 and 1 the last two: where these are in A
-      uint8_t* A = sm + Sh::oA + stage * Sh::kTriangles + (warp >> 2) * 512 + (t0 >> 3) * 256;
+      uint8_t* A = set + Sh::kA + (warp >> 2) * 512 + (t0 >> 3) * 256;
       if ((lane & 1) == 0) *reinterpret_cast<float*>(A + place) = v[0];
       if (lane < 2) *reinterpret_cast<float*>(A + place2) = v[16];
     }
@@ -460,34 +472,52 @@ struct Worker {
 #pragma unroll
       for (int t = 0; t < kHalf; ++t) x[t] = load2(reinterpret_cast<const T*>(st + Sh::kV + (t0 + t) * Sh::kRawPitch) + c);
 #pragma unroll
-      for (int t = 0; t < kHalf; ++t) store_split<Sh::V>(to + Sh::oVt + t * Sh::kPitch, Sh::kTerm, x[t]);
+      for (int t = 0; t < kHalf; ++t) store_split<Sh::V>(to + Sh::kVt + t * Sh::kPitch, Sh::kTerm, x[t]);
     }
   }
 
-  // Chunks of rows [begin, end): what comes before the state is needed, and the rest.
-  __device__ __forceinline__ void first_rows(int begin, int end) {
+  // Chunks of rows [begin, end), by the warps that make operands.  Chunk i + 1 is on its way while chunk i is worked on; sets and stages go on being used in
+  // turn from one piece of rows to the next, so that a piece's first chunks are made while the piece before it is multiplied.
+  __device__ __forceinline__ void make(int begin, int end) {
     const int n = (end - begin + kChunk - 1) / kChunk;
+    if (!kStateOnly) bonus = p.a.u ? load2(p.a.u + h * N + (warp >> 2) * 64 + lane * 2) : ones();
     fetch_from(begin);
-    fetch(0, end - begin);
-    if (n > 1) fetch(1, end - begin - kChunk);
-    if (n > 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
-    else asm volatile("cp.async.wait_group 0;" ::: "memory");
-    __syncthreads();
-    if (kStateOnly) state_operands(0);
-    else operands(0);
-    __syncthreads();
+    fetch(stage, end - begin);
+    for (int i = 0; i < n; ++i, ++count) {
+      const int set = count & 1;
+      if (count >= 2) bar_sync(kEmpty + set, 2 * Sh::kThreads);       // the chunk before the last is done with: its set of operands, and its stage
+      const int next = stage == Sh::kStages - 1 ? 0 : stage + 1;
+      if (i + 1 < n) {
+        fetch(next, end - begin - (i + 1) * kChunk);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+      } else {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+      }
+      bar_sync(kMakers, Sh::kThreads);
+      if (kStateOnly) state_operands(stage, sm + Sh::oSets + set * Sh::kSet);
+      else operands(stage, sm + Sh::oSets + set * Sh::kSet);
+      bar_arrive(kFull + set, 2 * Sh::kThreads);
+      stage = next;
+    }
   }
-  __device__ __forceinline__ void rows(int begin, int end) {
+  // Behind the last piece: what the other warps report is waited for, so that no barrier is left half done.
+  __device__ __forceinline__ void made() {
+    for (int i = max(count - 2, 0); i < count; ++i) bar_sync(kEmpty + (i & 1), 2 * Sh::kThreads);
+  }
+  // The same chunks by the warps that multiply.
+  __device__ __forceinline__ void multiply(int begin, int end) {
     const rwkvq_linattn_args& a = p.a;
     const int n = (end - begin + kChunk - 1) / kChunk, g = lane >> 2, q = lane & 3;
-    for (int i = 0; i < n; ++i) {
-      const int t0 = begin + i * kChunk;
+    for (int i = 0; i < n; ++i, ++count) {
+      const int t0 = begin + i * kChunk, turn = count & 1;
+      const uint8_t* set = sm + Sh::oSets + turn * Sh::kSet;
+      bar_sync(kFull + turn, 2 * Sh::kThreads);
       float o[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
       if (!kStateOnly) {
         {
           // the block of A below the triangles: warp w adds up sixteen keys.  Rows of r P' (lanes 0-15) and of k Q' (16-31), eight keys and the next
           float mid[4] = {0.f, 0.f, 0.f, 0.f};
-          const uint32_t half = smem_u32(sm + (lane < 16 ? Sh::oRp : Sh::oKp)) + (lane & 7) * Sh::kPitch + ((lane >> 3) & 1) * 16 + warp * 32;
+          const uint32_t half = smem_u32(set + (lane < 16 ? Sh::kRp : Sh::kKp)) + (lane & 7) * Sh::kPitch + ((lane >> 3) & 1) * 16 + warp * 32;
           uint32_t y[Sh::R][4];
 #pragma unroll
           for (int e = 0; e < Sh::R; ++e) ldsm4(half + e * Sh::kHalfTerm, y[e]);
@@ -500,7 +530,7 @@ struct Worker {
             }
           *reinterpret_cast<float2*>(sm + Sh::oMid + (warp * 64 + g * 8 + q * 2) * 4) = make_float2(mid[2], mid[3]);
         }
-        const uint32_t rt = smem_u32(sm + Sh::oRt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
+        const uint32_t rt = smem_u32(set + Sh::kRt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
 #pragma unroll
         for (int k = 0; k < Sh::kSteps; ++k) {
           uint32_t x[Sh::R][4], b[2][2][Sh::R];
@@ -524,12 +554,12 @@ struct Worker {
       {
         const int row = (lane & 7) + (lane >> 4) * 8, col = warp * 16 + ((lane >> 3) & 1) * 8;
         if constexpr (Sh::V > 2) {
-          const uint32_t at = smem_u32(sm + Sh::oVt) + row * Sh::kPitch + col * 2;
+          const uint32_t at = smem_u32(set + Sh::kVt) + row * Sh::kPitch + col * 2;
 #pragma unroll
           for (int e = 0; e < Sh::V; ++e) ldsm4t(at + e * Sh::kTerm, v[e]);
         } else {
           uint32_t x[4];
-          ldsm4t(smem_u32(sm + (i & 1) * Sh::kStage + Sh::kV) + row * Sh::kRawPitch + col * 2, x);
+          ldsm4t(smem_u32(sm + stage * Sh::kStage + Sh::kV) + row * Sh::kRawPitch + col * 2, x);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             if constexpr (Sh::V == 1) v[0][j] = x[j];
@@ -544,12 +574,12 @@ struct Worker {
       }
 #pragma unroll
       for (int j = 0; j < Sh::kTiles; ++j) {
-        const pair d = *reinterpret_cast<const pair*>(sm + Sh::oD + (j * 8 + q * 2) * 4);
+        const pair d = *reinterpret_cast<const pair*>(set + Sh::kD + (j * 8 + q * 2) * 4);
         const float2 lo = both(mul2(pair_of(S[j][0], S[j][1]), d)), hi = both(mul2(pair_of(S[j][2], S[j][3]), d));
         S[j][0] = lo.x; S[j][1] = lo.y; S[j][2] = hi.x; S[j][3] = hi.y;
       }
       {
-        const uint32_t kt = smem_u32(sm + Sh::oKt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
+        const uint32_t kt = smem_u32(set + Sh::kKt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
 #pragma unroll
         for (int f = 0; f < K3; ++f)
 #pragma unroll
@@ -563,11 +593,12 @@ struct Worker {
             }
           }
       }
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
-      __syncthreads();
-      if (i + 2 < n) fetch(i & 1, end - t0 - 2 * kChunk);
-      if (!kStateOnly) {
-        const float* A = reinterpret_cast<const float*>(sm + Sh::oA + (i & 1) * Sh::kTriangles) + g * 8 + q * 2;
+      stage = stage == Sh::kStages - 1 ? 0 : stage + 1;
+      if (kStateOnly) {
+        bar_arrive(kEmpty + turn, 2 * Sh::kThreads);
+      } else {
+        bar_sync(kMultipliers, Sh::kThreads);          // the sums of the block below the triangles
+        const float* A = reinterpret_cast<const float*>(set + Sh::kA) + g * 8 + q * 2;
         float2 up = *reinterpret_cast<const float2*>(A), dn = *reinterpret_cast<const float2*>(A + 64);
 #pragma unroll
         for (int x = 1; x < N / 64; ++x) {
@@ -577,6 +608,7 @@ struct Worker {
         pair mid = load2(reinterpret_cast<const float*>(sm + Sh::oMid) + g * 8 + q * 2);
 #pragma unroll
         for (int x = 1; x < Sh::kSteps; ++x) mid = add2(mid, load2(reinterpret_cast<const float*>(sm + Sh::oMid) + x * 64 + g * 8 + q * 2));
+        bar_arrive(kEmpty + turn, 2 * Sh::kThreads);
         uint32_t a0[Sh::R], a1[Sh::R], a3[Sh::R];
         split<Sh::R>(pair_of(up.x, up.y), a0);
         split<Sh::R>(mid, a1);
@@ -607,11 +639,6 @@ struct Worker {
           }
         }
       }
-      if (i + 1 < n) {
-        if (kStateOnly) state_operands((i + 1) & 1);
-        else operands((i + 1) & 1);
-      }
-      __syncthreads();
     }
   }
 
@@ -623,6 +650,12 @@ struct Worker {
 #pragma unroll
       for (int e = 0; e < 4; ++e) S[j][e] = s ? __ldg(s + (j * 8 + (lane & 3) * 2 + (e & 1)) * N + (e >> 1) * 8) : 0.f;
   }
+  __device__ __forceinline__ void clear_state() {
+#pragma unroll
+    for (int j = 0; j < Sh::kTiles; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[j][e] = 0.f;
+  }
   __device__ __forceinline__ void store_state(int slot) {
     float* s = p.a.state_out + ((size_t)slot * p.a.heads + h) * Sh::kStateFloats + warp * 16 + (lane >> 2);
 #pragma unroll
@@ -632,7 +665,7 @@ struct Worker {
   }
   // States in the workspace: as the registers hold them.  which: 0 what the block's last piece comes to, 1 what its sequence began with.
   __device__ __forceinline__ float* block_state(int block, int which) const {
-    return p.block_states + ((size_t)block * p.a.heads + h) * Sh::kBlockFloats + which * Sh::kStateFloats;
+    return p.block_states + (size_t)block * Sh::kBlockFloats + which * Sh::kStateFloats;
   }
   __device__ __forceinline__ void keep(float* to) const {
 #pragma unroll
@@ -642,118 +675,143 @@ struct Worker {
   __device__ __forceinline__ float4 kept(const float* from, int j) const { return reinterpret_cast<const float4*>(from)[(warp * Sh::kTiles + j) * 32 + lane]; }
 };
 
-// The next sequence from `from` on that has rows in [row0, row1) and is longer than the limit; n_seq: none.  Called by the whole block.
-__device__ __forceinline__ int next_sequence(const Args& p, int from, int row0, int row1, int* word) {
-  if (threadIdx.x == 0) *word = p.a.n_seq;
-  __syncthreads();
-  int found = p.a.n_seq;
-  for (int i = from + (int)threadIdx.x; i < p.a.n_seq; i += (int)blockDim.x) {
-    const Entry e = p.entries[i];
-    if (e.end - e.start > p.limit && e.end > row0 && e.start < row1) { found = i; break; }
+// A 64-bit division takes a hundred instructions, and few calls have as many rows.
+__device__ __forceinline__ int quotient(long long a, long long b) { return ((a | b) >> 32) != 0 ? (int)(a / b) : (int)((uint32_t)a / (uint32_t)b); }
+
+// The next sequence from `from` on that has rows in [row0, row1) and is longer than the limit; n_seq: none.  Called by whole warps.
+__device__ __forceinline__ int next_sequence(const Args& p, int from, int row0, int row1) {
+  for (int base = from; base < p.a.n_seq; base += 32) {
+    const int i = base + (int)(threadIdx.x & 31);
+    bool here = false;
+    if (i < p.a.n_seq) {
+      const Entry e = p.entries[i];
+      here = e.end - e.start > p.limit && e.end > row0 && e.start < row1;
+    }
+    const uint32_t found = __ballot_sync(0xFFFFFFFFu, here);
+    if (found) return base + __ffs((int)found) - 1;
   }
-  found = __reduce_min_sync(0xFFFFFFFFu, found);
-  if ((threadIdx.x & 31) == 0) atomicMin(word, found);
-  __syncthreads();
-  found = *word;
-  __syncthreads();
-  return found;
+  return p.a.n_seq;
 }
 
-#ifndef LA_PER_SM1
-#define LA_PER_SM1 5
-#endif
 #ifndef LA_PER_SM
-#define LA_PER_SM 4
+#define LA_PER_SM 2
 #endif
-constexpr int kPerSm = LA_PER_SM;
+constexpr int kPerSm = LA_PER_SM;      // blocks of 256 threads an SM holds
 template <typename T, int N, int kDecay, bool kStateOnly>
-__global__ void __launch_bounds__(2 * N, N == 64 && sizeof(T) == 2 ? (kStateOnly ? LA_PER_SM1 : kPerSm) : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
+__global__ void __launch_bounds__(4 * N, N == 64 ? (kStateOnly ? 3 : kPerSm) : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
   using Sh = Shape<T, N, kStateOnly>;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int word;
   Worker<T, N, kDecay, kStateOnly> w(p, smem);
-  const int block = blockIdx.x, row0 = block * p.block_rows, row1 = min(row0 + p.block_rows, p.a.tokens);
-  if (!kStateOnly) {
-    for (int i = threadIdx.x; i < 2 * Sh::kTriangles / 4; i += Sh::kThreads) reinterpret_cast<float*>(smem + Sh::oA)[i] = 0.f;       // above the diagonals it stays zero
+  const bool maker = threadIdx.x < Sh::kThreads;
+  const int block = blockIdx.x, tokens = p.a.tokens;
+  const long long f0 = block * p.block_rows, f1 = min(f0 + p.block_rows, p.a.heads * p.pitch);
+  if (kStateOnly) {
+    // the blocks' pass may begin as soon as there is room for it: it waits for this one where it needs the states
+    asm volatile("griddepcontrol.launch_dependents;");
+  } else {
+    // above the diagonals it stays zero
+    for (int i = w.tid; i < Sh::kTriangles / 4; i += Sh::kThreads) reinterpret_cast<float*>(smem + Sh::oSets + (maker ? 0 : Sh::kSet) + Sh::kA)[i] = 0.f;
+    __syncthreads();
   }
-  for (int seq = 0;; ++seq) {
-    Entry e = {0, p.a.tokens, 0, 0};
-    if (p.entries) {
-      seq = next_sequence(p, seq, row0, row1, &word);
-      if (seq >= p.a.n_seq) break;
-      e = p.entries[seq];
-    } else if (seq > 0) {
-      break;
-    }
-    const int begin = max(e.start, row0), end = min(e.end, row1);
-    if (kStateOnly) {
-      // the blocks' pass may begin as soon as there is room for it: it waits for this one where it needs the states
-      asm volatile("griddepcontrol.launch_dependents;");
-      if (e.end <= row1) continue;
-      if (e.start >= row0) {
-        w.load_state(e.slot);
-        w.keep(w.block_state(block, 1));       // for the pass that follows: by then the last of its blocks may have written the new state over it
-      } else {
-#pragma unroll
-        for (int j = 0; j < Sh::kTiles; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w.S[j][i] = 0.f;
+  // A block's head, or heads; of the states' pass the last one only, and of that the sequence that goes on behind the block.
+  for (w.h = quotient(kStateOnly ? f1 - 1 : f0, p.pitch); w.h * p.pitch < f1; ++w.h) {
+    const long long head0 = w.h * p.pitch;
+    const int row0 = (int)max(f0 - head0, 0ll), row1 = (int)min(f1 - head0, (long long)tokens);
+    for (int seq = 0;; ++seq) {
+      Entry e = {0, tokens, 0, 0};
+      if (p.entries) {
+        seq = next_sequence(p, seq, row0, row1);
+        if (seq >= p.a.n_seq) break;
+        e = p.entries[seq];
+      } else if (seq > 0) {
+        break;
       }
-      w.total = pair_of(0.f, 0.f);
-      w.first_rows(begin, end);
-      w.rows(begin, end);
-      w.keep(w.block_state(block, 0));
-      if ((w.warp & 3) == 3) {
-        const float2 f = both(w.total);
-        *reinterpret_cast<float2*>(w.block_state(block, 2) + (w.warp >> 2) * 64 + w.lane * 2) = make_float2(expf(f.x), expf(f.y));
-      }
-      return;
-    }
-    w.first_rows(begin, end);
-    if (e.start < row0 || e.end > row1) {
-      asm volatile("griddepcontrol.wait;" ::: "memory");
-      // from the workspace: what the sequence began with, or what the blocks before this one make of it
-      const int b0 = e.start >= row0 ? block : e.start / p.block_rows;
-      const float* from = w.block_state(b0, e.start >= row0 ? 1 : 0);
-#pragma unroll
-      for (int j = 0; j < Sh::kTiles; ++j) { const float4 x = w.kept(from, j); w.S[j][0] = x.x; w.S[j][1] = x.y; w.S[j][2] = x.z; w.S[j][3] = x.w; }
-#pragma unroll 2
-      for (int b = b0 + 1; b < block; ++b) {
-        const float* add = w.block_state(b, 0);
-        const float* decay = w.block_state(b, 2) + (w.lane & 3) * 2;
-#pragma unroll
-        for (int j = 0; j < Sh::kTiles; ++j) {
-          const float4 x = w.kept(add, j);
-          const float2 d = *reinterpret_cast<const float2*>(decay + j * 8);
-          w.S[j][0] = fmaf(w.S[j][0], d.x, x.x); w.S[j][1] = fmaf(w.S[j][1], d.y, x.y);
-          w.S[j][2] = fmaf(w.S[j][2], d.x, x.z); w.S[j][3] = fmaf(w.S[j][3], d.y, x.w);
+      const int begin = max(e.start, row0), end = min(e.end, row1);
+      if (kStateOnly) {
+        if (e.end <= row1) continue;
+        if (maker) {
+          w.total = pair_of(0.f, 0.f);
+          w.make(begin, end);
+          w.made();
+          if ((w.warp & 3) == 3) {
+            const float2 f = both(w.total);
+            *reinterpret_cast<float2*>(w.block_state(block, 2) + (w.warp >> 2) * 64 + w.lane * 2) = make_float2(expf(f.x), expf(f.y));
+          }
+          return;
         }
+        if (e.start >= row0) {
+          w.load_state(e.slot);
+          w.keep(w.block_state(block, 1));       // for the pass that follows: by then the last of its blocks may have written the new state over it
+        } else {
+          w.clear_state();
+        }
+        w.multiply(begin, end);
+        w.keep(w.block_state(block, 0));
+        return;
       }
-    } else {
-      w.load_state(e.slot);
+      if (maker) {
+        w.make(begin, end);
+        continue;
+      }
+      if (e.start < row0 || e.end > row1) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        // from the workspace: what the sequence began with, or what the blocks before this one make of it
+        const int b0 = e.start >= row0 ? block : quotient(head0 + e.start, p.block_rows);
+        const float* from = w.block_state(b0, e.start >= row0 ? 1 : 0);
+#pragma unroll
+        for (int j = 0; j < Sh::kTiles; ++j) { const float4 x = w.kept(from, j); w.S[j][0] = x.x; w.S[j][1] = x.y; w.S[j][2] = x.z; w.S[j][3] = x.w; }
+        for (int b = b0 + 1; b < block; ++b) {
+          const float* add = w.block_state(b, 0);
+          const float* decay = w.block_state(b, 2) + (w.lane & 3) * 2;
+#pragma unroll
+          for (int j = 0; j < Sh::kTiles; ++j) {
+            const float4 x = w.kept(add, j);
+            const float2 d = *reinterpret_cast<const float2*>(decay + j * 8);
+            w.S[j][0] = fmaf(w.S[j][0], d.x, x.x); w.S[j][1] = fmaf(w.S[j][1], d.y, x.y);
+            w.S[j][2] = fmaf(w.S[j][2], d.x, x.z); w.S[j][3] = fmaf(w.S[j][3], d.y, x.w);
+          }
+        }
+      } else {
+        w.load_state(e.slot);
+      }
+      w.multiply(begin, end);
+      if (e.end <= row1 && p.a.state_out && e.slot >= 0) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");      // it may be written where the pass before read it
+        w.store_state(e.slot);
+      }
     }
-    w.rows(begin, end);
-    asm volatile("griddepcontrol.wait;" ::: "memory");      // a state may be written where the pass before read it
-    if (e.end <= row1 && p.a.state_out && e.slot >= 0) w.store_state(e.slot);
   }
+  if (!kStateOnly && maker) w.made();
   if (!kStateOnly) asm volatile("griddepcontrol.wait;" ::: "memory");      // a block without rows does not end before the pass in front of it, either
 }
 
 // Rows of a block and how many blocks.  A block's warps work on one head; about four thread blocks fit an SM.
-struct Plan { int block_rows, blocks, limit; size_t entries_bytes, bytes; };
-constexpr int kShortest = 8;
+struct Plan { long long block_rows, pitch; int blocks, limit; size_t entries_bytes, bytes; };
+constexpr int kShortest = 8, kLeastChunks = 3;
 Plan plan_of(int tokens, int n_seq, int heads, int n) {
-  Plan l = {0, 0, 0x7FFFFFFF, 0, 0};
-  if (tokens <= std::max<long long>(kShortest, 2ll * n_seq)) return l;        // all by the token kernel
-  const long long most = std::max<long long>(1, (long long)sm_count() * (n == 64 ? kPerSm : 1) / heads);
-  const long long rows = std::max<long long>(64, ((tokens + most - 1) / most + kChunk - 1) / kChunk * kChunk);
-  l.block_rows = (int)std::min<long long>(rows, 1 << 30);
-  l.blocks = (int)((tokens + (long long)l.block_rows - 1) / l.block_rows);
-  l.limit = kShortest;
+  Plan l = {0, 0, 0, 0x7FFFFFFF, 0, 0};
+  const int sms = sm_count(), per_sm = n == 64 ? kPerSm : 1;
+  const long long all = (long long)heads * tokens, most = (long long)sms * per_sm;
+  if (tokens <= kShortest) return l;
+  // as much as fewer tokens or sequences could ask for
   l.entries_bytes = round_up_sz((size_t)n_seq * sizeof(Entry), 256);
-  // as much as any fewer tokens could ask for
-  const long long bound = std::min<long long>(most, (tokens + 63ll) / 64);
-  l.bytes = l.entries_bytes + (bound > 1 ? (size_t)bound * heads * (2 * n * n + n) * 4 : 0);
+  l.bytes = l.entries_bytes + (size_t)std::min(most, all / (2 * kChunk) + 1) * (2 * n * n + n) * 4;
+  if (tokens <= 2ll * n_seq) return l;        // all by the token kernel
+  // An SM has kPerSm blocks at work, a chunk of 16 rows every so often (0.95 us with two or three, 1.05 alone); a sequence's last block adds up the states of
+  // those before it.  Blocks of one head each, or, where that leaves SMs idle, the heads' rows cut evenly: some blocks then begin anew at a second head (2048 rows of
+  // 64 heads: six blocks each 77.8 us, even 74.4; 203 of 32 heads: four each 11.1, even 16.5).
+  auto chunk_time = [&](long long blocks) { return std::max(0.95 * (double)((blocks + sms - 1) / sms), 1.05); };
+  double best = 0.0;
+  for (int b = 1; b == 1 || ((long long)b * heads <= most && b <= 64); ++b) {
+    const long long rows = ((long long)tokens + b - 1) / b, chunks = (rows + kChunk - 1) / kChunk;
+    if (b > 1 && chunks < kLeastChunks) break;
+    const double t = (double)chunks * chunk_time((long long)b * heads) + 0.4 * (b - 1) + (b > 1 ? 3.0 + 0.45 * (double)chunks * (b - 1) / b : 0.0);
+    if (b == 1 || t < best) { best = t; l.block_rows = chunks * kChunk; l.pitch = b * l.block_rows; l.blocks = b * heads; }
+  }
+  const long long even = std::max<long long>(kLeastChunks * kChunk, ((all + most - 1) / most + kChunk - 1) / kChunk * kChunk), blocks = (all + even - 1) / even;
+  const double t = (double)(even / kChunk + 1) * (chunk_time(blocks) + 0.45) + 0.4 * (double)(tokens / even) + 6.0;
+  if (t < best) { l.block_rows = even; l.pitch = tokens; l.blocks = (int)blocks; }
+  l.limit = kShortest;
   return l;
 }
 
@@ -763,20 +821,21 @@ cudaError_t launch_chunks(const Args& p, const Plan& l, cudaStream_t s) {
   using States = Shape<T, N, true>;
   static SmemOptIn opt_state(kCarveOut), opt_all(kCarveOut);
   cudaError_t e = opt_all((const void*)linattn_chunk_kernel<T, N, kDecay, false>, All::kBytes);
-  if (e == cudaSuccess && l.blocks > 1) {
+  const bool two_passes = l.pitch != l.block_rows;         // else every block is a whole head
+  if (e == cudaSuccess && two_passes) {
     e = opt_state((const void*)linattn_chunk_kernel<T, N, kDecay, true>, States::kBytes);
     if (e == cudaSuccess) {
-      linattn_chunk_kernel<T, N, kDecay, true><<<dim3((unsigned)l.blocks - 1, (unsigned)p.a.heads), States::kThreads, States::kBytes, s>>>(p);
+      linattn_chunk_kernel<T, N, kDecay, true><<<(unsigned)l.blocks - 1, 2 * States::kThreads, States::kBytes, s>>>(p);
       e = cudaGetLastError();
     }
   }
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)l.blocks, (unsigned)p.a.heads); cfg.blockDim = dim3(All::kThreads); cfg.dynamicSmemBytes = All::kBytes; cfg.stream = s;
+  cfg.gridDim = dim3((unsigned)l.blocks); cfg.blockDim = dim3(2 * All::kThreads); cfg.dynamicSmemBytes = All::kBytes; cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr; cfg.numAttrs = l.blocks > 1 ? 1 : 0;
+  cfg.attrs = attr; cfg.numAttrs = two_passes ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, linattn_chunk_kernel<T, N, kDecay, false>, p);
 }
 template <typename T, int N>
@@ -837,9 +896,9 @@ rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace, size
     if (x < y + bytes && y < x + bytes) return RWKVQ_EINVAL;
   }
   const la::Plan l = la::plan_of(a.tokens, a.n_seq, a.heads, a.n);
-  if (l.bytes > 0 && (!workspace || workspace_bytes < l.bytes)) return RWKVQ_ENOMEM;
+  if (l.blocks > 0 && (!workspace || workspace_bytes < l.bytes)) return RWKVQ_ENOMEM;
   if (!aligned16(workspace)) return RWKVQ_EALIGN;
-  p.limit = l.limit; p.block_rows = l.block_rows; p.blocks = l.blocks;
+  p.limit = l.limit; p.block_rows = l.block_rows; p.pitch = l.pitch; p.blocks = l.blocks;
   p.entries = l.blocks > 0 && (a.seq_start || a.slots) ? static_cast<la::Entry*>(workspace) : nullptr;
   p.block_states = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + l.entries_bytes);
   p.status = device_status_ptr();

@@ -50,11 +50,12 @@ def test_binding_refuses():
 
 def test_workspace():
     size = B.rwkvq_linattn_workspace_bytes
-    assert size(1, 1, 4, 64) == size(64, 64, 4, 64) == size(100, 1, 4, 32) == size(-1, 1, 4, 64) == size(5, 0, 4, 64) == 0
+    assert size(1, 1, 4, 64) == size(8, 8, 4, 64) == size(100, 1, 4, 32) == size(-1, 1, 4, 64) == size(5, 0, 4, 64) == 0
     for heads, n in ((1, 64), (32, 64), (64, 64), (300, 64), (5, 128)):
         last = 0
         for tokens in list(range(9, 700, 7)) + [1000, 2048, 4100, 9999, 70001]:
             assert size(tokens, 1, heads, n) >= last, (tokens, heads, n)
+            assert size(tokens, tokens, heads, n) >= size(tokens, 1, heads, n)
             last = size(tokens, 1, heads, n)
     need = size(5000, 2, 2, 64)
     assert need > 0
