@@ -252,6 +252,7 @@ struct Worker {
   static constexpr int kPieces = N * (int)sizeof(T) / 16, kRowsAtOnce = Sh::kThreads / kPieces;
   static constexpr int kDecaySize = kDecay == DECAY_F32 ? 4 : (int)sizeof(T), kDecayPieces = N * kDecaySize / 16, kDecayRowsAtOnce = Sh::kThreads / kDecayPieces;
   const uint8_t *rp, *kp, *vp, *lp;
+  float ahead;
   pair bonus;                  // u of this thread's channels
   int place, place2;           // bytes into a triangle of A of the entries that this lane ends up with
 
@@ -272,6 +273,11 @@ struct Worker {
     if (kDecay == DECAY_HEAD) lp = static_cast<const uint8_t*>(a.logw) + ((t0 + (tid & 15)) * a.logw_row + h) * (a.decay_dtype == RWKVQ_F32 ? 4 : (int)sizeof(T));
     else lp = static_cast<const uint8_t*>(a.logw) + ((t0 + tid / kDecayPieces) * a.logw_row + (long long)h * N) * kDecaySize + tid % kDecayPieces * 16;
   }
+  // One decay per head: the next chunk's, `left` rows of it in the sequence.
+  __device__ __forceinline__ void head_decay(int left) {
+    if (tid < kChunk && tid < left)
+      ahead = p.a.decay_dtype == RWKVQ_F32 ? *reinterpret_cast<const float*>(lp) : to_f32(*reinterpret_cast<const T*>(lp));
+  }
   // The next 16 rows into a raw stage, `left` of them in the sequence; zeros (no decay, nothing to add) behind.
   __device__ __forceinline__ void fetch(int stage, int left) {
     const rwkvq_linattn_args& a = p.a;
@@ -288,9 +294,10 @@ struct Worker {
     }
     uint8_t* lw = sm + stage * Sh::kStage + Sh::kL;
     if (kDecay == DECAY_HEAD) {
-      const bool f32 = a.decay_dtype == RWKVQ_F32;
-      if (tid < kChunk) reinterpret_cast<float*>(lw)[tid] = tid >= left ? 0.f : f32 ? *reinterpret_cast<const float*>(lp) : to_f32(*reinterpret_cast<const T*>(lp));
-      lp += a.logw_row * ((f32 ? 4 : (int)sizeof(T)) * kChunk);
+      // a plain load, one chunk ahead: what it brings is stored when the next chunk is asked for
+      if (tid < kChunk) reinterpret_cast<float*>(lw)[tid] = tid < left ? ahead : 0.f;
+      lp += a.logw_row * ((a.decay_dtype == RWKVQ_F32 ? 4 : (int)sizeof(T)) * kChunk);
+      head_decay(left - kChunk);
     } else {
 #pragma unroll
       for (int i = 0; i < kChunk / kDecayRowsAtOnce; ++i) {
@@ -482,6 +489,7 @@ struct Worker {
     const int n = (end - begin + kChunk - 1) / kChunk;
     if (!kStateOnly) bonus = p.a.u ? load2(p.a.u + h * N + (warp >> 2) * 64 + lane * 2) : ones();
     fetch_from(begin);
+    if (kDecay == DECAY_HEAD) head_decay(end - begin);
     fetch(stage, end - begin);
     for (int i = 0; i < n; ++i, ++count) {
       const int set = count & 1;
