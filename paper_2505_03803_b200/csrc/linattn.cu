@@ -148,20 +148,24 @@ constexpr int kChunk = 16, kHalf = 8, K3 = 3;
 
 template <typename T, int N, bool kStateOnly>
 struct Shape {
-  static constexpr int kThreads = 2 * N, kTiles = N / 8, kSteps = N / 16;
+  // Warps that make operands, warps that multiply: each of these has kValues tiles of 16 value columns.  Two, so that what they read of r P and k Q serves more
+  // products: 72.3 -> 69.2 us (2048 tokens, 64 heads, bf16); with fp16's two terms of v it is slower, 174 -> 185 (ragged, 5000 rows), and of heads of 128 the states of two
+  // would not fit the registers.
+  static constexpr int kValues = N == 64 && Terms<T>::V == 1 ? 2 : 1, kThreads = 2 * N, kMulThreads = 2 * N / kValues, kAll = kThreads + kMulThreads;
+  static constexpr int kTiles = N / 8, kSteps = N / 16, kMidSteps = kSteps / (kMulThreads / 32);
   static constexpr int R = Terms<T>::R, V = Terms<T>::V;
   static constexpr int kPitch = (N + 8) * 2;                      // bytes of a row of terms: an odd number of 16 bytes, no conflicts for ldmatrix
   static constexpr int kRawPitch = N * (int)sizeof(T) + 16, kDecayPitch = N * 4 + 16;
   static constexpr int kTerm = kChunk * kPitch, kHalfTerm = kHalf * kPitch, kRaw = kChunk * kRawPitch;
   // a raw stage: r (where there are outputs), k, v, logarithms of decays
-  static constexpr int kStages = 3;
+  static constexpr int kStages = 3, kAhead = kStages - 2;      // chunks on their way
   static constexpr int kR = 0, kK = kStateOnly ? 0 : kRaw, kV = kK + kRaw, kL = kV + kRaw, kStage = kL + kChunk * kDecayPitch;
   // a set of operands
   static constexpr int kKt = 0, kD = kKt + K3 * kTerm, kVt = kD + N * 4, kRt = kVt + (V > 2 ? V * kTerm : 0);
   // what only outputs need
   static constexpr int kRp = kRt + R * kTerm, kKp = kRp + R * kHalfTerm, kA = kKp + R * kHalfTerm, kTriangles = (N / 64) * 2 * 64 * 4;
   static constexpr int kSet = kStateOnly ? kRt : kA + kTriangles, oSets = kStages * kStage, oMid = oSets + 2 * kSet;
-  static constexpr int kBytes = oMid + (kStateOnly ? 0 : kSteps * 64 * 4);
+  static constexpr int kBytes = oMid + (kStateOnly ? 0 : kMulThreads / 32 * 64 * 4);
   static constexpr int kStateFloats = N * N, kBlockFloats = 2 * N * N + N;
 };
 
@@ -246,7 +250,7 @@ struct Worker {
   uint8_t* sm;
   int h, warp, lane, tid;      // tid, warp: in its role
   int count = 0, stage = 0;    // chunks so far, stage of the next one
-  float S[Sh::kTiles][4];      // S^T: values 16 warp + lane / 4 (+ 8: the last two), keys 8 j + 2 (lane % 4) and the next
+  float S[Sh::kValues][Sh::kTiles][4];      // S^T: values 16 (kValues warp + m) + lane / 4 (+ 8: the last two), keys 8 j + 2 (lane % 4) and the next
   pair total;                  // kStateOnly: sums of the logarithms of the decays of this thread's channels
   // This thread's pieces of 16 bytes of the next chunk to fetch, and bytes from row to row.
   static constexpr int kPieces = N * (int)sizeof(T) / 16, kRowsAtOnce = Sh::kThreads / kPieces;
@@ -483,34 +487,39 @@ struct Worker {
     }
   }
 
-  // Chunks of rows [begin, end), by the warps that make operands.  Chunk i + 1 is on its way while chunk i is worked on; sets and stages go on being used in
+  // Chunks of rows [begin, end), by the warps that make operands.  The next kAhead chunks are on their way while one is worked on; sets and stages go on being used in
   // turn from one piece of rows to the next, so that a piece's first chunks are made while the piece before it is multiplied.
   __device__ __forceinline__ void make(int begin, int end) {
     const int n = (end - begin + kChunk - 1) / kChunk;
     if (!kStateOnly) bonus = p.a.u ? load2(p.a.u + h * N + (warp >> 2) * 64 + lane * 2) : ones();
     fetch_from(begin);
     if (kDecay == DECAY_HEAD) head_decay(end - begin);
-    fetch(stage, end - begin);
+    int into = stage, left = end - begin;            // where the next chunk to fetch goes, and the rows from it on
+    auto next_chunk = [&]() {
+      fetch(into, left);
+      into = into == Sh::kStages - 1 ? 0 : into + 1;
+      left -= kChunk;
+    };
+    for (int i = 0; i < Sh::kAhead && i < n; ++i) next_chunk();
     for (int i = 0; i < n; ++i, ++count) {
       const int set = count & 1;
-      if (count >= 2) bar_sync(kEmpty + set, 2 * Sh::kThreads);       // the chunk before the last is done with: its set of operands, and its stage
-      const int next = stage == Sh::kStages - 1 ? 0 : stage + 1;
-      if (i + 1 < n) {
-        fetch(next, end - begin - (i + 1) * kChunk);
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
+      if (count >= 2) bar_sync(kEmpty + set, Sh::kAll);       // the chunk before the last is done with: its set of operands, and its stage
+      if (i + Sh::kAhead < n) {
+        next_chunk();
+        asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kAhead) : "memory");
       } else {
         asm volatile("cp.async.wait_group 0;" ::: "memory");
       }
       bar_sync(kMakers, Sh::kThreads);
       if (kStateOnly) state_operands(stage, sm + Sh::oSets + set * Sh::kSet);
       else operands(stage, sm + Sh::oSets + set * Sh::kSet);
-      bar_arrive(kFull + set, 2 * Sh::kThreads);
-      stage = next;
+      bar_arrive(kFull + set, Sh::kAll);
+      stage = stage == Sh::kStages - 1 ? 0 : stage + 1;
     }
   }
   // Behind the last piece: what the other warps report is waited for, so that no barrier is left half done.
   __device__ __forceinline__ void made() {
-    for (int i = max(count - 2, 0); i < count; ++i) bar_sync(kEmpty + (i & 1), 2 * Sh::kThreads);
+    for (int i = max(count - 2, 0); i < count; ++i) bar_sync(kEmpty + (i & 1), Sh::kAll);
   }
   // The same chunks by the warps that multiply.
   __device__ __forceinline__ void multiply(int begin, int end) {
@@ -519,63 +528,77 @@ struct Worker {
     for (int i = 0; i < n; ++i, ++count) {
       const int t0 = begin + i * kChunk, turn = count & 1;
       const uint8_t* set = sm + Sh::oSets + turn * Sh::kSet;
-      bar_sync(kFull + turn, 2 * Sh::kThreads);
-      float o[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      bar_sync(kFull + turn, Sh::kAll);
+      float o[Sh::kValues][2][4];
       if (!kStateOnly) {
+#pragma unroll
+        for (int m = 0; m < Sh::kValues; ++m)
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[m][nb][x] = 0.f;
         {
-          // the block of A below the triangles: warp w adds up sixteen keys.  Rows of r P' (lanes 0-15) and of k Q' (16-31), eight keys and the next
+          // the block of A below the triangles: each warp adds up its share of the keys.  Rows of r P' (lanes 0-15) and of k Q' (16-31), eight keys and the next
           float mid[4] = {0.f, 0.f, 0.f, 0.f};
-          const uint32_t half = smem_u32(set + (lane < 16 ? Sh::kRp : Sh::kKp)) + (lane & 7) * Sh::kPitch + ((lane >> 3) & 1) * 16 + warp * 32;
-          uint32_t y[Sh::R][4];
+          const uint32_t half = smem_u32(set + (lane < 16 ? Sh::kRp : Sh::kKp)) + (lane & 7) * Sh::kPitch + ((lane >> 3) & 1) * 16 + warp * Sh::kMidSteps * 32;
 #pragma unroll
-          for (int e = 0; e < Sh::R; ++e) ldsm4(half + e * Sh::kHalfTerm, y[e]);
+          for (int k = 0; k < Sh::kMidSteps; ++k) {
+            uint32_t y[Sh::R][4];
 #pragma unroll
-          for (int e = 0; e < Sh::R; ++e)
+            for (int e = 0; e < Sh::R; ++e) ldsm4(half + e * Sh::kHalfTerm + k * 32, y[e]);
 #pragma unroll
-            for (int f = 0; f < Sh::R - e; ++f) {
-              const uint32_t low[4] = {0u, y[e][0], 0u, y[e][1]};
-              mma(mid, low, y[f][2], y[f][3]);
-            }
+            for (int e = 0; e < Sh::R; ++e)
+#pragma unroll
+              for (int f = 0; f < Sh::R - e; ++f) {
+                const uint32_t low[4] = {0u, y[e][0], 0u, y[e][1]};
+                mma(mid, low, y[f][2], y[f][3]);
+              }
+          }
           *reinterpret_cast<float2*>(sm + Sh::oMid + (warp * 64 + g * 8 + q * 2) * 4) = make_float2(mid[2], mid[3]);
         }
         const uint32_t rt = smem_u32(set + Sh::kRt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
 #pragma unroll
         for (int k = 0; k < Sh::kSteps; ++k) {
-          uint32_t x[Sh::R][4], b[2][2][Sh::R];
+          uint32_t x[Sh::R][4];
 #pragma unroll
           for (int e = 0; e < Sh::R; ++e) ldsm4(rt + e * Sh::kTerm + k * 32, x[e]);
 #pragma unroll
-          for (int nb = 0; nb < 2; ++nb)
+          for (int m = 0; m < Sh::kValues; ++m) {
+            uint32_t b[2][2][Sh::R];
 #pragma unroll
-            for (int m = 0; m < 2; ++m) split<Sh::R>(pair_of(S[2 * k + m][2 * nb], S[2 * k + m][2 * nb + 1]), b[nb][m]);
+            for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-          for (int e = 0; e < Sh::R; ++e)
+              for (int i2 = 0; i2 < 2; ++i2) split<Sh::R>(pair_of(S[m][2 * k + i2][2 * nb], S[m][2 * k + i2][2 * nb + 1]), b[nb][i2]);
 #pragma unroll
-            for (int f = 0; f < Sh::R - e; ++f) {
-              mma(o[0], x[e], b[0][0][f], b[0][1][f]);
-              mma(o[1], x[e], b[1][0][f], b[1][1][f]);
-            }
+            for (int e = 0; e < Sh::R; ++e)
+#pragma unroll
+              for (int f = 0; f < Sh::R - e; ++f) {
+                mma(o[m][0], x[e], b[0][0][f], b[0][1][f]);
+                mma(o[m][1], x[e], b[1][0][f], b[1][1][f]);
+              }
+          }
         }
       }
       // values of the chunk's tokens: an operand of both products that follow
-      uint32_t v[Sh::V][4];
-      {
-        const int row = (lane & 7) + (lane >> 4) * 8, col = warp * 16 + ((lane >> 3) & 1) * 8;
+      uint32_t v[Sh::kValues][Sh::V][4];
+#pragma unroll
+      for (int m = 0; m < Sh::kValues; ++m) {
+        const int row = (lane & 7) + (lane >> 4) * 8, col = (warp * Sh::kValues + m) * 16 + ((lane >> 3) & 1) * 8;
         if constexpr (Sh::V > 2) {
           const uint32_t at = smem_u32(set + Sh::kVt) + row * Sh::kPitch + col * 2;
 #pragma unroll
-          for (int e = 0; e < Sh::V; ++e) ldsm4t(at + e * Sh::kTerm, v[e]);
+          for (int e = 0; e < Sh::V; ++e) ldsm4t(at + e * Sh::kTerm, v[m][e]);
         } else {
           uint32_t x[4];
           ldsm4t(smem_u32(sm + stage * Sh::kStage + Sh::kV) + row * Sh::kRawPitch + col * 2, x);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            if constexpr (Sh::V == 1) v[0][j] = x[j];
+            if constexpr (Sh::V == 1) v[m][0][j] = x[j];
             else {
               uint32_t t[Sh::V];
               split<Sh::V>(widen(x[j], T()), t);
 #pragma unroll
-              for (int e = 0; e < Sh::V; ++e) v[e][j] = t[e];
+              for (int e = 0; e < Sh::V; ++e) v[m][e][j] = t[e];
             }
           }
         }
@@ -583,8 +606,12 @@ struct Worker {
 #pragma unroll
       for (int j = 0; j < Sh::kTiles; ++j) {
         const pair d = *reinterpret_cast<const pair*>(set + Sh::kD + (j * 8 + q * 2) * 4);
-        const float2 lo = both(mul2(pair_of(S[j][0], S[j][1]), d)), hi = both(mul2(pair_of(S[j][2], S[j][3]), d));
-        S[j][0] = lo.x; S[j][1] = lo.y; S[j][2] = hi.x; S[j][3] = hi.y;
+#pragma unroll
+        for (int m = 0; m < Sh::kValues; ++m) {
+          float(&c)[4] = S[m][j];
+          const float2 lo = both(mul2(pair_of(c[0], c[1]), d)), hi = both(mul2(pair_of(c[2], c[3]), d));
+          c[0] = lo.x; c[1] = lo.y; c[2] = hi.x; c[3] = hi.y;
+        }
       }
       {
         const uint32_t kt = smem_u32(set + Sh::kKt) + (lane & 15) * Sh::kPitch + (lane >> 4) * 16;
@@ -595,55 +622,59 @@ struct Worker {
             uint32_t b[4];
             ldsm4t(kt + f * Sh::kTerm + k * 32, b);
 #pragma unroll
-            for (int e = 0; e < Sh::V && e + f < K3; ++e) {
-              mma(S[2 * k], v[e], b[0], b[1]);
-              mma(S[2 * k + 1], v[e], b[2], b[3]);
-            }
+            for (int m = 0; m < Sh::kValues; ++m)
+#pragma unroll
+              for (int e = 0; e < Sh::V && e + f < K3; ++e) {
+                mma(S[m][2 * k], v[m][e], b[0], b[1]);
+                mma(S[m][2 * k + 1], v[m][e], b[2], b[3]);
+              }
           }
       }
       stage = stage == Sh::kStages - 1 ? 0 : stage + 1;
       if (kStateOnly) {
-        bar_arrive(kEmpty + turn, 2 * Sh::kThreads);
+        bar_arrive(kEmpty + turn, Sh::kAll);
       } else {
-        bar_sync(kMultipliers, Sh::kThreads);          // the sums of the block below the triangles
+        bar_sync(kMultipliers, Sh::kMulThreads);          // the sums of the block below the triangles
         const float* A = reinterpret_cast<const float*>(set + Sh::kA) + g * 8 + q * 2;
-        float2 up = *reinterpret_cast<const float2*>(A), dn = *reinterpret_cast<const float2*>(A + 64);
+        pair up = load2(A), dn = load2(A + 64);
 #pragma unroll
-        for (int x = 1; x < N / 64; ++x) {
-          const float2 up2 = *reinterpret_cast<const float2*>(A + x * 128), dn2 = *reinterpret_cast<const float2*>(A + x * 128 + 64);
-          up.x += up2.x; up.y += up2.y; dn.x += dn2.x; dn.y += dn2.y;
-        }
+        for (int x = 1; x < N / 64; ++x) { up = add2(up, load2(A + x * 128)); dn = add2(dn, load2(A + x * 128 + 64)); }
         pair mid = load2(reinterpret_cast<const float*>(sm + Sh::oMid) + g * 8 + q * 2);
 #pragma unroll
-        for (int x = 1; x < Sh::kSteps; ++x) mid = add2(mid, load2(reinterpret_cast<const float*>(sm + Sh::oMid) + x * 64 + g * 8 + q * 2));
-        bar_arrive(kEmpty + turn, 2 * Sh::kThreads);
+        for (int x = 1; x < Sh::kMulThreads / 32; ++x) mid = add2(mid, load2(reinterpret_cast<const float*>(sm + Sh::oMid) + x * 64 + g * 8 + q * 2));
+        bar_arrive(kEmpty + turn, Sh::kAll);
         uint32_t a0[Sh::R], a1[Sh::R], a3[Sh::R];
-        split<Sh::R>(pair_of(up.x, up.y), a0);
+        split<Sh::R>(up, a0);
         split<Sh::R>(mid, a1);
-        split<Sh::R>(pair_of(dn.x, dn.y), a3);
+        split<Sh::R>(dn, a3);
 #pragma unroll
         for (int e = 0; e < Sh::R; ++e) {
           const uint32_t x[4] = {a0[e], a1[e], 0u, a3[e]};
 #pragma unroll
-          for (int f = 0; f < Sh::V && e + f < Sh::R; ++f) {
-            mma(o[0], x, v[f][0], v[f][2]);
-            mma(o[1], x, v[f][1], v[f][3]);
-          }
-        }
-        T* out = static_cast<T*>(a.out) + (long long)h * N + warp * 16 + q * 2;
+          for (int f = 0; f < Sh::V && e + f < Sh::R; ++f)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          const int row = t0 + g + 8 * m;
-          if (row < end) {
-#pragma unroll
-            for (int nb = 0; nb < 2; ++nb) {
-              T* at = out + row * a.out_row + nb * 8;
-              if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(at) = make_float2(o[nb][2 * m], o[nb][2 * m + 1]);
-              else {
-                const T pair[2] = {from_f32<T>(o[nb][2 * m]), from_f32<T>(o[nb][2 * m + 1])};
-                *reinterpret_cast<uint32_t*>(at) = *reinterpret_cast<const uint32_t*>(pair);
-              }
+            for (int m = 0; m < Sh::kValues; ++m) {
+              mma(o[m][0], x, v[m][f][0], v[m][f][2]);
+              mma(o[m][1], x, v[m][f][1], v[m][f][3]);
             }
+        }
+        T* out = static_cast<T*>(a.out) + (long long)h * N + warp * Sh::kValues * 16 + q * 2;
+#pragma unroll
+        for (int i2 = 0; i2 < 2; ++i2) {
+          const int row = t0 + g + 8 * i2;
+          if (row < end) {
+            T* at = out + row * a.out_row;
+#pragma unroll
+            for (int m = 0; m < Sh::kValues; ++m)
+#pragma unroll
+              for (int nb = 0; nb < 2; ++nb) {
+                const float x = o[m][nb][2 * i2], y = o[m][nb][2 * i2 + 1];
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(at + m * 16 + nb * 8) = make_float2(x, y);
+                else {
+                  const T two[2] = {from_f32<T>(x), from_f32<T>(y)};
+                  *reinterpret_cast<uint32_t*>(at + m * 16 + nb * 8) = *reinterpret_cast<const uint32_t*>(two);
+                }
+              }
           }
         }
       }
@@ -652,35 +683,64 @@ struct Worker {
 
   // States in the caller's layout [key][value].
   __device__ __forceinline__ void load_state(int slot) {
-    const float* s = p.a.state && slot >= 0 ? p.a.state + ((size_t)slot * p.a.heads + h) * Sh::kStateFloats + warp * 16 + (lane >> 2) : nullptr;
+    const float* s = p.a.state && slot >= 0 ? p.a.state + ((size_t)slot * p.a.heads + h) * Sh::kStateFloats + warp * Sh::kValues * 16 + (lane >> 2) : nullptr;
 #pragma unroll
-    for (int j = 0; j < Sh::kTiles; ++j)
+    for (int m = 0; m < Sh::kValues; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) S[j][e] = s ? __ldg(s + (j * 8 + (lane & 3) * 2 + (e & 1)) * N + (e >> 1) * 8) : 0.f;
+      for (int j = 0; j < Sh::kTiles; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[m][j][e] = s ? __ldg(s + (j * 8 + (lane & 3) * 2 + (e & 1)) * N + m * 16 + (e >> 1) * 8) : 0.f;
   }
   __device__ __forceinline__ void clear_state() {
 #pragma unroll
-    for (int j = 0; j < Sh::kTiles; ++j)
+    for (int m = 0; m < Sh::kValues; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) S[j][e] = 0.f;
+      for (int j = 0; j < Sh::kTiles; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[m][j][e] = 0.f;
   }
   __device__ __forceinline__ void store_state(int slot) {
-    float* s = p.a.state_out + ((size_t)slot * p.a.heads + h) * Sh::kStateFloats + warp * 16 + (lane >> 2);
+    float* s = p.a.state_out + ((size_t)slot * p.a.heads + h) * Sh::kStateFloats + warp * Sh::kValues * 16 + (lane >> 2);
 #pragma unroll
-    for (int j = 0; j < Sh::kTiles; ++j)
+    for (int m = 0; m < Sh::kValues; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[(j * 8 + (lane & 3) * 2 + (e & 1)) * N + (e >> 1) * 8] = S[j][e];
+      for (int j = 0; j < Sh::kTiles; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[(j * 8 + (lane & 3) * 2 + (e & 1)) * N + m * 16 + (e >> 1) * 8] = S[m][j][e];
   }
-  // States in the workspace: as the registers hold them.  which: 0 what the block's last piece comes to, 1 what its sequence began with.
+  // States in the workspace: as the registers hold them.  which: 0 what the block's last piece comes to, 1 what its sequence began with, 2 the piece's decays.
   __device__ __forceinline__ float* block_state(int block, int which) const {
     return p.block_states + (size_t)block * Sh::kBlockFloats + which * Sh::kStateFloats;
   }
+  __device__ __forceinline__ int kept_at(int m, int j) const { return ((warp * Sh::kValues + m) * Sh::kTiles + j) * 32 + lane; }
   __device__ __forceinline__ void keep(float* to) const {
 #pragma unroll
-    for (int j = 0; j < Sh::kTiles; ++j)
-      reinterpret_cast<float4*>(to)[(warp * Sh::kTiles + j) * 32 + lane] = make_float4(S[j][0], S[j][1], S[j][2], S[j][3]);
+    for (int m = 0; m < Sh::kValues; ++m)
+#pragma unroll
+      for (int j = 0; j < Sh::kTiles; ++j) reinterpret_cast<float4*>(to)[kept_at(m, j)] = make_float4(S[m][j][0], S[m][j][1], S[m][j][2], S[m][j][3]);
   }
-  __device__ __forceinline__ float4 kept(const float* from, int j) const { return reinterpret_cast<const float4*>(from)[(warp * Sh::kTiles + j) * 32 + lane]; }
+  __device__ __forceinline__ void take(const float* from) {
+#pragma unroll
+    for (int m = 0; m < Sh::kValues; ++m)
+#pragma unroll
+      for (int j = 0; j < Sh::kTiles; ++j) {
+        const float4 x = reinterpret_cast<const float4*>(from)[kept_at(m, j)];
+        S[m][j][0] = x.x; S[m][j][1] = x.y; S[m][j][2] = x.z; S[m][j][3] = x.w;
+      }
+  }
+  // A block's piece behind what is here.
+  __device__ __forceinline__ void behind(const float* add, const float* decay) {
+#pragma unroll
+    for (int j = 0; j < Sh::kTiles; ++j) {
+      const float2 d = *reinterpret_cast<const float2*>(decay + j * 8 + (lane & 3) * 2);
+#pragma unroll
+      for (int m = 0; m < Sh::kValues; ++m) {
+        const float4 x = reinterpret_cast<const float4*>(add)[kept_at(m, j)];
+        S[m][j][0] = fmaf(S[m][j][0], d.x, x.x); S[m][j][1] = fmaf(S[m][j][1], d.y, x.y);
+        S[m][j][2] = fmaf(S[m][j][2], d.x, x.z); S[m][j][3] = fmaf(S[m][j][3], d.y, x.w);
+      }
+    }
+  }
 };
 
 // A 64-bit division takes a hundred instructions, and few calls have as many rows.
@@ -701,12 +761,9 @@ __device__ __forceinline__ int next_sequence(const Args& p, int from, int row0, 
   return p.a.n_seq;
 }
 
-#ifndef LA_PER_SM
-#define LA_PER_SM 2
-#endif
-constexpr int kPerSm = LA_PER_SM;      // blocks of 256 threads an SM holds
+constexpr int kPerSm = 2, kStatesPerSm = 3;      // thread blocks an SM holds; three of the outputs' pass spill (71 -> 74 us, 9.8 -> 11.1 of 203 tokens)
 template <typename T, int N, int kDecay, bool kStateOnly>
-__global__ void __launch_bounds__(4 * N, N == 64 ? (kStateOnly ? 3 : kPerSm) : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
+__global__ void __launch_bounds__(Shape<T, N, kStateOnly>::kAll, N == 64 ? (kStateOnly ? kStatesPerSm : kPerSm) : 1) linattn_chunk_kernel(const __grid_constant__ Args p) {
   using Sh = Shape<T, N, kStateOnly>;
   extern __shared__ __align__(128) uint8_t smem[];
   Worker<T, N, kDecay, kStateOnly> w(p, smem);
@@ -718,7 +775,8 @@ __global__ void __launch_bounds__(4 * N, N == 64 ? (kStateOnly ? 3 : kPerSm) : 1
     asm volatile("griddepcontrol.launch_dependents;");
   } else {
     // above the diagonals it stays zero
-    for (int i = w.tid; i < Sh::kTriangles / 4; i += Sh::kThreads) reinterpret_cast<float*>(smem + Sh::oSets + (maker ? 0 : Sh::kSet) + Sh::kA)[i] = 0.f;
+    for (int i = (int)threadIdx.x; i < 2 * (Sh::kTriangles / 4); i += Sh::kAll)
+      reinterpret_cast<float*>(smem + Sh::oSets + Sh::kA + (i < Sh::kTriangles / 4 ? 0 : Sh::kSet - Sh::kTriangles))[i] = 0.f;
     __syncthreads();
   }
   // A block's head, or heads; of the states' pass the last one only, and of that the sequence that goes on behind the block.
@@ -765,20 +823,8 @@ __global__ void __launch_bounds__(4 * N, N == 64 ? (kStateOnly ? 3 : kPerSm) : 1
         asm volatile("griddepcontrol.wait;" ::: "memory");
         // from the workspace: what the sequence began with, or what the blocks before this one make of it
         const int b0 = e.start >= row0 ? block : quotient(head0 + e.start, p.block_rows);
-        const float* from = w.block_state(b0, e.start >= row0 ? 1 : 0);
-#pragma unroll
-        for (int j = 0; j < Sh::kTiles; ++j) { const float4 x = w.kept(from, j); w.S[j][0] = x.x; w.S[j][1] = x.y; w.S[j][2] = x.z; w.S[j][3] = x.w; }
-        for (int b = b0 + 1; b < block; ++b) {
-          const float* add = w.block_state(b, 0);
-          const float* decay = w.block_state(b, 2) + (w.lane & 3) * 2;
-#pragma unroll
-          for (int j = 0; j < Sh::kTiles; ++j) {
-            const float4 x = w.kept(add, j);
-            const float2 d = *reinterpret_cast<const float2*>(decay + j * 8);
-            w.S[j][0] = fmaf(w.S[j][0], d.x, x.x); w.S[j][1] = fmaf(w.S[j][1], d.y, x.y);
-            w.S[j][2] = fmaf(w.S[j][2], d.x, x.z); w.S[j][3] = fmaf(w.S[j][3], d.y, x.w);
-          }
-        }
+        w.take(w.block_state(b0, e.start >= row0 ? 1 : 0));
+        for (int b = b0 + 1; b < block; ++b) w.behind(w.block_state(b, 0), w.block_state(b, 2));
       } else {
         w.load_state(e.slot);
       }
@@ -833,13 +879,13 @@ cudaError_t launch_chunks(const Args& p, const Plan& l, cudaStream_t s) {
   if (e == cudaSuccess && two_passes) {
     e = opt_state((const void*)linattn_chunk_kernel<T, N, kDecay, true>, States::kBytes);
     if (e == cudaSuccess) {
-      linattn_chunk_kernel<T, N, kDecay, true><<<(unsigned)l.blocks - 1, 2 * States::kThreads, States::kBytes, s>>>(p);
+      linattn_chunk_kernel<T, N, kDecay, true><<<(unsigned)l.blocks - 1, States::kAll, States::kBytes, s>>>(p);
       e = cudaGetLastError();
     }
   }
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)l.blocks); cfg.blockDim = dim3(2 * All::kThreads); cfg.dynamicSmemBytes = All::kBytes; cfg.stream = s;
+  cfg.gridDim = dim3((unsigned)l.blocks); cfg.blockDim = dim3(All::kAll); cfg.dynamicSmemBytes = All::kBytes; cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
