@@ -580,7 +580,7 @@ struct Worker {
         }
       }
       // values of the chunk's tokens: an operand of both products that follow
-      uint32_t v[Sh::kValues][Sh::V][4];
+      uint32_t v[Sh::kValues][Sh::V][4], wild = 0;         // wild: the top bits of halves with infinities or NaN among them
 #pragma unroll
       for (int m = 0; m < Sh::kValues; ++m) {
         const int row = (lane & 7) + (lane >> 4) * 8, col = (warp * Sh::kValues + m) * 16 + ((lane >> 3) & 1) * 8;
@@ -588,11 +588,14 @@ struct Worker {
           const uint32_t at = smem_u32(set + Sh::kVt) + row * Sh::kPitch + col * 2;
 #pragma unroll
           for (int e = 0; e < Sh::V; ++e) ldsm4t(at + e * Sh::kTerm, v[m][e]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) wild |= (v[m][0][j] & 0x7F807F80u) + 0x00800080u;
         } else {
           uint32_t x[4];
           ldsm4t(smem_u32(sm + stage * Sh::kStage + Sh::kV) + row * Sh::kRawPitch + col * 2, x);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
+            wild |= Sh::V == 1 ? (x[j] & 0x7F807F80u) + 0x00800080u : (x[j] & 0x7C007C00u) + 0x04000400u;
             if constexpr (Sh::V == 1) v[m][0][j] = x[j];
             else {
               uint32_t t[Sh::V];
@@ -630,6 +633,7 @@ struct Worker {
               }
           }
       }
+      const T* values = reinterpret_cast<const T*>(sm + stage * Sh::kStage + Sh::kV);
       stage = stage == Sh::kStages - 1 ? 0 : stage + 1;
       if (kStateOnly) {
         bar_arrive(kEmpty + turn, Sh::kAll);
@@ -642,21 +646,49 @@ struct Worker {
         pair mid = load2(reinterpret_cast<const float*>(sm + Sh::oMid) + g * 8 + q * 2);
 #pragma unroll
         for (int x = 1; x < Sh::kMulThreads / 32; ++x) mid = add2(mid, load2(reinterpret_cast<const float*>(sm + Sh::oMid) + x * 64 + g * 8 + q * 2));
-        bar_arrive(kEmpty + turn, Sh::kAll);
-        uint32_t a0[Sh::R], a1[Sh::R], a3[Sh::R];
-        split<Sh::R>(up, a0);
-        split<Sh::R>(mid, a1);
-        split<Sh::R>(dn, a3);
+        if (__any_sync(0xFFFFFFFFu, (wild & 0x80008000u) != 0)) {
+          // Above the diagonal A is zero, and zero times infinity or NaN is not: a token must not see what comes after it, so its sum stops at itself.
+          const float* parts = reinterpret_cast<const float*>(set + Sh::kA);
+          const float* mids = reinterpret_cast<const float*>(sm + Sh::oMid);
+          for (int i2 = 0; i2 < 2; ++i2) {
+            for (int s = 0; s <= g + 8 * i2; ++s) {
+              float x = 0.f;
+              if (s / 8 == i2) {
+                for (int y = 0; y < N / 64; ++y) x += parts[y * 128 + i2 * 64 + g * 8 + s % 8];
+              } else {
+                for (int y = 0; y < Sh::kMulThreads / 32; ++y) x += mids[y * 64 + g * 8 + s];
+              }
+              const T* row = reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(values) + s * Sh::kRawPitch) + warp * Sh::kValues * 16 + q * 2;
 #pragma unroll
-        for (int e = 0; e < Sh::R; ++e) {
-          const uint32_t x[4] = {a0[e], a1[e], 0u, a3[e]};
+              for (int m = 0; m < Sh::kValues; ++m)
 #pragma unroll
-          for (int f = 0; f < Sh::V && e + f < Sh::R; ++f)
+                for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-            for (int m = 0; m < Sh::kValues; ++m) {
-              mma(o[m][0], x, v[m][f][0], v[m][f][2]);
-              mma(o[m][1], x, v[m][f][1], v[m][f][3]);
+                  for (int e = 0; e < 2; ++e) {
+                    const float y = fmaf(x, to_f32(row[m * 16 + nb * 8 + e]), i2 ? o[m][nb][2 + e] : o[m][nb][e]);
+                    if (i2) o[m][nb][2 + e] = y;
+                    else o[m][nb][e] = y;
+                  }
             }
+          }
+          bar_arrive(kEmpty + turn, Sh::kAll);
+        } else {
+          bar_arrive(kEmpty + turn, Sh::kAll);
+          uint32_t a0[Sh::R], a1[Sh::R], a3[Sh::R];
+          split<Sh::R>(up, a0);
+          split<Sh::R>(mid, a1);
+          split<Sh::R>(dn, a3);
+#pragma unroll
+          for (int e = 0; e < Sh::R; ++e) {
+            const uint32_t x[4] = {a0[e], a1[e], 0u, a3[e]};
+#pragma unroll
+            for (int f = 0; f < Sh::V && e + f < Sh::R; ++f)
+#pragma unroll
+              for (int m = 0; m < Sh::kValues; ++m) {
+                mma(o[m][0], x, v[m][f][0], v[m][f][2]);
+                mma(o[m][1], x, v[m][f][1], v[m][f][3]);
+              }
+          }
         }
         T* out = static_cast<T*>(a.out) + (long long)h * N + warp * Sh::kValues * 16 + q * 2;
 #pragma unroll

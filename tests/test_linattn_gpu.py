@@ -274,3 +274,28 @@ def test_repeated_captured_and_on_another_stream(lens):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, first) and torch.equal(st_out[c["slots"].long()], st[c["slots"].long()])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n", [64, 128])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_a_token_does_not_see_what_comes_after_it(dtype, n, value):
+    # infinities and NaN in one token's r, k or v: the outputs before it are what they are without it, and other heads' and value columns' are all
+    T, at = 75, 37
+    c = make(51, [T], 2, n, dtype, strong=False)
+    ref, tol, S, tolS = expected(c)
+    for which in range(3):
+        bad = dict(c, rkv=c["rkv"].clone())
+        bad["rkv"][at, which, 1, 5] = value
+        out, st, _ = call(bad)
+        near(out[:at], ref[:at], tol[:at], f"before {'rkv'[which]}")
+        near(out[:, 0], ref[:, 0], tol[:, 0], "the other head")
+        near(st[:, 0], S[:, 0], tolS[:, 0], "the other head's state")
+        if which == 0:
+            near(out[at + 1:], ref[at + 1:], tol[at + 1:], "r is its own token's alone")
+            near(st, S, tolS, "r is not in the state")
+        if which == 2:
+            columns = [j for j in range(n) if j != 5]
+            near(out[:, 1][:, columns], ref[:, 1][:, columns], tol[:, 1][:, columns], "other values")
+            near(st[:, 1][:, :, columns], S[:, 1][:, :, columns], tolS[:, 1][:, :, columns], "other values' state")
+            assert not torch.isfinite(out[at:, 1, 5].float()).any()
