@@ -2,7 +2,8 @@
 //   out_t = r_t (S + (u (.) k_t) v_t^T),   S <- diag(exp(lw_t)) S + k_t v_t^T.
 //
 // Single tokens and short sequences: linattn_token_kernel, the recurrence as it stands, S in registers.  One token reads and writes 2 * 4 * N * N bytes of
-// state for 4 N^2 operations: HBM, and with few sequences latency, is all that counts.
+// state for 4 N^2 operations: HBM, and with few sequences latency, is all that counts (96 sequences, 64 heads: 31 us, 6.5 TB/s; one, 32 heads: 2.0).
+// Prompts: chunks of sixteen tokens on the tensor cores, linattn_chunk_kernel, in two passes where a sequence is dealt out over several SMs.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -136,9 +137,17 @@ __global__ void __launch_bounds__(kTokenThreads) linattn_token_kernel(const __gr
 // (bf16 one, fp16 two); fp32 inputs take three of everything.  mma.sync and not tcgen05: S stays in registers from chunk to chunk as the accumulator of
 // S^T, in the layout in which the next product takes it as its operand; through tensor memory it would have to be read, split and written every 16 tokens.
 //
-// A block of N / 16 warps has one head; warp w the value columns 16 w to 16 w + 15, so that warps share r P, k Q and A but no sums.
+// A block has one head at a time.  Half of its warps or more make a chunk's operands (loads, exponentials, running products, splitting, the triangles) while
+// the others multiply the chunk before it; these have 16 or 32 value columns each, so that they share r P, k Q and A but no sums.  Two sets of operands and named
+// barriers go between them.  (All warps doing both in turn: 77 us where this takes 69, 2048 tokens of 64 heads; 14.8 and 11.2 with 203 of 32, where latency is all.)
 // Rows are cut into blocks of block_rows, dealt out over the SMs: first (kStateOnly) the state that each block's last piece adds up from zero (or from its
 // sequence's own), where the sequence goes on behind the block; then all blocks at once, each beginning with what those before it left.
+//
+// What bounds it, 2048 tokens, 64 heads, bf16, decays fp32: 23 us the states' pass, 52 the other (ncu, cold; 69 in all, warm and one under the other), of which HBM needs 15.5.
+// Shared memory's data path is busy 70 % of the cycles that an SM is active (operands are written once and read by all multiplying warps), issue slots 54 %, the tensor pipe 28 %:
+// about 3 100 warp instructions and 1 050 wavefronts a chunk.  Taken back: parts of a block halved over a cluster in the states' pass (no gain, 203 tokens 11.3 -> 13.2), five
+// stages of inputs (no gain), three or four blocks an SM (spills), the triangles through shared memory (82 us where registers took 77).
+// 203 tokens, 32 heads 11.2; 5000 rows of eleven sequences, one decay a head, fp16 175; fp32, N 128, 1111 tokens of 16 heads 56, six products where bf16 takes three.
 
 template <typename T> struct Terms;
 template <> struct Terms<__nv_bfloat16> { static constexpr int R = 2, V = 1; };
