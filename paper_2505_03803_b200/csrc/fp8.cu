@@ -236,7 +236,8 @@ cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int blo
 //
 // What bounds it.  One token: launch, the latency of the first loads and of the slices' meeting (4096 x 4096 7.3 us with weights from HBM, which needs 2.6).  Few tokens,
 // large matrices: HBM (65536 x 4096, 16 tokens, 45.6 us = 5.9 TB/s).  Many: what an SM takes in, 64 bytes a cycle (2048 x 14336 x 4096 104 us = 2.3 PFLOP/s; a stage of 240 tokens
-// takes 866 cycles, the tensor core 480 of them), and over longer times the power limit.
+// takes 866 cycles, the tensor core 480 of them), and over longer times the power limit.  Taken back: pairs of blocks (cta_group::2) that share a tile's tokens, which take in
+// a third less but no faster (41 bytes a cycle; 2048 x 14336 x 4096 111 us, 2048 x 4096 x 14336 122 where single blocks take 99).
 constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 12, kSfSlots = 2, kMaxSlices = 8, kThreads = 256;
 constexpr uint32_t kWBytes = kRows * kStageCols, kSfBytes = 512 + 1024, kSfCols = 16, kOutBytes = 4096, kCtrlBytes = 512;
 constexpr uint32_t kMaxSmemBytes = 232448;
@@ -362,6 +363,12 @@ __device__ __forceinline__ void add_slices(const GemmArgs& a, uint8_t* smem, int
   else add_slices<T, 8>(a, smem, slice, tile);
 }
 
+// A block that gives up leaves only when the copies it has asked for have arrived: `asked` of them, one a stage in turn (with a limit, as all waits).
+__device__ __forceinline__ void await_copies(Ctrl* ctrl, int asked, int stages) {
+  for (int i = max(0, asked - stages); i < asked; ++i)
+    for (uint32_t it = 0; it < kPollLimit && !mbar_try_wait(&ctrl->full[i % stages], (uint32_t)(i / stages) & 1u); ++it) {}
+}
+
 __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
@@ -392,12 +399,12 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
 
   if (warp == 0) {
     if (lane == 0) {
-      int st = 0;
+      int st = 0, asked = 0;
       uint32_t ph = 0;
       bool ok = true;
       for (int t = tile0; ok && t < a.tiles; t += step) {
         const int mt = t % a.MT, rb = t / a.MT;
-        for (int k = 0; k < n_k; ++k) {
+        for (int k = 0; k < n_k; ++k, ++asked) {
           if (!mbar_wait(&ctrl->empty[st], ph ^ 1u, abortp, a.status)) { ok = false; break; }
           uint8_t* w = smem + (uint32_t)st * stage_bytes;
           mbar_arrive_expect_tx(&ctrl->full[st], stage_bytes);
@@ -406,6 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
           if (++st == a.stages) { st = 0; ph ^= 1u; }
         }
       }
+      if (!ok) await_copies(ctrl, asked, a.stages);
     }
     __syncwarp();
   } else if (warp == 1) {

@@ -253,3 +253,22 @@ def test_product_captured_and_on_another_stream():
         torch.cuda.synchronize()
         assert torch.equal(y, first)
     check_product(y, "f32", wc, ws, xc, xs)
+
+
+# several tiles a block, the last one ragged either way
+@pytest.mark.parametrize("shape", [(224, 9472, 1024), (200, 9500, 528), (1000, 4096, 1040), (700, 5000, 2064), (1500, 2048, 640), (900, 4230, 272)], ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_product_of_many_tiles_against_64_bits(shape, dtype):
+    M, oc, ic = shape
+    wc, ws, xc, xs = product_inputs(M + oc + ic, M, oc, ic)
+    dev = [torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)]
+    wide = torch.full((M + 1, oc), 7.0, dtype=TYPES[dtype], device="cuda")
+    B.rwkvq_gemm_fp8(*dev, wide[:M])
+    torch.cuda.synchronize()
+    assert B.rwkvq_device_status() == 0
+    rows = np.unique(np.concatenate([np.arange(0, M, 37), np.arange(max(0, M - 3), M), np.arange(220, min(M, 228))]))
+    check_product(wide[:M][torch.from_numpy(rows).cuda()], dtype, wc, ws, xc[rows], xs[rows])
+    assert (wide[M] == 7).all()
+    again = torch.empty((M, oc), dtype=TYPES[dtype], device="cuda")
+    B.rwkvq_gemm_fp8(*dev, again)
+    assert torch.equal(again, wide[:M])
