@@ -673,11 +673,14 @@ def _refuse(where: str, why: str):
     raise e
 
 
+_CODES = _SCALES = ()  # torch's types of codes (e4m3) and of scales (exponents of eight bits); filled when torch is loaded
 _DTYPES = {}          # torch's types -> RWKVQ_F32 / F16 / BF16; filled when torch is loaded
 
 
 def _dtypes():
+    global _CODES, _SCALES
     t = _torch or _load_torch()
+    _CODES, _SCALES = (t.float8_e4m3fn, t.uint8), (t.uint8, t.float8_e8m0fnu)
     _DTYPES.update({t.float32: RWKVQ_F32, t.float16: RWKVQ_F16, t.bfloat16: RWKVQ_BF16})
     return _DTYPES
 
@@ -698,11 +701,11 @@ def rwkvq_fp8_scale_pitch(cols: int) -> int:
 
 
 # The checks of the three functions below ask a tensor for as little as they can: every attribute costs 60 to 200 ns, and the calls are short.
-def _check_bytes(where: str, x, shape, what: str, here: int):
+def _check_bytes(where: str, x, shape, what: str, here: int, types):
     if x.get_device() != here:
         _elsewhere(where, x, here)
-    if x.shape != shape or x.element_size() != 1 or not x.is_contiguous():
-        _refuse(where, f"{what} has to be contiguous, of one-byte elements, {list(shape)}")
+    if x.shape != shape or x.dtype not in types or not x.is_contiguous():
+        _refuse(where, f"{what} has to be contiguous, {list(shape)}, of a type among {', '.join(map(str, types))}")
 
 
 def rwkvq_fp8_quantize(x, codes, scale, block_rows: int, stream=None):
@@ -718,12 +721,12 @@ def rwkvq_fp8_quantize(x, codes, scale, block_rows: int, stream=None):
         _refuse(where, "x has to have its columns side by side")
     if block_rows != 1 and block_rows != 128:
         _refuse(where, "block_rows is 1 or 128")
-    here = _here()
+    types, here = _DTYPES or _dtypes(), _here()
     if x.get_device() != here:
         _elsewhere(where, x, here)
-    _check_bytes(where, codes, shape, "codes", here)
-    _check_bytes(where, scale, ((rows + block_rows - 1) // block_rows, (cols + 2047) // 2048 * 16), "scale", here)
-    status = (_lib or lib()).rwkvq_fp8_quantize(x.data_ptr(), (_DTYPES or _dtypes()).get(x.dtype, -1), rows, cols, x_row if rows > 1 else cols, block_rows,
+    _check_bytes(where, codes, shape, "codes", here, _CODES)
+    _check_bytes(where, scale, ((rows + block_rows - 1) // block_rows, (cols + 2047) // 2048 * 16), "scale", here, _SCALES)
+    status = (_lib or lib()).rwkvq_fp8_quantize(x.data_ptr(), types.get(x.dtype, -1), rows, cols, x_row if rows > 1 else cols, block_rows,
                                                 codes.data_ptr(), scale.data_ptr(), _stream_ptr(stream))
     if status:
         _check(status, where)
@@ -739,18 +742,18 @@ def rwkvq_gemm_fp8(w_codes, w_scale, x_codes, x_scale, Y, stream=None):
     oc, ic = w_shape
     M = y_shape[0]
     y_row, one = Y.stride()
-    here = _here()
+    types, here = _DTYPES or _dtypes(), _here()
     pitch = (ic + 2047) // 2048 * 16
-    _check_bytes(where, w_codes, w_shape, "w_codes", here)
-    _check_bytes(where, x_codes, (M, ic), "x_codes", here)
-    _check_bytes(where, w_scale, ((oc + 127) // 128, pitch), "w_scale", here)
-    _check_bytes(where, x_scale, (M, pitch), "x_scale", here)
+    _check_bytes(where, w_codes, w_shape, "w_codes", here, _CODES)
+    _check_bytes(where, x_codes, (M, ic), "x_codes", here, _CODES)
+    _check_bytes(where, w_scale, ((oc + 127) // 128, pitch), "w_scale", here, _SCALES)
+    _check_bytes(where, x_scale, (M, pitch), "x_scale", here, _SCALES)
     if y_shape[1] != oc or (one != 1 and oc > 1):
         _refuse(where, f"Y has to be [{M}, {oc}] with columns side by side")
     if Y.get_device() != here:
         _elsewhere(where, Y, here)
     status = (_lib or lib()).rwkvq_gemm_fp8(w_codes.data_ptr(), w_scale.data_ptr(), oc, ic, x_codes.data_ptr(), x_scale.data_ptr(), M, Y.data_ptr(),
-                                            (_DTYPES or _dtypes()).get(Y.dtype, -1), y_row if M > 1 else oc, _stream_ptr(stream))
+                                            types.get(Y.dtype, -1), y_row if M > 1 else oc, _stream_ptr(stream))
     if status:
         _check(status, where)
 

@@ -789,15 +789,20 @@ __device__ __forceinline__ int quotient(long long a, long long b) { return ((a |
 
 // The next sequence from `from` on that has rows in [row0, row1) and is longer than the limit; n_seq: none.  Called by whole warps.
 __device__ __forceinline__ int next_sequence(const Args& p, int from, int row0, int row1) {
-  for (int base = from; base < p.a.n_seq; base += 32) {
-    const int i = base + (int)(threadIdx.x & 31);
-    bool here = false;
-    if (i < p.a.n_seq) {
-      const Entry e = p.entries[i];
-      here = e.end - e.start > p.limit && e.end > row0 && e.start < row1;
+  constexpr int kAtOnce = 4;         // entries a lane has under way
+  for (int base = from; base < p.a.n_seq; base += 32 * kAtOnce) {
+    bool here[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const int i = base + 32 * j + (int)(threadIdx.x & 31);
+      const Entry e = i < p.a.n_seq ? p.entries[i] : Entry{0, 0, -1, 0};
+      here[j] = e.end - e.start > p.limit && e.end > row0 && e.start < row1;
     }
-    const uint32_t found = __ballot_sync(0xFFFFFFFFu, here);
-    if (found) return base + __ffs((int)found) - 1;
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const uint32_t found = __ballot_sync(0xFFFFFFFFu, here[j]);
+      if (found) return base + 32 * j + __ffs((int)found) - 1;
+    }
   }
   return p.a.n_seq;
 }

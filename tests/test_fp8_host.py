@@ -73,3 +73,5 @@ def test_binding_refuses_what_is_not_on_the_device_or_ill_shaped():
         B.rwkvq_fp8_quantize(x.T, codes, scale, 1)
     with pytest.raises(B.RwkvqError):
         B.rwkvq_gemm_fp8(codes, scale, codes, scale, x)
+    with pytest.raises(B.RwkvqError):
+        B.rwkvq_fp8_quantize(x, codes.view(torch.float8_e5m2), scale, 1)

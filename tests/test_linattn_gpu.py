@@ -17,14 +17,14 @@ E24 = 2.0 ** -24
 
 
 def reference(r, k, v, lw, u, S, parts):
-    """One sequence, double precision, on the CPU: r, k, v [T, H, N], lw [T, H, N], u [H, N], S [H, N, N].  Returns (out, its tolerance, S, its tolerance).
+    """One sequence, double precision: r, k, v [T, H, N], lw [T, H, N], u [H, N], S [H, N, N].  Returns (out, its tolerance, S, its tolerance).
 
     Tolerances: per token a decay (its exponential and the logarithms' sum) and two roundings, against the magnitudes M that were added up; a sum of x in
     logarithms that is off by 16 * 2^-24 * x makes a term e^-x off by x e^-x <= 0.74 e^(-x/2), so also against H, in which decays are square roots."""
     T, H, N = r.shape
     M, Hm = S.abs().clone(), S.abs().clone()
     E = torch.zeros_like(S)
-    out, tol = torch.empty((T, H, N), dtype=torch.float64), torch.empty((T, H, N), dtype=torch.float64)
+    out, tol = torch.empty_like(r), torch.empty_like(r)
     for t in range(T):
         kv = k[t].unsqueeze(-1) * v[t].unsqueeze(-2)
         cur = S + u.unsqueeze(-1) * kv
@@ -64,23 +64,25 @@ def make(seed, lens, heads, n, dtype, decay="channel", decay_f32=True, static=Fa
     return c
 
 
-def expected(c, state=True):
+def expected(c, state=True, device="cpu"):
+    c = {x: y.to(device) if torch.is_tensor(y) and x != "slots" else y for x, y in c.items()}
     r, k, v = (c["rkv"][:, i].double() for i in range(3))
     T, H, n = r.shape
     lw = c["lw"].double()
     if lw.dim() == 2:
         lw = lw.unsqueeze(-1).expand(lw.shape[0], H, n)
     lw = lw.expand(T, H, n)
-    u = c["u"].double() if c["u"] is not None else torch.ones((H, n), dtype=torch.float64)
-    S = c["state"].double().clone() if state else torch.zeros(c["state"].shape, dtype=torch.float64)
+    u = c["u"].double() if c["u"] is not None else torch.ones((H, n), dtype=torch.float64, device=device)
+    S = c["state"].double().clone() if state else torch.zeros_like(c["state"], dtype=torch.float64)
     tolS = torch.zeros_like(S)
-    out, tol = torch.zeros((T, H, n), dtype=torch.float64), torch.zeros((T, H, n), dtype=torch.float64)
+    out, tol = torch.zeros_like(r), torch.zeros_like(r)
     for i, (a, b) in enumerate(zip(c["starts"], c["starts"][1:])):
         s = i if c["slots"] is None else int(c["slots"][i])
         if a == b and state:
             continue
         out[a:b], tol[a:b], S[s], tolS[s] = reference(r[a:b], k[a:b], v[a:b], lw[a:b], u, S[s], SPLIT[c["dtype"]])
-    return out, tol + HALF_ULP[c["dtype"]] * out.abs() + 2.0 ** -24 * (c["dtype"] == "f16"), S, tolS
+    tol = tol + HALF_ULP[c["dtype"]] * out.abs() + 2.0 ** -24 * (c["dtype"] == "f16")
+    return out.cpu(), tol.cpu(), S.cpu(), tolS.cpu()
 
 
 def call(c, in_place=True, state=True, keep=True, stream=None, ragged=None):
@@ -299,3 +301,33 @@ def test_a_token_does_not_see_what_comes_after_it(dtype, n, value):
             near(out[:, 1][:, columns], ref[:, 1][:, columns], tol[:, 1][:, columns], "other values")
             near(st[:, 1][:, :, columns], S[:, 1][:, :, columns], tolS[:, 1][:, :, columns], "other values' state")
             assert not torch.isfinite(out[at:, 1, 5].float()).any()
+
+
+# sizes at which blocks of rows are dealt out evenly and some have rows of two heads, at which a head is one block, and at which it is several
+@pytest.mark.parametrize("lens,heads,n,dtype", [([2000], 64, 64, "bf16"), ([700, 1100, 1, 0, 300, 20], 64, 64, "f16"), ([1000], 80, 128, "bf16"), ([40], 200, 64, "f32"),
+                                                ([500], 150, 64, "bf16"), ([9] * 60, 40, 64, "bf16"), ([1500], 64, 64, "f32")], ids=str)
+def test_many_heads(lens, heads, n, dtype):
+    c = make(61, lens, heads, n, dtype)
+    out, st, _ = call(c)
+    assert B.rwkvq_device_status() == 0
+    ref, tol, S, tolS = expected(c, device="cuda")
+    near(out, ref, tol, "out")
+    near(st, S, tolS, "state")
+
+
+@pytest.mark.parametrize("lens", [[1, 1], [30, 100]], ids=str)
+def test_rows_in_front_of_the_first_sequence(lens):
+    c = make(62, lens, 2, 64, "bf16", pad=23)
+    c["starts"] = [x + 19 for x in c["starts"]]
+    out, st, _ = call(c, ragged=True)
+    ref, tol, S, tolS = expected(c)
+    a, b = c["starts"][0], c["starts"][-1]
+    near(out[a:b], ref[a:b], tol[a:b], "out")
+    near(st, S, tolS, "state")
+    assert (out[:a] == 7).all() and (out[b:] == 7).all()
+
+
+def test_one_sequence_with_a_slot():
+    for T in (1, 60):
+        c = make(63, [T], 2, 64, "f16", extra_slots=4)
+        check(c)
