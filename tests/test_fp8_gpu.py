@@ -272,3 +272,21 @@ def test_product_of_many_tiles_against_64_bits(shape, dtype):
     again = torch.empty((M, oc), dtype=TYPES[dtype], device="cuda")
     B.rwkvq_gemm_fp8(*dev, again)
     assert torch.equal(again, wide[:M])
+
+
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize_more_than_32_bits_of_elements(block):
+    rows, cols, last = 66000, 65536, 130
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    assert x.numel() > 2 ** 32
+    x[-last:] = torch.randn((last, cols), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    codes = torch.full((rows, cols), 0xAA, dtype=torch.uint8, device="cuda")
+    scale = torch.zeros((-(-rows // block), B.rwkvq_fp8_scale_pitch(cols)), dtype=torch.uint8, device="cuda")
+    B.rwkvq_fp8_quantize(x, codes, scale, block)
+    first = (rows - last) // block * block
+    part = slice(0, 1024), slice(cols - 1024, cols)
+    for c in part:
+        ref_codes, ref_scale = quantize_exact(x[first:, c].double().cpu().numpy(), block)
+        assert np.array_equal(codes[first:, c].cpu().numpy(), ref_codes)
+        assert np.array_equal(scale[first // block:, c.start // 128:c.stop // 128].cpu().numpy(), ref_scale)
+    assert (codes[:first] == 0).all() and (scale[:first // block] == 127).all()

@@ -331,3 +331,22 @@ def test_one_sequence_with_a_slot():
     for T in (1, 60):
         c = make(63, [T], 2, 64, "f16", extra_slots=4)
         check(c)
+
+
+def test_a_cache_of_more_than_32_bits():
+    # 8200 slots of 64 heads: the last state begins behind 2^31 numbers
+    slots, heads = 8200, 64
+    state = torch.empty((slots, heads, 64, 64), device="cuda")
+    assert state.numel() > 2 ** 31
+    for lens in ([1, 1], [40, 3]):
+        c = make(64, lens, heads, 64, "bf16")
+        ids = torch.tensor([slots - 1, 3], dtype=torch.int32)
+        state[ids.long()] = c["state"].cuda()
+        T = sum(lens)
+        rkv, out = c["rkv"].cuda(), torch.empty((T, heads, 64), dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(max(16, B.rwkvq_linattn_workspace_bytes(T, 2, heads, 64)), dtype=torch.uint8, device="cuda")
+        B.rwkvq_linattn(rkv[:, 0], rkv[:, 1], rkv[:, 2], c["lw"].cuda(), c["u"].cuda(), out, state, slots=ids.cuda(), workspace=ws,
+                        seq_start=torch.tensor(c["starts"], dtype=torch.int32, device="cuda"))
+        ref, tol, S, tolS = expected(c, device="cuda")
+        near(out, ref, tol, "out")
+        near(state[ids.long()], S, tolS, "state")
