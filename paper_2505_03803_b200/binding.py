@@ -780,9 +780,11 @@ def rwkvq_linattn(r, k, v, logw, u, out, state, state_out=None, seq_start=None, 
     for x in (r, k, v, out):
         if x.get_device() != here:
             _elsewhere(where, x, here)
-        row, head, one = x.stride() if x.dim() == 3 else (0, 0, 0)
-        if x.dtype is not dtype or x.shape != shape or (tokens and (one != 1 or (head != n and heads > 1))):
-            _refuse(where, f"r, k, v and out have to be [{tokens}, {heads}, {n}] of {dtype} with heads side by side")
+        if x.dtype is not dtype or x.shape != shape:
+            _refuse(where, f"r, k, v and out have to be [{tokens}, {heads}, {n}] of {dtype}")
+        row, head, one = x.stride()
+        if tokens and (one != 1 or (head != n and heads > 1)):
+            _refuse(where, "r, k, v and out have to have their heads side by side")
         rows.append(row if tokens > 1 else 0)
     w_shape, w_stride, w_dtype = logw.shape, logw.stride(), logw.dtype
     if logw.get_device() != here:
@@ -810,7 +812,7 @@ def rwkvq_linattn(r, k, v, logw, u, out, state, state_out=None, seq_start=None, 
         if x.get_device() != here:
             _elsewhere(where, x, here)
         s_shape = x.shape
-        if x.dtype is not t.float32 or s_shape[1:] != (heads, n, n) or not x.is_contiguous() or (n_slots and s_shape[0] != n_slots):
+        if x.dtype is not t.float32 or len(s_shape) != 4 or s_shape != (n_slots or s_shape[0], heads, n, n) or not x.is_contiguous():
             _refuse(where, f"states have to be float32 [slots, {heads}, {n}, {n}], contiguous, as many before as after")
         n_slots = s_shape[0]
     if u is not None:

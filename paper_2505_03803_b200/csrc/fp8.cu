@@ -235,9 +235,10 @@ cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int blo
 // of the copy to tensor memory (32 lanes x 16 bytes, row r in line r % 32, word r / 32), where they lie once per 32-lane quarter.
 //
 // What bounds it.  One token: launch, the latency of the first loads and of the slices' meeting (4096 x 4096 7.3 us with weights from HBM, which needs 2.6).  Few tokens,
-// large matrices: HBM (65536 x 4096, 16 tokens, 45.6 us = 5.9 TB/s).  Many: what an SM takes in, 64 bytes a cycle (2048 x 14336 x 4096 104 us = 2.3 PFLOP/s; a stage of 240 tokens
-// takes 866 cycles, the tensor core 480 of them), and over longer times the power limit.  Taken back: pairs of blocks (cta_group::2) that share a tile's tokens, which take in
-// a third less but no faster (41 bytes a cycle; 2048 x 14336 x 4096 111 us, 2048 x 4096 x 14336 122 where single blocks take 99).
+// large matrices: HBM (65536 x 4096, 16 tokens, 45.6 us = 5.9 TB/s).  Many: the tensor core at the clock that the power limit leaves (2048 x 14336 x 4096 104 us =
+// 2.3 PFLOP/s; with the tokens' copies left out 93, with three of four tensor-core instructions left out 75; a library's product with one scale takes 92).
+// Taken back: pairs of blocks (cta_group::2) that share a tile's tokens, which take in a third less but no faster (2048 x 14336 x 4096 111 us, 2048 x 4096 x 14336
+// 122 where single blocks take 99); eight warps for the epilogue (no gain); two blocks an SM for few tokens (7.5 us where one with more stages takes 7.3, 4096 x 4096).
 constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 12, kSfSlots = 2, kMaxSlices = 8, kThreads = 256;
 constexpr uint32_t kWBytes = kRows * kStageCols, kSfBytes = 512 + 1024, kSfCols = 16, kOutBytes = 4096, kCtrlBytes = 512;
 constexpr uint32_t kMaxSmemBytes = 232448;
@@ -529,7 +530,7 @@ bool encode_codes(CUtensorMap* map, const void* codes, int rows, int cols, int b
 
 // Tiles, slices and stages of a product: the cheapest by an estimate of an SM's cycles, fitted to 150 times of 17 products (1 to 1000 tokens, 1024 to 14336 x
 // 1024 to 14336), which it gives to within a tenth; over 16 others it is 2 % off the best choice on average, 9 % at most.  A stage takes 130 cycles and its
-// bytes at 64 a cycle, what an SM takes in, or the tensor core's 2 cycles a token where that is more; a tile's epilogue 14 a token; slices meet in 1500 and 45
+// bytes at 64 a cycle, or the tensor core's 2 cycles a token where that is more; a tile's epilogue 14 a token; slices meet in 1500 and 45
 // a token (but up to 112), and their blocks have to fit side by side (clusters of eight only up to 112 blocks); nothing is faster than HBM.  More tiles of
 // fewer tokens or more slices fill SMs: 203 tokens x 7168 x 2048 10.0 us as two tiles (one: 11.7; in two slices: 12.8), 2048 x 7168 12.2 as two in four slices (one in
 // four: 14.4, four in two: 13.8), one token x 4096 x 4096 7.3 in four slices, 8.9 in two, 12.3 in one.
