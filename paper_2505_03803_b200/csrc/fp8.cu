@@ -229,19 +229,25 @@ cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int blo
 // ---- product ----------------------------------------------------------------------------------------------
 // Y[t][i] = sum_g 2^(ex[t][g] + ew[i / 128][g]) sum_{k in group g} x[t][k] w[i][k].  Weights are the 128-row operand (a tile's rows are
 // one block of scales), tokens the other one, NT of them, so that a lane of an accumulator is an output channel and a warp writes 32
-// consecutive outputs of one token.  Roles of the eight warps of a CTA: (0) tensor-map copies of 128-column stages, (1) tensor-core
-// instructions, (2) scales, (3) tensor memory, (4-7) epilogue.  Two accumulators, so that a tile's epilogue runs under the next tile's sums.
+// consecutive outputs of one token.  Roles of a CTA's warps: (0) tensor-map copies of 128-column stages, (1) tensor-core
+// instructions, (2) scales, (3) tensor memory, (4 on) epilogue.  Two accumulators: for a tile's epilogue to run under the next tile's sums, or (W = 2) for two tiles of
+// weights with the same tokens.
 // Scales: four groups' bytes of a row are the word that the instruction picks its byte from; warp 2 deals the words of 512 columns out in the order
 // of the copy to tensor memory (32 lanes x 16 bytes, row r in line r % 32, word r / 32), where they lie once per 32-lane quarter.
 //
-// What bounds it.  One token: launch, the latency of the first loads and of the slices' meeting (4096 x 4096 7.3 us with weights from HBM, which needs 2.6).  Few tokens,
-// large matrices: HBM (65536 x 4096, 16 tokens, 45.6 us = 5.9 TB/s).  Many: the tensor core at the clock that the power limit leaves (2048 x 14336 x 4096 104 us =
-// 2.3 PFLOP/s; with the tokens' copies left out 93, with three of four tensor-core instructions left out 75; a library's product with one scale takes 92).
-// Taken back: pairs of blocks (cta_group::2) that share a tile's tokens, which take in a third less but no faster (2048 x 14336 x 4096 111 us, 2048 x 4096 x 14336
-// 122 where single blocks take 99); eight warps for the epilogue (no gain); two blocks an SM for few tokens (7.5 us where one with more stages takes 7.3, 4096 x 4096).
-constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 12, kSfSlots = 2, kMaxSlices = 8, kThreads = 256;
-constexpr uint32_t kWBytes = kRows * kStageCols, kSfBytes = 512 + 1024, kSfCols = 16, kOutBytes = 4096, kCtrlBytes = 512;
+// What bounds it.  One token: launch, the latency of the first loads and of the slices' meeting (4096 x 4096 7.1 us with weights from HBM, which needs 2.6).  Few tokens,
+// large matrices: HBM (65536 x 4096, 16 tokens, 45.6 us = 5.9 TB/s).  Many: power.  2048 x 4096 x 14336 over and over takes 110 us (2.2 PFLOP/s) at 990 W, the limit,
+// which leaves 1.47 of 1.97 GHz; 106 without scales, 125 with one tile of weights a block.  A stage of two brings 63 KB for 256 x 240 outputs, of one 47 KB for 128 x 240,
+// and shared memory, which these pass twice (in, and to the tensor core), is then busier than the tensor core.
+// Taken back: pairs of blocks (cta_group::2) that share a tile's tokens, which take in as little (2048 x 14336 x 4096 111 us with barriers of the other block's, 263 with
+// relayed ones); 2 KB of epilogue buffers and a stage more (no gain); two blocks an SM for few tokens (7.5 us where one with more stages takes 7.3, 4096 x 4096); the
+// scales' words 16 bytes at a time (65536 x 1024, 240 tokens, 24.3 -> 28.9); elections for every instruction of warp 1 (1000 x 4096 x 1024 9.6 us, one for all 8.8).
+constexpr int kRows = 128, kStageCols = 128, kMaxTokens = 240, kMaxStages = 12, kSfSlots = 2, kMaxSlices = 8;
+constexpr uint32_t kWBytes = kRows * kStageCols, kLineBytes = 512, kSfCols = 16, kOutBytes = 4096, kCtrlBytes = 512;
 constexpr uint32_t kMaxSmemBytes = 232448;
+// By the weights' tiles W (1 or 2) of a block's tile: their scales' lines and the tokens'; four warps of the epilogue for each.
+__host__ __device__ constexpr int threads_of(int W) { return 128 + 128 * W; }
+__host__ __device__ constexpr uint32_t sf_bytes(int W) { return kLineBytes * (uint32_t)(W + 2); }
 
 struct GemmArgs {
   CUtensorMap wmap, xmap;
@@ -271,23 +277,30 @@ __device__ __forceinline__ uint64_t smem_desc_lines(uint32_t saddr) {
 __device__ __forceinline__ uint32_t idesc_mx(int M, int N, uint32_t id) {
   return id << 4 | (uint32_t)(N >> 3) << 17 | 1u << 23 | (uint32_t)(M >> 7) << 27 | id << 29;
 }
+// The four that follow are for one thread: an election for each of them would take longer than the small tiles' instructions.
+__device__ __forceinline__ bool elected() {
+  uint32_t q;
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(q));
+  return q != 0;
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
 // 32 lines of scales to four columns of tensor memory, once per quarter of the lanes.
 __device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
-  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n @q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n}" ::"r"(tmem), "l"(desc) : "memory");
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
-// One stage: four instructions of 32 columns and the commit that frees it.
-__device__ __forceinline__ void mma_stage(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate,
-                                          uint32_t bar) {
+// One stage: four instructions of 32 columns.
+__device__ __forceinline__ void mma_stage(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
   asm volatile(
-      "{\n .reg .pred q, p, one;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n"
-      " elect.sync _|q, 0xffffffff;\n setp.ne.b32 p, %6, 0;\n setp.eq.b32 one, 0, 0;\n"
+      "{\n .reg .pred p, one;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      " setp.ne.b32 p, %6, 0;\n setp.eq.b32 one, 0, 0;\n"
       " add.u64 a1, %1, 2;\n add.u64 a2, %1, 4;\n add.u64 a3, %1, 6;\n add.u64 b1, %2, 2;\n add.u64 b2, %2, 4;\n add.u64 b3, %2, 6;\n"
-      " @q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n"
-      " @q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a1, b1, %3, [%4], [%5], one;\n"
-      " @q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a2, b2, %3, [%4], [%5], one;\n"
-      " @q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a3, b3, %3, [%4], [%5], one;\n"
-      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%7];\n}"
-      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(bar) : "memory");
+      " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n"
+      " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a1, b1, %3, [%4], [%5], one;\n"
+      " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a2, b2, %3, [%4], [%5], one;\n"
+      " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], a3, b3, %3, [%4], [%5], one;\n}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
 }
 
 template <typename T> __device__ __forceinline__ T to_out(float f);
@@ -295,28 +308,80 @@ template <> __device__ __forceinline__ float to_out<float>(float f) { return f; 
 template <> __device__ __forceinline__ __half to_out<__half>(float f) { return __float2half_rn(f); }
 template <> __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float f) { return __float2bfloat16_rn(f); }
 
-// A warp's 32 output channels of a tile's tokens.  A lane holds one channel, so that a store of it writes 32 elements of one token: through shared memory
-// (`stage`, 4 KB of the warp's own) it becomes 16 bytes a lane, several tokens a store.  `wide`: rows of Y begin on 16 bytes and all 32 channels are there.
+// Two numbers rounded, the first in the low half.
+__device__ __forceinline__ uint32_t two_of(uint32_t x, uint32_t y, __half) {
+  const __half2 v = __floats2half2_rn(__uint_as_float(x), __uint_as_float(y));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t two_of(uint32_t x, uint32_t y, __nv_bfloat16) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(x), __uint_as_float(y));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// 32 lanes x 32 columns in the tiles of stmatrix: register 16 h + 4 n + 2 x + e of lane l = D[lane base + 16 h + 8 x + l / 4][col + 8 n + 2 (l % 4) + e].
+__device__ __forceinline__ void tmem_ld_tiles_issue(uint32_t taddr, uint32_t (&r)[32]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[16 * h]), "=r"(r[16 * h + 1]), "=r"(r[16 * h + 2]), "=r"(r[16 * h + 3]), "=r"(r[16 * h + 4]), "=r"(r[16 * h + 5]), "=r"(r[16 * h + 6]),
+                   "=r"(r[16 * h + 7]), "=r"(r[16 * h + 8]), "=r"(r[16 * h + 9]), "=r"(r[16 * h + 10]), "=r"(r[16 * h + 11]), "=r"(r[16 * h + 12]),
+                   "=r"(r[16 * h + 13]), "=r"(r[16 * h + 14]), "=r"(r[16 * h + 15])
+                 : "r"(taddr + ((uint32_t)h << 20)) : "memory");
+}
+// A warp's 32 output channels of a tile's tokens; `done` is arrived at when they are read.  A lane of the accumulator is a channel, and 16 bytes of Y are eight channels
+// of one token: the way there is through shared memory (`stage`, 4 KB of the warp's own), for 16-bit types by stmatrix, which turns 8 x 8 numbers round at
+// once (2048 x 14336 x 4096, one tile of weights a block: 110.5 us, 112.6 with a store of two bytes for each number).  The 64 bytes of a token lie in an order of 16-byte pieces that spares banks.
+// Without a.wide (rows of Y begin on 16 bytes), or with fewer channels, a store for each number.
 template <typename T>
-__device__ __forceinline__ void store_tile(const GemmArgs& a, uint32_t tmem, int row0, int t0, int nt, uint8_t* stage, int lane) {
-  constexpr int kLanes = 32 * (int)sizeof(T) / 16, kTokens = 32 / kLanes;        // lanes of a token's 32 channels, tokens of a store
+__device__ __forceinline__ void store_tile(const GemmArgs& a, uint32_t tmem, int row0, int t0, int nt, uint8_t* stage, int lane, uint64_t* done) {
   T* y = static_cast<T*>(a.Y) + (long long)t0 * a.y_row + row0;
   const bool wide = a.wide && row0 + 32 <= a.oc;
+  auto is_read = [&]() { tc_fence_before(); mbar_arrive(done); };
+  uint32_t r[32];
+  if constexpr (sizeof(T) == 2) {
+    if (wide) {
+      const uint32_t to = smem_u32(stage) + (uint32_t)((lane & 7) * 64 + ((lane >> 3 ^ lane >> 1) & 3) * 16);
+      const uint8_t* from = stage + (lane >> 2) * 64 + ((lane ^ lane >> 3) & 3) * 16;
+      T* at = y + (long long)(lane >> 2) * a.y_row + (lane & 3) * 8;
+      tmem_ld_tiles_issue(tmem, r);
+      for (int c = 0; c < nt; c += 32) {
+        tmem_ld_wait(r);
+        uint32_t v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = two_of(r[2 * i], r[2 * i + 1], T());       // 8 h + 2 n + x
+        if (c + 32 < nt) tmem_ld_tiles_issue(tmem + (uint32_t)c + 32u, r);
+        else is_read();
+        const uint32_t half = (uint32_t)(c & 32) * 64u;        // in turn, so that no lane writes where another still reads
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+          asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(to + half + n * 512), "r"(v[2 * n]), "r"(v[2 * n + 1]), "r"(v[8 + 2 * n]),
+                       "r"(v[9 + 2 * n]) : "memory");
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint4 x = *reinterpret_cast<const uint4*>(from + half + i * 512);
+          if (c + i * 8 + (lane >> 2) < nt) *reinterpret_cast<uint4*>(at) = x;
+          at += 8 * a.y_row;
+        }
+      }
+      return;
+    }
+  }
   for (int c = 0; c < nt; c += 32) {
-    uint32_t r[32];
     tmem_ld32_issue(tmem + (uint32_t)c, r);
     tmem_ld_wait(r);
-    if (wide) {
-      T* st = reinterpret_cast<T*>(stage) + lane;
+    if (c + 32 >= nt) is_read();
+    if (sizeof(T) == 4 && wide) {
+      uint32_t* st = reinterpret_cast<uint32_t*>(stage) + lane;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) st[j * 32] = to_out<T>(__uint_as_float(r[j]));
+      for (int j = 0; j < 32; ++j) st[j * 32] = r[j];
       __syncwarp();
-      T* at = y + (long long)(c + lane / kLanes) * a.y_row + lane % kLanes * (16 / (int)sizeof(T));
+      T* at = y + (long long)(c + (lane >> 3)) * a.y_row + (lane & 7) * 4;
 #pragma unroll
-      for (int i = 0; i < 32 / kTokens; ++i) {
+      for (int i = 0; i < 8; ++i) {
         const uint4 v = *reinterpret_cast<const uint4*>(stage + i * 512 + lane * 16);
-        if (c + i * kTokens + lane / kLanes < nt) *reinterpret_cast<uint4*>(at) = v;
-        at += kTokens * a.y_row;
+        if (c + i * 4 + (lane >> 3) < nt) *reinterpret_cast<uint4*>(at) = v;
+        at += 4 * a.y_row;
       }
       __syncwarp();
     } else if (row0 + lane < a.oc) {
@@ -333,7 +398,7 @@ __device__ __forceinline__ void cluster_sync() {
 // A cluster's sums added up in the order of the slices: each block takes its share of the tokens, two at a time.
 template <typename T, int S>
 __device__ __forceinline__ void add_slices(const GemmArgs& a, uint8_t* smem, int slice, int tile) {
-  constexpr int kAtOnce = 16 / S, kStep = kThreads / kRows;      // sixteen loads from the other blocks' memories under way
+  constexpr int kAtOnce = 16 / S, kStep = threads_of(1) / kRows;      // sixteen loads from the other blocks' memories under way
   const int mt = tile % a.MT, t0 = mt * a.NT, nt = min(a.NT, a.M - t0), i = threadIdx.x % kRows, row = tile / a.MT * kRows + i;
   const int c1 = nt * (slice + 1) / S;
   uint32_t from[S];
@@ -370,12 +435,14 @@ __device__ __forceinline__ void await_copies(Ctrl* ctrl, int asked, int stages) 
     for (uint32_t it = 0; it < kPollLimit && !mbar_try_wait(&ctrl->full[i % stages], (uint32_t)(i / stages) & 1u); ++it) {}
 }
 
-__global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
+template <int W>
+__global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
-  const uint32_t stage_bytes = kWBytes + (uint32_t)a.NT * kStageCols;
+  constexpr uint32_t kSfBytes = sf_bytes(W);
+  const uint32_t stage_bytes = W * kWBytes + (uint32_t)a.NT * kStageCols;
   uint8_t* sf = smem + (uint32_t)a.stages * stage_bytes;
-  Ctrl* ctrl = reinterpret_cast<Ctrl*>(sf + kSfSlots * kSfBytes + 4 * kOutBytes);
+  Ctrl* ctrl = reinterpret_cast<Ctrl*>(sf + kSfSlots * kSfBytes + 4 * W * kOutBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abortp = &ctrl->abort_flag;
   if (threadIdx.x == 0) {
@@ -409,8 +476,8 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
           if (!mbar_wait(&ctrl->empty[st], ph ^ 1u, abortp, a.status)) { ok = false; break; }
           uint8_t* w = smem + (uint32_t)st * stage_bytes;
           mbar_arrive_expect_tx(&ctrl->full[st], stage_bytes);
-          tensor_g2s(w, &a.wmap, (k0 + k) * kStageCols, rb * kRows, &ctrl->full[st]);
-          tensor_g2s(w + kWBytes, &a.xmap, (k0 + k) * kStageCols, mt * a.NT, &ctrl->full[st]);
+          tensor_g2s(w, &a.wmap, (k0 + k) * kStageCols, rb * (W * kRows), &ctrl->full[st]);
+          tensor_g2s(w + W * kWBytes, &a.xmap, (k0 + k) * kStageCols, mt * a.NT, &ctrl->full[st]);
           if (++st == a.stages) { st = 0; ph ^= 1u; }
         }
       }
@@ -418,47 +485,58 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
     }
     __syncwarp();
   } else if (warp == 1) {
-    int st = 0, sl = 0;
-    uint32_t ph = 0, sph = 0, acc = 0, aph = 0;
-    bool ok = true;
-    for (int t = tile0; ok && t < a.tiles; t += step) {
-      if (!mbar_wait(&ctrl->accempty[acc], aph ^ 1u, abortp, a.status)) break;
-      tc_fence_after();
-      const uint32_t d = tmem + acc * (uint32_t)a.NT;
-      for (int k = 0; k < n_k; ++k) {
-        const uint32_t sfa = tmem + a.tmem_cols - (uint32_t)(kSfSlots - sl) * kSfCols, sfb = sfa + 4;
-        if ((k & 3) == 0) {
-          if (!mbar_wait(&ctrl->sffull[sl], sph, abortp, a.status)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t src = smem_u32(sf + sl * kSfBytes);
-          copy_scales(sfa, smem_desc_lines(src));
-          copy_scales(sfb, smem_desc_lines(src + 512));
-          if (a.NT > 128) copy_scales(sfb + 4, smem_desc_lines(src + 1024));
-        }
-        if (!mbar_wait(&ctrl->full[st], ph, abortp, a.status)) { ok = false; break; }
+    if (elected()) {
+      int st = 0, sl = 0;
+      uint32_t ph = 0, sph = 0, acc = 0, aph = 0;
+      bool ok = true;
+      const uint64_t wdesc = smem_desc_sw128(smem_u32(smem)), lines = smem_desc_lines(smem_u32(sf));
+      const uint32_t idesc = idesc_mx(kRows, a.NT, 0), stage_step = stage_bytes >> 4;
+      for (int t = tile0; ok && t < a.tiles; t += step) {
+        for (int i = 0; ok && i < W; ++i) ok = mbar_wait(&ctrl->accempty[W == 1 ? acc : (uint32_t)i], aph ^ 1u, abortp, a.status);
         tc_fence_after();
-        const uint32_t w = smem_u32(smem + (uint32_t)st * stage_bytes);
-        mma_stage(d, smem_desc_sw128(w), smem_desc_sw128(w + kWBytes), idesc_mx(kRows, a.NT, (uint32_t)(k & 3)), sfa, sfb, k != 0, smem_u32(&ctrl->empty[st]));
-        if (++st == a.stages) { st = 0; ph ^= 1u; }
-        if ((k & 3) == 3 || k + 1 == n_k) {
-          umma_commit(&ctrl->sfempty[sl]);
-          if (++sl == kSfSlots) { sl = 0; sph ^= 1u; }
+        for (int k = 0; ok && k < n_k; ++k) {
+          const uint32_t sfa = tmem + a.tmem_cols - (uint32_t)(kSfSlots - sl) * kSfCols, sfb = sfa + 4 * W;
+          if ((k & 3) == 0) {
+            if (!mbar_wait(&ctrl->sffull[sl], sph, abortp, a.status)) { ok = false; break; }
+            tc_fence_after();
+            const uint64_t src = lines + (uint32_t)sl * (kSfBytes >> 4);
+#pragma unroll
+            for (int i = 0; i < W; ++i) copy_scales(sfa + 4 * i, src + (uint32_t)i * (kLineBytes >> 4));
+            copy_scales(sfb, src + W * (kLineBytes >> 4));
+            if (a.NT > 128) copy_scales(sfb + 4, src + (W + 1) * (kLineBytes >> 4));
+          }
+          if (!mbar_wait(&ctrl->full[st], ph, abortp, a.status)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t w = wdesc + (uint32_t)st * stage_step;
+          const uint32_t id = idesc | (uint32_t)(k & 3) << 4 | (uint32_t)(k & 3) << 29;
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            mma_stage(tmem + (W == 1 ? acc : (uint32_t)i) * (uint32_t)a.NT, w + (uint32_t)i * (kWBytes >> 4), w + W * (kWBytes >> 4), id, sfa + 4 * i, sfb, k != 0);
+            if (i + 1 == W) commit(smem_u32(&ctrl->empty[st]));
+            if (k + 1 == n_k) commit(smem_u32(&ctrl->accfull[W == 1 ? acc : (uint32_t)i]));
+          }
+          if (++st == a.stages) { st = 0; ph ^= 1u; }
+          if ((k & 3) == 3 || k + 1 == n_k) {
+            commit(smem_u32(&ctrl->sfempty[sl]));
+            if (++sl == kSfSlots) { sl = 0; sph ^= 1u; }
+          }
         }
+        if (W == 1) acc ^= 1u;
+        if (W > 1 || acc == 0) aph ^= 1u;
       }
-      if (!ok) break;
-      umma_commit(&ctrl->accfull[acc]);
-      acc ^= 1u;
-      if (acc == 0) aph ^= 1u;
     }
+    __syncwarp();
   } else if (warp == 2) {
     int sl = 0;
     uint32_t sph = 0;
     bool ok = true;
     for (int t = tile0; ok && t < a.tiles; t += step) {
       const int mt = t % a.MT, rb = t / a.MT;
-      const uint8_t* ws = a.w_scale + (size_t)rb * a.pitch;
+      const uint8_t* ws = a.w_scale + (size_t)rb * W * a.pitch;
+      const bool second = W > 1 && rb * (W * kRows) + kRows < a.oc;
       for (int k = 0; k < n_k; k += 4) {
         const uint32_t ww = *reinterpret_cast<const uint32_t*>(ws + k0 + k);
+        const uint32_t ww2 = second ? *reinterpret_cast<const uint32_t*>(ws + a.pitch + k0 + k) : 0x7F7F7F7Fu;
         uint32_t xw[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -468,23 +546,24 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
         if (!mbar_wait(&ctrl->sfempty[sl], sph ^ 1u, abortp, a.status)) { ok = false; break; }
         uint4* dst = reinterpret_cast<uint4*>(sf + sl * kSfBytes) + lane;
         dst[0] = make_uint4(ww, ww, ww, ww);
-        dst[32] = make_uint4(xw[0], xw[1], xw[2], xw[3]);
-        dst[64] = make_uint4(xw[4], xw[5], xw[6], xw[7]);
+        if (W > 1) dst[32] = make_uint4(ww2, ww2, ww2, ww2);
+        dst[32 * W] = make_uint4(xw[0], xw[1], xw[2], xw[3]);
+        dst[32 * W + 32] = make_uint4(xw[4], xw[5], xw[6], xw[7]);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(&ctrl->sffull[sl]);
         if (++sl == kSfSlots) { sl = 0; sph ^= 1u; }
       }
     }
   } else if (warp >= 4) {
-    uint32_t acc = 0, aph = 0;
+    uint32_t acc = W > 1 ? (uint32_t)(warp >> 2) - 1u : 0u, aph = 0;        // with two tiles of weights each has its warps
     for (int t = tile0; t < a.tiles; t += step) {
       const int mt = t % a.MT, rb = t / a.MT, t0 = mt * a.NT;
       if (!mbar_wait(&ctrl->accfull[acc], aph, abortp, a.status)) break;
       tc_fence_after();
-      const uint32_t src = tmem + acc * (uint32_t)a.NT + ((uint32_t)(warp - 4) << 21);
-      const int row0 = rb * kRows + (warp - 4) * 32, nt = min(a.NT, a.M - t0);
+      const uint32_t src = tmem + acc * (uint32_t)a.NT + ((uint32_t)(warp & 3) << 21);
+      const int row0 = rb * (W * kRows) + (warp - 4) * 32, nt = min(a.NT, a.M - t0);
       uint8_t* out = sf + kSfSlots * kSfBytes + (warp - 4) * kOutBytes;
-      if (a.slices > 1) {
+      if (W == 1 && a.slices > 1) {
         // this slice's sums, where the stages were: [token][row]
         float* part = reinterpret_cast<float*>(smem) + (warp - 4) * 32 + lane;
         for (int c = 0; c < nt; c += 32) {
@@ -495,17 +574,17 @@ __global__ void __launch_bounds__(kThreads, 1) fp8_gemm_kernel(const __grid_cons
           for (int j = 0; j < 32; ++j)
             if (c + j < nt) part[(c + j) * kRows] = __uint_as_float(r[j]);
         }
-      } else if (a.y_dtype == RWKVQ_F32) store_tile<float>(a, src, row0, t0, nt, out, lane);
-      else if (a.y_dtype == RWKVQ_F16) store_tile<__half>(a, src, row0, t0, nt, out, lane);
-      else store_tile<__nv_bfloat16>(a, src, row0, t0, nt, out, lane);
-      tc_fence_before();
-      mbar_arrive(&ctrl->accempty[acc]);
-      acc ^= 1u;
-      if (acc == 0) aph ^= 1u;
+        tc_fence_before();
+        mbar_arrive(&ctrl->accempty[acc]);
+      } else if (a.y_dtype == RWKVQ_F32) store_tile<float>(a, src, row0, t0, nt, out, lane, &ctrl->accempty[acc]);
+      else if (a.y_dtype == RWKVQ_F16) store_tile<__half>(a, src, row0, t0, nt, out, lane, &ctrl->accempty[acc]);
+      else store_tile<__nv_bfloat16>(a, src, row0, t0, nt, out, lane, &ctrl->accempty[acc]);
+      if (W == 1) acc ^= 1u;
+      if (W > 1 || acc == 0) aph ^= 1u;
     }
   }
   __syncwarp();
-  if (a.slices > 1) {
+  if (W == 1 && a.slices > 1) {
     cluster_sync();
     if (a.y_dtype == RWKVQ_F32) add_slices<float>(a, smem, slice, tile0);
     else if (a.y_dtype == RWKVQ_F16) add_slices<__half>(a, smem, slice, tile0);
@@ -528,35 +607,38 @@ bool encode_codes(CUtensorMap* map, const void* codes, int rows, int cols, int b
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Tiles, slices and stages of a product: the cheapest by an estimate of an SM's cycles, fitted to 150 times of 17 products (1 to 1000 tokens, 1024 to 14336 x
-// 1024 to 14336), which it gives to within a tenth; over 16 others it is 2 % off the best choice on average, 9 % at most.  A stage takes 130 cycles and its
-// bytes at 64 a cycle, or the tensor core's 2 cycles a token where that is more; a tile's epilogue 14 a token; slices meet in 1500 and 45
-// a token (but up to 112), and their blocks have to fit side by side (clusters of eight only up to 112 blocks); nothing is faster than HBM.  More tiles of
-// fewer tokens or more slices fill SMs: 203 tokens x 7168 x 2048 10.0 us as two tiles (one: 11.7; in two slices: 12.8), 2048 x 7168 12.2 as two in four slices (one in
-// four: 14.4, four in two: 13.8), one token x 4096 x 4096 7.3 in four slices, 8.9 in two, 12.3 in one.
-struct Plan { int NT, MT, slices, stages; uint32_t tmem_cols, smem_bytes; };
-constexpr uint32_t kFixedBytes = 1024 + kSfSlots * kSfBytes + 4 * kOutBytes + kCtrlBytes;
+// Tiles, slices and stages of a product: the cheapest by an estimate of an SM's cycles, fitted to 145 times of 29 products (1 to 4096 tokens, 512 to 14336 x
+// 512 to 14336), which it gives to within a tenth (6 % on average); what it chooses is at most 3 % off the best of them, over 12 others as well.  A stage takes 290 cycles and its
+// bytes at 80 a cycle, or the tensor core's 2 cycles a token where that is more, and with two tiles of weights 1.72 times as much; the epilogue 16 a token, of one tile where
+// the next one's sums cover the others; slices meet in 2100 and 29 a token, and their blocks have to fit side by side (clusters of eight only up to 112 blocks); nothing is
+// faster than HBM.  More tiles of fewer tokens or more slices fill SMs: 203 tokens x 7168 x 2048 9.5 us as two tiles (one: 11.0; in two slices: 12.8), 2048 x 7168 12.0 as
+// two in four slices (one in four: 14.3, four in two: 13.5), one token x 4096 x 4096 7.1 in four slices, 8.6 in two, 11.8 in one.  Two tiles of weights take in a third less for
+// each product, but their epilogue stands alone and they fill SMs by larger steps: 1024 x 4096 x 4096 22.5 (one: 26.0), 512 x 4096 x 4096 17.5 (one: 14.7).
+struct Plan { int W, NT, MT, slices, stages; uint32_t tmem_cols, smem_bytes; };
+constexpr uint32_t fixed_bytes(int W) { return 1024 + kSfSlots * sf_bytes(W) + 4 * (uint32_t)W * kOutBytes + kCtrlBytes; }
 Plan plan_of(int M, int oc, int groups) {
   const int words = (groups + 3) / 4, sms = sm_count(), first = (int)(((long long)M + kMaxTokens - 1) / kMaxTokens);
-  const double hbm = ((double)oc + M) * groups * 128.0 / 3300.0;
+  const double hbm = ((double)oc + M) * groups * 128.0 / 2750.0;
   double best = 0.0;
   Plan l = {};
   for (int i = 0; i < 12; ++i) {
     const int NT = (int)((((long long)M + first + i - 1) / (first + i) + 15) / 16 * 16), MT = (int)(((long long)M + NT - 1) / NT);
-    if (NT == l.NT) continue;
     const long long tiles = (long long)blocks_of(oc) * MT;
-    const double stage = std::max(2.0 * NT, 130.0 + (kWBytes + NT * kStageCols) / 64.0);
+    const double stage = std::max(2.0 * NT, 290.0 + (kWBytes + NT * kStageCols) / 80.0);
     for (int S = 1; S <= kMaxSlices && S <= words; S *= 2) {
       if (S > 1 && tiles * S > (S == 8 ? std::min(112, sms) : sms)) break;
       const long long waves = S > 1 ? 1 : (tiles + sms - 1) / sms;
       const int stages = S > 1 ? (words + S - 1) / S * 4 : groups;
-      const double cost = std::max((double)waves * stages * stage, hbm) + 14.0 * NT + (S > 1 ? 1500.0 + 45.0 * std::min(NT, 112) : 0.0);
-      if (l.NT == 0 || cost < best) { best = cost; l.NT = NT; l.MT = MT; l.slices = S; }
+      const double cost = std::max((double)waves * stages * stage, hbm) + 16.0 * NT + (S > 1 ? 2100.0 + 29.0 * NT : 0.0);
+      if (l.NT == 0 || cost < best) { best = cost; l.W = 1; l.NT = NT; l.MT = MT; l.slices = S; }
     }
+    const long long tall = (blocks_of(oc) + 1) / 2 * (long long)MT;
+    const double cost = std::max((double)((tall + sms - 1) / sms) * (groups * 1.72 * stage + 16.0 * NT), hbm);
+    if (cost < best) { best = cost; l.W = 2; l.NT = NT; l.MT = MT; l.slices = 1; }
   }
-  const uint32_t stage = kWBytes + (uint32_t)l.NT * kStageCols;
-  l.stages = (int)std::min<uint32_t>(kMaxStages, (kMaxSmemBytes - kFixedBytes) / stage);
-  l.smem_bytes = kFixedBytes + (uint32_t)l.stages * stage;
+  const uint32_t stage = (uint32_t)l.W * kWBytes + (uint32_t)l.NT * kStageCols;
+  l.stages = (int)std::min<uint32_t>(kMaxStages, (kMaxSmemBytes - fixed_bytes(l.W)) / stage);
+  l.smem_bytes = fixed_bytes(l.W) + (uint32_t)l.stages * stage;
   l.tmem_cols = 32;
   while (l.tmem_cols < (uint32_t)l.NT * 2u + kSfSlots * kSfCols) l.tmem_cols *= 2;
   return l;
@@ -597,24 +679,25 @@ rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, in
   a.Y = Y; a.y_row = y_row; a.wide = (y_row * f8::element_size(y_dtype)) % 16 == 0; a.oc = oc; a.M = M; a.y_dtype = y_dtype;
   a.groups = f8::blocks_of(ic); a.pitch = (int)f8::scale_pitch(ic);
   const f8::Plan l = f8::plan_of(M, oc, a.groups);
-  const long long tiles = (long long)f8::blocks_of(oc) * l.MT;
+  const long long tiles = (long long)((f8::blocks_of(oc) + l.W - 1) / l.W) * l.MT;
   if (tiles > (1ll << 28)) return RWKVQ_EUNSUPPORTED;
   a.NT = l.NT; a.MT = l.MT; a.slices = l.slices; a.stages = l.stages; a.tiles = (int)tiles; a.tmem_cols = l.tmem_cols;
   a.status = device_status_ptr();
   if (!a.status) return RWKVQ_ECUDA;
-  if (!f8::encode_codes(&a.wmap, w_codes, oc, ic, f8::kRows) || !f8::encode_codes(&a.xmap, x_codes, M, ic, a.NT)) return RWKVQ_ECUDA;
-  static SmemOptIn opt_in(kCarveOut);
-  const cudaError_t e = opt_in((const void*)f8::fp8_gemm_kernel, (int)f8::kMaxSmemBytes);
+  if (!f8::encode_codes(&a.wmap, w_codes, oc, ic, l.W * f8::kRows) || !f8::encode_codes(&a.xmap, x_codes, M, ic, a.NT)) return RWKVQ_ECUDA;
+  static SmemOptIn opt_in[2] = {SmemOptIn(kCarveOut), SmemOptIn(kCarveOut)};
+  const auto kernel = l.W == 2 ? f8::fp8_gemm_kernel<2> : f8::fp8_gemm_kernel<1>;
+  const cudaError_t e = opt_in[l.W - 1]((const void*)kernel, (int)f8::kMaxSmemBytes);
   if (e != cudaSuccess) return cuda_status(e);
   cudaLaunchAttribute attr[2];
   const unsigned blocks = l.slices > 1 ? (unsigned)(a.tiles * l.slices) : (unsigned)std::min<int>(a.tiles, sm_count());
-  cudaLaunchConfig_t cfg = f8::launch_config(dim3(blocks), f8::kThreads, l.smem_bytes, static_cast<cudaStream_t>(stream), attr);
+  cudaLaunchConfig_t cfg = f8::launch_config(dim3(blocks), f8::threads_of(l.W), l.smem_bytes, static_cast<cudaStream_t>(stream), attr);
   if (l.slices > 1) {
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = (unsigned)l.slices; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.numAttrs = 2;
   }
-  return cuda_status(cudaLaunchKernelEx(&cfg, f8::fp8_gemm_kernel, a));
+  return cuda_status(cudaLaunchKernelEx(&cfg, kernel, a));
 }
 
 }  // extern "C"

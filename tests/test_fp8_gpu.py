@@ -290,3 +290,37 @@ def test_quantize_more_than_32_bits_of_elements(block):
         assert np.array_equal(codes[first:, c].cpu().numpy(), ref_codes)
         assert np.array_equal(scale[first // block:, c.start // 128:c.stop // 128].cpu().numpy(), ref_scale)
     assert (codes[:first] == 0).all() and (scale[:first // block] == 127).all()
+
+
+# shapes for which a block of the product takes two tiles of weights at a time: one stage and many, the second tile ragged or not there, rows of Y on and off 16 bytes
+TALL = [(1500, 1604, 16), (2100, 2312, 2064), (700, 4176, 144), (2100, 1104, 128), (4000, 1604, 400), (1000, 4130, 2064)]
+
+
+@pytest.mark.parametrize("shape", TALL, ids=str)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_product_of_many_tokens_against_64_bits(shape, dtype):
+    M, oc, ic = shape
+    wc, ws, xc, xs = product_inputs(M + oc + ic, M, oc, ic, *((114, 121) if dtype == "f16" else (120, 134)))
+    dev = [torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)]
+    wide = torch.full((M + 1, oc), 7.0, dtype=TYPES[dtype], device="cuda")
+    B.rwkvq_gemm_fp8(*dev, wide[:M])
+    torch.cuda.synchronize()
+    assert B.rwkvq_device_status() == 0
+    rows = np.unique(np.concatenate([np.arange(0, M, 61), np.arange(90, 114), np.arange(M - 3, M)]))
+    check_product(wide[:M][torch.from_numpy(rows).cuda()], dtype, wc, ws, xc[rows], xs[rows])
+    assert (wide[M] == 7).all()
+    again = torch.empty((M, oc), dtype=TYPES[dtype], device="cuda")
+    B.rwkvq_gemm_fp8(*dev, again)
+    assert torch.equal(again, wide[:M])
+
+
+def test_product_of_many_tokens_every_scale_has_its_place():
+    # as above, sums of powers of two: 2100 tokens, nineteen blocks of weights
+    M, oc, ic = 2100, 2312, 1664
+    gen = np.random.default_rng(6)
+    wc, xc = np.full((oc, ic), 0x38, np.uint8), np.full((M, ic), 0x38, np.uint8)
+    ws, xs = random_scales(gen, 19, ic, 124, 131), random_scales(gen, M, ic, 124, 131)
+    y = torch.empty((M, oc), device="cuda")
+    B.rwkvq_gemm_fp8(*[torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)], y)
+    ref = 2.0 ** (xs[:, :13].astype(np.float64) - 127.0) @ (128.0 * 2.0 ** (ws[:, :13].astype(np.float64) - 127.0)).T
+    assert np.array_equal(y.double().cpu().numpy(), np.repeat(ref, 128, 1)[:, :oc])
