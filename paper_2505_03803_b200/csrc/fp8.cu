@@ -332,7 +332,9 @@ __device__ __forceinline__ void tmem_ld_tiles_issue(uint32_t taddr, uint32_t (&r
 // of one token: the way there is through shared memory (`stage`, 4 KB of the warp's own), for 16-bit types by stmatrix, which turns 8 x 8 numbers round at
 // once (2048 x 14336 x 4096, one tile of weights a block: 110.5 us, 112.6 with a store of two bytes for each number).  The 64 bytes of a token lie in an order of 16-byte pieces that spares banks.
 // Without a.wide (rows of Y begin on 16 bytes), or with fewer channels, a store for each number.
-template <typename T>
+// The last 32 kHeld tokens are read before the first of them is stored: where the next tile's sums wait for `done`, the stores go on under them (three: 8192 x 7168 x 2048 124 ->
+// 119 us, 2048 x 14336 x 4096 117.5 -> 115.3; five spill).
+template <typename T, int kHeld>
 __device__ __forceinline__ void store_tile(const GemmArgs& a, uint32_t tmem, int row0, int t0, int nt, uint8_t* stage, int lane, uint64_t* done) {
   T* y = static_cast<T*>(a.Y) + (long long)t0 * a.y_row + row0;
   const bool wide = a.wide && row0 + 32 <= a.oc;
@@ -343,14 +345,12 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, uint32_t tmem, int
       const uint32_t to = smem_u32(stage) + (uint32_t)((lane & 7) * 64 + ((lane >> 3 ^ lane >> 1) & 3) * 16);
       const uint8_t* from = stage + (lane >> 2) * 64 + ((lane ^ lane >> 3) & 3) * 16;
       T* at = y + (long long)(lane >> 2) * a.y_row + (lane & 3) * 8;
-      tmem_ld_tiles_issue(tmem, r);
-      for (int c = 0; c < nt; c += 32) {
+      auto pack = [&](uint32_t (&v)[16]) {
         tmem_ld_wait(r);
-        uint32_t v[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = two_of(r[2 * i], r[2 * i + 1], T());       // 8 h + 2 n + x
-        if (c + 32 < nt) tmem_ld_tiles_issue(tmem + (uint32_t)c + 32u, r);
-        else is_read();
+      };
+      auto store = [&](int c, const uint32_t (&v)[16]) {
         const uint32_t half = (uint32_t)(c & 32) * 64u;        // in turn, so that no lane writes where another still reads
 #pragma unroll
         for (int n = 0; n < 4; ++n)
@@ -363,7 +363,25 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, uint32_t tmem, int
           if (c + i * 8 + (lane >> 2) < nt) *reinterpret_cast<uint4*>(at) = x;
           at += 8 * a.y_row;
         }
+      };
+      uint32_t v[kHeld][16];
+      int c = 0;
+      tmem_ld_tiles_issue(tmem, r);
+      for (; nt - c > 32 * kHeld; c += 32) {
+        pack(v[0]);
+        tmem_ld_tiles_issue(tmem + (uint32_t)c + 32u, r);
+        store(c, v[0]);
       }
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (c + 32 * i < nt) {
+          pack(v[i]);
+          if (c + 32 * i + 32 < nt) tmem_ld_tiles_issue(tmem + (uint32_t)(c + 32 * i) + 32u, r);
+        }
+      is_read();
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (c + 32 * i < nt) store(c + 32 * i, v[i]);
       return;
     }
   }
@@ -555,6 +573,7 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
       }
     }
   } else if (warp >= 4) {
+    constexpr int kHeld = W > 1 ? 3 : 1;
     uint32_t acc = W > 1 ? (uint32_t)(warp >> 2) - 1u : 0u, aph = 0;        // with two tiles of weights each has its warps
     for (int t = tile0; t < a.tiles; t += step) {
       const int mt = t % a.MT, rb = t / a.MT, t0 = mt * a.NT;
@@ -576,9 +595,9 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
         }
         tc_fence_before();
         mbar_arrive(&ctrl->accempty[acc]);
-      } else if (a.y_dtype == RWKVQ_F32) store_tile<float>(a, src, row0, t0, nt, out, lane, &ctrl->accempty[acc]);
-      else if (a.y_dtype == RWKVQ_F16) store_tile<__half>(a, src, row0, t0, nt, out, lane, &ctrl->accempty[acc]);
-      else store_tile<__nv_bfloat16>(a, src, row0, t0, nt, out, lane, &ctrl->accempty[acc]);
+      } else if (a.y_dtype == RWKVQ_F32) store_tile<float, kHeld>(a, src, row0, t0, nt, out, lane, &ctrl->accempty[acc]);
+      else if (a.y_dtype == RWKVQ_F16) store_tile<__half, kHeld>(a, src, row0, t0, nt, out, lane, &ctrl->accempty[acc]);
+      else store_tile<__nv_bfloat16, kHeld>(a, src, row0, t0, nt, out, lane, &ctrl->accempty[acc]);
       if (W == 1) acc ^= 1u;
       if (W > 1 || acc == 0) aph ^= 1u;
     }
