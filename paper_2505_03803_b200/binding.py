@@ -820,8 +820,11 @@ def rwkvq_linattn(r, k, v, logw, u, out, state, state_out=None, seq_start=None, 
             _elsewhere(where, u, here)
         if u.dtype is not t.float32 or u.shape != (heads, n) or not u.is_contiguous():
             _refuse(where, f"u has to be float32 [{heads}, {n}], contiguous")
-    if workspace is not None and workspace.get_device() != here:
-        _elsewhere(where, workspace, here)
+    if workspace is not None:
+        if workspace.get_device() != here:
+            _elsewhere(where, workspace, here)
+        if not workspace.is_contiguous():
+            _refuse(where, "workspace has to be contiguous")
     types = _DTYPES or _dtypes()
     at = 0 if state is None else state.data_ptr()
     args = _LINATTN_ARGS.pack(r.data_ptr(), k.data_ptr(), v.data_ptr(), logw.data_ptr(), 0 if u is None else u.data_ptr(), out.data_ptr(), at,

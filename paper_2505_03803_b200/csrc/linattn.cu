@@ -144,8 +144,8 @@ __global__ void __launch_bounds__(kTokenThreads) linattn_token_kernel(const __gr
 // sequence's own), where the sequence goes on behind the block; then all blocks at once, each beginning with what those before it left.
 //
 // What bounds it, 2048 tokens, 64 heads, bf16, decays fp32: 23 us the states' pass, 52 the other (ncu, cold; 69 in all, warm and one under the other), of which HBM needs 15.5.
-// Shared memory's data path is busy 70 % of the cycles that an SM is active (operands are written once and read by all multiplying warps), issue slots 54 %, the tensor pipe 28 %:
-// about 3 100 warp instructions and 1 050 wavefronts a chunk.  Taken back: parts of a block halved over a cluster in the states' pass (no gain, 203 tokens 11.3 -> 13.2), five
+// Of the cycles that an SM is active, shared memory's data path is busy 53 % (operands are written once and read by all multiplying warps), issue slots 49 %, the tensor pipe 28 %, with
+// twelve warps in 168 registers: neither a full pipe nor enough warps to wait beside one another.  A chunk is about 3 100 warp instructions.  Taken back: parts of a block halved over a cluster in the states' pass (no gain, 203 tokens 11.3 -> 13.2), five
 // stages of inputs (no gain), three or four blocks an SM (spills), the triangles through shared memory (82 us where registers took 77).
 // 203 tokens, 32 heads 11.2; 5000 rows of eleven sequences, one decay a head, fp16 175; fp32, N 128, 1111 tokens of 16 heads 56, six products where bf16 takes three.
 

@@ -350,3 +350,25 @@ def test_a_cache_of_more_than_32_bits():
         ref, tol, S, tolS = expected(c, device="cuda")
         near(out, ref, tol, "out")
         near(state[ids.long()], S, tolS, "state")
+
+
+@pytest.mark.parametrize("what", ["heads apart", "values apart", "another type", "short logw", "decays of a third type", "u in half", "states in half", "states strided",
+                                  "states of another count", "slots short", "slots of 64 bits", "rows on the host", "workspace short", "workspace strided"])
+def test_binding_refuses(what):
+    T, H, N, n_seq = 64, 2, 64, 2
+    z = lambda *s, dtype=torch.float16: torch.zeros(s, dtype=dtype, device="cuda")
+    size = B.rwkvq_linattn_workspace_bytes(T, n_seq, H, N)
+    a = dict(r=z(T, H, N), k=z(T, H, N), v=z(T, H, N), logw=z(T, H, N), u=z(H, N, dtype=torch.float32), out=z(T, H, N), state=z(3, H, N, N, dtype=torch.float32),
+             seq_start=torch.tensor([0, 30, 64], dtype=torch.int32, device="cuda"), slots=torch.tensor([2, 0], dtype=torch.int32, device="cuda"),
+             workspace=z(size, dtype=torch.uint8))
+    bad = {"heads apart": dict(r=z(T, 2 * H, N)[:, ::2]), "values apart": dict(v=z(T, H, 2 * N)[..., ::2]), "another type": dict(k=z(T, H, N, dtype=torch.bfloat16)),
+           "short logw": dict(logw=z(T - 1, H, N)), "decays of a third type": dict(logw=z(T, H, N, dtype=torch.bfloat16)), "u in half": dict(u=z(H, N)),
+           "states in half": dict(state=z(3, H, N, N)), "states strided": dict(state=z(3, H, N, 2 * N, dtype=torch.float32)[..., ::2]),
+           "states of another count": dict(state_out=z(4, H, N, N, dtype=torch.float32)), "slots short": dict(slots=a["slots"][:1]),
+           "slots of 64 bits": dict(slots=a["slots"].long()), "rows on the host": dict(seq_start=a["seq_start"].cpu()),
+           "workspace short": dict(workspace=z(size - 16, dtype=torch.uint8)), "workspace strided": dict(workspace=z(2 * size, dtype=torch.uint8)[::2])}
+    B.rwkvq_linattn(**a)
+    with pytest.raises(B.RwkvqError):
+        B.rwkvq_linattn(**dict(a, **bad[what]))
+    torch.cuda.synchronize()
+    assert B.rwkvq_device_status() == 0
