@@ -235,7 +235,7 @@ cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int blo
 // Scales: four groups' bytes of a row are the word that the instruction picks its byte from; warp 2 deals the words of 512 columns out in the order
 // of the copy to tensor memory (32 lanes x 16 bytes, row r in line r % 32, word r / 32), where they lie once per 32-lane quarter.
 //
-// What bounds it.  One token: launch, the latency of the first loads and of the slices' meeting (4096 x 4096 7.1 us with weights from HBM, which needs 2.6).  Few tokens,
+// What bounds it.  One token: launch, the latency of the first loads and of the slices' meeting (4096 x 4096 6.6 us with weights from HBM, which needs 2.6).  Few tokens,
 // large matrices: HBM (65536 x 4096, 16 tokens, 45.6 us = 5.9 TB/s).  Many: power.  2048 x 4096 x 14336 over and over takes 110 us (2.2 PFLOP/s) at 990 W, the limit,
 // which leaves 1.47 of 1.97 GHz; 106 without scales, 125 with one tile of weights a block.  A stage of two brings 63 KB for 256 x 240 outputs, of one 47 KB for 128 x 240,
 // and shared memory, which these pass twice (in, and to the tensor core), is then busier than the tensor core.
@@ -468,34 +468,42 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
     for (int i = 0; i < kSfSlots; ++i) { mbar_init(&ctrl->sffull[i], 32); mbar_init(&ctrl->sfempty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&ctrl->accfull[i], 1); mbar_init(&ctrl->accempty[i], 128); }
     ctrl->abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;\nfence.proxy.async.shared::cta;" ::: "memory");
   }
-  asm volatile("griddepcontrol.launch_dependents;");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  // Only now: tensor memory taken while an earlier kernel still wants some would be waited for by it, and it by this one.
-  if (warp == 3) tmem_alloc(&ctrl->tmem_base, a.tmem_cols);
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = ctrl->tmem_base;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   // A cluster of `slices` blocks has one tile, each a range of its columns (whole words of scales); without slices a block goes from tile to tile.
   const int slice = a.slices > 1 ? (int)(blockIdx.x % (unsigned)a.slices) : 0, tile0 = (int)(blockIdx.x / (unsigned)a.slices);
   const int step = a.slices > 1 ? a.tiles : (int)gridDim.x;
   const int words = (a.groups + 3) / 4, k0 = words * slice / a.slices * 4, n_k = min(a.groups, words * (slice + 1) / a.slices * 4) - k0;
-
+  auto fetch = [&](int t, int k, int st) {
+    uint8_t* w = smem + (uint32_t)st * stage_bytes;
+    mbar_arrive_expect_tx(&ctrl->full[st], stage_bytes);
+    tensor_g2s(w, &a.wmap, (k0 + k) * kStageCols, t / a.MT * (W * kRows), &ctrl->full[st]);
+    tensor_g2s(w + W * kWBytes, &a.xmap, (k0 + k) * kStageCols, t % a.MT * a.NT, &ctrl->full[st]);
+  };
+  // The first two stages are on their way before anything else, and copies and scales do not wait for tensor memory (one token, 4096 x 4096, 7.0 -> 6.4 us; 13 tokens, 4096 x 14336,
+  // 15.2 -> 13.9).
+  const int first = min(n_k, 2);               // there are at least three stages
+  if (threadIdx.x == 0) {
+    for (int k = 0; k < first; ++k) fetch(tile0, k, k);
+  }
+  // Only now: tensor memory taken while an earlier kernel still wants some would be waited for by it, and it by this one.
+  if (warp == 3) tmem_alloc(&ctrl->tmem_base, a.tmem_cols);
+  tc_fence_before();
+  if (warp != 2 && warp != 0) asm volatile("bar.sync 1, %0;" ::"n"(threads_of(W) - 64) : "memory");
+  tc_fence_after();
+  asm volatile("griddepcontrol.launch_dependents;");
+  const uint32_t tmem = ctrl->tmem_base;       // warps 0 and 2, which do not wait for it, have no use for it
   if (warp == 0) {
     if (lane == 0) {
-      int st = 0, asked = 0;
+      int st = first, asked = first;
       uint32_t ph = 0;
       bool ok = true;
       for (int t = tile0; ok && t < a.tiles; t += step) {
-        const int mt = t % a.MT, rb = t / a.MT;
-        for (int k = 0; k < n_k; ++k, ++asked) {
+        for (int k = t == tile0 ? first : 0; k < n_k; ++k, ++asked) {
           if (!mbar_wait(&ctrl->empty[st], ph ^ 1u, abortp, a.status)) { ok = false; break; }
-          uint8_t* w = smem + (uint32_t)st * stage_bytes;
-          mbar_arrive_expect_tx(&ctrl->full[st], stage_bytes);
-          tensor_g2s(w, &a.wmap, (k0 + k) * kStageCols, rb * (W * kRows), &ctrl->full[st]);
-          tensor_g2s(w + W * kWBytes, &a.xmap, (k0 + k) * kStageCols, mt * a.NT, &ctrl->full[st]);
+          fetch(t, k, st);
           if (++st == a.stages) { st = 0; ph ^= 1u; }
         }
       }
