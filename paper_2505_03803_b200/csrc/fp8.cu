@@ -638,9 +638,9 @@ bool encode_codes(CUtensorMap* map, const void* codes, int rows, int cols, int b
 // 512 to 14336), which it gives to within a tenth (6 % on average); what it chooses is at most 3 % off the best of them, over 12 others as well.  A stage takes 290 cycles and its
 // bytes at 80 a cycle, or the tensor core's 2 cycles a token where that is more, and with two tiles of weights 1.72 times as much; the epilogue 16 a token, of one tile where
 // the next one's sums cover the others; slices meet in 2100 and 29 a token, and their blocks have to fit side by side (clusters of eight only up to 112 blocks); nothing is
-// faster than HBM.  More tiles of fewer tokens or more slices fill SMs: 203 tokens x 7168 x 2048 9.5 us as two tiles (one: 11.0; in two slices: 12.8), 2048 x 7168 12.0 as
-// two in four slices (one in four: 14.3, four in two: 13.5), one token x 4096 x 4096 7.1 in four slices, 8.6 in two, 11.8 in one.  Two tiles of weights take in a third less for
-// each product, but their epilogue stands alone and they fill SMs by larger steps: 1024 x 4096 x 4096 22.5 (one: 26.0), 512 x 4096 x 4096 17.5 (one: 14.7).
+// faster than HBM.  More tiles of fewer tokens or more slices fill SMs: 203 tokens x 7168 x 2048 8.9 us as two tiles (one: 10.5; in two slices: 12.2), 2048 x 7168 11.7 as
+// two in four slices (one in four: 14.0, four in two: 13.7), one token x 4096 x 4096 6.5 in four slices, 8.6 in two, 12.3 in one.  Two tiles of weights take in a third less for
+// each product, but their epilogue stands alone and they fill SMs by larger steps: 1024 x 4096 x 4096 20.8 (one: 24.9), 512 x 4096 x 4096 17.7 (one: 14.5).
 struct Plan { int W, NT, MT, slices, stages; uint32_t tmem_cols, smem_bytes; };
 constexpr uint32_t fixed_bytes(int W) { return 1024 + kSfSlots * sf_bytes(W) + 4 * (uint32_t)W * kOutBytes + kCtrlBytes; }
 Plan plan_of(int M, int oc, int groups) {
