@@ -450,8 +450,9 @@ rwkvq_status rwkvq_gemm_fp8(const void* w_codes_dev, const void* w_scale_dev, in
  *  state, state_out: [n_slots][heads][n][n] fp32 (keys, values), the same buffer (updated in place) or two that do not overlap.  slots: [n_seq]
  *      which of them belongs to each sequence (NULL: sequence i has state i), device memory; -1: begins with zeros, is not kept.  state NULL: all begin with
  *      zeros; state_out NULL: none is kept.  States of no sequence are not touched.
- * Rows of seq_start out of order, a slot that does not exist, or that an earlier sequence of the call has: that sequence is left out (outputs and
- * state as they were) and rwkvq_device_status reports EINVAL.
+ * A sequence that ends in front of its beginning or behind the rows, that begins in front of any entry of seq_start before its own, whose slot does not exist, or
+ * whose slot an earlier sequence of the call has: it is left out (outputs and state as they were), the others are computed, and rwkvq_device_status
+ * reports EINVAL.
  * workspace_dev: rwkvq_linattn_workspace_bytes() bytes (enough for fewer tokens and sequences, too), 16-byte aligned, contents irrelevant, not shared by calls in flight at the same time.
  * Pointers (and rows of r, k, v, out, and of logw without decay_per_head) 16-byte aligned; out overlaps no input.  Asynchronous on `stream`.
  * Errors: EINVAL, EALIGN, EUNSUPPORTED (another n, more than 65535 sequences or heads, more than 2^30 tokens), ENOMEM (workspace too small), ECUDA.

@@ -74,7 +74,14 @@ __global__ void __launch_bounds__(kTokenThreads) linattn_token_kernel(const __gr
   if (a.slots) {
     slot = a.slots[seq];
     bad = bad || slot < -1 || slot >= a.n_slots;
-    for (int j = tid; j < seq; j += kTokenThreads) bad = bad || (slot >= 0 && a.slots[j] == slot);      // a state belongs to one sequence of a call
+  }
+  // Sequences of a call share neither a state nor rows: one that begins in front of an entry of the list before its own could have rows of a sequence that is computed, and
+  // the chunk kernels' blocks keep one state each for a sequence that goes on behind them.
+  if (a.slots || a.seq_start) {
+    for (int j = tid; j < seq; j += kTokenThreads) {
+      const int other = a.slots ? a.slots[j] : -1, before = a.seq_start ? a.seq_start[j] : 0;
+      bad = bad | (slot >= 0 && other == slot) | (before > start);
+    }
   }
   bad = __syncthreads_or(bad);
   if (tid == 0 && h == 0 && v0 == 0) {

@@ -372,3 +372,25 @@ def test_binding_refuses(what):
         B.rwkvq_linattn(**dict(a, **bad[what]))
     torch.cuda.synchronize()
     assert B.rwkvq_device_status() == 0
+
+
+# lists that fall back: a sequence that begins in front of an entry before its own may share rows with one that is computed
+@pytest.mark.parametrize("starts,good,heads", [([0, 100, 50, 150], [0], 2), ([0, 2000, 1000, 2500], [0], 64), ([0, 30, 20, 64, 90], [0, 3], 3), ([40, 10, 50, 90], [2], 2),
+                                               ([0, 3, 1, 5], [0], 2), ([0, 700, 600, 1300, 1300, 1290, 1400], [0, 3], 40)], ids=str)
+@pytest.mark.parametrize("slots", [False, True])
+def test_a_sequence_that_begins_in_front_of_an_earlier_one_is_left_out(starts, good, heads, slots):
+    n_seq = len(starts) - 1
+    c = make(71, [max(starts)], heads, 64, "bf16", extra_slots=n_seq + 1)
+    c["lens"], c["starts"] = [0] * n_seq, starts
+    c["slots"] = torch.randperm(n_seq + 2, generator=torch.Generator().manual_seed(5))[:n_seq].to(torch.int32) if slots else None
+    out, st, _ = call(c, ragged=True)
+    assert B.rwkvq_device_status() == 1 and B.rwkvq_device_status() == 0
+    rest, kept = torch.ones(c["T"], dtype=torch.bool), torch.ones(n_seq + 2, dtype=torch.bool)
+    for i in good:
+        a, b, s = starts[i], starts[i + 1], int(c["slots"][i]) if slots else i
+        one = dict(c, starts=[a, b], slots=torch.tensor([s], dtype=torch.int32))
+        ref, tol, S, tolS = expected(one, device="cuda")
+        near(out[a:b], ref[a:b], tol[a:b], f"sequence {i}")
+        near(st[s], S[s], tolS[s], f"state of sequence {i}")
+        rest[a:b], kept[s] = False, False
+    assert (out[rest.cuda()] == 7).all() and torch.equal(st.cpu()[kept], c["state"][kept])
