@@ -435,6 +435,14 @@ rwkvq_status rwkvq_fp8_quantize(const void* x_dev, int dtype, int rows, int cols
                                 void* codes_dev, void* scale_dev, void* stream);
 rwkvq_status rwkvq_gemm_fp8(const void* w_codes_dev, const void* w_scale_dev, int oc, int ic, const void* x_codes_dev,
                             const void* x_scale_dev, int M, void* Y_dev, int y_dtype, long long y_row, void* stream);
+/*
+ * rwkvq_gemm_fp8 with another limit for its waits (polls; 0 = default) and thread blocks that announce scales only for the first `announced` pieces of 512 columns that they
+ * work on: the wait for the next runs out.  lost_dev[4] (int32, added to): blocks that gave up, stages whose copies these had asked for, blocks that saw
+ * all of these arrive before they left, blocks that saw the tensor core done.  The outputs are not to be used.  Exists so that a test can watch the blocks leave.
+ */
+rwkvq_status rwkvq_gemm_fp8_lost(const void* w_codes_dev, const void* w_scale_dev, int oc, int ic, const void* x_codes_dev,
+                                 const void* x_scale_dev, int M, void* Y_dev, int y_dtype, long long y_row, uint32_t poll_limit,
+                                 int announced, int32_t* lost_dev, void* stream);
 
 /*
  * Linear attention with decaying state, what an RWKV-6-shaped block has between its R, K, V and O projections: for each sequence and head, with

@@ -258,14 +258,18 @@ struct GemmArgs {
   int oc, M, groups, pitch, NT, MT, tiles, stages, slices, y_dtype, wide;
   uint32_t tmem_cols;
   int* status;
+  // For a test (rwkvq_gemm_fp8_lost), kernels of their own: the limit of a wait in polls, how many words of scales a block announces, where blocks that give up are counted.
+  uint32_t poll_limit;
+  int announced;
+  int* lost;
 };
 
 struct Ctrl {
   uint64_t full[kMaxStages], empty[kMaxStages];
   uint64_t sffull[kSfSlots], sfempty[kSfSlots];
-  uint64_t accfull[2], accempty[2];
+  uint64_t accfull[2], accempty[2], drained;
   uint32_t tmem_base;
-  int abort_flag;
+  int abort_flag, asked;        // asked: copies of stages
 };
 static_assert(sizeof(Ctrl) <= kCtrlBytes, "control block");
 
@@ -447,13 +451,30 @@ __device__ __forceinline__ void add_slices(const GemmArgs& a, uint8_t* smem, int
   else add_slices<T, 8>(a, smem, slice, tile);
 }
 
-// A block that gives up leaves only when the copies it has asked for have arrived: `asked` of them, one a stage in turn (with a limit, as all waits).
-__device__ __forceinline__ void await_copies(Ctrl* ctrl, int asked, int stages) {
-  for (int i = max(0, asked - stages); i < asked; ++i)
-    for (uint32_t it = 0; it < kPollLimit && !mbar_try_wait(&ctrl->full[i % stages], (uint32_t)(i / stages) & 1u); ++it) {}
+// A block that gives up, whichever of its roles ran out of polls, leaves only when the copies that it has asked for have arrived, one a stage in turn, and the tensor core is done
+// with what it was told: until then they write to its shared and tensor memory and read it.  Called by all threads once the roles have joined; each wait has a limit, as all waits.
+template <bool kLost>
+__device__ __forceinline__ void leave_in_order(const GemmArgs& a, Ctrl* ctrl) {
+  auto arrived = [](uint64_t* bar, uint32_t parity) {
+    uint32_t it = 0;
+    while (it < kPollLimit && !mbar_try_wait(bar, parity)) ++it;
+    return it < kPollLimit;
+  };
+  if (threadIdx.x == 0) {
+    bool all = true;
+    for (int i = max(0, ctrl->asked - a.stages); i < ctrl->asked; ++i) all = arrived(&ctrl->full[i % a.stages], (uint32_t)(i / a.stages) & 1u) && all;
+    if (kLost) { atomicAdd(a.lost, 1); atomicAdd(a.lost + 1, ctrl->asked); if (all) atomicAdd(a.lost + 2, 1); }
+  }
+  if (threadIdx.x >> 5 == 1 && elected()) {         // the thread that issued the instructions
+    commit(smem_u32(&ctrl->drained));
+    const bool done = arrived(&ctrl->drained, 0);
+    if (kLost && done) atomicAdd(a.lost + 3, 1);
+  }
+  __syncthreads();
 }
 
-template <int W>
+// kLost: see GemmArgs.  (A limit that is not a constant costs some 40 cycles a stage: 2048 x 14336 x 4096 113.2 -> 115.8 us.)
+template <int W, bool kLost>
 __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid_constant__ GemmArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
@@ -463,10 +484,12 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
   Ctrl* ctrl = reinterpret_cast<Ctrl*>(sf + kSfSlots * kSfBytes + 4 * W * kOutBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abortp = &ctrl->abort_flag;
+  const uint32_t limit = kLost ? a.poll_limit : kPollLimit;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kMaxStages; ++i) { mbar_init(&ctrl->full[i], 1); mbar_init(&ctrl->empty[i], 1); }
     for (int i = 0; i < kSfSlots; ++i) { mbar_init(&ctrl->sffull[i], 32); mbar_init(&ctrl->sfempty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&ctrl->accfull[i], 1); mbar_init(&ctrl->accempty[i], 128); }
+    mbar_init(&ctrl->drained, 1);
     ctrl->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\nfence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -502,12 +525,12 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
       bool ok = true;
       for (int t = tile0; ok && t < a.tiles; t += step) {
         for (int k = t == tile0 ? first : 0; k < n_k; ++k, ++asked) {
-          if (!mbar_wait(&ctrl->empty[st], ph ^ 1u, abortp, a.status)) { ok = false; break; }
+          if (!mbar_wait(&ctrl->empty[st], ph ^ 1u, abortp, a.status, limit)) { ok = false; break; }
           fetch(t, k, st);
           if (++st == a.stages) { st = 0; ph ^= 1u; }
         }
       }
-      if (!ok) await_copies(ctrl, asked, a.stages);
+      ctrl->asked = asked;
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -518,12 +541,12 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
       const uint64_t wdesc = smem_desc_sw128(smem_u32(smem)), lines = smem_desc_lines(smem_u32(sf));
       const uint32_t idesc = idesc_mx(kRows, a.NT, 0), stage_step = stage_bytes >> 4;
       for (int t = tile0; ok && t < a.tiles; t += step) {
-        for (int i = 0; ok && i < W; ++i) ok = mbar_wait(&ctrl->accempty[W == 1 ? acc : (uint32_t)i], aph ^ 1u, abortp, a.status);
+        for (int i = 0; ok && i < W; ++i) ok = mbar_wait(&ctrl->accempty[W == 1 ? acc : (uint32_t)i], aph ^ 1u, abortp, a.status, limit);
         tc_fence_after();
         for (int k = 0; ok && k < n_k; ++k) {
           const uint32_t sfa = tmem + a.tmem_cols - (uint32_t)(kSfSlots - sl) * kSfCols, sfb = sfa + 4 * W;
           if ((k & 3) == 0) {
-            if (!mbar_wait(&ctrl->sffull[sl], sph, abortp, a.status)) { ok = false; break; }
+            if (!mbar_wait(&ctrl->sffull[sl], sph, abortp, a.status, limit)) { ok = false; break; }
             tc_fence_after();
             const uint64_t src = lines + (uint32_t)sl * (kSfBytes >> 4);
 #pragma unroll
@@ -531,7 +554,7 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
             copy_scales(sfb, src + W * (kLineBytes >> 4));
             if (a.NT > 128) copy_scales(sfb + 4, src + (W + 1) * (kLineBytes >> 4));
           }
-          if (!mbar_wait(&ctrl->full[st], ph, abortp, a.status)) { ok = false; break; }
+          if (!mbar_wait(&ctrl->full[st], ph, abortp, a.status, limit)) { ok = false; break; }
           tc_fence_after();
           const uint64_t w = wdesc + (uint32_t)st * stage_step;
           const uint32_t id = idesc | (uint32_t)(k & 3) << 4 | (uint32_t)(k & 3) << 29;
@@ -553,7 +576,7 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
     }
     __syncwarp();
   } else if (warp == 2) {
-    int sl = 0;
+    int sl = 0, said = 0;
     uint32_t sph = 0;
     bool ok = true;
     for (int t = tile0; ok && t < a.tiles; t += step) {
@@ -569,14 +592,14 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
           const int r = j * 32 + lane, tok = mt * a.NT + r;
           xw[j] = r < a.NT && tok < a.M ? *reinterpret_cast<const uint32_t*>(a.x_scale + (size_t)tok * a.pitch + k0 + k) : 0x7F7F7F7Fu;
         }
-        if (!mbar_wait(&ctrl->sfempty[sl], sph ^ 1u, abortp, a.status)) { ok = false; break; }
+        if (!mbar_wait(&ctrl->sfempty[sl], sph ^ 1u, abortp, a.status, limit)) { ok = false; break; }
         uint4* dst = reinterpret_cast<uint4*>(sf + sl * kSfBytes) + lane;
         dst[0] = make_uint4(ww, ww, ww, ww);
         if (W > 1) dst[32] = make_uint4(ww2, ww2, ww2, ww2);
         dst[32 * W] = make_uint4(xw[0], xw[1], xw[2], xw[3]);
         dst[32 * W + 32] = make_uint4(xw[4], xw[5], xw[6], xw[7]);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(&ctrl->sffull[sl]);
+        if (!kLost || said++ < a.announced) mbar_arrive(&ctrl->sffull[sl]);
         if (++sl == kSfSlots) { sl = 0; sph ^= 1u; }
       }
     }
@@ -585,7 +608,7 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
     uint32_t acc = W > 1 ? (uint32_t)(warp >> 2) - 1u : 0u, aph = 0;        // with two tiles of weights each has its warps
     for (int t = tile0; t < a.tiles; t += step) {
       const int mt = t % a.MT, rb = t / a.MT, t0 = mt * a.NT;
-      if (!mbar_wait(&ctrl->accfull[acc], aph, abortp, a.status)) break;
+      if (!mbar_wait(&ctrl->accfull[acc], aph, abortp, a.status, limit)) break;
       tc_fence_after();
       const uint32_t src = tmem + acc * (uint32_t)a.NT + ((uint32_t)(warp & 3) << 21);
       const int row0 = rb * (W * kRows) + (warp - 4) * 32, nt = min(a.NT, a.M - t0);
@@ -621,6 +644,7 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (ctrl->abort_flag) leave_in_order<kLost>(a, ctrl);
   if (warp == 3) tmem_dealloc(tmem, a.tmem_cols);
 }
 
@@ -676,6 +700,7 @@ int element_size(int dtype) { return dtype == RWKVQ_F32 ? 4 : dtype == RWKVQ_F16
 }  // namespace rwkvq
 
 using namespace rwkvq;
+using tc5::kPollLimit;
 
 extern "C" {
 
@@ -695,8 +720,8 @@ rwkvq_status rwkvq_fp8_quantize(const void* x, int dtype, int rows, int cols, lo
   return cuda_status(f8::quantize<__nv_bfloat16>(x, x_row, rows, cols, block_rows, codes, scale, pitch, s));
 }
 
-rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, int ic, const void* x_codes, const void* x_scale, int M, void* Y, int y_dtype,
-                            long long y_row, void* stream) {
+static rwkvq_status gemm_fp8(const void* w_codes, const void* w_scale, int oc, int ic, const void* x_codes, const void* x_scale, int M, void* Y, int y_dtype,
+                             long long y_row, uint32_t poll_limit, int announced, int* lost, void* stream) {
   if (!w_codes || !w_scale || !x_codes || !x_scale || !Y || oc <= 0 || ic <= 0 || M <= 0 || f8::element_size(y_dtype) == 0 || y_row < oc) return RWKVQ_EINVAL;
   if (ic % 16) return RWKVQ_ESHAPE;
   if (!aligned16(w_codes) || !aligned16(w_scale) || !aligned16(x_codes) || !aligned16(x_scale) || !aligned16(Y)) return RWKVQ_EALIGN;
@@ -711,10 +736,12 @@ rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, in
   a.NT = l.NT; a.MT = l.MT; a.slices = l.slices; a.stages = l.stages; a.tiles = (int)tiles; a.tmem_cols = l.tmem_cols;
   a.status = device_status_ptr();
   if (!a.status) return RWKVQ_ECUDA;
+  a.poll_limit = poll_limit; a.lost = lost; a.announced = announced;
   if (!f8::encode_codes(&a.wmap, w_codes, oc, ic, l.W * f8::kRows) || !f8::encode_codes(&a.xmap, x_codes, M, ic, a.NT)) return RWKVQ_ECUDA;
-  static SmemOptIn opt_in[2] = {SmemOptIn(kCarveOut), SmemOptIn(kCarveOut)};
-  const auto kernel = l.W == 2 ? f8::fp8_gemm_kernel<2> : f8::fp8_gemm_kernel<1>;
-  const cudaError_t e = opt_in[l.W - 1]((const void*)kernel, (int)f8::kMaxSmemBytes);
+  static SmemOptIn opt_in[4] = {SmemOptIn(kCarveOut), SmemOptIn(kCarveOut), SmemOptIn(kCarveOut), SmemOptIn(kCarveOut)};
+  const auto kernel = lost ? (l.W == 2 ? f8::fp8_gemm_kernel<2, true> : f8::fp8_gemm_kernel<1, true>)
+                           : (l.W == 2 ? f8::fp8_gemm_kernel<2, false> : f8::fp8_gemm_kernel<1, false>);
+  const cudaError_t e = opt_in[(lost ? 2 : 0) + l.W - 1]((const void*)kernel, (int)f8::kMaxSmemBytes);
   if (e != cudaSuccess) return cuda_status(e);
   cudaLaunchAttribute attr[2];
   const unsigned blocks = l.slices > 1 ? (unsigned)(a.tiles * l.slices) : (unsigned)std::min<int>(a.tiles, sm_count());
@@ -725,6 +752,17 @@ rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, in
     cfg.numAttrs = 2;
   }
   return cuda_status(cudaLaunchKernelEx(&cfg, kernel, a));
+}
+
+rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, int ic, const void* x_codes, const void* x_scale, int M, void* Y, int y_dtype,
+                            long long y_row, void* stream) {
+  return gemm_fp8(w_codes, w_scale, oc, ic, x_codes, x_scale, M, Y, y_dtype, y_row, kPollLimit, 0, nullptr, stream);
+}
+
+rwkvq_status rwkvq_gemm_fp8_lost(const void* w_codes, const void* w_scale, int oc, int ic, const void* x_codes, const void* x_scale, int M, void* Y, int y_dtype,
+                                 long long y_row, uint32_t poll_limit, int announced, int32_t* lost, void* stream) {
+  if (!lost || announced < 0) return RWKVQ_EINVAL;
+  return gemm_fp8(w_codes, w_scale, oc, ic, x_codes, x_scale, M, Y, y_dtype, y_row, poll_limit ? poll_limit : kPollLimit, announced, lost, stream);
 }
 
 }  // extern "C"

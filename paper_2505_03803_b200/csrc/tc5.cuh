@@ -37,9 +37,9 @@ __device__ __forceinline__ uint32_t mbar_test(uint32_t bar, uint32_t parity) {
   asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok;
 }
-// Bounded wait: false after kPollLimit polls (status word set) or once another role has given up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
-  for (uint32_t it = 0; it < kPollLimit; ++it) {
+// Bounded wait: false after `limit` polls (status word set) or once another role has given up.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, uint32_t limit = kPollLimit) {
+  for (uint32_t it = 0; it < limit; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
     if ((it & 63u) == 63u && *abort_flag) return false;
   }
@@ -47,8 +47,8 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   atomicExch(status, (int)RWKVQ_ETIMEOUT);
   return false;
 }
-__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status) {
-  return mbar_wait(smem_u32(bar), parity, abort_flag, status);
+__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, uint32_t limit = kPollLimit) {
+  return mbar_wait(smem_u32(bar), parity, abort_flag, status, limit);
 }
 // A tile of a row-major matrix through its tensor map: the box at column x (x * element size a multiple of 16) and row y, zeros outside.
 __device__ __forceinline__ void tensor_g2s(void* dst_smem, const CUtensorMap* map, int x, int y, uint64_t* bar) {

@@ -324,3 +324,29 @@ def test_product_of_many_tokens_every_scale_has_its_place():
     B.rwkvq_gemm_fp8(*[torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)], y)
     ref = 2.0 ** (xs[:, :13].astype(np.float64) - 127.0) @ (128.0 * 2.0 ** (ws[:, :13].astype(np.float64) - 127.0)).T
     assert np.array_equal(y.double().cpu().numpy(), np.repeat(ref, 128, 1)[:, :oc])
+
+
+# blocks that announce scales for so many pieces of 512 columns only: one token in slices whose copies are all asked for at once, a block that asks for more than it has room for, two tiles
+# of weights a block; the tensor core idle, or at work on what came before
+GIVEN_UP = [((1, 4096, 4096), 0), ((1, 4096, 4096), 1), ((16, 9472, 4096), 0), ((240, 256, 8192), 1), ((1500, 1604, 2064), 0), ((1500, 1604, 2064), 2)]
+
+
+@pytest.mark.parametrize("shape,announced", GIVEN_UP, ids=str)
+@pytest.mark.parametrize("polls", [200, 3000])
+def test_blocks_that_give_up_leave_in_order(shape, announced, polls):
+    """Whichever role's wait runs out, a block leaves only when what it has asked for has arrived; the status is reported once, the call after it is right."""
+    M, oc, ic = shape
+    wc, ws, xc, xs = product_inputs(14, M, oc, ic)
+    dev = [torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)]
+    want, y = torch.empty((M, oc), device="cuda"), torch.empty((M, oc), device="cuda")
+    B.rwkvq_gemm_fp8(*dev, want)
+    lost = torch.zeros(4, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    assert B.rwkvq_device_status() == 0
+    B.rwkvq_gemm_fp8_lost(*dev, y, polls, announced, lost)
+    torch.cuda.synchronize()
+    assert B.rwkvq_device_status() == 8 and B.rwkvq_device_status() == 0
+    gave_up, asked, arrived, done = lost.tolist()
+    assert gave_up > 0 and asked >= 2 * gave_up and arrived == gave_up and done == gave_up
+    B.rwkvq_gemm_fp8(*dev, y)
+    assert torch.equal(y, want) and B.rwkvq_device_status() == 0

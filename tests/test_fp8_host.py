@@ -75,3 +75,9 @@ def test_binding_refuses_what_is_not_on_the_device_or_ill_shaped():
         B.rwkvq_gemm_fp8(codes, scale, codes, scale, x)
     with pytest.raises(B.RwkvqError):
         B.rwkvq_fp8_quantize(x, codes.view(torch.float8_e5m2), scale, 1)
+
+
+def test_the_call_that_loses_scales_refuses():
+    buf, p = _aligned()
+    call = lambda announced, lost: B.lib().rwkvq_gemm_fp8_lost(p, p, 64, 128, p, p, 4, p, 0, 64, 0, announced, lost, None)
+    assert call(0, None) == EINVAL and call(-1, p) == EINVAL
