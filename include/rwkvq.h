@@ -435,6 +435,9 @@ rwkvq_status rwkvq_fp8_quantize(const void* x_dev, int dtype, int rows, int cols
                                 void* codes_dev, void* scale_dev, void* stream);
 rwkvq_status rwkvq_gemm_fp8(const void* w_codes_dev, const void* w_scale_dev, int oc, int ic, const void* x_codes_dev,
                             const void* x_scale_dev, int M, void* Y_dev, int y_dtype, long long y_row, void* stream);
+/* How rwkvq_gemm_fp8 cuts such a product on the current device (148 multiprocessors where there is none); host only.  plan[6]: rows of w and of x of a tile, slices of
+ * the columns, tiles, thread blocks (several tiles each where there are more tiles), stages of 128 columns that a block has under way.  Errors: EINVAL, ESHAPE, EUNSUPPORTED. */
+rwkvq_status rwkvq_gemm_fp8_plan(int M, int oc, int ic, int32_t* plan);
 /*
  * rwkvq_gemm_fp8 with another limit for its waits (polls; 0 = default) and thread blocks that announce scales only for the first `announced` pieces of 512 columns that they
  * work on: the wait for the next runs out.  lost_dev[4] (int32, added to): blocks that gave up, stages whose copies these had asked for, blocks that saw

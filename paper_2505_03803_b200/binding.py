@@ -88,7 +88,7 @@ EXPORTS = [
     "rwkvq_proxy_segments_workspace_bytes", "rwkvq_proxy_segments", "rwkvq_tau_for_fraction", "rwkvq_tau_largest_gap", "rwkvq_quant_error_workspace_bytes", "rwkvq_quant_error",
     "rwkvq_desc_for", "rwkvq_quantize_workspace_bytes", "rwkvq_quantize_dev", "rwkvq_calib_representative",
     "rwkvq_quantize_dev_async", "rwkvq_quantize_dev_lost", "rwkvq_quantize_check",
-    "rwkvq_fp8_scale_pitch", "rwkvq_fp8_quantize", "rwkvq_gemm_fp8", "rwkvq_gemm_fp8_lost", "rwkvq_linattn_workspace_bytes", "rwkvq_linattn",
+    "rwkvq_fp8_scale_pitch", "rwkvq_fp8_quantize", "rwkvq_gemm_fp8", "rwkvq_gemm_fp8_lost", "rwkvq_gemm_fp8_plan", "rwkvq_linattn_workspace_bytes", "rwkvq_linattn",
 ]
 
 _lib = None
@@ -178,6 +178,7 @@ def lib() -> C.CDLL:
         L.rwkvq_fp8_scale_pitch.restype = sz
         L.rwkvq_fp8_quantize.argtypes = [vp, i32, i32, i32, i64, i32, vp, vp, vp]
         L.rwkvq_gemm_fp8.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, i64, vp]
+        L.rwkvq_gemm_fp8_plan.argtypes = [i32, i32, i32, C.POINTER(i32)]
         L.rwkvq_gemm_fp8_lost.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, i64, C.c_uint32, i32, vp, vp]
     if hasattr(L, "rwkvq_linattn"):
         L.rwkvq_linattn_workspace_bytes.argtypes = [i32, i32, i32, i32]
@@ -757,6 +758,13 @@ def rwkvq_gemm_fp8(w_codes, w_scale, x_codes, x_scale, Y, stream=None):
                                             types.get(Y.dtype, -1), y_row if M > 1 else oc, _stream_ptr(stream))
     if status:
         _check(status, where)
+
+
+def rwkvq_gemm_fp8_plan(M: int, oc: int, ic: int) -> dict:
+    """How rwkvq_gemm_fp8 cuts a product of these sizes: w_rows and x_rows of a tile, slices, tiles, blocks, stages."""
+    plan = (C.c_int32 * 6)()
+    _check(lib().rwkvq_gemm_fp8_plan(M, oc, ic, plan), "rwkvq_gemm_fp8_plan")
+    return dict(zip(("w_rows", "x_rows", "slices", "tiles", "blocks", "stages"), plan))
 
 
 def rwkvq_gemm_fp8_lost(w_codes, w_scale, x_codes, x_scale, Y, poll_limit: int, announced: int, lost, stream=None):

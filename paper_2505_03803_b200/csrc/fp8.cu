@@ -694,6 +694,8 @@ Plan plan_of(int M, int oc, int groups) {
   while (l.tmem_cols < (uint32_t)l.NT * 2u + kSfSlots * kSfCols) l.tmem_cols *= 2;
   return l;
 }
+long long tiles_of(const Plan& l, int oc) { return (long long)((blocks_of(oc) + l.W - 1) / l.W) * l.MT; }
+int thread_blocks_of(const Plan& l, int tiles) { return l.slices > 1 ? tiles * l.slices : std::min(tiles, sm_count()); }
 int element_size(int dtype) { return dtype == RWKVQ_F32 ? 4 : dtype == RWKVQ_F16 || dtype == RWKVQ_BF16 ? 2 : 0; }
 
 }  // namespace f8
@@ -731,7 +733,7 @@ static rwkvq_status gemm_fp8(const void* w_codes, const void* w_scale, int oc, i
   a.Y = Y; a.y_row = y_row; a.wide = (y_row * f8::element_size(y_dtype)) % 16 == 0; a.oc = oc; a.M = M; a.y_dtype = y_dtype;
   a.groups = f8::blocks_of(ic); a.pitch = (int)f8::scale_pitch(ic);
   const f8::Plan l = f8::plan_of(M, oc, a.groups);
-  const long long tiles = (long long)((f8::blocks_of(oc) + l.W - 1) / l.W) * l.MT;
+  const long long tiles = f8::tiles_of(l, oc);
   if (tiles > (1ll << 28)) return RWKVQ_EUNSUPPORTED;
   a.NT = l.NT; a.MT = l.MT; a.slices = l.slices; a.stages = l.stages; a.tiles = (int)tiles; a.tmem_cols = l.tmem_cols;
   a.status = device_status_ptr();
@@ -744,7 +746,7 @@ static rwkvq_status gemm_fp8(const void* w_codes, const void* w_scale, int oc, i
   const cudaError_t e = opt_in[(lost ? 2 : 0) + l.W - 1]((const void*)kernel, (int)f8::kMaxSmemBytes);
   if (e != cudaSuccess) return cuda_status(e);
   cudaLaunchAttribute attr[2];
-  const unsigned blocks = l.slices > 1 ? (unsigned)(a.tiles * l.slices) : (unsigned)std::min<int>(a.tiles, sm_count());
+  const unsigned blocks = (unsigned)f8::thread_blocks_of(l, a.tiles);
   cudaLaunchConfig_t cfg = f8::launch_config(dim3(blocks), f8::threads_of(l.W), l.smem_bytes, static_cast<cudaStream_t>(stream), attr);
   if (l.slices > 1) {
     attr[1].id = cudaLaunchAttributeClusterDimension;
@@ -757,6 +759,16 @@ static rwkvq_status gemm_fp8(const void* w_codes, const void* w_scale, int oc, i
 rwkvq_status rwkvq_gemm_fp8(const void* w_codes, const void* w_scale, int oc, int ic, const void* x_codes, const void* x_scale, int M, void* Y, int y_dtype,
                             long long y_row, void* stream) {
   return gemm_fp8(w_codes, w_scale, oc, ic, x_codes, x_scale, M, Y, y_dtype, y_row, kPollLimit, 0, nullptr, stream);
+}
+
+rwkvq_status rwkvq_gemm_fp8_plan(int M, int oc, int ic, int32_t* plan) {
+  if (!plan || M <= 0 || oc <= 0 || ic <= 0) return RWKVQ_EINVAL;
+  if (ic % 16) return RWKVQ_ESHAPE;
+  const f8::Plan l = f8::plan_of(M, oc, f8::blocks_of(ic));
+  const long long tiles = f8::tiles_of(l, oc);
+  if (tiles > (1ll << 28)) return RWKVQ_EUNSUPPORTED;
+  plan[0] = l.W * f8::kRows; plan[1] = l.NT; plan[2] = l.slices; plan[3] = (int32_t)tiles; plan[4] = f8::thread_blocks_of(l, (int)tiles); plan[5] = l.stages;
+  return RWKVQ_OK;
 }
 
 rwkvq_status rwkvq_gemm_fp8_lost(const void* w_codes, const void* w_scale, int oc, int ic, const void* x_codes, const void* x_scale, int M, void* Y, int y_dtype,

@@ -350,3 +350,47 @@ def test_blocks_that_give_up_leave_in_order(shape, announced, polls):
     assert gave_up > 0 and asked >= 2 * gave_up and arrived == gave_up and done == gave_up
     B.rwkvq_gemm_fp8(*dev, y)
     assert torch.equal(y, want) and B.rwkvq_device_status() == 0
+
+
+# (shape, rows of weights of a tile, slices).  Blocks that go from tile to tile, with fewer columns than they can have under way and with more; the last tile ragged either way
+FORMS = [((2048, 4100, 272), 128, 1), ((240, 20000, 272), 128, 1), ((136, 7463, 80), 128, 1), ((1456, 5573, 672), 128, 1), ((3640, 2352, 704), 128, 1),
+         ((1, 65536, 128), 256, 1), ((253, 28546, 784), 256, 1), ((1229, 9474, 928), 256, 1), ((580, 15055, 1504), 256, 1)]
+# a tile for each cluster of blocks: two, four and eight slices of a tile of few tokens and of more than 32
+FORMS += [((1, 5120, 2048), 128, 2), ((7, 7100, 2064), 128, 2), ((488, 648, 1808), 128, 2), ((1008, 411, 1920), 128, 2), ((624, 33, 1664), 128, 4), ((460, 350, 2224), 128, 4),
+          ((200, 300, 4112), 128, 8), ((466, 34, 5424), 128, 8)]
+
+
+@pytest.mark.parametrize("shape,w_rows,slices", FORMS, ids=str)
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_product_in_every_form_against_64_bits(shape, w_rows, slices, dtype):
+    M, oc, ic = shape
+    plan = B.rwkvq_gemm_fp8_plan(M, oc, ic)
+    assert plan["w_rows"] == w_rows and plan["slices"] == slices, "another form than the test is for"
+    assert plan["blocks"] < plan["tiles"] if slices == 1 else plan["blocks"] == plan["tiles"] * slices
+    wc, ws, xc, xs = product_inputs(M + oc + ic, M, oc, ic, *((114, 121) if dtype == "f16" else (120, 134)))
+    dev = [torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)]
+    wide = torch.full((M + 1, oc), 7.0, dtype=TYPES[dtype], device="cuda")
+    B.rwkvq_gemm_fp8(*dev, wide[:M])
+    torch.cuda.synchronize()
+    assert B.rwkvq_device_status() == 0
+    rows = np.unique(np.concatenate([np.arange(0, M, 23), np.arange(max(0, M - 3), M)]))
+    check_product(wide[:M][torch.from_numpy(rows).cuda()], dtype, wc, ws, xc[rows], xs[rows])
+    assert (wide[M] == 7).all()
+    # the outputs in rows that are further apart, off 16 bytes: stored number by number, the same bits
+    apart = torch.full((M + 1, oc + 3), 7.0, dtype=TYPES[dtype], device="cuda")
+    B.rwkvq_gemm_fp8(*dev, apart[:M, :oc])
+    assert torch.equal(apart[:M, :oc], wide[:M]) and (apart[M] == 7).all() and (apart[:, oc:] == 7).all()
+
+
+@pytest.mark.parametrize("M,oc,ic,w_rows,slices", [(795, 7433, 1152, 128, 1), (1229, 9474, 1664, 256, 1), (1008, 411, 1920, 128, 2), (200, 300, 4224, 128, 8)])
+def test_product_in_every_form_every_scale_has_its_place(M, oc, ic, w_rows, slices):
+    plan = B.rwkvq_gemm_fp8_plan(M, oc, ic)
+    assert plan["w_rows"] == w_rows and plan["slices"] == slices and (slices > 1 or plan["blocks"] < plan["tiles"]), plan
+    gen = np.random.default_rng(7)
+    groups = ic // 128
+    wc, xc = np.full((oc, ic), 0x38, np.uint8), np.full((M, ic), 0x38, np.uint8)
+    ws, xs = random_scales(gen, -(-oc // 128), ic, 124, 131), random_scales(gen, M, ic, 124, 131)
+    y = torch.empty((M, oc), device="cuda")
+    B.rwkvq_gemm_fp8(*[torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)], y)
+    ref = 2.0 ** (xs[:, :groups].astype(np.float64) - 127.0) @ (128.0 * 2.0 ** (ws[:, :groups].astype(np.float64) - 127.0)).T
+    assert np.array_equal(y.double().cpu().numpy(), np.repeat(ref, 128, 1)[:, :oc])         # exact: sums of few bits

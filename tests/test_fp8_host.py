@@ -81,3 +81,20 @@ def test_the_call_that_loses_scales_refuses():
     buf, p = _aligned()
     call = lambda announced, lost: B.lib().rwkvq_gemm_fp8_lost(p, p, 64, 128, p, p, 4, p, 0, 64, 0, announced, lost, None)
     assert call(0, None) == EINVAL and call(-1, p) == EINVAL
+
+
+def test_plan():
+    plan = (C.c_int32 * 6)()
+    for args, status in [((0, 64, 128), EINVAL), ((1, 0, 128), EINVAL), ((1, 64, 0), EINVAL), ((1, 64, 120), ESHAPE), ((2**31 - 1, 2**31 - 1, 128), EUNSUPPORTED), ((1, 64, 128), 0)]:
+        assert B.lib().rwkvq_gemm_fp8_plan(*args, plan) == status
+    assert B.lib().rwkvq_gemm_fp8_plan(1, 64, 128, None) == EINVAL
+    for M in (1, 16, 100, 241, 2048, 70000):
+        for oc in (1, 128, 4100, 65536):
+            for ic in (16, 2048, 4112, 14336):
+                p = B.rwkvq_gemm_fp8_plan(M, oc, ic)
+                tall, wide = -(-oc // p["w_rows"]), -(-M // p["x_rows"])
+                assert p["w_rows"] in (128, 256) and p["x_rows"] % 16 == 0 and 16 <= p["x_rows"] <= 240 and p["tiles"] == tall * wide
+                assert p["slices"] in (1, 2, 4, 8) and p["slices"] * 4 <= -(-ic // 128) + 3 and 3 <= p["stages"] <= 12
+                assert p["blocks"] == (p["tiles"] * p["slices"] if p["slices"] > 1 else min(p["tiles"], p["blocks"])) and p["blocks"] <= 148
+    with pytest.raises(B.RwkvqError):
+        B.rwkvq_gemm_fp8_plan(1, 64, 8)
