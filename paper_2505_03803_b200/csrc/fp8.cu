@@ -608,7 +608,7 @@ __global__ void __launch_bounds__(threads_of(W), 1) fp8_gemm_kernel(const __grid
     uint32_t acc = W > 1 ? (uint32_t)(warp >> 2) - 1u : 0u, aph = 0;        // with two tiles of weights each has its warps
     for (int t = tile0; t < a.tiles; t += step) {
       const int mt = t % a.MT, rb = t / a.MT, t0 = mt * a.NT;
-      if (!mbar_wait(&ctrl->accfull[acc], aph, abortp, a.status, limit)) break;
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctrl->accfull[acc], aph, abortp, a.status, limit))) break;        // a warp reads tensor memory as a whole or not at all
       tc_fence_after();
       const uint32_t src = tmem + acc * (uint32_t)a.NT + ((uint32_t)(warp & 3) << 21);
       const int row0 = rb * (W * kRows) + (warp - 4) * 32, nt = min(a.NT, a.M - t0);

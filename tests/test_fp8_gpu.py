@@ -394,3 +394,13 @@ def test_product_in_every_form_every_scale_has_its_place(M, oc, ic, w_rows, slic
     B.rwkvq_gemm_fp8(*[torch.from_numpy(a).cuda() for a in (wc, ws, xc, xs)], y)
     ref = 2.0 ** (xs[:, :groups].astype(np.float64) - 127.0) @ (128.0 * 2.0 ** (ws[:, :groups].astype(np.float64) - 127.0)).T
     assert np.array_equal(y.double().cpu().numpy(), np.repeat(ref, 128, 1)[:, :oc])         # exact: sums of few bits
+
+
+# the same with several tiles a block, the first of them announced whole: the epilogue stores it, or waits for the second, while another role gives up
+@pytest.mark.parametrize("shape,announced", [((2048, 4100, 272), 1), ((1456, 5573, 672), 2), ((1456, 5573, 672), 3), ((1, 65536, 128), 1), ((580, 15055, 1504), 3), ((580, 15055, 1504), 4)],
+                         ids=str)
+@pytest.mark.parametrize("polls", [200, 1000, 5000])
+def test_blocks_that_give_up_behind_a_tile_leave_in_order(shape, announced, polls):
+    plan = B.rwkvq_gemm_fp8_plan(*shape)
+    assert plan["slices"] == 1 and plan["blocks"] < plan["tiles"]
+    test_blocks_that_give_up_leave_in_order(shape, announced, polls)
