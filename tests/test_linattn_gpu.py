@@ -394,3 +394,47 @@ def test_a_sequence_that_begins_in_front_of_an_earlier_one_is_left_out(starts, g
         near(st[s], S[s], tolS[s], f"state of sequence {i}")
         rest[a:b], kept[s] = False, False
     assert (out[rest.cuda()] == 7).all() and torch.equal(st.cpu()[kept], c["state"][kept])
+
+
+def apart(x, gap, fill=float("nan")):
+    """x on the device, its rows `gap` elements further apart than they are long (NaN between them)."""
+    T, row = x.shape[0], x[0].numel()
+    wide = torch.full((T, row + gap), fill, dtype=x.dtype, device="cuda")
+    view = wide[:, :row].view(x.shape)
+    view.copy_(x)
+    return view, wide[:, row:]
+
+
+@pytest.mark.parametrize("lens", [[1], [7], [16], [90], [1] * 6, [40, 0, 1, 70, 5]], ids=lambda l: "-".join(map(str, l)))
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("decay", ["channel", "head"])
+@pytest.mark.parametrize("n", [64, 128])
+def test_every_row_stride_is_its_own(lens, dtype, decay, n):
+    # r, k, v, logw and out each with another distance from row to row: none can be taken for another's
+    heads = 4
+    c = make(sum(lens) + 81, lens, heads, n, dtype, decay=decay, decay_f32=len(lens) % 2 == 1)
+    r, k, v = (apart(c["rkv"][:, i], gap)[0] for i, gap in enumerate((8, 24, 40)))
+    lw = apart(c["lw"], 56)[0]
+    out, between = apart(torch.full((c["T"], heads, n), 7.0, dtype=TYPES[dtype]), 72, 5.0)
+    state = c["state"].cuda()
+    ws = torch.empty(max(16, B.rwkvq_linattn_workspace_bytes(c["T"], len(lens), heads, n)), dtype=torch.uint8, device="cuda")
+    starts = torch.tensor(c["starts"], dtype=torch.int32, device="cuda") if len(lens) > 1 else None
+    B.rwkvq_linattn(r, k, v, lw, c["u"].cuda(), out, state, seq_start=starts, workspace=ws)
+    torch.cuda.synchronize()
+    assert B.rwkvq_device_status() == 0
+    ref, tol, S, tolS = expected(c)
+    near(out, ref, tol, "out")
+    near(state, S, tolS, "state")
+    assert (between == 5).all()
+
+
+def test_every_row_stride_is_its_own_where_rows_are_cut():
+    c = make(82, [1300], 64, 64, "bf16")
+    r, k, v = (apart(c["rkv"][:, i], gap)[0] for i, gap in enumerate((8, 24, 40)))
+    lw, (out, between), state = apart(c["lw"], 56)[0], apart(torch.full((1300, 64, 64), 7.0, dtype=torch.bfloat16), 72, 5.0), c["state"].cuda()
+    ws = torch.empty(B.rwkvq_linattn_workspace_bytes(1300, 1, 64, 64), dtype=torch.uint8, device="cuda")
+    B.rwkvq_linattn(r, k, v, lw, c["u"].cuda(), out, state, workspace=ws)
+    ref, tol, S, tolS = expected(c, device="cuda")
+    near(out, ref, tol, "out")
+    near(state, S, tolS, "state")
+    assert (between == 5).all()
