@@ -404,3 +404,34 @@ def test_blocks_that_give_up_behind_a_tile_leave_in_order(shape, announced, poll
     plan = B.rwkvq_gemm_fp8_plan(*shape)
     assert plan["slices"] == 1 and plan["blocks"] < plan["tiles"]
     test_blocks_that_give_up_leave_in_order(shape, announced, polls)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("shape", [(1, 144), (130, 1040), (257, 272)], ids=str)
+def test_quantize_strided_rows_of_every_type(dtype, block, shape):
+    rows, cols = shape
+    wide = torch.full((rows, cols + 48), float("inf"), device="cuda")
+    wide[:, 16:16 + cols] = torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(rows), device="cuda")
+    check_quantize(wide.to(TYPES[dtype])[:, 16:16 + cols], block)
+
+
+def test_scales_as_exponents():
+    # scales held as torch's type of eight exponent bits: the same bytes in and out
+    e8 = torch.float8_e8m0fnu
+    x, w = torch.randn((9, 528), device="cuda"), torch.randn((140, 528), device="cuda") * 0.02
+    got = {}
+    for kind in (torch.uint8, e8):
+        xc, wc = (torch.empty(t.shape, dtype=torch.float8_e4m3fn, device="cuda") for t in (x, w))
+        xs, ws = (torch.zeros((rows, B.rwkvq_fp8_scale_pitch(528)), dtype=torch.uint8, device="cuda").view(kind) for rows in (9, 2))
+        y = torch.empty((9, 140), device="cuda")
+        B.rwkvq_fp8_quantize(x, xc, xs, 1)
+        B.rwkvq_fp8_quantize(w, wc, ws, 128)
+        B.rwkvq_gemm_fp8(wc, ws, xc, xs, y)
+        got[kind] = [t.view(torch.uint8).cpu().numpy() for t in (wc, ws, xc, xs)], y
+    for a, b in zip(got[torch.uint8][0], got[e8][0]):
+        assert np.array_equal(a, b)
+    check_product(got[e8][1], "f32", *got[e8][0])
+    assert torch.equal(got[e8][1], got[torch.uint8][1])
+    # and what they stand for, as torch reads them
+    assert np.array_equal(torch.from_numpy(got[e8][0][3][:, :5].copy()).view(e8).float().numpy(), 2.0 ** (got[e8][0][3][:, :5].astype(np.float32) - 127))
