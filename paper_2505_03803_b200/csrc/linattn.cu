@@ -894,7 +894,7 @@ __global__ void __launch_bounds__(Shape<T, N, kStateOnly>::kAll, N == 64 ? (kSta
 
 // Rows of a block and how many blocks.  A block's warps work on one head; about four thread blocks fit an SM.
 struct Plan { long long block_rows, pitch; int blocks, limit; size_t entries_bytes, bytes; };
-constexpr int kShortest = 8, kLeastChunks = 3;
+constexpr int kShortest = 8, kLeastChunks = 3, kFewMore = 16;
 Plan plan_of(int tokens, int n_seq, int heads, int n) {
   Plan l = {0, 0, 0, 0x7FFFFFFF, 0, 0};
   const int sms = sm_count(), per_sm = n == 64 ? kPerSm : 1;
@@ -903,7 +903,10 @@ Plan plan_of(int tokens, int n_seq, int heads, int n) {
   // as much as fewer tokens or sequences could ask for
   l.entries_bytes = round_up_sz((size_t)n_seq * sizeof(Entry), 256);
   l.bytes = l.entries_bytes + (size_t)std::min(most, all / (2 * kChunk) + 1) * (2 * n * n + n) * 4;
-  if (tokens <= 2ll * n_seq) return l;        // all by the token kernel
+  // The lengths are on the device.  With fewer than kFewMore more rows than sequences all are taken for short ones: a batch of single tokens does not pay for launches that find
+  // nothing (96 sequences of two tokens, 64 heads, 37.8 us without them, 41.0 with), and a sequence of 16 among single tokens is as fast by the recurrence.  Longer ones are not (one
+  // among 95 single tokens: of 32 rows 52 us by the recurrence, 40.5 in chunks, of 96 rows 106 and 47; 299 rows among 300 tokens 370 and 129).  An empty sequence hides a row.
+  if (tokens < (long long)n_seq + kFewMore) return l;
   // An SM has kPerSm blocks at work, a chunk of 16 rows every so often (0.95 us with two or three, 1.05 alone); a sequence's last block adds up the states of
   // those before it.  Blocks of one head each, or, where that leaves SMs idle, the heads' rows cut evenly: some blocks then begin anew at a second head (2048 rows of
   // 64 heads: six blocks each 77.8 us, even 74.4; 203 of 32 heads: four each 11.1, even 16.5).

@@ -438,3 +438,18 @@ def test_every_row_stride_is_its_own_where_rows_are_cut():
     near(out, ref, tol, "out")
     near(state, S, tolS, "state")
     assert (between == 5).all()
+
+
+@pytest.mark.parametrize("lens", [[1] * 40 + [30], [200] + [1] * 199, [1] * 150 + [0] * 60 + [170, 1, 0], [2] * 30, [0] * 100 + [90] + [1] * 5, [3, 1, 9, 1, 1, 1, 25] + [1] * 45], ids=lambda l: f"{len(l)}-{max(l)}")
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_long_sequence_among_short_ones(lens, dtype):
+    check(make(91 + len(lens), lens, 2, 64, dtype, extra_slots=3))
+
+
+def test_a_long_sequence_among_short_ones_where_rows_are_cut():
+    c = make(92, [1] * 700 + [800] + [1] * 150, 24, 64, "bf16")
+    out, st, _ = call(c)
+    assert B.rwkvq_device_status() == 0
+    ref, tol, S, tolS = expected(c, device="cuda")
+    near(out, ref, tol, "out")
+    near(st, S, tolS, "state")

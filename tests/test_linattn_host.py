@@ -61,3 +61,10 @@ def test_workspace():
     assert need > 0
     assert status(tokens=5000, ws_bytes=need - 1) == ENOMEM and status(tokens=5000, ws_at=0, ws_bytes=need) == ENOMEM
     assert status(tokens=5000, ws_at=P + (1 << 21) + 4, ws_bytes=need) == EALIGN
+
+
+def test_a_long_sequence_among_short_ones_is_not_gone_through_token_by_token():
+    # whatever the average length: a list that leaves room for a long sequence takes the chunks' passes, which need the workspace
+    assert status(tokens=600, n_seq=400, n_slots=400, ws_at=0, ws_bytes=0) == ENOMEM
+    assert status(tokens=2000, n_seq=1000, n_slots=1000, ws_at=0, ws_bytes=0) == ENOMEM
+    assert status(tokens=400, n_seq=400, n_slots=400, ws_at=0, ws_bytes=0) != ENOMEM       # single tokens do not
