@@ -452,7 +452,9 @@ rwkvq_status rwkvq_gemm_fp8_lost(const void* w_codes_dev, const void* w_scale_de
  * S [n keys][n values], token after token
  *     out_t[j] = sum_i r_t[i] * (S[i][j] + u[i] * k_t[i] * v_t[j]);    S[i][j] = exp(logw_t[i]) * S[i][j] + k_t[i] * v_t[j].
  * (The step's RWKVQ_IN_WKV is the per-channel recurrence of Eq. 23.)  Prompts, ragged batches and single tokens through one call; sums, decays and
- * states in fp32.
+ * states in fp32.  Longer sequences run on the tensor cores, whose operands are fp32 numbers as two bf16 terms (three for F32, and for what goes into a state): an
+ * output is then off by up to 2^-14 (F32: 10 * 2^-24) of the sum of the magnitudes that make it up, next to its own rounding.  An infinity or NaN in r is seen by its
+ * token's outputs alone; in k, v, logw or a state by that head's outputs from its token on (v: that column's), where an infinity may come out as NaN.
  *  r, k, v, out: [tokens][heads][n] of `dtype` (F32, F16, BF16), n 64 or 128; *_row elements from row to row, so that they may lie side by side.
  *  logw: logarithms of the decays, <= 0, -inf = forget, of decay_dtype (F32 or `dtype`): [tokens][heads][n], or [tokens][heads] with decay_per_head;
  *      logw_row = 0: the same for all tokens.  u: [heads][n] fp32, NULL = ones.

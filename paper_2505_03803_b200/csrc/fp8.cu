@@ -99,8 +99,8 @@ __device__ __forceinline__ uint2 encode8(const Eight<T>& e, float inv) {
   return make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
 }
 
-// Rows: a warp takes 256 columns per 16-byte load (16 lanes a group), four loads under way, and writes the eight scales together.  HBM: 8192 x 7168 bf16 in 34.7 us
-// (5.1 TB/s), 2048 x 4096 in 6.8, of which HBM needs 3.9.
+// Rows: a warp takes 256 columns per 16-byte load (16 lanes a group), four loads under way, and writes the eight scales together.  HBM: 8192 x 7168 bf16 in 33.4 us
+// (5.3 TB/s), 2048 x 4096 in 6.7, of which HBM needs 3.9.
 constexpr int kRowWarps = 8, kRowChunks = 4, kRowCols = kRowChunks * 256;
 template <typename T>
 __global__ void __launch_bounds__(kRowWarps * 32) fp8_rows_kernel(const T* x, long long x_row, int rows, int cols, int pieces, uint8_t* codes,
@@ -143,8 +143,8 @@ __global__ void __launch_bounds__(kRowWarps * 32) fp8_rows_kernel(const T* x, lo
   if (lane == 0) *reinterpret_cast<uint2*>(scale + row * pitch + (c0 >> 7)) = make_uint2(lo, hi);
 }
 
-// Blocks of 128 x 128: one thread block each, its elements in registers between the maximum and the codes.  HBM: 14336 x 4096 in 34.4 us from fp16 (5.1 TB/s), 45.5 from
-// fp32 (6.45 TB/s); 47 with the codes' checks for infinities on every element and 256 threads.
+// Blocks of 128 x 128: one thread block each, its elements in registers between the maximum and the codes.  HBM: 14336 x 4096 in 33.0 us from fp16 (5.3 TB/s), 44.6 from
+// fp32 (6.6 TB/s); 47 with the codes' checks for infinities on every element and 256 threads.
 constexpr int kBlockThreads = 512;
 template <typename T>
 __global__ void __launch_bounds__(kBlockThreads, 2) fp8_blocks_kernel(const T* x, long long x_row, int rows, int cols, int groups, uint8_t* codes,
@@ -235,8 +235,8 @@ cudaError_t quantize(const void* x, long long x_row, int rows, int cols, int blo
 // Scales: four groups' bytes of a row are the word that the instruction picks its byte from; warp 2 deals the words of 512 columns out in the order
 // of the copy to tensor memory (32 lanes x 16 bytes, row r in line r % 32, word r / 32), where they lie once per 32-lane quarter.
 //
-// What bounds it.  One token: launch, the latency of the first loads and of the slices' meeting (4096 x 4096 6.6 us with weights from HBM, which needs 2.6).  Few tokens,
-// large matrices: HBM (65536 x 4096, 16 tokens, 45.6 us = 5.9 TB/s).  Many: power.  2048 x 4096 x 14336 over and over takes 110 us (2.2 PFLOP/s) at 990 W, the limit,
+// What bounds it.  One token: launch, the latency of the first loads and of the slices' meeting (4096 x 4096 6.5 us with weights from HBM, which needs 2.6).  Few tokens,
+// large matrices: HBM (65536 x 4096, 16 tokens, 43.2 us = 6.3 TB/s).  Many: power.  2048 x 4096 x 14336 over and over takes 105 to 110 us (2.2 PFLOP/s) at 990 W, the limit,
 // which leaves 1.47 of 1.97 GHz; 106 without scales, 125 with one tile of weights a block.  A stage of two brings 63 KB for 256 x 240 outputs, of one 47 KB for 128 x 240,
 // and shared memory, which these pass twice (in, and to the tensor core), is then busier than the tensor core.
 // Taken back: pairs of blocks (cta_group::2) that share a tile's tokens, which take in as little (2048 x 14336 x 4096 111 us with barriers of the other block's, 263 with

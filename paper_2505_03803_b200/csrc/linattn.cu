@@ -2,7 +2,7 @@
 //   out_t = r_t (S + (u (.) k_t) v_t^T),   S <- diag(exp(lw_t)) S + k_t v_t^T.
 //
 // Single tokens and short sequences: linattn_token_kernel, the recurrence as it stands, S in registers.  One token reads and writes 2 * 4 * N * N bytes of
-// state for 4 N^2 operations: HBM, and with few sequences latency, is all that counts (96 sequences, 64 heads: 31 us, 6.5 TB/s; one, 32 heads: 2.0).
+// state for 4 N^2 operations: HBM, and with few sequences latency, is all that counts (96 sequences, 64 heads: 33.4 us, 6.2 TB/s; one, 32 heads: 2.4).
 // Prompts: chunks of sixteen tokens on the tensor cores, linattn_chunk_kernel, in two passes where a sequence is dealt out over several SMs.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -30,7 +30,6 @@ struct Args {
   // The chunk kernels' blocks: so many rows each of all heads' rows one head after the other, a head's rows `pitch` apart (more than there are, where no
   // block is to have rows of two heads).
   long long block_rows, pitch;
-  int blocks;
   Entry* entries;           // [n_seq], written by the token kernel; nullptr: one sequence, all rows, slot 0
   float* block_states;      // [blocks]: the state a block's last piece adds up, the one its sequence began with, the piece's decays
 };
@@ -150,11 +149,13 @@ __global__ void __launch_bounds__(kTokenThreads) linattn_token_kernel(const __gr
 // Rows are cut into blocks of block_rows, dealt out over the SMs: first (kStateOnly) the state that each block's last piece adds up from zero (or from its
 // sequence's own), where the sequence goes on behind the block; then all blocks at once, each beginning with what those before it left.
 //
-// What bounds it, 2048 tokens, 64 heads, bf16, decays fp32: 23 us the states' pass, 52 the other (ncu, cold; 69 in all, warm and one under the other), of which HBM needs 15.5.
+// What bounds it, 2048 tokens, 64 heads, bf16, decays fp32: 25 us the states' pass, 57 the other (ncu, cold and alone; 71 in all, call after call and one under the other), of which HBM needs 15.5.
 // Of the cycles that an SM is active, shared memory's data path is busy 53 % (operands are written once and read by all multiplying warps), issue slots 49 %, the tensor pipe 28 %, with
 // twelve warps in 168 registers: neither a full pipe nor enough warps to wait beside one another.  A chunk is about 3 100 warp instructions.  Taken back: parts of a block halved over a cluster in the states' pass (no gain, 203 tokens 11.3 -> 13.2), five
 // stages of inputs (no gain), three or four blocks an SM (spills), the triangles through shared memory (82 us where registers took 77).
-// 203 tokens, 32 heads 11.2; 5000 rows of eleven sequences, one decay a head, fp16 175; fp32, N 128, 1111 tokens of 16 heads 56, six products where bf16 takes three.
+// 203 tokens, 32 heads 12.3; 5000 rows of eleven sequences, one decay a head, fp16 179; fp32, N 128, 1111 tokens of 16 heads 57 (no pipe full there either: tensor
+// pipe 36 %, issue slots 34 %, data path 45 %, one block of sixteen warps an SM; in 128 registers a thread the outputs' pass spills 48 bytes, with a decay per head 24, and 68 with
+// fp16, N 128 and a decay per head).
 
 template <typename T> struct Terms;
 template <> struct Terms<__nv_bfloat16> { static constexpr int R = 2, V = 1; };
@@ -892,7 +893,7 @@ __global__ void __launch_bounds__(Shape<T, N, kStateOnly>::kAll, N == 64 ? (kSta
   if (!kStateOnly) asm volatile("griddepcontrol.wait;" ::: "memory");      // a block without rows does not end before the pass in front of it, either
 }
 
-// Rows of a block and how many blocks.  A block's warps work on one head; about four thread blocks fit an SM.
+// Rows of a block and how many blocks.  A block's warps work on one head at a time; an SM holds kPerSm thread blocks of the outputs' pass with heads of 64, one with heads of 128.
 struct Plan { long long block_rows, pitch; int blocks, limit; size_t entries_bytes, bytes; };
 constexpr int kShortest = 8, kLeastChunks = 3, kFewMore = 16;
 Plan plan_of(int tokens, int n_seq, int heads, int n) {
@@ -907,7 +908,8 @@ Plan plan_of(int tokens, int n_seq, int heads, int n) {
   // nothing (96 sequences of two tokens, 64 heads, 37.8 us without them, 41.0 with), and a sequence of 16 among single tokens is as fast by the recurrence.  Longer ones are not (one
   // among 95 single tokens: of 32 rows 52 us by the recurrence, 40.5 in chunks, of 96 rows 106 and 47; 299 rows among 300 tokens 370 and 129).  An empty sequence hides a row.
   if (tokens < (long long)n_seq + kFewMore) return l;
-  // An SM has kPerSm blocks at work, a chunk of 16 rows every so often (0.95 us with two or three, 1.05 alone); a sequence's last block adds up the states of
+  // An SM has kPerSm blocks at work, a chunk of 16 rows every so often (0.95 us with two or three, 1.05 alone: measured with bf16 and heads of 64, and taken for all; 1111 rows
+  // of 16 heads of 128 in fp32 it takes for 18 us where they are 57); a sequence's last block adds up the states of
   // those before it.  Blocks of one head each, or, where that leaves SMs idle, the heads' rows cut evenly: some blocks then begin anew at a second head (2048 rows of
   // 64 heads: six blocks each 77.8 us, even 74.4; 203 of 32 heads: four each 11.1, even 16.5).
   auto chunk_time = [&](long long blocks) { return std::max(0.95 * (double)((blocks + sms - 1) / sms), 1.05); };
@@ -1008,7 +1010,7 @@ rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace, size
   const la::Plan l = la::plan_of(a.tokens, a.n_seq, a.heads, a.n);
   if (l.blocks > 0 && (!workspace || workspace_bytes < l.bytes)) return RWKVQ_ENOMEM;
   if (!aligned16(workspace)) return RWKVQ_EALIGN;
-  p.limit = l.limit; p.block_rows = l.block_rows; p.pitch = l.pitch; p.blocks = l.blocks;
+  p.limit = l.limit; p.block_rows = l.block_rows; p.pitch = l.pitch;
   p.entries = l.blocks > 0 && (a.seq_start || a.slots) ? static_cast<la::Entry*>(workspace) : nullptr;
   p.block_states = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + l.entries_bytes);
   p.status = device_status_ptr();
