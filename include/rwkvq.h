@@ -459,8 +459,8 @@ rwkvq_status rwkvq_gemm_fp8_lost(const void* w_codes_dev, const void* w_scale_de
  *  logw: logarithms of the decays, <= 0, -inf = forget, of decay_dtype (F32 or `dtype`): [tokens][heads][n], or [tokens][heads] with decay_per_head;
  *      logw_row = 0: the same for all tokens.  u: [heads][n] fp32, NULL = ones.
  *  seq_start: [n_seq + 1] rows where the sequences begin, rising, device memory (NULL: n_seq is 1 and has all rows).  A sequence may be empty; rows in front
- *      of the first and behind the last are not touched.  A call of fewer than n_seq + 16 tokens goes through each sequence token by token (about 0.8 us each), as
- *      suits single tokens: a list of empty sequences around a long one is better given without these.
+ *      of the first and behind the last are not touched.  A call of at most two tokens a sequence on average, and fewer than n_seq + 16, goes through each sequence token by token
+ *      (about 0.6 us each), as suits single tokens: a list of empty sequences around a long one is better given without these.
  *  state, state_out: [n_slots][heads][n][n] fp32 (keys, values), the same buffer (updated in place) or two that do not overlap.  slots: [n_seq]
  *      which of them belongs to each sequence (NULL: sequence i has state i), device memory; -1: begins with zeros, is not kept.  state NULL: all begin with
  *      zeros; state_out NULL: none is kept.  States of no sequence are not touched.

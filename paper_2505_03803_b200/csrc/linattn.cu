@@ -904,10 +904,10 @@ Plan plan_of(int tokens, int n_seq, int heads, int n) {
   // as much as fewer tokens or sequences could ask for
   l.entries_bytes = round_up_sz((size_t)n_seq * sizeof(Entry), 256);
   l.bytes = l.entries_bytes + (size_t)std::min(most, all / (2 * kChunk) + 1) * (2 * n * n + n) * 4;
-  // The lengths are on the device.  With fewer than kFewMore more rows than sequences all are taken for short ones: a batch of single tokens does not pay for launches that find
+  // The lengths are on the device.  With at most two rows a sequence on average, and fewer than kFewMore more than sequences, all are taken for short ones: a batch of single tokens does not pay for launches that find
   // nothing (96 sequences of two tokens, 64 heads, 37.8 us without them, 41.0 with), and a sequence of 16 among single tokens is as fast by the recurrence.  Longer ones are not (one
   // among 95 single tokens: of 32 rows 52 us by the recurrence, 40.5 in chunks, of 96 rows 106 and 47; 299 rows among 300 tokens 370 and 129).  An empty sequence hides a row.
-  if (tokens < (long long)n_seq + kFewMore) return l;
+  if (tokens <= 2ll * n_seq && tokens < (long long)n_seq + kFewMore) return l;
   // An SM has kPerSm blocks at work, a chunk of 16 rows every so often (0.95 us with two or three, 1.05 alone: measured with bf16 and heads of 64, and taken for all; 1111 rows
   // of 16 heads of 128 in fp32 it takes for 18 us where they are 57); a sequence's last block adds up the states of
   // those before it.  Blocks of one head each, or, where that leaves SMs idle, the heads' rows cut evenly: some blocks then begin anew at a second head (2048 rows of

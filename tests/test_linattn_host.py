@@ -68,3 +68,10 @@ def test_a_long_sequence_among_short_ones_is_not_gone_through_token_by_token():
     assert status(tokens=600, n_seq=400, n_slots=400, ws_at=0, ws_bytes=0) == ENOMEM
     assert status(tokens=2000, n_seq=1000, n_slots=1000, ws_at=0, ws_bytes=0) == ENOMEM
     assert status(tokens=400, n_seq=400, n_slots=400, ws_at=0, ws_bytes=0) != ENOMEM       # single tokens do not
+
+
+def test_few_sequences_take_the_chunks_from_nine_tokens_on():
+    for n_seq, tokens in ((1, 9), (1, 16), (2, 9), (3, 12), (4, 19), (8, 17), (16, 33)):
+        assert status(tokens=tokens, n_seq=n_seq, n_slots=n_seq, ws_at=0, ws_bytes=0) == ENOMEM, (n_seq, tokens)
+    for n_seq, tokens in ((1, 8), (5, 10), (8, 16), (16, 31), (96, 111)):
+        assert status(tokens=tokens, n_seq=n_seq, n_slots=n_seq, ws_at=0, ws_bytes=0) != ENOMEM, (n_seq, tokens)
