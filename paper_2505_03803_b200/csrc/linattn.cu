@@ -2,7 +2,7 @@
 //   out_t = r_t (S + (u (.) k_t) v_t^T),   S <- diag(exp(lw_t)) S + k_t v_t^T.
 //
 // Single tokens and short sequences: linattn_token_kernel, the recurrence as it stands, S in registers.  One token reads and writes 2 * 4 * N * N bytes of
-// state for 4 N^2 operations: HBM, and with few sequences latency, is all that counts (96 sequences, 64 heads: 33.4 us, 6.2 TB/s; one, 32 heads: 2.4).
+// state for 4 N^2 operations: HBM, and with few sequences latency, is all that counts (96 sequences, 64 heads: 33.0 us, 6.2 TB/s; one, 32 heads: 2.4).
 // Prompts: chunks of sixteen tokens on the tensor cores, linattn_chunk_kernel, in two passes where a sequence is dealt out over several SMs.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -53,7 +53,7 @@ __device__ __forceinline__ float log_decay(const rwkvq_linattn_args& a, long lon
 __device__ __forceinline__ bool rows_of(const Args& p, int i, int& start, int& end) {
   start = 0; end = p.a.tokens;
   if (p.a.seq_start) { start = p.a.seq_start[i]; end = p.a.seq_start[i + 1]; }
-  return start >= 0 && start <= end && end <= p.a.tokens;
+  return (start >= 0) & (start <= end) & (end <= p.a.tokens);
 }
 
 constexpr int kTokenThreads = 128, kCols = 64;      // value columns of a block
@@ -69,10 +69,11 @@ __global__ void __launch_bounds__(kTokenThreads) linattn_token_kernel(const __gr
   const int tid = threadIdx.x, h = blockIdx.x, seq = blockIdx.y, v0 = blockIdx.z * kCols;
   const int kg = tid >> 4, col = (tid & 15) * 4;
   int start, end, slot = seq;
+  // (without branches on what is loaded: all loads of the lists are under way at once)
   bool bad = !rows_of(p, seq, start, end);
   if (a.slots) {
     slot = a.slots[seq];
-    bad = bad || slot < -1 || slot >= a.n_slots;
+    bad = bad | (slot < -1) | (slot >= a.n_slots);
   }
   // Sequences of a call share neither a state nor rows: one that begins in front of an entry of the list before its own could have rows of a sequence that is computed, and
   // the chunk kernels' blocks keep one state each for a sequence that goes on behind them.
