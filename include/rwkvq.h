@@ -489,6 +489,88 @@ size_t rwkvq_linattn_workspace_bytes(int tokens, int n_seq, int heads, int n);
 rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /*
+ * Low-rank adapters of many sequences beside a shared projection: y[t] += scale[a] * B_a (A_a x_mix[t]), a = adapter[sequence of t].  Packed weights
+ * cannot take an adapter in; it stays beside them, and each sequence of a batch may have another.  Called behind any of the products above, on their outputs.
+ *  x: [tokens][ic] of x_dtype (F32, F16, BF16), x_row elements from row to row.  y: [tokens][oc] of y_dtype (F32, F16, BF16), y_row elements from row to row, updated in place.
+ *  A: [n_adapters][rank][ic], B: [n_adapters][oc][rank] of w_dtype (F16, BF16).  ranks: [n_adapters] ranks of their own, 0 to rank (NULL: rank); what lies behind them in
+ *      A and B is not read into anything.  scale: [n_adapters] fp32 (NULL: 1).
+ *  adapter: [n_seq], -1: none (the rows stay as they are).  seq_start: [n_seq + 1] rows where the sequences begin, rising; NULL: n_seq is 1 and has all rows, or n_seq is
+ *      `tokens` and each row is a sequence.  A sequence may be empty; rows in front of the first and behind the last are not touched.  All lists lie on the device, so that a
+ *      captured call serves other batches.
+ *  mu_desc, mu_image (both or neither): the token shift of the products, x_mix = x + (x_prev - x) (.) mu_hat, rounded to x_dtype as theirs is.  x_prev[tokens][ic] (x_prev_row
+ *      elements from row to row, as in rwkvq_gemv), or NULL: the row before in the sequence, and in front of its first xprev0[n_seq][ic] (NULL: zeros; as in rwkvq_gemm_prefill).
+ * Products are exact and summed in fp32; A x goes on in two parts of eight bits where y has 16 bits (off by up to 2^-16 of it), three (all of it) where y has 32.  Sums are
+ * added up in a fixed order.  An infinity or NaN in x is seen by its own row alone, where an infinity may come out as NaN.
+ * A sequence whose rows do not exist or that begins in front of any entry of seq_start before its own, whose adapter does not exist, or whose adapter's rank is not in range: it is left out, the others are computed, and
+ * rwkvq_device_status reports EINVAL.
+ * Pointers (lists, ranks, scale: 4 bytes) and rows 16-byte aligned; y overlaps no input.  Asynchronous on `stream`, no workspace.
+ * Errors: EINVAL, ESHAPE (ic, oc or rank not a multiple of 8), EALIGN, EUNSUPPORTED (rank above 128, more than 65535 sequences, 2^24 tokens, columns or rows of B), ECUDA.
+ */
+typedef struct {
+  const void* x;
+  const void* A;
+  const void* B;
+  void* y;
+  const int32_t* adapter;
+  const int32_t* seq_start;
+  const int32_t* ranks;
+  const float* scale;
+  const void* x_prev;
+  const void* xprev0;
+  int64_t x_row, y_row, x_prev_row;
+  int32_t tokens, n_seq, ic, oc, rank, n_adapters, x_dtype, w_dtype, y_dtype;
+} rwkvq_lowrank_args;
+rwkvq_status rwkvq_lowrank(const rwkvq_lowrank_args* args, const rwkvq_desc* mu_desc, const void* mu_image_dev, void* stream);
+
+/*
+ * Beam search's selection: of all tokens v of all beams k of a request the `picks` with the largest total[k][v] = scores[k] + logits[k][v] - log sum_v e^logits[k][v],
+ * falling; equal ones by the lowest beam, then the lowest token.
+ *  logits: [requests * beams][vocab] of dtype (F32, F16, BF16), logits_row elements from row to row.  A logit of -inf or NaN has probability zero and does not count; those
+ *      of +inf, if there are any, share their beam's probability.  scores: [requests][beams] fp32; a beam whose score is infinite or NaN is dead: its
+ *      totals are -inf, and its logits are not read.  Where fewer than `picks` totals are above -inf, the lowest (k, v) of the others follow with -inf.
+ *  finished: [requests][beams] bytes, or NULL: a beam that has ended (not 0) has one candidate, token eos with its score unchanged, and its logits are not read.
+ *  next_scores, parents, tokens: [requests][picks]: the totals (fp32), their beams and tokens.  finished_out: [requests][picks] bytes, or NULL: whether the parent had ended or the token is eos.
+ *      next_scores, finished_out and scores, finished are different buffers.
+ * Maxima and sums of a thread are fp32, of a row and the totals fp64: they are compared before they are rounded (and where they are equal, within a beam the logits).
+ * workspace_dev: rwkvq_beam_select_workspace_bytes() bytes (enough for fewer requests, beams, tokens and picks, too), 16-byte aligned, contents irrelevant, not shared by calls in flight at the same time.
+ * logits aligned to their type, scores and outputs to 4 bytes.  Asynchronous on `stream`.  rwkvq_state_reorder moves the states as `parents` says.
+ * Errors: EINVAL (picks above beams * vocab, eos outside the vocabulary with `finished` or `finished_out`, ...), EALIGN, EUNSUPPORTED (more than 64 beams or picks, 2^24 tokens,
+ * 65535 beams in all), ENOMEM (workspace too small), ECUDA.
+ */
+typedef struct {
+  const void* logits;
+  const float* scores;
+  const uint8_t* finished;
+  float* next_scores;
+  int32_t* parents;
+  int32_t* tokens;
+  uint8_t* finished_out;
+  int64_t logits_row;
+  int32_t requests, beams, vocab, picks, eos, dtype;
+} rwkvq_beam_select_args;
+size_t rwkvq_beam_select_workspace_bytes(int requests, int beams, int vocab, int picks);
+rwkvq_status rwkvq_beam_select(const rwkvq_beam_select_args* args, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
+ * The states of recurrent layers follow their beams: in every part state[slots[r][b]] becomes what state[slots[r][parents[r][b]]] was before the call, in place, for
+ * all requests r and beams b.  Slots that no beam has are not touched.
+ *  parts_host: n_parts buffers (host array, read during the call), each n_slots slots of `bytes` bytes, slot_row bytes from slot to slot: rwkvq_linattn's states, rows of tokens
+ *      before, the sums of RWKVQ_IN_WKV, ... of all layers.  No two parts share a byte.
+ *  parents: [requests][beams], device memory; slots: [requests][beams], device memory (NULL: beam b of request r has slot r * beams + b).
+ * A request of which a parent or slot does not exist, or a slot is an earlier entry of the list, too: its states stay as they were, the others are moved,
+ * and rwkvq_device_status reports EINVAL.  (ETIMEOUT if a bounded wait ran out.)
+ * Parts, their bytes and slot_row are multiples of 16, lists of 4.  Asynchronous on `stream`, no workspace; parts are moved in launches of 128.
+ * Errors: EINVAL (parts that overlap, ...), EALIGN, EUNSUPPORTED (more than 64 beams, 2^20 beams in all, RWKVQ_MOST_STATE_PARTS parts, 2^47 bytes), ECUDA.
+ */
+#define RWKVQ_MOST_STATE_PARTS 1024
+typedef struct {
+  void* base;
+  uint64_t slot_row, bytes;
+} rwkvq_state_part;
+rwkvq_status rwkvq_state_reorder(const rwkvq_state_part* parts_host, int n_parts, int n_slots, const int32_t* parents_dev, const int32_t* slots_dev, int requests,
+                                 int beams, void* stream);
+
+/*
  * Decode the packed matrix to out_dev[oc][ic]: F32 = the exact value s*(q-z) (two IEEE fp32
  * operations: subtract, then multiply) or the fp16 codebook entry; BF16 = that value rounded to
  * nearest even.  Uses the same device unpack routines as the products (test surface for
@@ -579,7 +661,7 @@ rwkvq_status rwkvq_quant_error(const void* w_fp16_dev, const rwkvq_desc* W_desc,
                                void* stream);
 
 /* Device status word of the last launches on this device: RWKVQ_OK, ETIMEOUT if a bounded
- * wait inside a kernel gave up, or EINVAL (rwkvq_linattn's lists).  Synchronizes `stream`; clears the word. */
+ * wait inside a kernel gave up, or EINVAL (lists of rwkvq_linattn, rwkvq_lowrank, rwkvq_state_reorder).  Synchronizes `stream`; clears the word. */
 rwkvq_status rwkvq_device_status(void* stream);
 const char* rwkvq_status_str(rwkvq_status s);
 /* Text of the last CUDA error seen by this thread's library calls ("" if none). */

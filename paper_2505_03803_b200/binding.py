@@ -89,6 +89,7 @@ EXPORTS = [
     "rwkvq_desc_for", "rwkvq_quantize_workspace_bytes", "rwkvq_quantize_dev", "rwkvq_calib_representative",
     "rwkvq_quantize_dev_async", "rwkvq_quantize_dev_lost", "rwkvq_quantize_check",
     "rwkvq_fp8_scale_pitch", "rwkvq_fp8_quantize", "rwkvq_gemm_fp8", "rwkvq_gemm_fp8_lost", "rwkvq_gemm_fp8_plan", "rwkvq_linattn_workspace_bytes", "rwkvq_linattn",
+    "rwkvq_lowrank", "rwkvq_beam_select_workspace_bytes", "rwkvq_beam_select", "rwkvq_state_reorder",
 ]
 
 _lib = None
@@ -184,6 +185,12 @@ def lib() -> C.CDLL:
         L.rwkvq_linattn_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.rwkvq_linattn_workspace_bytes.restype = sz
         L.rwkvq_linattn.argtypes = [C.c_char_p, vp, sz, vp]
+    if hasattr(L, "rwkvq_lowrank"):
+        L.rwkvq_lowrank.argtypes = [C.c_char_p, C.POINTER(Desc), vp, vp]
+        L.rwkvq_beam_select_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.rwkvq_beam_select_workspace_bytes.restype = sz
+        L.rwkvq_beam_select.argtypes = [C.c_char_p, vp, sz, vp]
+        L.rwkvq_state_reorder.argtypes = [C.c_char_p, i32, i32, vp, vp, i32, i32, vp]
     _lib = L
     return L
 
@@ -848,5 +855,161 @@ def rwkvq_linattn(r, k, v, logw, u, out, state, state_out=None, seq_start=None, 
                               0 if slots is None else slots.data_ptr(), rows[0], rows[1], rows[2], w_stride[0] if tokens > 1 else 0, rows[3],
                               tokens, n_seq, heads, n, n_slots, types.get(dtype, -1), types.get(w_dtype, -1), per_head)
     status = (_lib or lib()).rwkvq_linattn(args, *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)), _stream_ptr(stream))
+    if status:
+        _check(status, where)
+
+
+_LOWRANK_ARGS = struct.Struct("@10P3q9i4x")          # rwkvq_lowrank_args
+
+
+def _check_list(where: str, x, size, what: str, here: int, dtype):
+    if x.get_device() != here:
+        _elsewhere(where, x, here)
+    if x.dtype is not dtype or x.numel() != size or not x.is_contiguous():
+        _refuse(where, f"{what} has to be {dtype} of {size} elements, contiguous")
+
+
+def rwkvq_lowrank(x, A, B, y, adapter, seq_start=None, ranks=None, scale=None, x_prev=None, xprev0=None, mu_desc: Desc | None = None, mu_image=None, stream=None):
+    """rwkvq_lowrank: y[t] += scale[a] B[a] (A[a] x_mix[t]).  x [tokens, ic] and y [tokens, oc] float32, float16 or bfloat16 (rows may be strided), A [n_adapters, rank, ic] and
+    B [n_adapters, oc, rank] float16 or bfloat16, adapter int32 [n_seq], seq_start int32 [n_seq + 1], ranks int32 and scale float32 [n_adapters], x_prev like x,
+    xprev0 [n_seq, ic] of x's type, mu_desc and mu_image a packed token-shift vector."""
+    where = "rwkvq_lowrank"
+    t = _torch or _load_torch()
+    x_shape, y_shape, a_shape, dtype, w_dtype, here = x.shape, y.shape, A.shape, x.dtype, A.dtype, _here()
+    if len(x_shape) != 2 or len(y_shape) != 2 or len(a_shape) != 3:
+        _refuse(where, "x and y have to be two-dimensional, A three-dimensional")
+    tokens, ic = x_shape
+    n_adapters, rank, _ = a_shape
+    oc = y_shape[1]
+    if y_shape[0] != tokens:
+        _refuse(where, f"y has to have {tokens} rows")
+    rows = []
+    for z in (x, y) if x_prev is None else (x, y, x_prev):
+        if z.get_device() != here:
+            _elsewhere(where, z, here)
+        row, one = z.stride()
+        if tokens and one != 1 and z.shape[1] > 1:
+            _refuse(where, "x, y and x_prev have to have their columns side by side")
+        rows.append(row if tokens > 1 else z.shape[1])
+    for z, shape in ((A, (n_adapters, rank, ic)), (B, (n_adapters, oc, rank))):
+        if z.get_device() != here:
+            _elsewhere(where, z, here)
+        if z.dtype is not w_dtype or z.shape != shape or not z.is_contiguous():
+            _refuse(where, f"A and B have to be [{n_adapters}, {rank}, {ic}] and [{n_adapters}, {oc}, {rank}] of one type, contiguous")
+    n_seq = adapter.numel()
+    _check_list(where, adapter, n_seq, "adapter", here, t.int32)
+    if seq_start is not None:
+        _check_list(where, seq_start, n_seq + 1, "seq_start", here, t.int32)
+    elif n_seq != 1 and n_seq != tokens:
+        _refuse(where, f"adapter has to be one number, or {tokens}, where there is no seq_start")
+    if ranks is not None:
+        _check_list(where, ranks, n_adapters, "ranks", here, t.int32)
+    if scale is not None:
+        _check_list(where, scale, n_adapters, "scale", here, t.float32)
+    if x_prev is not None and (x_prev.dtype is not dtype or x_prev.shape != x_shape):
+        _refuse(where, f"x_prev has to be {list(x_shape)} of {dtype}")
+    if xprev0 is not None:
+        _check_list(where, xprev0, n_seq * ic, "xprev0", here, dtype)
+    if (mu_image is None) != (mu_desc is None) or (mu_image is None and not (x_prev is None and xprev0 is None)):
+        _refuse(where, "a token shift has mu_desc and mu_image")
+    if mu_image is not None and mu_image.get_device() != here:
+        _elsewhere(where, mu_image, here)
+    types = _DTYPES or _dtypes()
+    args = _LOWRANK_ARGS.pack(x.data_ptr(), A.data_ptr(), B.data_ptr(), y.data_ptr(), adapter.data_ptr(), 0 if seq_start is None else seq_start.data_ptr(),
+                              0 if ranks is None else ranks.data_ptr(), 0 if scale is None else scale.data_ptr(), 0 if x_prev is None else x_prev.data_ptr(),
+                              0 if xprev0 is None else xprev0.data_ptr(), rows[0], rows[1], 0 if x_prev is None else rows[2], tokens, n_seq, ic, oc, rank, n_adapters,
+                              types.get(dtype, -1), types.get(w_dtype, -1), types.get(y.dtype, -1))
+    status = (_lib or lib()).rwkvq_lowrank(args, None if mu_desc is None else C.byref(mu_desc), None if mu_image is None else mu_image.data_ptr(), _stream_ptr(stream))
+    if status:
+        _check(status, where)
+
+
+_BEAM_SELECT_ARGS = struct.Struct("@7Pq6i")          # rwkvq_beam_select_args
+
+
+def rwkvq_beam_select_workspace_bytes(requests: int, beams: int, vocab: int, picks: int) -> int:
+    return int(lib().rwkvq_beam_select_workspace_bytes(requests, beams, vocab, picks))
+
+
+def rwkvq_beam_select(logits, scores, next_scores, parents, tokens, finished=None, eos: int = -1, finished_out=None, workspace=None, stream=None):
+    """rwkvq_beam_select: logits [requests * beams, vocab] float32, float16 or bfloat16 (rows may be strided), scores float32 [requests, beams], next_scores float32 and
+    parents, tokens int32 [requests, picks], finished uint8 or bool [requests, beams], finished_out of such a type [requests, picks], workspace uint8."""
+    where = "rwkvq_beam_select"
+    t = _torch or _load_torch()
+    shape, out, here = scores.shape, next_scores.shape, _here()
+    if len(shape) != 2 or len(out) != 2 or logits.dim() != 2:
+        _refuse(where, "logits, scores and next_scores have to be two-dimensional")
+    requests, beams = shape
+    vocab, picks = logits.shape[1], out[1]
+    if logits.get_device() != here:
+        _elsewhere(where, logits, here)
+    row, one = logits.stride()
+    if logits.shape[0] != requests * beams or (one != 1 and vocab > 1):
+        _refuse(where, f"logits have to be [{requests * beams}, vocab] with their columns side by side")
+    if out[0] != requests or parents.shape != out or tokens.shape != out:
+        _refuse(where, f"next_scores, parents and tokens have to be [{requests}, picks]")
+    _check_list(where, scores, requests * beams, "scores", here, t.float32)
+    _check_list(where, next_scores, requests * picks, "next_scores", here, t.float32)
+    _check_list(where, parents, requests * picks, "parents", here, t.int32)
+    _check_list(where, tokens, requests * picks, "tokens", here, t.int32)
+    if finished is not None:
+        _check_list(where, finished, requests * beams, "finished", here, t.bool if finished.dtype is t.bool else t.uint8)
+    if finished_out is not None:
+        _check_list(where, finished_out, requests * picks, "finished_out", here, t.bool if finished_out.dtype is t.bool else t.uint8)
+    if workspace is not None:
+        if workspace.get_device() != here:
+            _elsewhere(where, workspace, here)
+        if not workspace.is_contiguous():
+            _refuse(where, "workspace has to be contiguous")
+    args = _BEAM_SELECT_ARGS.pack(logits.data_ptr(), scores.data_ptr(), 0 if finished is None else finished.data_ptr(), next_scores.data_ptr(), parents.data_ptr(),
+                                  tokens.data_ptr(), 0 if finished_out is None else finished_out.data_ptr(), row if requests * beams > 1 else vocab, requests, beams, vocab,
+                                  picks, eos, (_DTYPES or _dtypes()).get(logits.dtype, -1))
+    status = (_lib or lib()).rwkvq_beam_select(args, *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)), _stream_ptr(stream))
+    if status:
+        _check(status, where)
+
+
+class StateParts:
+    """Buffers of states for rwkvq_state_reorder, from make_state_parts; keeps them alive."""
+    __slots__ = ("data", "n", "n_slots", "device", "keep")
+
+
+def make_state_parts(states) -> StateParts:
+    """states: CUDA tensors [n_slots, ...] (all of them as many slots), the elements of a slot side by side; slots may be strided."""
+    where = "make_state_parts"
+    states = list(states)
+    if not states:
+        _refuse(where, "there are no states")
+    p = StateParts()
+    p.n, p.n_slots, p.device, p.keep = len(states), states[0].shape[0] if states[0].dim() else 0, states[0].get_device(), states
+    out = []
+    for x in states:
+        if x.dim() < 2 or x.shape[0] != p.n_slots or x.get_device() != p.device or p.device < 0:
+            _refuse(where, f"states have to be [{p.n_slots}, ...] on one CUDA device")
+        if p.n_slots and not x[0].is_contiguous():
+            _refuse(where, "the elements of a slot have to lie side by side")
+        bytes_ = (x.numel() // p.n_slots if p.n_slots else 0) * x.element_size()
+        out += [x.data_ptr(), x.stride(0) * x.element_size() if p.n_slots > 1 else bytes_, bytes_]
+    p.data = struct.pack(f"@{3 * p.n}Q", *out)
+    return p
+
+
+def rwkvq_state_reorder(parts, parents, slots=None, stream=None):
+    """rwkvq_state_reorder: parts from make_state_parts (or a list of tensors for it), parents int32 [requests, beams], slots int32 [requests, beams] or None."""
+    where = "rwkvq_state_reorder"
+    t = _torch or _load_torch()
+    if not isinstance(parts, StateParts):
+        parts = make_state_parts(parts)
+    shape, here = parents.shape, _here()
+    if len(shape) != 2:
+        _refuse(where, "parents have to be [requests, beams]")
+    if parts.device != here:
+        _elsewhere(where, parts.keep[0], here)
+    requests, beams = shape
+    _check_list(where, parents, requests * beams, "parents", here, t.int32)
+    if slots is not None:
+        _check_list(where, slots, requests * beams, "slots", here, t.int32)
+    status = (_lib or lib()).rwkvq_state_reorder(parts.data, parts.n, parts.n_slots, parents.data_ptr(), None if slots is None else slots.data_ptr(), requests, beams,
+                                                 _stream_ptr(stream))
     if status:
         _check(status, where)
