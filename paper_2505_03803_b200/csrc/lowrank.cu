@@ -32,6 +32,7 @@ struct Args {
   const uint8_t* mu;             // index stream of the token-shift vector, or nullptr
   const uint32_t* mu_codebook;
   int mu_bits, mu_entries;
+  int splits;                    // clusters to a tile
   int* status;
 };
 
@@ -98,30 +99,57 @@ __device__ void find_tile(const Args& p, long long item, Tile& t, int* scratch) 
   if (tid == 0) t.n = 0;
   __syncthreads();
   if (!a.seq_start && a.n_seq == a.tokens && a.n_seq > 1) {
-    // one row a sequence: the first, seventeenth, ... row of an adapter takes it and the next fifteen of the same adapter
-    const int mine = a.adapter[item];
-    if (mine < 0 || mine >= a.n_adapters) {
-      if (tid == 0 && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
-      return;
-    }
-    int before = 0;
-    for (int i = tid; i < item; i += kThreads) before += a.adapter[i] == mine;
-    for (int o = 16; o > 0; o /= 2) before += __shfl_xor_sync(~0u, before, o);
-    if ((tid & 31) == 0) scratch[tid / 32] = before;
-    __syncthreads();
-    before = 0;
-    for (int w = 0; w < kWarps; ++w) before += scratch[w];
-    if (before % kRows) return;
-    if (tid < 32) {
-      int n = 0;
-      for (int i0 = (int)item; i0 < a.n_seq && n < kRows; i0 += 32) {
-        const int i = i0 + tid;
-        const uint32_t same = __ballot_sync(~0u, i < a.n_seq && a.adapter[i] == mine);
-        const int at = n + __popc(same & ((1u << tid) - 1));
-        if ((same >> tid & 1) && at < kRows) { t.rows[at] = i; t.seqs[at] = i; }
-        n = min(kRows, n + __popc(same));
+    // one row a sequence.  Rows of the same adapter are taken sixteen at a time; the item-th of these groups, in the order of their first rows.
+    if (a.n_seq <= kThreads) {
+      const int mine = tid < a.n_seq ? a.adapter[tid] : -1;
+      scratch[tid] = mine;
+      __syncthreads();
+      int before = 0;
+      for (int i = 0; i < min(tid, a.n_seq); ++i) before += scratch[i] == mine;
+      const bool ok = mine >= 0 && mine < a.n_adapters;
+      if (!ok && tid < a.n_seq && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
+      const bool leads = ok && before % kRows == 0;
+      const uint32_t vote = __ballot_sync(~0u, leads);
+      int* const heads = scratch + kThreads;
+      if ((tid & 31) == 0) heads[tid / 32] = __popc(vote);
+      if (tid == 0) heads[kWarps] = -1;
+      __syncthreads();
+      int at = __popc(vote & ((1u << (tid & 31)) - 1));
+      for (int w = 0; w < tid / 32; ++w) at += heads[w];
+      if (leads && at == item) { heads[kWarps] = mine; heads[kWarps + 1] = before; }
+      __syncthreads();
+      const int adapter = heads[kWarps], from = heads[kWarps + 1];
+      if (adapter < 0) return;
+      const bool in = mine == adapter && before >= from && before < from + kRows;
+      if (in) { t.rows[before - from] = tid; t.seqs[before - from] = tid; }
+      const int n = __syncthreads_count(in);
+      if (tid == 0) { t.n = n; t.adapter = adapter; }
+    } else {
+      // many rows: an item is a row, which takes the next fifteen of its adapter if it is the first, seventeenth, ... of these
+      const int mine = a.adapter[item];
+      if (mine < 0 || mine >= a.n_adapters) {
+        if (tid == 0 && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
+        return;
       }
-      if (tid == 0) { t.n = n; t.adapter = mine; }
+      int before = 0;
+      for (int i = tid; i < item; i += kThreads) before += a.adapter[i] == mine;
+      for (int o = 16; o > 0; o /= 2) before += __shfl_xor_sync(~0u, before, o);
+      if ((tid & 31) == 0) scratch[tid / 32] = before;
+      __syncthreads();
+      before = 0;
+      for (int w = 0; w < kWarps; ++w) before += scratch[w];
+      if (before % kRows) return;
+      if (tid < 32) {
+        int n = 0;
+        for (int i0 = (int)item; i0 < a.n_seq && n < kRows; i0 += 32) {
+          const int i = i0 + tid;
+          const uint32_t same = __ballot_sync(~0u, i < a.n_seq && a.adapter[i] == mine);
+          const int at = n + __popc(same & ((1u << tid) - 1));
+          if ((same >> tid & 1) && at < kRows) { t.rows[at] = i; t.seqs[at] = i; }
+          n = min(kRows, n + __popc(same));
+        }
+        if (tid == 0) { t.n = n; t.adapter = mine; }
+      }
     }
   } else {
     int seq = 0, first = (int)item * kRows, last = min(first + kRows, a.tokens), start = 0;
@@ -180,15 +208,6 @@ __device__ __forceinline__ __nv_bfloat16 term(float& x) {
   return __ushort_as_bfloat16((unsigned short)(__float_as_uint(hi) >> 16));
 }
 
-template <bool kHalf>
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&w)[4], uint32_t x0, uint32_t x1) {
-  if constexpr (kHalf)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(x0), "r"(x1));
-  else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(x0), "r"(x1));
-}
 // A pair of f16 weights as two pairs of bf16: eleven bits are eight and three.
 __device__ __forceinline__ void apart(uint32_t w, uint32_t& hi, uint32_t& lo) {
   float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
@@ -196,6 +215,22 @@ __device__ __forceinline__ void apart(uint32_t w, uint32_t& hi, uint32_t& lo) {
   h.x = term(f.x); h.y = term(f.y);
   l.x = term(f.x); l.y = term(f.y);
   hi = *reinterpret_cast<const uint32_t*>(&h); lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+
+// y[at], y[at + 1] += v.  Each element of y is added to once in a call, so that a reduction in memory is as good as a load, an addition and a store, and
+// nothing waits for it (it takes subnormal numbers for zeros).
+__device__ __forceinline__ void add_pair(void* y, int dtype, long long at, float v0, float v1) {
+  if (dtype == RWKVQ_F32) {
+    asm volatile("red.relaxed.gpu.global.add.v2.f32 [%0], {%1, %2};" ::"l"(static_cast<float*>(y) + at), "f"(v0), "f"(v1) : "memory");
+  } else if (dtype == RWKVQ_F16) {
+    __half2* const p = reinterpret_cast<__half2*>(static_cast<__half*>(y) + at);
+    const float2 f = __half22float2(*p);
+    *p = __floats2half2_rn(f.x + v0, f.y + v1);
+  } else {
+    __nv_bfloat162* const p = reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(y) + at);
+    const float2 f = __bfloat1622float2(*p);
+    *p = __floats2bfloat162_rn(f.x + v0, f.y + v1);
+  }
 }
 
 // How x and the weights go into the tensor cores.
@@ -212,59 +247,128 @@ __device__ __forceinline__ uint32_t mu_pair(const Args& p, const uint32_t* codeb
   return codebook[(two >> (bit & 7u)) & ((1u << p.mu_bits) - 1u)];
 }
 
+// ---- few rows: the weights straight from memory into registers ----------------------------------------------
+// A unit is sixteen rows of a weight matrix by 32 columns: lane (g, q) holds columns 8q to 8q + 7 of rows g and g + 8, the operands of four steps whose columns are
+// numbered so that the first four of the eight are one step's and the others the next one's.
+struct Unit { uint4 lo, hi; };        // row g, row g + 8
+constexpr int kAhead = 4;             // units that a warp has on their way
+
+// `lanes`: of the lane's eight columns, those that exist (the others come out as zeros: they may hold anything).
+template <typename W>
+__device__ __forceinline__ Unit load_unit(const W* m, long long row, long long rows, long long pitch, int col, int cols) {
+  Unit u;
+  u.lo = u.hi = make_uint4(0, 0, 0, 0);
+  if (col < cols) {
+    if (row < rows) u.lo = __ldg(reinterpret_cast<const uint4*>(m + row * pitch + col));
+    if (row + 8 < rows) u.hi = __ldg(reinterpret_cast<const uint4*>(m + (row + 8) * pitch + col));
+  }
+  return u;
+}
+__device__ __forceinline__ void keep(uint4& w, int n) {        // the first n of eight numbers of two bytes
+  auto of = [n](int i) { return n >= 2 * i + 2 ? ~0u : n == 2 * i + 1 ? 0xFFFFu : 0u; };
+  w.x &= of(0); w.y &= of(1); w.z &= of(2); w.w &= of(3);
+}
+
+// d[0], d[1]: sixteen rows of x (a: row g, b: row g + 8 of the lane's columns) by the unit's rows 0 to 7 and 8 to 15.
+template <bool kHalf>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (kHalf)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <bool kHalf>
+__device__ __forceinline__ void mma_unit(float (&d)[2][4], const uint4& xa, const uint4& xb, const Unit& w) {
+  mma<kHalf>(d[0], xa.x, xb.x, xa.y, xb.y, w.lo.x, w.lo.y);
+  mma<kHalf>(d[1], xa.x, xb.x, xa.y, xb.y, w.hi.x, w.hi.y);
+  mma<kHalf>(d[0], xa.z, xb.z, xa.w, xb.w, w.lo.z, w.lo.w);
+  mma<kHalf>(d[1], xa.z, xb.z, xa.w, xb.w, w.hi.z, w.hi.w);
+}
+__device__ __forceinline__ void apart(const uint4& w, uint4& hi, uint4& lo) {
+  apart(w.x, hi.x, lo.x); apart(w.y, hi.y, lo.y); apart(w.z, hi.z, lo.z); apart(w.w, hi.w, lo.w);
+}
+// All terms of x (`pitch` bytes from row to row, `next` from term to term) by a unit of weights, which are taken apart if they have to be: the small products first.
+template <bool kHalf, bool kApart, int kTerms>
+__device__ __forceinline__ void multiply(float (&d)[2][4], const uint8_t* x, uint32_t pitch, uint32_t next, int terms, const Unit& w) {
+  Unit hi = w, lo;
+  if constexpr (kApart) { apart(w.lo, hi.lo, lo.lo); apart(w.hi, hi.hi, lo.hi); }
+#pragma unroll
+  for (int k = kTerms - 1; k >= 0; --k) {
+    if (k >= terms) continue;
+    const uint4 xa = *reinterpret_cast<const uint4*>(x + k * next), xb = *reinterpret_cast<const uint4*>(x + k * next + 8 * pitch);
+    if constexpr (kApart) mma_unit<kHalf>(d, xa, xb, lo);
+    mma_unit<kHalf>(d, xa, xb, hi);
+  }
+}
+
 template <typename X, typename W>
 struct Shape {
   static constexpr int kTerms = Form<X, W>::kX;
-  static constexpr int kPitch = kMostCols * 2 + 64;                   // bytes of a row of x in shared memory: 16-byte reads of two rows meet no bank twice
+  // bytes of a row in shared memory: 16-byte reads of two neighbouring rows meet no bank twice
+  static constexpr int kPitch = kMostCols * 2 + 64, kHPitch = kMostRank * 2 + 64, kSharePitch = kMostRank;
   static constexpr int kXBytes = kTerms * kRows * kPitch;
-  static constexpr int kPart = kWarps * 16 * kRows * 4;               // partial sums: [group of warps][rank][row]
-  static constexpr int kHPitch = kMostRank * 2 + 16;
+  static constexpr int kPart = kWarps * 16 * kRows * 4;               // partial sums: [group of warps][block of 16][row][16]
+  static constexpr int kShare = kRows * kSharePitch * 4;
   static constexpr int kHBytes = 3 * kRows * kHPitch;
-  static constexpr int kBytes = kXBytes + kPart + kMostRank * kRows * 4 + kHBytes + 256 * 4;
+  static constexpr int kBytes = (kXBytes > kHBytes ? kXBytes : kHBytes) + kPart + kShare + 256 * 4;
 };
 
 template <typename X, typename W>
-__global__ void __launch_bounds__(kThreads) lowrank_kernel(const Args p) {
+__global__ void __launch_bounds__(kThreads, 2) lowrank_kernel(const Args p) {
   using S = Shape<X, W>;
   using F = Form<X, W>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Tile t;
   __shared__ int scratch[2 * kThreads + 2];
-  uint8_t* const xs = smem;
-  float* const part = reinterpret_cast<float*>(smem + S::kXBytes);
-  float* const share = reinterpret_cast<float*>(smem + S::kXBytes + S::kPart);          // this block's share of A x: [rank][row]
-  uint8_t* const hs = smem + S::kXBytes + S::kPart + kMostRank * kRows * 4;              // [term][row][rank]
-  uint32_t* const codebook = reinterpret_cast<uint32_t*>(hs + S::kHBytes);
+  uint8_t* const xs = smem;                                                             // [term][row][column], then A x: [term][row][rank]
+  uint8_t* const hs = smem;
+  float* const part = reinterpret_cast<float*>(smem + (S::kXBytes > S::kHBytes ? S::kXBytes : S::kHBytes));
+  float* const share = part + S::kPart / 4;                                             // this block's share of A x: [row][rank]
+  uint32_t* const codebook = reinterpret_cast<uint32_t*>(share + S::kShare / 4);
   const rwkvq_lowrank_args& a = p.a;
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  find_tile(p, blockIdx.x / C, t, scratch);
+  const int id = (int)(blockIdx.x / C), item = id / p.splits, split = id - item * p.splits;
+  find_tile(p, item, t, scratch);
   __syncthreads();
   const int n = t.n;
   if (n == 0) return;            // the same for all blocks of the cluster
-  const int rank = t.rank, blocks = (rank + 15) / 16, blocks2 = (n + 7) / 8;
-  if (p.mu)
-    for (int i = tid; i < p.mu_entries; i += kThreads) codebook[i] = p.mu_codebook[i];
+  const int rank = t.rank, blocks = (rank + 15) / 16;
+  const float scale = a.scale ? a.scale[t.adapter] : 1.f;
 
-  // ---- A x over this block's columns
+  // ---- A x over this block's columns.  Warps side by side along the rank as far as it reaches, the others along the columns
   const int units = (a.ic + 31) / 32, u0 = (int)((long long)units * c / C), u1 = (int)((long long)units * (c + 1) / C);
-  // warps side by side along the rank as far as it reaches, the others along the columns
   int along = 1;
   while (along < kWarps && along < blocks) along *= 2;
   const int groups = kWarps / along, group = warp / along, wr = warp % along;
   const W* const A = static_cast<const W*>(a.A) + (long long)t.adapter * a.rank * a.ic;
+  const int live = wr < blocks ? rank : 0;          // warps beyond the rank have nothing to read
+  Unit w[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) {
+    const int u = u0 + group + j * groups;
+    w[j] = load_unit(A, wr * 16 + g, live, a.ic, u * 32 + q * 8, u < u1 ? a.ic : 0);
+  }
+  if (p.mu) {
+    for (int i = tid; i < p.mu_entries; i += kThreads) codebook[i] = p.mu_codebook[i];
+    __syncthreads();
+  }
   float acc[2][4] = {};
   for (int uc = u0; uc < u1; uc += kMostCols / 32) {
-    const int ue = min(uc + kMostCols / 32, u1), cols = (ue - uc) * 32, eights = cols / 8;
-    __syncthreads();
-    for (int i = tid; i < kRows * eights; i += kThreads) {
+    const int ue = min(uc + kMostCols / 32, u1), eights = (ue - uc) * 4;
+    if (uc > u0) __syncthreads();
+    for (int i = tid; i < n * eights; i += kThreads) {
       const int r = i / eights, col8 = i - r * eights, col = uc * 32 + col8 * 8;
       float x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = 0.f;
-      if (r < n && col < a.ic) {
+      if (col < a.ic) {
         load8(static_cast<const X*>(a.x) + (long long)t.rows[r] * a.x_row + col, x);
         if (p.mu) {
           float y[8];
@@ -285,145 +389,137 @@ __global__ void __launch_bounds__(kThreads) lowrank_kernel(const Args p) {
       }
 #pragma unroll
       for (int k = 0; k < F::kX; ++k) {
-        uint32_t w[4];
+        uint32_t v[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           if constexpr (F::kHalf) {
             const __half2 h = __floats2half2_rn(x[2 * j], x[2 * j + 1]);
-            w[j] = *reinterpret_cast<const uint32_t*>(&h);
+            v[j] = *reinterpret_cast<const uint32_t*>(&h);
           } else {
             __nv_bfloat162 h;
             h.x = term(x[2 * j]); h.y = term(x[2 * j + 1]);
-            w[j] = *reinterpret_cast<const uint32_t*>(&h);
+            v[j] = *reinterpret_cast<const uint32_t*>(&h);
           }
         }
-        *reinterpret_cast<uint4*>(xs + (k * kRows + r) * S::kPitch + col8 * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(xs + (k * kRows + r) * S::kPitch + col8 * 16) = make_uint4(v[0], v[1], v[2], v[3]);
       }
     }
     __syncthreads();
+    // rows of x behind the n-th hold whatever was there: a row meets its own outputs alone
     if (wr < blocks) {
-      const int r0 = wr * 16 + g, r1 = r0 + 8;
-      for (int u = uc + group; u < ue; u += groups) {
-        const int col = u * 32 + q * 8;
-        uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
-        if (r0 < rank && col < a.ic) w0 = *reinterpret_cast<const uint4*>(A + (long long)r0 * a.ic + col);
-        if (r1 < rank && col < a.ic) w1 = *reinterpret_cast<const uint4*>(A + (long long)r1 * a.ic + col);
-        const uint32_t f[2][4] = {{w0.x, w1.x, w0.y, w1.y}, {w0.z, w1.z, w0.w, w1.w}};
-        uint32_t hi[2][4], lo[2][4];
-        if constexpr (F::kApart) {
+      for (int u = uc + group; u < ue; u += kAhead * groups) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) apart(f[h][j], hi[h][j], lo[h][j]);
+        for (int j = 0; j < kAhead; ++j) {
+          const int v = u + j * groups;
+          if (v >= ue) continue;
+          multiply<F::kHalf, F::kApart, F::kX>(acc, xs + g * S::kPitch + ((v - uc) * 32 + q * 8) * 2, S::kPitch, kRows * S::kPitch, F::kX, w[j]);
         }
+        const int next = u + kAhead * groups < ue ? u + kAhead * groups : ue + group;
 #pragma unroll
-        for (int k = F::kX - 1; k >= 0; --k)
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            if (b >= blocks2) continue;
-            const uint4 xv = *reinterpret_cast<const uint4*>(xs + (k * kRows + b * 8 + g) * S::kPitch + ((u - uc) * 32 + q * 8) * 2);
-            if constexpr (F::kApart) {
-              mma<false>(acc[b], lo[0], xv.x, xv.y); mma<false>(acc[b], lo[1], xv.z, xv.w);
-              mma<false>(acc[b], hi[0], xv.x, xv.y); mma<false>(acc[b], hi[1], xv.z, xv.w);
-            } else {
-              mma<F::kHalf>(acc[b], f[0], xv.x, xv.y); mma<F::kHalf>(acc[b], f[1], xv.z, xv.w);
-            }
-          }
+        for (int j = 0; j < kAhead; ++j) {
+          const int v = next + j * groups;
+          w[j] = load_unit(A, wr * 16 + g, live, a.ic, v * 32 + q * 8, v < u1 ? a.ic : 0);
+        }
       }
     }
   }
+
+  // ---- B's first units on their way
+  const int tiles = (a.oc + 15) / 16, all_parts = C * p.splits, part_id = split * C + c;
+  const int o0 = (int)((long long)tiles * part_id / all_parts), o1 = (int)((long long)tiles * (part_id + 1) / all_parts);
+  const W* const Bm = static_cast<const W*>(a.B) + (long long)t.adapter * a.oc * a.rank;
+  const int kb = (rank + 31) / 32, mine = o0 + warp < o1 ? (o1 - o0 - warp + kWarps - 1) / kWarps * kb : 0;        // units of this warp, tile after tile
+  auto load_b = [&](int i) {
+    const int tile = i / kb, k = i - tile * kb, col = k * 32 + q * 8;
+    Unit u = load_unit(Bm, (long long)(o0 + warp + tile * kWarps) * 16 + g, i < mine ? a.oc : 0, a.rank, col, rank);
+    if (col + 8 > rank) { keep(u.lo, rank - col); keep(u.hi, rank - col); }        // what lies behind the adapter's rank may be anything
+    return u;
+  };
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) w[j] = load_b(j);
+
+  // ---- the block's share: its groups of warps added up
   if (wr < blocks) {
     float* at = part + (group * along + wr) * 16 * kRows;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      *reinterpret_cast<float2*>(at + g * kRows + b * 8 + q * 2) = make_float2(acc[b][0], acc[b][1]);
-      *reinterpret_cast<float2*>(at + (g + 8) * kRows + b * 8 + q * 2) = make_float2(acc[b][2], acc[b][3]);
+    for (int h = 0; h < 2; ++h) {
+      *reinterpret_cast<float2*>(at + g * 16 + h * 8 + q * 2) = make_float2(acc[h][0], acc[h][1]);
+      *reinterpret_cast<float2*>(at + (g + 8) * 16 + h * 8 + q * 2) = make_float2(acc[h][2], acc[h][3]);
     }
   }
   __syncthreads();
-  for (int i = tid; i < blocks * 16 * kRows; i += kThreads) {
+  for (int i = tid; i < n * blocks * 16; i += kThreads) {
+    const int row = i / (blocks * 16), r = i - row * blocks * 16, at = (r / 16 * kRows + row) * 16 + r % 16;
     float s = 0.f;
-    for (int k = 0; k < groups; ++k) s += part[k * along * 16 * kRows + i];
-    share[i] = s;
+    for (int k = 0; k < groups; ++k) s += part[k * along * 16 * kRows + at];
+    share[row * S::kSharePitch + r] = s;
   }
   cluster.sync();
 
   // ---- all of A x, as operands
-  const int last_term = a.y_dtype == RWKVQ_F32 ? 2 : 1;
-  const float scale = a.scale ? a.scale[t.adapter] : 1.f;
-  for (int i = tid; i < blocks * 16 * kRows; i += kThreads) {
+  const int last_term = a.y_dtype == RWKVQ_F32 ? 2 : 1, width = kb * 32;
+  for (int i = tid; i < n * width; i += kThreads) {
+    const int row = i / width, r = i - row * width;
     float s = 0.f;
-    for (int k = 0; k < C; ++k) s += cluster.map_shared_rank(share, k)[i];
-    s *= scale;
-    const int r = i / kRows, row = i % kRows;
+    if (r < rank) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = k < C ? cluster.map_shared_rank(share, k)[row * S::kSharePitch + r] : 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[k];
+      s *= scale;
+    }
     __nv_bfloat16* const at = reinterpret_cast<__nv_bfloat16*>(hs + row * S::kHPitch + r * 2);
     at[0] = term(s);
     at[kRows * S::kHPitch / 2] = last_term == 1 ? __float2bfloat16_rn(s) : term(s);
     if (last_term == 2) at[2 * kRows * S::kHPitch / 2] = term(s);
   }
-  cluster.sync();                // also: no block ends while another reads its share
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  __syncthreads();
 
   // ---- B (A x) for this block's rows of B
-  const int tiles = (a.oc + 15) / 16, o0 = (int)((long long)tiles * c / C), o1 = (int)((long long)tiles * (c + 1) / C);
-  const W* const Bm = static_cast<const W*>(a.B) + (long long)t.adapter * a.oc * a.rank;
-  for (int o = o0 + warp; o < o1; o += kWarps) {
-    const int r0 = o * 16 + g, r1 = r0 + 8;
-    float d[2][4] = {};
-    for (int ks = 0; ks < blocks; ++ks) {
-      const int col = ks * 16 + q * 4;
-      uint2 w0 = make_uint2(0, 0), w1 = w0;
-      if (r0 < a.oc && col < rank) w0 = *reinterpret_cast<const uint2*>(Bm + (long long)r0 * a.rank + col);
-      if (r1 < a.oc && col < rank) w1 = *reinterpret_cast<const uint2*>(Bm + (long long)r1 * a.rank + col);
-      if (col + 4 > rank) {        // what lies behind the adapter's rank may be anything
-        const uint32_t x = col + 2 > rank ? (col + 1 > rank ? 0u : 0xFFFFu) : ~0u, y = col + 4 > rank ? (col + 3 > rank ? 0u : 0xFFFFu) : ~0u;
-        w0.x &= x; w1.x &= x; w0.y &= y; w1.y &= y;
-      }
-      const uint32_t f[4] = {w0.x, w1.x, w0.y, w1.y};
-      uint32_t hi[4], lo[4];
-      if constexpr (std::is_same<W, __half>::value) {
+  float d[2][4] = {};
+  for (int i = 0; i < mine; i += kAhead) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) apart(f[j], hi[j], lo[j]);
-      }
-      for (int k = last_term; k >= 0; --k)
+    for (int j = 0; j < kAhead; ++j) {
+      if (i + j >= mine) continue;
+      const int tile = (i + j) / kb, k = i + j - tile * kb;
+      multiply<false, std::is_same<W, __half>::value, 3>(d, hs + g * S::kHPitch + (k * 32 + q * 8) * 2, S::kHPitch, kRows * S::kHPitch, last_term + 1, w[j]);
+      w[j] = load_b(i + j + kAhead);
+      if (k + 1 < kb) continue;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          if (b >= blocks2) continue;
-          const uint2 h = *reinterpret_cast<const uint2*>(hs + (k * kRows + b * 8 + g) * S::kHPitch + col * 2);
-          if constexpr (std::is_same<W, __half>::value) {
-            mma<false>(d[b], lo, h.x, h.y);
-            mma<false>(d[b], hi, h.x, h.y);
-          } else {
-            mma<false>(d[b], f, h.x, h.y);
-          }
+      for (int h = 0; h < 2; ++h) {
+        const int col = (o0 + warp + tile * kWarps) * 16 + h * 8 + q * 2;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int row = g + e * 8;
+          const float v0 = d[h][2 * e], v1 = d[h][2 * e + 1];
+          if (row < n && col < a.oc) add_pair(a.y, a.y_dtype, (long long)t.rows[row] * a.y_row + col, v0, v1);
+          d[h][2 * e] = d[h][2 * e + 1] = 0.f;
         }
-    }
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int row = b * 8 + q * 2 + (j & 1), col = j < 2 ? r0 : r1;
-        if (row >= n || col >= a.oc) continue;
-        const long long at = (long long)t.rows[row] * a.y_row + col;
-        if (a.y_dtype == RWKVQ_F32) static_cast<float*>(a.y)[at] += d[b][j];
-        else if (a.y_dtype == RWKVQ_F16) static_cast<__half*>(a.y)[at] = __float2half_rn(__half2float(static_cast<__half*>(a.y)[at]) + d[b][j]);
-        else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(__bfloat162float(static_cast<__nv_bfloat16*>(a.y)[at]) + d[b][j]);
       }
+    }
   }
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // no block ends while another reads its share
 }
 
 template <typename X, typename W>
-cudaError_t launch(const Args& p, long long items, cudaStream_t s) {
+cudaError_t launch(Args p, long long items, cudaStream_t s) {
   using S = Shape<X, W>;
   static SmemOptIn opt_in(kCarveOut);
   cudaError_t e = opt_in((const void*)lowrank_kernel<X, W>, S::kBytes);
   if (e != cudaSuccess) return e;
   const unsigned C = 8;
+  // where there are few tiles, several clusters divide a tile's rows of B, and each multiplies A x for itself
+  p.splits = (int)std::max<long long>(1, std::min<long long>({2ll * sm_count() / (items * C), (p.a.oc + 16 * C * kWarps - 1) / (16 * C * kWarps), 16}));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)items * C); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = S::kBytes; cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = S::kBytes; cfg.stream = s;
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr; cfg.numAttrs = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, lowrank_kernel<X, W>, p);
 }
 template <typename X>
@@ -472,7 +568,8 @@ rwkvq_status rwkvq_lowrank(const rwkvq_lowrank_args* args, const rwkvq_desc* mu_
   if (!p.status) return RWKVQ_ECUDA;
   // tiles that there can be
   const long long full = ((long long)a.tokens + lr::kRows - 1) / lr::kRows;
-  const long long items = a.seq_start ? std::min<long long>(a.tokens, full + a.n_seq) : a.n_seq == 1 ? full : a.n_seq;
+  const long long items = a.seq_start ? std::min<long long>(a.tokens, full + a.n_seq) : a.n_seq == 1 ? full :
+                          a.n_seq <= lr::kThreads ? std::min<long long>(a.n_seq, a.n_adapters + full) : a.n_seq;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (a.x_dtype == RWKVQ_F32) return cuda_status(lr::launch_x<float>(p, items, s));
   if (a.x_dtype == RWKVQ_F16) return cuda_status(lr::launch_x<__half>(p, items, s));

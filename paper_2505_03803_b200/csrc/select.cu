@@ -5,9 +5,9 @@
 // and takes the best of the pieces' best (beam_merge_kernel).  Sums are fp32 within a thread and fp64 behind it; totals are compared in fp64, because
 // candidates of different beams come near one another.
 //
-// Finding the best of a piece: no sort.  A thread holds 32 elements of a tile in registers, and knows the largest.  The q-th largest of a warp's 32 largest
+// Finding the best of a piece: no sort.  A thread holds 64 bytes of a tile in registers, and knows the largest element.  The q-th largest of a warp's 32 largest
 // ones, q = ceil(picks / 8), is passed by q elements in each of the block's eight warps, so that what is below the least of these eight cannot be among the best:
-// a few dozen elements of 8192 are left, and ranked by counting.  From the second tile on the last best element is the bound, and hardly any tile has one above it.
+// a few dozen elements of the tile are left, and ranked by counting.  From the second tile on the last best element is the bound, and hardly any tile has one above it.
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -21,7 +21,8 @@
 namespace rwkvq {
 namespace bs {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kHold = 32, kTile = kThreads * kHold, kMostPicks = 64, kMostBeams = 64, kMostPieces = 64, kMostVocab = 1 << 24;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kLoads = 4, kMostPicks = 64, kMostBeams = 64, kMostPieces = 64, kMostVocab = 1 << 24;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kList = 256;          // candidates that are ranked by counting; more (many equal ones) are taken out one by one
 
 struct Args {
@@ -36,46 +37,66 @@ struct Args {
   int requests, beams, vocab, picks, eos, pieces, piece_vecs;
   double* sums;            // [rows][pieces]: sum of e^(logit - m) of the piece
   float* tops;             // [rows][pieces]: m
-  int* counts;             // [rows][pieces]: best logits that there are
-  uint2* best;             // [rows][pieces][picks]: logit (bits), token; falling, equal ones by rising token
+  uint2* best;             // [rows][pieces][picks]: logit (bits), token; falling, equal ones by rising token, behind the last -inf
 };
 
-// A number by which fp32 numbers compare as whole ones; NaN counts as -inf, which is left out everywhere (0).
+// A number by which fp32 numbers compare as whole ones; both zeros are one; NaN counts as -inf, which is left out everywhere (0).
 __device__ __forceinline__ uint32_t order_of(float x) {
-  const uint32_t b = __float_as_uint(x);
+  const uint32_t b = __float_as_uint(x + 0.f);
   return x > -INFINITY ? (b & 0x80000000u ? ~b : b | 0x80000000u) : 0u;
 }
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
+__device__ __forceinline__ uint64_t order_of(double x) {
+  const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
+  return b >> 63 ? ~b : b | 1ull << 63;
+}
+__device__ __forceinline__ double value_of(uint64_t o) { return __longlong_as_double((long long)(o >> 63 ? o & ~(1ull << 63) : ~o)); }
 
+__device__ __forceinline__ float exp2_of(float x) {        // 2^x, 2^-126 and less as 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 z, x, y;\n mov.b64 {%0, %1}, z;\n}" : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mul.rn.f32x2 z, x, y;\n mov.b64 {%0, %1}, z;\n}" : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// Elements as they lie in memory: kPer to a word of 32 bits.
 template <typename T> struct Raw;
 template <> struct Raw<float> {
-  static constexpr int kVec = 4;
-  static __device__ __forceinline__ void values(const uint4& w, float* f) {
-    f[0] = __uint_as_float(w.x); f[1] = __uint_as_float(w.y); f[2] = __uint_as_float(w.z); f[3] = __uint_as_float(w.w);
-  }
+  static constexpr int kPer = 1;
+  static constexpr uint32_t kNone = 0xFF800000u;        // -inf
+  static __device__ __forceinline__ float value(uint32_t w, int) { return __uint_as_float(w); }
+  static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }      // of a NaN and a number the number
+  static __device__ __forceinline__ uint32_t word(const float* p) { return __float_as_uint(*p); }
 };
 template <> struct Raw<__half> {
-  static constexpr int kVec = 8;
-  static __device__ __forceinline__ void values(const uint4& w, float* f) {
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
-      f[2 * i] = p.x; f[2 * i + 1] = p.y;
-    }
+  static constexpr int kPer = 2;
+  static constexpr uint32_t kNone = 0xFC00u;
+  static __device__ __forceinline__ float value(uint32_t w, int i) { return __half2float(__ushort_as_half((unsigned short)(i ? w >> 16 : w & 0xFFFFu))); }
+  static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) {
+    const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
   }
+  static __device__ __forceinline__ uint32_t word(const __half* p) { return __half_as_ushort(*p); }
 };
 template <> struct Raw<__nv_bfloat16> {
-  static constexpr int kVec = 8;
-  static __device__ __forceinline__ void values(const uint4& w, float* f) {
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(v[i] << 16); f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u); }
+  static constexpr int kPer = 2;
+  static constexpr uint32_t kNone = 0xFF80u;
+  static __device__ __forceinline__ float value(uint32_t w, int i) { return __uint_as_float(i ? w & 0xFFFF0000u : w << 16); }
+  static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
   }
+  static __device__ __forceinline__ uint32_t word(const __nv_bfloat16* p) { return __bfloat16_as_ushort(*p); }
 };
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 // The 16 bytes that begin `skew` bytes behind those of a, which b follows.
 __device__ __forceinline__ uint4 joined(const uint4& a, const uint4& b, uint32_t skew) {
@@ -90,14 +111,6 @@ __device__ __forceinline__ uint4 joined(const uint4& a, const uint4& b, uint32_t
   return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
 }
 
-// Candidates of a block: keys that are all different, larger = better.  hi: the value's order; lo: ~index.
-struct Best {
-  uint64_t list[kList + kMostPicks];
-  uint64_t ranked[kMostPicks];
-  uint32_t warp_top[kWarps], warp_low[kWarps];
-  int count, owner;
-};
-
 // The q-th largest of a warp's 32 numbers (0 where fewer are above 0).
 __device__ __forceinline__ uint32_t qth_of_warp(uint32_t x, int q) {
   uint32_t top = 0;
@@ -109,21 +122,18 @@ __device__ __forceinline__ uint32_t qth_of_warp(uint32_t x, int q) {
   return top;
 }
 
-// The first `picks` of the n keys in list, falling, to ranked, and the number of them.  All threads; n <= kList + kMostPicks.
-__device__ __forceinline__ int rank(Best& b, int n, int picks) {
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const uint64_t mine = b.list[i];
-    int above = 0;
-    for (int j = 0; j < n; ++j) above += b.list[j] > mine;
-    if (above < picks) b.ranked[above] = mine;
-  }
-  __syncthreads();
-  return min(n, picks);
-}
+// Candidates of a block: keys that are all different, larger = better.  High half: the value's order; low half: ~index.
+struct Best {
+  uint64_t list[kList];
+  uint64_t ranked[kMostPicks];
+  uint32_t warp_top[kWarps], warp_low[kWarps];
+  int count;
+};
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) beam_scan_kernel(const Args a) {
-  constexpr int V = Raw<T>::kVec, kLoads = kHold / V;
+__global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const Args a) {
+  using R = Raw<T>;
+  constexpr int kWords = 4 * kLoads, kHold = kWords * R::kPer, V = 4 * R::kPer;
   __shared__ Best b;
   __shared__ float warp_m[kWarps];
   __shared__ double warp_s[kWarps];
@@ -140,98 +150,147 @@ __global__ void __launch_bounds__(kThreads) beam_scan_kernel(const Args a) {
   const int n_vecs = (a.vocab + V - 1) / V;
   const int v0 = min((int)blockIdx.x * a.piece_vecs, n_vecs), v1 = min(v0 + a.piece_vecs, n_vecs);
   const int q = (a.picks + kWarps - 1) / kWarps;
-  float m = -INFINITY, s = 0.f;
-  int have = 0;                     // ranked[0 .. have) are the best so far
-  uint32_t floor_order = 0;         // order of ranked[picks - 1], once there are as many: later elements have to be above it
-  for (int t0 = v0; t0 < v1; t0 += kThreads * kLoads) {
-    float f[kHold];
+  auto load = [&](int t0, uint4 (&w)[kLoads]) {
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) {
       const int v = t0 + l * kThreads + tid, first = v * V;
-      float* x = f + l * V;
       if (skew == 0 && v < v1 && first + V <= a.vocab) {
-        Raw<T>::values(__ldg(vecs + v), x);
+        w[l] = __ldg(vecs + v);
       } else if (skew != 0 && v < v1 && v > 0 && first + 2 * V <= a.vocab) {
-        Raw<T>::values(joined(__ldg(vecs + v), __ldg(vecs + v + 1), skew), x);
+        w[l] = joined(__ldg(vecs + v), __ldg(vecs + v + 1), skew);
       } else {
+        uint32_t x[4];
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = v < v1 && first + j < a.vocab ? to_float(row[first + j]) : -INFINITY;
+        for (int i = 0; i < 4; ++i) {
+          uint32_t e[R::kPer];
+#pragma unroll
+          for (int j = 0; j < R::kPer; ++j) {
+            const int at = first + i * R::kPer + j;
+            e[j] = v < v1 && at < a.vocab ? R::word(row + at) : R::kNone;
+          }
+          x[i] = R::kPer == 1 ? e[0] : e[0] | e[R::kPer - 1] << 16;
+        }
+        w[l] = make_uint4(x[0], x[1], x[2], x[3]);
       }
     }
-    float top = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < kHold; ++j) top = fmaxf(top, f[j]);        // of a NaN and a number the number
-    if (top > -INFINITY) {
-      if (top > m) { s *= m > -INFINITY ? exp2f((m - top) * 1.4426950408889634f) : 0.f; m = top; }
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < kHold; ++j) {
-        const float e = exp2f((f[j] - m) * 1.4426950408889634f);        // the difference first: m may be the type's lowest value
-        part[j & 3] += m < INFINITY ? (f[j] > -INFINITY ? e : 0.f) : (f[j] == m ? 1.f : 0.f);
+  };
+  // The best of the elements [e0, e1) that are above `floor` to b.list behind the `have` best so far, one after another, where there are too many to count (equal
+  // ones): the owner of the last one taken looks for its next.  Returns how many there are then.  All threads.
+  auto one_by_one = [&](int e0, int e1, int have, float floor) {
+    uint64_t key = 0;
+    auto next = [&](uint64_t below) {
+      key = 0;
+#pragma unroll 1
+      for (int e = e0 + tid; e < e1; e += kThreads) {
+        const float x = R::value(R::word(row + e), 0);
+        const uint64_t k = x > floor ? (uint64_t)order_of(x) << 32 | (uint32_t)~e : 0ull;
+        if (k < below && k > key) key = k;
       }
-      s += (part[0] + part[1]) + (part[2] + part[3]);
-    }
-    const uint32_t mine = order_of(top);
-    if (!__syncthreads_or(mine > floor_order)) continue;
-    uint32_t bound = floor_order;
-    if (have < a.picks) {
-      const uint32_t low = qth_of_warp(mine, q);
-      if (lane == 0) b.warp_low[warp] = low;
-    }
-    if (tid < have) b.list[tid] = b.ranked[tid];
-    if (tid == 0) b.count = have;
+    };
+    next(~0ull);
     __syncthreads();
-    if (have < a.picks) {
-      uint32_t low = ~0u;
-      for (int w = 0; w < kWarps; ++w) low = min(low, b.warp_low[w]);
-      bound = low == 0 ? 0 : low - 1;
+    int n = have;
+    if (tid < have) b.list[tid] = b.ranked[tid];
+    for (int i = 0; i < a.picks; ++i) {
+      const uint32_t hi = __reduce_max_sync(~0u, (uint32_t)(key >> 32));
+      const uint32_t lo = __reduce_max_sync(~0u, (uint32_t)(key >> 32) == hi ? (uint32_t)key : 0u);
+      if (lane == 0) { b.warp_top[warp] = hi; b.warp_low[warp] = lo; }
+      __syncthreads();
+      uint64_t best = 0;
+      for (int k = 0; k < kWarps; ++k) best = max(best, (uint64_t)b.warp_top[k] << 32 | b.warp_low[k]);
+      if (best == 0) break;
+      if (key == best) { b.list[have + i] = best; next(best); }
+      n = have + i + 1;
+      __syncthreads();
     }
-    if (mine > bound) {
+    __syncthreads();
+    return n;
+  };
+  float m = -INFINITY, s = 0.f;
+  int have = 0;                     // ranked[0 .. have) are the best so far
+  float floor = -INFINITY;          // value of ranked[picks - 1], once there are as many: later elements have to be above it
+  int since = v0;                   // first vector whose candidates are not among these
+  uint4 ahead[kLoads];
+  load(v0, ahead);
+  int k = 1;
+  for (int t0 = v0; t0 < v1; t0 += kThreads * kLoads, ++k) {
+    const int t1 = t0 + kThreads * kLoads;
+    uint32_t w[kWords];
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) { w[4 * l] = ahead[l].x; w[4 * l + 1] = ahead[l].y; w[4 * l + 2] = ahead[l].z; w[4 * l + 3] = ahead[l].w; }
+    if (t1 < v1) load(t1, ahead);
+    uint32_t most = R::kNone | (R::kPer == 2 ? R::kNone << 16 : 0u);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) most = R::most(most, w[i]);
+    float top = R::value(most, 0);
+    if (R::kPer == 2) top = fmaxf(top, R::value(most, 1));
+    if (top > -INFINITY) {
+      if (top > m) { s *= exp2_of((m - top) * kLog2e); m = top; }
+      const float2 shift = make_float2(-m, -m), scale = make_float2(kLog2e, kLog2e);
+      float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+      for (int j = 0; j < kHold; j += 2) {
+        // the difference first: m may be large, up to the type's lowest value
+        const float2 x = mul2(add2(make_float2(R::value(w[j / R::kPer], 0), R::value(w[(j + 1) / R::kPer], R::kPer - 1)), shift), scale);
+        part[j / 2 & 1] = add2(part[j / 2 & 1], make_float2(exp2_of(x.x), exp2_of(x.y)));
+      }
+      part[0] = add2(part[0], part[1]);
+      float sum = part[0].x + part[0].y;
+      if (!(sum < INFINITY)) {      // a NaN among the logits, which does not count, or an infinity, beside which only others do
+        sum = 0.f;
+#pragma unroll 1
+        for (int e = 0; e < kHold; ++e) {
+          const int at = (t0 + (e / V) * kThreads + tid) * V + e % V;
+          const float x = at < min(v1 * V, a.vocab) ? R::value(R::word(row + at), 0) : -INFINITY;
+          sum += x == m ? 1.f : x < m ? exp2_of((x - m) * kLog2e) : 0.f;
+        }
+      }
+      s += sum;
+    }
+    // The first tile finds a bound; those behind it add what is above it, and the bound is raised where the tiles are twice as many as at the last time, when about
+    // as many more as there are places have come together.
+    float least = -INFINITY;
+    if (k == 1) {
+      const uint32_t low = qth_of_warp(order_of(top), q);
+      if (lane == 0) b.warp_low[warp] = low;
+      if (tid == 0) b.count = 0;
+      __syncthreads();
+      uint32_t l = ~0u;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) l = min(l, b.warp_low[i]);
+      if (l) least = value_of(l);
+    }
+    if (top > floor && top >= least) {
 #pragma unroll
       for (int j = 0; j < kHold; ++j) {
-        const uint32_t o = order_of(f[j]);
-        if (o > bound) {
+        const float x = R::value(w[j / R::kPer], j % R::kPer);
+        if (x > floor && x >= least) {
           const int at = atomicAdd(&b.count, 1);
           const uint32_t index = (uint32_t)((t0 + (j / V) * kThreads + tid) * V + j % V);
-          if (at < kList) b.list[at] = (uint64_t)o << 32 | (uint32_t)~index;
+          if (at < kList) b.list[at] = (uint64_t)order_of(x) << 32 | (uint32_t)~index;
         }
       }
     }
+    if ((k & (k - 1)) && t1 < v1) continue;
     __syncthreads();
     int n = b.count;
-    if (n > kList) {
-      // too many to count: the tile's best one after another.  A thread's best key below the last one taken is looked for anew by its owner alone.
-      __syncthreads();
-      uint64_t key = 0;
-      auto next = [&](uint64_t below) {
-        key = 0;
-#pragma unroll
-        for (int j = 0; j < kHold; ++j) {
-          const uint32_t index = (uint32_t)((t0 + (j / V) * kThreads + tid) * V + j % V);
-          const uint32_t o = order_of(f[j]);
-          const uint64_t k = o > floor_order ? (uint64_t)o << 32 | (uint32_t)~index : 0ull;
-          if (k < below && k > key) key = k;
-        }
-      };
-      next(~0ull);
-      n = have;
+    if (n > kList) n = one_by_one(since * V, min(min(t1, v1) * V, a.vocab), have, floor);
+    since = t1;
+    // ranked: how many are above each
+    if (tid < n) {
+      const uint64_t mine = b.list[tid];
+      int above = 0;
+      for (int j = 0; j < n; ++j) above += b.list[j] > mine;
+      if (above < a.picks) b.ranked[above] = mine;
+    }
+    __syncthreads();
+    have = min(n, a.picks);
+    if (have == a.picks) floor = value_of((uint32_t)(b.ranked[have - 1] >> 32));
+    if (t1 < v1) {
       if (tid < have) b.list[tid] = b.ranked[tid];
-      for (int i = 0; i < a.picks; ++i) {
-        const uint32_t hi = __reduce_max_sync(~0u, (uint32_t)(key >> 32));
-        const uint32_t lo = __reduce_max_sync(~0u, (uint32_t)(key >> 32) == hi ? (uint32_t)key : 0u);
-        if (lane == 0) { b.warp_top[warp] = hi; b.warp_low[warp] = lo; }
-        __syncthreads();
-        uint64_t best = 0;
-        for (int w = 0; w < kWarps; ++w) best = max(best, (uint64_t)b.warp_top[w] << 32 | b.warp_low[w]);
-        if (best == 0) break;
-        if (key == best) { b.list[have + i] = best; next(best); }
-        n = have + i + 1;
-        __syncthreads();
-      }
+      if (tid == 0) b.count = have;
       __syncthreads();
     }
-    have = rank(b, n, a.picks);
-    if (have == a.picks) floor_order = (uint32_t)(b.ranked[have - 1] >> 32);
   }
   // the block's sum
   float M = m;
@@ -239,8 +298,9 @@ __global__ void __launch_bounds__(kThreads) beam_scan_kernel(const Args a) {
   for (int o = 16; o > 0; o /= 2) M = fmaxf(M, __shfl_xor_sync(~0u, M, o));
   if (lane == 0) warp_m[warp] = M;
   __syncthreads();
-  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, warp_m[w]);
-  double S = m > -INFINITY ? (m == M ? (double)s : (double)(s * exp2f((m - M) * 1.4426950408889634f))) : 0.0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) M = fmaxf(M, warp_m[i]);
+  double S = m > -INFINITY ? (double)(m == M ? s : s * exp2_of((m - M) * kLog2e)) : 0.0;
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) S += __shfl_xor_sync(~0u, S, o);
   if (lane == 0) warp_s[warp] = S;
@@ -248,12 +308,14 @@ __global__ void __launch_bounds__(kThreads) beam_scan_kernel(const Args a) {
   const long long piece = r * a.pieces + blockIdx.x;
   if (tid == 0) {
     S = 0.0;
-    for (int w = 0; w < kWarps; ++w) S += warp_s[w];
+    for (int i = 0; i < kWarps; ++i) S += warp_s[i];
     a.sums[piece] = S;
     a.tops[piece] = M;
-    a.counts[piece] = have;
   }
-  if (tid < have) a.best[piece * a.picks + tid] = make_uint2(__float_as_uint(value_of((uint32_t)(b.ranked[tid] >> 32))), ~(uint32_t)b.ranked[tid]);
+  if (tid < a.picks) {
+    const uint64_t k = tid < have ? b.ranked[tid] : 0ull;
+    a.best[piece * a.picks + tid] = make_uint2(k ? __float_as_uint(value_of((uint32_t)(k >> 32))) : 0xFF800000u, ~(uint32_t)k);
+  }
 }
 
 // One request: the beams' logarithms, then the best of all candidates: by their totals, and among equal ones by beam, logit (fp64 totals of tiny logits can be equal
@@ -263,142 +325,171 @@ __device__ __forceinline__ uint64_t place_of(int k, float logit, uint32_t token)
 }
 __device__ __forceinline__ int beam_of(uint64_t place) { return kMostBeams - 1 - (int)(place >> 56); }
 __device__ __forceinline__ int token_of(uint64_t place) { return kMostVocab - 1 - (int)(place & (kMostVocab - 1)); }
-__device__ __forceinline__ bool better(double x, uint64_t xp, double y, uint64_t yp) { return x > y || (x == y && xp > yp); }
+struct __align__(16) Candidate { uint64_t total, place; };        // total: its order
+__device__ __forceinline__ bool above(const Candidate& x, const Candidate& y) { return x.total > y.total || (x.total == y.total && x.place > y.place); }
 
 __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
   __shared__ double offset[kMostBeams], most[kMostBeams];      // score - log(sum) and m, of which a logit's total is offset + (logit - m); of a beam that ended, its score
   __shared__ int kind[kMostBeams];                 // 0: no candidates, 1: of its logits, 2: ended, 3: of its logits, the largest of which is +inf
-  __shared__ double list_total[kMostPicks];
-  __shared__ uint64_t list_at[kMostPicks];
-  __shared__ double warp_total[kWarps];
-  __shared__ uint64_t warp_at[kWarps];
+  __shared__ int alive[kMostBeams], n_alive;       // beams of kind 1 to 3
+  __shared__ Candidate list[kList], warp_best[kWarps];
+  __shared__ uint32_t warp_low[kWarps];
+  __shared__ int count;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.beams, P = a.picks;
   const long long r0 = (long long)blockIdx.x * K;
+  if (tid == 0) count = 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   for (int k = warp; k < K; k += kWarps) {
     const float score = a.scores[r0 + k];
-    const bool alive = score > -INFINITY && score < INFINITY;
+    const bool live = score > -INFINITY && score < INFINITY;
     const bool done = a.finished && a.finished[r0 + k];
     float M = -INFINITY;
     double S = 0.0;
-    if (alive && !done) {
-      for (int i = lane; i < a.pieces; i += 32) M = fmaxf(M, a.tops[(r0 + k) * a.pieces + i]);
+    if (live && !done) {
+      const long long at = (r0 + k) * a.pieces;
+      const float m0 = lane < a.pieces ? a.tops[at + lane] : -INFINITY, m1 = lane + 32 < a.pieces ? a.tops[at + lane + 32] : -INFINITY;
+      const double s0 = lane < a.pieces ? a.sums[at + lane] : 0.0, s1 = lane + 32 < a.pieces ? a.sums[at + lane + 32] : 0.0;
+      M = fmaxf(m0, m1);
 #pragma unroll
       for (int o = 16; o > 0; o /= 2) M = fmaxf(M, __shfl_xor_sync(~0u, M, o));
-      for (int i = lane; i < a.pieces; i += 32) {
-        const float m = a.tops[(r0 + k) * a.pieces + i];
-        if (m > -INFINITY) S += a.sums[(r0 + k) * a.pieces + i] * (m == M ? 1.0 : exp((double)m - (double)M));
-      }
+      if (m0 > -INFINITY) S += s0 * (m0 == M ? 1.0 : exp((double)m0 - (double)M));
+      if (m1 > -INFINITY) S += s1 * (m1 == M ? 1.0 : exp((double)m1 - (double)M));
 #pragma unroll
       for (int o = 16; o > 0; o /= 2) S += __shfl_xor_sync(~0u, S, o);
     }
     if (lane == 0) {
-      kind[k] = !alive ? 0 : done ? 2 : M == INFINITY ? 3 : M > -INFINITY ? 1 : 0;
-      offset[k] = !alive ? 0.0 : done ? (double)score : M > -INFINITY ? (double)score - log(S) : 0.0;
+      kind[k] = !live ? 0 : done ? 2 : M == INFINITY ? 3 : M > -INFINITY ? 1 : 0;
+      offset[k] = !live ? 0.0 : done ? (double)score : M > -INFINITY ? (double)score - log(S) : 0.0;
       most[k] = (double)M;
     }
   }
   __syncthreads();
-  // candidate c: piece c / P, place c % P of beam c / (pieces * P)
-  const int each = a.pieces * P, all = K * each;
-  auto candidate = [&](int c, double& total, uint64_t& at) {
-    const int k = c / each, i = c - k * each;
+  if (warp == 0) {
+    const bool x = lane < K && kind[lane], y = lane + 32 < K && kind[lane + 32];
+    const uint32_t bx = __ballot_sync(~0u, x), by = __ballot_sync(~0u, y), low = (1u << lane) - 1;
+    if (x) alive[__popc(bx & low)] = lane;
+    if (y) alive[__popc(bx) + __popc(by & low)] = lane + 32;
+    if (lane == 0) n_alive = __popc(bx) + __popc(by);
+  }
+  __syncthreads();
+  // candidate c of all: place c % (pieces * P) of the c / (pieces * P)-th beam that has any
+  const int each = a.pieces * P, all = n_alive * each;
+  auto candidate = [&](int c, Candidate& x) {
+    const int l = c / each, i = c - l * each, k = alive[l];
     if (kind[k] == 2) {
-      total = offset[k]; at = place_of(k, 0.f, (uint32_t)a.eos);
+      x.total = order_of(offset[k]); x.place = place_of(k, 0.f, (uint32_t)a.eos);
       return i == 0;
     }
-    if (kind[k] == 0) return false;
-    const long long piece = (r0 + k) * a.pieces + i / P;
-    if (i % P >= a.counts[piece]) return false;
-    const uint2 b = a.best[piece * P + i % P];
-    const float l = __uint_as_float(b.x);
-    if (kind[k] == 3 && l < INFINITY) return false;
-    total = kind[k] == 3 ? offset[k] : offset[k] + ((double)l - most[k]);
-    at = place_of(k, l, b.y);
+    const uint2 b = a.best[(r0 + k) * each + i];
+    const float v = __uint_as_float(b.x);
+    if (kind[k] == 3 ? v < INFINITY : v == -INFINITY) return false;
+    x.total = order_of(kind[k] == 3 ? offset[k] : offset[k] + ((double)v - most[k])); x.place = place_of(k, v, b.y);
     return true;
   };
-  double last = INFINITY;
-  uint64_t last_at = 0;
-  bool first = true;
-  int n = 0;
-  double mine = -INFINITY;
-  uint64_t mine_at = 0;
-  bool some = false;
-  auto look = [&]() {
-    some = false;
-    for (int c = tid; c < all; c += kThreads) {
-      double t;
-      uint64_t at;
-      if (candidate(c, t, at) && (first || better(last, last_at, t, at)) && (!some || better(t, at, mine, mine_at))) { mine = t; mine_at = at; some = true; }
-    }
-    if (!some) { mine = -INFINITY; mine_at = 0; }
-  };
-  look();
-  first = false;
-  for (; n < P; ++n) {
-    double t = mine;
-    uint64_t at = mine_at;
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) {
-      const double ot = __shfl_xor_sync(~0u, t, o);
-      const uint64_t oat = __shfl_xor_sync(~0u, at, o);
-      if (better(ot, oat, t, at)) { t = ot; at = oat; }
-    }
-    if (lane == 0) { warp_total[warp] = t; warp_at[warp] = at; }
+  // As in a piece: a warp's q-th best are passed by q candidates, those of all warps by enough.  By the total rounded to fp32, which keeps the order.
+  // Each warp takes its candidates from all lists alike: neighbouring ones, of one list, go to different warps.
+  const int full = min(kWarps, all / 32), q = full > 0 ? (P + full - 1) / full : 33;
+  uint32_t bound = 0;
+  if (q <= 32) {
+    uint32_t top = 0;
+    if (warp < full)
+      for (int c = lane * full + warp; c < all; c += 32 * full) {
+        Candidate x;
+        if (candidate(c, x)) top = max(top, order_of((float)value_of(x.total)));
+      }
+    const uint32_t low = qth_of_warp(top, q);
+    if (lane == 0) warp_low[warp] = low;
     __syncthreads();
-    t = warp_total[0]; at = warp_at[0];
-    for (int w = 1; w < kWarps; ++w)
-      if (better(warp_total[w], warp_at[w], t, at)) { t = warp_total[w]; at = warp_at[w]; }
-    if (at == 0) break;
-    last = t; last_at = at;
-    if (some && mine_at == at) look();
-    if (tid == 0) { list_total[n] = t; list_at[n] = at; }
-    __syncthreads();
+    bound = ~0u;
+    for (int i = 0; i < full; ++i) bound = min(bound, warp_low[i]);
+  }
+  for (int c = tid; c < all; c += kThreads) {
+    Candidate x;
+    if (candidate(c, x) && order_of((float)value_of(x.total)) >= bound) {
+      const int at = atomicAdd(&count, 1);
+      if (at < kList) list[at] = x;
+    }
   }
   __syncthreads();
-  // fewer candidates than places: what is left has probability zero, lowest beam and token first
-  if (tid == 0 && n < P) {
-    const int found = n;
+  int n = count;
+  if (n > kList) {
+    // too many to count (equal ones): one after another
+    __syncthreads();
+    Candidate mine, last = {~0ull, ~0ull};
+    auto next = [&]() {
+      mine = Candidate{0, 0};
+      for (int c = tid; c < all; c += kThreads) {
+        Candidate x;
+        if (candidate(c, x) && above(last, x) && above(x, mine)) mine = x;
+      }
+    };
+    next();
+    for (n = 0; n < P; ++n) {
+      Candidate x = mine;
+#pragma unroll
+      for (int o = 16; o > 0; o /= 2) {
+        const Candidate y = {__shfl_xor_sync(~0u, x.total, o), __shfl_xor_sync(~0u, x.place, o)};
+        if (above(y, x)) x = y;
+      }
+      if (lane == 0) warp_best[warp] = x;
+      __syncthreads();
+      x = warp_best[0];
+      for (int i = 1; i < kWarps; ++i)
+        if (above(warp_best[i], x)) x = warp_best[i];
+      if (x.place == 0) break;
+      const bool taken = mine.place == x.place && mine.total == x.total;
+      last = x;
+      if (taken) next();
+      if (tid == 0) list[n] = x;
+      __syncthreads();
+    }
+    __syncthreads();
+  }
+  auto put = [&](int i, float total, int k, int v) {
+    const long long o = (long long)blockIdx.x * P + i;
+    a.next_scores[o] = total;
+    a.parents[o] = k;
+    a.tokens[o] = v;
+    if (a.finished_out) a.finished_out[o] = (a.finished && a.finished[r0 + k]) || v == a.eos;
+  };
+  if (tid < n) {
+    const Candidate mine = list[tid];
+    int better = 0;
+    for (int j = 0; j < n; ++j) better += above(list[j], mine);
+    if (better < P) put(better, (float)value_of(mine.total), beam_of(mine.place), token_of(mine.place));
+  }
+  if (n < P && tid >= n && tid < P) {
+    // fewer candidates than places (all of them in the list): what is left has probability zero, lowest beam and token first
     int k = 0, v = 0;
-    for (int i = found; i < P;) {
+    for (int skip = tid - n;; ) {
       bool taken = false;
-      for (int j = 0; j < found; ++j) taken |= beam_of(list_at[j]) == k && token_of(list_at[j]) == v;
-      if (!taken) { list_total[i] = -INFINITY; list_at[i] = place_of(k, 0.f, (uint32_t)v); ++i; }
+      for (int j = 0; j < n; ++j) taken |= beam_of(list[j].place) == k && token_of(list[j].place) == v;
+      if (!taken && skip-- == 0) break;
       if (++v == a.vocab) { v = 0; ++k; }
     }
-  }
-  __syncthreads();
-  if (tid < P) {
-    const long long o = (long long)blockIdx.x * P + tid;
-    const int parent = beam_of(list_at[tid]), token = token_of(list_at[tid]);
-    a.next_scores[o] = (float)list_total[tid];
-    a.parents[o] = parent;
-    a.tokens[o] = token;
-    if (a.finished_out) a.finished_out[o] = (a.finished && a.finished[r0 + parent]) || token == a.eos;
+    put(tid, -INFINITY, k, v);
   }
 }
 
 // Pieces of a row: as many blocks as the SMs hold at once, but no piece so short that a block has less than a tile's share of work.
-struct Plan { int pieces, piece_vecs; size_t bytes, off_tops, off_counts, off_best; };
+struct Plan { int pieces; size_t bytes, off_tops, off_best; };
 Plan plan_of(int requests, int beams, int vocab, int picks) {
   Plan p;
   const long long rows = (long long)requests * beams;
   const int least = 2048;
   const long long want = std::max<long long>(1, 4ll * sm_count() / rows);
   p.pieces = (int)std::min<long long>({want, (vocab + least - 1) / least, kMostPieces});
-  p.piece_vecs = 0;
   // rows * pieces is at most either of these, and both grow with the sizes: what is enough for a call is enough for smaller ones
   const size_t n = (size_t)std::min(std::max<long long>(rows, 4ll * sm_count()), rows * std::min(kMostPieces, (vocab + least - 1) / least));
   p.off_tops = n * 8;
-  p.off_counts = p.off_tops + n * 4;
-  p.off_best = round_up_sz(p.off_counts + n * 4, 16);
+  p.off_best = round_up_sz(p.off_tops + n * 4, 16);
   p.bytes = p.off_best + n * picks * 8;
   return p;
 }
 
 template <typename T>
 cudaError_t launch(Args a, cudaStream_t s) {
-  const int V = Raw<T>::kVec;
+  const int V = 4 * Raw<T>::kPer;
   a.piece_vecs = ((a.vocab + V - 1) / V + a.pieces - 1) / a.pieces;
   beam_scan_kernel<T><<<dim3((unsigned)a.pieces, (unsigned)(a.requests * a.beams)), kThreads, 0, s>>>(a);
   cudaError_t e = cudaGetLastError();
@@ -453,7 +544,6 @@ rwkvq_status rwkvq_beam_select(const rwkvq_beam_select_args* args, void* workspa
   uint8_t* w = static_cast<uint8_t*>(workspace);
   a.sums = reinterpret_cast<double*>(w);
   a.tops = reinterpret_cast<float*>(w + l.off_tops);
-  a.counts = reinterpret_cast<int*>(w + l.off_counts);
   a.best = reinterpret_cast<uint2*>(w + l.off_best);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (g.dtype == RWKVQ_F32) return cuda_status(bs::launch<float>(a, s));

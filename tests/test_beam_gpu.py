@@ -121,6 +121,14 @@ def test_ties_go_to_the_lowest(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+def test_both_zeros_are_one(dtype):
+    logits = torch.zeros((2, 700))
+    logits[:, ::2] = -0.0
+    ns, pa, to, _ = select(logits.to(TYPES[dtype]), torch.tensor([[-0.0, 0.0]]), 9)
+    assert pa.tolist() == [[0] * 9] and to.tolist() == [list(range(9))]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("low", ["inf", "least"])
 def test_masks(dtype, low):
     low = -math.inf if low == "inf" else torch.finfo(TYPES[dtype]).min
