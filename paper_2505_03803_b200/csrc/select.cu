@@ -159,18 +159,14 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const Args a) {
       } else if (skew != 0 && v < v1 && v > 0 && first + 2 * V <= a.vocab) {
         w[l] = joined(__ldg(vecs + v), __ldg(vecs + v + 1), skew);
       } else {
-        uint32_t x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t e[R::kPer];
-#pragma unroll
-          for (int j = 0; j < R::kPer; ++j) {
-            const int at = first + i * R::kPer + j;
-            e[j] = v < v1 && at < a.vocab ? R::word(row + at) : R::kNone;
-          }
-          x[i] = R::kPer == 1 ? e[0] : e[0] | e[R::kPer - 1] << 16;
+        uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+        for (int j = V - 1; j >= 0; --j) {
+          constexpr int kBits = 32 / R::kPer;
+          hi = hi << kBits | lo >> (64 - kBits);
+          lo = lo << kBits | (v < v1 && first + j < a.vocab ? R::word(row + first + j) : R::kNone);
         }
-        w[l] = make_uint4(x[0], x[1], x[2], x[3]);
+        w[l] = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
       }
     }
   };
@@ -210,20 +206,23 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const Args a) {
   int have = 0;                     // ranked[0 .. have) are the best so far
   float floor = -INFINITY;          // value of ranked[picks - 1], once there are as many: later elements have to be above it
   int since = v0;                   // first vector whose candidates are not among these
-  uint4 ahead[kLoads];
-  load(v0, ahead);
-  int k = 1;
-  for (int t0 = v0; t0 < v1; t0 += kThreads * kLoads, ++k) {
+  uint4 ahead[kLoads] = {};
+  int k = 0;                        // tiles so far
+  for (int t0 = v0 - kThreads * kLoads; t0 < v1; t0 += kThreads * kLoads, ++k) {
     const int t1 = t0 + kThreads * kLoads;
     uint32_t w[kWords];
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) { w[4 * l] = ahead[l].x; w[4 * l + 1] = ahead[l].y; w[4 * l + 2] = ahead[l].z; w[4 * l + 3] = ahead[l].w; }
     if (t1 < v1) load(t1, ahead);
-    uint32_t most = R::kNone | (R::kPer == 2 ? R::kNone << 16 : 0u);
+    if (k == 0) continue;
+    uint32_t most[kLoads];
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) most = R::most(most, w[i]);
-    float top = R::value(most, 0);
-    if (R::kPer == 2) top = fmaxf(top, R::value(most, 1));
+    for (int l = 0; l < kLoads; ++l) most[l] = R::most(R::most(w[4 * l], w[4 * l + 1]), R::most(w[4 * l + 2], w[4 * l + 3]));
+    float top = -INFINITY;
+    {
+      const uint32_t x = R::most(R::most(most[0], most[1]), R::most(most[2], most[3]));
+      top = fmaxf(top, fmaxf(R::value(x, 0), R::value(x, R::kPer - 1)));
+    }
     if (top > -INFINITY) {
       if (top > m) { s *= exp2_of((m - top) * kLog2e); m = top; }
       const float2 shift = make_float2(-m, -m), scale = make_float2(kLog2e, kLog2e);
@@ -262,12 +261,17 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const Args a) {
     }
     if (top > floor && top >= least) {
 #pragma unroll
-      for (int j = 0; j < kHold; ++j) {
-        const float x = R::value(w[j / R::kPer], j % R::kPer);
-        if (x > floor && x >= least) {
-          const int at = atomicAdd(&b.count, 1);
-          const uint32_t index = (uint32_t)((t0 + (j / V) * kThreads + tid) * V + j % V);
-          if (at < kList) b.list[at] = (uint64_t)order_of(x) << 32 | (uint32_t)~index;
+      for (int l = 0; l < kLoads; ++l) {
+        const float here = fmaxf(R::value(most[l], 0), R::value(most[l], R::kPer - 1));
+        if (!(here > floor && here >= least)) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float x = R::value(w[4 * l + j / R::kPer], j % R::kPer);
+          if (x > floor && x >= least) {
+            const int at = atomicAdd(&b.count, 1);
+            const uint32_t index = (uint32_t)((t0 + l * kThreads + tid) * V + j);
+            if (at < kList) b.list[at] = (uint64_t)order_of(x) << 32 | (uint32_t)~index;
+          }
         }
       }
     }
@@ -337,39 +341,42 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
   __shared__ int count;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.beams, P = a.picks;
   const long long r0 = (long long)blockIdx.x * K;
-  if (tid == 0) count = 0;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (int k = warp; k < K; k += kWarps) {
-    const float score = a.scores[r0 + k];
-    const bool live = score > -INFINITY && score < INFINITY;
-    const bool done = a.finished && a.finished[r0 + k];
-    float M = -INFINITY;
-    double S = 0.0;
-    if (live && !done) {
-      const long long at = (r0 + k) * a.pieces;
-      const float m0 = lane < a.pieces ? a.tops[at + lane] : -INFINITY, m1 = lane + 32 < a.pieces ? a.tops[at + lane + 32] : -INFINITY;
-      const double s0 = lane < a.pieces ? a.sums[at + lane] : 0.0, s1 = lane + 32 < a.pieces ? a.sums[at + lane + 32] : 0.0;
-      M = fmaxf(m0, m1);
+  // what the beams are is known before the scan, which nothing in front of it overlaps with, is done
+  if (warp == 0) {
+    int kinds[2];
 #pragma unroll
-      for (int o = 16; o > 0; o /= 2) M = fmaxf(M, __shfl_xor_sync(~0u, M, o));
-      if (m0 > -INFINITY) S += s0 * (m0 == M ? 1.0 : exp((double)m0 - (double)M));
-      if (m1 > -INFINITY) S += s1 * (m1 == M ? 1.0 : exp((double)m1 - (double)M));
-#pragma unroll
-      for (int o = 16; o > 0; o /= 2) S += __shfl_xor_sync(~0u, S, o);
+    for (int h = 0; h < 2; ++h) {
+      const int k = lane + 32 * h;
+      const float score = k < K ? a.scores[r0 + k] : INFINITY;
+      kinds[h] = !(score > -INFINITY && score < INFINITY) ? 0 : a.finished && a.finished[r0 + k] ? 2 : 1;
+      if (k < K) { kind[k] = kinds[h]; offset[k] = (double)score; }
     }
-    if (lane == 0) {
-      kind[k] = !live ? 0 : done ? 2 : M == INFINITY ? 3 : M > -INFINITY ? 1 : 0;
-      offset[k] = !live ? 0.0 : done ? (double)score : M > -INFINITY ? (double)score - log(S) : 0.0;
-      most[k] = (double)M;
-    }
+    const uint32_t bx = __ballot_sync(~0u, kinds[0]), by = __ballot_sync(~0u, kinds[1]), low = (1u << lane) - 1;
+    if (kinds[0]) alive[__popc(bx & low)] = lane;
+    if (kinds[1]) alive[__popc(bx) + __popc(by & low)] = lane + 32;
+    if (lane == 0) { n_alive = __popc(bx) + __popc(by); count = 0; }
   }
   __syncthreads();
-  if (warp == 0) {
-    const bool x = lane < K && kind[lane], y = lane + 32 < K && kind[lane + 32];
-    const uint32_t bx = __ballot_sync(~0u, x), by = __ballot_sync(~0u, y), low = (1u << lane) - 1;
-    if (x) alive[__popc(bx & low)] = lane;
-    if (y) alive[__popc(bx) + __popc(by & low)] = lane + 32;
-    if (lane == 0) n_alive = __popc(bx) + __popc(by);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  for (int l = warp; l < n_alive; l += kWarps) {
+    const int k = alive[l];
+    if (kind[k] != 1) continue;
+    const long long at = (r0 + k) * a.pieces;
+    const float m0 = lane < a.pieces ? a.tops[at + lane] : -INFINITY, m1 = lane + 32 < a.pieces ? a.tops[at + lane + 32] : -INFINITY;
+    const double s0 = lane < a.pieces ? a.sums[at + lane] : 0.0, s1 = lane + 32 < a.pieces ? a.sums[at + lane + 32] : 0.0;
+    float M = fmaxf(m0, m1);
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) M = fmaxf(M, __shfl_xor_sync(~0u, M, o));
+    double S = 0.0;
+    if (m0 > -INFINITY) S += m0 == M ? s0 : s0 * (double)exp2_of((m0 - M) * kLog2e);
+    if (m1 > -INFINITY) S += m1 == M ? s1 : s1 * (double)exp2_of((m1 - M) * kLog2e);
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) S += __shfl_xor_sync(~0u, S, o);
+    if (lane == 0) {
+      if (M == INFINITY) kind[k] = 3;
+      if (M > -INFINITY) offset[k] -= log(S);
+      most[k] = (double)M;
+    }
   }
   __syncthreads();
   // candidate c of all: place c % (pieces * P) of the c / (pieces * P)-th beam that has any
