@@ -131,7 +131,7 @@ struct Best {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const Args a) {
+__global__ void __launch_bounds__(kThreads, 4) beam_scan_kernel(const Args a) {
   using R = Raw<T>;
   constexpr int kWords = 4 * kLoads, kHold = kWords * R::kPer, V = 4 * R::kPer;
   __shared__ Best b;
@@ -208,6 +208,8 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const Args a) {
   int since = v0;                   // first vector whose candidates are not among these
   uint4 ahead[kLoads] = {};
   int k = 0;                        // tiles so far
+  int raise = 1;                    // when the bound is raised
+  const int spread = max(2, 64 / a.picks);
   for (int t0 = v0 - kThreads * kLoads; t0 < v1; t0 += kThreads * kLoads, ++k) {
     const int t1 = t0 + kThreads * kLoads;
     uint32_t w[kWords];
@@ -246,8 +248,8 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const Args a) {
       }
       s += sum;
     }
-    // The first tile finds a bound; those behind it add what is above it, and the bound is raised where the tiles are twice as many as at the last time, when about
-    // as many more as there are places have come together.
+    // The first tile finds a bound; those behind it add what is above it, and the bound is raised where the tiles are `spread` times as many as at the last time, when
+    // about as many times the places have come together.
     float least = -INFINITY;
     if (k == 1) {
       const uint32_t low = qth_of_warp(order_of(top), q);
@@ -275,7 +277,8 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const Args a) {
         }
       }
     }
-    if ((k & (k - 1)) && t1 < v1) continue;
+    if (k < raise && t1 < v1) continue;
+    raise = k * spread;
     __syncthreads();
     int n = b.count;
     if (n > kList) n = one_by_one(since * V, min(min(t1, v1) * V, a.vocab), have, floor);
