@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_scan_kernel(const Args a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long r = blockIdx.y;
   const float score = a.scores[r];
-  if (!(score > -INFINITY && score < INFINITY) || (a.finished && a.finished[r])) return;      // its candidates do not come from its logits
+  const bool ended = a.finished && a.finished[r];
   const T* row = static_cast<const T*>(a.logits) + r * a.row;
   // Vectors of 16 bytes' elements, counted from the row's first, wherever that lies: rows with the same logits have the same sum to the last bit, and their beams tie.
   // A row that begins `skew` bytes behind a boundary of 16 has its vectors put together from two aligned ones.
@@ -216,7 +216,10 @@ __global__ void __launch_bounds__(kThreads, 4) beam_scan_kernel(const Args a) {
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) { w[4 * l] = ahead[l].x; w[4 * l + 1] = ahead[l].y; w[4 * l + 2] = ahead[l].z; w[4 * l + 3] = ahead[l].w; }
     if (t1 < v1) load(t1, ahead);
-    if (k == 0) continue;
+    if (k == 0) {
+      if (!(score > -INFINITY && score < INFINITY) || ended) return;      // its candidates do not come from its logits
+      continue;
+    }
     uint32_t most[kLoads];
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) most[l] = R::most(R::most(w[4 * l], w[4 * l + 1]), R::most(w[4 * l + 2], w[4 * l + 3]));
@@ -283,12 +286,16 @@ __global__ void __launch_bounds__(kThreads, 4) beam_scan_kernel(const Args a) {
     int n = b.count;
     if (n > kList) n = one_by_one(since * V, min(min(t1, v1) * V, a.vocab), have, floor);
     since = t1;
-    // ranked: how many are above each
-    if (tid < n) {
-      const uint64_t mine = b.list[tid];
+    // ranked: how many are above each, counted by four threads
+    for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+      const int i = i0 + tid / 4;
+      const uint64_t mine = b.list[min(i, n - 1)];
       int above = 0;
-      for (int j = 0; j < n; ++j) above += b.list[j] > mine;
-      if (above < a.picks) b.ranked[above] = mine;
+#pragma unroll 4
+      for (int j = tid & 3; j < n; j += 4) above += b.list[j] > mine ? 1 : 0;
+      above += __shfl_xor_sync(~0u, above, 1);
+      above += __shfl_xor_sync(~0u, above, 2);
+      if (i < n && above < a.picks && (tid & 3) == 0) b.ranked[above] = mine;
     }
     __syncthreads();
     have = min(n, a.picks);
@@ -333,9 +340,10 @@ __device__ __forceinline__ uint64_t place_of(int k, float logit, uint32_t token)
 __device__ __forceinline__ int beam_of(uint64_t place) { return kMostBeams - 1 - (int)(place >> 56); }
 __device__ __forceinline__ int token_of(uint64_t place) { return kMostVocab - 1 - (int)(place & (kMostVocab - 1)); }
 struct __align__(16) Candidate { uint64_t total, place; };        // total: its order
-__device__ __forceinline__ bool above(const Candidate& x, const Candidate& y) { return x.total > y.total || (x.total == y.total && x.place > y.place); }
+__device__ __forceinline__ bool above(const Candidate& x, const Candidate& y) { return (x.total > y.total) | ((x.total == y.total) & (x.place > y.place)); }
 
 __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
+  constexpr int kHeld = 2;                         // candidates that a thread keeps; those behind them are made anew where they are needed
   __shared__ double offset[kMostBeams], most[kMostBeams];      // score - log(sum) and m, of which a logit's total is offset + (logit - m); of a beam that ended, its score
   __shared__ int kind[kMostBeams];                 // 0: no candidates, 1: of its logits, 2: ended, 3: of its logits, the largest of which is +inf
   __shared__ int alive[kMostBeams], n_alive;       // beams of kind 1 to 3
@@ -360,65 +368,86 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
     if (lane == 0) { n_alive = __popc(bx) + __popc(by); count = 0; }
   }
   __syncthreads();
+  // Candidate c of all: place c % (pieces * P) of the c / (pieces * P)-th beam that has any.  Each warp takes its candidates from all lists alike: neighbouring ones,
+  // of one list, go to different warps; `full` warps have something for each lane.
+  const int each = a.pieces * P, all = n_alive * each, full = max(1, min(kWarps, all / 32)), step = 32 * full;
+  const int c0 = warp < full ? lane * full + warp : all;
+  auto fetch = [&](int c, int& k) {
+    const int l = c / each;
+    k = alive[l];
+    return kind[k] == 2 ? make_uint2(0u, c - l * each) : a.best[(r0 + k) * each + (c - l * each)];
+  };
+  auto candidate = [&](int k, const uint2& b, Candidate& x) {
+    if (kind[k] == 2) {
+      x.total = order_of(offset[k]); x.place = place_of(k, 0.f, (uint32_t)a.eos);
+      return b.y == 0;
+    }
+    const float v = __uint_as_float(b.x);
+    x.total = order_of(kind[k] == 3 ? offset[k] : offset[k] + ((double)v - most[k])); x.place = place_of(k, v, b.y);
+    return kind[k] == 3 ? v == INFINITY : v > -INFINITY;
+  };
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  uint2 held[kHeld];
+  int held_k[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (c0 + i * step < all) held[i] = fetch(c0 + i * step, held_k[i]);
   for (int l = warp; l < n_alive; l += kWarps) {
     const int k = alive[l];
     if (kind[k] != 1) continue;
     const long long at = (r0 + k) * a.pieces;
     const float m0 = lane < a.pieces ? a.tops[at + lane] : -INFINITY, m1 = lane + 32 < a.pieces ? a.tops[at + lane + 32] : -INFINITY;
     const double s0 = lane < a.pieces ? a.sums[at + lane] : 0.0, s1 = lane + 32 < a.pieces ? a.sums[at + lane + 32] : 0.0;
-    float M = fmaxf(m0, m1);
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) M = fmaxf(M, __shfl_xor_sync(~0u, M, o));
+    const float M = value_of(max(__reduce_max_sync(~0u, order_of(m0)), __reduce_max_sync(~0u, order_of(m1))));
+    const bool some = __any_sync(~0u, m0 > -INFINITY || m1 > -INFINITY);
     double S = 0.0;
     if (m0 > -INFINITY) S += m0 == M ? s0 : s0 * (double)exp2_of((m0 - M) * kLog2e);
     if (m1 > -INFINITY) S += m1 == M ? s1 : s1 * (double)exp2_of((m1 - M) * kLog2e);
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) S += __shfl_xor_sync(~0u, S, o);
-    if (lane == 0) {
-      if (M == INFINITY) kind[k] = 3;
-      if (M > -INFINITY) offset[k] -= log(S);
+    if (lane == 0 && some) {
+      offset[k] -= log(S);
       most[k] = (double)M;
+      if (M == INFINITY) kind[k] = 3;
     }
   }
   __syncthreads();
-  // candidate c of all: place c % (pieces * P) of the c / (pieces * P)-th beam that has any
-  const int each = a.pieces * P, all = n_alive * each;
-  auto candidate = [&](int c, Candidate& x) {
-    const int l = c / each, i = c - l * each, k = alive[l];
-    if (kind[k] == 2) {
-      x.total = order_of(offset[k]); x.place = place_of(k, 0.f, (uint32_t)a.eos);
-      return i == 0;
-    }
-    const uint2 b = a.best[(r0 + k) * each + i];
-    const float v = __uint_as_float(b.x);
-    if (kind[k] == 3 ? v < INFINITY : v == -INFINITY) return false;
-    x.total = order_of(kind[k] == 3 ? offset[k] : offset[k] + ((double)v - most[k])); x.place = place_of(k, v, b.y);
-    return true;
-  };
-  // As in a piece: a warp's q-th best are passed by q candidates, those of all warps by enough.  By the total rounded to fp32, which keeps the order.
-  // Each warp takes its candidates from all lists alike: neighbouring ones, of one list, go to different warps.
-  const int full = min(kWarps, all / 32), q = full > 0 ? (P + full - 1) / full : 33;
-  uint32_t bound = 0;
-  if (q <= 32) {
-    uint32_t top = 0;
-    if (warp < full)
-      for (int c = lane * full + warp; c < all; c += 32 * full) {
-        Candidate x;
-        if (candidate(c, x)) top = max(top, order_of((float)value_of(x.total)));
-      }
+  // As in a piece: a warp's q-th best are passed by q candidates, those of all full warps by enough.  By the total rounded to fp32, which keeps the order.
+  Candidate x[kHeld];
+  uint32_t order[kHeld], top = 0, bound = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    order[i] = c0 + i * step < all && candidate(held_k[i], held[i], x[i]) ? order_of((float)value_of(x[i].total)) : 0u;
+    top = max(top, order[i]);
+  }
+#pragma unroll 1
+  for (int c = c0 + kHeld * step; c < all; c += step) {
+    Candidate y;
+    int k;
+    const uint2 b = fetch(c, k);
+    if (candidate(k, b, y)) top = max(top, order_of((float)value_of(y.total)));
+  }
+  const int q = (P + full - 1) / full;
+  if (q <= 32 && all >= 32) {
     const uint32_t low = qth_of_warp(top, q);
     if (lane == 0) warp_low[warp] = low;
     __syncthreads();
     bound = ~0u;
     for (int i = 0; i < full; ++i) bound = min(bound, warp_low[i]);
   }
-  for (int c = tid; c < all; c += kThreads) {
-    Candidate x;
-    if (candidate(c, x) && order_of((float)value_of(x.total)) >= bound) {
-      const int at = atomicAdd(&count, 1);
-      if (at < kList) list[at] = x;
-    }
+  auto keep = [&](const Candidate& y) {
+    const int at = atomicAdd(&count, 1);
+    if (at < kList) list[at] = y;
+  };
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (order[i] && order[i] >= bound) keep(x[i]);
+#pragma unroll 1
+  for (int c = c0 + kHeld * step; c < all; c += step) {
+    Candidate y;
+    int k;
+    const uint2 b = fetch(c, k);
+    if (candidate(k, b, y) && order_of((float)value_of(y.total)) >= bound) keep(y);
   }
   __syncthreads();
   int n = count;
@@ -428,29 +457,32 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
     Candidate mine, last = {~0ull, ~0ull};
     auto next = [&]() {
       mine = Candidate{0, 0};
-      for (int c = tid; c < all; c += kThreads) {
-        Candidate x;
-        if (candidate(c, x) && above(last, x) && above(x, mine)) mine = x;
+#pragma unroll 1
+      for (int c = c0; c < all; c += step) {
+        Candidate y;
+        int k;
+        const uint2 b = fetch(c, k);
+        if (candidate(k, b, y) && above(last, y) && above(y, mine)) mine = y;
       }
     };
     next();
     for (n = 0; n < P; ++n) {
-      Candidate x = mine;
+      Candidate y = mine;
 #pragma unroll
       for (int o = 16; o > 0; o /= 2) {
-        const Candidate y = {__shfl_xor_sync(~0u, x.total, o), __shfl_xor_sync(~0u, x.place, o)};
-        if (above(y, x)) x = y;
+        const Candidate z = {__shfl_xor_sync(~0u, y.total, o), __shfl_xor_sync(~0u, y.place, o)};
+        if (above(z, y)) y = z;
       }
-      if (lane == 0) warp_best[warp] = x;
+      if (lane == 0) warp_best[warp] = y;
       __syncthreads();
-      x = warp_best[0];
+      y = warp_best[0];
       for (int i = 1; i < kWarps; ++i)
-        if (above(warp_best[i], x)) x = warp_best[i];
-      if (x.place == 0) break;
-      const bool taken = mine.place == x.place && mine.total == x.total;
-      last = x;
+        if (above(warp_best[i], y)) y = warp_best[i];
+      if (y.place == 0) break;
+      const bool taken = mine.place == y.place && mine.total == y.total;
+      last = y;
       if (taken) next();
-      if (tid == 0) list[n] = x;
+      if (tid == 0) list[n] = y;
       __syncthreads();
     }
     __syncthreads();
@@ -462,11 +494,15 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
     a.tokens[o] = v;
     if (a.finished_out) a.finished_out[o] = (a.finished && a.finished[r0 + k]) || v == a.eos;
   };
-  if (tid < n) {
-    const Candidate mine = list[tid];
+  for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+    const int i = i0 + tid / 4;
+    const Candidate mine = list[min(i, n - 1)];
     int better = 0;
-    for (int j = 0; j < n; ++j) better += above(list[j], mine);
-    if (better < P) put(better, (float)value_of(mine.total), beam_of(mine.place), token_of(mine.place));
+#pragma unroll 4
+    for (int j = tid & 3; j < n; j += 4) better += above(list[j], mine) ? 1 : 0;
+    better += __shfl_xor_sync(~0u, better, 1);
+    better += __shfl_xor_sync(~0u, better, 2);
+    if (i < n && better < P && (tid & 3) == 0) put(better, (float)value_of(mine.total), beam_of(mine.place), token_of(mine.place));
   }
   if (n < P && tid >= n && tid < P) {
     // fewer candidates than places (all of them in the list): what is left has probability zero, lowest beam and token first
