@@ -25,7 +25,7 @@ namespace rwkvq {
 int* device_status_ptr();  // api_misc.cu
 namespace lr {
 
-constexpr int kThreads = 256, kWarps = 8, kRows = 16, kMostRank = 128, kMostCols = 512;
+constexpr int kThreads = 256, kWarps = 8, kRows = 16, kMostRank = 128, kMostCols = 512, kMostCounted = 1024;
 
 struct Args {
   rwkvq_lowrank_args a;
@@ -40,6 +40,7 @@ struct Args {
 struct Tile {
   int rows[kRows], seqs[kRows];       // seqs: of a row that is its sequence's first, else -1 - sequence
   int n, adapter, rank;
+  float scale;
 };
 
 // The sequence and tile of `item` among all tiles of sixteen rows of the sequences in seq_start, or n = 0.  A sequence counts whose rows exist and that
@@ -93,37 +94,53 @@ __device__ void find_in_list(const Args& p, long long item, int& seq, int& first
   __syncthreads();
 }
 
-__device__ void find_tile(const Args& p, long long item, Tile& t, int* scratch) {
+__host__ __device__ inline bool by_groups(const rwkvq_lowrank_args& a) { return a.n_seq <= kThreads && a.n_adapters <= kMostCounted; }
+
+// scratch: 2 * kThreads + 2 numbers; memory: 8 * kMostCounted bytes.
+__device__ void find_tile(const Args& p, long long item, Tile& t, int* scratch, void* memory) {
   const rwkvq_lowrank_args& a = p.a;
   const int tid = threadIdx.x;
   if (tid == 0) t.n = 0;
   __syncthreads();
   if (!a.seq_start && a.n_seq == a.tokens && a.n_seq > 1) {
     // one row a sequence.  Rows of the same adapter are taken sixteen at a time; the item-th of these groups, in the order of their first rows.
-    if (a.n_seq <= kThreads) {
-      const int mine = tid < a.n_seq ? a.adapter[tid] : -1;
-      scratch[tid] = mine;
-      __syncthreads();
-      int before = 0;
-      for (int i = 0; i < min(tid, a.n_seq); ++i) before += scratch[i] == mine;
+    if (by_groups(a)) {
+      // how many rows of an adapter each warp has, a byte each, from which a row knows how many are before it
+      uint64_t* const table = static_cast<uint64_t*>(memory);
+      int* const heads = scratch;
+      const int warp = tid >> 5, lane = tid & 31, mine = tid < a.n_seq ? a.adapter[tid] : -1;
       const bool ok = mine >= 0 && mine < a.n_adapters;
-      if (!ok && tid < a.n_seq && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
+      if (!ok && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
+      const int rank = ok && a.ranks ? a.ranks[mine] : a.rank;
+      const float scale = ok && a.scale ? a.scale[mine] : 1.f;
+      for (int i = tid; i < a.n_adapters; i += kThreads) table[i] = 0;
+      const uint32_t same = __match_any_sync(~0u, mine), earlier = same & ((1u << lane) - 1);
+      __syncthreads();
+      if (ok && earlier == 0) reinterpret_cast<uint8_t*>(table + mine)[warp] = (uint8_t)__popc(same);
+      __syncthreads();
+      const uint64_t others = ok && warp > 0 ? table[mine] << (64 - 8 * warp) : 0ull;
+      const int before = (int)((others * 0x0101010101010101ull) >> 56) + __popc(earlier);
       const bool leads = ok && before % kRows == 0;
       const uint32_t vote = __ballot_sync(~0u, leads);
-      int* const heads = scratch + kThreads;
-      if ((tid & 31) == 0) heads[tid / 32] = __popc(vote);
-      if (tid == 0) heads[kWarps] = -1;
+      if (lane == 0) heads[warp] = __popc(vote);
+      if (tid == 0) t.adapter = -1;
       __syncthreads();
-      int at = __popc(vote & ((1u << (tid & 31)) - 1));
-      for (int w = 0; w < tid / 32; ++w) at += heads[w];
-      if (leads && at == item) { heads[kWarps] = mine; heads[kWarps + 1] = before; }
+      int at = __popc(vote & ((1u << lane) - 1));
+      for (int w = 0; w < warp; ++w) at += heads[w];
+      if (leads && at == item) { t.adapter = mine; t.rank = rank; t.scale = scale; heads[kWarps] = before; }
       __syncthreads();
-      const int adapter = heads[kWarps], from = heads[kWarps + 1];
-      if (adapter < 0) return;
-      const bool in = mine == adapter && before >= from && before < from + kRows;
+      if (t.adapter < 0) return;
+      const int from = heads[kWarps];
+      const bool in = mine == t.adapter && before >= from && before < from + kRows;
       if (in) { t.rows[before - from] = tid; t.seqs[before - from] = tid; }
       const int n = __syncthreads_count(in);
-      if (tid == 0) { t.n = n; t.adapter = adapter; }
+      if (tid == 0) {
+        t.n = n;
+        if (t.rank < 0 || t.rank > a.rank) { atomicExch(p.status, (int)RWKVQ_EINVAL); t.n = 0; }
+        if (t.rank == 0) t.n = 0;
+      }
+      __syncthreads();
+      return;
     } else {
       // many rows: an item is a row, which takes the next fifteen of its adapter if it is the first, seventeenth, ... of these
       const int mine = a.adapter[item];
@@ -168,6 +185,7 @@ __device__ void find_tile(const Args& p, long long item, Tile& t, int* scratch) 
   }
   if (tid == 0) {
     const int rank = a.ranks ? a.ranks[t.adapter] : a.rank;
+    t.scale = a.scale ? a.scale[t.adapter] : 1.f;
     t.rank = rank;
     if (rank < 0 || rank > a.rank) { atomicExch(p.status, (int)RWKVQ_EINVAL); t.n = 0; }
     if (rank == 0) t.n = 0;
@@ -208,13 +226,13 @@ __device__ __forceinline__ __nv_bfloat16 term(float& x) {
   return __ushort_as_bfloat16((unsigned short)(__float_as_uint(hi) >> 16));
 }
 
-// A pair of f16 weights as two pairs of bf16: eleven bits are eight and three.
+// A pair of f16 weights as two pairs of bf16: eleven bits are eight and three.  (Of an infinity the second is NaN.)
 __device__ __forceinline__ void apart(uint32_t w, uint32_t& hi, uint32_t& lo) {
-  float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-  __nv_bfloat162 h, l;
-  h.x = term(f.x); h.y = term(f.y);
-  l.x = term(f.x); l.y = term(f.y);
-  hi = *reinterpret_cast<const uint32_t*>(&h); lo = *reinterpret_cast<const uint32_t*>(&l);
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  const uint32_t x = __float_as_uint(f.x), y = __float_as_uint(f.y);
+  hi = __byte_perm(x, y, 0x7632);
+  const __nv_bfloat162 l = __floats2bfloat162_rn(f.x - __uint_as_float(x & 0xFFFF0000u), f.y - __uint_as_float(y & 0xFFFF0000u));
+  lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 
 // y[at], y[at + 1] += v.  Each element of y is added to once in a call, so that a reduction in memory is as good as a load, an addition and a store, and
@@ -240,20 +258,24 @@ template <typename X, typename W> struct Form {
   static constexpr bool kApart = std::is_same<W, __half>::value && !kHalf;
 };
 
-__device__ __forceinline__ uint32_t mu_pair(const Args& p, const uint32_t* codebook, int pair) {
-  const uint32_t bit = (uint32_t)pair * (uint32_t)p.mu_bits;
-  const uint8_t* at = p.mu + (bit >> 3);
-  const uint32_t two = (uint32_t)at[0] | ((bit & 7u) + p.mu_bits > 8u ? (uint32_t)at[1] << 8 : 0u);
-  return codebook[(two >> (bit & 7u)) & ((1u << p.mu_bits) - 1u)];
+// The token-shift vector's pairs of columns col to col + 7 (col a multiple of 8), whose indices are four times mu_bits neighbouring bits from a byte's beginning.
+__device__ __forceinline__ void mu_eight(const Args& p, const uint32_t* codebook, int col, float2 (&m)[4]) {
+  const uint32_t byte = (uint32_t)(col >> 3) * (uint32_t)p.mu_bits >> 1, shift = (byte & 3u) * 8u;
+  const uint32_t* const words = reinterpret_cast<const uint32_t*>(p.mu) + (byte >> 2);
+  const uint32_t lo = __ldg(words), hi = shift + 4u * (uint32_t)p.mu_bits > 32u ? __ldg(words + 1) : 0u, f = __funnelshift_r(lo, hi, shift), mask = (1u << p.mu_bits) - 1u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t pair = codebook[f >> (uint32_t)(j * p.mu_bits) & mask];
+    m[j] = __half22float2(*reinterpret_cast<const __half2*>(&pair));
+  }
 }
 
 // ---- few rows: the weights straight from memory into registers ----------------------------------------------
 // A unit is sixteen rows of a weight matrix by 32 columns: lane (g, q) holds columns 8q to 8q + 7 of rows g and g + 8, the operands of four steps whose columns are
 // numbered so that the first four of the eight are one step's and the others the next one's.
 struct Unit { uint4 lo, hi; };        // row g, row g + 8
-constexpr int kAhead = 4;             // units that a warp has on their way
+constexpr int kSide = 4, kDeep = 2;        // units that a warp has on their way: four side by side (blocks of rank, or tiles of B), two along the columns
 
-// `lanes`: of the lane's eight columns, those that exist (the others come out as zeros: they may hold anything).
 template <typename W>
 __device__ __forceinline__ Unit load_unit(const W* m, long long row, long long rows, long long pitch, int col, int cols) {
   Unit u;
@@ -289,17 +311,25 @@ __device__ __forceinline__ void mma_unit(float (&d)[2][4], const uint4& xa, cons
 __device__ __forceinline__ void apart(const uint4& w, uint4& hi, uint4& lo) {
   apart(w.x, hi.x, lo.x); apart(w.y, hi.y, lo.y); apart(w.z, hi.z, lo.z); apart(w.w, hi.w, lo.w);
 }
-// All terms of x (`pitch` bytes from row to row, `next` from term to term) by a unit of weights, which are taken apart if they have to be: the small products first.
+// All terms of x (`pitch` bytes from row to row, `next` from term to term) by up to kSide units of weights, the small products first.
 template <bool kHalf, bool kApart, int kTerms>
-__device__ __forceinline__ void multiply(float (&d)[2][4], const uint8_t* x, uint32_t pitch, uint32_t next, int terms, const Unit& w) {
-  Unit hi = w, lo;
-  if constexpr (kApart) { apart(w.lo, hi.lo, lo.lo); apart(w.hi, hi.hi, lo.hi); }
+__device__ __forceinline__ void multiply(float (&d)[kSide][2][4], const uint8_t* x, uint32_t pitch, uint32_t next, int terms, const Unit* w, int units) {
 #pragma unroll
   for (int k = kTerms - 1; k >= 0; --k) {
     if (k >= terms) continue;
     const uint4 xa = *reinterpret_cast<const uint4*>(x + k * next), xb = *reinterpret_cast<const uint4*>(x + k * next + 8 * pitch);
-    if constexpr (kApart) mma_unit<kHalf>(d, xa, xb, lo);
-    mma_unit<kHalf>(d, xa, xb, hi);
+#pragma unroll
+    for (int u = 0; u < kSide; ++u) {
+      if (u >= units) continue;
+      if constexpr (kApart) {
+        Unit hi, lo;
+        apart(w[u].lo, hi.lo, lo.lo); apart(w[u].hi, hi.hi, lo.hi);
+        mma_unit<kHalf>(d[u], xa, xb, lo);
+        mma_unit<kHalf>(d[u], xa, xb, hi);
+      } else {
+        mma_unit<kHalf>(d[u], xa, xb, w[u]);
+      }
+    }
   }
 }
 
@@ -307,12 +337,12 @@ template <typename X, typename W>
 struct Shape {
   static constexpr int kTerms = Form<X, W>::kX;
   // bytes of a row in shared memory: 16-byte reads of two neighbouring rows meet no bank twice
-  static constexpr int kPitch = kMostCols * 2 + 64, kHPitch = kMostRank * 2 + 64, kSharePitch = kMostRank;
-  static constexpr int kXBytes = kTerms * kRows * kPitch;
-  static constexpr int kPart = kWarps * 16 * kRows * 4;               // partial sums: [group of warps][block of 16][row][16]
-  static constexpr int kShare = kRows * kSharePitch * 4;
-  static constexpr int kHBytes = 3 * kRows * kHPitch;
-  static constexpr int kBytes = (kXBytes > kHBytes ? kXBytes : kHBytes) + kPart + kShare + 256 * 4;
+  static constexpr int kPitch = kMostCols * 2 + 64, kHPitch = kMostRank * 2 + 64, kPartPitch = kSide * 16 + 8;
+  static constexpr int kXBytes = kTerms * kRows * kPitch, kHBytes = 3 * kRows * kHPitch, kFront = kXBytes > kHBytes ? kXBytes : kHBytes;
+  static constexpr int kPart = kWarps * kRows * kPartPitch * 4;       // sums of each warp: [warp][row][64 of the rank]
+  static constexpr int kShare = kRows * kMostRank * 4;
+  static constexpr int kBytes = kFront + kPart + kShare + 256 * 4;
+  static_assert(kPart >= 8 * kMostCounted, "room for counting the rows of adapters");
 };
 
 template <typename X, typename W>
@@ -322,10 +352,10 @@ __global__ void __launch_bounds__(kThreads, 2) lowrank_kernel(const Args p) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Tile t;
   __shared__ int scratch[2 * kThreads + 2];
-  uint8_t* const xs = smem;                                                             // [term][row][column], then A x: [term][row][rank]
+  uint8_t* const xs = smem;                                              // [term][row][column], then A x: [term][row][rank]
   uint8_t* const hs = smem;
-  float* const part = reinterpret_cast<float*>(smem + (S::kXBytes > S::kHBytes ? S::kXBytes : S::kHBytes));
-  float* const share = part + S::kPart / 4;                                             // this block's share of A x: [row][rank]
+  float* const part = reinterpret_cast<float*>(smem + S::kFront);
+  float* const share = part + S::kPart / 4;                              // this block's share of A x: [row][rank]
   uint32_t* const codebook = reinterpret_cast<uint32_t*>(share + S::kShare / 4);
   const rwkvq_lowrank_args& a = p.a;
   cg::cluster_group cluster = cg::this_cluster();
@@ -334,137 +364,140 @@ __global__ void __launch_bounds__(kThreads, 2) lowrank_kernel(const Args p) {
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
+  if (p.mu)
+    for (int i = tid; i < p.mu_entries; i += kThreads) codebook[i] = p.mu_codebook[i];
   const int id = (int)(blockIdx.x / C), item = id / p.splits, split = id - item * p.splits;
-  find_tile(p, item, t, scratch);
+  find_tile(p, item, t, scratch, part);
   __syncthreads();
   const int n = t.n;
   if (n == 0) return;            // the same for all blocks of the cluster
-  const int rank = t.rank, blocks = (rank + 15) / 16;
-  const float scale = a.scale ? a.scale[t.adapter] : 1.f;
+  const int rank = t.rank;
 
-  // ---- A x over this block's columns.  Warps side by side along the rank as far as it reaches, the others along the columns
+  // ---- A x over this block's columns, 64 of the rank at a time.  Each warp takes every eighth unit of columns, for all of these.
   const int units = (a.ic + 31) / 32, u0 = (int)((long long)units * c / C), u1 = (int)((long long)units * (c + 1) / C);
-  int along = 1;
-  while (along < kWarps && along < blocks) along *= 2;
-  const int groups = kWarps / along, group = warp / along, wr = warp % along;
   const W* const A = static_cast<const W*>(a.A) + (long long)t.adapter * a.rank * a.ic;
-  const int live = wr < blocks ? rank : 0;          // warps beyond the rank have nothing to read
-  Unit w[kAhead];
+  Unit w[kDeep * kSide];
+  auto load_a = [&](int uc, int r0) {
 #pragma unroll
-  for (int j = 0; j < kAhead; ++j) {
-    const int u = u0 + group + j * groups;
-    w[j] = load_unit(A, wr * 16 + g, live, a.ic, u * 32 + q * 8, u < u1 ? a.ic : 0);
-  }
-  if (p.mu) {
-    for (int i = tid; i < p.mu_entries; i += kThreads) codebook[i] = p.mu_codebook[i];
-    __syncthreads();
-  }
-  float acc[2][4] = {};
-  for (int uc = u0; uc < u1; uc += kMostCols / 32) {
-    const int ue = min(uc + kMostCols / 32, u1), eights = (ue - uc) * 4;
-    if (uc > u0) __syncthreads();
-    for (int i = tid; i < n * eights; i += kThreads) {
-      const int r = i / eights, col8 = i - r * eights, col = uc * 32 + col8 * 8;
-      float x[8];
+    for (int k = 0; k < kDeep; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = 0.f;
-      if (col < a.ic) {
-        load8(static_cast<const X*>(a.x) + (long long)t.rows[r] * a.x_row + col, x);
-        if (p.mu) {
-          float y[8];
+      for (int j = 0; j < kSide; ++j) {
+        const int u = uc + warp + k * kWarps;
+        w[k * kSide + j] = load_unit(A, r0 + j * 16 + g, rank, a.ic, u * 32 + q * 8, u < u1 ? a.ic : 0);
+      }
+  };
+  load_a(u0, 0);
+  for (int r0 = 0; r0 < rank; r0 += kSide * 16) {
+    const int side = min(kSide, (rank - r0 + 15) / 16);
+    float acc[kSide][2][4] = {};
+    for (int uc = u0; uc < u1 || uc == u0; uc += kMostCols / 32) {
+      const int ue = min(uc + kMostCols / 32, u1), eights = (ue - uc) * 4;
+      if (r0 == 0 || u1 - u0 > kMostCols / 32) {
+        if (uc > u0 || r0 > 0) __syncthreads();
+        for (int i = tid; i < n * eights; i += kThreads) {
+          const int r = i / eights, col8 = i - r * eights, col = uc * 32 + col8 * 8;
+          float x[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = 0.f;
-          const int seq = t.seqs[r];
-          if (a.x_prev) load8(static_cast<const X*>(a.x_prev) + (long long)t.rows[r] * a.x_prev_row + col, y);
-          else if (seq < 0) load8(static_cast<const X*>(a.x) + (long long)(t.rows[r] - 1) * a.x_row + col, y);
-          else if (a.xprev0) load8(static_cast<const X*>(a.xprev0) + (long long)seq * a.ic + col, y);
+          for (int j = 0; j < 8; ++j) x[j] = 0.f;
+          if (col < a.ic) {
+            load8(static_cast<const X*>(a.x) + (long long)t.rows[r] * a.x_row + col, x);
+            if (p.mu) {
+              float y[8];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t m2 = mu_pair(p, codebook, col / 2 + j);
-            const float2 m = __half22float2(*reinterpret_cast<const __half2*>(&m2));
-            x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m.x, x[2 * j])));
-            x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m.y, x[2 * j + 1])));
+              for (int j = 0; j < 8; ++j) y[j] = 0.f;
+              const int seq = t.seqs[r];
+              if (a.x_prev) load8(static_cast<const X*>(a.x_prev) + (long long)t.rows[r] * a.x_prev_row + col, y);
+              else if (seq < 0) load8(static_cast<const X*>(a.x) + (long long)(t.rows[r] - 1) * a.x_row + col, y);
+              else if (a.xprev0) load8(static_cast<const X*>(a.xprev0) + (long long)seq * a.ic + col, y);
+              float2 m[4];
+              mu_eight(p, codebook, col, m);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m[j].x, x[2 * j])));
+                x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m[j].y, x[2 * j + 1])));
+              }
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < F::kX; ++k) {
+            uint32_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if constexpr (F::kHalf) {
+                const __half2 h = __floats2half2_rn(x[2 * j], x[2 * j + 1]);
+                v[j] = *reinterpret_cast<const uint32_t*>(&h);
+              } else if constexpr (F::kX == 1) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+                v[j] = *reinterpret_cast<const uint32_t*>(&h);
+              } else {
+                __nv_bfloat162 h;
+                h.x = term(x[2 * j]); h.y = term(x[2 * j + 1]);
+                v[j] = *reinterpret_cast<const uint32_t*>(&h);
+              }
+            }
+            *reinterpret_cast<uint4*>(xs + (k * kRows + r) * S::kPitch + col8 * 16) = make_uint4(v[0], v[1], v[2], v[3]);
           }
         }
+        __syncthreads();
       }
+      // rows of x behind the n-th hold whatever was there: a row meets its own outputs alone
 #pragma unroll
-      for (int k = 0; k < F::kX; ++k) {
-        uint32_t v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (F::kHalf) {
-            const __half2 h = __floats2half2_rn(x[2 * j], x[2 * j + 1]);
-            v[j] = *reinterpret_cast<const uint32_t*>(&h);
-          } else {
-            __nv_bfloat162 h;
-            h.x = term(x[2 * j]); h.y = term(x[2 * j + 1]);
-            v[j] = *reinterpret_cast<const uint32_t*>(&h);
-          }
-        }
-        *reinterpret_cast<uint4*>(xs + (k * kRows + r) * S::kPitch + col8 * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+      for (int k = 0; k < kDeep; ++k) {
+        const int u = uc + warp + k * kWarps;
+        if (u < ue) multiply<F::kHalf, F::kApart, F::kX>(acc, xs + g * S::kPitch + ((u - uc) * 32 + q * 8) * 2, S::kPitch, kRows * S::kPitch, F::kX, w + k * kSide, side);
       }
+      if (ue < u1) load_a(ue, r0);
+      else if (r0 + kSide * 16 < rank) load_a(u0, r0 + kSide * 16);
     }
+    if (r0 > 0) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSide; ++j)
+      if (j < side)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2)
+          if (g + e * 4 < n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              *reinterpret_cast<float2*>(part + (warp * kRows + g + e * 4) * S::kPartPitch + j * 16 + h * 8 + q * 2) = make_float2(acc[j][h][e], acc[j][h][e + 1]);
     __syncthreads();
-    // rows of x behind the n-th hold whatever was there: a row meets its own outputs alone
-    if (wr < blocks) {
-      for (int u = uc + group; u < ue; u += kAhead * groups) {
+    for (int i = tid; i < n * kSide * 16; i += kThreads) {
+      const int row = i / (kSide * 16), r = i % (kSide * 16);
+      if (r >= side * 16) continue;
+      float s = 0.f;
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          const int v = u + j * groups;
-          if (v >= ue) continue;
-          multiply<F::kHalf, F::kApart, F::kX>(acc, xs + g * S::kPitch + ((v - uc) * 32 + q * 8) * 2, S::kPitch, kRows * S::kPitch, F::kX, w[j]);
-        }
-        const int next = u + kAhead * groups < ue ? u + kAhead * groups : ue + group;
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          const int v = next + j * groups;
-          w[j] = load_unit(A, wr * 16 + g, live, a.ic, v * 32 + q * 8, v < u1 ? a.ic : 0);
-        }
-      }
+      for (int k = 0; k < kWarps; ++k) s += part[(k * kRows + row) * S::kPartPitch + r];
+      share[row * kMostRank + r0 + r] = s;
     }
   }
 
-  // ---- B's first units on their way
+  // ---- B's first units on their way, and y where it is read
   const int tiles = (a.oc + 15) / 16, all_parts = C * p.splits, part_id = split * C + c;
   const int o0 = (int)((long long)tiles * part_id / all_parts), o1 = (int)((long long)tiles * (part_id + 1) / all_parts);
   const W* const Bm = static_cast<const W*>(a.B) + (long long)t.adapter * a.oc * a.rank;
-  const int kb = (rank + 31) / 32, mine = o0 + warp < o1 ? (o1 - o0 - warp + kWarps - 1) / kWarps * kb : 0;        // units of this warp, tile after tile
-  auto load_b = [&](int i) {
-    const int tile = i / kb, k = i - tile * kb, col = k * 32 + q * 8;
-    Unit u = load_unit(Bm, (long long)(o0 + warp + tile * kWarps) * 16 + g, i < mine ? a.oc : 0, a.rank, col, rank);
-    if (col + 8 > rank) { keep(u.lo, rank - col); keep(u.hi, rank - col); }        // what lies behind the adapter's rank may be anything
-    return u;
+  auto load_b = [&](int o, int col0) {
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k)
+#pragma unroll
+      for (int j = 0; j < kSide; ++j) {
+        const int tile = o + j * kWarps, col = col0 + k * 32 + q * 8;
+        Unit& u = w[k * kSide + j];
+        u = load_unit(Bm, (long long)tile * 16 + g, tile < o1 ? a.oc : 0, a.rank, col, rank);
+        if (col + 8 > rank) { keep(u.lo, rank - col); keep(u.hi, rank - col); }        // what lies behind the adapter's rank may be anything
+      }
   };
-#pragma unroll
-  for (int j = 0; j < kAhead; ++j) w[j] = load_b(j);
-
-  // ---- the block's share: its groups of warps added up
-  if (wr < blocks) {
-    float* at = part + (group * along + wr) * 16 * kRows;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      *reinterpret_cast<float2*>(at + g * 16 + h * 8 + q * 2) = make_float2(acc[h][0], acc[h][1]);
-      *reinterpret_cast<float2*>(at + (g + 8) * 16 + h * 8 + q * 2) = make_float2(acc[h][2], acc[h][3]);
-    }
-  }
-  __syncthreads();
-  for (int i = tid; i < n * blocks * 16; i += kThreads) {
-    const int row = i / (blocks * 16), r = i - row * blocks * 16, at = (r / 16 * kRows + row) * 16 + r % 16;
-    float s = 0.f;
-    for (int k = 0; k < groups; ++k) s += part[k * along * 16 * kRows + at];
-    share[row * S::kSharePitch + r] = s;
-  }
+  load_b(o0 + warp, 0);
   cluster.sync();
 
   // ---- all of A x, as operands
-  const int last_term = a.y_dtype == RWKVQ_F32 ? 2 : 1, width = kb * 32;
+  const int last_term = a.y_dtype == RWKVQ_F32 ? 2 : 1, width = (rank + 31) / 32 * 32;
+  const float scale = t.scale;
   for (int i = tid; i < n * width; i += kThreads) {
     const int row = i / width, r = i - row * width;
     float s = 0.f;
     if (r < rank) {
       float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = k < C ? cluster.map_shared_rank(share, k)[row * S::kSharePitch + r] : 0.f;
+      for (int k = 0; k < 8; ++k) v[k] = k < C ? cluster.map_shared_rank(share, k)[row * kMostRank + r] : 0.f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) s += v[k];
       s *= scale;
@@ -478,26 +511,28 @@ __global__ void __launch_bounds__(kThreads, 2) lowrank_kernel(const Args p) {
   __syncthreads();
 
   // ---- B (A x) for this block's rows of B
-  float d[2][4] = {};
-  for (int i = 0; i < mine; i += kAhead) {
+  for (int o = o0 + warp; o < o1; o += kSide * kWarps) {
+    const int side = min(kSide, (o1 - o + kWarps - 1) / kWarps);
+    float d[kSide][2][4] = {};
+    for (int col0 = 0; col0 < rank; col0 += kDeep * 32) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      if (i + j >= mine) continue;
-      const int tile = (i + j) / kb, k = i + j - tile * kb;
-      multiply<false, std::is_same<W, __half>::value, 3>(d, hs + g * S::kHPitch + (k * 32 + q * 8) * 2, S::kHPitch, kRows * S::kHPitch, last_term + 1, w[j]);
-      w[j] = load_b(i + j + kAhead);
-      if (k + 1 < kb) continue;
+      for (int k = 0; k < kDeep; ++k)
+        if (col0 + k * 32 < rank)
+          multiply<false, std::is_same<W, __half>::value, 3>(d, hs + g * S::kHPitch + (col0 + k * 32 + q * 8) * 2, S::kHPitch, kRows * S::kHPitch, last_term + 1, w + k * kSide, side);
+      if (col0 + kDeep * 32 < rank) load_b(o, col0 + kDeep * 32);
+      else if (o + kSide * kWarps < o1) load_b(o + kSide * kWarps, 0);
+    }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int col = (o0 + warp + tile * kWarps) * 16 + h * 8 + q * 2;
+    for (int e = 0; e < 4; e += 2) {
+      if (g + e * 4 >= n) continue;
+      const long long at = (long long)t.rows[g + e * 4] * a.y_row;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int row = g + e * 8;
-          const float v0 = d[h][2 * e], v1 = d[h][2 * e + 1];
-          if (row < n && col < a.oc) add_pair(a.y, a.y_dtype, (long long)t.rows[row] * a.y_row + col, v0, v1);
-          d[h][2 * e] = d[h][2 * e + 1] = 0.f;
+      for (int j = 0; j < kSide; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int col = (o + j * kWarps) * 16 + h * 8 + q * 2;
+          if (j < side && col < a.oc) add_pair(a.y, a.y_dtype, at + col, d[j][h][e], d[j][h][e + 1]);
         }
-      }
     }
   }
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // no block ends while another reads its share
@@ -569,7 +604,7 @@ rwkvq_status rwkvq_lowrank(const rwkvq_lowrank_args* args, const rwkvq_desc* mu_
   // tiles that there can be
   const long long full = ((long long)a.tokens + lr::kRows - 1) / lr::kRows;
   const long long items = a.seq_start ? std::min<long long>(a.tokens, full + a.n_seq) : a.n_seq == 1 ? full :
-                          a.n_seq <= lr::kThreads ? std::min<long long>(a.n_seq, a.n_adapters + full) : a.n_seq;
+                          lr::by_groups(a) ? std::min<long long>(a.n_seq, a.n_adapters + full) : a.n_seq;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (a.x_dtype == RWKVQ_F32) return cuda_status(lr::launch_x<float>(p, items, s));
   if (a.x_dtype == RWKVQ_F16) return cuda_status(lr::launch_x<__half>(p, items, s));
