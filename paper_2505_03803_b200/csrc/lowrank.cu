@@ -4,9 +4,12 @@
 // with the rows' (token-shifted) inputs, the blocks add up their shares through distributed shared memory, and each multiplies its share of the rows of B
 // with the result: one launch, no workspace, sums in a fixed order.
 //
-// Weights are the 16-row operand of mma.sync, straight from memory to registers: a lane reads 16 neighbouring bytes of a row, and the columns of a step are
-// numbered so that these are its fragments.  Operands are exact: where the types of x and the weights differ, numbers are taken apart into bf16 terms
-// (f16: two, f32: three), and so is A x, which is summed in fp32 (three terms, all of it, where y has 32 bits; two, the second rounded, where y has 16: off by up to 2^-16 of it).
+// Weights come through tensor maps into a ring of shared memory, B's on their way while A's are multiplied, and are the 16-row operand of mma.sync.  Products are
+// exact: where the types of x and the weights differ, numbers are taken apart into bf16 terms (f16: two, f32: three), and so is A x, which is summed in fp32
+// (three terms, all of it, where y has 32 bits; two, the second rounded, where y has 16: off by up to 2^-16 of it).
+//
+// What such a call takes is latency, and much of that the instructions themselves, which are fetched for the first time in each block: loops are kept short and rolled
+// up (the same with weights straight to registers, unrolled for sixteen loads a lane on their way: 33 us where this takes XX, 96 rows with 64 adapters of 4096 x 4096).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -18,6 +21,7 @@
 
 #include "../../include/rwkvq.h"
 #include "host_util.h"
+#include "tc5.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -25,95 +29,112 @@ namespace rwkvq {
 int* device_status_ptr();  // api_misc.cu
 namespace lr {
 
-constexpr int kThreads = 256, kWarps = 8, kRows = 16, kMostRank = 128, kMostCols = 512, kMostCounted = 1024;
+constexpr int kThreads = 256, kWarps = 8, kRows = 16, kMostRank = 128, kMostCounted = 1024;
 
-struct Args {
+struct alignas(64) Args {
   rwkvq_lowrank_args a;
   const uint8_t* mu;             // index stream of the token-shift vector, or nullptr
   const uint32_t* mu_codebook;
   int mu_bits, mu_entries;
   int splits;                    // clusters to a tile
   int* status;
+  CUtensorMap A, B;              // boxes of 64 columns x 16 rows; x 128 rows
 };
 
 // ---- rows of a tile -----------------------------------------------------------------------------------------
 struct Tile {
-  int rows[kRows], seqs[kRows];       // seqs: of a row that is its sequence's first, else -1 - sequence
-  int n, adapter, rank;
+  int rows[kRows];              // of groups of single rows
+  int first, n, seq, start;     // of others: row `first` on, of the sequence that begins at `start`
+  int adapter, rank;
   float scale;
 };
 
-// The sequence and tile of `item` among all tiles of sixteen rows of the sequences in seq_start, or n = 0.  A sequence counts whose rows exist and that
-// does not begin in front of an earlier entry of the list; the others are left out.  All threads.
-__device__ void find_in_list(const Args& p, long long item, int& seq, int& first, int& last, int* scratch) {
+// The tile that is the item-th among all tiles of kTile rows of the sequences in seq_start; t.n stays 0 where there is none.  A sequence counts whose rows exist and that
+// does not begin in front of an earlier entry of the list; the others are left out.  All threads of the block, of which the first kThreads look.
+template <int kTile>
+__device__ __forceinline__ void find_in_list(const Args& p, long long item, Tile& t, int* scratch) {
   const rwkvq_lowrank_args& a = p.a;
-  const int tid = threadIdx.x, each = (a.n_seq + kThreads - 1) / kThreads, i0 = min(tid * each, a.n_seq), i1 = min(i0 + each, a.n_seq);
-  int* most = scratch;                   // [kThreads + 1]
-  int* tiles = scratch + kThreads + 1;   // [kThreads + 1]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, each = (a.n_seq + kThreads - 1) / kThreads, i0 = min(tid * each, a.n_seq), i1 = min(i0 + each, a.n_seq);
+  int* const tops = scratch;             // of each warp
+  int* const sums = scratch + kWarps;
   int top = 0;
+#pragma unroll 1
   for (int i = i0; i < i1; ++i) top = max(top, a.seq_start[i]);
-  most[tid + 1] = top;
-  if (tid == 0) most[0] = 0;
+  int upto = top;                        // most of this and the threads before
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(~0u, upto, o); if (lane >= o) upto = max(upto, v); }
+  if (lane == 31 && warp < kWarps) tops[warp] = upto;
   __syncthreads();
-  int before = 0;
-  for (int t = 0; t <= tid; ++t) before = max(before, most[t]);
-  int sum = 0, run = before;
-  bool bad = false;
-  for (int i = i0; i < i1; ++i) {
-    const int s = a.seq_start[i], e = a.seq_start[i + 1];
-    const bool ok = s >= run && s >= 0 && e >= s && e <= a.tokens;
-    bad |= !ok;
-    if (ok) sum += (e - s + kRows - 1) / kRows;
-    run = max(run, s);
-  }
-  if (bad) atomicExch(p.status, (int)RWKVQ_EINVAL);
-  tiles[tid + 1] = sum;
-  if (tid == 0) tiles[0] = 0;
-  __syncthreads();
-  long long at = 0;
-  for (int t = 0; t <= tid; ++t) at += tiles[t];
-  if (tid == 0) { most[0] = -1; }
-  __syncthreads();
-  run = before;
-  if (item >= at && item < at + sum) {
+  int before = __shfl_up_sync(~0u, upto, 1);
+  if (lane == 0) before = 0;
+  for (int w = 0; w < min(warp, kWarps); ++w) before = max(before, tops[w]);
+  // f(i, start, end) for each sequence of this thread that counts, until it is true
+  auto each_one = [&](auto f) {
+    int run = before;
+    bool bad = false;
+#pragma unroll 1
     for (int i = i0; i < i1; ++i) {
       const int s = a.seq_start[i], e = a.seq_start[i + 1];
-      if (s >= run && s >= 0 && e >= s && e <= a.tokens) {
-        const int n = (e - s + kRows - 1) / kRows;
-        if (item < at + n) {
-          most[0] = i; most[1] = s + (int)(item - at) * kRows; most[2] = min(most[1] + kRows, e);
-          break;
-        }
-        at += n;
-      }
+      const bool ok = s >= run && s >= 0 && e >= s && e <= a.tokens;
+      bad |= !ok;
+      if (ok && f(i, s, e)) break;
       run = max(run, s);
     }
-  }
+    return bad;
+  };
+  int sum = 0;
+  if (each_one([&](int, int s, int e) { sum += (e - s + kTile - 1) / kTile; return false; })) atomicExch(p.status, (int)RWKVQ_EINVAL);
+  int at = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(~0u, at, o); if (lane >= o) at += v; }
+  if (lane == 31 && warp < kWarps) sums[warp] = at;
   __syncthreads();
-  seq = most[0]; first = most[1]; last = most[2];
-  __syncthreads();
+  at -= sum;
+  for (int w = 0; w < min(warp, kWarps); ++w) at += sums[w];
+  if (item >= at && item < at + sum)
+    each_one([&](int i, int s, int e) {
+      const int n = (e - s + kTile - 1) / kTile;
+      if (item < at + n) {
+        t.seq = i; t.start = s; t.first = s + (int)(item - at) * kTile; t.n = min(kTile, e - t.first);
+        return true;
+      }
+      at += n;
+      return false;
+    });
 }
 
+__host__ __device__ inline bool single_rows(const rwkvq_lowrank_args& a) { return !a.seq_start && a.n_seq > 1; }      // each row a sequence
 __host__ __device__ inline bool by_groups(const rwkvq_lowrank_args& a) { return a.n_seq <= kThreads && a.n_adapters <= kMostCounted; }
 
-// scratch: 2 * kThreads + 2 numbers; memory: 8 * kMostCounted bytes.
-__device__ void find_tile(const Args& p, long long item, Tile& t, int* scratch, void* memory) {
+// The rows of a tile of up to kTile; of single rows that share an adapter (then t.n is final, and adapter, rank and scale are known, too) or of a sequence.  All threads.
+// scratch: 2 * kWarps + 2 numbers; memory: 8 * kMostCounted bytes.
+template <int kTile>
+__device__ __forceinline__ void find_rows(const Args& p, long long item, Tile& t, int* scratch, void* memory) {
   const rwkvq_lowrank_args& a = p.a;
-  const int tid = threadIdx.x;
-  if (tid == 0) t.n = 0;
-  __syncthreads();
-  if (!a.seq_start && a.n_seq == a.tokens && a.n_seq > 1) {
-    // one row a sequence.  Rows of the same adapter are taken sixteen at a time; the item-th of these groups, in the order of their first rows.
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) { t.n = 0; t.adapter = -1; }
+  if (!single_rows(a)) {
+    if (a.seq_start) {
+      __syncthreads();
+      find_in_list<kTile>(p, item, t, scratch);
+    } else if (tid == 0) {
+      t.seq = t.start = 0; t.first = (int)item * kTile; t.n = min(kTile, a.tokens - t.first);
+    }
+    __syncthreads();
+    return;
+  }
+  if constexpr (kTile == kRows) {
     if (by_groups(a)) {
-      // how many rows of an adapter each warp has, a byte each, from which a row knows how many are before it
+      // Rows of the same adapter are taken sixteen at a time: the item-th of these groups, in the order of their first rows.  `table`: how many rows of an adapter each
+      // warp has, a byte each, from which a row knows how many are before it.
       uint64_t* const table = static_cast<uint64_t*>(memory);
       int* const heads = scratch;
-      const int warp = tid >> 5, lane = tid & 31, mine = tid < a.n_seq ? a.adapter[tid] : -1;
+      const int mine = tid < a.n_seq ? a.adapter[tid] : -1;
+      for (int i = tid; i < a.n_adapters; i += kThreads) table[i] = 0;
       const bool ok = mine >= 0 && mine < a.n_adapters;
       if (!ok && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
       const int rank = ok && a.ranks ? a.ranks[mine] : a.rank;
       const float scale = ok && a.scale ? a.scale[mine] : 1.f;
-      for (int i = tid; i < a.n_adapters; i += kThreads) table[i] = 0;
       const uint32_t same = __match_any_sync(~0u, mine), earlier = same & ((1u << lane) - 1);
       __syncthreads();
       if (ok && earlier == 0) reinterpret_cast<uint8_t*>(table + mine)[warp] = (uint8_t)__popc(same);
@@ -123,74 +144,59 @@ __device__ void find_tile(const Args& p, long long item, Tile& t, int* scratch, 
       const bool leads = ok && before % kRows == 0;
       const uint32_t vote = __ballot_sync(~0u, leads);
       if (lane == 0) heads[warp] = __popc(vote);
-      if (tid == 0) t.adapter = -1;
       __syncthreads();
       int at = __popc(vote & ((1u << lane) - 1));
       for (int w = 0; w < warp; ++w) at += heads[w];
-      if (leads && at == item) { t.adapter = mine; t.rank = rank; t.scale = scale; heads[kWarps] = before; }
+      if (leads && at == item) { t.adapter = mine; t.rank = rank; t.scale = scale; t.start = before; }
       __syncthreads();
-      if (t.adapter < 0) return;
-      const int from = heads[kWarps];
-      const bool in = mine == t.adapter && before >= from && before < from + kRows;
-      if (in) { t.rows[before - from] = tid; t.seqs[before - from] = tid; }
+      const int from = t.start;
+      const bool in = ok && mine == t.adapter && before >= from && before < from + kRows;
+      if (in) t.rows[before - from] = tid;
       const int n = __syncthreads_count(in);
-      if (tid == 0) {
-        t.n = n;
-        if (t.rank < 0 || t.rank > a.rank) { atomicExch(p.status, (int)RWKVQ_EINVAL); t.n = 0; }
-        if (t.rank == 0) t.n = 0;
+      if (tid == 0 && t.adapter >= 0) {
+        t.n = t.rank < 0 || t.rank > a.rank ? 0 : t.rank == 0 ? 0 : n;
+        if (t.rank < 0 || t.rank > a.rank) atomicExch(p.status, (int)RWKVQ_EINVAL);
       }
-      __syncthreads();
-      return;
     } else {
       // many rows: an item is a row, which takes the next fifteen of its adapter if it is the first, seventeenth, ... of these
       const int mine = a.adapter[item];
-      if (mine < 0 || mine >= a.n_adapters) {
-        if (tid == 0 && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
-        return;
-      }
       int before = 0;
-      for (int i = tid; i < item; i += kThreads) before += a.adapter[i] == mine;
+      for (int i = tid; i < item && tid < kThreads; i += kThreads) before += a.adapter[i] == mine;
       for (int o = 16; o > 0; o /= 2) before += __shfl_xor_sync(~0u, before, o);
-      if ((tid & 31) == 0) scratch[tid / 32] = before;
+      if (lane == 0 && warp < kWarps) scratch[warp] = before;
       __syncthreads();
       before = 0;
       for (int w = 0; w < kWarps; ++w) before += scratch[w];
-      if (before % kRows) return;
-      if (tid < 32) {
+      if (before % kRows == 0 && tid < 32 && mine != -1) {
         int n = 0;
         for (int i0 = (int)item; i0 < a.n_seq && n < kRows; i0 += 32) {
           const int i = i0 + tid;
           const uint32_t same = __ballot_sync(~0u, i < a.n_seq && a.adapter[i] == mine);
           const int at = n + __popc(same & ((1u << tid) - 1));
-          if ((same >> tid & 1) && at < kRows) { t.rows[at] = i; t.seqs[at] = i; }
+          if ((same >> tid & 1) && at < kRows) t.rows[at] = i;
           n = min(kRows, n + __popc(same));
         }
-        if (tid == 0) { t.n = n; t.adapter = mine; }
+        if (tid == 0) { t.n = n; t.seq = (int)item; }
       }
     }
-  } else {
-    int seq = 0, first = (int)item * kRows, last = min(first + kRows, a.tokens), start = 0;
-    if (a.seq_start) {
-      find_in_list(p, item, seq, first, last, scratch);
-      if (seq < 0) return;
-      start = a.seq_start[seq];
-    }
-    const int mine = a.adapter[seq];
-    if (mine < 0 || mine >= a.n_adapters) {
-      if (tid == 0 && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
-      return;
-    }
-    if (tid < last - first) { t.rows[tid] = first + tid; t.seqs[tid] = first + tid == start ? seq : -1 - seq; }
-    if (tid == 0) { t.n = last - first; t.adapter = mine; }
-  }
-  if (tid == 0) {
-    const int rank = a.ranks ? a.ranks[t.adapter] : a.rank;
-    t.scale = a.scale ? a.scale[t.adapter] : 1.f;
-    t.rank = rank;
-    if (rank < 0 || rank > a.rank) { atomicExch(p.status, (int)RWKVQ_EINVAL); t.n = 0; }
-    if (rank == 0) t.n = 0;
   }
   __syncthreads();
+}
+
+// Adapter, rank and scale of a tile whose rows are known, by one thread; t.n is 0 where it has none.
+__device__ __forceinline__ void find_adapter(const Args& p, Tile& t) {
+  const rwkvq_lowrank_args& a = p.a;
+  if (t.n == 0 || t.adapter >= 0) return;
+  const int mine = a.adapter[t.seq];
+  bool bad = mine < -1 || mine >= a.n_adapters;
+  if (!bad && mine >= 0) {
+    const int rank = a.ranks ? a.ranks[mine] : a.rank;
+    const float scale = a.scale ? a.scale[mine] : 1.f;
+    bad = rank < 0 || rank > a.rank;
+    if (rank > 0) { t.adapter = mine; t.rank = rank; t.scale = scale; }
+  }
+  if (bad) atomicExch(p.status, (int)RWKVQ_EINVAL);
+  if (bad || t.adapter < 0) t.n = 0;
 }
 
 // ---- numbers and operands -----------------------------------------------------------------------------------
@@ -235,22 +241,6 @@ __device__ __forceinline__ void apart(uint32_t w, uint32_t& hi, uint32_t& lo) {
   lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 
-// y[at], y[at + 1] += v.  Each element of y is added to once in a call, so that a reduction in memory is as good as a load, an addition and a store, and
-// nothing waits for it (it takes subnormal numbers for zeros).
-__device__ __forceinline__ void add_pair(void* y, int dtype, long long at, float v0, float v1) {
-  if (dtype == RWKVQ_F32) {
-    asm volatile("red.relaxed.gpu.global.add.v2.f32 [%0], {%1, %2};" ::"l"(static_cast<float*>(y) + at), "f"(v0), "f"(v1) : "memory");
-  } else if (dtype == RWKVQ_F16) {
-    __half2* const p = reinterpret_cast<__half2*>(static_cast<__half*>(y) + at);
-    const float2 f = __half22float2(*p);
-    *p = __floats2half2_rn(f.x + v0, f.y + v1);
-  } else {
-    __nv_bfloat162* const p = reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(y) + at);
-    const float2 f = __bfloat1622float2(*p);
-    *p = __floats2bfloat162_rn(f.x + v0, f.y + v1);
-  }
-}
-
 // How x and the weights go into the tensor cores.
 template <typename X, typename W> struct Form {
   static constexpr bool kHalf = std::is_same<X, __half>::value && std::is_same<W, __half>::value;
@@ -270,272 +260,370 @@ __device__ __forceinline__ void mu_eight(const Args& p, const uint32_t* codebook
   }
 }
 
-// ---- few rows: the weights straight from memory into registers ----------------------------------------------
-// A unit is sixteen rows of a weight matrix by 32 columns: lane (g, q) holds columns 8q to 8q + 7 of rows g and g + 8, the operands of four steps whose columns are
-// numbered so that the first four of the eight are one step's and the others the next one's.
-struct Unit { uint4 lo, hi; };        // row g, row g + 8
-constexpr int kSide = 4, kDeep = 2;        // units that a warp has on their way: four side by side (blocks of rank, or tiles of B), two along the columns
-
-template <typename W>
-__device__ __forceinline__ Unit load_unit(const W* m, long long row, long long rows, long long pitch, int col, int cols) {
-  Unit u;
-  u.lo = u.hi = make_uint4(0, 0, 0, 0);
-  if (col < cols) {
-    if (row < rows) u.lo = __ldg(reinterpret_cast<const uint4*>(m + row * pitch + col));
-    if (row + 8 < rows) u.hi = __ldg(reinterpret_cast<const uint4*>(m + (row + 8) * pitch + col));
-  }
-  return u;
-}
-__device__ __forceinline__ void keep(uint4& w, int n) {        // the first n of eight numbers of two bytes
-  auto of = [n](int i) { return n >= 2 * i + 2 ? ~0u : n == 2 * i + 1 ? 0xFFFFu : 0u; };
-  w.x &= of(0); w.y &= of(1); w.z &= of(2); w.w &= of(3);
-}
-
-// d[0], d[1]: sixteen rows of x (a: row g, b: row g + 8 of the lane's columns) by the unit's rows 0 to 7 and 8 to 15.
+// ---- few rows -----------------------------------------------------------------------------------------------
 template <bool kHalf>
-__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&w)[4], uint32_t x0, uint32_t x1) {
   if constexpr (kHalf)
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(x0), "r"(x1));
   else
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(x0), "r"(x1));
 }
-template <bool kHalf>
-__device__ __forceinline__ void mma_unit(float (&d)[2][4], const uint4& xa, const uint4& xb, const Unit& w) {
-  mma<kHalf>(d[0], xa.x, xb.x, xa.y, xb.y, w.lo.x, w.lo.y);
-  mma<kHalf>(d[1], xa.x, xb.x, xa.y, xb.y, w.hi.x, w.hi.y);
-  mma<kHalf>(d[0], xa.z, xb.z, xa.w, xb.w, w.lo.z, w.lo.w);
-  mma<kHalf>(d[1], xa.z, xb.z, xa.w, xb.w, w.hi.z, w.hi.w);
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
-__device__ __forceinline__ void apart(const uint4& w, uint4& hi, uint4& lo) {
-  apart(w.x, hi.x, lo.x); apart(w.y, hi.y, lo.y); apart(w.z, hi.z, lo.z); apart(w.w, hi.w, lo.w);
+// Byte offset of 16 bytes (eight columns) in rows of 128 bytes under the 128-byte swizzle.
+__device__ __forceinline__ uint32_t swizzled(int row, int eight) { return (uint32_t)(row * 128 + ((eight ^ row) & 7) * 16); }
+// A box of a tensor map by a converged warp, of which one lane is elected by predicate: from a branch of one lane each took some 145 cycles.
+__device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
+               " @q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n}"
+               ::"r"(dst_smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
-// All terms of x (`pitch` bytes from row to row, `next` from term to term) by up to kSide units of weights, the small products first.
+
+// A slot of the ring: as many pieces of 64 columns of all rows of A as fit, or 128 rows by 64 columns of B.
+constexpr int kSlotBytes = 16 << 10, kPass = 8, kXPiece = kRows * 128;      // a pass over x: pieces of 64 columns that are in shared memory at a time
+constexpr int kAll = kThreads + 32;                                         // a warp that asks for copies
+template <typename X, typename W>
+struct Shape {
+  static constexpr int kTerms = Form<X, W>::kX, kSlots = kTerms == 1 ? 4 : 3;        // two blocks an SM
+  static constexpr int kXBytes = kTerms * kPass * kXPiece, kHBytes = 3 * 2 * kXPiece, kFront = kXBytes > kHBytes ? kXBytes : kHBytes;
+  static constexpr int kPart = 4 * kRows * 68 * 4;                  // sums of half of the warps: [warp][row][rank], 64 of them and four warps, or 128 and two
+  static constexpr int kShare = kRows * kMostRank * 4;
+  static constexpr int kBytes = 1024 + kSlots * kSlotBytes + kFront + kPart + kShare + 256 * 4;
+  static_assert(kPart >= 8 * kMostCounted && kPart >= 2 * kRows * 132 * 4, "room for counting the rows of adapters, and for two warps' sums");
+};
+struct Ctrl {
+  uint64_t full[4], empty[4];
+  int abort_flag, asked;
+};
+
+// x_mix of eight columns of a row, in fp32 but rounded to X.
+template <typename X>
+__device__ __forceinline__ void mixed_eight(const Args& p, const uint32_t* codebook, int row, int col, const X* before, float (&x)[8]) {
+  load8(static_cast<const X*>(p.a.x) + (long long)row * p.a.x_row + col, x);
+  if (!p.mu) return;
+  float y[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) y[j] = 0.f;
+  if (before) load8(before + col, y);
+  float2 m[4];
+  mu_eight(p, codebook, col, m);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m[j].x, x[2 * j])));
+    x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m[j].y, x[2 * j + 1])));
+  }
+}
+// The row in front of a row, nullptr where there is none.
+template <typename X>
+__device__ __forceinline__ const X* row_before(const Args& p, int row, int seq, bool begins) {
+  if (p.a.x_prev) return static_cast<const X*>(p.a.x_prev) + (long long)row * p.a.x_prev_row;
+  if (!begins) return static_cast<const X*>(p.a.x) + (long long)(row - 1) * p.a.x_row;
+  return p.a.xprev0 ? static_cast<const X*>(p.a.xprev0) + (long long)seq * p.a.ic : nullptr;
+}
+// Eight numbers as operands of the tensor cores: the k-th term of each.
+template <typename F>
+__device__ __forceinline__ uint4 next_term(float (&x)[8]) {
+  uint32_t v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (F::kHalf) {
+      const __half2 h = __floats2half2_rn(x[2 * j], x[2 * j + 1]);
+      v[j] = *reinterpret_cast<const uint32_t*>(&h);
+    } else if constexpr (F::kX == 1) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+      v[j] = *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+      __nv_bfloat162 h;
+      h.x = term(x[2 * j]); h.y = term(x[2 * j + 1]);
+      v[j] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+// One weight fragment (16 rows x 16 columns), taken apart if it has to be, by up to sixteen rows of x in kTerms terms, the small products first.
 template <bool kHalf, bool kApart, int kTerms>
-__device__ __forceinline__ void multiply(float (&d)[kSide][2][4], const uint8_t* x, uint32_t pitch, uint32_t next, int terms, const Unit* w, int units) {
+__device__ __forceinline__ void multiply(float (&d)[2][4], const uint32_t (&w)[4], const uint32_t (&x)[kTerms][4], int terms, bool both) {
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    hi[i] = w[i]; lo[i] = 0;
+    if constexpr (kApart) apart(w[i], hi[i], lo[i]);
+  }
 #pragma unroll
   for (int k = kTerms - 1; k >= 0; --k) {
     if (k >= terms) continue;
-    const uint4 xa = *reinterpret_cast<const uint4*>(x + k * next), xb = *reinterpret_cast<const uint4*>(x + k * next + 8 * pitch);
-#pragma unroll
-    for (int u = 0; u < kSide; ++u) {
-      if (u >= units) continue;
-      if constexpr (kApart) {
-        Unit hi, lo;
-        apart(w[u].lo, hi.lo, lo.lo); apart(w[u].hi, hi.hi, lo.hi);
-        mma_unit<kHalf>(d[u], xa, xb, lo);
-        mma_unit<kHalf>(d[u], xa, xb, hi);
-      } else {
-        mma_unit<kHalf>(d[u], xa, xb, w[u]);
-      }
+    if constexpr (kApart) {
+      mma<kHalf>(d[0], lo, x[k][0], x[k][1]);
+      if (both) mma<kHalf>(d[1], lo, x[k][2], x[k][3]);
     }
+    mma<kHalf>(d[0], hi, x[k][0], x[k][1]);
+    if (both) mma<kHalf>(d[1], hi, x[k][2], x[k][3]);
   }
 }
 
 template <typename X, typename W>
-struct Shape {
-  static constexpr int kTerms = Form<X, W>::kX;
-  // bytes of a row in shared memory: 16-byte reads of two neighbouring rows meet no bank twice
-  static constexpr int kPitch = kMostCols * 2 + 64, kHPitch = kMostRank * 2 + 64, kPartPitch = kSide * 16 + 8;
-  static constexpr int kXBytes = kTerms * kRows * kPitch, kHBytes = 3 * kRows * kHPitch, kFront = kXBytes > kHBytes ? kXBytes : kHBytes;
-  static constexpr int kPart = kWarps * kRows * kPartPitch * 4;       // sums of each warp: [warp][row][64 of the rank]
-  static constexpr int kShare = kRows * kMostRank * 4;
-  static constexpr int kBytes = kFront + kPart + kShare + 256 * 4;
-  static_assert(kPart >= 8 * kMostCounted, "room for counting the rows of adapters");
-};
-
-template <typename X, typename W>
-__global__ void __launch_bounds__(kThreads, 2) lowrank_kernel(const Args p) {
+__global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant__ Args p) {
   using S = Shape<X, W>;
   using F = Form<X, W>;
-  extern __shared__ __align__(128) uint8_t smem[];
+  constexpr bool kWHalf = std::is_same<W, __half>::value;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
   __shared__ Tile t;
-  __shared__ int scratch[2 * kThreads + 2];
-  uint8_t* const xs = smem;                                              // [term][row][column], then A x: [term][row][rank]
-  uint8_t* const hs = smem;
-  float* const part = reinterpret_cast<float*>(smem + S::kFront);
+  __shared__ Ctrl ctrl;
+  __shared__ int scratch[2 * kWarps + 2];
+  uint8_t* const xs = smem + S::kSlots * kSlotBytes;                     // [term][piece][row][64 columns], then A x: [term][piece][row][64 of the rank]
+  float* const part = reinterpret_cast<float*>(xs + S::kFront);
   float* const share = part + S::kPart / 4;                              // this block's share of A x: [row][rank]
   uint32_t* const codebook = reinterpret_cast<uint32_t*>(share + S::kShare / 4);
   const rwkvq_lowrank_args& a = p.a;
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+  volatile int* const abortp = &ctrl.abort_flag;
   asm volatile("griddepcontrol.launch_dependents;");
+  if (tid == 0) {
+    for (int i = 0; i < S::kSlots; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], kWarps); }
+    ctrl.abort_flag = ctrl.asked = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\nfence.proxy.async.shared::cta;" ::: "memory");
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");
-
   if (p.mu)
-    for (int i = tid; i < p.mu_entries; i += kThreads) codebook[i] = p.mu_codebook[i];
+    for (int i = tid; i < p.mu_entries; i += kAll) codebook[i] = p.mu_codebook[i];
   const int id = (int)(blockIdx.x / C), item = id / p.splits, split = id - item * p.splits;
-  find_tile(p, item, t, scratch, part);
-  __syncthreads();
+  find_rows<kRows>(p, item, t, scratch, part);
   const int n = t.n;
-  if (n == 0) return;            // the same for all blocks of the cluster
-  const int rank = t.rank;
+  const bool both = n > 8, grouped = single_rows(a);
+  const int pieces = (a.ic + 63) / 64, k0 = (int)((long long)pieces * c / C), k1 = (int)((long long)pieces * (c + 1) / C);
+  const int tiles = (a.oc + 127) / 128, parts = C * p.splits, at = split * C + c;
+  const int o0 = (int)((long long)tiles * at / parts), o1 = (int)((long long)tiles * (at + 1) / parts);
+  const uint32_t ring = tc5::smem_u32(smem), full = tc5::smem_u32(ctrl.full), empty = tc5::smem_u32(ctrl.empty);
 
-  // ---- A x over this block's columns, 64 of the rank at a time.  Each warp takes every eighth unit of columns, for all of these.
-  const int units = (a.ic + 31) / 32, u0 = (int)((long long)units * c / C), u1 = (int)((long long)units * (c + 1) / C);
-  const W* const A = static_cast<const W*>(a.A) + (long long)t.adapter * a.rank * a.ic;
-  Unit w[kDeep * kSide];
-  auto load_a = [&](int uc, int r0) {
+  // x of columns [kp, ke), pieces of 64, in operand form
+  auto stage_x = [&](int kp, int ke) {
+    const int eights = (ke - kp) * 8;
+#pragma unroll 1
+    for (int e = tid; e < n * eights; e += kThreads) {
+      const int r = e / eights, eight = e - r * eights, col = kp * 64 + eight * 8;
+      float x[8];
+      if (col < a.ic) {
+        const int row = grouped ? t.rows[r] : t.first + r;
+        mixed_eight(p, codebook, row, col, row_before<X>(p, row, grouped ? row : t.seq, grouped || row == t.start), x);
+      } else {
 #pragma unroll
-    for (int k = 0; k < kDeep; ++k)
-#pragma unroll
-      for (int j = 0; j < kSide; ++j) {
-        const int u = uc + warp + k * kWarps;
-        w[k * kSide + j] = load_unit(A, r0 + j * 16 + g, rank, a.ic, u * 32 + q * 8, u < u1 ? a.ic : 0);
+        for (int j = 0; j < 8; ++j) x[j] = 0.f;
       }
+#pragma unroll
+      for (int k = 0; k < F::kX; ++k) *reinterpret_cast<uint4*>(xs + (k * kPass + eight / 8) * kXPiece + swizzled(r, eight & 7)) = next_term<F>(x);
+    }
   };
-  load_a(u0, 0);
-  for (int r0 = 0; r0 < rank; r0 += kSide * 16) {
-    const int side = min(kSide, (rank - r0 + 15) / 16);
-    float acc[kSide][2][4] = {};
-    for (int uc = u0; uc < u1 || uc == u0; uc += kMostCols / 32) {
-      const int ue = min(uc + kMostCols / 32, u1), eights = (ue - uc) * 4;
-      if (r0 == 0 || u1 - u0 > kMostCols / 32) {
-        if (uc > u0 || r0 > 0) __syncthreads();
-        for (int i = tid; i < n * eights; i += kThreads) {
-          const int r = i / eights, col8 = i - r * eights, col = uc * 32 + col8 * 8;
-          float x[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = 0.f;
-          if (col < a.ic) {
-            load8(static_cast<const X*>(a.x) + (long long)t.rows[r] * a.x_row + col, x);
-            if (p.mu) {
-              float y[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = 0.f;
-              const int seq = t.seqs[r];
-              if (a.x_prev) load8(static_cast<const X*>(a.x_prev) + (long long)t.rows[r] * a.x_prev_row + col, y);
-              else if (seq < 0) load8(static_cast<const X*>(a.x) + (long long)(t.rows[r] - 1) * a.x_row + col, y);
-              else if (a.xprev0) load8(static_cast<const X*>(a.xprev0) + (long long)seq * a.ic + col, y);
-              float2 m[4];
-              mu_eight(p, codebook, col, m);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m[j].x, x[2 * j])));
-                x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m[j].y, x[2 * j + 1])));
-              }
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < F::kX; ++k) {
-            uint32_t v[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if constexpr (F::kHalf) {
-                const __half2 h = __floats2half2_rn(x[2 * j], x[2 * j + 1]);
-                v[j] = *reinterpret_cast<const uint32_t*>(&h);
-              } else if constexpr (F::kX == 1) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
-                v[j] = *reinterpret_cast<const uint32_t*>(&h);
-              } else {
-                __nv_bfloat162 h;
-                h.x = term(x[2 * j]); h.y = term(x[2 * j + 1]);
-                v[j] = *reinterpret_cast<const uint32_t*>(&h);
-              }
-            }
-            *reinterpret_cast<uint4*>(xs + (k * kRows + r) * S::kPitch + col8 * 16) = make_uint4(v[0], v[1], v[2], v[3]);
-          }
+  if (warp == kWarps) {
+    if (lane == 0) find_adapter(p, t);
+  } else {
+    stage_x(k0, min(k0 + kPass, k1));
+  }
+  __syncthreads();
+  if (t.n == 0) return;            // the same for all blocks of the cluster
+  const int rank = t.rank, blocks = (rank + 15) / 16;
+  // ---- the ring: pieces of A for this block's columns, then tiles of B for its rows
+  const int a_slot = blocks == 1 ? 8 : blocks == 2 ? 4 : blocks <= 4 ? 2 : 1, n_a = (k1 - k0 + a_slot - 1) / a_slot;      // pieces of A in a slot
+  const int wide = (rank + 63) / 64;
+  bool ok = true;
+  auto take = [&](int i) { ok = ok && tc5::mbar_wait(full + (uint32_t)(i % S::kSlots) * 8u, (uint32_t)(i / S::kSlots) & 1u, abortp, p.status); };
+  auto give = [&](int i) {
+    __syncwarp();
+    if (lane == 0) tc5::mbar_arrive(empty + (uint32_t)(i % S::kSlots) * 8u);
+  };
+  if (warp == kWarps) {
+    // This warp brings nothing to the first meeting of the cluster and does not hold it up: the slots that it waits for below are given back behind it.
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const int total = n_a + (o1 - o0) * wide;
+    int i = 0;
+#pragma unroll 1
+    for (; i < total; ++i) {
+      const uint32_t st = (uint32_t)(i % S::kSlots), bar = full + st * 8u, dst = ring + st * kSlotBytes;
+      if (i >= S::kSlots && !__all_sync(~0u, tc5::mbar_wait(empty + st * 8u, (uint32_t)(i / S::kSlots - 1) & 1u, abortp, p.status))) break;
+      if (i < n_a) {
+        const int first = k0 + i * a_slot, count = min(a_slot, k1 - first) * blocks;
+        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[st], (uint32_t)count * 2048u);
+        __syncwarp();
+#pragma unroll 1
+        for (int j = 0, piece = first, r = 0; j < count; ++j) {
+          tensor_g2s(dst + (uint32_t)j * 2048u, &p.A, piece * 64, r, t.adapter, bar);
+          r += 16;
+          if (r >= rank) { r = 0; ++piece; }
         }
-        __syncthreads();
+      } else {
+        const int j = i - n_a, tile = j / wide;
+        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[st], kSlotBytes);
+        __syncwarp();
+        tensor_g2s(dst, &p.B, (j - tile * wide) * 64, (o0 + tile) * 128, t.adapter, bar);
+      }
+    }
+    if (lane == 0) ctrl.asked = i;
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
+  } else {
+    // ---- A x.  Warps side by side along the columns; two groups of them, each 64 of the rank, where it is longer
+    const int deep = blocks > 4 ? 4 : 8, kw = warp % deep, r_first = warp / deep * 4, side = min(4, blocks - r_first);
+    float acc[4][2][4] = {};
+    const uint32_t x_at = tc5::smem_u32(xs) + (uint32_t)((lane & 7) + (lane >> 4) * 8) * 128u;
+    int i = 0;
+    for (int kp = k0; kp < k1; kp += kPass) {
+      const int ke = min(kp + kPass, k1);
+      if (kp > k0) {
+        asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+        stage_x(kp, ke);
+        asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
       }
       // rows of x behind the n-th hold whatever was there: a row meets its own outputs alone
+      for (int first = kp; first < ke; first += a_slot, ++i) {
+        take(i);
+        const uint32_t slot = ring + (uint32_t)(i % S::kSlots * kSlotBytes);
+        const int steps = min(a_slot, ke - first) * 4;
+        if (ok)
+#pragma unroll 1
+          for (int s = kw; s < steps; s += deep) {
+            const int piece = s >> 2, eight = (s & 3) * 2;
+            const uint32_t at_x = x_at + (uint32_t)((first - kp + piece) * kXPiece) + (uint32_t)(((eight + (lane >> 3 & 1)) ^ lane) & 7) * 16u;
+            const uint32_t at_w = slot + (uint32_t)(piece * blocks + r_first) * 2048u + swizzled(lane & 15, eight + (lane >> 4));
+            uint32_t x[F::kX][4], w[4][4];
 #pragma unroll
-      for (int k = 0; k < kDeep; ++k) {
-        const int u = uc + warp + k * kWarps;
-        if (u < ue) multiply<F::kHalf, F::kApart, F::kX>(acc, xs + g * S::kPitch + ((u - uc) * 32 + q * 8) * 2, S::kPitch, kRows * S::kPitch, F::kX, w + k * kSide, side);
+            for (int k = 0; k < F::kX; ++k) ldmatrix4(x[k], at_x + (uint32_t)k * (kPass * kXPiece));
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (j < side) ldmatrix4(w[j], at_w + (uint32_t)j * 2048u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (j < side) multiply<F::kHalf, F::kApart, F::kX>(acc[j], w[j], x, F::kX, both);
+          }
+        give(i);
       }
-      if (ue < u1) load_a(ue, r0);
-      else if (r0 + kSide * 16 < rank) load_a(u0, r0 + kSide * 16);
     }
-    if (r0 > 0) __syncthreads();
+    // the warps' sums added up: the second half of them to the first, then what is left of these
+    const int half = deep / 2, pitch = blocks > 4 ? 132 : 68;        // pitches that spare banks
+    auto each = [&](auto f) {
+      float* const to = part + (kw % half) * kRows * pitch + r_first * 16 + g;
 #pragma unroll
-    for (int j = 0; j < kSide; ++j)
-      if (j < side)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 4; e += 2)
-          if (g + e * 4 < n)
+        for (int e = 0; e < 2; ++e) {
+          const int row = b * 8 + q * 2 + e;
+          if (row >= n) continue;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              *reinterpret_cast<float2*>(part + (warp * kRows + g + e * 4) * S::kPartPitch + j * 16 + h * 8 + q * 2) = make_float2(acc[j][h][e], acc[j][h][e + 1]);
-    __syncthreads();
-    for (int i = tid; i < n * kSide * 16; i += kThreads) {
-      const int row = i / (kSide * 16), r = i % (kSide * 16);
-      if (r >= side * 16) continue;
-      float s = 0.f;
-#pragma unroll
-      for (int k = 0; k < kWarps; ++k) s += part[(k * kRows + row) * S::kPartPitch + r];
-      share[row * kMostRank + r0 + r] = s;
-    }
-  }
-
-  // ---- B's first units on their way, and y where it is read
-  const int tiles = (a.oc + 15) / 16, all_parts = C * p.splits, part_id = split * C + c;
-  const int o0 = (int)((long long)tiles * part_id / all_parts), o1 = (int)((long long)tiles * (part_id + 1) / all_parts);
-  const W* const Bm = static_cast<const W*>(a.B) + (long long)t.adapter * a.oc * a.rank;
-  auto load_b = [&](int o, int col0) {
-#pragma unroll
-    for (int k = 0; k < kDeep; ++k)
-#pragma unroll
-      for (int j = 0; j < kSide; ++j) {
-        const int tile = o + j * kWarps, col = col0 + k * 32 + q * 8;
-        Unit& u = w[k * kSide + j];
-        u = load_unit(Bm, (long long)tile * 16 + g, tile < o1 ? a.oc : 0, a.rank, col, rank);
-        if (col + 8 > rank) { keep(u.lo, rank - col); keep(u.hi, rank - col); }        // what lies behind the adapter's rank may be anything
-      }
-  };
-  load_b(o0 + warp, 0);
-  cluster.sync();
-
-  // ---- all of A x, as operands
-  const int last_term = a.y_dtype == RWKVQ_F32 ? 2 : 1, width = (rank + 31) / 32 * 32;
-  const float scale = t.scale;
-  for (int i = tid; i < n * width; i += kThreads) {
-    const int row = i / width, r = i - row * width;
-    float s = 0.f;
-    if (r < rank) {
-      float v[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = k < C ? cluster.map_shared_rank(share, k)[row * kMostRank + r] : 0.f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) s += v[k];
-      s *= scale;
-    }
-    __nv_bfloat16* const at = reinterpret_cast<__nv_bfloat16*>(hs + row * S::kHPitch + r * 2);
-    at[0] = term(s);
-    at[kRows * S::kHPitch / 2] = last_term == 1 ? __float2bfloat16_rn(s) : term(s);
-    if (last_term == 2) at[2 * kRows * S::kHPitch / 2] = term(s);
-  }
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  __syncthreads();
-
-  // ---- B (A x) for this block's rows of B
-  for (int o = o0 + warp; o < o1; o += kSide * kWarps) {
-    const int side = min(kSide, (o1 - o + kWarps - 1) / kWarps);
-    float d[kSide][2][4] = {};
-    for (int col0 = 0; col0 < rank; col0 += kDeep * 32) {
-#pragma unroll
-      for (int k = 0; k < kDeep; ++k)
-        if (col0 + k * 32 < rank)
-          multiply<false, std::is_same<W, __half>::value, 3>(d, hs + g * S::kHPitch + (col0 + k * 32 + q * 8) * 2, S::kHPitch, kRows * S::kHPitch, last_term + 1, w + k * kSide, side);
-      if (col0 + kDeep * 32 < rank) load_b(o, col0 + kDeep * 32);
-      else if (o + kSide * kWarps < o1) load_b(o + kSide * kWarps, 0);
-    }
-#pragma unroll
-    for (int e = 0; e < 4; e += 2) {
-      if (g + e * 4 >= n) continue;
-      const long long at = (long long)t.rows[g + e * 4] * a.y_row;
-#pragma unroll
-      for (int j = 0; j < kSide; ++j)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int col = (o + j * kWarps) * 16 + h * 8 + q * 2;
-          if (j < side && col < a.oc) add_pair(a.y, a.y_dtype, at + col, d[j][h][e], d[j][h][e + 1]);
+          for (int j = 0; j < 4; ++j)
+            if (j < side) { f(to[row * pitch + j * 16], acc[j][b][e]); f(to[row * pitch + j * 16 + 8], acc[j][b][e + 2]); }
         }
+    };
+    if (kw >= half) each([](float& s, float v) { s = v; });
+    asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+    if (kw < half) each([](float& s, float v) { s += v; });
+    asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+    for (int row = warp; row < n; row += kWarps)
+      for (int r = lane; r < blocks * 16; r += 32) {
+        float s = part[row * pitch + r] + part[(kRows + row) * pitch + r];
+        if (half == 4) s += part[(2 * kRows + row) * pitch + r] + part[(3 * kRows + row) * pitch + r];
+        share[row * kMostRank + r] = s;
+      }
+    cluster.sync();
+
+    // ---- all of A x, as operands
+    const int last_term = a.y_dtype == RWKVQ_F32 ? 2 : 1;
+    const float scale = t.scale;
+    for (int row = warp; row < n; row += kWarps)
+#pragma unroll 1
+      for (int r = lane; r < blocks * 16; r += 32) {
+        float s = 0.f;
+        if (r < rank) {
+          float v[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = k < C ? cluster.map_shared_rank(share, k)[row * kMostRank + r] : 0.f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s += v[k];
+          s *= scale;
+        }
+        uint8_t* const to = xs + r / 64 * kXPiece + swizzled(row, r / 8 & 7) + (r & 7) * 2;
+        *reinterpret_cast<__nv_bfloat16*>(to) = term(s);
+        *reinterpret_cast<__nv_bfloat16*>(to + 2 * kXPiece) = last_term == 1 ? __float2bfloat16_rn(s) : term(s);
+        if (last_term == 2) *reinterpret_cast<__nv_bfloat16*>(to + 4 * kXPiece) = term(s);
+      }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+
+    // ---- B (A x) for this block's rows of B, sixteen of a tile's for each warp
+    i = n_a;
+    for (int o = o0; o < o1; ++o) {
+      float d[2][4] = {};
+      for (int k = 0; k < wide; ++k, ++i) {
+        take(i);
+        const uint32_t slot = ring + (uint32_t)(i % S::kSlots * kSlotBytes + warp * 2048);
+        const int steps = min(4, blocks - k * 4);
+        if (ok)
+#pragma unroll 1
+          for (int s = 0; s < steps; ++s) {
+            uint32_t x[3][4], w[1][4];
+            ldmatrix4(w[0], slot + swizzled(lane & 15, s * 2 + (lane >> 4)));
+            const uint32_t at_x = x_at + (uint32_t)(k * kXPiece) + (uint32_t)(((s * 2 + (lane >> 3 & 1)) ^ lane) & 7) * 16u;
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+              if (j <= last_term) ldmatrix4(x[j], at_x + (uint32_t)j * (2 * kXPiece));
+            const int left = rank - (k * 64 + s * 16);
+            if (left < 16) {        // what lies behind the adapter's rank may be anything
+              const uint32_t lo = q * 2 + 2 <= left ? ~0u : q * 2 + 1 <= left ? 0xFFFFu : 0u, hi = q * 2 + 10 <= left ? ~0u : q * 2 + 9 <= left ? 0xFFFFu : 0u;
+              w[0][0] &= lo; w[0][1] &= lo; w[0][2] &= hi; w[0][3] &= hi;
+            }
+            multiply<false, kWHalf, 3>(d, w[0], x, last_term + 1, both);
+          }
+        give(i);
+      }
+      if (!ok) break;
+      // y: all that is read first, then the sums
+      const int col = o * 128 + warp * 16 + g;
+      auto y_at = [&](int b, int e) { const int r = b * 8 + q * 2 + (e & 1); return (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row + col + (e >> 1) * 8; };
+      auto there = [&](int b, int e) { return b * 8 + q * 2 + (e & 1) < n && col + (e >> 1) * 8 < a.oc; };
+      if (a.y_dtype == RWKVQ_F32) {
+        // Each element of y is added to once in a call, so that a reduction in memory is as good as a load, an addition and a store, and nothing waits for it (it
+        // takes subnormal numbers for zeros).
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (there(b, e)) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(static_cast<float*>(a.y) + y_at(b, e)), "f"(d[b][e]) : "memory");
+      } else {
+        unsigned short* const y = static_cast<unsigned short*>(a.y);
+        unsigned short old[2][4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) old[b][e] = there(b, e) ? y[y_at(b, e)] : (unsigned short)0;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (there(b, e))
+              y[y_at(b, e)] = a.y_dtype == RWKVQ_F16 ? __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(old[b][e])) + d[b][e]))
+                                                     : __bfloat16_as_ushort(__float2bfloat16_rn(__bfloat162float(__ushort_as_bfloat16(old[b][e])) + d[b][e]));
+      }
     }
   }
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // no block ends while another reads its share
+  __syncthreads();
+  // a block that gave up leaves when its copies have arrived
+  if (ctrl.abort_flag && tid == 0)
+    for (int i = max(0, ctrl.asked - S::kSlots); i < ctrl.asked; ++i)
+      for (uint32_t k = 0; k < tc5::kPollLimit && !tc5::mbar_try_wait(full + (uint32_t)(i % S::kSlots) * 8u, (uint32_t)(i / S::kSlots) & 1u); ++k) {}
+}
+
+// [n][rows][cols] of 16-bit numbers as boxes of 64 columns x box_rows rows in the 128-byte swizzle; what lies outside reads as zero.
+bool encode(CUtensorMap* map, const void* at, bool half, int cols, int rows, int n, int box_rows) {
+  const tc5::EncodeTiledFn fn = tc5::encode_tiled();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)n}, strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * 2 * (cuuint64_t)rows};
+  const cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u}, step[3] = {1u, 1u, 1u};
+  return fn(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(at), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename X, typename W>
@@ -544,11 +632,13 @@ cudaError_t launch(Args p, long long items, cudaStream_t s) {
   static SmemOptIn opt_in(kCarveOut);
   cudaError_t e = opt_in((const void*)lowrank_kernel<X, W>, S::kBytes);
   if (e != cudaSuccess) return e;
-  const unsigned C = 8;
+  // blocks that are there at once, two an SM: clusters as wide as that allows
+  unsigned C = 8;
+  while (C > 1 && items * C > 2ll * sm_count()) C /= 2;
   // where there are few tiles, several clusters divide a tile's rows of B, and each multiplies A x for itself
-  p.splits = (int)std::max<long long>(1, std::min<long long>({2ll * sm_count() / (items * C), (p.a.oc + 16 * C * kWarps - 1) / (16 * C * kWarps), 16}));
+  p.splits = (int)std::max<long long>(1, std::min<long long>({2ll * sm_count() / (items * C), (p.a.oc + 128 * C - 1) / (128 * C), 16}));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = S::kBytes; cfg.stream = s;
+  cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(kAll); cfg.dynamicSmemBytes = S::kBytes; cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
@@ -605,6 +695,8 @@ rwkvq_status rwkvq_lowrank(const rwkvq_lowrank_args* args, const rwkvq_desc* mu_
   const long long full = ((long long)a.tokens + lr::kRows - 1) / lr::kRows;
   const long long items = a.seq_start ? std::min<long long>(a.tokens, full + a.n_seq) : a.n_seq == 1 ? full :
                           lr::by_groups(a) ? std::min<long long>(a.n_seq, a.n_adapters + full) : a.n_seq;
+  const bool half = a.w_dtype == RWKVQ_F16;
+  if (!lr::encode(&p.A, a.A, half, a.ic, a.rank, a.n_adapters, 16) || !lr::encode(&p.B, a.B, half, a.rank, a.oc, a.n_adapters, 128)) return cuda_status(cudaErrorUnknown);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (a.x_dtype == RWKVQ_F32) return cuda_status(lr::launch_x<float>(p, items, s));
   if (a.x_dtype == RWKVQ_F16) return cuda_status(lr::launch_x<__half>(p, items, s));
