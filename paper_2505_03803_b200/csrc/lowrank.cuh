@@ -1,0 +1,319 @@
+// What the kernels of low-rank adapters share: the rows of a tile, and numbers as operands of the tensor cores.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "../../include/rwkvq.h"
+#include "host_util.h"
+#include "tc5.cuh"
+
+namespace rwkvq {
+int* device_status_ptr();  // api_misc.cu
+namespace lr {
+
+constexpr int kThreads = 256, kWarps = 8, kRows = 16, kMostRank = 128, kMostCounted = 1024;
+
+struct alignas(64) Args {
+  rwkvq_lowrank_args a;
+  const uint8_t* mu;             // index stream of the token-shift vector, or nullptr
+  const uint32_t* mu_codebook;
+  int mu_bits, mu_entries;
+  int splits;                    // clusters to a tile
+  int* status;
+  int x_by_map;                  // x goes to shared memory as it is, through a map
+  CUtensorMap A[4], B, X;        // boxes of 64 columns x 16, 32, 64, 128 rows (as far as the rank goes); x 128 rows; x a tile's rows
+};
+
+// ---- rows of a tile -----------------------------------------------------------------------------------------
+struct Tile {
+  int rows[kRows];              // of groups of single rows
+  int first, n, seq, start;     // of others: row `first` on, of the sequence that begins at `start`
+  int adapter, rank;
+  float scale;
+};
+
+// The tile that is the item-th among all tiles of kTile rows of the sequences in seq_start; t.n stays 0 where there is none.  A sequence counts whose rows exist and that
+// does not begin in front of an earlier entry of the list; the others are left out.  All threads of the block, of which the first kThreads look.
+template <int kTile>
+__device__ __forceinline__ void find_in_list(const Args& p, long long item, Tile& t, int* scratch) {
+  const rwkvq_lowrank_args& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, each = (a.n_seq + kThreads - 1) / kThreads, i0 = min(tid * each, a.n_seq), i1 = min(i0 + each, a.n_seq);
+  int* const tops = scratch;             // of each warp
+  int* const sums = scratch + kWarps;
+  int top = 0;
+#pragma unroll 1
+  for (int i = i0; i < i1; ++i) top = max(top, a.seq_start[i]);
+  int upto = top;                        // most of this and the threads before
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(~0u, upto, o); if (lane >= o) upto = max(upto, v); }
+  if (lane == 31 && warp < kWarps) tops[warp] = upto;
+  __syncthreads();
+  int before = __shfl_up_sync(~0u, upto, 1);
+  if (lane == 0) before = 0;
+  for (int w = 0; w < min(warp, kWarps); ++w) before = max(before, tops[w]);
+  // f(i, start, end) for each sequence of this thread that counts, until it is true
+  auto each_one = [&](auto f) {
+    int run = before;
+    bool bad = false;
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) {
+      const int s = a.seq_start[i], e = a.seq_start[i + 1];
+      const bool ok = s >= run && s >= 0 && e >= s && e <= a.tokens;
+      bad |= !ok;
+      if (ok && f(i, s, e)) break;
+      run = max(run, s);
+    }
+    return bad;
+  };
+  int sum = 0;
+  if (each_one([&](int, int s, int e) { sum += (e - s + kTile - 1) / kTile; return false; })) atomicExch(p.status, (int)RWKVQ_EINVAL);
+  int at = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) { const int v = __shfl_up_sync(~0u, at, o); if (lane >= o) at += v; }
+  if (lane == 31 && warp < kWarps) sums[warp] = at;
+  __syncthreads();
+  at -= sum;
+  for (int w = 0; w < min(warp, kWarps); ++w) at += sums[w];
+  if (item >= at && item < at + sum)
+    each_one([&](int i, int s, int e) {
+      const int n = (e - s + kTile - 1) / kTile;
+      if (item < at + n) {
+        t.seq = i; t.start = s; t.first = s + (int)(item - at) * kTile; t.n = min(kTile, e - t.first);
+        return true;
+      }
+      at += n;
+      return false;
+    });
+}
+
+__host__ __device__ inline bool single_rows(const rwkvq_lowrank_args& a) { return !a.seq_start && a.n_seq > 1; }      // each row a sequence
+__host__ __device__ inline bool by_groups(const rwkvq_lowrank_args& a) { return a.n_seq <= kThreads && a.n_adapters <= kMostCounted; }
+
+// The rows of a tile of up to kTile; of single rows that share an adapter (then t.n is final, and adapter, rank and scale are known, too) or of a sequence.  All threads.
+// scratch: 2 * kWarps + 2 numbers; memory: 8 * kMostCounted bytes.
+template <int kTile>
+__device__ __forceinline__ void find_rows(const Args& p, long long item, Tile& t, int* scratch, void* memory) {
+  const rwkvq_lowrank_args& a = p.a;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) { t.n = 0; t.adapter = -1; }
+  if (!single_rows(a)) {
+    if (a.seq_start) {
+      __syncthreads();
+      find_in_list<kTile>(p, item, t, scratch);
+    } else if (tid == 0) {
+      t.seq = t.start = 0; t.first = (int)item * kTile; t.n = min(kTile, a.tokens - t.first);
+    }
+    __syncthreads();
+    return;
+  }
+  if constexpr (kTile == kRows) {
+    if (by_groups(a)) {
+      // Rows of the same adapter are taken sixteen at a time: the item-th of these groups, in the order of their first rows.  `table`: how many rows of an adapter each
+      // warp has, a byte each, from which a row knows how many are before it.
+      uint64_t* const table = static_cast<uint64_t*>(memory);
+      int* const heads = scratch;
+      const int mine = tid < a.n_seq ? a.adapter[tid] : -1;
+      for (int i = tid; i < a.n_adapters; i += kThreads) table[i] = 0;
+      const bool ok = mine >= 0 && mine < a.n_adapters;
+      if (!ok && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
+      const int rank = ok && a.ranks ? a.ranks[mine] : a.rank;
+      const float scale = ok && a.scale ? a.scale[mine] : 1.f;
+      const uint32_t same = __match_any_sync(~0u, mine), earlier = same & ((1u << lane) - 1);
+      __syncthreads();
+      if (ok && earlier == 0) reinterpret_cast<uint8_t*>(table + mine)[warp] = (uint8_t)__popc(same);
+      __syncthreads();
+      const uint64_t others = ok && warp > 0 ? table[mine] << (64 - 8 * warp) : 0ull;
+      const int before = (int)((others * 0x0101010101010101ull) >> 56) + __popc(earlier);
+      const bool leads = ok && before % kRows == 0;
+      const uint32_t vote = __ballot_sync(~0u, leads);
+      if (lane == 0) heads[warp] = __popc(vote);
+      __syncthreads();
+      int at = __popc(vote & ((1u << lane) - 1));
+      for (int w = 0; w < warp; ++w) at += heads[w];
+      if (leads && at == item) { t.adapter = mine; t.rank = rank; t.scale = scale; t.start = before; }
+      __syncthreads();
+      const int from = t.start;
+      const bool in = ok && mine == t.adapter && before >= from && before < from + kRows;
+      if (in) t.rows[before - from] = tid;
+      const int n = __syncthreads_count(in);
+      if (tid == 0 && t.adapter >= 0) {
+        t.n = t.rank < 0 || t.rank > a.rank ? 0 : t.rank == 0 ? 0 : n;
+        if (t.rank < 0 || t.rank > a.rank) atomicExch(p.status, (int)RWKVQ_EINVAL);
+      }
+    } else {
+      // many rows: an item is a row, which takes the next fifteen of its adapter if it is the first, seventeenth, ... of these
+      const int mine = a.adapter[item];
+      int before = 0;
+      for (int i = tid; i < item && tid < kThreads; i += kThreads) before += a.adapter[i] == mine;
+      for (int o = 16; o > 0; o /= 2) before += __shfl_xor_sync(~0u, before, o);
+      if (lane == 0 && warp < kWarps) scratch[warp] = before;
+      __syncthreads();
+      before = 0;
+      for (int w = 0; w < kWarps; ++w) before += scratch[w];
+      if (before % kRows == 0 && tid < 32 && mine != -1) {
+        int n = 0;
+        for (int i0 = (int)item; i0 < a.n_seq && n < kRows; i0 += 32) {
+          const int i = i0 + tid;
+          const uint32_t same = __ballot_sync(~0u, i < a.n_seq && a.adapter[i] == mine);
+          const int at = n + __popc(same & ((1u << tid) - 1));
+          if ((same >> tid & 1) && at < kRows) t.rows[at] = i;
+          n = min(kRows, n + __popc(same));
+        }
+        if (tid == 0) { t.n = n; t.seq = (int)item; }
+      }
+    }
+  }
+  __syncthreads();
+}
+
+// Adapter, rank and scale of a tile whose rows are known, by one thread; t.n is 0 where it has none.
+__device__ __forceinline__ void find_adapter(const Args& p, Tile& t) {
+  const rwkvq_lowrank_args& a = p.a;
+  if (t.n == 0 || t.adapter >= 0) return;
+  const int mine = a.adapter[t.seq];
+  bool bad = mine < -1 || mine >= a.n_adapters;
+  if (!bad && mine >= 0) {
+    const int rank = a.ranks ? a.ranks[mine] : a.rank;
+    const float scale = a.scale ? a.scale[mine] : 1.f;
+    bad = rank < 0 || rank > a.rank;
+    if (rank > 0) { t.adapter = mine; t.rank = rank; t.scale = scale; }
+  }
+  if (bad) atomicExch(p.status, (int)RWKVQ_EINVAL);
+  if (bad || t.adapter < 0) t.n = 0;
+}
+
+// ---- numbers and operands -----------------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ float to_float(T x);
+template <> __device__ __forceinline__ float to_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ float to_float<__half>(__half x) { return __half2float(x); }
+template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+template <typename T> struct Eight { T v[8]; };
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float* f) {
+  if constexpr (sizeof(T) == 4) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  } else {
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    const Eight<T> e = *reinterpret_cast<const Eight<T>*>(&w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = to_float<T>(e.v[i]);
+  }
+}
+
+// The next bf16 term of x, which is left with what the term leaves.  Cut off, not rounded, so that the largest numbers do not become infinite; of an infinity or
+// NaN nothing is left.
+__device__ __forceinline__ __nv_bfloat16 term(float& x) {
+  const uint32_t b = __float_as_uint(x);
+  const float hi = __uint_as_float((b & 0x7F800000u) == 0x7F800000u ? (b & 0x007FFFFFu ? b | 0x00400000u : b) & 0xFFFF0000u : b & 0xFFFF0000u);
+  x = (b & 0x7F800000u) == 0x7F800000u ? 0.f : x - hi;
+  return __ushort_as_bfloat16((unsigned short)(__float_as_uint(hi) >> 16));
+}
+
+// A pair of f16 weights as two pairs of bf16: eleven bits are eight and three.  (Of an infinity the second is NaN.)
+__device__ __forceinline__ void apart(uint32_t w, uint32_t& hi, uint32_t& lo) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+  const uint32_t x = __float_as_uint(f.x), y = __float_as_uint(f.y);
+  hi = __byte_perm(x, y, 0x7632);
+  const __nv_bfloat162 l = __floats2bfloat162_rn(f.x - __uint_as_float(x & 0xFFFF0000u), f.y - __uint_as_float(y & 0xFFFF0000u));
+  lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+
+// How x and the weights go into the tensor cores.
+template <typename X, typename W> struct Form {
+  static constexpr bool kHalf = std::is_same<X, __half>::value && std::is_same<W, __half>::value;
+  static constexpr int kX = std::is_same<X, W>::value ? 1 : std::is_same<X, float>::value ? 3 : std::is_same<X, __half>::value ? 2 : 1;
+  static constexpr bool kApart = std::is_same<W, __half>::value && !kHalf;
+};
+
+// The token-shift vector's pairs of columns col to col + 7 (col a multiple of 8), whose indices are four times mu_bits neighbouring bits from a byte's beginning.
+__device__ __forceinline__ void mu_eight(const Args& p, const uint32_t* codebook, int col, float2 (&m)[4]) {
+  const uint32_t byte = (uint32_t)(col >> 3) * (uint32_t)p.mu_bits >> 1, shift = (byte & 3u) * 8u;
+  const uint32_t* const words = reinterpret_cast<const uint32_t*>(p.mu) + (byte >> 2);
+  const uint32_t lo = __ldg(words), hi = shift + 4u * (uint32_t)p.mu_bits > 32u ? __ldg(words + 1) : 0u, f = __funnelshift_r(lo, hi, shift), mask = (1u << p.mu_bits) - 1u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t pair = codebook[f >> (uint32_t)(j * p.mu_bits) & mask];
+    m[j] = __half22float2(*reinterpret_cast<const __half2*>(&pair));
+  }
+}
+
+// Byte offset of 16 bytes (eight columns) in rows of 128 bytes under the 128-byte swizzle.
+__device__ __forceinline__ uint32_t swizzled(int row, int eight) { return (uint32_t)(row * 128 + ((eight ^ row) & 7) * 16); }
+// A box of a tensor map by a converged warp, of which one lane is elected by predicate: from a branch of one lane each took some 145 cycles.
+__device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
+               " @q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n}"
+               ::"r"(dst_smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+
+// x_mix of eight columns of a row, in fp32 but rounded to X.
+template <typename X>
+__device__ __forceinline__ void mixed_eight(const Args& p, const uint32_t* codebook, int row, int col, const X* before, float (&x)[8]) {
+  load8(static_cast<const X*>(p.a.x) + (long long)row * p.a.x_row + col, x);
+  if (!p.mu) return;
+  float y[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) y[j] = 0.f;
+  if (before) load8(before + col, y);
+  float2 m[4];
+  mu_eight(p, codebook, col, m);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m[j].x, x[2 * j])));
+    x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m[j].y, x[2 * j + 1])));
+  }
+}
+// The row in front of a row, nullptr where there is none.
+template <typename X>
+__device__ __forceinline__ const X* row_before(const Args& p, int row, int seq, bool begins) {
+  if (p.a.x_prev) return static_cast<const X*>(p.a.x_prev) + (long long)row * p.a.x_prev_row;
+  if (!begins) return static_cast<const X*>(p.a.x) + (long long)(row - 1) * p.a.x_row;
+  return p.a.xprev0 ? static_cast<const X*>(p.a.xprev0) + (long long)seq * p.a.ic : nullptr;
+}
+// Eight numbers as operands of the tensor cores: the k-th term of each.
+template <typename F>
+__device__ __forceinline__ uint4 next_term(float (&x)[8]) {
+  uint32_t v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (F::kHalf) {
+      const __half2 h = __floats2half2_rn(x[2 * j], x[2 * j + 1]);
+      v[j] = *reinterpret_cast<const uint32_t*>(&h);
+    } else if constexpr (F::kX == 1) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+      v[j] = *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+      __nv_bfloat162 h;
+      h.x = term(x[2 * j]); h.y = term(x[2 * j + 1]);
+      v[j] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+// [n][rows][cols] of 16-bit numbers as boxes of 64 columns x box_rows rows in the 128-byte swizzle; what lies outside reads as zero.
+inline bool encode(CUtensorMap* map, const void* at, bool half, int cols, int rows, int n, int box_rows) {
+  const tc5::EncodeTiledFn fn = tc5::encode_tiled();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)n}, strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * 2 * (cuuint64_t)rows};
+  const cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, 1u}, step[3] = {1u, 1u, 1u};
+  return fn(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(at), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tiles on the tcgen05 tensor cores (lowrank_tile.cu): whether they take operands of these types, and a launch (p complete but for maps and clusters).
+bool tiles_take(int x_dtype, int w_dtype);
+cudaError_t launch_tiles(Args& p, cudaStream_t s);
+
+}  // namespace lr
+}  // namespace rwkvq

@@ -1,0 +1,478 @@
+// Low-rank adapters on the tcgen05 tensor cores: tiles of up to 64 rows of a sequence, or of up to sixteen rows that share an adapter.
+//
+// The rows are the 16- to 64-column operand and the weights the 128-row one: A x is one accumulator of 128 (of the rank) by the tile's rows, B (A x) one for each 128 rows
+// of B, whose lanes are neighbouring columns of y.  A cluster of blocks divides the columns of A and the rows of B; A x is summed over the blocks through distributed
+// shared memory in their order.  Weights come through tensor maps into a ring of seven slots, B's under the meeting of the blocks; x through a map, too, or, where
+// it has to be mixed with the row before or taken apart into bf16 terms (f16: two, f32: three), by the warps that read the accumulators later.
+//
+// A x goes on in bf16 terms (three, all of it, where y has 32 bits; two, the second rounded, where y has 16: off by up to 2^-16 of it), or, where the weights are f16, in
+// two f16 terms under a power of two per row that brings its largest number to 2^14 (off by up to 2^-22 of it, or 2^-38 of the row's largest).
+//
+// A block takes all of an SM's shared memory, so that no other one that wants tensor memory is beside it: tcgen05.alloc has no limit to its wait, and a block
+// that holds tensor memory waits for the others of its cluster.
+#include <cooperative_groups.h>
+
+#include "lowrank.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace rwkvq {
+namespace lr {
+
+using tc5::smem_u32;
+
+constexpr int kTileAll = kThreads + 64;                            // eight warps that make operands and read accumulators, one that asks for copies, one that multiplies
+constexpr int kRing = 7, kSlotBytes = 16 << 10, kMostXSlots = 16, kMostAcc = 4;
+constexpr int kSmemBytes = 224 << 10;
+
+template <typename X, typename W, int NT>
+struct TileShape {
+  static constexpr int kTerms = Form<X, W>::kX, kTileBytes = NT * 128, kPieceBytes = kTerms * kTileBytes;      // a piece: 64 columns of the tile's rows, a tile for each term
+  static constexpr int kXSlots = NT == 64 ? (kTerms == 1 ? 8 : kTerms == 2 ? 4 : 3) : (kTerms < 3 ? 16 : 12);
+  static constexpr int kXBytes = kXSlots * kPieceBytes, kShare = NT * kMostRank * 4;
+  static constexpr int kGroup = NT == 64 ? 2 : 8, kPer = kGroup * NT * 8 / kThreads;      // pieces that are made at once, and eights of columns of them for each thread
+  static constexpr int kAcc = NT == 64 ? 2 : 4, kTmemCols = NT == 64 ? 256 : 128;
+  static_assert(kXBytes >= 6 * kTileBytes, "A x takes x's place");
+  static_assert(1024 + kRing * kSlotBytes + kXBytes + kShare + 1024 <= kSmemBytes, "shared memory");
+  static_assert(kShare >= 8 * kMostCounted || NT == 64, "room for counting the rows of adapters");
+};
+struct TileCtrl {
+  uint64_t full[kRing], empty[kRing], xfull[kMostXSlots], xempty[kMostXSlots], a_done, h_ready, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
+  int abort_flag, asked, x_asked;
+  uint32_t tmem_base;
+  float back[64];                 // of each row: the power of two that its A x was divided by
+};
+
+// Both operands of a type (bf16, or f16), K-major -> fp32, 128 x N.
+__device__ __forceinline__ constexpr uint32_t idesc_of(bool half, int N) {
+  return (1u << 4) | (half ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
+}
+// Sixteen columns of both operands, by a converged warp.
+__device__ __forceinline__ void umma(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+  asm volatile("{\n .reg .pred q, p;\n elect.sync _|q, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
+               " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
+}
+// 32 lanes x kCols columns; see tc5::tmem_ld32_issue.  Waits for them.
+template <int kCols>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[kCols]) {
+  if constexpr (kCols == 32) {
+    tc5::tmem_ld32_issue(taddr, r);
+    tc5::tmem_ld_wait(r);
+  } else {
+    static_assert(kCols == 8, "");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]) :: "memory");
+  }
+}
+__device__ __forceinline__ void tensor_g2s_2d(uint32_t dst_smem, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
+               " @q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n}"
+               ::"r"(dst_smem), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t pair_bits(__nv_bfloat16 x, __nv_bfloat16 y) { return (uint32_t)__bfloat16_as_ushort(x) | (uint32_t)__bfloat16_as_ushort(y) << 16; }
+__device__ __forceinline__ uint32_t pair_bits(__half x, __half y) { return (uint32_t)__half_as_ushort(x) | (uint32_t)__half_as_ushort(y) << 16; }
+
+template <typename X, typename W, int NT>
+__global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_constant__ Args p) {
+  using S = TileShape<X, W, NT>;
+  using F = Form<X, W>;
+  constexpr bool kHalf = std::is_same<W, __half>::value;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
+  __shared__ Tile t;
+  __shared__ TileCtrl ctrl;
+  __shared__ int scratch[2 * kWarps + 2];
+  uint8_t* const xs = smem + kRing * kSlotBytes;                         // [slot][term][row][64 columns], then A x: [term][64 of the rank][row][64]
+  float* const share = reinterpret_cast<float*>(xs + S::kXBytes);        // this block's share of A x: [row][rank]
+  uint32_t* const codebook = reinterpret_cast<uint32_t*>(share + S::kShare / 4);
+  const rwkvq_lowrank_args& a = p.a;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  volatile int* const abortp = &ctrl.abort_flag;
+  asm volatile("griddepcontrol.launch_dependents;");
+  if (tid == 0) {
+    for (int i = 0; i < kRing; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], 1); }
+    for (int i = 0; i < S::kXSlots; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : kWarps); tc5::mbar_init(&ctrl.xempty[i], 1); }
+    for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], kWarps); }
+    tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.h_ready, kWarps); tc5::mbar_init(&ctrl.drained, 1);
+    ctrl.abort_flag = ctrl.asked = ctrl.x_asked = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\nfence.proxy.async.shared::cta;" ::: "memory");
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (p.mu)
+    for (int i = tid; i < p.mu_entries; i += kTileAll) codebook[i] = p.mu_codebook[i];
+  const int id = (int)(blockIdx.x / C), item = id / p.splits, split = id - item * p.splits;
+  find_rows<NT>(p, item, t, scratch, share);
+  const int n = t.n;
+  const bool grouped = NT == kRows && single_rows(a);
+  const int pieces = (a.ic + 63) / 64, k0 = (int)((long long)pieces * c / C), np = (int)((long long)pieces * (c + 1) / C) - k0;
+  const int tiles = (a.oc + 127) / 128, parts = C * p.splits, at = split * C + c;
+  const int o0 = (int)((long long)tiles * at / parts), o1 = (int)((long long)tiles * (at + 1) / parts);
+  const uint32_t ring = smem_u32(smem), xring = smem_u32(xs), full = smem_u32(ctrl.full), empty = smem_u32(ctrl.empty), xfull = smem_u32(ctrl.xfull), xempty = smem_u32(ctrl.xempty);
+  bool ok = true;
+  auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && tc5::mbar_wait(bar, parity, abortp, p.status); };
+  auto row_of = [&](int r) { return grouped ? t.rows[r] : t.first + r; };
+
+  // pieces [g0, g0 + kGroup) of x in operand form
+  auto stage_x = [&](int g0) {
+    float x[S::kPer][8];
+#pragma unroll
+    for (int j = 0; j < S::kPer; ++j) {
+      const int e = tid + j * kThreads, piece = g0 + e / (NT * 8), r = e / 8 % NT, col = (k0 + piece) * 64 + (e & 7) * 8;
+      if (r < n && piece < np && col < a.ic) {
+        const int row = row_of(r);
+        mixed_eight(p, codebook, row, col, row_before<X>(p, row, grouped ? row : t.seq, grouped || row == t.start), x[j]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
+      }
+    }
+    if (g0 >= S::kXSlots)
+      for (int i = g0; i < min(g0 + S::kGroup, np); ++i) wait(xempty + (uint32_t)(i % S::kXSlots) * 8u, (uint32_t)(i / S::kXSlots - 1) & 1u);
+#pragma unroll
+    for (int j = 0; j < S::kPer; ++j) {
+      const int e = tid + j * kThreads, piece = g0 + e / (NT * 8), r = e / 8 % NT;
+      if (r < n && piece < np && ok)
+#pragma unroll
+        for (int k = 0; k < F::kX; ++k)
+          *reinterpret_cast<uint4*>(xs + piece % S::kXSlots * S::kPieceBytes + k * S::kTileBytes + swizzled(r, e & 7)) = next_term<F>(x[j]);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0)
+      for (int i = g0; i < min(g0 + S::kGroup, np); ++i) tc5::mbar_arrive(xfull + (uint32_t)(i % S::kXSlots) * 8u);
+  };
+  if (warp == kWarps) {
+    if (lane == 0) find_adapter(p, t);
+  } else if (warp == kWarps + 1) {
+    tc5::tmem_alloc(&ctrl.tmem_base, S::kTmemCols);
+  } else {
+    if (!p.x_by_map && np > 0 && n > 0) stage_x(0);
+    // y's rows, which are needed last, on their way to the second-level cache
+    const int y_bytes = (min(o1 * 128, a.oc) - o0 * 128) * (a.y_dtype == RWKVQ_F32 ? 4 : 2);
+    if (tid < n && y_bytes > 0)
+      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(a.y) + ((long long)row_of(tid) * a.y_row + o0 * 128) * (a.y_dtype == RWKVQ_F32 ? 4 : 2)), "r"(y_bytes) : "memory");
+  }
+  tc5::tc_fence_before();
+  __syncthreads();
+  tc5::tc_fence_after();
+  const uint32_t tmem = ctrl.tmem_base;
+  if (t.n == 0) {                // the same for all blocks of the cluster
+    if (warp == kWarps + 1) tc5::tmem_dealloc(tmem, S::kTmemCols);
+    return;
+  }
+  const int rank = t.rank, blocks = (rank + 15) / 16, wide = (rank + 63) / 64;
+  const int a_slot = 8 / (blocks == 1 ? 1 : blocks == 2 ? 2 : blocks <= 4 ? 4 : 8), n_a = (np + a_slot - 1) / a_slot;      // pieces of A in a slot
+  const int last_term = kHalf ? 1 : a.y_dtype == RWKVQ_F32 ? 2 : 1;
+
+  if (warp == kWarps) {
+    // ---- copies.  This warp and the next bring nothing to the first meeting of the cluster and do not hold it up: what they wait for below comes behind it.
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const int total = n_a + (o1 - o0) * wide;
+    int i = 0, px = 0;
+#pragma unroll 1
+    for (; i < total; ++i) {
+      const uint32_t st = (uint32_t)(i % kRing), bar = full + st * 8u, dst = ring + st * kSlotBytes;
+      if (i >= kRing) wait(empty + st * 8u, (uint32_t)(i / kRing - 1) & 1u);
+      if (!__all_sync(~0u, ok)) break;
+      if (i < n_a) {
+        const int first = i * a_slot, count = min(a_slot, np - first);
+        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[st], (uint32_t)(count * blocks) * 2048u);
+        __syncwarp();
+#pragma unroll 1
+        for (int j = 0; j < count; ++j) {
+          // as few boxes as the rank has binary digits
+          int r = 0;
+#pragma unroll
+          for (int h = 3; h >= 0; --h)
+            if (blocks >> h & 1) {
+              tensor_g2s(dst + (uint32_t)((j * blocks + r) * 2048), &p.A[h], (k0 + first + j) * 64, r * 16, t.adapter, bar);
+              r += 1 << h;
+            }
+        }
+        if (p.x_by_map)
+#pragma unroll 1
+          for (; px < first + count; ++px) {
+            const uint32_t xst = (uint32_t)(px % S::kXSlots);
+            if (px >= S::kXSlots) wait(xempty + xst * 8u, (uint32_t)(px / S::kXSlots - 1) & 1u);
+            if (!__all_sync(~0u, ok)) break;
+            if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.xfull[xst], S::kTileBytes);
+            __syncwarp();
+            tensor_g2s_2d(xring + xst * S::kPieceBytes, &p.X, (k0 + px) * 64, t.first, xfull + xst * 8u);
+          }
+      } else {
+        const int j = i - n_a, tile = j / wide;
+        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[st], kSlotBytes);
+        __syncwarp();
+        tensor_g2s(dst, &p.B, (j - tile * wide) * 64, (o0 + tile) * 128, t.adapter, bar);
+      }
+    }
+    if (lane == 0) { ctrl.asked = i; ctrl.x_asked = px; }
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
+  } else if (warp == kWarps + 1) {
+    // ---- products
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const uint64_t ring_desc = tc5::smem_desc_sw128(ring), x_desc = tc5::smem_desc_sw128(xring);
+    constexpr uint32_t kA = idesc_of(F::kHalf, NT), kB = idesc_of(kHalf, NT);
+#pragma unroll 1
+    for (int i = 0, px = 0; i < n_a; ++i) {
+      const uint32_t st = (uint32_t)(i % kRing);
+      wait(full + st * 8u, (uint32_t)(i / kRing) & 1u);
+#pragma unroll 1
+      for (int j = 0; j < a_slot && px < np; ++j, ++px) {
+        const uint32_t xst = (uint32_t)(px % S::kXSlots);
+        wait(xfull + xst * 8u, (uint32_t)(px / S::kXSlots) & 1u);
+        if (!__all_sync(~0u, ok)) break;
+        tc5::tc_fence_after();
+        const uint64_t w = ring_desc + (st * kSlotBytes + (uint32_t)(j * blocks) * 2048u >> 4), x = x_desc + (xst * S::kPieceBytes >> 4);
+#pragma unroll
+        for (int k = F::kX - 1; k >= 0; --k)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) umma(tmem, w + s * 2, x + (uint32_t)(k * S::kTileBytes / 16 + s * 2), kA, px > 0 || k < F::kX - 1 || s > 0);
+        tc5::umma_commit(&ctrl.xempty[xst]);
+      }
+      if (!__all_sync(~0u, ok)) break;
+      tc5::umma_commit(&ctrl.empty[st]);
+    }
+    if (__all_sync(~0u, ok)) tc5::umma_commit(&ctrl.a_done);
+    wait(smem_u32(&ctrl.h_ready), 0);
+    int i = n_a;
+#pragma unroll 1
+    for (int o = 0; o < o1 - o0; ++o) {
+      const uint32_t acc = (uint32_t)(o % S::kAcc), d = tmem + NT + acc * NT;
+      wait(smem_u32(&ctrl.empty_acc[acc]), (uint32_t)(o / S::kAcc + 1) & 1u);
+#pragma unroll 1
+      for (int k = 0; k < wide; ++k, ++i) {
+        const uint32_t st = (uint32_t)(i % kRing);
+        wait(full + st * 8u, (uint32_t)(i / kRing) & 1u);
+        if (!__all_sync(~0u, ok)) break;
+        const int steps = min(4, blocks - k * 4), tail = rank - k * 64;
+        if (tail < steps * 16) {
+          // what lies behind the adapter's rank may be anything: up to where the last sixteen columns end, zeros
+          uint8_t* const slot = smem + st * kSlotBytes;
+#pragma unroll 1
+          for (int e = tail / 8; e < steps * 2; ++e) {
+            const int keep = max(tail - e * 8, 0);
+            auto of = [keep](int j) { return keep >= 2 * j + 2 ? ~0u : keep == 2 * j + 1 ? 0xFFFFu : 0u; };
+#pragma unroll 1
+            for (int r = lane; r < 128; r += 32) {
+              uint4* const v = reinterpret_cast<uint4*>(slot + swizzled(r, e));
+              const uint4 old = *v;
+              *v = make_uint4(old.x & of(0), old.y & of(1), old.z & of(2), old.w & of(3));
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+        tc5::tc_fence_after();
+        const uint64_t w = ring_desc + (st * kSlotBytes >> 4), h = x_desc + (uint32_t)(k * S::kTileBytes / 16);
+        for (int j = last_term; j >= 0; --j)
+#pragma unroll 1
+          for (int s = 0; s < steps; ++s) umma(d, w + (uint32_t)(s * 2), h + (uint32_t)(j * wide * S::kTileBytes / 16 + s * 2), kB, k > 0 || j < last_term || s > 0);
+        tc5::umma_commit(&ctrl.empty[st]);
+      }
+      if (!__all_sync(~0u, ok)) break;
+      tc5::umma_commit(&ctrl.full_acc[acc]);
+    }
+    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
+  } else {
+    if (!p.x_by_map)
+#pragma unroll 1
+      for (int g = S::kGroup; g < np; g += S::kGroup) stage_x(g);
+    // ---- this block's share of A x: lanes are the rank
+    constexpr int kCols = NT / 2;
+    const int quarter = warp & 3, col0 = (warp >> 2) * kCols;
+    const uint32_t lanes = tmem + ((uint32_t)quarter << 21) + (uint32_t)col0;
+    uint32_t v[kCols];
+    if (np > 0) {
+      wait(smem_u32(&ctrl.a_done), 0);
+      tc5::tc_fence_after();
+    }
+    if (quarter * 32 < blocks * 16) {
+      if (np > 0) {
+        tmem_ld<kCols>(lanes, v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) v[j] = 0;
+      }
+#pragma unroll
+      for (int j = 0; j < kCols; ++j)
+        if (col0 + j < n) share[(col0 + j) * kMostRank + quarter * 32 + lane] = __uint_as_float(v[j]);
+    }
+    tc5::tc_fence_before();
+    cluster.sync();
+
+    // ---- all of A x, as operands: as many lanes to a row as there are fours of the rank
+    const int wl = blocks == 1 ? 4 : blocks == 2 ? 8 : blocks <= 4 ? 16 : 32, r4 = lane % wl * 4;
+    const float scale = t.scale;
+#pragma unroll 1
+    for (int row0 = warp * (32 / wl); row0 < n; row0 += kWarps * (32 / wl)) {
+      const int row = row0 + lane / wl;
+      float h[4] = {0.f, 0.f, 0.f, 0.f};
+      if (row < n && r4 < rank) {
+        float4 s[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < C) s[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(share, k) + row * kMostRank + r4);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < C) { h[0] += s[k].x; h[1] += s[k].y; h[2] += s[k].z; h[3] += s[k].w; }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = r4 + j < rank ? h[j] * scale : 0.f;
+      }
+      uint8_t* const to = xs + r4 / 64 * S::kTileBytes + swizzled(row, r4 / 8 & 7) + (r4 & 4) * 2;
+      const bool there = row < n && r4 < blocks * 16;
+      if constexpr (kHalf) {
+        float top = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
+        for (int o = 1; o < wl; o *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+        // 2^up brings the largest number to 2^14; an infinity or NaN stays what it is
+        const int up = top > 0.f && top < INFINITY ? min(14 - ilogbf(top), 126) : 0;
+        const float by = __uint_as_float((uint32_t)(127 + max(up, -126)) << 23);
+        if (there && r4 == 0) ctrl.back[row] = __uint_as_float((uint32_t)(127 - max(up, -126)) << 23);
+        __half hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float x = h[j] * by;
+          hi[j] = __float2half_rn(x);
+          lo[j] = fabsf(x) < INFINITY ? __float2half_rn(x - __half2float(hi[j])) : __float2half_rn(0.f);
+        }
+        if (there) {
+          *reinterpret_cast<uint2*>(to) = make_uint2(pair_bits(hi[0], hi[1]), pair_bits(hi[2], hi[3]));
+          *reinterpret_cast<uint2*>(to + wide * S::kTileBytes) = make_uint2(pair_bits(lo[0], lo[1]), pair_bits(lo[2], lo[3]));
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          if (k > last_term) continue;
+          __nv_bfloat16 b[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) b[j] = k == 1 && last_term == 1 ? __float2bfloat16_rn(h[j]) : term(h[j]);
+          if (there) *reinterpret_cast<uint2*>(to + k * wide * S::kTileBytes) = make_uint2(pair_bits(b[0], b[1]), pair_bits(b[2], b[3]));
+        }
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) tc5::mbar_arrive(&ctrl.h_ready);
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+
+    // ---- y, 32 columns of it for a warp, as many rows as half a tile
+#pragma unroll 1
+    for (int o = 0; o < o1 - o0; ++o) {
+      const uint32_t acc = (uint32_t)(o % S::kAcc);
+      const int col = (o0 + o) * 128 + quarter * 32 + lane;
+      const bool there = col < a.oc;
+      unsigned short old[kCols];
+      unsigned short* const y16 = static_cast<unsigned short*>(a.y) + col;
+      if (a.y_dtype != RWKVQ_F32) {
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+          if (there && col0 + j < n) old[j] = y16[(long long)row_of(col0 + j) * a.y_row];
+      }
+      wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / S::kAcc) & 1u);
+      if (!__all_sync(~0u, ok)) break;
+      tc5::tc_fence_after();
+      tmem_ld<kCols>(lanes + NT + acc * NT, v);
+      tc5::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc5::mbar_arrive(&ctrl.empty_acc[acc]);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) {
+        const int r = col0 + j;
+        if (!there || r >= n) continue;
+        const float d = kHalf ? __uint_as_float(v[j]) * ctrl.back[r] : __uint_as_float(v[j]);
+        const long long at_y = (long long)row_of(r) * a.y_row;
+        if (a.y_dtype == RWKVQ_F32) {
+          // Each element of y is added to once in a call, so that a reduction in memory is as good as a load, an addition and a store, and nothing waits for it (it
+          // takes subnormal numbers for zeros).
+          asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(static_cast<float*>(a.y) + at_y + col), "f"(d) : "memory");
+        } else if (a.y_dtype == RWKVQ_F16) {
+          y16[at_y] = __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(old[j])) + d));
+        } else {
+          y16[at_y] = __bfloat16_as_ushort(__float2bfloat16_rn(__bfloat162float(__ushort_as_bfloat16(old[j])) + d));
+        }
+      }
+    }
+  }
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // no block ends while another reads its share
+  tc5::tc_fence_before();
+  __syncthreads();
+  tc5::tc_fence_after();
+  if (ctrl.abort_flag) {
+    // a block that gave up leaves when its copies have arrived and the tensor core is done
+    auto arrived = [](uint32_t bar, uint32_t parity) {
+      for (uint32_t k = 0; k < tc5::kPollLimit && !tc5::mbar_try_wait(bar, parity); ++k) {}
+    };
+    if (tid == 0) {
+      for (int i = max(0, ctrl.asked - kRing); i < ctrl.asked; ++i) arrived(full + (uint32_t)(i % kRing) * 8u, (uint32_t)(i / kRing) & 1u);
+      for (int i = max(0, ctrl.x_asked - S::kXSlots); i < ctrl.x_asked; ++i) arrived(xfull + (uint32_t)(i % S::kXSlots) * 8u, (uint32_t)(i / S::kXSlots) & 1u);
+    }
+    if (warp == kWarps + 1) {
+      tc5::umma_commit(&ctrl.drained);
+      arrived(smem_u32(&ctrl.drained), 0);
+    }
+    __syncthreads();
+  }
+  if (warp == kWarps + 1) tc5::tmem_dealloc(tmem, S::kTmemCols);
+}
+
+template <typename X, typename W, int NT>
+cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
+  using S = TileShape<X, W, NT>;
+  const rwkvq_lowrank_args& a = p.a;
+  const bool half = a.w_dtype == RWKVQ_F16;
+  for (int h = 0; h < 4 && (h == 0 || (a.rank + 15) / 16 >= 1 << h); ++h)
+    if (!encode(&p.A[h], a.A, half, a.ic, a.rank, a.n_adapters, 16 << h)) return cudaErrorUnknown;
+  if (!encode(&p.B, a.B, half, a.rank, a.oc, a.n_adapters, 128)) return cudaErrorUnknown;
+  p.x_by_map = !p.mu && S::kTerms == 1 && !(NT == kRows && single_rows(a));
+  if (p.x_by_map) {
+    const cuuint64_t dims[2] = {(cuuint64_t)a.ic, (cuuint64_t)a.tokens}, strides[1] = {(cuuint64_t)(a.tokens > 1 ? a.x_row : a.ic) * 2};
+    const cuuint32_t box[2] = {64u, (cuuint32_t)NT}, step[2] = {1u, 1u};
+    const tc5::EncodeTiledFn fn = tc5::encode_tiled();
+    if (!fn || fn(&p.X, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.x), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return cudaErrorUnknown;
+  }
+  static SmemOptIn opt_in(kCarveOut);
+  const cudaError_t e = opt_in((const void*)lowrank_tile_kernel<X, W, NT>, kSmemBytes);
+  if (e != cudaSuccess) return e;
+  // one block an SM: clusters as wide as that allows, then several that divide a tile's rows of B and each multiply A x for themselves
+  const long long sms = sm_count();
+  unsigned C = 8;
+  while (C > 1 && items * C > sms) C /= 2;
+  p.splits = (int)std::max<long long>(1, std::min<long long>({sms / (items * C), (a.oc + 128ll * C - 1) / (128 * C), 16}));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(kTileAll); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, lowrank_tile_kernel<X, W, NT>, p);
+}
+template <typename X, typename W>
+cudaError_t launch_form(Args& p, cudaStream_t s) {
+  const rwkvq_lowrank_args& a = p.a;
+  auto tiles = [&](int rows) {
+    const long long whole = ((long long)a.tokens + rows - 1) / rows;
+    return a.seq_start ? std::min<long long>(a.tokens, whole + a.n_seq) : !single_rows(a) ? whole : by_groups(a) ? std::min<long long>(a.n_seq, a.n_adapters + whole) : (long long)a.n_seq;
+  };
+  // tiles of 64 rows where sequences have half of that and more on average
+  if (!single_rows(a) && a.tokens >= 32ll * a.n_seq) return launch_tile<X, W, 64>(p, tiles(64), s);
+  return launch_tile<X, W, kRows>(p, tiles(kRows), s);
+}
+
+bool tiles_take(int x_dtype, int w_dtype) { return w_dtype == RWKVQ_BF16 || x_dtype == RWKVQ_F16; }
+cudaError_t launch_tiles(Args& p, cudaStream_t s) {
+  if (p.a.w_dtype == RWKVQ_F16) return launch_form<__half, __half>(p, s);
+  if (p.a.x_dtype == RWKVQ_F32) return launch_form<float, __nv_bfloat16>(p, s);
+  if (p.a.x_dtype == RWKVQ_F16) return launch_form<__half, __nv_bfloat16>(p, s);
+  return launch_form<__nv_bfloat16, __nv_bfloat16>(p, s);
+}
+
+}  // namespace lr
+}  // namespace rwkvq
