@@ -108,27 +108,23 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
   const uint32_t ring = tc5::smem_u32(smem), full = tc5::smem_u32(ctrl.full), empty = tc5::smem_u32(ctrl.empty);
 
   // x of columns [kp, ke), pieces of 64, in operand form
-  auto stage_x = [&](int kp, int ke) {
+  auto stage_x = [&](auto mix, int kp, int ke) {
     const int eights = (ke - kp) * 8;
 #pragma unroll 1
     for (int e = tid; e < n * eights; e += kThreads) {
-      const int r = e / eights, eight = e - r * eights, col = kp * 64 + eight * 8;
+      const int r = e / eights, eight = e - r * eights, col = kp * 64 + eight * 8, row = grouped ? t.rows[r] : t.first + r;
+      const Eights<X> raw = load_eights<X, decltype(mix)::value>(p, row, grouped ? row : t.seq, grouped || row == t.start, col);
       float x[8];
-      if (col < a.ic) {
-        const int row = grouped ? t.rows[r] : t.first + r;
-        mixed_eight(p, codebook, row, col, row_before<X>(p, row, grouped ? row : t.seq, grouped || row == t.start), x);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = 0.f;
-      }
+      mix_eights<X, decltype(mix)::value>(p, codebook, raw, min(col, a.ic - 8), x);
 #pragma unroll
       for (int k = 0; k < F::kX; ++k) *reinterpret_cast<uint4*>(xs + (k * kPass + eight / 8) * kXPiece + swizzled(r, eight & 7)) = next_term<F>(x);
     }
   };
+  auto stage = [&](int kp, int ke) { if (p.mu) stage_x(std::true_type(), kp, ke); else stage_x(std::false_type(), kp, ke); };
   if (warp == kWarps) {
     if (lane == 0) find_adapter(p, t);
   } else {
-    stage_x(k0, min(k0 + kPass, k1));
+    stage(k0, min(k0 + kPass, k1));
   }
   __syncthreads();
   if (t.n == 0) return;            // the same for all blocks of the cluster
@@ -181,7 +177,7 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
       const int ke = min(kp + kPass, k1);
       if (kp > k0) {
         asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
-        stage_x(kp, ke);
+        stage(kp, ke);
         asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
       }
       // rows of x behind the n-th hold whatever was there: a row meets its own outputs alone
@@ -300,10 +296,11 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
       } else {
         unsigned short* const y = static_cast<unsigned short*>(a.y);
         unsigned short old[2][4];
+        const long long y_at_first = (long long)(grouped ? t.rows[0] : t.first) * a.y_row;        // somewhere valid
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) old[b][e] = there(b, e) ? y[y_at(b, e)] : (unsigned short)0;
+          for (int e = 0; e < 4; ++e) old[b][e] = y[there(b, e) ? y_at(b, e) : y_at_first];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll

@@ -121,8 +121,11 @@ __device__ __forceinline__ void find_rows(const Args& p, long long item, Tile& t
       for (int i = tid; i < a.n_adapters; i += kThreads) table[i] = 0;
       const bool ok = mine >= 0 && mine < a.n_adapters;
       if (!ok && mine != -1) atomicExch(p.status, (int)RWKVQ_EINVAL);
-      const int rank = ok && a.ranks ? a.ranks[mine] : a.rank;
-      const float scale = ok && a.scale ? a.scale[mine] : 1.f;
+      const int there = ok ? mine : 0;
+      const int rank_there = *(a.ranks ? a.ranks + there : a.adapter);
+      const float scale_there = *(a.scale ? a.scale + there : reinterpret_cast<const float*>(a.adapter));
+      const int rank = a.ranks ? rank_there : a.rank;
+      const float scale = a.scale ? scale_there : 1.f;
       const uint32_t same = __match_any_sync(~0u, mine), earlier = same & ((1u << lane) - 1);
       __syncthreads();
       if (ok && earlier == 0) reinterpret_cast<uint8_t*>(table + mine)[warp] = (uint8_t)__popc(same);
@@ -175,14 +178,13 @@ __device__ __forceinline__ void find_rows(const Args& p, long long item, Tile& t
 __device__ __forceinline__ void find_adapter(const Args& p, Tile& t) {
   const rwkvq_lowrank_args& a = p.a;
   if (t.n == 0 || t.adapter >= 0) return;
-  const int mine = a.adapter[t.seq];
-  bool bad = mine < -1 || mine >= a.n_adapters;
-  if (!bad && mine >= 0) {
-    const int rank = a.ranks ? a.ranks[mine] : a.rank;
-    const float scale = a.scale ? a.scale[mine] : 1.f;
-    bad = rank < 0 || rank > a.rank;
-    if (rank > 0) { t.adapter = mine; t.rank = rank; t.scale = scale; }
-  }
+  const int mine = a.adapter[t.seq], at = min(max(mine, 0), a.n_adapters - 1);
+  // both loads at once, from where something is
+  const int rank_there = *(a.ranks ? a.ranks + at : a.adapter);
+  const float scale_there = *(a.scale ? a.scale + at : reinterpret_cast<const float*>(a.adapter));
+  const int rank = a.ranks ? rank_there : a.rank;
+  const bool bad = mine < -1 || mine >= a.n_adapters || (mine >= 0 && (rank < 0 || rank > a.rank));
+  if (!bad && mine >= 0 && rank > 0) { t.adapter = mine; t.rank = rank; t.scale = a.scale ? scale_there : 1.f; }
   if (bad) atomicExch(p.status, (int)RWKVQ_EINVAL);
   if (bad || t.adapter < 0) t.n = 0;
 }
@@ -198,19 +200,6 @@ template <> __device__ __forceinline__ __half from_float<__half>(float x) { retu
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 template <typename T> struct Eight { T v[8]; };
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* f) {
-  if constexpr (sizeof(T) == 4) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-  } else {
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
-    const Eight<T> e = *reinterpret_cast<const Eight<T>*>(&w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = to_float<T>(e.v[i]);
-  }
-}
-
 // The next bf16 term of x, which is left with what the term leaves.  Cut off, not rounded, so that the largest numbers do not become infinite; of an infinity or
 // NaN nothing is left.
 __device__ __forceinline__ __nv_bfloat16 term(float& x) {
@@ -236,18 +225,6 @@ template <typename X, typename W> struct Form {
   static constexpr bool kApart = std::is_same<W, __half>::value && !kHalf;
 };
 
-// The token-shift vector's pairs of columns col to col + 7 (col a multiple of 8), whose indices are four times mu_bits neighbouring bits from a byte's beginning.
-__device__ __forceinline__ void mu_eight(const Args& p, const uint32_t* codebook, int col, float2 (&m)[4]) {
-  const uint32_t byte = (uint32_t)(col >> 3) * (uint32_t)p.mu_bits >> 1, shift = (byte & 3u) * 8u;
-  const uint32_t* const words = reinterpret_cast<const uint32_t*>(p.mu) + (byte >> 2);
-  const uint32_t lo = __ldg(words), hi = shift + 4u * (uint32_t)p.mu_bits > 32u ? __ldg(words + 1) : 0u, f = __funnelshift_r(lo, hi, shift), mask = (1u << p.mu_bits) - 1u;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t pair = codebook[f >> (uint32_t)(j * p.mu_bits) & mask];
-    m[j] = __half22float2(*reinterpret_cast<const __half2*>(&pair));
-  }
-}
-
 // Byte offset of 16 bytes (eight columns) in rows of 128 bytes under the 128-byte swizzle.
 __device__ __forceinline__ uint32_t swizzled(int row, int eight) { return (uint32_t)(row * 128 + ((eight ^ row) & 7) * 16); }
 // A box of a tensor map by a converged warp, of which one lane is elected by predicate: from a branch of one lane each took some 145 cycles.
@@ -257,29 +234,59 @@ __device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const CUtensorMap*
                ::"r"(dst_smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
-// x_mix of eight columns of a row, in fp32 but rounded to X.
-template <typename X>
-__device__ __forceinline__ void mixed_eight(const Args& p, const uint32_t* codebook, int row, int col, const X* before, float (&x)[8]) {
-  load8(static_cast<const X*>(p.a.x) + (long long)row * p.a.x_row + col, x);
-  if (!p.mu) return;
-  float y[8];
+// Eight columns of a row of x, of the row in front of it, and their indices of the token-shift vector, as they lie in memory.  All loads come from somewhere valid and none
+// is in a branch of its own, so that they are on their way together; `there` says what counts.
+template <typename X> struct Eights {
+  uint4 x[sizeof(X) / 2], before[sizeof(X) / 2];
+  uint32_t lo, hi;
+  bool there, has_before;
+};
+template <typename X, bool kMix>
+__device__ __forceinline__ Eights<X> load_eights(const Args& p, int row, int seq, bool begins, int col) {
+  const rwkvq_lowrank_args& a = p.a;
+  Eights<X> e;
+  e.there = col < a.ic;
+  col = min(col, a.ic - 8);
+  const X* const x = static_cast<const X*>(a.x) + (long long)row * a.x_row + col;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) y[j] = 0.f;
-  if (before) load8(before + col, y);
-  float2 m[4];
-  mu_eight(p, codebook, col, m);
+  for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.x[i] = __ldg(reinterpret_cast<const uint4*>(x) + i);
+  if constexpr (kMix) {
+    const X* b = a.x_prev ? static_cast<const X*>(a.x_prev) + (long long)row * a.x_prev_row + col : !begins ? x - a.x_row : a.xprev0 ? static_cast<const X*>(a.xprev0) + (long long)seq * a.ic + col : x;
+    e.has_before = a.x_prev || !begins || a.xprev0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m[j].x, x[2 * j])));
-    x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m[j].y, x[2 * j + 1])));
+    for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.before[i] = __ldg(reinterpret_cast<const uint4*>(b) + i);
+    // four indices are 4 * mu_bits neighbouring bits from a byte's beginning; behind the indices lies the codebook
+    const uint32_t* const words = reinterpret_cast<const uint32_t*>(p.mu) + ((uint32_t)(col >> 3) * (uint32_t)p.mu_bits >> 3);
+    e.lo = __ldg(words);
+    e.hi = __ldg(words + 1);
   }
+  return e;
 }
-// The row in front of a row, nullptr where there is none.
 template <typename X>
-__device__ __forceinline__ const X* row_before(const Args& p, int row, int seq, bool begins) {
-  if (p.a.x_prev) return static_cast<const X*>(p.a.x_prev) + (long long)row * p.a.x_prev_row;
-  if (!begins) return static_cast<const X*>(p.a.x) + (long long)(row - 1) * p.a.x_row;
-  return p.a.xprev0 ? static_cast<const X*>(p.a.xprev0) + (long long)seq * p.a.ic : nullptr;
+__device__ __forceinline__ void numbers(const uint4 (&w)[sizeof(X) / 2], float (&f)[8]) {
+  const Eight<X> e = *reinterpret_cast<const Eight<X>*>(w);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = to_float<X>(e.v[i]);
+}
+// x_mix of eight columns, in fp32 but rounded to X; zeros behind the last column.
+template <typename X, bool kMix>
+__device__ __forceinline__ void mix_eights(const Args& p, const uint32_t* codebook, const Eights<X>& e, int col, float (&x)[8]) {
+  numbers<X>(e.x, x);
+  if constexpr (kMix) {
+    float y[8];
+    numbers<X>(e.before, y);
+    const uint32_t bits = (uint32_t)p.mu_bits, f = __funnelshift_r(e.lo, e.hi, ((uint32_t)(col >> 3) * bits >> 1 & 3u) * 8u), mask = (1u << bits) - 1u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t pair = codebook[f >> (uint32_t)j * bits & mask];
+      const float2 m = __half22float2(*reinterpret_cast<const __half2*>(&pair));
+      const float y0 = e.has_before ? y[2 * j] : 0.f, y1 = e.has_before ? y[2 * j + 1] : 0.f;
+      x[2 * j] = to_float<X>(from_float<X>(fmaf(y0 - x[2 * j], m.x, x[2 * j])));
+      x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y1 - x[2 * j + 1], m.y, x[2 * j + 1])));
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = e.there ? x[j] : 0.f;
 }
 // Eight numbers as operands of the tensor cores: the k-th term of each.
 template <typename F>

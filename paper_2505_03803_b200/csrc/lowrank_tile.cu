@@ -73,6 +73,59 @@ __device__ __forceinline__ void tensor_g2s_2d(uint32_t dst_smem, const CUtensorM
 __device__ __forceinline__ uint32_t pair_bits(__nv_bfloat16 x, __nv_bfloat16 y) { return (uint32_t)__bfloat16_as_ushort(x) | (uint32_t)__bfloat16_as_ushort(y) << 16; }
 __device__ __forceinline__ uint32_t pair_bits(__half x, __half y) { return (uint32_t)__half_as_ushort(x) | (uint32_t)__half_as_ushort(y) << 16; }
 
+// Four neighbouring numbers of y and as many that are added to them.
+template <typename Y> struct Four { typename std::conditional<sizeof(Y) == 4, uint4, uint2>::type w; };
+template <typename Y>
+__device__ __forceinline__ void add_four(Four<Y>& y, const float4& d) {
+  Y* const v = reinterpret_cast<Y*>(&y.w);
+  v[0] = from_float<Y>(to_float<Y>(v[0]) + d.x); v[1] = from_float<Y>(to_float<Y>(v[1]) + d.y);
+  v[2] = from_float<Y>(to_float<Y>(v[2]) + d.z); v[3] = from_float<Y>(to_float<Y>(v[3]) + d.w);
+}
+// The accumulators of tiles [o0, o1) of B to y: kCols of the tile's rows from col0 on, by one warp.
+template <int kCols, typename Y, bool kScaled>
+__device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int acc_cols, int accs, int o0, int o1, int quarter, int col0, int n, bool grouped, float* turn,
+                                        int quad, int r_lane, volatile int* abortp, bool& ok) {
+  const rwkvq_lowrank_args& a = p.a;
+  const int lane = threadIdx.x & 31;
+  const int rows = min(n - col0, kCols);             // of this warp, maybe none
+  Y* at[kCols / 4];                                  // rows r_lane, r_lane + 4, ...; those behind the last are read, where there are any at all, as the last
+#pragma unroll
+  for (int i = 0; i < kCols / 4; ++i) {
+    const int r = col0 + max(min(i * 4 + r_lane, rows - 1), -col0);
+    at[i] = static_cast<Y*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row;
+  }
+#pragma unroll 1
+  for (int o = 0; o < o1 - o0; ++o) {
+    const int acc = o % accs, col = (o0 + o) * 128 + quarter * 32 + quad * 4, col_there = min(col, a.oc - 4);
+    Four<Y> y[kCols / 4];
+    if (rows > 0)
+#pragma unroll
+      for (int i = 0; i < kCols / 4; ++i) y[i] = *reinterpret_cast<const Four<Y>*>(at[i] + col_there);
+    ok = ok && tc5::mbar_wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / accs) & 1u, abortp, p.status);
+    if (!__all_sync(~0u, ok)) break;
+    tc5::tc_fence_after();
+    uint32_t v[kCols];
+    tmem_ld<kCols>(acc0 + (uint32_t)(acc * acc_cols), v);
+    tc5::tc_fence_before();
+    __syncwarp();
+    if (lane == 0) tc5::mbar_arrive(&ctrl.empty_acc[acc]);
+    if (rows <= 0) continue;
+    // [row][column], rows of 128 bytes: each lane a column, then each quarter of a warp a row
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) turn[j * 32 + lane] = __uint_as_float(v[j]);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kCols / 4; ++i) {
+      const int r = i * 4 + r_lane;
+      float4 d = *reinterpret_cast<const float4*>(turn + r * 32 + quad * 4);
+      if constexpr (kScaled) { const float back = ctrl.back[min(col0 + r, n - 1)]; d.x *= back; d.y *= back; d.z *= back; d.w *= back; }
+      add_four<Y>(y[i], d);
+      if (r < rows && col < a.oc) *reinterpret_cast<Four<Y>*>(at[i] + col) = y[i];
+    }
+    __syncwarp();
+  }
+}
+
 template <typename X, typename W, int NT>
 __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_constant__ Args p) {
   using S = TileShape<X, W, NT>;
@@ -115,41 +168,46 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && tc5::mbar_wait(bar, parity, abortp, p.status); };
   auto row_of = [&](int r) { return grouped ? t.rows[r] : t.first + r; };
 
-  // pieces [g0, g0 + kGroup) of x in operand form
-  auto stage_x = [&](int g0) {
-    float x[S::kPer][8];
+  // Pieces [g0, g0 + kGroup) of x in operand form.  Four neighbouring rows are a warp's; warps whose rows are behind the last have nothing to make.
+  auto stage_x = [&](auto mix, int g0) {
+    auto r_of = [&](int j) { return (tid / 8 + j * (kThreads / 8)) % NT; };
+    auto emptied = [&] {
+      for (int i = max(g0, S::kXSlots); i < min(g0 + S::kGroup, np); ++i) wait(xempty + (uint32_t)(i % S::kXSlots) * 8u, (uint32_t)(i / S::kXSlots - 1) & 1u);
+    };
+    if ((warp * 4) % NT < n) {
+      Eights<X> raw[S::kPer];
 #pragma unroll
-    for (int j = 0; j < S::kPer; ++j) {
-      const int e = tid + j * kThreads, piece = g0 + e / (NT * 8), r = e / 8 % NT, col = (k0 + piece) * 64 + (e & 7) * 8;
-      if (r < n && piece < np && col < a.ic) {
-        const int row = row_of(r);
-        mixed_eight(p, codebook, row, col, row_before<X>(p, row, grouped ? row : t.seq, grouped || row == t.start), x[j]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
+      for (int j = 0; j < S::kPer; ++j) {
+        const int row = row_of(min(r_of(j), n - 1));
+        raw[j] = load_eights<X, decltype(mix)::value>(p, row, grouped ? row : t.seq, grouped || row == t.start,
+                                                      (k0 + min(g0 + (tid + j * kThreads) / (NT * 8), np - 1)) * 64 + (tid & 7) * 8);
       }
-    }
-    if (g0 >= S::kXSlots)
-      for (int i = g0; i < min(g0 + S::kGroup, np); ++i) wait(xempty + (uint32_t)(i % S::kXSlots) * 8u, (uint32_t)(i / S::kXSlots - 1) & 1u);
+      emptied();
 #pragma unroll
-    for (int j = 0; j < S::kPer; ++j) {
-      const int e = tid + j * kThreads, piece = g0 + e / (NT * 8), r = e / 8 % NT;
-      if (r < n && piece < np && ok)
+      for (int j = 0; j < S::kPer; ++j) {
+        const int piece = g0 + (tid + j * kThreads) / (NT * 8), r = r_of(j);
+        float x[8];
+        mix_eights<X, decltype(mix)::value>(p, codebook, raw[j], min((k0 + piece) * 64 + (tid & 7) * 8, a.ic - 8), x);
+        if (r < n && piece < np && ok)
 #pragma unroll
-        for (int k = 0; k < F::kX; ++k)
-          *reinterpret_cast<uint4*>(xs + piece % S::kXSlots * S::kPieceBytes + k * S::kTileBytes + swizzled(r, e & 7)) = next_term<F>(x[j]);
+          for (int k = 0; k < F::kX; ++k)
+            *reinterpret_cast<uint4*>(xs + piece % S::kXSlots * S::kPieceBytes + k * S::kTileBytes + swizzled(r, tid & 7)) = next_term<F>(x);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    } else {
+      emptied();          // it reports for a piece when it is that piece's turn
     }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0)
       for (int i = g0; i < min(g0 + S::kGroup, np); ++i) tc5::mbar_arrive(xfull + (uint32_t)(i % S::kXSlots) * 8u);
   };
+  auto stage = [&](int g0) { if (p.mu) stage_x(std::true_type(), g0); else stage_x(std::false_type(), g0); };
   if (warp == kWarps) {
     if (lane == 0) find_adapter(p, t);
   } else if (warp == kWarps + 1) {
     tc5::tmem_alloc(&ctrl.tmem_base, S::kTmemCols);
   } else {
-    if (!p.x_by_map && np > 0 && n > 0) stage_x(0);
+    if (!p.x_by_map && np > 0 && n > 0) stage(0);
     // y's rows, which are needed last, on their way to the second-level cache
     const int y_bytes = (min(o1 * 128, a.oc) - o0 * 128) * (a.y_dtype == RWKVQ_F32 ? 4 : 2);
     if (tid < n && y_bytes > 0)
@@ -171,9 +229,14 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     // ---- copies.  This warp and the next bring nothing to the first meeting of the cluster and do not hold it up: what they wait for below comes behind it.
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     const int total = n_a + (o1 - o0) * wide;
+    // The warps that store y wait for the second meeting, in which the blocks have read one another's shares, before they give anything back: it is not held up, either,
+    // by waits for slots that B had.
+    auto second = [] { asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory"); };
+    bool met = false;
     int i = 0, px = 0;
 #pragma unroll 1
     for (; i < total; ++i) {
+      if (i - kRing >= n_a && !met) { second(); met = true; }
       const uint32_t st = (uint32_t)(i % kRing), bar = full + st * 8u, dst = ring + st * kSlotBytes;
       if (i >= kRing) wait(empty + st * 8u, (uint32_t)(i / kRing - 1) & 1u);
       if (!__all_sync(~0u, ok)) break;
@@ -211,7 +274,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     }
     if (lane == 0) { ctrl.asked = i; ctrl.x_asked = px; }
     __syncwarp();
-    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (!met) second();
   } else if (warp == kWarps + 1) {
     // ---- products
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -239,6 +302,8 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     }
     if (__all_sync(~0u, ok)) tc5::umma_commit(&ctrl.a_done);
     wait(smem_u32(&ctrl.h_ready), 0);
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
     int i = n_a;
 #pragma unroll 1
     for (int o = 0; o < o1 - o0; ++o) {
@@ -277,11 +342,10 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       if (!__all_sync(~0u, ok)) break;
       tc5::umma_commit(&ctrl.full_acc[acc]);
     }
-    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
   } else {
     if (!p.x_by_map)
 #pragma unroll 1
-      for (int g = S::kGroup; g < np; g += S::kGroup) stage_x(g);
+      for (int g = S::kGroup; g < np; g += S::kGroup) stage(g);
     // ---- this block's share of A x: lanes are the rank
     constexpr int kCols = NT / 2;
     const int quarter = warp & 3, col0 = (warp >> 2) * kCols;
@@ -306,23 +370,21 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     cluster.sync();
 
     // ---- all of A x, as operands: as many lanes to a row as there are fours of the rank
+    auto gather = [&](auto blocks_of_cluster) {
+    constexpr int kC = decltype(blocks_of_cluster)::value;
     const int wl = blocks == 1 ? 4 : blocks == 2 ? 8 : blocks <= 4 ? 16 : 32, r4 = lane % wl * 4;
     const float scale = t.scale;
 #pragma unroll 1
     for (int row0 = warp * (32 / wl); row0 < n; row0 += kWarps * (32 / wl)) {
       const int row = row0 + lane / wl;
       float h[4] = {0.f, 0.f, 0.f, 0.f};
-      if (row < n && r4 < rank) {
-        float4 s[8];
+      float4 s[kC];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < C) s[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(share, k) + row * kMostRank + r4);
+      for (int k = 0; k < kC; ++k) s[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(share, k) + min(row, n - 1) * kMostRank + r4);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k < C) { h[0] += s[k].x; h[1] += s[k].y; h[2] += s[k].z; h[3] += s[k].w; }
+      for (int k = 0; k < kC; ++k) { h[0] += s[k].x; h[1] += s[k].y; h[2] += s[k].z; h[3] += s[k].w; }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) h[j] = r4 + j < rank ? h[j] * scale : 0.f;
-      }
+      for (int j = 0; j < 4; ++j) h[j] = r4 + j < rank ? h[j] * scale : 0.f;
       uint8_t* const to = xs + r4 / 64 * S::kTileBytes + swizzled(row, r4 / 8 & 7) + (r4 & 4) * 2;
       const bool there = row < n && r4 < blocks * 16;
       if constexpr (kHalf) {
@@ -354,50 +416,26 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
         }
       }
     }
+    };
+    if (C == 8) gather(std::integral_constant<int, 8>());
+    else if (C == 4) gather(std::integral_constant<int, 4>());
+    else if (C == 2) gather(std::integral_constant<int, 2>());
+    else gather(std::integral_constant<int, 1>());
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) tc5::mbar_arrive(&ctrl.h_ready);
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 
-    // ---- y, 32 columns of it for a warp, as many rows as half a tile
-#pragma unroll 1
-    for (int o = 0; o < o1 - o0; ++o) {
-      const uint32_t acc = (uint32_t)(o % S::kAcc);
-      const int col = (o0 + o) * 128 + quarter * 32 + lane;
-      const bool there = col < a.oc;
-      unsigned short old[kCols];
-      unsigned short* const y16 = static_cast<unsigned short*>(a.y) + col;
-      if (a.y_dtype != RWKVQ_F32) {
-#pragma unroll
-        for (int j = 0; j < kCols; ++j)
-          if (there && col0 + j < n) old[j] = y16[(long long)row_of(col0 + j) * a.y_row];
-      }
-      wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / S::kAcc) & 1u);
-      if (!__all_sync(~0u, ok)) break;
-      tc5::tc_fence_after();
-      tmem_ld<kCols>(lanes + NT + acc * NT, v);
-      tc5::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) tc5::mbar_arrive(&ctrl.empty_acc[acc]);
-#pragma unroll
-      for (int j = 0; j < kCols; ++j) {
-        const int r = col0 + j;
-        if (!there || r >= n) continue;
-        const float d = kHalf ? __uint_as_float(v[j]) * ctrl.back[r] : __uint_as_float(v[j]);
-        const long long at_y = (long long)row_of(r) * a.y_row;
-        if (a.y_dtype == RWKVQ_F32) {
-          // Each element of y is added to once in a call, so that a reduction in memory is as good as a load, an addition and a store, and nothing waits for it (it
-          // takes subnormal numbers for zeros).
-          asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(static_cast<float*>(a.y) + at_y + col), "f"(d) : "memory");
-        } else if (a.y_dtype == RWKVQ_F16) {
-          y16[at_y] = __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(old[j])) + d));
-        } else {
-          y16[at_y] = __bfloat16_as_ushort(__float2bfloat16_rn(__bfloat162float(__ushort_as_bfloat16(old[j])) + d));
-        }
-      }
-    }
+    // ---- y: 32 columns of it for a warp, and half of the tile's rows.  A lane of the accumulator is a column; the way to four neighbouring columns a lane is through
+    // shared memory, where the other blocks have read the shares.
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    float* const turn = share + warp * kCols * 32;
+    const int quad = lane & 7, r_lane = lane >> 3;
+    if (a.y_dtype == RWKVQ_F32) store_y<kCols, float, kHalf>(p, t, ctrl, lanes + NT, NT, S::kAcc, o0, o1, quarter, col0, n, grouped, turn, quad, r_lane, abortp, ok);
+    else if (a.y_dtype == RWKVQ_F16) store_y<kCols, __half, kHalf>(p, t, ctrl, lanes + NT, NT, S::kAcc, o0, o1, quarter, col0, n, grouped, turn, quad, r_lane, abortp, ok);
+    else store_y<kCols, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + NT, NT, S::kAcc, o0, o1, quarter, col0, n, grouped, turn, quad, r_lane, abortp, ok);
   }
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // no block ends while another reads its share
+  if (warp >= kWarps) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // no block ends while another reads its share
   tc5::tc_fence_before();
   __syncthreads();
   tc5::tc_fence_after();

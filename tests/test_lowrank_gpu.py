@@ -128,6 +128,14 @@ def test_ragged(lens):
     check(c)
 
 
+@pytest.mark.parametrize("x,w", [("bf16", "bf16"), ("f16", "f16"), ("f16", "bf16"), ("f32", "bf16"), ("bf16", "f16")])
+@pytest.mark.parametrize("lens", [[3, 70, 1, 40, 33] * 6, [1, 2] * 60, [65] * 150])
+def test_many_tiles_of_long_rows(x, w, lens):
+    """More tiles than the machine has clusters for, so that a block has all columns and its buffers go round, with tiles that are partly filled."""
+    c = Case(len(lens), lens, 2056, 392, 40, [i % 4 - 1 for i in range(len(lens))], x, w, "f32", mix="first" if x != "bf16" else None)
+    check(c)
+
+
 @pytest.mark.parametrize("n,adapters", [(1, 1), (2, 1), (16, 1), (17, 1), (33, 2), (50, 7), (96, 96), (300, 3)])
 @pytest.mark.parametrize("mix", [None, "rows", "first", "zeros"])
 def test_one_row_a_sequence(n, adapters, mix):
