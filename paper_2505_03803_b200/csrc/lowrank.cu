@@ -116,8 +116,7 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
       const Eights<X> raw = load_eights<X, decltype(mix)::value>(p, row, grouped ? row : t.seq, grouped || row == t.start, col);
       float x[8];
       mix_eights<X, decltype(mix)::value>(p, codebook, raw, min(col, a.ic - 8), x);
-#pragma unroll
-      for (int k = 0; k < F::kX; ++k) *reinterpret_cast<uint4*>(xs + (k * kPass + eight / 8) * kXPiece + swizzled(r, eight & 7)) = next_term<F>(x);
+      put_terms<F>(xs + eight / 8 * kXPiece + swizzled(r, eight & 7), kPass * kXPiece, x);
     }
   };
   auto stage = [&](int kp, int ke) { if (p.mu) stage_x(std::true_type(), kp, ke); else stage_x(std::false_type(), kp, ke); };

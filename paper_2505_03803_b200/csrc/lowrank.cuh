@@ -26,7 +26,8 @@ struct alignas(64) Args {
   int splits;                    // clusters to a tile
   int* status;
   int x_by_map;                  // x goes to shared memory as it is, through a map
-  CUtensorMap A[4], B, X;        // boxes of 64 columns x 16, 32, 64, 128 rows (as far as the rank goes); x 128 rows; x a tile's rows
+  int whole;                     // columns are a multiple of 64: a box holds several pieces of 64 columns
+  CUtensorMap A[8], B, X;        // A: for each sixteen of the rank, as far as it goes, boxes of so many rows; B: 64 columns x 128 rows; X: 64 columns x a tile's rows
 };
 
 // ---- rows of a tile -----------------------------------------------------------------------------------------
@@ -271,25 +272,29 @@ __device__ __forceinline__ void numbers(const uint4 (&w)[sizeof(X) / 2], float (
 // x_mix of eight columns, in fp32 but rounded to X; zeros behind the last column.
 template <typename X, bool kMix>
 __device__ __forceinline__ void mix_eights(const Args& p, const uint32_t* codebook, const Eights<X>& e, int col, float (&x)[8]) {
-  numbers<X>(e.x, x);
+  auto counts = [](const uint4& w, bool yes) { return make_uint4(yes ? w.x : 0u, yes ? w.y : 0u, yes ? w.z : 0u, yes ? w.w : 0u); };
+  uint4 w[sizeof(X) / 2];
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(X) / 2; ++i) w[i] = counts(e.x[i], e.there);
+  numbers<X>(w, x);
   if constexpr (kMix) {
     float y[8];
-    numbers<X>(e.before, y);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(X) / 2; ++i) w[i] = counts(e.before[i], e.there && e.has_before);
+    numbers<X>(w, y);
     const uint32_t bits = (uint32_t)p.mu_bits, f = __funnelshift_r(e.lo, e.hi, ((uint32_t)(col >> 3) * bits >> 1 & 3u) * 8u), mask = (1u << bits) - 1u;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t pair = codebook[f >> (uint32_t)j * bits & mask];
       const float2 m = __half22float2(*reinterpret_cast<const __half2*>(&pair));
-      const float y0 = e.has_before ? y[2 * j] : 0.f, y1 = e.has_before ? y[2 * j + 1] : 0.f;
-      x[2 * j] = to_float<X>(from_float<X>(fmaf(y0 - x[2 * j], m.x, x[2 * j])));
-      x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y1 - x[2 * j + 1], m.y, x[2 * j + 1])));
+      x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m.x, x[2 * j])));
+      x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m.y, x[2 * j + 1])));
     }
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = e.there ? x[j] : 0.f;
 }
-// Eight numbers as operands of the tensor cores: the k-th term of each.
-template <typename F>
+// Eight numbers as operands of the tensor cores: the next term of each (kX in all), which is taken from them.  All but the last of several terms are cut off to bf16, the last
+// is exact.  (What is left of an infinity is NaN.)
+template <typename F, bool kLast>
 __device__ __forceinline__ uint4 next_term(float (&x)[8]) {
   uint32_t v[4];
 #pragma unroll
@@ -297,17 +302,26 @@ __device__ __forceinline__ uint4 next_term(float (&x)[8]) {
     if constexpr (F::kHalf) {
       const __half2 h = __floats2half2_rn(x[2 * j], x[2 * j + 1]);
       v[j] = *reinterpret_cast<const uint32_t*>(&h);
-    } else if constexpr (F::kX == 1) {
+    } else if constexpr (kLast) {
       const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
       v[j] = *reinterpret_cast<const uint32_t*>(&h);
     } else {
-      __nv_bfloat162 h;
-      h.x = term(x[2 * j]); h.y = term(x[2 * j + 1]);
-      v[j] = *reinterpret_cast<const uint32_t*>(&h);
+      const uint32_t lo = __float_as_uint(x[2 * j]), hi = __float_as_uint(x[2 * j + 1]);
+      v[j] = __byte_perm(lo, hi, 0x7632);
+      x[2 * j] -= __uint_as_float(lo & 0xFFFF0000u);
+      x[2 * j + 1] -= __uint_as_float(hi & 0xFFFF0000u);
     }
   }
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
+// All terms, `next` bytes from one to the next.
+template <typename F>
+__device__ __forceinline__ void put_terms(uint8_t* to, uint32_t next, float (&x)[8]) {
+  if constexpr (F::kX >= 2) { *reinterpret_cast<uint4*>(to) = next_term<F, false>(x); to += next; }
+  if constexpr (F::kX == 3) { *reinterpret_cast<uint4*>(to) = next_term<F, false>(x); to += next; }
+  *reinterpret_cast<uint4*>(to) = next_term<F, true>(x);
+}
+
 // [n][rows][cols] of 16-bit numbers as boxes of 64 columns x box_rows rows in the 128-byte swizzle; what lies outside reads as zero.
 inline bool encode(CUtensorMap* map, const void* at, bool half, int cols, int rows, int n, int box_rows) {
   const tc5::EncodeTiledFn fn = tc5::encode_tiled();

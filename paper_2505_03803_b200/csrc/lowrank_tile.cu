@@ -22,25 +22,34 @@ namespace lr {
 using tc5::smem_u32;
 
 constexpr int kTileAll = kThreads + 64;                            // eight warps that make operands and read accumulators, one that asks for copies, one that multiplies
-constexpr int kRing = 7, kSlotBytes = 16 << 10, kMostXSlots = 16, kMostAcc = 4;
+constexpr int kRing = 7, kSlotBytes = 16 << 10, kMostGroups = 4, kMostAcc = 4;
 constexpr int kSmemBytes = 224 << 10;
+
+// Pieces of 64 columns of A that a slot holds where the rank is up to 16 * blocks.
+__host__ __device__ constexpr int pieces_of(int blocks) { return blocks == 1 ? 8 : blocks == 2 ? 4 : blocks <= 4 ? 2 : 1; }
 
 template <typename X, typename W, int NT>
 struct TileShape {
   static constexpr int kTerms = Form<X, W>::kX, kTileBytes = NT * 128, kPieceBytes = kTerms * kTileBytes;      // a piece: 64 columns of the tile's rows, a tile for each term
-  static constexpr int kXSlots = NT == 64 ? (kTerms == 1 ? 8 : kTerms == 2 ? 4 : 3) : (kTerms < 3 ? 16 : 12);
-  static constexpr int kXBytes = kXSlots * kPieceBytes, kShare = NT * kMostRank * 4;
-  static constexpr int kGroup = NT == 64 ? 2 : 8, kPer = kGroup * NT * 8 / kThreads;      // pieces that are made at once, and eights of columns of them for each thread
+  static constexpr int kGroup = NT == 64 ? 2 : 8, kGroups = NT == 16 ? 2 : kTerms == 1 ? 4 : kTerms == 2 ? 2 : 1;      // pieces that come at once, and how many such groups there is room for
+  static constexpr int kXBytes = kGroup * kGroups * kPieceBytes, kShare = NT * kMostRank * 4;
+  static constexpr int kEights = kGroup * 8, kPer = kEights * NT / kThreads;       // of a row in a group, and those of a thread where the tile is full
   static constexpr int kAcc = NT == 64 ? 2 : 4, kTmemCols = NT == 64 ? 256 : 128;
   static_assert(kXBytes >= 6 * kTileBytes, "A x takes x's place");
   static_assert(1024 + kRing * kSlotBytes + kXBytes + kShare + 1024 <= kSmemBytes, "shared memory");
   static_assert(kShare >= 8 * kMostCounted || NT == 64, "room for counting the rows of adapters");
 };
 struct TileCtrl {
-  uint64_t full[kRing], empty[kRing], xfull[kMostXSlots], xempty[kMostXSlots], a_done, h_ready, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
+  uint64_t full[kRing], empty[kRing], xfull[kMostGroups], xempty[kMostGroups], a_done, h_ready, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
   int abort_flag, asked, x_asked;
   uint32_t tmem_base;
   float back[64];                 // of each row: the power of two that its A x was divided by
+};
+// Slots of a ring in turn.
+template <int N>
+struct Turn {
+  uint32_t at = 0, parity = 0;
+  __device__ __forceinline__ void next() { if (++at == N) { at = 0; parity ^= 1u; } }
 };
 
 // Both operands of a type (bf16, or f16), K-major -> fp32, 128 x N.
@@ -65,10 +74,10 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[kCols]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]) :: "memory");
   }
 }
-__device__ __forceinline__ void tensor_g2s_2d(uint32_t dst_smem, const CUtensorMap* map, int x, int y, uint32_t bar) {
+__device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, int v, uint32_t bar) {
   asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
-               " @q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n}"
-               ::"r"(dst_smem), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+               " @q cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n}"
+               ::"r"(dst_smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(v), "r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t pair_bits(__nv_bfloat16 x, __nv_bfloat16 y) { return (uint32_t)__bfloat16_as_ushort(x) | (uint32_t)__bfloat16_as_ushort(y) << 16; }
 __device__ __forceinline__ uint32_t pair_bits(__half x, __half y) { return (uint32_t)__half_as_ushort(x) | (uint32_t)__half_as_ushort(y) << 16; }
@@ -94,13 +103,21 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
     const int r = col0 + max(min(i * 4 + r_lane, rows - 1), -col0);
     at[i] = static_cast<Y*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row;
   }
-#pragma unroll 1
-  for (int o = 0; o < o1 - o0; ++o) {
-    const int acc = o % accs, col = (o0 + o) * 128 + quarter * 32 + quad * 4, col_there = min(col, a.oc - 4);
-    Four<Y> y[kCols / 4];
+  // y of the next tile is on its way while this one's is added to
+  Four<Y> y[kCols / 4], ahead[kCols / 4];
+  auto load = [&](int o) {
+    const int col = min((o0 + o) * 128 + quarter * 32 + quad * 4, a.oc - 4);
     if (rows > 0)
 #pragma unroll
-      for (int i = 0; i < kCols / 4; ++i) y[i] = *reinterpret_cast<const Four<Y>*>(at[i] + col_there);
+      for (int i = 0; i < kCols / 4; ++i) ahead[i] = *reinterpret_cast<const Four<Y>*>(at[i] + col);
+  };
+  load(0);
+#pragma unroll 1
+  for (int o = 0; o < o1 - o0; ++o) {
+    const int acc = o % accs, col = (o0 + o) * 128 + quarter * 32 + quad * 4;
+#pragma unroll
+    for (int i = 0; i < kCols / 4; ++i) y[i] = ahead[i];
+    if (o + 1 < o1 - o0) load(o + 1);
     ok = ok && tc5::mbar_wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / accs) & 1u, abortp, p.status);
     if (!__all_sync(~0u, ok)) break;
     tc5::tc_fence_after();
@@ -147,7 +164,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   asm volatile("griddepcontrol.launch_dependents;");
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], 1); }
-    for (int i = 0; i < S::kXSlots; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : kWarps); tc5::mbar_init(&ctrl.xempty[i], 1); }
+    for (int i = 0; i < S::kGroups; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : kWarps); tc5::mbar_init(&ctrl.xempty[i], 1); }
     for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], kWarps); }
     tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.h_ready, kWarps); tc5::mbar_init(&ctrl.drained, 1);
     ctrl.abort_flag = ctrl.asked = ctrl.x_asked = 0;
@@ -168,50 +185,66 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && tc5::mbar_wait(bar, parity, abortp, p.status); };
   auto row_of = [&](int r) { return grouped ? t.rows[r] : t.first + r; };
 
-  // Pieces [g0, g0 + kGroup) of x in operand form.  Four neighbouring rows are a warp's; warps whose rows are behind the last have nothing to make.
-  auto stage_x = [&](auto mix, int g0) {
-    auto r_of = [&](int j) { return (tid / 8 + j * (kThreads / 8)) % NT; };
-    auto emptied = [&] {
-      for (int i = max(g0, S::kXSlots); i < min(g0 + S::kGroup, np); ++i) wait(xempty + (uint32_t)(i % S::kXSlots) * 8u, (uint32_t)(i / S::kXSlots - 1) & 1u);
-    };
-    if ((warp * 4) % NT < n) {
-      Eights<X> raw[S::kPer];
+  // All groups of x in operand form, by the eight warps, or those before `last`: the loads of a group are on their way while the one before it is made.  A thread has kN eights of
+  // columns of a group, one where the tile has few rows.
+  auto stage_all = [&](auto mix, auto per) {
+    constexpr bool kMix = decltype(mix)::value;
+    constexpr int kN = decltype(per)::value;
+    Turn<S::kGroups> turn;
+    Eights<X> raw[kN], ahead[kN];
+    auto load = [&](int g, Eights<X> (&e)[kN]) {
 #pragma unroll
-      for (int j = 0; j < S::kPer; ++j) {
-        const int row = row_of(min(r_of(j), n - 1));
-        raw[j] = load_eights<X, decltype(mix)::value>(p, row, grouped ? row : t.seq, grouped || row == t.start,
-                                                      (k0 + min(g0 + (tid + j * kThreads) / (NT * 8), np - 1)) * 64 + (tid & 7) * 8);
+      for (int j = 0; j < kN; ++j) {
+        const int i = tid + j * kThreads, r = min(i / S::kEights, n - 1), row = row_of(r);
+        e[j] = load_eights<X, kMix>(p, row, grouped ? row : t.seq, grouped || row == t.start, (k0 + min(g * S::kGroup + i % S::kEights / 8, np - 1)) * 64 + (i & 7) * 8);
       }
-      emptied();
+    };
+    load(0, ahead);
+#pragma unroll 1
+    for (int g = 0; g * S::kGroup < np; ++g) {
 #pragma unroll
-      for (int j = 0; j < S::kPer; ++j) {
-        const int piece = g0 + (tid + j * kThreads) / (NT * 8), r = r_of(j);
+      for (int j = 0; j < kN; ++j) raw[j] = ahead[j];
+      if ((g + 1) * S::kGroup < np) load(g + 1, ahead);
+      if (g >= S::kGroups) wait(xempty + turn.at * 8u, turn.parity ^ 1u);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const int i = tid + j * kThreads, row = i / S::kEights, piece = i % S::kEights / 8;
+        if (j * kThreads / S::kEights >= n) continue;          // of no thread
         float x[8];
-        mix_eights<X, decltype(mix)::value>(p, codebook, raw[j], min((k0 + piece) * 64 + (tid & 7) * 8, a.ic - 8), x);
-        if (r < n && piece < np && ok)
-#pragma unroll
-          for (int k = 0; k < F::kX; ++k)
-            *reinterpret_cast<uint4*>(xs + piece % S::kXSlots * S::kPieceBytes + k * S::kTileBytes + swizzled(r, tid & 7)) = next_term<F>(x);
+        mix_eights<X, kMix>(p, codebook, raw[j], min((k0 + g * S::kGroup + piece) * 64 + (i & 7) * 8, a.ic - 8), x);
+        if (row < n) put_terms<F>(xs + (turn.at * S::kGroup + piece) * S::kPieceBytes + swizzled(row, i & 7), S::kTileBytes, x);
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    } else {
-      emptied();          // it reports for a piece when it is that piece's turn
+      __syncwarp();
+      if (lane == 0) tc5::mbar_arrive(xfull + turn.at * 8u);
+      turn.next();
     }
-    __syncwarp();
-    if (lane == 0)
-      for (int i = g0; i < min(g0 + S::kGroup, np); ++i) tc5::mbar_arrive(xfull + (uint32_t)(i % S::kXSlots) * 8u);
   };
-  auto stage = [&](int g0) { if (p.mu) stage_x(std::true_type(), g0); else stage_x(std::false_type(), g0); };
+  auto stage = [&] {
+    const bool few = n * S::kEights <= kThreads;
+    if (p.mu) {
+      if (few) stage_all(std::true_type(), std::integral_constant<int, 1>());
+      else stage_all(std::true_type(), std::integral_constant<int, S::kPer>());
+    } else {
+      if (few) stage_all(std::false_type(), std::integral_constant<int, 1>());
+      else stage_all(std::false_type(), std::integral_constant<int, S::kPer>());
+    }
+  };
   if (warp == kWarps) {
     if (lane == 0) find_adapter(p, t);
   } else if (warp == kWarps + 1) {
     tc5::tmem_alloc(&ctrl.tmem_base, S::kTmemCols);
   } else {
-    if (!p.x_by_map && np > 0 && n > 0) stage(0);
-    // y's rows, which are needed last, on their way to the second-level cache
-    const int y_bytes = (min(o1 * 128, a.oc) - o0 * 128) * (a.y_dtype == RWKVQ_F32 ? 4 : 2);
-    if (tid < n && y_bytes > 0)
-      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(a.y) + ((long long)row_of(tid) * a.y_row + o0 * 128) * (a.y_dtype == RWKVQ_F32 ? 4 : 2)), "r"(y_bytes) : "memory");
+    // x's and y's rows on their way to the second-level cache while the adapter is looked up
+    auto fetch = [](const void* base, long long at, int bytes, int size) {
+      if (bytes > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(base) + at * size), "r"(bytes * size) : "memory");
+    };
+    if (tid < n) {
+      const int columns = min((k0 + np) * 64, a.ic) - k0 * 64;
+      fetch(a.x, (long long)row_of(tid) * a.x_row + k0 * 64, columns, (int)sizeof(X));
+      if (a.x_prev) fetch(a.x_prev, (long long)row_of(tid) * a.x_prev_row + k0 * 64, columns, (int)sizeof(X));
+      fetch(a.y, (long long)row_of(tid) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
+    }
   }
   tc5::tc_fence_before();
   __syncthreads();
@@ -222,7 +255,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     return;
   }
   const int rank = t.rank, blocks = (rank + 15) / 16, wide = (rank + 63) / 64;
-  const int a_slot = 8 / (blocks == 1 ? 1 : blocks == 2 ? 2 : blocks <= 4 ? 4 : 8), n_a = (np + a_slot - 1) / a_slot;      // pieces of A in a slot
+  const int a_slot = pieces_of(blocks), n_a = (np + a_slot - 1) / a_slot;      // pieces of A in a slot
   const int last_term = kHalf ? 1 : a.y_dtype == RWKVQ_F32 ? 2 : 1;
 
   if (warp == kWarps) {
@@ -233,46 +266,56 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     // by waits for slots that B had.
     auto second = [] { asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory"); };
     bool met = false;
-    int i = 0, px = 0;
+    int i = 0, px = 0, gx = 0;
+    Turn<kRing> slot;
+    Turn<S::kGroups> group;
+    const CUtensorMap* const a_map = &p.A[blocks - 1];
+    const uint32_t a_bytes = (uint32_t)(a_slot * blocks) * 2048u;
+    auto ask_x = [&](int upto) {
 #pragma unroll 1
-    for (; i < total; ++i) {
-      if (i - kRing >= n_a && !met) { second(); met = true; }
-      const uint32_t st = (uint32_t)(i % kRing), bar = full + st * 8u, dst = ring + st * kSlotBytes;
-      if (i >= kRing) wait(empty + st * 8u, (uint32_t)(i / kRing - 1) & 1u);
-      if (!__all_sync(~0u, ok)) break;
-      if (i < n_a) {
-        const int first = i * a_slot, count = min(a_slot, np - first);
-        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[st], (uint32_t)(count * blocks) * 2048u);
+      for (; px < upto; px += S::kGroup, ++gx) {
+        if (gx >= S::kGroups) wait(xempty + group.at * 8u, group.parity ^ 1u);
+        if (!__all_sync(~0u, ok)) return;
+        const uint32_t bar = xfull + group.at * 8u, to = xring + group.at * (S::kGroup * S::kPieceBytes);
+        const int count = p.whole ? S::kGroup : min(S::kGroup, np - px);
+        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.xfull[group.at], (uint32_t)(count * S::kTileBytes));
         __syncwarp();
+        if (p.whole) tensor_g2s(to, &p.X, 0, t.first, k0 + px, bar);
+        else
 #pragma unroll 1
-        for (int j = 0; j < count; ++j) {
-          // as few boxes as the rank has binary digits
-          int r = 0;
-#pragma unroll
-          for (int h = 3; h >= 0; --h)
-            if (blocks >> h & 1) {
-              tensor_g2s(dst + (uint32_t)((j * blocks + r) * 2048), &p.A[h], (k0 + first + j) * 64, r * 16, t.adapter, bar);
-              r += 1 << h;
-            }
-        }
-        if (p.x_by_map)
-#pragma unroll 1
-          for (; px < first + count; ++px) {
-            const uint32_t xst = (uint32_t)(px % S::kXSlots);
-            if (px >= S::kXSlots) wait(xempty + xst * 8u, (uint32_t)(px / S::kXSlots - 1) & 1u);
-            if (!__all_sync(~0u, ok)) break;
-            if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.xfull[xst], S::kTileBytes);
-            __syncwarp();
-            tensor_g2s_2d(xring + xst * S::kPieceBytes, &p.X, (k0 + px) * 64, t.first, xfull + xst * 8u);
-          }
-      } else {
-        const int j = i - n_a, tile = j / wide;
-        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[st], kSlotBytes);
-        __syncwarp();
-        tensor_g2s(dst, &p.B, (j - tile * wide) * 64, (o0 + tile) * 128, t.adapter, bar);
+          for (int j = 0; j < count; ++j) tensor_g2s(to + (uint32_t)(j * S::kTileBytes), &p.X, (k0 + px + j) * 64, t.first, 0, bar);
+        group.next();
       }
+    };
+    if (p.x_by_map) ask_x(min(np, S::kGroup));
+#pragma unroll 1
+    for (; i < n_a; ++i) {
+      const uint32_t bar = full + slot.at * 8u, dst = ring + slot.at * kSlotBytes;
+      if (i >= kRing) wait(empty + slot.at * 8u, slot.parity ^ 1u);
+      if (!__all_sync(~0u, ok)) break;
+      const int first = i * a_slot, count = p.whole ? a_slot : min(a_slot, np - first);
+      if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[slot.at], p.whole ? a_bytes : (uint32_t)(count * blocks) * 2048u);
+      __syncwarp();
+      if (p.whole) tensor_g2s(dst, a_map, 0, 0, k0 + first, t.adapter, bar);
+      else
+#pragma unroll 1
+        for (int j = 0; j < count; ++j) tensor_g2s(dst + (uint32_t)(j * blocks) * 2048u, a_map, (k0 + first + j) * 64, 0, t.adapter, bar);
+      slot.next();
+      if (p.x_by_map) ask_x(min(np, first + a_slot + S::kGroup));        // a group ahead
     }
-    if (lane == 0) { ctrl.asked = i; ctrl.x_asked = px; }
+#pragma unroll 1
+    for (int tile = o0, k = 0; i < total; ++i) {
+      if (i - kRing >= n_a && !met) { second(); met = true; }
+      const uint32_t bar = full + slot.at * 8u;
+      if (i >= kRing) wait(empty + slot.at * 8u, slot.parity ^ 1u);
+      if (!__all_sync(~0u, ok)) break;
+      if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[slot.at], kSlotBytes);
+      __syncwarp();
+      tensor_g2s(ring + slot.at * kSlotBytes, &p.B, k * 64, tile * 128, t.adapter, bar);
+      if (++k == wide) { k = 0; ++tile; }
+      slot.next();
+    }
+    if (lane == 0) { ctrl.asked = i; ctrl.x_asked = gx; }
     __syncwarp();
     if (!met) second();
   } else if (warp == kWarps + 1) {
@@ -280,51 +323,59 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     const uint64_t ring_desc = tc5::smem_desc_sw128(ring), x_desc = tc5::smem_desc_sw128(xring);
     constexpr uint32_t kA = idesc_of(F::kHalf, NT), kB = idesc_of(kHalf, NT);
+    Turn<kRing> slot;
+    {
+      Turn<S::kGroups> group;
+      uint32_t in_group = 0;
 #pragma unroll 1
-    for (int i = 0, px = 0; i < n_a; ++i) {
-      const uint32_t st = (uint32_t)(i % kRing);
-      wait(full + st * 8u, (uint32_t)(i / kRing) & 1u);
+      for (int i = 0, px = 0; i < n_a; ++i) {
+        wait(full + slot.at * 8u, slot.parity);
+        uint64_t w = ring_desc + (slot.at * kSlotBytes >> 4);
 #pragma unroll 1
-      for (int j = 0; j < a_slot && px < np; ++j, ++px) {
-        const uint32_t xst = (uint32_t)(px % S::kXSlots);
-        wait(xfull + xst * 8u, (uint32_t)(px / S::kXSlots) & 1u);
+        for (int j = 0; j < a_slot && px < np; ++j, ++px) {
+          if (in_group == 0) wait(xfull + group.at * 8u, group.parity);
+          if (!__all_sync(~0u, ok)) break;
+          tc5::tc_fence_after();
+          const uint64_t x = x_desc + ((group.at * S::kGroup + in_group) * S::kPieceBytes >> 4);
+#pragma unroll
+          for (int k = F::kX - 1; k >= 0; --k)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) umma(tmem, w + s * 2, x + (uint32_t)(k * S::kTileBytes / 16 + s * 2), kA, px > 0 || k < F::kX - 1 || s > 0);
+          w += (uint32_t)blocks * 128u;
+          if (++in_group == S::kGroup) {
+            tc5::umma_commit(&ctrl.xempty[group.at]);
+            group.next();
+            in_group = 0;
+          }
+        }
         if (!__all_sync(~0u, ok)) break;
-        tc5::tc_fence_after();
-        const uint64_t w = ring_desc + (st * kSlotBytes + (uint32_t)(j * blocks) * 2048u >> 4), x = x_desc + (xst * S::kPieceBytes >> 4);
-#pragma unroll
-        for (int k = F::kX - 1; k >= 0; --k)
-#pragma unroll
-          for (int s = 0; s < 4; ++s) umma(tmem, w + s * 2, x + (uint32_t)(k * S::kTileBytes / 16 + s * 2), kA, px > 0 || k < F::kX - 1 || s > 0);
-        tc5::umma_commit(&ctrl.xempty[xst]);
+        tc5::umma_commit(&ctrl.empty[slot.at]);
+        slot.next();
       }
-      if (!__all_sync(~0u, ok)) break;
-      tc5::umma_commit(&ctrl.empty[st]);
     }
     if (__all_sync(~0u, ok)) tc5::umma_commit(&ctrl.a_done);
     wait(smem_u32(&ctrl.h_ready), 0);
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
-    int i = n_a;
 #pragma unroll 1
     for (int o = 0; o < o1 - o0; ++o) {
       const uint32_t acc = (uint32_t)(o % S::kAcc), d = tmem + NT + acc * NT;
       wait(smem_u32(&ctrl.empty_acc[acc]), (uint32_t)(o / S::kAcc + 1) & 1u);
 #pragma unroll 1
-      for (int k = 0; k < wide; ++k, ++i) {
-        const uint32_t st = (uint32_t)(i % kRing);
-        wait(full + st * 8u, (uint32_t)(i / kRing) & 1u);
+      for (int k = 0; k < wide; ++k) {
+        wait(full + slot.at * 8u, slot.parity);
         if (!__all_sync(~0u, ok)) break;
         const int steps = min(4, blocks - k * 4), tail = rank - k * 64;
         if (tail < steps * 16) {
           // what lies behind the adapter's rank may be anything: up to where the last sixteen columns end, zeros
-          uint8_t* const slot = smem + st * kSlotBytes;
+          uint8_t* const weights = smem + slot.at * kSlotBytes;
 #pragma unroll 1
           for (int e = tail / 8; e < steps * 2; ++e) {
             const int keep = max(tail - e * 8, 0);
             auto of = [keep](int j) { return keep >= 2 * j + 2 ? ~0u : keep == 2 * j + 1 ? 0xFFFFu : 0u; };
 #pragma unroll 1
             for (int r = lane; r < 128; r += 32) {
-              uint4* const v = reinterpret_cast<uint4*>(slot + swizzled(r, e));
+              uint4* const v = reinterpret_cast<uint4*>(weights + swizzled(r, e));
               const uint4 old = *v;
               *v = make_uint4(old.x & of(0), old.y & of(1), old.z & of(2), old.w & of(3));
             }
@@ -333,19 +384,18 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
           __syncwarp();
         }
         tc5::tc_fence_after();
-        const uint64_t w = ring_desc + (st * kSlotBytes >> 4), h = x_desc + (uint32_t)(k * S::kTileBytes / 16);
+        const uint64_t w = ring_desc + (slot.at * kSlotBytes >> 4), h = x_desc + (uint32_t)(k * S::kTileBytes / 16);
         for (int j = last_term; j >= 0; --j)
 #pragma unroll 1
           for (int s = 0; s < steps; ++s) umma(d, w + (uint32_t)(s * 2), h + (uint32_t)(j * wide * S::kTileBytes / 16 + s * 2), kB, k > 0 || j < last_term || s > 0);
-        tc5::umma_commit(&ctrl.empty[st]);
+        tc5::umma_commit(&ctrl.empty[slot.at]);
+        slot.next();
       }
       if (!__all_sync(~0u, ok)) break;
       tc5::umma_commit(&ctrl.full_acc[acc]);
     }
   } else {
-    if (!p.x_by_map)
-#pragma unroll 1
-      for (int g = S::kGroup; g < np; g += S::kGroup) stage(g);
+    if (!p.x_by_map && np > 0) stage();
     // ---- this block's share of A x: lanes are the rank
     constexpr int kCols = NT / 2;
     const int quarter = warp & 3, col0 = (warp >> 2) * kCols;
@@ -446,7 +496,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     };
     if (tid == 0) {
       for (int i = max(0, ctrl.asked - kRing); i < ctrl.asked; ++i) arrived(full + (uint32_t)(i % kRing) * 8u, (uint32_t)(i / kRing) & 1u);
-      for (int i = max(0, ctrl.x_asked - S::kXSlots); i < ctrl.x_asked; ++i) arrived(xfull + (uint32_t)(i % S::kXSlots) * 8u, (uint32_t)(i / S::kXSlots) & 1u);
+      for (int i = max(0, ctrl.x_asked - S::kGroups); i < ctrl.x_asked; ++i) arrived(xfull + (uint32_t)(i % S::kGroups) * 8u, (uint32_t)(i / S::kGroups) & 1u);
     }
     if (warp == kWarps + 1) {
       tc5::umma_commit(&ctrl.drained);
@@ -462,16 +512,29 @@ cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
   using S = TileShape<X, W, NT>;
   const rwkvq_lowrank_args& a = p.a;
   const bool half = a.w_dtype == RWKVQ_F16;
-  for (int h = 0; h < 4 && (h == 0 || (a.rank + 15) / 16 >= 1 << h); ++h)
-    if (!encode(&p.A[h], a.A, half, a.ic, a.rank, a.n_adapters, 16 << h)) return cudaErrorUnknown;
-  if (!encode(&p.B, a.B, half, a.rank, a.oc, a.n_adapters, 128)) return cudaErrorUnknown;
+  const tc5::EncodeTiledFn fn = tc5::encode_tiled();
+  if (!fn || !encode(&p.B, a.B, half, a.rank, a.oc, a.n_adapters, 128)) return cudaErrorUnknown;
+  // Where columns are whole pieces of 64, a box has several of them one behind the other, as many as a slot holds of so many rows; else one.  Boxes for every sixteen of the rank
+  // that an adapter may have.
+  p.whole = a.ic % 64 == 0;
+  const CUtensorMapDataType type = half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  auto map = [&](CUtensorMap* m, const void* at, cuuint64_t rows, cuuint64_t row, cuuint64_t n, cuuint32_t box_rows, cuuint32_t box_pieces) {
+    const cuuint64_t pieces = (cuuint64_t)a.ic / 64, dims4[4] = {64, rows, pieces, n}, strides4[3] = {row * 2, 128, row * 2 * rows};
+    const cuuint64_t dims3[3] = {(cuuint64_t)a.ic, rows, n}, strides3[2] = {row * 2, row * 2 * rows};
+    const cuuint32_t box4[4] = {64, box_rows, box_pieces, 1}, box3[3] = {64, box_rows, 1}, step[4] = {1, 1, 1, 1};
+    return fn(m, type, p.whole ? 4 : 3, const_cast<void*>(at), p.whole ? dims4 : dims3, p.whole ? strides4 : strides3, p.whole ? box4 : box3, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  const int most = (a.rank + 15) / 16;
+  for (int blocks = a.ranks ? 1 : most; blocks <= most; ++blocks)
+    if (!map(&p.A[blocks - 1], a.A, (cuuint64_t)a.rank, (cuuint64_t)a.ic, (cuuint64_t)a.n_adapters, 16u * (cuuint32_t)blocks, (cuuint32_t)pieces_of(blocks))) return cudaErrorUnknown;
   p.x_by_map = !p.mu && S::kTerms == 1 && !(NT == kRows && single_rows(a));
   if (p.x_by_map) {
-    const cuuint64_t dims[2] = {(cuuint64_t)a.ic, (cuuint64_t)a.tokens}, strides[1] = {(cuuint64_t)(a.tokens > 1 ? a.x_row : a.ic) * 2};
-    const cuuint32_t box[2] = {64u, (cuuint32_t)NT}, step[2] = {1u, 1u};
-    const tc5::EncodeTiledFn fn = tc5::encode_tiled();
-    if (!fn || fn(&p.X, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.x), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    const cuuint64_t row = (cuuint64_t)(a.tokens > 1 ? a.x_row : a.ic);
+    const cuuint64_t dims[3] = {p.whole ? 64 : (cuuint64_t)a.ic, (cuuint64_t)a.tokens, p.whole ? (cuuint64_t)a.ic / 64 : 1}, strides[2] = {row * 2, p.whole ? 128 : row * 2};
+    const cuuint32_t box[3] = {64, NT, p.whole ? (cuuint32_t)S::kGroup : 1}, step[3] = {1, 1, 1};
+    if (fn(&p.X, type, 3, const_cast<void*>(a.x), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return cudaErrorUnknown;
   }
   static SmemOptIn opt_in(kCarveOut);
