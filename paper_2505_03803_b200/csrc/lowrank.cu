@@ -114,8 +114,11 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
     for (int e = tid; e < n * eights; e += kThreads) {
       const int r = e / eights, eight = e - r * eights, col = kp * 64 + eight * 8, row = grouped ? t.rows[r] : t.first + r;
       const Eights<X> raw = load_eights<X, decltype(mix)::value>(p, row, grouped ? row : t.seq, grouped || row == t.start, col);
+      const MuWords words = load_mu<decltype(mix)::value>(p, col);
+      float2 mu[4];
+      mu_of<decltype(mix)::value>(p, codebook, words, col, mu);
       float x[8];
-      mix_eights<X, decltype(mix)::value>(p, codebook, raw, min(col, a.ic - 8), x);
+      mix_eights<X, decltype(mix)::value>(raw, mu, x);
       put_terms<F>(xs + eight / 8 * kXPiece + swizzled(r, eight & 7), kPass * kXPiece, x);
     }
   };

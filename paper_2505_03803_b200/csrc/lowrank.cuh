@@ -235,11 +235,10 @@ __device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const CUtensorMap*
                ::"r"(dst_smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
-// Eight columns of a row of x, of the row in front of it, and their indices of the token-shift vector, as they lie in memory.  All loads come from somewhere valid and none
-// is in a branch of its own, so that they are on their way together; `there` says what counts.
+// Eight columns of a row of x and of the row in front of it, as they lie in memory.  All loads come from somewhere valid and none is in a branch of its own, so that they are on their
+// way together; `there` says what counts.
 template <typename X> struct Eights {
   uint4 x[sizeof(X) / 2], before[sizeof(X) / 2];
-  uint32_t lo, hi;
   bool there, has_before;
 };
 template <typename X, bool kMix>
@@ -256,12 +255,31 @@ __device__ __forceinline__ Eights<X> load_eights(const Args& p, int row, int seq
     e.has_before = a.x_prev || !begins || a.xprev0;
 #pragma unroll
     for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.before[i] = __ldg(reinterpret_cast<const uint4*>(b) + i);
-    // four indices are 4 * mu_bits neighbouring bits from a byte's beginning; behind the indices lies the codebook
-    const uint32_t* const words = reinterpret_cast<const uint32_t*>(p.mu) + ((uint32_t)(col >> 3) * (uint32_t)p.mu_bits >> 3);
-    e.lo = __ldg(words);
-    e.hi = __ldg(words + 1);
   }
   return e;
+}
+// Their indices of the token-shift vector: four are 4 * mu_bits neighbouring bits from a byte's beginning; behind the indices lies the codebook.
+struct MuWords { uint32_t lo, hi; };
+template <bool kMix>
+__device__ __forceinline__ MuWords load_mu(const Args& p, int col) {
+  MuWords m = {0, 0};
+  if constexpr (kMix) {
+    const uint32_t* const words = reinterpret_cast<const uint32_t*>(p.mu) + ((uint32_t)(min(col, p.a.ic - 8) >> 3) * (uint32_t)p.mu_bits >> 3);
+    m.lo = __ldg(words);
+    m.hi = __ldg(words + 1);
+  }
+  return m;
+}
+template <bool kMix>
+__device__ __forceinline__ void mu_of(const Args& p, const uint32_t* codebook, const MuWords& w, int col, float2 (&m)[4]) {
+  if constexpr (kMix) {
+    const uint32_t bits = (uint32_t)p.mu_bits, f = __funnelshift_r(w.lo, w.hi, ((uint32_t)(min(col, p.a.ic - 8) >> 3) * bits >> 1 & 3u) * 8u), mask = (1u << bits) - 1u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t pair = codebook[f >> (uint32_t)j * bits & mask];
+      m[j] = __half22float2(*reinterpret_cast<const __half2*>(&pair));
+    }
+  }
 }
 template <typename X>
 __device__ __forceinline__ void numbers(const uint4 (&w)[sizeof(X) / 2], float (&f)[8]) {
@@ -271,7 +289,7 @@ __device__ __forceinline__ void numbers(const uint4 (&w)[sizeof(X) / 2], float (
 }
 // x_mix of eight columns, in fp32 but rounded to X; zeros behind the last column.
 template <typename X, bool kMix>
-__device__ __forceinline__ void mix_eights(const Args& p, const uint32_t* codebook, const Eights<X>& e, int col, float (&x)[8]) {
+__device__ __forceinline__ void mix_eights(const Eights<X>& e, const float2 (&m)[4], float (&x)[8]) {
   auto counts = [](const uint4& w, bool yes) { return make_uint4(yes ? w.x : 0u, yes ? w.y : 0u, yes ? w.z : 0u, yes ? w.w : 0u); };
   uint4 w[sizeof(X) / 2];
 #pragma unroll
@@ -282,13 +300,10 @@ __device__ __forceinline__ void mix_eights(const Args& p, const uint32_t* codebo
 #pragma unroll
     for (int i = 0; i < (int)sizeof(X) / 2; ++i) w[i] = counts(e.before[i], e.there && e.has_before);
     numbers<X>(w, y);
-    const uint32_t bits = (uint32_t)p.mu_bits, f = __funnelshift_r(e.lo, e.hi, ((uint32_t)(col >> 3) * bits >> 1 & 3u) * 8u), mask = (1u << bits) - 1u;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t pair = codebook[f >> (uint32_t)j * bits & mask];
-      const float2 m = __half22float2(*reinterpret_cast<const __half2*>(&pair));
-      x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m.x, x[2 * j])));
-      x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m.y, x[2 * j + 1])));
+      x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m[j].x, x[2 * j])));
+      x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m[j].y, x[2 * j + 1])));
     }
   }
 }

@@ -40,7 +40,7 @@ struct TileShape {
   static_assert(kShare >= 8 * kMostCounted || NT == 64, "room for counting the rows of adapters");
 };
 struct TileCtrl {
-  uint64_t full[kRing], empty[kRing], xfull[kMostGroups], xempty[kMostGroups], a_done, h_ready, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
+  uint64_t full[kRing], empty[kRing], xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
   int abort_flag, asked, x_asked;
   uint32_t tmem_base;
   float back[64];                 // of each row: the power of two that its A x was divided by
@@ -103,21 +103,27 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
     const int r = col0 + max(min(i * 4 + r_lane, rows - 1), -col0);
     at[i] = static_cast<Y*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row;
   }
-  // y of the next tile is on its way while this one's is added to
-  Four<Y> y[kCols / 4], ahead[kCols / 4];
-  auto load = [&](int o) {
+  // y of the next tiles is on its way while this one's is added to: some 48 to 64 KB an SM
+  constexpr int kDepth = sizeof(Y) == 2 ? 3 : 2;
+  Four<Y> y[kCols / 4], ahead[kDepth][kCols / 4];
+  auto load = [&](int o, Four<Y> (&to)[kCols / 4]) {
     const int col = min((o0 + o) * 128 + quarter * 32 + quad * 4, a.oc - 4);
-    if (rows > 0)
+    if (rows > 0 && o < o1 - o0)
 #pragma unroll
-      for (int i = 0; i < kCols / 4; ++i) ahead[i] = *reinterpret_cast<const Four<Y>*>(at[i] + col);
+      for (int i = 0; i < kCols / 4; ++i) to[i] = *reinterpret_cast<const Four<Y>*>(at[i] + col);
   };
-  load(0);
+#pragma unroll
+  for (int k = 0; k < kDepth; ++k) load(k, ahead[k]);
 #pragma unroll 1
   for (int o = 0; o < o1 - o0; ++o) {
     const int acc = o % accs, col = (o0 + o) * 128 + quarter * 32 + quad * 4;
 #pragma unroll
-    for (int i = 0; i < kCols / 4; ++i) y[i] = ahead[i];
-    if (o + 1 < o1 - o0) load(o + 1);
+    for (int i = 0; i < kCols / 4; ++i) {
+      y[i] = ahead[0][i];
+#pragma unroll
+      for (int k = 0; k + 1 < kDepth; ++k) ahead[k][i] = ahead[k + 1][i];
+    }
+    load(o + kDepth, ahead[kDepth - 1]);
     ok = ok && tc5::mbar_wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / accs) & 1u, abortp, p.status);
     if (!__all_sync(~0u, ok)) break;
     tc5::tc_fence_after();
@@ -166,9 +172,15 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     for (int i = 0; i < kRing; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], 1); }
     for (int i = 0; i < S::kGroups; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : kWarps); tc5::mbar_init(&ctrl.xempty[i], 1); }
     for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], kWarps); }
-    tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.h_ready, kWarps); tc5::mbar_init(&ctrl.drained, 1);
+    tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.drained, 1);
     ctrl.abort_flag = ctrl.asked = ctrl.x_asked = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\nfence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (tid == kThreads) {          // the maps themselves are fetched from memory, too
+    auto fetch = [](const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); };
+    fetch(&p.A[(a.rank + 15) / 16 - 1]);
+    fetch(&p.B);
+    if (p.x_by_map) fetch(&p.X);
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (p.mu)
@@ -192,11 +204,16 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     constexpr int kN = decltype(per)::value;
     Turn<S::kGroups> turn;
     Eights<X> raw[kN], ahead[kN];
+    MuWords words, words_ahead;
+    // kThreads is a multiple of a row's eights: the columns are the same for all rows of a thread
+    const int piece = tid % S::kEights / 8;
+    auto col_of = [&](int g) { return (k0 + min(g * S::kGroup + piece, np - 1)) * 64 + (tid & 7) * 8; };
     auto load = [&](int g, Eights<X> (&e)[kN]) {
+      words_ahead = load_mu<kMix>(p, col_of(g));
 #pragma unroll
       for (int j = 0; j < kN; ++j) {
         const int i = tid + j * kThreads, r = min(i / S::kEights, n - 1), row = row_of(r);
-        e[j] = load_eights<X, kMix>(p, row, grouped ? row : t.seq, grouped || row == t.start, (k0 + min(g * S::kGroup + i % S::kEights / 8, np - 1)) * 64 + (i & 7) * 8);
+        e[j] = load_eights<X, kMix>(p, row, grouped ? row : t.seq, grouped || row == t.start, col_of(g));
       }
     };
     load(0, ahead);
@@ -204,15 +221,18 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     for (int g = 0; g * S::kGroup < np; ++g) {
 #pragma unroll
       for (int j = 0; j < kN; ++j) raw[j] = ahead[j];
+      words = words_ahead;
       if ((g + 1) * S::kGroup < np) load(g + 1, ahead);
       if (g >= S::kGroups) wait(xempty + turn.at * 8u, turn.parity ^ 1u);
+      float2 mu[4];
+      mu_of<kMix>(p, codebook, words, col_of(g), mu);
 #pragma unroll
       for (int j = 0; j < kN; ++j) {
-        const int i = tid + j * kThreads, row = i / S::kEights, piece = i % S::kEights / 8;
+        const int row = (tid + j * kThreads) / S::kEights;
         if (j * kThreads / S::kEights >= n) continue;          // of no thread
         float x[8];
-        mix_eights<X, kMix>(p, codebook, raw[j], min((k0 + g * S::kGroup + piece) * 64 + (i & 7) * 8, a.ic - 8), x);
-        if (row < n) put_terms<F>(xs + (turn.at * S::kGroup + piece) * S::kPieceBytes + swizzled(row, i & 7), S::kTileBytes, x);
+        mix_eights<X, kMix>(raw[j], mu, x);
+        if (row < n) put_terms<F>(xs + (turn.at * S::kGroup + piece) * S::kPieceBytes + swizzled(row, tid & 7), S::kTileBytes, x);
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
@@ -234,17 +254,6 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     if (lane == 0) find_adapter(p, t);
   } else if (warp == kWarps + 1) {
     tc5::tmem_alloc(&ctrl.tmem_base, S::kTmemCols);
-  } else {
-    // x's and y's rows on their way to the second-level cache while the adapter is looked up
-    auto fetch = [](const void* base, long long at, int bytes, int size) {
-      if (bytes > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(base) + at * size), "r"(bytes * size) : "memory");
-    };
-    if (tid < n) {
-      const int columns = min((k0 + np) * 64, a.ic) - k0 * 64;
-      fetch(a.x, (long long)row_of(tid) * a.x_row + k0 * 64, columns, (int)sizeof(X));
-      if (a.x_prev) fetch(a.x_prev, (long long)row_of(tid) * a.x_prev_row + k0 * 64, columns, (int)sizeof(X));
-      fetch(a.y, (long long)row_of(tid) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
-    }
   }
   tc5::tc_fence_before();
   __syncthreads();
@@ -262,8 +271,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     // ---- copies.  This warp and the next bring nothing to the first meeting of the cluster and do not hold it up: what they wait for below comes behind it.
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     const int total = n_a + (o1 - o0) * wide;
-    // The warps that store y wait for the second meeting, in which the blocks have read one another's shares, before they give anything back: it is not held up, either,
-    // by waits for slots that B had.
+    // Nor does it hold up the second one by waits for slots that B had, which are given back behind that.
     auto second = [] { asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory"); };
     bool met = false;
     int i = 0, px = 0, gx = 0;
@@ -354,9 +362,10 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       }
     }
     if (__all_sync(~0u, ok)) tc5::umma_commit(&ctrl.a_done);
-    wait(smem_u32(&ctrl.h_ready), 0);
+    // the second meeting: A x is there, from all blocks
     __syncwarp();
-    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("fence.proxy.async;" ::: "memory");
 #pragma unroll 1
     for (int o = 0; o < o1 - o0; ++o) {
       const uint32_t acc = (uint32_t)(o % S::kAcc), d = tmem + NT + acc * NT;
@@ -369,16 +378,17 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
         if (tail < steps * 16) {
           // what lies behind the adapter's rank may be anything: up to where the last sixteen columns end, zeros
           uint8_t* const weights = smem + slot.at * kSlotBytes;
-#pragma unroll 1
-          for (int e = tail / 8; e < steps * 2; ++e) {
-            const int keep = max(tail - e * 8, 0);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int e = tail / 8 + h, keep = max(tail - e * 8, 0);
             auto of = [keep](int j) { return keep >= 2 * j + 2 ? ~0u : keep == 2 * j + 1 ? 0xFFFFu : 0u; };
-#pragma unroll 1
-            for (int r = lane; r < 128; r += 32) {
-              uint4* const v = reinterpret_cast<uint4*>(weights + swizzled(r, e));
-              const uint4 old = *v;
-              *v = make_uint4(old.x & of(0), old.y & of(1), old.z & of(2), old.w & of(3));
-            }
+            if (e >= steps * 2) continue;
+            uint4 v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const uint4*>(weights + swizzled(r * 32 + lane, e));
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              *reinterpret_cast<uint4*>(weights + swizzled(r * 32 + lane, e)) = make_uint4(v[r].x & of(0), v[r].y & of(1), v[r].z & of(2), v[r].w & of(3));
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
@@ -419,73 +429,79 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     tc5::tc_fence_before();
     cluster.sync();
 
-    // ---- all of A x, as operands: as many lanes to a row as there are fours of the rank
-    auto gather = [&](auto blocks_of_cluster) {
-    constexpr int kC = decltype(blocks_of_cluster)::value;
-    const int wl = blocks == 1 ? 4 : blocks == 2 ? 8 : blocks <= 4 ? 16 : 32, r4 = lane % wl * 4;
+    // ---- A x: each block adds up a share of the rows, and gives them to all as operands.  As many lanes to a row as there are fours of the rank
     const float scale = t.scale;
+    auto add_up = [&](auto blocks_of_cluster) {
+      constexpr int kC = decltype(blocks_of_cluster)::value;
+      const int wl = blocks == 1 ? 4 : blocks == 2 ? 8 : blocks <= 4 ? 16 : 32, r4 = lane % wl * 4, row1 = n * (c + 1) / kC;
 #pragma unroll 1
-    for (int row0 = warp * (32 / wl); row0 < n; row0 += kWarps * (32 / wl)) {
-      const int row = row0 + lane / wl;
-      float h[4] = {0.f, 0.f, 0.f, 0.f};
-      float4 s[kC];
+      for (int row0 = n * c / kC + warp * (32 / wl); row0 < row1; row0 += kWarps * (32 / wl)) {
+        const int row = row0 + lane / wl;
+        const bool there = row < row1 && r4 < blocks * 16;
+        float h[4] = {0.f, 0.f, 0.f, 0.f};
+        float4 s[kC];
 #pragma unroll
-      for (int k = 0; k < kC; ++k) s[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(share, k) + min(row, n - 1) * kMostRank + r4);
+        for (int k = 0; k < kC; ++k) s[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(share, k) + min(row, n - 1) * kMostRank + r4);
 #pragma unroll
-      for (int k = 0; k < kC; ++k) { h[0] += s[k].x; h[1] += s[k].y; h[2] += s[k].z; h[3] += s[k].w; }
+        for (int k = 0; k < kC; ++k) { h[0] += s[k].x; h[1] += s[k].y; h[2] += s[k].z; h[3] += s[k].w; }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) h[j] = r4 + j < rank ? h[j] * scale : 0.f;
-      uint8_t* const to = xs + r4 / 64 * S::kTileBytes + swizzled(row, r4 / 8 & 7) + (r4 & 4) * 2;
-      const bool there = row < n && r4 < blocks * 16;
-      if constexpr (kHalf) {
-        float top = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
-        for (int o = 1; o < wl; o *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-        // 2^up brings the largest number to 2^14; an infinity or NaN stays what it is
-        const int up = top > 0.f && top < INFINITY ? min(14 - ilogbf(top), 126) : 0;
-        const float by = __uint_as_float((uint32_t)(127 + max(up, -126)) << 23);
-        if (there && r4 == 0) ctrl.back[row] = __uint_as_float((uint32_t)(127 - max(up, -126)) << 23);
-        __half hi[4], lo[4];
+        for (int j = 0; j < 4; ++j) h[j] = r4 + j < rank ? h[j] * scale : 0.f;
+        uint8_t* const to = xs + r4 / 64 * S::kTileBytes + swizzled(row, r4 / 8 & 7) + (r4 & 4) * 2;
+        uint2 terms[3];
+        float back = 1.f;
+        if constexpr (kHalf) {
+          float top = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
+          for (int o = 1; o < wl; o *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+          // 2^up brings the largest number to 2^14; an infinity or NaN stays what it is
+          const int up = top > 0.f && top < INFINITY ? max(min(14 - ilogbf(top), 126), -126) : 0;
+          const float by = __uint_as_float((uint32_t)(127 + up) << 23);
+          back = __uint_as_float((uint32_t)(127 - up) << 23);
+          __half hi[4], lo[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float x = h[j] * by;
-          hi[j] = __float2half_rn(x);
-          lo[j] = fabsf(x) < INFINITY ? __float2half_rn(x - __half2float(hi[j])) : __float2half_rn(0.f);
+          for (int j = 0; j < 4; ++j) {
+            const float x = h[j] * by;
+            hi[j] = __float2half_rn(x);
+            lo[j] = fabsf(x) < INFINITY ? __float2half_rn(x - __half2float(hi[j])) : __float2half_rn(0.f);
+          }
+          terms[0] = make_uint2(pair_bits(hi[0], hi[1]), pair_bits(hi[2], hi[3]));
+          terms[1] = make_uint2(pair_bits(lo[0], lo[1]), pair_bits(lo[2], lo[3]));
+        } else {
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            __nv_bfloat16 b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = k == 1 && last_term == 1 ? __float2bfloat16_rn(h[j]) : term(h[j]);
+            terms[k] = make_uint2(pair_bits(b[0], b[1]), pair_bits(b[2], b[3]));
+          }
         }
-        if (there) {
-          *reinterpret_cast<uint2*>(to) = make_uint2(pair_bits(hi[0], hi[1]), pair_bits(hi[2], hi[3]));
-          *reinterpret_cast<uint2*>(to + wide * S::kTileBytes) = make_uint2(pair_bits(lo[0], lo[1]), pair_bits(lo[2], lo[3]));
-        }
-      } else {
+        if (there)
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          if (k > last_term) continue;
-          __nv_bfloat16 b[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) b[j] = k == 1 && last_term == 1 ? __float2bfloat16_rn(h[j]) : term(h[j]);
-          if (there) *reinterpret_cast<uint2*>(to + k * wide * S::kTileBytes) = make_uint2(pair_bits(b[0], b[1]), pair_bits(b[2], b[3]));
-        }
+          for (int k = 0; k < kC; ++k) {
+            uint8_t* const there_to = cluster.map_shared_rank(to, k);
+            *reinterpret_cast<uint2*>(there_to) = terms[0];
+            *reinterpret_cast<uint2*>(there_to + wide * S::kTileBytes) = terms[1];
+            if (!kHalf && last_term == 2) *reinterpret_cast<uint2*>(there_to + 2 * wide * S::kTileBytes) = terms[2];
+            if (kHalf && r4 == 0) *cluster.map_shared_rank(&ctrl.back[row], k) = back;
+          }
       }
-    }
     };
-    if (C == 8) gather(std::integral_constant<int, 8>());
-    else if (C == 4) gather(std::integral_constant<int, 4>());
-    else if (C == 2) gather(std::integral_constant<int, 2>());
-    else gather(std::integral_constant<int, 1>());
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    if (lane == 0) tc5::mbar_arrive(&ctrl.h_ready);
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (C == 8) add_up(std::integral_constant<int, 8>());
+    else if (C == 4) add_up(std::integral_constant<int, 4>());
+    else if (C == 2) add_up(std::integral_constant<int, 2>());
+    else add_up(std::integral_constant<int, 1>());
+    asm volatile("fence.proxy.async;" ::: "memory");
+    // the second meeting, behind which no block touches another's memory
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 
     // ---- y: 32 columns of it for a warp, and half of the tile's rows.  A lane of the accumulator is a column; the way to four neighbouring columns a lane is through
-    // shared memory, where the other blocks have read the shares.
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    // shared memory, where the shares were.
     float* const turn = share + warp * kCols * 32;
     const int quad = lane & 7, r_lane = lane >> 3;
     if (a.y_dtype == RWKVQ_F32) store_y<kCols, float, kHalf>(p, t, ctrl, lanes + NT, NT, S::kAcc, o0, o1, quarter, col0, n, grouped, turn, quad, r_lane, abortp, ok);
     else if (a.y_dtype == RWKVQ_F16) store_y<kCols, __half, kHalf>(p, t, ctrl, lanes + NT, NT, S::kAcc, o0, o1, quarter, col0, n, grouped, turn, quad, r_lane, abortp, ok);
     else store_y<kCols, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + NT, NT, S::kAcc, o0, o1, quarter, col0, n, grouped, turn, quad, r_lane, abortp, ok);
   }
-  if (warp >= kWarps) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // no block ends while another reads its share
+  if (warp == kWarps) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   tc5::tc_fence_before();
   __syncthreads();
   tc5::tc_fence_after();
