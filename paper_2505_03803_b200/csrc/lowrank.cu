@@ -117,9 +117,7 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
       const MuWords words = load_mu<decltype(mix)::value>(p, col);
       float2 mu[4];
       mu_of<decltype(mix)::value>(p, codebook, words, col, mu);
-      float x[8];
-      mix_eights<X, decltype(mix)::value>(raw, mu, x);
-      put_terms<F>(xs + eight / 8 * kXPiece + swizzled(r, eight & 7), kPass * kXPiece, x);
+      put_eights<X, F, decltype(mix)::value>(raw, mu, xs + eight / 8 * kXPiece + swizzled(r, eight & 7), kPass * kXPiece);
     }
   };
   auto stage = [&](int kp, int ke) { if (p.mu) stage_x(std::true_type(), kp, ke); else stage_x(std::false_type(), kp, ke); };

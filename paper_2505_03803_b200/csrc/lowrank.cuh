@@ -200,7 +200,6 @@ template <> __device__ __forceinline__ float from_float<float>(float x) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-template <typename T> struct Eight { T v[8]; };
 // The next bf16 term of x, which is left with what the term leaves.  Cut off, not rounded, so that the largest numbers do not become infinite; of an infinity or
 // NaN nothing is left.
 __device__ __forceinline__ __nv_bfloat16 term(float& x) {
@@ -281,60 +280,69 @@ __device__ __forceinline__ void mu_of(const Args& p, const uint32_t* codebook, c
     }
   }
 }
-template <typename X>
-__device__ __forceinline__ void numbers(const uint4 (&w)[sizeof(X) / 2], float (&f)[8]) {
-  const Eight<X> e = *reinterpret_cast<const Eight<X>*>(w);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = to_float<X>(e.v[i]);
+// Pairs of 16-bit numbers; packed conversions, which take a fraction of what single ones do.
+__device__ __forceinline__ float2 pair_of(uint32_t w, __half) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ float2 pair_of(uint32_t w, __nv_bfloat16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ uint32_t rounded(float2 f, __half) {
+  const __half2 h = __floats2half2_rn(f.x, f.y);
+  return *reinterpret_cast<const uint32_t*>(&h);
 }
-// x_mix of eight columns, in fp32 but rounded to X; zeros behind the last column.
-template <typename X, bool kMix>
-__device__ __forceinline__ void mix_eights(const Eights<X>& e, const float2 (&m)[4], float (&x)[8]) {
+__device__ __forceinline__ uint32_t rounded(float2 f, __nv_bfloat16) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// A pair as its next bf16 term, cut off, and what that leaves.
+__device__ __forceinline__ uint32_t cut_off(float2& f) {
+  const uint32_t lo = __float_as_uint(f.x), hi = __float_as_uint(f.y);
+  f.x -= __uint_as_float(lo & 0xFFFF0000u);
+  f.y -= __uint_as_float(hi & 0xFFFF0000u);
+  return __byte_perm(lo, hi, 0x7632);
+}
+__device__ __forceinline__ float2 mixed(float2 x, float2 y, float2 m) { return make_float2(fmaf(y.x - x.x, m.x, x.x), fmaf(y.y - x.y, m.y, x.y)); }
+
+// x_mix of eight columns, rounded to X, as operands of the tensor cores: F::kX terms, `next` bytes from one to the next; zeros behind the last column.  (What the first terms leave of
+// an infinity is NaN.)
+template <typename X, typename F, bool kMix>
+__device__ __forceinline__ void put_eights(const Eights<X>& e, const float2 (&m)[4], uint8_t* to, uint32_t next) {
   auto counts = [](const uint4& w, bool yes) { return make_uint4(yes ? w.x : 0u, yes ? w.y : 0u, yes ? w.z : 0u, yes ? w.w : 0u); };
-  uint4 w[sizeof(X) / 2];
+  uint32_t out[3][4];
+  if constexpr (sizeof(X) == 2) {
+    const uint4 x4 = counts(e.x[0], e.there);
+    uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+    if constexpr (kMix) {
+      const uint4 y4 = counts(e.before[0], e.there && e.has_before);
+      const uint32_t y[4] = {y4.x, y4.y, y4.z, y4.w};
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(X) / 2; ++i) w[i] = counts(e.x[i], e.there);
-  numbers<X>(w, x);
-  if constexpr (kMix) {
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(X) / 2; ++i) w[i] = counts(e.before[i], e.there && e.has_before);
-    numbers<X>(w, y);
+      for (int j = 0; j < 4; ++j) x[j] = rounded(mixed(pair_of(x[j], X()), pair_of(y[j], X()), m[j]), X());
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      x[2 * j] = to_float<X>(from_float<X>(fmaf(y[2 * j] - x[2 * j], m[j].x, x[2 * j])));
-      x[2 * j + 1] = to_float<X>(from_float<X>(fmaf(y[2 * j + 1] - x[2 * j + 1], m[j].y, x[2 * j + 1])));
+      out[0][j] = x[j];
+      if constexpr (F::kX == 2) {
+        float2 f = pair_of(x[j], X());
+        out[0][j] = cut_off(f);
+        out[1][j] = rounded(f, __nv_bfloat16());
+      }
     }
-  }
-}
-// Eight numbers as operands of the tensor cores: the next term of each (kX in all), which is taken from them.  All but the last of several terms are cut off to bf16, the last
-// is exact.  (What is left of an infinity is NaN.)
-template <typename F, bool kLast>
-__device__ __forceinline__ uint4 next_term(float (&x)[8]) {
-  uint32_t v[4];
+  } else {
+    const uint4 a4 = counts(e.x[0], e.there), b4 = counts(e.x[1], e.there);
+    const uint32_t x[8] = {a4.x, a4.y, a4.z, a4.w, b4.x, b4.y, b4.z, b4.w};
+    uint32_t y[8] = {};
+    if constexpr (kMix) {
+      const uint4 c4 = counts(e.before[0], e.there && e.has_before), d4 = counts(e.before[1], e.there && e.has_before);
+      y[0] = c4.x; y[1] = c4.y; y[2] = c4.z; y[3] = c4.w; y[4] = d4.x; y[5] = d4.y; y[6] = d4.z; y[7] = d4.w;
+    }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if constexpr (F::kHalf) {
-      const __half2 h = __floats2half2_rn(x[2 * j], x[2 * j + 1]);
-      v[j] = *reinterpret_cast<const uint32_t*>(&h);
-    } else if constexpr (kLast) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
-      v[j] = *reinterpret_cast<const uint32_t*>(&h);
-    } else {
-      const uint32_t lo = __float_as_uint(x[2 * j]), hi = __float_as_uint(x[2 * j + 1]);
-      v[j] = __byte_perm(lo, hi, 0x7632);
-      x[2 * j] -= __uint_as_float(lo & 0xFFFF0000u);
-      x[2 * j + 1] -= __uint_as_float(hi & 0xFFFF0000u);
+    for (int j = 0; j < 4; ++j) {
+      float2 f = make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
+      if constexpr (kMix) f = mixed(f, make_float2(__uint_as_float(y[2 * j]), __uint_as_float(y[2 * j + 1])), m[j]);
+      out[0][j] = cut_off(f);
+      out[1][j] = cut_off(f);
+      out[2][j] = rounded(f, __nv_bfloat16());
     }
   }
-  return make_uint4(v[0], v[1], v[2], v[3]);
-}
-// All terms, `next` bytes from one to the next.
-template <typename F>
-__device__ __forceinline__ void put_terms(uint8_t* to, uint32_t next, float (&x)[8]) {
-  if constexpr (F::kX >= 2) { *reinterpret_cast<uint4*>(to) = next_term<F, false>(x); to += next; }
-  if constexpr (F::kX == 3) { *reinterpret_cast<uint4*>(to) = next_term<F, false>(x); to += next; }
-  *reinterpret_cast<uint4*>(to) = next_term<F, true>(x);
+#pragma unroll
+  for (int k = 0; k < F::kX; ++k) *reinterpret_cast<uint4*>(to + k * next) = make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]);
 }
 
 // [n][rows][cols] of 16-bit numbers as boxes of 64 columns x box_rows rows in the 128-byte swizzle; what lies outside reads as zero.

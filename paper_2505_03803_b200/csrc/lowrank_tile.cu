@@ -56,10 +56,18 @@ struct Turn {
 __device__ __forceinline__ constexpr uint32_t idesc_of(bool half, int N) {
   return (1u << 4) | (half ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
 }
-// Sixteen columns of both operands, by a converged warp.
-__device__ __forceinline__ void umma(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
-  asm volatile("{\n .reg .pred q, p;\n elect.sync _|q, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
-               " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
+// Up to four steps of sixteen columns of both operands, by a converged warp: one lane is elected for all of them (a step at a time took some 100 cycles each).
+__device__ __forceinline__ void umma(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate, int steps) {
+  asm volatile(
+      "{\n .reg .pred q, p, one, q1, q2, q3;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      " elect.sync _|q, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n setp.eq.b32 one, 0, 0;\n"
+      " setp.gt.and.s32 q1, %5, 1, q;\n setp.gt.and.s32 q2, %5, 2, q;\n setp.gt.and.s32 q3, %5, 3, q;\n"
+      " add.u64 a1, %1, 2;\n add.u64 a2, %1, 4;\n add.u64 a3, %1, 6;\n add.u64 b1, %2, 2;\n add.u64 b2, %2, 4;\n add.u64 b3, %2, 6;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      " @q1 tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, one;\n"
+      " @q2 tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, one;\n"
+      " @q3 tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, one;\n}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate), "r"(steps) : "memory");
 }
 // 32 lanes x kCols columns; see tc5::tmem_ld32_issue.  Waits for them.
 template <int kCols>
@@ -230,9 +238,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       for (int j = 0; j < kN; ++j) {
         const int row = (tid + j * kThreads) / S::kEights;
         if (j * kThreads / S::kEights >= n) continue;          // of no thread
-        float x[8];
-        mix_eights<X, kMix>(raw[j], mu, x);
-        if (row < n) put_terms<F>(xs + (turn.at * S::kGroup + piece) * S::kPieceBytes + swizzled(row, tid & 7), S::kTileBytes, x);
+        if (row < n) put_eights<X, F, kMix>(raw[j], mu, xs + (turn.at * S::kGroup + piece) * S::kPieceBytes + swizzled(row, tid & 7), S::kTileBytes);
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
@@ -346,9 +352,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
           tc5::tc_fence_after();
           const uint64_t x = x_desc + ((group.at * S::kGroup + in_group) * S::kPieceBytes >> 4);
 #pragma unroll
-          for (int k = F::kX - 1; k >= 0; --k)
-#pragma unroll
-            for (int s = 0; s < 4; ++s) umma(tmem, w + s * 2, x + (uint32_t)(k * S::kTileBytes / 16 + s * 2), kA, px > 0 || k < F::kX - 1 || s > 0);
+          for (int k = F::kX - 1; k >= 0; --k) umma(tmem, w, x + (uint32_t)(k * S::kTileBytes / 16), kA, px > 0 || k < F::kX - 1, 4);
           w += (uint32_t)blocks * 128u;
           if (++in_group == S::kGroup) {
             tc5::umma_commit(&ctrl.xempty[group.at]);
@@ -395,9 +399,8 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
         }
         tc5::tc_fence_after();
         const uint64_t w = ring_desc + (slot.at * kSlotBytes >> 4), h = x_desc + (uint32_t)(k * S::kTileBytes / 16);
-        for (int j = last_term; j >= 0; --j)
 #pragma unroll 1
-          for (int s = 0; s < steps; ++s) umma(d, w + (uint32_t)(s * 2), h + (uint32_t)(j * wide * S::kTileBytes / 16 + s * 2), kB, k > 0 || j < last_term || s > 0);
+        for (int j = last_term; j >= 0; --j) umma(d, w, h + (uint32_t)(j * wide * S::kTileBytes / 16), kB, k > 0 || j < last_term, steps);
         tc5::umma_commit(&ctrl.empty[slot.at]);
         slot.next();
       }
@@ -523,6 +526,23 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   if (warp == kWarps + 1) tc5::tmem_dealloc(tmem, S::kTmemCols);
 }
 
+// Clusters of C blocks that are on the device at once; asked for once per device (the kernels are alike in this: one block an SM).
+long long clusters_at_once(const void* kernel, unsigned C) {
+  static std::atomic<int> known[kMaxDevices][4];
+  const int dev = current_device(), h = C == 8 ? 3 : C == 4 ? 2 : C == 2 ? 1 : 0;
+  int n = dev >= 0 ? known[dev][h].load(std::memory_order_relaxed) : 0;
+  if (n > 0) return n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(C); cfg.blockDim = dim3(kTileAll); cfg.dynamicSmemBytes = kSmemBytes;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) { cudaGetLastError(); return std::max(1u, sm_count() * 3 / 4 / C); }
+  if (dev >= 0) known[dev][h].store(n, std::memory_order_relaxed);
+  return n;
+}
+
 template <typename X, typename W, int NT>
 cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
   using S = TileShape<X, W, NT>;
@@ -556,11 +576,11 @@ cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
   static SmemOptIn opt_in(kCarveOut);
   const cudaError_t e = opt_in((const void*)lowrank_tile_kernel<X, W, NT>, kSmemBytes);
   if (e != cudaSuccess) return e;
-  // one block an SM: clusters as wide as that allows, then several that divide a tile's rows of B and each multiply A x for themselves
-  const long long sms = sm_count();
+  // One block an SM: clusters as wide as are there at once, then several that divide a tile's rows of B and each multiply A x for themselves.  Wide clusters leave SMs over
+  // (132 of 148 can be in clusters of four, 120 in clusters of eight: what is behind them starts when all is done).
   unsigned C = 8;
-  while (C > 1 && items * C > sms) C /= 2;
-  p.splits = (int)std::max<long long>(1, std::min<long long>({sms / (items * C), (a.oc + 128ll * C - 1) / (128 * C), 16}));
+  while (C > 1 && items > clusters_at_once((const void*)lowrank_tile_kernel<X, W, NT>, C)) C /= 2;
+  p.splits = (int)std::max<long long>(1, std::min<long long>({clusters_at_once((const void*)lowrank_tile_kernel<X, W, NT>, C) / items, (a.oc + 128ll * C - 1) / (128 * C), 16}));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(kTileAll); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = s;
   cudaLaunchAttribute attr[2];
