@@ -34,7 +34,14 @@ struct TileShape {
   static constexpr int kGroup = NT == 64 ? 2 : 8, kGroups = NT == 16 ? 2 : kTerms == 1 ? 4 : kTerms == 2 ? 2 : 1;      // pieces that come at once, and how many such groups there is room for
   static constexpr int kXBytes = kGroup * kGroups * kPieceBytes, kShare = NT * kMostRank * 4;
   static constexpr int kEights = kGroup * 8, kPer = kEights * NT / kThreads;       // of a row in a group, and those of a thread where the tile is full
-  static constexpr int kAcc = NT == 64 ? 2 : 4, kTmemCols = NT == 64 ? 256 : 128;
+  // Few rows: the terms lie side by side, as more columns of one product, and are added up when they are read (a product of few columns takes as long as its 128 weight rows take to
+  // read).  Many rows: one product after another into the same accumulator.
+  static constexpr bool kBeside = NT == 16;
+  static constexpr int kColsA = kBeside ? NT * kTerms : NT, kColsB = kBeside ? NT * 3 : NT;        // of an accumulator
+  static constexpr int kAcc = NT == 64 ? 2 : 4, kTmemCols = 256;
+  static_assert(kColsA + kAcc * kColsB <= kTmemCols, "tensor memory");
+  // The warps that read an accumulator, and how many of its rows' columns each reads: half of 64 rows, or all of sixteen, of every second tile.
+  static constexpr int kReaders = NT == 64 ? 8 : 4, kReadCols = NT == 64 ? 32 : 16;
   static_assert(kXBytes >= 6 * kTileBytes, "A x takes x's place");
   static_assert(1024 + kRing * kSlotBytes + kXBytes + kShare + 1024 <= kSmemBytes, "shared memory");
   static_assert(kShare >= 8 * kMostCounted || NT == 64, "room for counting the rows of adapters");
@@ -76,10 +83,19 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[kCols]) {
     tc5::tmem_ld32_issue(taddr, r);
     tc5::tmem_ld_wait(r);
   } else {
-    static_assert(kCols == 8, "");
+    static_assert(kCols == 8 || kCols == 16, "");
+    if constexpr (kCols == 16) {
+      asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+                     "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+      asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+      return;
+    } else {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
     asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]) :: "memory");
+    }
   }
 }
 __device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, int v, uint32_t bar) {
@@ -98,13 +114,16 @@ __device__ __forceinline__ void add_four(Four<Y>& y, const float4& d) {
   v[0] = from_float<Y>(to_float<Y>(v[0]) + d.x); v[1] = from_float<Y>(to_float<Y>(v[1]) + d.y);
   v[2] = from_float<Y>(to_float<Y>(v[2]) + d.z); v[3] = from_float<Y>(to_float<Y>(v[3]) + d.w);
 }
-// The accumulators of tiles [o0, o1) of B to y: kCols of the tile's rows from col0 on, by one warp.
-template <int kCols, typename Y, bool kScaled>
-__device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int acc_cols, int accs, int o0, int o1, int quarter, int col0, int n, bool grouped, float* turn,
-                                        int quad, int r_lane, volatile int* abortp, bool& ok) {
+// The accumulators of tiles [o0, o1) of B to y, by one of eight warps: 32 lanes of a tile, and half of its rows, or all of every second tile's.
+template <typename S, typename Y, bool kScaled>
+__device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, bool grouped, float* share, int last_term, bool& ok) {
   const rwkvq_lowrank_args& a = p.a;
-  const int lane = threadIdx.x & 31;
+  constexpr int kCols = S::kReadCols, kStep = kWarps / S::kReaders;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = warp & 3, quad = lane & 7, r_lane = lane >> 3;
+  const int col0 = kStep == 1 ? (warp >> 2) * kCols : 0, first = kStep == 1 ? 0 : warp >> 2;
   const int rows = min(n - col0, kCols);             // of this warp, maybe none
+  float* const turn = share + warp * (kMostRank * S::kTileBytes / 128 / kWarps);       // its part of the share's place: 32 columns by kCols rows, or half of them at a time
+  constexpr int kTurn = S::kTileBytes / 128 * kMostRank / kWarps / 32;                 // rows that it holds
   Y* at[kCols / 4];                                  // rows r_lane, r_lane + 4, ...; those behind the last are read, where there are any at all, as the last
 #pragma unroll
   for (int i = 0; i < kCols / 4; ++i) {
@@ -121,39 +140,57 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
       for (int i = 0; i < kCols / 4; ++i) to[i] = *reinterpret_cast<const Four<Y>*>(at[i] + col);
   };
 #pragma unroll
-  for (int k = 0; k < kDepth; ++k) load(k, ahead[k]);
+  for (int k = 0; k < kDepth; ++k) load(first + k * kStep, ahead[k]);
 #pragma unroll 1
-  for (int o = 0; o < o1 - o0; ++o) {
-    const int acc = o % accs, col = (o0 + o) * 128 + quarter * 32 + quad * 4;
+  for (int o = first; o < o1 - o0; o += kStep) {
+    const int acc = o % S::kAcc, col = (o0 + o) * 128 + quarter * 32 + quad * 4;
 #pragma unroll
     for (int i = 0; i < kCols / 4; ++i) {
       y[i] = ahead[0][i];
 #pragma unroll
       for (int k = 0; k + 1 < kDepth; ++k) ahead[k][i] = ahead[k + 1][i];
     }
-    load(o + kDepth, ahead[kDepth - 1]);
-    ok = ok && tc5::mbar_wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / accs) & 1u, abortp, p.status);
+    load(o + kDepth * kStep, ahead[kDepth - 1]);
+    ok = ok && tc5::mbar_wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / S::kAcc) & 1u, &ctrl.abort_flag, p.status);
     if (!__all_sync(~0u, ok)) break;
     tc5::tc_fence_after();
-    uint32_t v[kCols];
-    tmem_ld<kCols>(acc0 + (uint32_t)(acc * acc_cols), v);
+    float sum[kCols];
+    const uint32_t from = acc0 + (uint32_t)(acc * S::kColsB + col0);
+    {
+      uint32_t v[kCols];
+      tmem_ld<kCols>(from, v);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) sum[j] = __uint_as_float(v[j]);
+      if constexpr (S::kBeside)
+#pragma unroll 1
+        for (int k = 1; k <= last_term; ++k) {
+          tmem_ld<kCols>(from + (uint32_t)(k * kCols), v);
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) sum[j] += __uint_as_float(v[j]);
+        }
+    }
     tc5::tc_fence_before();
     __syncwarp();
     if (lane == 0) tc5::mbar_arrive(&ctrl.empty_acc[acc]);
     if (rows <= 0) continue;
     // [row][column], rows of 128 bytes: each lane a column, then each quarter of a warp a row
 #pragma unroll
-    for (int j = 0; j < kCols; ++j) turn[j * 32 + lane] = __uint_as_float(v[j]);
-    __syncwarp();
+    for (int h = 0; h < kCols / kTurn; ++h) {
+      if (h * kTurn >= rows) continue;
 #pragma unroll
-    for (int i = 0; i < kCols / 4; ++i) {
-      const int r = i * 4 + r_lane;
-      float4 d = *reinterpret_cast<const float4*>(turn + r * 32 + quad * 4);
-      if constexpr (kScaled) { const float back = ctrl.back[min(col0 + r, n - 1)]; d.x *= back; d.y *= back; d.z *= back; d.w *= back; }
-      add_four<Y>(y[i], d);
-      if (r < rows && col < a.oc) *reinterpret_cast<Four<Y>*>(at[i] + col) = y[i];
+      for (int j = 0; j < kTurn; ++j) turn[j * 32 + lane] = sum[h * kTurn + j];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kTurn / 4; ++i) {
+        const int r = h * kTurn + i * 4 + r_lane;
+        float4 d = *reinterpret_cast<const float4*>(turn + (i * 4 + r_lane) * 32 + quad * 4);
+        if constexpr (kScaled) { const float back = ctrl.back[min(col0 + r, n - 1)]; d.x *= back; d.y *= back; d.z *= back; d.w *= back; }
+        Four<Y>& mine = y[h * kTurn / 4 + i];
+        add_four<Y>(mine, d);
+        if (r < rows && col < a.oc) *reinterpret_cast<Four<Y>*>(at[h * kTurn / 4 + i] + col) = mine;
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
 }
 
@@ -167,7 +204,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   __shared__ Tile t;
   __shared__ TileCtrl ctrl;
   __shared__ int scratch[2 * kWarps + 2];
-  uint8_t* const xs = smem + kRing * kSlotBytes;                         // [slot][term][row][64 columns], then A x: [term][64 of the rank][row][64]
+  uint8_t* const xs = smem + kRing * kSlotBytes;                         // [slot][term][row][64 columns], then A x: [term][64 of the rank][row][64], or [64 of the rank][term][row][64]
   float* const share = reinterpret_cast<float*>(xs + S::kXBytes);        // this block's share of A x: [row][rank]
   uint32_t* const codebook = reinterpret_cast<uint32_t*>(share + S::kShare / 4);
   const rwkvq_lowrank_args& a = p.a;
@@ -179,7 +216,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], 1); }
     for (int i = 0; i < S::kGroups; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : kWarps); tc5::mbar_init(&ctrl.xempty[i], 1); }
-    for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], kWarps); }
+    for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], S::kReaders); }
     tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.drained, 1);
     ctrl.abort_flag = ctrl.asked = ctrl.x_asked = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\nfence.proxy.async.shared::cta;" ::: "memory");
@@ -257,7 +294,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     }
   };
   if (warp == kWarps) {
-    if (lane == 0) find_adapter(p, t);
+    if (lane == 0 && !(grouped && by_groups(a))) find_adapter(p, t);
   } else if (warp == kWarps + 1) {
     tc5::tmem_alloc(&ctrl.tmem_base, S::kTmemCols);
   }
@@ -336,7 +373,8 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     // ---- products
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     const uint64_t ring_desc = tc5::smem_desc_sw128(ring), x_desc = tc5::smem_desc_sw128(xring);
-    constexpr uint32_t kA = idesc_of(F::kHalf, NT), kB = idesc_of(kHalf, NT);
+    constexpr uint32_t kA = idesc_of(F::kHalf, S::kColsA);
+    const uint32_t kB = idesc_of(kHalf, S::kBeside ? NT * (last_term + 1) : NT);
     Turn<kRing> slot;
     {
       Turn<S::kGroups> group;
@@ -352,7 +390,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
           tc5::tc_fence_after();
           const uint64_t x = x_desc + ((group.at * S::kGroup + in_group) * S::kPieceBytes >> 4);
 #pragma unroll
-          for (int k = F::kX - 1; k >= 0; --k) umma(tmem, w, x + (uint32_t)(k * S::kTileBytes / 16), kA, px > 0 || k < F::kX - 1, 4);
+          for (int k = S::kBeside ? 0 : F::kX - 1; k >= 0; --k) umma(tmem, w, x + (uint32_t)(k * S::kTileBytes / 16), kA, px > 0 || (!S::kBeside && k < F::kX - 1), 4);
           w += (uint32_t)blocks * 128u;
           if (++in_group == S::kGroup) {
             tc5::umma_commit(&ctrl.xempty[group.at]);
@@ -372,7 +410,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     asm volatile("fence.proxy.async;" ::: "memory");
 #pragma unroll 1
     for (int o = 0; o < o1 - o0; ++o) {
-      const uint32_t acc = (uint32_t)(o % S::kAcc), d = tmem + NT + acc * NT;
+      const uint32_t acc = (uint32_t)(o % S::kAcc), d = tmem + S::kColsA + acc * S::kColsB;
       wait(smem_u32(&ctrl.empty_acc[acc]), (uint32_t)(o / S::kAcc + 1) & 1u);
 #pragma unroll 1
       for (int k = 0; k < wide; ++k) {
@@ -398,9 +436,9 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
           __syncwarp();
         }
         tc5::tc_fence_after();
-        const uint64_t w = ring_desc + (slot.at * kSlotBytes >> 4), h = x_desc + (uint32_t)(k * S::kTileBytes / 16);
+        const uint64_t w = ring_desc + (slot.at * kSlotBytes >> 4), h = x_desc + (uint32_t)(k * (S::kBeside ? 3 : 1) * S::kTileBytes / 16);
 #pragma unroll 1
-        for (int j = last_term; j >= 0; --j) umma(d, w, h + (uint32_t)(j * wide * S::kTileBytes / 16), kB, k > 0 || j < last_term, steps);
+        for (int j = S::kBeside ? 0 : last_term; j >= 0; --j) umma(d, w, h + (uint32_t)(j * wide * S::kTileBytes / 16), kB, k > 0 || (!S::kBeside && j < last_term), steps);
         tc5::umma_commit(&ctrl.empty[slot.at]);
         slot.next();
       }
@@ -412,22 +450,26 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     // ---- this block's share of A x: lanes are the rank
     constexpr int kCols = NT / 2;
     const int quarter = warp & 3, col0 = (warp >> 2) * kCols;
-    const uint32_t lanes = tmem + ((uint32_t)quarter << 21) + (uint32_t)col0;
-    uint32_t v[kCols];
+    const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
     if (np > 0) {
       wait(smem_u32(&ctrl.a_done), 0);
       tc5::tc_fence_after();
     }
     if (quarter * 32 < blocks * 16) {
-      if (np > 0) {
-        tmem_ld<kCols>(lanes, v);
-      } else {
+      float sum[kCols];
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) v[j] = 0;
-      }
+      for (int j = 0; j < kCols; ++j) sum[j] = 0.f;
+      if (np > 0)
+#pragma unroll
+        for (int k = (S::kBeside ? F::kX : 1) - 1; k >= 0; --k) {
+          uint32_t v[kCols];
+          tmem_ld<kCols>(lanes + (uint32_t)(k * NT + col0), v);
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) sum[j] += __uint_as_float(v[j]);
+        }
 #pragma unroll
       for (int j = 0; j < kCols; ++j)
-        if (col0 + j < n) share[(col0 + j) * kMostRank + quarter * 32 + lane] = __uint_as_float(v[j]);
+        if (col0 + j < n) share[(col0 + j) * kMostRank + quarter * 32 + lane] = sum[j];
     }
     tc5::tc_fence_before();
     cluster.sync();
@@ -449,7 +491,8 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
         for (int k = 0; k < kC; ++k) { h[0] += s[k].x; h[1] += s[k].y; h[2] += s[k].z; h[3] += s[k].w; }
 #pragma unroll
         for (int j = 0; j < 4; ++j) h[j] = r4 + j < rank ? h[j] * scale : 0.f;
-        uint8_t* const to = xs + r4 / 64 * S::kTileBytes + swizzled(row, r4 / 8 & 7) + (r4 & 4) * 2;
+        uint8_t* const to = xs + r4 / 64 * (S::kBeside ? 3 : 1) * S::kTileBytes + swizzled(row, r4 / 8 & 7) + (r4 & 4) * 2;
+        const int next = (S::kBeside ? 1 : wide) * S::kTileBytes;
         uint2 terms[3];
         float back = 1.f;
         if constexpr (kHalf) {
@@ -482,8 +525,8 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
           for (int k = 0; k < kC; ++k) {
             uint8_t* const there_to = cluster.map_shared_rank(to, k);
             *reinterpret_cast<uint2*>(there_to) = terms[0];
-            *reinterpret_cast<uint2*>(there_to + wide * S::kTileBytes) = terms[1];
-            if (!kHalf && last_term == 2) *reinterpret_cast<uint2*>(there_to + 2 * wide * S::kTileBytes) = terms[2];
+            *reinterpret_cast<uint2*>(there_to + next) = terms[1];
+            if (!kHalf && last_term == 2) *reinterpret_cast<uint2*>(there_to + 2 * next) = terms[2];
             if (kHalf && r4 == 0) *cluster.map_shared_rank(&ctrl.back[row], k) = back;
           }
       }
@@ -498,11 +541,9 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
 
     // ---- y: 32 columns of it for a warp, and half of the tile's rows.  A lane of the accumulator is a column; the way to four neighbouring columns a lane is through
     // shared memory, where the shares were.
-    float* const turn = share + warp * kCols * 32;
-    const int quad = lane & 7, r_lane = lane >> 3;
-    if (a.y_dtype == RWKVQ_F32) store_y<kCols, float, kHalf>(p, t, ctrl, lanes + NT, NT, S::kAcc, o0, o1, quarter, col0, n, grouped, turn, quad, r_lane, abortp, ok);
-    else if (a.y_dtype == RWKVQ_F16) store_y<kCols, __half, kHalf>(p, t, ctrl, lanes + NT, NT, S::kAcc, o0, o1, quarter, col0, n, grouped, turn, quad, r_lane, abortp, ok);
-    else store_y<kCols, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + NT, NT, S::kAcc, o0, o1, quarter, col0, n, grouped, turn, quad, r_lane, abortp, ok);
+    if (a.y_dtype == RWKVQ_F32) store_y<S, float, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
+    else if (a.y_dtype == RWKVQ_F16) store_y<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
+    else store_y<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
   }
   if (warp == kWarps) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   tc5::tc_fence_before();
