@@ -21,7 +21,7 @@ namespace lr {
 
 using tc5::smem_u32;
 
-constexpr int kTileAll = kThreads + 64;                            // eight warps that make operands and read accumulators, one that asks for copies, one that multiplies
+constexpr int kTileAll = kThreads + 128;                           // eight warps that make operands and read accumulators, one that asks for copies, one that multiplies, two that mask
 constexpr int kRing = 7, kSlotBytes = 16 << 10, kMostGroups = 4, kMostAcc = 4;
 constexpr int kSmemBytes = 224 << 10;
 
@@ -47,7 +47,7 @@ struct TileShape {
   static_assert(kShare >= 8 * kMostCounted || NT == 64, "room for counting the rows of adapters");
 };
 struct TileCtrl {
-  uint64_t full[kRing], empty[kRing], xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
+  uint64_t full[kRing], empty[kRing], masked[kRing + 1], xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
   int abort_flag, asked, x_asked;
   uint32_t tmem_base;
   float back[64];                 // of each row: the power of two that its A x was divided by
@@ -130,9 +130,9 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
     const int r = col0 + max(min(i * 4 + r_lane, rows - 1), -col0);
     at[i] = static_cast<Y*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row;
   }
-  // y of the next tiles is on its way while this one's is added to: some 48 to 64 KB an SM
+  // y of the next tiles is on its way while this one's is added to, some 48 to 64 KB an SM (into buffers that take turns, not moved: a move waits for what it moves)
   constexpr int kDepth = sizeof(Y) == 2 ? 3 : 2;
-  Four<Y> y[kCols / 4], ahead[kDepth][kCols / 4];
+  Four<Y> buffers[kDepth][kCols / 4];
   auto load = [&](int o, Four<Y> (&to)[kCols / 4]) {
     const int col = min((o0 + o) * 128 + quarter * 32 + quad * 4, a.oc - 4);
     if (rows > 0 && o < o1 - o0)
@@ -140,19 +140,16 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
       for (int i = 0; i < kCols / 4; ++i) to[i] = *reinterpret_cast<const Four<Y>*>(at[i] + col);
   };
 #pragma unroll
-  for (int k = 0; k < kDepth; ++k) load(first + k * kStep, ahead[k]);
+  for (int k = 0; k < kDepth; ++k) load(first + k * kStep, buffers[k]);
 #pragma unroll 1
-  for (int o = first; o < o1 - o0; o += kStep) {
-    const int acc = o % S::kAcc, col = (o0 + o) * 128 + quarter * 32 + quad * 4;
+  for (int round = first; round < o1 - o0; round += kDepth * kStep)
 #pragma unroll
-    for (int i = 0; i < kCols / 4; ++i) {
-      y[i] = ahead[0][i];
-#pragma unroll
-      for (int k = 0; k + 1 < kDepth; ++k) ahead[k][i] = ahead[k + 1][i];
-    }
-    load(o + kDepth * kStep, ahead[kDepth - 1]);
+  for (int turn_of = 0; turn_of < kDepth; ++turn_of) {
+    const int o = round + turn_of * kStep, acc = o % S::kAcc, col = (o0 + o) * 128 + quarter * 32 + quad * 4;
+    if (o >= o1 - o0) continue;
+    Four<Y> (&y)[kCols / 4] = buffers[turn_of];
     ok = ok && tc5::mbar_wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / S::kAcc) & 1u, &ctrl.abort_flag, p.status);
-    if (!__all_sync(~0u, ok)) break;
+    if (!__all_sync(~0u, ok)) return;
     tc5::tc_fence_after();
     float sum[kCols];
     const uint32_t from = acc0 + (uint32_t)(acc * S::kColsB + col0);
@@ -191,6 +188,7 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
       }
       __syncwarp();
     }
+    load(o + kDepth * kStep, y);
   }
 }
 
@@ -215,6 +213,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   asm volatile("griddepcontrol.launch_dependents;");
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], 1); }
+    for (int i = 0; i <= kRing; ++i) tc5::mbar_init(&ctrl.masked[i], 1);
     for (int i = 0; i < S::kGroups; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : kWarps); tc5::mbar_init(&ctrl.xempty[i], 1); }
     for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], S::kReaders); }
     tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.drained, 1);
@@ -242,54 +241,56 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && tc5::mbar_wait(bar, parity, abortp, p.status); };
   auto row_of = [&](int r) { return grouped ? t.rows[r] : t.first + r; };
 
-  // All groups of x in operand form, by the eight warps, or those before `last`: the loads of a group are on their way while the one before it is made.  A thread has kN eights of
-  // columns of a group, one where the tile has few rows.
+  // All groups of x in operand form, by the eight warps: the loads of two groups are on their way while one is made (into buffers that take turns, not moved: a move
+  // waits for what it moves).  A thread has kN eights of columns of a group, one where the tile has few rows.
   auto stage_all = [&](auto mix, auto per) {
     constexpr bool kMix = decltype(mix)::value;
     constexpr int kN = decltype(per)::value;
     Turn<S::kGroups> turn;
-    Eights<X> raw[kN], ahead[kN];
-    MuWords words, words_ahead;
+    Eights<X> raw[2][kN];
+    MuWords words[2];
     // kThreads is a multiple of a row's eights: the columns are the same for all rows of a thread
-    const int piece = tid % S::kEights / 8;
+    const int piece = tid % S::kEights / 8, groups = (np + S::kGroup - 1) / S::kGroup;
     auto col_of = [&](int g) { return (k0 + min(g * S::kGroup + piece, np - 1)) * 64 + (tid & 7) * 8; };
-    auto load = [&](int g, Eights<X> (&e)[kN]) {
-      words_ahead = load_mu<kMix>(p, col_of(g));
+    auto load = [&](int g, Eights<X> (&e)[kN], MuWords& m) {
+      m = load_mu<kMix>(p, col_of(g));
 #pragma unroll
       for (int j = 0; j < kN; ++j) {
-        const int i = tid + j * kThreads, r = min(i / S::kEights, n - 1), row = row_of(r);
+        const int row = row_of(min((tid + j * kThreads) / S::kEights, n - 1));
         e[j] = load_eights<X, kMix>(p, row, grouped ? row : t.seq, grouped || row == t.start, col_of(g));
       }
     };
-    load(0, ahead);
+    load(0, raw[0], words[0]);
+    load(1, raw[1], words[1]);
 #pragma unroll 1
-    for (int g = 0; g * S::kGroup < np; ++g) {
+    for (int g0 = 0; g0 < groups; g0 += 2)
 #pragma unroll
-      for (int j = 0; j < kN; ++j) raw[j] = ahead[j];
-      words = words_ahead;
-      if ((g + 1) * S::kGroup < np) load(g + 1, ahead);
-      if (g >= S::kGroups) wait(xempty + turn.at * 8u, turn.parity ^ 1u);
-      float2 mu[4];
-      mu_of<kMix>(p, codebook, words, col_of(g), mu);
+      for (int h = 0; h < 2; ++h) {
+        const int g = g0 + h;
+        if (g >= groups) continue;
+        if (g >= S::kGroups) wait(xempty + turn.at * 8u, turn.parity ^ 1u);
+        float2 mu[4];
+        mu_of<kMix>(p, codebook, words[h], col_of(g), mu);
 #pragma unroll
-      for (int j = 0; j < kN; ++j) {
-        const int row = (tid + j * kThreads) / S::kEights;
-        if (j * kThreads / S::kEights >= n) continue;          // of no thread
-        if (row < n) put_eights<X, F, kMix>(raw[j], mu, xs + (turn.at * S::kGroup + piece) * S::kPieceBytes + swizzled(row, tid & 7), S::kTileBytes);
+        for (int j = 0; j < kN; ++j) {
+          const int row = (tid + j * kThreads) / S::kEights;
+          if (j * kThreads / S::kEights >= n) continue;          // of no thread
+          if (row < n) put_eights<X, F, kMix>(raw[h][j], mu, xs + (turn.at * S::kGroup + piece) * S::kPieceBytes + swizzled(row, tid & 7), S::kTileBytes);
+        }
+        if (g + 2 < groups) load(g + 2, raw[h], words[h]);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) tc5::mbar_arrive(xfull + turn.at * 8u);
+        turn.next();
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) tc5::mbar_arrive(xfull + turn.at * 8u);
-      turn.next();
-    }
   };
   auto stage = [&] {
-    const bool few = n * S::kEights <= kThreads;
+    const bool few = NT == kRows && n * S::kEights <= kThreads;
     if (p.mu) {
-      if (few) stage_all(std::true_type(), std::integral_constant<int, 1>());
+      if (few) stage_all(std::true_type(), std::integral_constant<int, NT == kRows ? 1 : S::kPer>());
       else stage_all(std::true_type(), std::integral_constant<int, S::kPer>());
     } else {
-      if (few) stage_all(std::false_type(), std::integral_constant<int, 1>());
+      if (few) stage_all(std::false_type(), std::integral_constant<int, NT == kRows ? 1 : S::kPer>());
       else stage_all(std::false_type(), std::integral_constant<int, S::kPer>());
     }
   };
@@ -309,6 +310,8 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   const int rank = t.rank, blocks = (rank + 15) / 16, wide = (rank + 63) / 64;
   const int a_slot = pieces_of(blocks), n_a = (np + a_slot - 1) / a_slot;      // pieces of A in a slot
   const int last_term = kHalf ? 1 : a.y_dtype == RWKVQ_F32 ? 2 : 1;
+  // What lies behind the adapter's rank may be anything: in B's last sixteen columns it is masked, unless these end the rows, where a box has zeros.
+  const bool masks = rank % 16 != 0 && rank < a.rank;
 
   if (warp == kWarps) {
     // ---- copies.  This warp and the next bring nothing to the first meeting of the cluster and do not hold it up: what they wait for below comes behind it.
@@ -414,27 +417,13 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       wait(smem_u32(&ctrl.empty_acc[acc]), (uint32_t)(o / S::kAcc + 1) & 1u);
 #pragma unroll 1
       for (int k = 0; k < wide; ++k) {
-        wait(full + slot.at * 8u, slot.parity);
-        if (!__all_sync(~0u, ok)) break;
-        const int steps = min(4, blocks - k * 4), tail = rank - k * 64;
-        if (tail < steps * 16) {
-          // what lies behind the adapter's rank may be anything: up to where the last sixteen columns end, zeros
-          uint8_t* const weights = smem + slot.at * kSlotBytes;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int e = tail / 8 + h, keep = max(tail - e * 8, 0);
-            auto of = [keep](int j) { return keep >= 2 * j + 2 ? ~0u : keep == 2 * j + 1 ? 0xFFFFu : 0u; };
-            if (e >= steps * 2) continue;
-            uint4 v[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const uint4*>(weights + swizzled(r * 32 + lane, e));
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              *reinterpret_cast<uint4*>(weights + swizzled(r * 32 + lane, e)) = make_uint4(v[r].x & of(0), v[r].y & of(1), v[r].z & of(2), v[r].w & of(3));
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
+        if (masks && k + 1 == wide) {
+          wait(smem_u32(&ctrl.masked[o % (kRing + 1)]), (uint32_t)(o / (kRing + 1)) & 1u);
+        } else {
+          wait(full + slot.at * 8u, slot.parity);
         }
+        if (!__all_sync(~0u, ok)) break;
+        const int steps = min(4, blocks - k * 4);
         tc5::tc_fence_after();
         const uint64_t w = ring_desc + (slot.at * kSlotBytes >> 4), h = x_desc + (uint32_t)(k * (S::kBeside ? 3 : 1) * S::kTileBytes / 16);
 #pragma unroll 1
@@ -445,6 +434,34 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       if (!__all_sync(~0u, ok)) break;
       tc5::umma_commit(&ctrl.full_acc[acc]);
     }
+  } else if (warp > kWarps + 1) {
+    // ---- masks, each of two warps for every second tile of B: no more tiles ahead of the products than the ring has slots
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (masks)
+#pragma unroll 1
+      for (int o = warp - kWarps - 2; o < o1 - o0; o += 2) {
+        const int i = n_a + o * wide + wide - 1, tail = rank - (wide - 1) * 64;
+        uint8_t* const weights = smem + i % kRing * kSlotBytes;
+        wait(full + (uint32_t)(i % kRing) * 8u, (uint32_t)(i / kRing) & 1u);
+        if (!__all_sync(~0u, ok)) break;
+        uint4 v[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[h][r] = *reinterpret_cast<const uint4*>(weights + swizzled(r * 32 + lane, min(tail / 8 + h, 7)));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int e = tail / 8 + h, keep = max(tail - e * 8, 0);
+          auto of = [keep](int j) { return keep >= 2 * j + 2 ? ~0u : keep == 2 * j + 1 ? 0xFFFFu : 0u; };
+          if (e * 8 >= (tail + 15) / 16 * 16) continue;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            *reinterpret_cast<uint4*>(weights + swizzled(r * 32 + lane, e)) = make_uint4(v[h][r].x & of(0), v[h][r].y & of(1), v[h][r].z & of(2), v[h][r].w & of(3));
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) tc5::mbar_arrive(&ctrl.masked[o % (kRing + 1)]);
+      }
   } else {
     if (!p.x_by_map && np > 0) stage();
     // ---- this block's share of A x: lanes are the rank
@@ -545,7 +562,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     else if (a.y_dtype == RWKVQ_F16) store_y<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
     else store_y<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
   }
-  if (warp == kWarps) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (warp == kWarps || warp > kWarps + 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   tc5::tc_fence_before();
   __syncthreads();
   tc5::tc_fence_after();
