@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
 #pragma unroll 1
     for (int e = tid; e < n * eights; e += kThreads) {
       const int r = e / eights, eight = e - r * eights, col = kp * 64 + eight * 8, row = grouped ? t.rows[r] : t.first + r;
-      const Eights<X> raw = load_eights<X, decltype(mix)::value>(p, row, grouped ? row : t.seq, grouped || row == t.start, col);
+      const Eights<X> raw = load_eights<X, decltype(mix)::value>(p, row_at<X>(p, row, grouped ? row : t.seq, grouped || row == t.start), col);
       const MuWords words = load_mu<decltype(mix)::value>(p, col);
       float2 mu[4];
       mu_of<decltype(mix)::value>(p, codebook, words, col, mu);

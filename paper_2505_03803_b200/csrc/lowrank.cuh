@@ -240,21 +240,32 @@ template <typename X> struct Eights {
   uint4 x[sizeof(X) / 2], before[sizeof(X) / 2];
   bool there, has_before;
 };
-template <typename X, bool kMix>
-__device__ __forceinline__ Eights<X> load_eights(const Args& p, int row, int seq, bool begins, int col) {
+// A row of x, and the one in front of it (x itself, where there is none).
+template <typename X> struct RowOf {
+  const X* x;
+  const X* before;
+  bool has_before;
+};
+template <typename X>
+__device__ __forceinline__ RowOf<X> row_at(const Args& p, int row, int seq, bool begins) {
   const rwkvq_lowrank_args& a = p.a;
+  RowOf<X> r;
+  r.x = static_cast<const X*>(a.x) + (long long)row * a.x_row;
+  r.before = a.x_prev ? static_cast<const X*>(a.x_prev) + (long long)row * a.x_prev_row : !begins ? r.x - a.x_row : a.xprev0 ? static_cast<const X*>(a.xprev0) + (long long)seq * a.ic : r.x;
+  r.has_before = a.x_prev || !begins || a.xprev0;
+  return r;
+}
+template <typename X, bool kMix>
+__device__ __forceinline__ Eights<X> load_eights(const Args& p, const RowOf<X>& r, int col) {
   Eights<X> e;
-  e.there = col < a.ic;
-  col = min(col, a.ic - 8);
-  const X* const x = static_cast<const X*>(a.x) + (long long)row * a.x_row + col;
+  e.there = col < p.a.ic;
+  e.has_before = r.has_before;
+  col = min(col, p.a.ic - 8);
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.x[i] = __ldg(reinterpret_cast<const uint4*>(x) + i);
-  if constexpr (kMix) {
-    const X* b = a.x_prev ? static_cast<const X*>(a.x_prev) + (long long)row * a.x_prev_row + col : !begins ? x - a.x_row : a.xprev0 ? static_cast<const X*>(a.xprev0) + (long long)seq * a.ic + col : x;
-    e.has_before = a.x_prev || !begins || a.xprev0;
+  for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.x[i] = __ldg(reinterpret_cast<const uint4*>(r.x + col) + i);
+  if constexpr (kMix)
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.before[i] = __ldg(reinterpret_cast<const uint4*>(b) + i);
-  }
+    for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.before[i] = __ldg(reinterpret_cast<const uint4*>(r.before + col) + i);
   return e;
 }
 // Their indices of the token-shift vector: four are 4 * mu_bits neighbouring bits from a byte's beginning; behind the indices lies the codebook.

@@ -252,13 +252,17 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     // kThreads is a multiple of a row's eights: the columns are the same for all rows of a thread
     const int piece = tid % S::kEights / 8, groups = (np + S::kGroup - 1) / S::kGroup;
     auto col_of = [&](int g) { return (k0 + min(g * S::kGroup + piece, np - 1)) * 64 + (tid & 7) * 8; };
-    auto load = [&](int g, Eights<X> (&e)[kN], MuWords& m) {
-      m = load_mu<kMix>(p, col_of(g));
+    RowOf<X> rows[kN];
 #pragma unroll
-      for (int j = 0; j < kN; ++j) {
-        const int row = row_of(min((tid + j * kThreads) / S::kEights, n - 1));
-        e[j] = load_eights<X, kMix>(p, row, grouped ? row : t.seq, grouped || row == t.start, col_of(g));
-      }
+    for (int j = 0; j < kN; ++j) {
+      const int row = row_of(min((tid + j * kThreads) / S::kEights, n - 1));
+      rows[j] = row_at<X>(p, row, grouped ? row : t.seq, grouped || row == t.start);
+    }
+    auto load = [&](int g, Eights<X> (&e)[kN], MuWords& m) {
+      const int col = col_of(g);
+      m = load_mu<kMix>(p, col);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) e[j] = load_eights<X, kMix>(p, rows[j], col);
     };
     load(0, raw[0], words[0]);
     load(1, raw[1], words[1]);
@@ -436,6 +440,16 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     }
   } else if (warp > kWarps + 1) {
     // ---- masks, each of two warps for every second tile of B: no more tiles ahead of the products than the ring has slots
+    // two warps that have nothing to do yet have y's rows fetched to the second-level cache, which are read when all else is done, and those of x
+    auto fetch = [](const void* base, long long at, int elements, int size) {
+      if (elements > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(base) + at * size), "r"(elements * size) : "memory");
+    };
+    for (int r = lane; r < n; r += 32) {
+      const int columns = min((k0 + np) * 64, a.ic) - k0 * 64;
+      if (warp == kWarps + 3) fetch(a.x, (long long)row_of(r) * a.x_row + k0 * 64, columns, (int)sizeof(X));
+      if (warp == kWarps + 3 && a.x_prev) fetch(a.x_prev, (long long)row_of(r) * a.x_prev_row + k0 * 64, columns, (int)sizeof(X));
+      if (warp == kWarps + 2) fetch(a.y, (long long)row_of(r) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
+    }
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
     if (masks)
 #pragma unroll 1
