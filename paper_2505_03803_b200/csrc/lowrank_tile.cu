@@ -21,7 +21,6 @@ namespace lr {
 
 using tc5::smem_u32;
 
-constexpr int kTileAll = kThreads + 128;                           // eight warps that make operands and read accumulators, one that asks for copies, one that multiplies, two that mask
 constexpr int kRing = 7, kSlotBytes = 16 << 10, kMostGroups = 4, kMostAcc = 4;
 constexpr int kSmemBytes = 224 << 10;
 
@@ -33,21 +32,23 @@ struct TileShape {
   static constexpr int kTerms = Form<X, W>::kX, kTileBytes = NT * 128, kPieceBytes = kTerms * kTileBytes;      // a piece: 64 columns of the tile's rows, a tile for each term
   static constexpr int kGroup = NT == 64 ? 2 : 8, kGroups = NT == 16 ? 2 : kTerms == 1 ? 4 : kTerms == 2 ? 2 : 1;      // pieces that come at once, and how many such groups there is room for
   static constexpr int kXBytes = kGroup * kGroups * kPieceBytes, kShare = NT * kMostRank * 4;
-  static constexpr int kEights = kGroup * 8, kPer = kEights * NT / kThreads;       // of a row in a group, and those of a thread where the tile is full
+  // Warps that make operands and read accumulators; behind them one that asks for copies, one that multiplies, two that mask.
+  static constexpr int kWorkers = NT == 64 ? 16 : 8, kWork = kWorkers * 32, kAll = kWork + 128;
+  static constexpr int kEights = kGroup * 8, kPer = kEights * NT / kWork;          // of a row in a group, and those of a thread where the tile is full
   // Few rows: the terms lie side by side, as more columns of one product, and are added up when they are read (a product of few columns takes as long as its 128 weight rows take to
   // read).  Many rows: one product after another into the same accumulator.
   static constexpr bool kBeside = NT == 16;
   static constexpr int kColsA = kBeside ? NT * kTerms : NT, kColsB = kBeside ? NT * 3 : NT;        // of an accumulator
   static constexpr int kAcc = NT == 64 ? 2 : 4, kTmemCols = 256;
   static_assert(kColsA + kAcc * kColsB <= kTmemCols, "tensor memory");
-  // The warps that read an accumulator, and how many of its rows' columns each reads: half of 64 rows, or all of sixteen, of every second tile.
-  static constexpr int kReaders = NT == 64 ? 8 : 4, kReadCols = NT == 64 ? 32 : 16;
+  // The warps that read an accumulator, sixteen of its rows' columns each: a quarter of 64 rows, or all of sixteen, of every second tile.
+  static constexpr int kReaders = NT == 64 ? 16 : 4, kReadCols = 16;
   static_assert(kXBytes >= 6 * kTileBytes, "A x takes x's place");
   static_assert(1024 + kRing * kSlotBytes + kXBytes + kShare + 1024 <= kSmemBytes, "shared memory");
   static_assert(kShare >= 8 * kMostCounted || NT == 64, "room for counting the rows of adapters");
 };
 struct TileCtrl {
-  uint64_t full[kRing], empty[kRing], masked[kRing + 1], xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
+  uint64_t full[kRing], empty[kRing], masked[kRing + 1], ready, xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
   int abort_flag, asked, x_asked;
   uint32_t tmem_base;
   float back[64];                 // of each row: the power of two that its A x was divided by
@@ -114,16 +115,16 @@ __device__ __forceinline__ void add_four(Four<Y>& y, const float4& d) {
   v[0] = from_float<Y>(to_float<Y>(v[0]) + d.x); v[1] = from_float<Y>(to_float<Y>(v[1]) + d.y);
   v[2] = from_float<Y>(to_float<Y>(v[2]) + d.z); v[3] = from_float<Y>(to_float<Y>(v[3]) + d.w);
 }
-// The accumulators of tiles [o0, o1) of B to y, by one of eight warps: 32 lanes of a tile, and half of its rows, or all of every second tile's.
+// The accumulators of tiles [o0, o1) of B to y, by one of the warps: 32 lanes of a tile, and a quarter of its rows, or all of every second tile's.
 template <typename S, typename Y, bool kScaled>
 __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, bool grouped, float* share, int last_term, bool& ok) {
   const rwkvq_lowrank_args& a = p.a;
-  constexpr int kCols = S::kReadCols, kStep = kWarps / S::kReaders;
+  constexpr int kCols = S::kReadCols, kStep = S::kWorkers / S::kReaders;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = warp & 3, quad = lane & 7, r_lane = lane >> 3;
   const int col0 = kStep == 1 ? (warp >> 2) * kCols : 0, first = kStep == 1 ? 0 : warp >> 2;
   const int rows = min(n - col0, kCols);             // of this warp, maybe none
-  float* const turn = share + warp * (kMostRank * S::kTileBytes / 128 / kWarps);       // its part of the share's place: 32 columns by kCols rows, or half of them at a time
-  constexpr int kTurn = S::kTileBytes / 128 * kMostRank / kWarps / 32;                 // rows that it holds
+  float* const turn = share + warp * (kMostRank * S::kTileBytes / 128 / S::kWorkers);       // its part of the share's place: 32 columns by kCols rows, or half of them at a time
+  constexpr int kTurn = S::kTileBytes / 128 * kMostRank / S::kWorkers / 32;                 // rows that it holds
   Y* at[kCols / 4];                                  // rows r_lane, r_lane + 4, ...; those behind the last are read, where there are any at all, as the last
 #pragma unroll
   for (int i = 0; i < kCols / 4; ++i) {
@@ -193,7 +194,7 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
 }
 
 template <typename X, typename W, int NT>
-__global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_constant__ Args p) {
+__global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_kernel(const __grid_constant__ Args p) {
   using S = TileShape<X, W, NT>;
   using F = Form<X, W>;
   constexpr bool kHalf = std::is_same<W, __half>::value;
@@ -214,13 +215,13 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], 1); }
     for (int i = 0; i <= kRing; ++i) tc5::mbar_init(&ctrl.masked[i], 1);
-    for (int i = 0; i < S::kGroups; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : kWarps); tc5::mbar_init(&ctrl.xempty[i], 1); }
+    for (int i = 0; i < S::kGroups; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : S::kWorkers); tc5::mbar_init(&ctrl.xempty[i], 1); }
     for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], S::kReaders); }
-    tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.drained, 1);
+    tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.ready, 1); tc5::mbar_init(&ctrl.drained, 1);
     ctrl.abort_flag = ctrl.asked = ctrl.x_asked = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\nfence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (tid == kThreads) {          // the maps themselves are fetched from memory, too
+  if (tid == S::kWork) {          // the maps themselves are fetched from memory, too
     auto fetch = [](const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); };
     fetch(&p.A[(a.rank + 15) / 16 - 1]);
     fetch(&p.B);
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (p.mu)
-    for (int i = tid; i < p.mu_entries; i += kTileAll) codebook[i] = p.mu_codebook[i];
+    for (int i = tid; i < p.mu_entries; i += S::kAll) codebook[i] = p.mu_codebook[i];
   const int id = (int)(blockIdx.x / C), item = id / p.splits, split = id - item * p.splits;
   find_rows<NT>(p, item, t, scratch, share);
   const int n = t.n;
@@ -241,7 +242,21 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
   auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && tc5::mbar_wait(bar, parity, abortp, p.status); };
   auto row_of = [&](int r) { return grouped ? t.rows[r] : t.first + r; };
 
-  // All groups of x in operand form, by the eight warps: the loads of two groups are on their way while one is made (into buffers that take turns, not moved: a move
+  // What depends on the adapter, which one thread looks up while x is on its way; false where there is none: the same for all blocks of the cluster.
+  int rank = 0, blocks = 0, wide = 0, a_slot = 1, n_a = 0;
+  bool masks = false;
+  const int last_term = kHalf ? 1 : a.y_dtype == RWKVQ_F32 ? 2 : 1;
+  auto settle = [&] {
+    wait(smem_u32(&ctrl.ready), 0);
+    if (t.n == 0) return false;
+    rank = t.rank; blocks = (rank + 15) / 16; wide = (rank + 63) / 64;
+    a_slot = pieces_of(blocks); n_a = (np + a_slot - 1) / a_slot;          // pieces of A in a slot, and slots
+    // What lies behind the adapter's rank may be anything: in B's last sixteen columns it is masked, unless these end the rows, where a box has zeros.
+    masks = rank % 16 != 0 && rank < a.rank;
+    return true;
+  };
+
+  // All groups of x in operand form, by the workers: the loads of two groups are on their way while one is made (into buffers that take turns, not moved: a move
   // waits for what it moves).  A thread has kN eights of columns of a group, one where the tile has few rows.
   auto stage_all = [&](auto mix, auto per) {
     constexpr bool kMix = decltype(mix)::value;
@@ -249,13 +264,13 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     Turn<S::kGroups> turn;
     Eights<X> raw[2][kN];
     MuWords words[2];
-    // kThreads is a multiple of a row's eights: the columns are the same for all rows of a thread
+    // kWork is a multiple of a row's eights: the columns are the same for all rows of a thread
     const int piece = tid % S::kEights / 8, groups = (np + S::kGroup - 1) / S::kGroup;
     auto col_of = [&](int g) { return (k0 + min(g * S::kGroup + piece, np - 1)) * 64 + (tid & 7) * 8; };
     RowOf<X> rows[kN];
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
-      const int row = row_of(min((tid + j * kThreads) / S::kEights, n - 1));
+      const int row = row_of(min((tid + j * S::kWork) / S::kEights, n - 1));
       rows[j] = row_at<X>(p, row, grouped ? row : t.seq, grouped || row == t.start);
     }
     auto load = [&](int g, Eights<X> (&e)[kN], MuWords& m) {
@@ -272,13 +287,16 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       for (int h = 0; h < 2; ++h) {
         const int g = g0 + h;
         if (g >= groups) continue;
-        if (g >= S::kGroups) wait(xempty + turn.at * 8u, turn.parity ^ 1u);
+        if (g >= S::kGroups) {
+          if (g == S::kGroups && !settle()) return;          // nothing is multiplied where there is no adapter
+          wait(xempty + turn.at * 8u, turn.parity ^ 1u);
+        }
         float2 mu[4];
         mu_of<kMix>(p, codebook, words[h], col_of(g), mu);
 #pragma unroll
         for (int j = 0; j < kN; ++j) {
-          const int row = (tid + j * kThreads) / S::kEights;
-          if (j * kThreads / S::kEights >= n) continue;          // of no thread
+          const int row = (tid + j * S::kWork) / S::kEights;
+          if (j * S::kWork / S::kEights >= n) continue;          // of no thread
           if (row < n) put_eights<X, F, kMix>(raw[h][j], mu, xs + (turn.at * S::kGroup + piece) * S::kPieceBytes + swizzled(row, tid & 7), S::kTileBytes);
         }
         if (g + 2 < groups) load(g + 2, raw[h], words[h]);
@@ -289,7 +307,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       }
   };
   auto stage = [&] {
-    const bool few = NT == kRows && n * S::kEights <= kThreads;
+    const bool few = NT == kRows && n * S::kEights <= S::kWork;
     if (p.mu) {
       if (few) stage_all(std::true_type(), std::integral_constant<int, NT == kRows ? 1 : S::kPer>());
       else stage_all(std::true_type(), std::integral_constant<int, S::kPer>());
@@ -298,37 +316,11 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       else stage_all(std::false_type(), std::integral_constant<int, S::kPer>());
     }
   };
-  if (warp == kWarps) {
-    if (lane == 0 && !(grouped && by_groups(a))) find_adapter(p, t);
-  } else if (warp == kWarps + 1) {
-    tc5::tmem_alloc(&ctrl.tmem_base, S::kTmemCols);
-  }
-  tc5::tc_fence_before();
-  __syncthreads();
-  tc5::tc_fence_after();
-  const uint32_t tmem = ctrl.tmem_base;
-  if (t.n == 0) {                // the same for all blocks of the cluster
-    if (warp == kWarps + 1) tc5::tmem_dealloc(tmem, S::kTmemCols);
-    return;
-  }
-  const int rank = t.rank, blocks = (rank + 15) / 16, wide = (rank + 63) / 64;
-  const int a_slot = pieces_of(blocks), n_a = (np + a_slot - 1) / a_slot;      // pieces of A in a slot
-  const int last_term = kHalf ? 1 : a.y_dtype == RWKVQ_F32 ? 2 : 1;
-  // What lies behind the adapter's rank may be anything: in B's last sixteen columns it is masked, unless these end the rows, where a box has zeros.
-  const bool masks = rank % 16 != 0 && rank < a.rank;
-
-  if (warp == kWarps) {
-    // ---- copies.  This warp and the next bring nothing to the first meeting of the cluster and do not hold it up: what they wait for below comes behind it.
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    const int total = n_a + (o1 - o0) * wide;
-    // Nor does it hold up the second one by waits for slots that B had, which are given back behind that.
-    auto second = [] { asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory"); };
-    bool met = false;
+  if (warp == S::kWorkers) {
+    // ---- copies
     int i = 0, px = 0, gx = 0;
     Turn<kRing> slot;
     Turn<S::kGroups> group;
-    const CUtensorMap* const a_map = &p.A[blocks - 1];
-    const uint32_t a_bytes = (uint32_t)(a_slot * blocks) * 2048u;
     auto ask_x = [&](int upto) {
 #pragma unroll 1
       for (; px < upto; px += S::kGroup, ++gx) {
@@ -345,7 +337,24 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
         group.next();
       }
     };
-    if (p.x_by_map) ask_x(min(np, S::kGroup));
+    if (p.x_by_map && n > 0) ask_x(min(np, S::kGroup * S::kGroups));        // as much as there is room for, whatever the adapter
+    if (lane == 0) {
+      if (!(grouped && by_groups(a))) find_adapter(p, t);
+      tc5::mbar_arrive(&ctrl.ready);
+    }
+    __syncwarp();
+    if (!settle()) {
+      for (int j = 0; j < gx; ++j) wait(xfull + (uint32_t)j * 8u, 0);
+      return;
+    }
+    // This warp and those behind it bring nothing to the first meeting of the cluster and do not hold it up: what they wait for below comes behind it.
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const int total = n_a + (o1 - o0) * wide;
+    // Nor does this one hold up the second by waits for slots that B had, which are given back behind that.
+    auto second = [] { asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory"); };
+    bool met = false;
+    const CUtensorMap* const a_map = &p.A[blocks - 1];
+    const uint32_t a_bytes = (uint32_t)(a_slot * blocks) * 2048u;
 #pragma unroll 1
     for (; i < n_a; ++i) {
       const uint32_t bar = full + slot.at * 8u, dst = ring + slot.at * kSlotBytes;
@@ -376,8 +385,18 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     if (lane == 0) { ctrl.asked = i; ctrl.x_asked = gx; }
     __syncwarp();
     if (!met) second();
-  } else if (warp == kWarps + 1) {
+  } else if (warp == S::kWorkers + 1) {
     // ---- products
+    tc5::tmem_alloc(&ctrl.tmem_base, S::kTmemCols);
+    tc5::tc_fence_before();
+    __syncwarp();
+    const bool goes_on = settle();
+    tc5::tc_fence_after();
+    const uint32_t tmem = *static_cast<volatile uint32_t*>(&ctrl.tmem_base);
+    if (!goes_on) {
+      tc5::tmem_dealloc(tmem, S::kTmemCols);
+      return;
+    }
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     const uint64_t ring_desc = tc5::smem_desc_sw128(ring), x_desc = tc5::smem_desc_sw128(xring);
     constexpr uint32_t kA = idesc_of(F::kHalf, S::kColsA);
@@ -438,7 +457,8 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       if (!__all_sync(~0u, ok)) break;
       tc5::umma_commit(&ctrl.full_acc[acc]);
     }
-  } else if (warp > kWarps + 1) {
+  } else if (warp > S::kWorkers + 1) {
+    if (!settle()) return;
     // ---- masks, each of two warps for every second tile of B: no more tiles ahead of the products than the ring has slots
     // two warps that have nothing to do yet have y's rows fetched to the second-level cache, which are read when all else is done, and those of x
     auto fetch = [](const void* base, long long at, int elements, int size) {
@@ -446,14 +466,14 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     };
     for (int r = lane; r < n; r += 32) {
       const int columns = min((k0 + np) * 64, a.ic) - k0 * 64;
-      if (warp == kWarps + 3) fetch(a.x, (long long)row_of(r) * a.x_row + k0 * 64, columns, (int)sizeof(X));
-      if (warp == kWarps + 3 && a.x_prev) fetch(a.x_prev, (long long)row_of(r) * a.x_prev_row + k0 * 64, columns, (int)sizeof(X));
-      if (warp == kWarps + 2) fetch(a.y, (long long)row_of(r) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
+      if (warp == S::kWorkers + 3) fetch(a.x, (long long)row_of(r) * a.x_row + k0 * 64, columns, (int)sizeof(X));
+      if (warp == S::kWorkers + 3 && a.x_prev) fetch(a.x_prev, (long long)row_of(r) * a.x_prev_row + k0 * 64, columns, (int)sizeof(X));
+      if (warp == S::kWorkers + 2) fetch(a.y, (long long)row_of(r) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
     }
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
     if (masks)
 #pragma unroll 1
-      for (int o = warp - kWarps - 2; o < o1 - o0; o += 2) {
+      for (int o = warp - S::kWorkers - 2; o < o1 - o0; o += 2) {
         const int i = n_a + o * wide + wide - 1, tail = rank - (wide - 1) * 64;
         uint8_t* const weights = smem + i % kRing * kSlotBytes;
         wait(full + (uint32_t)(i % kRing) * 8u, (uint32_t)(i / kRing) & 1u);
@@ -477,15 +497,14 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
         if (lane == 0) tc5::mbar_arrive(&ctrl.masked[o % (kRing + 1)]);
       }
   } else {
-    if (!p.x_by_map && np > 0) stage();
+    if (!p.x_by_map && np > 0 && n > 0) stage();
+    if (!settle()) return;
     // ---- this block's share of A x: lanes are the rank
-    constexpr int kCols = NT / 2;
+    constexpr int kCols = NT * 4 / S::kWorkers;
     const int quarter = warp & 3, col0 = (warp >> 2) * kCols;
-    const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
-    if (np > 0) {
-      wait(smem_u32(&ctrl.a_done), 0);
-      tc5::tc_fence_after();
-    }
+    wait(smem_u32(&ctrl.a_done), 0);
+    tc5::tc_fence_after();
+    const uint32_t lanes = *static_cast<volatile uint32_t*>(&ctrl.tmem_base) + ((uint32_t)quarter << 21);
     if (quarter * 32 < blocks * 16) {
       float sum[kCols];
 #pragma unroll
@@ -511,7 +530,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       constexpr int kC = decltype(blocks_of_cluster)::value;
       const int wl = blocks == 1 ? 4 : blocks == 2 ? 8 : blocks <= 4 ? 16 : 32, r4 = lane % wl * 4, row1 = n * (c + 1) / kC;
 #pragma unroll 1
-      for (int row0 = n * c / kC + warp * (32 / wl); row0 < row1; row0 += kWarps * (32 / wl)) {
+      for (int row0 = n * c / kC + warp * (32 / wl); row0 < row1; row0 += S::kWorkers * (32 / wl)) {
         const int row = row0 + lane / wl;
         const bool there = row < row1 && r4 < blocks * 16;
         float h[4] = {0.f, 0.f, 0.f, 0.f};
@@ -576,7 +595,7 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
     else if (a.y_dtype == RWKVQ_F16) store_y<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
     else store_y<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
   }
-  if (warp == kWarps || warp > kWarps + 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (warp == S::kWorkers || warp > S::kWorkers + 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   tc5::tc_fence_before();
   __syncthreads();
   tc5::tc_fence_after();
@@ -589,13 +608,13 @@ __global__ void __launch_bounds__(kTileAll, 1) lowrank_tile_kernel(const __grid_
       for (int i = max(0, ctrl.asked - kRing); i < ctrl.asked; ++i) arrived(full + (uint32_t)(i % kRing) * 8u, (uint32_t)(i / kRing) & 1u);
       for (int i = max(0, ctrl.x_asked - S::kGroups); i < ctrl.x_asked; ++i) arrived(xfull + (uint32_t)(i % S::kGroups) * 8u, (uint32_t)(i / S::kGroups) & 1u);
     }
-    if (warp == kWarps + 1) {
+    if (warp == S::kWorkers + 1) {
       tc5::umma_commit(&ctrl.drained);
       arrived(smem_u32(&ctrl.drained), 0);
     }
     __syncthreads();
   }
-  if (warp == kWarps + 1) tc5::tmem_dealloc(tmem, S::kTmemCols);
+  if (warp == S::kWorkers + 1) tc5::tmem_dealloc(ctrl.tmem_base, S::kTmemCols);
 }
 
 // Clusters of C blocks that are on the device at once; asked for once per device (the kernels are alike in this: one block an SM).
@@ -605,7 +624,7 @@ long long clusters_at_once(const void* kernel, unsigned C) {
   int n = dev >= 0 ? known[dev][h].load(std::memory_order_relaxed) : 0;
   if (n > 0) return n;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(C); cfg.blockDim = dim3(kTileAll); cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.gridDim = dim3(C); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmemBytes;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
@@ -654,7 +673,7 @@ cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
   while (C > 1 && items > clusters_at_once((const void*)lowrank_tile_kernel<X, W, NT>, C)) C /= 2;
   p.splits = (int)std::max<long long>(1, std::min<long long>({clusters_at_once((const void*)lowrank_tile_kernel<X, W, NT>, C) / items, (a.oc + 128ll * C - 1) / (128 * C), 16}));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(kTileAll); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = s;
+  cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(S::kAll); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
