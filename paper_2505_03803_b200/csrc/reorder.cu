@@ -17,7 +17,7 @@ int* device_status_ptr();  // api_misc.cu
 namespace ro {
 
 constexpr int kMostParts = 128, kMostBeams = 64;
-constexpr uint32_t kBuffer = 32 << 10;          // bytes of shared memory for a block's pieces: seven blocks an SM
+constexpr uint32_t kBuffer = 16 << 10;          // bytes of shared memory for a block's pieces: thirteen blocks an SM
 
 struct Part { uint8_t* base; uint64_t row, bytes; };
 struct Args {
@@ -86,15 +86,15 @@ __global__ void __launch_bounds__(32) state_reorder_kernel(const __grid_constant
   }
   __syncwarp();
   const long long each = a.first[a.n_parts], all = each * a.requests;
-  long long i = all * blockIdx.x / gridDim.x;
-  const long long end = all * (blockIdx.x + 1ll) / gridDim.x;
+  // One request after the other, by all blocks: requests differ in how many of their beams move.
+  long long i = blockIdx.x;
   Request q;
   int r = -1;
   uint32_t parity = 0;
-  while (i < end) {
+  while (i < all) {
     const int now = (int)(i / each);
     if (now != r) { r = now; q.take(a, r); }
-    if (!q.any) { i = (r + 1ll) * each; continue; }
+    if (!q.any) { i += ((r + 1ll) * each - i + gridDim.x - 1) / gridDim.x * gridDim.x; continue; }
     const uint32_t c = (uint32_t)(i - r * each);
     int p = 0;
     for (int step = kMostParts / 2; step > 0; step /= 2)
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(32) state_reorder_kernel(const __grid_constant
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();
-    ++i;
+    i += gridDim.x;
   }
   asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
@@ -190,7 +190,8 @@ rwkvq_status rwkvq_state_reorder(const rwkvq_state_part* parts, int n_parts, int
       a.first[i + 1] = a.first[i] + (uint32_t)((all[at + i].bytes + chunk - 1) / chunk);
     }
     const long long pieces = (long long)a.first[a.n_parts] * requests, most = (long long)sm_count() * std::min<uint32_t>(32, (224u << 10) / (bytes + 1024));
-    ro::state_reorder_kernel<<<(unsigned)std::min(pieces, most), 32, bytes, static_cast<cudaStream_t>(stream)>>>(a);
+    const long long each = (pieces + most - 1) / most;          // as many pieces for every block
+    ro::state_reorder_kernel<<<(unsigned)((pieces + each - 1) / each), 32, bytes, static_cast<cudaStream_t>(stream)>>>(a);
     e = cudaGetLastError();
   }
   return cuda_status(e);

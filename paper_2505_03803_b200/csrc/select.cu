@@ -6,7 +6,7 @@
 // candidates of different beams come near one another.
 //
 // Finding the best of a piece: no sort.  A thread holds 64 bytes of a tile in registers, and knows the largest element.  The q-th largest of a warp's 32 largest
-// ones, q = ceil(picks / 8), is passed by q elements in each of the block's eight warps, so that what is below the least of these eight cannot be among the best:
+// ones, q = ceil(picks / 8), is passed by q elements in each of the block's eight warps (or as many as a short row has elements for), so that what is below the least of these cannot be among the best:
 // a few dozen elements of the tile are left, and ranked by counting.  From the second tile on the last best element is the bound, and hardly any tile has one above it.
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
@@ -149,7 +149,8 @@ __global__ void __launch_bounds__(kThreads, 4) beam_scan_kernel(const Args a) {
   const uint4* const vecs = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row) - skew);
   const int n_vecs = (a.vocab + V - 1) / V;
   const int v0 = min((int)blockIdx.x * a.piece_vecs, n_vecs), v1 = min(v0 + a.piece_vecs, n_vecs);
-  const int q = (a.picks + kWarps - 1) / kWarps;
+  // warps that have an element for each lane in the first tile
+  const int full = min(kWarps, (v1 - v0) / 32), q = full > 0 ? (a.picks + full - 1) / full : 33;
   auto load = [&](int t0, uint4 (&w)[kLoads]) {
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) {
@@ -159,14 +160,12 @@ __global__ void __launch_bounds__(kThreads, 4) beam_scan_kernel(const Args a) {
       } else if (skew != 0 && v < v1 && v > 0 && first + 2 * V <= a.vocab) {
         w[l] = joined(__ldg(vecs + v), __ldg(vecs + v + 1), skew);
       } else {
-        uint64_t lo = 0, hi = 0;
-#pragma unroll 1
-        for (int j = V - 1; j >= 0; --j) {
-          constexpr int kBits = 32 / R::kPer;
-          hi = hi << kBits | lo >> (64 - kBits);
-          lo = lo << kBits | (v < v1 && first + j < a.vocab ? R::word(row + first + j) : R::kNone);
-        }
-        w[l] = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+        // the ends of a row: an element at a time, all on their way together
+        uint32_t e[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) e[j] = v < v1 && first + j < a.vocab ? R::word(row + first + j) : R::kNone;
+        if constexpr (R::kPer == 2) w[l] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4 % V] | e[5 % V] << 16, e[6 % V] | e[7 % V] << 16);
+        else w[l] = make_uint4(e[0], e[1], e[2], e[3]);
       }
     }
   };
@@ -255,13 +254,13 @@ __global__ void __launch_bounds__(kThreads, 4) beam_scan_kernel(const Args a) {
     // about as many times the places have come together.
     float least = -INFINITY;
     if (k == 1) {
-      const uint32_t low = qth_of_warp(order_of(top), q);
+      const uint32_t low = q <= 32 ? qth_of_warp(order_of(top), q) : 0u;
       if (lane == 0) b.warp_low[warp] = low;
       if (tid == 0) b.count = 0;
       __syncthreads();
       uint32_t l = ~0u;
 #pragma unroll
-      for (int i = 0; i < kWarps; ++i) l = min(l, b.warp_low[i]);
+      for (int i = 0; i < kWarps; ++i) l = i < max(full, 1) ? min(l, b.warp_low[i]) : l;
       if (l) least = value_of(l);
     }
     if (top > floor && top >= least) {
