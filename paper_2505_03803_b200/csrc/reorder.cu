@@ -85,6 +85,8 @@ __global__ void __launch_bounds__(32) state_reorder_kernel(const __grid_constant
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncwarp();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
   const long long each = a.first[a.n_parts], all = each * a.requests;
   // One request after the other, by all blocks: requests differ in how many of their beams move.
   long long i = blockIdx.x;
@@ -191,8 +193,13 @@ rwkvq_status rwkvq_state_reorder(const rwkvq_state_part* parts, int n_parts, int
     }
     const long long pieces = (long long)a.first[a.n_parts] * requests, most = (long long)sm_count() * std::min<uint32_t>(32, (224u << 10) / (bytes + 1024));
     const long long each = (pieces + most - 1) / most;          // as many pieces for every block
-    ro::state_reorder_kernel<<<(unsigned)((pieces + each - 1) / each), 32, bytes, static_cast<cudaStream_t>(stream)>>>(a);
-    e = cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((pieces + each - 1) / each)); cfg.blockDim = dim3(32); cfg.dynamicSmemBytes = bytes; cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, ro::state_reorder_kernel, a);
   }
   return cuda_status(e);
 }

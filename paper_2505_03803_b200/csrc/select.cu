@@ -137,7 +137,8 @@ __global__ void __launch_bounds__(kThreads, 4) beam_scan_kernel(const Args a) {
   __shared__ Best b;
   __shared__ float warp_m[kWarps];
   __shared__ double warp_s[kWarps];
-  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");        // only now: the second kernel reads the beams' scores before this one is done
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long r = blockIdx.y;
   const float score = a.scores[r];
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
   __shared__ int count;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, K = a.beams, P = a.picks;
   const long long r0 = (long long)blockIdx.x * K;
-  // what the beams are is known before the scan, which nothing in front of it overlaps with, is done
+  // what the beams are is known before the scan is done, which let this kernel begin when all in front of it was
   if (warp == 0) {
     int kinds[2];
 #pragma unroll
@@ -536,15 +537,15 @@ template <typename T>
 cudaError_t launch(Args a, cudaStream_t s) {
   const int V = 4 * Raw<T>::kPer;
   a.piece_vecs = ((a.vocab + V - 1) / V + a.pieces - 1) / a.pieces;
-  beam_scan_kernel<T><<<dim3((unsigned)a.pieces, (unsigned)(a.requests * a.beams)), kThreads, 0, s>>>(a);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.requests); cfg.blockDim = dim3(kThreads); cfg.stream = s;
+  cfg.gridDim = dim3((unsigned)a.pieces, (unsigned)(a.requests * a.beams)); cfg.blockDim = dim3(kThreads); cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, beam_scan_kernel<T>, a);
+  if (e != cudaSuccess) return e;
+  cfg.gridDim = dim3((unsigned)a.requests);
   return cudaLaunchKernelEx(&cfg, beam_merge_kernel, a);
 }
 
