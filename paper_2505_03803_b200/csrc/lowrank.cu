@@ -20,14 +20,15 @@ namespace rwkvq {
 namespace lr {
 
 // ---- few rows -----------------------------------------------------------------------------------------------
-template <bool kHalf>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&w)[4], uint32_t x0, uint32_t x1) {
-  if constexpr (kHalf)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(x0), "r"(x1));
-  else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(x0), "r"(x1));
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(x0), "r"(x1));
+}
+// A pair of f16 weights as two pairs of bf16: eleven bits are eight and three.  (Of an infinity the second is NaN.)
+__device__ __forceinline__ void apart(uint32_t w, uint32_t& hi, uint32_t& lo) {
+  float2 f = pair_of(w, __half());
+  hi = cut_off(f);
+  lo = rounded(f, __nv_bfloat16());
 }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -35,9 +36,9 @@ __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
 // A slot of the ring: as many pieces of 64 columns of all rows of A as fit, or 128 rows by 64 columns of B.
 constexpr int kSlotBytes = 16 << 10, kPass = 8, kXPiece = kRows * 128;      // a pass over x: pieces of 64 columns that are in shared memory at a time
 constexpr int kAll = kThreads + 32;                                         // a warp that asks for copies
-template <typename X, typename W>
+template <typename X>
 struct Shape {
-  static constexpr int kTerms = Form<X, W>::kX, kSlots = kTerms == 1 ? 4 : 3;        // two blocks an SM
+  static constexpr int kTerms = Form<X, __half>::kX, kSlots = kTerms == 1 ? 4 : 3;        // two blocks an SM
   static constexpr int kXBytes = kTerms * kPass * kXPiece, kHBytes = 3 * 2 * kXPiece, kFront = kXBytes > kHBytes ? kXBytes : kHBytes;
   static constexpr int kPart = 4 * kRows * 68 * 4;                  // sums of half of the warps: [warp][row][rank], 64 of them and four warps, or 128 and two
   static constexpr int kShare = kRows * kMostRank * 4;
@@ -49,32 +50,26 @@ struct Ctrl {
   int abort_flag, asked;
 };
 
-// One weight fragment (16 rows x 16 columns), taken apart if it has to be, by up to sixteen rows of x in kTerms terms, the small products first.
-template <bool kHalf, bool kApart, int kTerms>
+// One weight fragment (16 rows x 16 columns), taken apart, by up to sixteen rows of x in kTerms terms, the small products first.
+template <int kTerms>
 __device__ __forceinline__ void multiply(float (&d)[2][4], const uint32_t (&w)[4], const uint32_t (&x)[kTerms][4], int terms, bool both) {
   uint32_t hi[4], lo[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    hi[i] = w[i]; lo[i] = 0;
-    if constexpr (kApart) apart(w[i], hi[i], lo[i]);
-  }
+  for (int i = 0; i < 4; ++i) apart(w[i], hi[i], lo[i]);
 #pragma unroll
   for (int k = kTerms - 1; k >= 0; --k) {
     if (k >= terms) continue;
-    if constexpr (kApart) {
-      mma<kHalf>(d[0], lo, x[k][0], x[k][1]);
-      if (both) mma<kHalf>(d[1], lo, x[k][2], x[k][3]);
-    }
-    mma<kHalf>(d[0], hi, x[k][0], x[k][1]);
-    if (both) mma<kHalf>(d[1], hi, x[k][2], x[k][3]);
+    mma(d[0], lo, x[k][0], x[k][1]);
+    if (both) mma(d[1], lo, x[k][2], x[k][3]);
+    mma(d[0], hi, x[k][0], x[k][1]);
+    if (both) mma(d[1], hi, x[k][2], x[k][3]);
   }
 }
 
-template <typename X, typename W>
+template <typename X>
 __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant__ Args p) {
-  using S = Shape<X, W>;
-  using F = Form<X, W>;
-  constexpr bool kWHalf = std::is_same<W, __half>::value;
+  using S = Shape<X>;
+  using F = Form<X, __half>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
   __shared__ Tile t;
@@ -199,7 +194,7 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
               if (j < side) ldmatrix4(w[j], at_w + (uint32_t)j * 2048u);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              if (j < side) multiply<F::kHalf, F::kApart, F::kX>(acc[j], w[j], x, F::kX, both);
+              if (j < side) multiply<F::kX>(acc[j], w[j], x, F::kX, both);
           }
         give(i);
       }
@@ -276,7 +271,7 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
               const uint32_t lo = q * 2 + 2 <= left ? ~0u : q * 2 + 1 <= left ? 0xFFFFu : 0u, hi = q * 2 + 10 <= left ? ~0u : q * 2 + 9 <= left ? 0xFFFFu : 0u;
               w[0][0] &= lo; w[0][1] &= lo; w[0][2] &= hi; w[0][3] &= hi;
             }
-            multiply<false, kWHalf, 3>(d, w[0], x, last_term + 1, both);
+            multiply<3>(d, w[0], x, last_term + 1, both);
           }
         give(i);
       }
@@ -319,17 +314,19 @@ __global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant_
       for (uint32_t k = 0; k < tc5::kPollLimit && !tc5::mbar_try_wait(full + (uint32_t)(i % S::kSlots) * 8u, (uint32_t)(i / S::kSlots) & 1u); ++k) {}
 }
 
-template <typename X, typename W>
-cudaError_t launch(Args p, long long items, cudaStream_t s) {
-  using S = Shape<X, W>;
+template <typename X>
+cudaError_t launch(Args& p, long long items, cudaStream_t s) {
+  using S = Shape<X>;
+  const rwkvq_lowrank_args& a = p.a;
+  if (!encode(p.A, a.A, true, a.ic, a.rank, a.n_adapters, 16) || !encode(&p.B, a.B, true, a.rank, a.oc, a.n_adapters, 128)) return cudaErrorUnknown;
   static SmemOptIn opt_in(kCarveOut);
-  cudaError_t e = opt_in((const void*)lowrank_kernel<X, W>, S::kBytes);
+  cudaError_t e = opt_in((const void*)lowrank_kernel<X>, S::kBytes);
   if (e != cudaSuccess) return e;
   // blocks that are there at once, two an SM: clusters as wide as that allows
   unsigned C = 8;
   while (C > 1 && items * C > 2ll * sm_count()) C /= 2;
   // where there are few tiles, several clusters divide a tile's rows of B, and each multiplies A x for itself
-  p.splits = (int)std::max<long long>(1, std::min<long long>({2ll * sm_count() / (items * C), (p.a.oc + 128 * C - 1) / (128 * C), 16}));
+  p.splits = (int)std::max<long long>(1, std::min<long long>({2ll * sm_count() / (items * C), (a.oc + 128ll * C - 1) / (128 * C), 16}));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(kAll); cfg.dynamicSmemBytes = S::kBytes; cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -338,11 +335,12 @@ cudaError_t launch(Args p, long long items, cudaStream_t s) {
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, lowrank_kernel<X, W>, p);
+  return cudaLaunchKernelEx(&cfg, lowrank_kernel<X>, p);
 }
-template <typename X>
-cudaError_t launch_x(const Args& p, long long items, cudaStream_t s) {
-  return p.a.w_dtype == RWKVQ_F16 ? launch<X, __half>(p, items, s) : launch<X, __nv_bfloat16>(p, items, s);
+cudaError_t launch(Args& p, cudaStream_t s) {
+  if (tiles_take(p.a.x_dtype, p.a.w_dtype)) return launch_tiles(p, s);
+  const long long items = most_tiles(p.a, kRows);
+  return p.a.x_dtype == RWKVQ_F32 ? launch<float>(p, items, s) : launch<__nv_bfloat16>(p, items, s);
 }
 
 int bytes_of(int dtype) { return dtype == RWKVQ_F32 ? 4 : dtype == RWKVQ_F16 || dtype == RWKVQ_BF16 ? 2 : 0; }
@@ -384,17 +382,7 @@ rwkvq_status rwkvq_lowrank(const rwkvq_lowrank_args* args, const rwkvq_desc* mu_
   }
   p.status = device_status_ptr();
   if (!p.status) return RWKVQ_ECUDA;
-  // tiles that there can be
-  const long long full = ((long long)a.tokens + lr::kRows - 1) / lr::kRows;
-  const long long items = a.seq_start ? std::min<long long>(a.tokens, full + a.n_seq) : a.n_seq == 1 ? full :
-                          lr::by_groups(a) ? std::min<long long>(a.n_seq, a.n_adapters + full) : a.n_seq;
-  const bool half = a.w_dtype == RWKVQ_F16;
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (lr::tiles_take(a.x_dtype, a.w_dtype)) return cuda_status(lr::launch_tiles(p, s));
-  if (!lr::encode(p.A, a.A, half, a.ic, a.rank, a.n_adapters, 16) || !lr::encode(&p.B, a.B, half, a.rank, a.oc, a.n_adapters, 128)) return cuda_status(cudaErrorUnknown);
-  if (a.x_dtype == RWKVQ_F32) return cuda_status(lr::launch_x<float>(p, items, s));
-  if (a.x_dtype == RWKVQ_F16) return cuda_status(lr::launch_x<__half>(p, items, s));
-  return cuda_status(lr::launch_x<__nv_bfloat16>(p, items, s));
+  return cuda_status(lr::launch(p, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

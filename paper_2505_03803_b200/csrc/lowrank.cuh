@@ -94,6 +94,11 @@ __device__ __forceinline__ void find_in_list(const Args& p, long long item, Tile
 
 __host__ __device__ inline bool single_rows(const rwkvq_lowrank_args& a) { return !a.seq_start && a.n_seq > 1; }      // each row a sequence
 __host__ __device__ inline bool by_groups(const rwkvq_lowrank_args& a) { return a.n_seq <= kThreads && a.n_adapters <= kMostCounted; }
+// Tiles of so many rows that there can be.
+inline long long most_tiles(const rwkvq_lowrank_args& a, int rows) {
+  const long long whole = ((long long)a.tokens + rows - 1) / rows;
+  return a.seq_start ? std::min<long long>(a.tokens, whole + a.n_seq) : !single_rows(a) ? whole : by_groups(a) ? std::min<long long>(a.n_seq, a.n_adapters + whole) : (long long)a.n_seq;
+}
 
 // The rows of a tile of up to kTile; of single rows that share an adapter (then t.n is final, and adapter, rank and scale are known, too) or of a sequence.  All threads.
 // scratch: 2 * kWarps + 2 numbers; memory: 8 * kMostCounted bytes.
@@ -209,20 +214,10 @@ __device__ __forceinline__ __nv_bfloat16 term(float& x) {
   return __ushort_as_bfloat16((unsigned short)(__float_as_uint(hi) >> 16));
 }
 
-// A pair of f16 weights as two pairs of bf16: eleven bits are eight and three.  (Of an infinity the second is NaN.)
-__device__ __forceinline__ void apart(uint32_t w, uint32_t& hi, uint32_t& lo) {
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-  const uint32_t x = __float_as_uint(f.x), y = __float_as_uint(f.y);
-  hi = __byte_perm(x, y, 0x7632);
-  const __nv_bfloat162 l = __floats2bfloat162_rn(f.x - __uint_as_float(x & 0xFFFF0000u), f.y - __uint_as_float(y & 0xFFFF0000u));
-  lo = *reinterpret_cast<const uint32_t*>(&l);
-}
-
-// How x and the weights go into the tensor cores.
+// How x goes into the tensor cores: as it is, or in bf16 terms.
 template <typename X, typename W> struct Form {
   static constexpr bool kHalf = std::is_same<X, __half>::value && std::is_same<W, __half>::value;
-  static constexpr int kX = std::is_same<X, W>::value ? 1 : std::is_same<X, float>::value ? 3 : std::is_same<X, __half>::value ? 2 : 1;
-  static constexpr bool kApart = std::is_same<W, __half>::value && !kHalf;
+  static constexpr int kX = kHalf || std::is_same<X, __nv_bfloat16>::value ? 1 : std::is_same<X, float>::value ? 3 : 2;
 };
 
 // Byte offset of 16 bytes (eight columns) in rows of 128 bytes under the 128-byte swizzle.
@@ -262,10 +257,10 @@ __device__ __forceinline__ Eights<X> load_eights(const Args& p, const RowOf<X>& 
   e.has_before = r.has_before;
   col = min(col, p.a.ic - 8);
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.x[i] = __ldg(reinterpret_cast<const uint4*>(r.x + col) + i);
+  for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.x[i] = reinterpret_cast<const uint4*>(r.x + col)[i];
   if constexpr (kMix)
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.before[i] = __ldg(reinterpret_cast<const uint4*>(r.before + col) + i);
+    for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.before[i] = reinterpret_cast<const uint4*>(r.before + col)[i];
   return e;
 }
 // Their indices of the token-shift vector: four are 4 * mu_bits neighbouring bits from a byte's beginning; behind the indices lies the codebook.

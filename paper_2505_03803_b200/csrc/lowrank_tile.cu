@@ -685,13 +685,9 @@ cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
 template <typename X, typename W>
 cudaError_t launch_form(Args& p, cudaStream_t s) {
   const rwkvq_lowrank_args& a = p.a;
-  auto tiles = [&](int rows) {
-    const long long whole = ((long long)a.tokens + rows - 1) / rows;
-    return a.seq_start ? std::min<long long>(a.tokens, whole + a.n_seq) : !single_rows(a) ? whole : by_groups(a) ? std::min<long long>(a.n_seq, a.n_adapters + whole) : (long long)a.n_seq;
-  };
   // tiles of 64 rows where sequences have half of that and more on average
-  if (!single_rows(a) && a.tokens >= 32ll * a.n_seq) return launch_tile<X, W, 64>(p, tiles(64), s);
-  return launch_tile<X, W, kRows>(p, tiles(kRows), s);
+  if (!single_rows(a) && a.tokens >= 32ll * a.n_seq) return launch_tile<X, W, 64>(p, most_tiles(a, 64), s);
+  return launch_tile<X, W, kRows>(p, most_tiles(a, kRows), s);
 }
 
 bool tiles_take(int x_dtype, int w_dtype) { return w_dtype == RWKVQ_BF16 || x_dtype == RWKVQ_F16; }

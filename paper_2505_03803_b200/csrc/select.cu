@@ -157,9 +157,9 @@ __global__ void __launch_bounds__(kThreads, 4) beam_scan_kernel(const Args a) {
     for (int l = 0; l < kLoads; ++l) {
       const int v = t0 + l * kThreads + tid, first = v * V;
       if (skew == 0 && v < v1 && first + V <= a.vocab) {
-        w[l] = __ldg(vecs + v);
+        w[l] = vecs[v];
       } else if (skew != 0 && v < v1 && v > 0 && first + 2 * V <= a.vocab) {
-        w[l] = joined(__ldg(vecs + v), __ldg(vecs + v + 1), skew);
+        w[l] = joined(vecs[v], vecs[v + 1], skew);
       } else {
         // the ends of a row: an element at a time, all on their way together
         uint32_t e[V];
