@@ -527,8 +527,8 @@ rwkvq_status rwkvq_lowrank(const rwkvq_lowrank_args* args, const rwkvq_desc* mu_
  * falling; equal ones by the lowest beam, then the lowest token.
  *  logits: [requests * beams][vocab] of dtype (F32, F16, BF16), logits_row elements from row to row.  A logit of -inf or NaN has probability zero and does not count; those
  *      of +inf, if there are any, share their beam's probability.  scores: [requests][beams] fp32; a beam whose score is infinite or NaN is dead: its
- *      totals are -inf, and its logits are not read.  Where fewer than `picks` totals are above -inf, the lowest (k, v) of the others follow with -inf.
- *  finished: [requests][beams] bytes, or NULL: a beam that has ended (not 0) has one candidate, token eos with its score unchanged, and its logits are not read.
+ *      totals are -inf, and its logits do not count.  Where fewer than `picks` totals are above -inf, the lowest (k, v) of the others follow with -inf.
+ *  finished: [requests][beams] bytes, or NULL: a beam that has ended (not 0) has one candidate, token eos with its score unchanged, and its logits do not count.
  *  next_scores, parents, tokens: [requests][picks]: the totals (fp32), their beams and tokens.  finished_out: [requests][picks] bytes, or NULL: whether the parent had ended or the token is eos.
  *      next_scores, finished_out and scores, finished are different buffers.
  * Maxima and sums of a thread are fp32, of a row and the totals fp64: they are compared before they are rounded (and where they are equal, within a beam the logits).

@@ -700,6 +700,11 @@ def _here() -> int:
     return t._C._cuda_getDevice() if t.cuda.is_initialized() else -2
 
 
+def _stream_here(stream, here: int):
+    """_stream_ptr where the current device is known."""
+    return _raw_stream(here) if stream is None and here >= 0 and _raw_stream is not None else _stream_ptr(stream)
+
+
 def _elsewhere(where: str, x, here: int):
     _refuse(where, f"a tensor is on {x.device}, the current device is {'not in use yet' if here < 0 else f'cuda:{here}'}")
 
@@ -919,7 +924,7 @@ def rwkvq_lowrank(x, A, B, y, adapter, seq_start=None, ranks=None, scale=None, x
                               0 if ranks is None else ranks.data_ptr(), 0 if scale is None else scale.data_ptr(), 0 if x_prev is None else x_prev.data_ptr(),
                               0 if xprev0 is None else xprev0.data_ptr(), rows[0], rows[1], 0 if x_prev is None else rows[2], tokens, n_seq, ic, oc, rank, n_adapters,
                               types.get(dtype, -1), types.get(w_dtype, -1), types.get(y.dtype, -1))
-    status = (_lib or lib()).rwkvq_lowrank(args, None if mu_desc is None else C.byref(mu_desc), None if mu_image is None else mu_image.data_ptr(), _stream_ptr(stream))
+    status = (_lib or lib()).rwkvq_lowrank(args, None if mu_desc is None else C.byref(mu_desc), None if mu_image is None else mu_image.data_ptr(), _stream_here(stream, here))
     if status:
         _check(status, where)
 
@@ -964,7 +969,7 @@ def rwkvq_beam_select(logits, scores, next_scores, parents, tokens, finished=Non
     args = _BEAM_SELECT_ARGS.pack(logits.data_ptr(), scores.data_ptr(), 0 if finished is None else finished.data_ptr(), next_scores.data_ptr(), parents.data_ptr(),
                                   tokens.data_ptr(), 0 if finished_out is None else finished_out.data_ptr(), row if requests * beams > 1 else vocab, requests, beams, vocab,
                                   picks, eos, (_DTYPES or _dtypes()).get(logits.dtype, -1))
-    status = (_lib or lib()).rwkvq_beam_select(args, *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)), _stream_ptr(stream))
+    status = (_lib or lib()).rwkvq_beam_select(args, *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)), _stream_here(stream, here))
     if status:
         _check(status, where)
 
@@ -1010,6 +1015,6 @@ def rwkvq_state_reorder(parts, parents, slots=None, stream=None):
     if slots is not None:
         _check_list(where, slots, requests * beams, "slots", here, t.int32)
     status = (_lib or lib()).rwkvq_state_reorder(parts.data, parts.n, parts.n_slots, parents.data_ptr(), None if slots is None else slots.data_ptr(), requests, beams,
-                                                 _stream_ptr(stream))
+                                                 _stream_here(stream, here))
     if status:
         _check(status, where)

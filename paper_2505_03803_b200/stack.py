@@ -392,6 +392,7 @@ class BlockStack:
         self._plan = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         B.rwkvq_step_plan(ops_arr, batch, self._plan)
         torch.cuda.synchronize()
+        self._parts = None
 
     def reset_state(self):
         """Start of a sequence: empty WKV history, zero previous-token inputs."""
@@ -400,6 +401,15 @@ class BlockStack:
         for o in self.ops:
             if o.xprev is not None:
                 o.xprev.zero_()
+
+    def follow(self, parents, stream=None):
+        """Beam search: the batch's sequences, `beams` to a request, go on from their parents, int32 [requests, beams] on the device (rwkvq_beam_select's): WKV history
+        and previous-token inputs of every block become those of the parents."""
+        if parents.numel() != self.batch:
+            raise ValueError(f"parents have to be [requests, beams] of {self.batch} sequences")
+        if self._parts is None:
+            self._parts = B.make_state_parts([st[k] for st in self.states for k in "abp"] + [o.xprev for o in self.ops if o.xprev is not None])
+        B.rwkvq_state_reorder(self._parts, parents, stream=stream)
 
     def set_token(self, seed: int):
         """A fresh seeded token (fp16 activations with outlier channels) in the pinned host buffer."""
