@@ -1,15 +1,16 @@
-// Low-rank adapters of many sequences beside a shared projection: y_t += s_a B_a (A_a x_t), a the adapter of t's sequence.
+// Low-rank adapters of many sequences beside a shared projection: y_t += s_a B_a (A_a x_t), a the adapter of t's sequence.  On the tcgen05 tensor cores, in tiles of up to 64 rows
+// of a sequence, or of up to sixteen rows that share an adapter.
 //
-// A tile is up to sixteen rows that have the same adapter; a cluster of thread blocks works on one.  Each block multiplies its share of the columns of A
-// with the rows' (token-shifted) inputs, the blocks add up their shares through distributed shared memory, and each multiplies its share of the rows of B
-// with the result: one launch, no workspace, sums in a fixed order.
+// The rows are the 16- to 64-column operand and the weights the 128-row one: A x is one accumulator of 128 (of the rank) by the tile's rows, B (A x) one for each 128 rows
+// of B, whose lanes are neighbouring columns of y.  A cluster of blocks divides the columns of A and the rows of B; A x is summed over the blocks through distributed
+// shared memory in their order: one launch, no workspace.  Weights come through tensor maps into a ring of seven slots, B's under the meeting of the blocks; x through a map, too, or,
+// where it has to be mixed with the row before or taken apart (see Form), by the warps that read the accumulators later.
 //
-// Weights come through tensor maps into a ring of shared memory, B's on their way while A's are multiplied, and are the 16-row operand of mma.sync.  Products are
-// exact: where the types of x and the weights differ, numbers are taken apart into bf16 terms (f16: two, f32: three), and so is A x, which is summed in fp32
-// (three terms, all of it, where y has 32 bits; two, the second rounded, where y has 16: off by up to 2^-16 of it).
+// A x, in fp32, goes on in bf16 terms (three, all of it, where y has 32 bits; two, the second rounded, where y has 16: off by up to 2^-16 of it), or, where the weights are f16,
+// in two f16 terms under a power of two per row that brings its largest number to 2^14 (off by up to 2^-22 of it, or 2^-38 of the row's largest).
 //
-// What such a call takes is latency, and much of that the instructions themselves, which are fetched for the first time in each block: loops are kept short and rolled
-// up (the same with weights straight to registers, unrolled for sixteen loads a lane on their way: 33 us where this takes XX, 96 rows with 64 adapters of 4096 x 4096).
+// A block takes all of an SM's shared memory, so that no other one that wants tensor memory is beside it: tcgen05.alloc has no limit to its wait, and a block
+// that holds tensor memory waits for the others of its cluster.
 #include <cooperative_groups.h>
 
 #include "lowrank.cuh"
@@ -19,328 +20,727 @@ namespace cg = cooperative_groups;
 namespace rwkvq {
 namespace lr {
 
-// ---- few rows -----------------------------------------------------------------------------------------------
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&w)[4], uint32_t x0, uint32_t x1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(x0), "r"(x1));
-}
-// A pair of f16 weights as two pairs of bf16: eleven bits are eight and three.  (Of an infinity the second is NaN.)
-__device__ __forceinline__ void apart(uint32_t w, uint32_t& hi, uint32_t& lo) {
-  float2 f = pair_of(w, __half());
-  hi = cut_off(f);
-  lo = rounded(f, __nv_bfloat16());
-}
-__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-// A slot of the ring: as many pieces of 64 columns of all rows of A as fit, or 128 rows by 64 columns of B.
-constexpr int kSlotBytes = 16 << 10, kPass = 8, kXPiece = kRows * 128;      // a pass over x: pieces of 64 columns that are in shared memory at a time
-constexpr int kAll = kThreads + 32;                                         // a warp that asks for copies
-template <typename X>
-struct Shape {
-  static constexpr int kTerms = Form<X, __half>::kX, kSlots = kTerms == 1 ? 4 : 3;        // two blocks an SM
-  static constexpr int kXBytes = kTerms * kPass * kXPiece, kHBytes = 3 * 2 * kXPiece, kFront = kXBytes > kHBytes ? kXBytes : kHBytes;
-  static constexpr int kPart = 4 * kRows * 68 * 4;                  // sums of half of the warps: [warp][row][rank], 64 of them and four warps, or 128 and two
-  static constexpr int kShare = kRows * kMostRank * 4;
-  static constexpr int kBytes = 1024 + kSlots * kSlotBytes + kFront + kPart + kShare + 256 * 4;
-  static_assert(kPart >= 8 * kMostCounted && kPart >= 2 * kRows * 132 * 4, "room for counting the rows of adapters, and for two warps' sums");
+using tc5::smem_u32;
+
+constexpr int kRing = 7, kSlotBytes = 16 << 10, kMostGroups = 4, kMostAcc = 4;
+constexpr int kSmemBytes = 224 << 10;
+
+// Pieces of 64 columns of A that a slot holds where the rank is up to 16 * blocks.
+__host__ __device__ constexpr int pieces_of(int blocks) { return blocks == 1 ? 8 : blocks == 2 ? 4 : blocks <= 4 ? 2 : 1; }
+
+template <typename X, typename W, int NT>
+struct TileShape {
+  static constexpr int kTerms = Form<X, W>::kX, kTileBytes = NT * 128, kPieceBytes = kTerms * kTileBytes;      // a piece: 64 columns of the tile's rows, a tile for each term
+  static constexpr int kGroup = NT == 64 ? 2 : 8, kGroups = NT == 16 ? 2 : kTerms == 1 ? 4 : kTerms == 2 ? 2 : 1;      // pieces that come at once, and how many such groups there is room for
+  static constexpr int kXBytes = kGroup * kGroups * kPieceBytes, kShare = NT * kMostRank * 4;
+  // Warps that make operands and read accumulators; behind them one that asks for copies, one that multiplies, two that mask.
+  static constexpr int kWorkers = NT == 64 ? 16 : 8, kWork = kWorkers * 32, kAll = kWork + 128;
+  static constexpr int kEights = kGroup * 8, kPer = kEights * NT / kWork;          // of a row in a group, and those of a thread where the tile is full
+  // Few rows: the terms lie side by side, as more columns of one product, and are added up when they are read (a product of few columns takes as long as its 128 weight rows take to
+  // read).  Many rows: one product after another into the same accumulator.
+  static constexpr bool kBeside = NT == 16;
+  static constexpr int kColsA = kBeside ? NT * kTerms : NT, kColsB = kBeside ? NT * 3 : NT;        // of an accumulator
+  static constexpr int kAcc = NT == 64 ? 2 : 4, kTmemCols = 256;
+  static_assert(kColsA + kAcc * kColsB <= kTmemCols, "tensor memory");
+  // The warps that read an accumulator, sixteen of its rows' columns each: a quarter of 64 rows, or all of sixteen, of every second tile.
+  static constexpr int kReaders = NT == 64 ? 16 : 4, kReadCols = 16;
+  static_assert(kXBytes >= 6 * kTileBytes, "A x takes x's place");
+  static_assert(1024 + kRing * kSlotBytes + kXBytes + kShare + 1024 <= kSmemBytes, "shared memory");
+  static_assert(kShare >= 8 * kMostCounted || NT == 64, "room for counting the rows of adapters");
 };
-struct Ctrl {
-  uint64_t full[4], empty[4];
-  int abort_flag, asked;
+struct TileCtrl {
+  uint64_t full[kRing], empty[kRing], masked[kRing + 1], ready, xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
+  int abort_flag, asked, x_asked;
+  uint32_t tmem_base;
+  float back[64];                 // of each row: the power of two that its A x was divided by
+  int top[64];                    // the bits of the largest finite number of a row that this block has
+};
+// Slots of a ring in turn.
+template <int N>
+struct Turn {
+  uint32_t at = 0, parity = 0;
+  __device__ __forceinline__ void next() { if (++at == N) { at = 0; parity ^= 1u; } }
 };
 
-// One weight fragment (16 rows x 16 columns), taken apart, by up to sixteen rows of x in kTerms terms, the small products first.
-template <int kTerms>
-__device__ __forceinline__ void multiply(float (&d)[2][4], const uint32_t (&w)[4], const uint32_t (&x)[kTerms][4], int terms, bool both) {
-  uint32_t hi[4], lo[4];
+// Both operands of a type (bf16, or f16), K-major -> fp32, 128 x N.
+__device__ __forceinline__ constexpr uint32_t idesc_of(bool half, int N) {
+  return (1u << 4) | (half ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24);
+}
+// Up to four steps of sixteen columns of both operands, by a converged warp: one lane is elected for all of them (a step at a time took some 100 cycles each).
+__device__ __forceinline__ void umma(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate, int steps) {
+  asm volatile(
+      "{\n .reg .pred q, p, one, q1, q2, q3;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      " elect.sync _|q, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n setp.eq.b32 one, 0, 0;\n"
+      " setp.gt.and.s32 q1, %5, 1, q;\n setp.gt.and.s32 q2, %5, 2, q;\n setp.gt.and.s32 q3, %5, 3, q;\n"
+      " add.u64 a1, %1, 2;\n add.u64 a2, %1, 4;\n add.u64 a3, %1, 6;\n add.u64 b1, %2, 2;\n add.u64 b2, %2, 4;\n add.u64 b3, %2, 6;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      " @q1 tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, one;\n"
+      " @q2 tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, one;\n"
+      " @q3 tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, one;\n}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate), "r"(steps) : "memory");
+}
+// 32 lanes x kCols columns; see tc5::tmem_ld32_issue.  Waits for them.
+template <int kCols>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[kCols]) {
+  if constexpr (kCols == 32) {
+    tc5::tmem_ld32_issue(taddr, r);
+    tc5::tmem_ld_wait(r);
+  } else {
+    static_assert(kCols == 8 || kCols == 16, "");
+    if constexpr (kCols == 16) {
+      asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+                     "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+      asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+      return;
+    } else {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]) :: "memory");
+    }
+  }
+}
+__device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, int v, uint32_t bar) {
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
+               " @q cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n}"
+               ::"r"(dst_smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(v), "r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t pair_bits(__nv_bfloat16 x, __nv_bfloat16 y) { return (uint32_t)__bfloat16_as_ushort(x) | (uint32_t)__bfloat16_as_ushort(y) << 16; }
+__device__ __forceinline__ uint32_t pair_bits(__half x, __half y) { return (uint32_t)__half_as_ushort(x) | (uint32_t)__half_as_ushort(y) << 16; }
+
+// Four neighbouring numbers of y and as many that are added to them.
+template <typename Y> struct Four { typename std::conditional<sizeof(Y) == 4, uint4, uint2>::type w; };
+template <typename Y>
+__device__ __forceinline__ void add_four(Four<Y>& y, const float4& d) {
+  Y* const v = reinterpret_cast<Y*>(&y.w);
+  v[0] = from_float<Y>(to_float<Y>(v[0]) + d.x); v[1] = from_float<Y>(to_float<Y>(v[1]) + d.y);
+  v[2] = from_float<Y>(to_float<Y>(v[2]) + d.z); v[3] = from_float<Y>(to_float<Y>(v[3]) + d.w);
+}
+// The accumulators of tiles [o0, o1) of B to y, by one of the warps: 32 lanes of a tile, and a quarter of its rows, or all of every second tile's.
+template <typename S, typename Y, bool kScaled>
+__device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, bool grouped, float* share, int last_term, bool& ok) {
+  const rwkvq_lowrank_args& a = p.a;
+  constexpr int kCols = S::kReadCols, kStep = S::kWorkers / S::kReaders;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = warp & 3, quad = lane & 7, r_lane = lane >> 3;
+  const int col0 = kStep == 1 ? (warp >> 2) * kCols : 0, first = kStep == 1 ? 0 : warp >> 2;
+  const int rows = min(n - col0, kCols);             // of this warp, maybe none
+  float* const turn = share + warp * (kMostRank * S::kTileBytes / 128 / S::kWorkers);       // its part of the share's place: 32 columns by kCols rows, or half of them at a time
+  constexpr int kTurn = S::kTileBytes / 128 * kMostRank / S::kWorkers / 32;                 // rows that it holds
+  Y* at[kCols / 4];                                  // rows r_lane, r_lane + 4, ...; those behind the last are read, where there are any at all, as the last
 #pragma unroll
-  for (int i = 0; i < 4; ++i) apart(w[i], hi[i], lo[i]);
+  for (int i = 0; i < kCols / 4; ++i) {
+    const int r = col0 + max(min(i * 4 + r_lane, rows - 1), -col0);
+    at[i] = static_cast<Y*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row;
+  }
+  // y of the next tiles is on its way while this one's is added to, some 48 to 64 KB an SM (into buffers that take turns, not moved: a move waits for what it moves)
+  constexpr int kDepth = sizeof(Y) == 2 ? 3 : 2;
+  Four<Y> buffers[kDepth][kCols / 4];
+  auto load = [&](int o, Four<Y> (&to)[kCols / 4]) {
+    const int col = min((o0 + o) * 128 + quarter * 32 + quad * 4, a.oc - 4);
+    if (rows > 0 && o < o1 - o0)
 #pragma unroll
-  for (int k = kTerms - 1; k >= 0; --k) {
-    if (k >= terms) continue;
-    mma(d[0], lo, x[k][0], x[k][1]);
-    if (both) mma(d[1], lo, x[k][2], x[k][3]);
-    mma(d[0], hi, x[k][0], x[k][1]);
-    if (both) mma(d[1], hi, x[k][2], x[k][3]);
+      for (int i = 0; i < kCols / 4; ++i) to[i] = *reinterpret_cast<const Four<Y>*>(at[i] + col);
+  };
+#pragma unroll
+  for (int k = 0; k < kDepth; ++k) load(first + k * kStep, buffers[k]);
+#pragma unroll 1
+  for (int round = first; round < o1 - o0; round += kDepth * kStep)
+#pragma unroll
+  for (int turn_of = 0; turn_of < kDepth; ++turn_of) {
+    const int o = round + turn_of * kStep, acc = o % S::kAcc, col = (o0 + o) * 128 + quarter * 32 + quad * 4;
+    if (o >= o1 - o0) continue;
+    Four<Y> (&y)[kCols / 4] = buffers[turn_of];
+    ok = ok && tc5::mbar_wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / S::kAcc) & 1u, &ctrl.abort_flag, p.status);
+    if (!__all_sync(~0u, ok)) return;
+    tc5::tc_fence_after();
+    float sum[kCols];
+    const uint32_t from = acc0 + (uint32_t)(acc * S::kColsB + col0);
+    {
+      uint32_t v[kCols];
+      tmem_ld<kCols>(from, v);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) sum[j] = __uint_as_float(v[j]);
+      if constexpr (S::kBeside) {
+#pragma unroll 1
+        for (int k = 1; k <= last_term; ++k) {
+          tmem_ld<kCols>(from + (uint32_t)(k * kCols), v);
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) sum[j] += __uint_as_float(v[j]);
+        }
+      }
+    }
+    tc5::tc_fence_before();
+    __syncwarp();
+    if (lane == 0) tc5::mbar_arrive(&ctrl.empty_acc[acc]);
+    if (rows <= 0) continue;
+    // [row][column], rows of 128 bytes: each lane a column, then each quarter of a warp a row
+#pragma unroll
+    for (int h = 0; h < kCols / kTurn; ++h) {
+      if (h * kTurn >= rows) continue;
+#pragma unroll
+      for (int j = 0; j < kTurn; ++j) turn[j * 32 + lane] = sum[h * kTurn + j];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kTurn / 4; ++i) {
+        const int r = h * kTurn + i * 4 + r_lane;
+        float4 d = *reinterpret_cast<const float4*>(turn + (i * 4 + r_lane) * 32 + quad * 4);
+        if constexpr (kScaled) { const float back = ctrl.back[min(col0 + r, n - 1)]; d.x *= back; d.y *= back; d.z *= back; d.w *= back; }
+        Four<Y>& mine = y[h * kTurn / 4 + i];
+        add_four<Y>(mine, d);
+        if (r < rows && col < a.oc) *reinterpret_cast<Four<Y>*>(at[h * kTurn / 4 + i] + col) = mine;
+      }
+      __syncwarp();
+    }
+    load(o + kDepth * kStep, y);
   }
 }
 
-template <typename X>
-__global__ void __launch_bounds__(kAll, 2) lowrank_kernel(const __grid_constant__ Args p) {
-  using S = Shape<X>;
-  using F = Form<X, __half>;
+template <typename X, typename W, int NT>
+__global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_kernel(const __grid_constant__ Args p) {
+  using S = TileShape<X, W, NT>;
+  using F = Form<X, W>;
+  constexpr bool kHalf = std::is_same<W, __half>::value;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~(uintptr_t)1023u);
   __shared__ Tile t;
-  __shared__ Ctrl ctrl;
+  __shared__ TileCtrl ctrl;
   __shared__ int scratch[2 * kWarps + 2];
-  uint8_t* const xs = smem + S::kSlots * kSlotBytes;                     // [term][piece][row][64 columns], then A x: [term][piece][row][64 of the rank]
-  float* const part = reinterpret_cast<float*>(xs + S::kFront);
-  float* const share = part + S::kPart / 4;                              // this block's share of A x: [row][rank]
+  uint8_t* const xs = smem + kRing * kSlotBytes;                         // [slot][term][row][64 columns], then A x: [term][64 of the rank][row][64], or [64 of the rank][term][row][64]
+  float* const share = reinterpret_cast<float*>(xs + S::kXBytes);        // this block's share of A x: [row][rank]
   uint32_t* const codebook = reinterpret_cast<uint32_t*>(share + S::kShare / 4);
   const rwkvq_lowrank_args& a = p.a;
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   volatile int* const abortp = &ctrl.abort_flag;
   asm volatile("griddepcontrol.launch_dependents;");
+  if (tid < 64) ctrl.top[tid] = 0;
   if (tid == 0) {
-    for (int i = 0; i < S::kSlots; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], kWarps); }
-    ctrl.abort_flag = ctrl.asked = 0;
+    for (int i = 0; i < kRing; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], 1); }
+    for (int i = 0; i <= kRing; ++i) tc5::mbar_init(&ctrl.masked[i], 1);
+    for (int i = 0; i < S::kGroups; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : S::kWorkers); tc5::mbar_init(&ctrl.xempty[i], 1); }
+    for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], S::kReaders); }
+    tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.ready, 1); tc5::mbar_init(&ctrl.drained, 1);
+    ctrl.abort_flag = ctrl.asked = ctrl.x_asked = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\nfence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (tid == S::kWork) {          // the maps themselves are fetched from memory, too
+    auto fetch = [](const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); };
+    fetch(&p.A[(a.rank + 15) / 16 - 1]);
+    fetch(&p.B);
+    if (p.x_by_map) fetch(&p.X);
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (p.mu)
-    for (int i = tid; i < p.mu_entries; i += kAll) codebook[i] = p.mu_codebook[i];
+    for (int i = tid; i < p.mu_entries; i += S::kAll) codebook[i] = p.mu_codebook[i];
   const int id = (int)(blockIdx.x / C), item = id / p.splits, split = id - item * p.splits;
-  find_rows<kRows>(p, item, t, scratch, part);
+  find_rows<NT>(p, item, t, scratch, share);
   const int n = t.n;
-  const bool both = n > 8, grouped = single_rows(a);
-  const int pieces = (a.ic + 63) / 64, k0 = (int)((long long)pieces * c / C), k1 = (int)((long long)pieces * (c + 1) / C);
+  const bool grouped = NT == kRows && single_rows(a);
+  const int pieces = (a.ic + 63) / 64, k0 = (int)((long long)pieces * c / C), np = (int)((long long)pieces * (c + 1) / C) - k0;
   const int tiles = (a.oc + 127) / 128, parts = C * p.splits, at = split * C + c;
   const int o0 = (int)((long long)tiles * at / parts), o1 = (int)((long long)tiles * (at + 1) / parts);
-  const uint32_t ring = tc5::smem_u32(smem), full = tc5::smem_u32(ctrl.full), empty = tc5::smem_u32(ctrl.empty);
+  const uint32_t ring = smem_u32(smem), xring = smem_u32(xs), full = smem_u32(ctrl.full), empty = smem_u32(ctrl.empty), xfull = smem_u32(ctrl.xfull), xempty = smem_u32(ctrl.xempty);
+  bool ok = true;
+  auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && tc5::mbar_wait(bar, parity, abortp, p.status); };
+  auto row_of = [&](int r) { return grouped ? t.rows[r] : t.first + r; };
 
-  // x of columns [kp, ke), pieces of 64, in operand form
-  auto stage_x = [&](auto mix, int kp, int ke) {
-    const int eights = (ke - kp) * 8;
+  // What depends on the adapter, which one thread looks up while x is on its way; false where there is none: the same for all blocks of the cluster.
+  int rank = 0, blocks = 0, wide = 0, a_slot = 1, n_a = 0;
+  bool masks = false;
+  const int last_term = kHalf ? 1 : a.y_dtype == RWKVQ_F32 ? 2 : 1;
+  auto settle = [&] {
+    wait(smem_u32(&ctrl.ready), 0);
+    if (t.n == 0) return false;
+    rank = t.rank; blocks = (rank + 15) / 16; wide = (rank + 63) / 64;
+    a_slot = pieces_of(blocks); n_a = (np + a_slot - 1) / a_slot;          // pieces of A in a slot, and slots
+    // What lies behind the adapter's rank may be anything: in B's last sixteen columns it is masked, unless these end the rows, where a box has zeros.
+    masks = rank % 16 != 0 && rank < a.rank;
+    return true;
+  };
+
+  // All groups of x in operand form, by the workers: the loads of two groups are on their way while one is made (into buffers that take turns, not moved: a move
+  // waits for what it moves).  A thread has kN eights of columns of a group, one where the tile has few rows.
+  auto stage_all = [&](auto mix, auto per) {
+    constexpr bool kMix = decltype(mix)::value;
+    constexpr int kN = decltype(per)::value;
+    Turn<S::kGroups> turn;
+    Eights<X> raw[2][kN];
+    MuWords words[2];
+    // kWork is a multiple of a row's eights: the columns are the same for all rows of a thread
+    const int piece = tid % S::kEights / 8, groups = (np + S::kGroup - 1) / S::kGroup;
+    auto col_of = [&](int g) { return (k0 + min(g * S::kGroup + piece, np - 1)) * 64 + (tid & 7) * 8; };
+    RowOf<X> rows[kN];
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const int row = row_of(min((tid + j * S::kWork) / S::kEights, n - 1));
+      rows[j] = row_at<X>(p, row, grouped ? row : t.seq, grouped || row == t.start);
+    }
+    auto load = [&](int g, Eights<X> (&e)[kN], MuWords& m) {
+      const int col = col_of(g);
+      m = load_mu<kMix>(p, col);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) e[j] = load_eights<X, kMix>(p, rows[j], col);
+    };
+    load(0, raw[0], words[0]);
+    load(1, raw[1], words[1]);
+    float by[kN];
+    if constexpr (F::kScaled) {          // first the largest number of each row: all groups are read twice but the first two
+      int top[kN] = {};
+      auto look = [&](int g, const Eights<X> (&e)[kN], const MuWords& m) {
+        float2 mu[4], f[4];
+        mu_of<kMix>(p, codebook, m, col_of(g), mu);
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          mix_eights<X, kMix>(e[j], mu, f);
+          top[j] = max(top[j], top_of(f));
+        }
+      };
 #pragma unroll 1
-    for (int e = tid; e < n * eights; e += kThreads) {
-      const int r = e / eights, eight = e - r * eights, col = kp * 64 + eight * 8, row = grouped ? t.rows[r] : t.first + r;
-      const Eights<X> raw = load_eights<X, decltype(mix)::value>(p, row_at<X>(p, row, grouped ? row : t.seq, grouped || row == t.start), col);
-      const MuWords words = load_mu<decltype(mix)::value>(p, col);
-      float2 mu[4];
-      mu_of<decltype(mix)::value>(p, codebook, words, col, mu);
-      put_eights<X, F, decltype(mix)::value>(raw, mu, xs + eight / 8 * kXPiece + swizzled(r, eight & 7), kPass * kXPiece);
+      for (int g = 2; g < groups; ++g) {
+        Eights<X> e[kN];
+        MuWords m;
+        load(g, e, m);
+        look(g, e, m);
+      }
+      look(0, raw[0], words[0]);
+      look(1, raw[1], words[1]);
+      // the lanes of a row: all of a warp, or a half
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        int best = top[j];
+#pragma unroll
+        for (int o = 1; o < (S::kEights < 32 ? S::kEights : 32); o *= 2) best = max(best, __shfl_xor_sync(~0u, best, o));
+        if (lane % S::kEights == 0) atomicMax(&ctrl.top[(tid + j * S::kWork) / S::kEights], best);
+      }
+      asm volatile("bar.sync 1, %0;" ::"n"(S::kWork) : "memory");
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        float back;
+        powers_of(ctrl.top[(tid + j * S::kWork) / S::kEights], by[j], back);
+      }
+    }
+#pragma unroll 1
+    for (int g0 = 0; g0 < groups; g0 += 2)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int g = g0 + h;
+        if (g >= groups) continue;
+        if (g >= S::kGroups) {
+          if (g == S::kGroups && !settle()) return;          // nothing is multiplied where there is no adapter
+          wait(xempty + turn.at * 8u, turn.parity ^ 1u);
+        }
+        float2 mu[4];
+        mu_of<kMix>(p, codebook, words[h], col_of(g), mu);
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          const int row = (tid + j * S::kWork) / S::kEights;
+          if (j * S::kWork / S::kEights >= n) continue;          // of no thread
+          if (row < n) put_eights<X, F, kMix>(raw[h][j], mu, xs + (turn.at * S::kGroup + piece) * S::kPieceBytes + swizzled(row, tid & 7), S::kTileBytes, F::kScaled ? by[j] : 1.f);
+        }
+        if (g + 2 < groups) load(g + 2, raw[h], words[h]);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) tc5::mbar_arrive(xfull + turn.at * 8u);
+        turn.next();
+      }
+  };
+  auto stage = [&] {
+    const bool few = NT == kRows && n * S::kEights <= S::kWork;
+    if (p.mu) {
+      if (few) stage_all(std::true_type(), std::integral_constant<int, NT == kRows ? 1 : S::kPer>());
+      else stage_all(std::true_type(), std::integral_constant<int, S::kPer>());
+    } else {
+      if (few) stage_all(std::false_type(), std::integral_constant<int, NT == kRows ? 1 : S::kPer>());
+      else stage_all(std::false_type(), std::integral_constant<int, S::kPer>());
     }
   };
-  auto stage = [&](int kp, int ke) { if (p.mu) stage_x(std::true_type(), kp, ke); else stage_x(std::false_type(), kp, ke); };
-  if (warp == kWarps) {
-    if (lane == 0) find_adapter(p, t);
-  } else {
-    stage(k0, min(k0 + kPass, k1));
-  }
-  __syncthreads();
-  if (t.n == 0) return;            // the same for all blocks of the cluster
-  const int rank = t.rank, blocks = (rank + 15) / 16;
-  // ---- the ring: pieces of A for this block's columns, then tiles of B for its rows
-  const int a_slot = blocks == 1 ? 8 : blocks == 2 ? 4 : blocks <= 4 ? 2 : 1, n_a = (k1 - k0 + a_slot - 1) / a_slot;      // pieces of A in a slot
-  const int wide = (rank + 63) / 64;
-  bool ok = true;
-  auto take = [&](int i) { ok = ok && tc5::mbar_wait(full + (uint32_t)(i % S::kSlots) * 8u, (uint32_t)(i / S::kSlots) & 1u, abortp, p.status); };
-  auto give = [&](int i) {
+  if (warp == S::kWorkers) {
+    // ---- copies
+    int i = 0, px = 0, gx = 0;
+    Turn<kRing> slot;
+    Turn<S::kGroups> group;
+    auto ask_x = [&](int upto) {
+#pragma unroll 1
+      for (; px < upto; px += S::kGroup, ++gx) {
+        if (gx >= S::kGroups) wait(xempty + group.at * 8u, group.parity ^ 1u);
+        if (!__all_sync(~0u, ok)) return;
+        const uint32_t bar = xfull + group.at * 8u, to = xring + group.at * (S::kGroup * S::kPieceBytes);
+        const int count = p.whole ? S::kGroup : min(S::kGroup, np - px);
+        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.xfull[group.at], (uint32_t)(count * S::kTileBytes));
+        __syncwarp();
+        if (p.whole) tensor_g2s(to, &p.X, 0, t.first, k0 + px, bar);
+        else
+#pragma unroll 1
+          for (int j = 0; j < count; ++j) tensor_g2s(to + (uint32_t)(j * S::kTileBytes), &p.X, (k0 + px + j) * 64, t.first, 0, bar);
+        group.next();
+      }
+    };
+    if (p.x_by_map && n > 0) ask_x(min(np, S::kGroup * S::kGroups));        // as much as there is room for, whatever the adapter
+    if (lane == 0) {
+      if (!(grouped && by_groups(a))) find_adapter(p, t);
+      tc5::mbar_arrive(&ctrl.ready);
+    }
     __syncwarp();
-    if (lane == 0) tc5::mbar_arrive(empty + (uint32_t)(i % S::kSlots) * 8u);
-  };
-  if (warp == kWarps) {
-    // This warp brings nothing to the first meeting of the cluster and does not hold it up: the slots that it waits for below are given back behind it.
+    if (!settle()) {
+      for (int j = 0; j < gx; ++j) wait(xfull + (uint32_t)j * 8u, 0);
+      return;
+    }
+    // This warp and those behind it bring nothing to the first meeting of the cluster and do not hold it up: what they wait for below comes behind it.
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     const int total = n_a + (o1 - o0) * wide;
-    int i = 0;
+    // Nor does this one hold up the second by waits for slots that B had, which are given back behind that.
+    auto second = [] { asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory"); };
+    bool met = false;
+    const CUtensorMap* const a_map = &p.A[blocks - 1];
+    const uint32_t a_bytes = (uint32_t)(a_slot * blocks) * 2048u;
 #pragma unroll 1
-    for (; i < total; ++i) {
-      const uint32_t st = (uint32_t)(i % S::kSlots), bar = full + st * 8u, dst = ring + st * kSlotBytes;
-      if (i >= S::kSlots && !__all_sync(~0u, tc5::mbar_wait(empty + st * 8u, (uint32_t)(i / S::kSlots - 1) & 1u, abortp, p.status))) break;
-      if (i < n_a) {
-        const int first = k0 + i * a_slot, count = min(a_slot, k1 - first) * blocks;
-        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[st], (uint32_t)count * 2048u);
-        __syncwarp();
+    for (; i < n_a; ++i) {
+      const uint32_t bar = full + slot.at * 8u, dst = ring + slot.at * kSlotBytes;
+      if (i >= kRing) wait(empty + slot.at * 8u, slot.parity ^ 1u);
+      if (!__all_sync(~0u, ok)) break;
+      const int first = i * a_slot, count = p.whole ? a_slot : min(a_slot, np - first);
+      if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[slot.at], p.whole ? a_bytes : (uint32_t)(count * blocks) * 2048u);
+      __syncwarp();
+      if (p.whole) tensor_g2s(dst, a_map, 0, 0, k0 + first, t.adapter, bar);
+      else
 #pragma unroll 1
-        for (int j = 0, piece = first, r = 0; j < count; ++j) {
-          tensor_g2s(dst + (uint32_t)j * 2048u, &p.A[0], piece * 64, r, t.adapter, bar);
-          r += 16;
-          if (r >= rank) { r = 0; ++piece; }
-        }
-      } else {
-        const int j = i - n_a, tile = j / wide;
-        if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[st], kSlotBytes);
-        __syncwarp();
-        tensor_g2s(dst, &p.B, (j - tile * wide) * 64, (o0 + tile) * 128, t.adapter, bar);
-      }
+        for (int j = 0; j < count; ++j) tensor_g2s(dst + (uint32_t)(j * blocks) * 2048u, a_map, (k0 + first + j) * 64, 0, t.adapter, bar);
+      slot.next();
+      if (p.x_by_map) ask_x(min(np, first + a_slot + S::kGroup));        // a group ahead
     }
-    if (lane == 0) ctrl.asked = i;
+#pragma unroll 1
+    for (int tile = o0, k = 0; i < total; ++i) {
+      if (i - kRing >= n_a && !met) { second(); met = true; }
+      const uint32_t bar = full + slot.at * 8u;
+      if (i >= kRing) wait(empty + slot.at * 8u, slot.parity ^ 1u);
+      if (!__all_sync(~0u, ok)) break;
+      if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[slot.at], kSlotBytes);
+      __syncwarp();
+      tensor_g2s(ring + slot.at * kSlotBytes, &p.B, k * 64, tile * 128, t.adapter, bar);
+      if (++k == wide) { k = 0; ++tile; }
+      slot.next();
+    }
+    if (lane == 0) { ctrl.asked = i; ctrl.x_asked = gx; }
     __syncwarp();
-    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
-  } else {
-    // ---- A x.  Warps side by side along the columns; two groups of them, each 64 of the rank, where it is longer
-    const int deep = blocks > 4 ? 4 : 8, kw = warp % deep, r_first = warp / deep * 4, side = min(4, blocks - r_first);
-    float acc[4][2][4] = {};
-    const uint32_t x_at = tc5::smem_u32(xs) + (uint32_t)((lane & 7) + (lane >> 4) * 8) * 128u;
-    int i = 0;
-    for (int kp = k0; kp < k1; kp += kPass) {
-      const int ke = min(kp + kPass, k1);
-      if (kp > k0) {
-        asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
-        stage(kp, ke);
-        asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
-      }
-      // rows of x behind the n-th hold whatever was there: a row meets its own outputs alone
-      for (int first = kp; first < ke; first += a_slot, ++i) {
-        take(i);
-        const uint32_t slot = ring + (uint32_t)(i % S::kSlots * kSlotBytes);
-        const int steps = min(a_slot, ke - first) * 4;
-        if (ok)
+    if (!met) second();
+  } else if (warp == S::kWorkers + 1) {
+    // ---- products
+    tc5::tmem_alloc(&ctrl.tmem_base, S::kTmemCols);
+    tc5::tc_fence_before();
+    __syncwarp();
+    const bool goes_on = settle();
+    tc5::tc_fence_after();
+    const uint32_t tmem = *static_cast<volatile uint32_t*>(&ctrl.tmem_base);
+    if (!goes_on) {
+      tc5::tmem_dealloc(tmem, S::kTmemCols);
+      return;
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const uint64_t ring_desc = tc5::smem_desc_sw128(ring), x_desc = tc5::smem_desc_sw128(xring);
+    constexpr uint32_t kA = idesc_of(F::kHalf, S::kColsA);
+    const uint32_t kB = idesc_of(kHalf, S::kBeside ? NT * (last_term + 1) : NT);
+    Turn<kRing> slot;
+    {
+      Turn<S::kGroups> group;
+      uint32_t in_group = 0;
 #pragma unroll 1
-          for (int s = kw; s < steps; s += deep) {
-            const int piece = s >> 2, eight = (s & 3) * 2;
-            const uint32_t at_x = x_at + (uint32_t)((first - kp + piece) * kXPiece) + (uint32_t)(((eight + (lane >> 3 & 1)) ^ lane) & 7) * 16u;
-            const uint32_t at_w = slot + (uint32_t)(piece * blocks + r_first) * 2048u + swizzled(lane & 15, eight + (lane >> 4));
-            uint32_t x[F::kX][4], w[4][4];
+      for (int i = 0, px = 0; i < n_a; ++i) {
+        wait(full + slot.at * 8u, slot.parity);
+        uint64_t w = ring_desc + (slot.at * kSlotBytes >> 4);
+#pragma unroll 1
+        for (int j = 0; j < a_slot && px < np; ++j, ++px) {
+          if (in_group == 0) wait(xfull + group.at * 8u, group.parity);
+          if (!__all_sync(~0u, ok)) break;
+          tc5::tc_fence_after();
+          const uint64_t x = x_desc + ((group.at * S::kGroup + in_group) * S::kPieceBytes >> 4);
 #pragma unroll
-            for (int k = 0; k < F::kX; ++k) ldmatrix4(x[k], at_x + (uint32_t)k * (kPass * kXPiece));
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (j < side) ldmatrix4(w[j], at_w + (uint32_t)j * 2048u);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (j < side) multiply<F::kX>(acc[j], w[j], x, F::kX, both);
+          for (int k = S::kBeside ? 0 : F::kX - 1; k >= 0; --k) umma(tmem, w, x + (uint32_t)(k * S::kTileBytes / 16), kA, px > 0 || (!S::kBeside && k < F::kX - 1), 4);
+          w += (uint32_t)blocks * 128u;
+          if (++in_group == S::kGroup) {
+            tc5::umma_commit(&ctrl.xempty[group.at]);
+            group.next();
+            in_group = 0;
           }
-        give(i);
+        }
+        if (!__all_sync(~0u, ok)) break;
+        tc5::umma_commit(&ctrl.empty[slot.at]);
+        slot.next();
       }
     }
-    // the warps' sums added up: the second half of them to the first, then what is left of these
-    const int half = deep / 2, pitch = blocks > 4 ? 132 : 68;        // pitches that spare banks
-    auto each = [&](auto f) {
-      float* const to = part + (kw % half) * kRows * pitch + r_first * 16 + g;
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int row = b * 8 + q * 2 + e;
-          if (row >= n) continue;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (j < side) { f(to[row * pitch + j * 16], acc[j][b][e]); f(to[row * pitch + j * 16 + 8], acc[j][b][e + 2]); }
+    if (__all_sync(~0u, ok)) tc5::umma_commit(&ctrl.a_done);
+    // the second meeting: A x is there, from all blocks
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("fence.proxy.async;" ::: "memory");
+#pragma unroll 1
+    for (int o = 0; o < o1 - o0; ++o) {
+      const uint32_t acc = (uint32_t)(o % S::kAcc), d = tmem + S::kColsA + acc * S::kColsB;
+      wait(smem_u32(&ctrl.empty_acc[acc]), (uint32_t)(o / S::kAcc + 1) & 1u);
+#pragma unroll 1
+      for (int k = 0; k < wide; ++k) {
+        if (masks && k + 1 == wide) {
+          wait(smem_u32(&ctrl.masked[o % (kRing + 1)]), (uint32_t)(o / (kRing + 1)) & 1u);
+        } else {
+          wait(full + slot.at * 8u, slot.parity);
         }
-    };
-    if (kw >= half) each([](float& s, float v) { s = v; });
-    asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
-    if (kw < half) each([](float& s, float v) { s += v; });
-    asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
-    for (int row = warp; row < n; row += kWarps)
-      for (int r = lane; r < blocks * 16; r += 32) {
-        float s = part[row * pitch + r] + part[(kRows + row) * pitch + r];
-        if (half == 4) s += part[(2 * kRows + row) * pitch + r] + part[(3 * kRows + row) * pitch + r];
-        share[row * kMostRank + r] = s;
+        if (!__all_sync(~0u, ok)) break;
+        const int steps = min(4, blocks - k * 4);
+        tc5::tc_fence_after();
+        const uint64_t w = ring_desc + (slot.at * kSlotBytes >> 4), h = x_desc + (uint32_t)(k * (S::kBeside ? 3 : 1) * S::kTileBytes / 16);
+#pragma unroll 1
+        for (int j = S::kBeside ? 0 : last_term; j >= 0; --j) umma(d, w, h + (uint32_t)(j * wide * S::kTileBytes / 16), kB, k > 0 || (!S::kBeside && j < last_term), steps);
+        tc5::umma_commit(&ctrl.empty[slot.at]);
+        slot.next();
       }
+      if (!__all_sync(~0u, ok)) break;
+      tc5::umma_commit(&ctrl.full_acc[acc]);
+    }
+  } else if (warp > S::kWorkers + 1) {
+    if (!settle()) return;
+    // ---- masks, each of two warps for every second tile of B: no more tiles ahead of the products than the ring has slots
+    // two warps that have nothing to do yet have y's rows fetched to the second-level cache, which are read when all else is done, and those of x
+    auto fetch = [](const void* base, long long at, int elements, int size) {
+      if (elements > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(base) + at * size), "r"(elements * size) : "memory");
+    };
+    for (int r = lane; r < n; r += 32) {
+      const int columns = min((k0 + np) * 64, a.ic) - k0 * 64;
+      if (warp == S::kWorkers + 3) fetch(a.x, (long long)row_of(r) * a.x_row + k0 * 64, columns, (int)sizeof(X));
+      if (warp == S::kWorkers + 3 && a.x_prev) fetch(a.x_prev, (long long)row_of(r) * a.x_prev_row + k0 * 64, columns, (int)sizeof(X));
+      if (warp == S::kWorkers + 2) fetch(a.y, (long long)row_of(r) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (masks)
+#pragma unroll 1
+      for (int o = warp - S::kWorkers - 2; o < o1 - o0; o += 2) {
+        const int i = n_a + o * wide + wide - 1, tail = rank - (wide - 1) * 64;
+        uint8_t* const weights = smem + i % kRing * kSlotBytes;
+        wait(full + (uint32_t)(i % kRing) * 8u, (uint32_t)(i / kRing) & 1u);
+        if (!__all_sync(~0u, ok)) break;
+        uint4 v[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[h][r] = *reinterpret_cast<const uint4*>(weights + swizzled(r * 32 + lane, min(tail / 8 + h, 7)));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int e = tail / 8 + h, keep = max(tail - e * 8, 0);
+          auto of = [keep](int j) { return keep >= 2 * j + 2 ? ~0u : keep == 2 * j + 1 ? 0xFFFFu : 0u; };
+          if (e * 8 >= (tail + 15) / 16 * 16) continue;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            *reinterpret_cast<uint4*>(weights + swizzled(r * 32 + lane, e)) = make_uint4(v[h][r].x & of(0), v[h][r].y & of(1), v[h][r].z & of(2), v[h][r].w & of(3));
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) tc5::mbar_arrive(&ctrl.masked[o % (kRing + 1)]);
+      }
+  } else {
+    if (!p.x_by_map && np > 0 && n > 0) stage();
+    if (!settle()) return;
+    // ---- this block's share of A x: lanes are the rank
+    constexpr int kCols = NT * 4 / S::kWorkers;
+    const int quarter = warp & 3, col0 = (warp >> 2) * kCols;
+    wait(smem_u32(&ctrl.a_done), 0);
+    tc5::tc_fence_after();
+    const uint32_t lanes = *static_cast<volatile uint32_t*>(&ctrl.tmem_base) + ((uint32_t)quarter << 21);
+    if (quarter * 32 < blocks * 16) {
+      float sum[kCols];
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) sum[j] = 0.f;
+      if (np > 0)
+#pragma unroll
+        for (int k = (S::kBeside ? F::kX : 1) - 1; k >= 0; --k) {
+          uint32_t v[kCols];
+          tmem_ld<kCols>(lanes + (uint32_t)(k * NT + col0), v);
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) sum[j] += __uint_as_float(v[j]);
+        }
+      if constexpr (F::kScaled) {
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) {
+          float by, back;
+          powers_of(ctrl.top[col0 + j], by, back);
+          sum[j] *= back;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kCols; ++j)
+        if (col0 + j < n) share[(col0 + j) * kMostRank + quarter * 32 + lane] = sum[j];
+    }
+    tc5::tc_fence_before();
     cluster.sync();
 
-    // ---- all of A x, as operands
-    const int last_term = a.y_dtype == RWKVQ_F32 ? 2 : 1;
+    // ---- A x: each block adds up a share of the rows, and gives them to all as operands.  As many lanes to a row as there are fours of the rank
     const float scale = t.scale;
-    for (int row = warp; row < n; row += kWarps)
+    auto add_up = [&](auto blocks_of_cluster) {
+      constexpr int kC = decltype(blocks_of_cluster)::value;
+      const int wl = blocks == 1 ? 4 : blocks == 2 ? 8 : blocks <= 4 ? 16 : 32, r4 = lane % wl * 4, row1 = n * (c + 1) / kC;
 #pragma unroll 1
-      for (int r = lane; r < blocks * 16; r += 32) {
-        float s = 0.f;
-        if (r < rank) {
-          float v[8];
+      for (int row0 = n * c / kC + warp * (32 / wl); row0 < row1; row0 += S::kWorkers * (32 / wl)) {
+        const int row = row0 + lane / wl;
+        const bool there = row < row1 && r4 < blocks * 16;
+        float h[4] = {0.f, 0.f, 0.f, 0.f};
+        float4 s[kC];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = k < C ? cluster.map_shared_rank(share, k)[row * kMostRank + r] : 0.f;
+        for (int k = 0; k < kC; ++k) s[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(share, k) + min(row, n - 1) * kMostRank + r4);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) s += v[k];
-          s *= scale;
-        }
-        uint8_t* const to = xs + r / 64 * kXPiece + swizzled(row, r / 8 & 7) + (r & 7) * 2;
-        *reinterpret_cast<__nv_bfloat16*>(to) = term(s);
-        *reinterpret_cast<__nv_bfloat16*>(to + 2 * kXPiece) = last_term == 1 ? __float2bfloat16_rn(s) : term(s);
-        if (last_term == 2) *reinterpret_cast<__nv_bfloat16*>(to + 4 * kXPiece) = term(s);
-      }
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
-
-    // ---- B (A x) for this block's rows of B, sixteen of a tile's for each warp
-    i = n_a;
-    for (int o = o0; o < o1; ++o) {
-      float d[2][4] = {};
-      for (int k = 0; k < wide; ++k, ++i) {
-        take(i);
-        const uint32_t slot = ring + (uint32_t)(i % S::kSlots * kSlotBytes + warp * 2048);
-        const int steps = min(4, blocks - k * 4);
-        if (ok)
-#pragma unroll 1
-          for (int s = 0; s < steps; ++s) {
-            uint32_t x[3][4], w[1][4];
-            ldmatrix4(w[0], slot + swizzled(lane & 15, s * 2 + (lane >> 4)));
-            const uint32_t at_x = x_at + (uint32_t)(k * kXPiece) + (uint32_t)(((s * 2 + (lane >> 3 & 1)) ^ lane) & 7) * 16u;
+        for (int k = 0; k < kC; ++k) { h[0] += s[k].x; h[1] += s[k].y; h[2] += s[k].z; h[3] += s[k].w; }
 #pragma unroll
-            for (int j = 0; j < 3; ++j)
-              if (j <= last_term) ldmatrix4(x[j], at_x + (uint32_t)j * (2 * kXPiece));
-            const int left = rank - (k * 64 + s * 16);
-            if (left < 16) {        // what lies behind the adapter's rank may be anything
-              const uint32_t lo = q * 2 + 2 <= left ? ~0u : q * 2 + 1 <= left ? 0xFFFFu : 0u, hi = q * 2 + 10 <= left ? ~0u : q * 2 + 9 <= left ? 0xFFFFu : 0u;
-              w[0][0] &= lo; w[0][1] &= lo; w[0][2] &= hi; w[0][3] &= hi;
-            }
-            multiply<3>(d, w[0], x, last_term + 1, both);
+        for (int j = 0; j < 4; ++j) h[j] = r4 + j < rank ? h[j] * scale : 0.f;
+        uint8_t* const to = xs + r4 / 64 * (S::kBeside ? 3 : 1) * S::kTileBytes + swizzled(row, r4 / 8 & 7) + (r4 & 4) * 2;
+        const int next = (S::kBeside ? 1 : wide) * S::kTileBytes;
+        uint2 terms[3];
+        float back = 1.f;
+        if constexpr (kHalf) {
+          float top = fmaxf(fmaxf(fabsf(h[0]), fabsf(h[1])), fmaxf(fabsf(h[2]), fabsf(h[3])));
+          for (int o = 1; o < wl; o *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+          // 2^up brings the largest number to 2^14; an infinity or NaN stays what it is
+          const int up = top > 0.f && top < INFINITY ? max(min(14 - ilogbf(top), 126), -126) : 0;
+          const float by = __uint_as_float((uint32_t)(127 + up) << 23);
+          back = __uint_as_float((uint32_t)(127 - up) << 23);
+          __half hi[4], lo[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float x = h[j] * by;
+            hi[j] = __float2half_rn(x);
+            lo[j] = fabsf(x) < INFINITY ? __float2half_rn(x - __half2float(hi[j])) : __float2half_rn(0.f);
           }
-        give(i);
+          terms[0] = make_uint2(pair_bits(hi[0], hi[1]), pair_bits(hi[2], hi[3]));
+          terms[1] = make_uint2(pair_bits(lo[0], lo[1]), pair_bits(lo[2], lo[3]));
+        } else {
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            __nv_bfloat16 b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = k == 1 && last_term == 1 ? __float2bfloat16_rn(h[j]) : term(h[j]);
+            terms[k] = make_uint2(pair_bits(b[0], b[1]), pair_bits(b[2], b[3]));
+          }
+        }
+        if (there)
+#pragma unroll
+          for (int k = 0; k < kC; ++k) {
+            uint8_t* const there_to = cluster.map_shared_rank(to, k);
+            *reinterpret_cast<uint2*>(there_to) = terms[0];
+            *reinterpret_cast<uint2*>(there_to + next) = terms[1];
+            if (!kHalf && last_term == 2) *reinterpret_cast<uint2*>(there_to + 2 * next) = terms[2];
+            if (kHalf && r4 == 0) *cluster.map_shared_rank(&ctrl.back[row], k) = back;
+          }
       }
-      if (!ok) break;
-      // y: all that is read first, then the sums
-      const int col = o * 128 + warp * 16 + g;
-      auto y_at = [&](int b, int e) { const int r = b * 8 + q * 2 + (e & 1); return (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row + col + (e >> 1) * 8; };
-      auto there = [&](int b, int e) { return b * 8 + q * 2 + (e & 1) < n && col + (e >> 1) * 8 < a.oc; };
-      if (a.y_dtype == RWKVQ_F32) {
-        // Each element of y is added to once in a call, so that a reduction in memory is as good as a load, an addition and a store, and nothing waits for it (it
-        // takes subnormal numbers for zeros).
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (there(b, e)) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(static_cast<float*>(a.y) + y_at(b, e)), "f"(d[b][e]) : "memory");
-      } else {
-        unsigned short* const y = static_cast<unsigned short*>(a.y);
-        unsigned short old[2][4];
-        const long long y_at_first = (long long)(grouped ? t.rows[0] : t.first) * a.y_row;        // somewhere valid
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) old[b][e] = y[there(b, e) ? y_at(b, e) : y_at_first];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (there(b, e))
-              y[y_at(b, e)] = a.y_dtype == RWKVQ_F16 ? __half_as_ushort(__float2half_rn(__half2float(__ushort_as_half(old[b][e])) + d[b][e]))
-                                                     : __bfloat16_as_ushort(__float2bfloat16_rn(__bfloat162float(__ushort_as_bfloat16(old[b][e])) + d[b][e]));
-      }
-    }
+    };
+    if (C == 8) add_up(std::integral_constant<int, 8>());
+    else if (C == 4) add_up(std::integral_constant<int, 4>());
+    else if (C == 2) add_up(std::integral_constant<int, 2>());
+    else add_up(std::integral_constant<int, 1>());
+    asm volatile("fence.proxy.async;" ::: "memory");
+    // the second meeting, behind which no block touches another's memory
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+
+    // ---- y: 32 columns of it for a warp, and half of the tile's rows.  A lane of the accumulator is a column; the way to four neighbouring columns a lane is through
+    // shared memory, where the shares were.
+    if (a.y_dtype == RWKVQ_F32) store_y<S, float, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
+    else if (a.y_dtype == RWKVQ_F16) store_y<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
+    else store_y<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
   }
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // no block ends while another reads its share
+  if (warp == S::kWorkers || warp > S::kWorkers + 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  tc5::tc_fence_before();
   __syncthreads();
-  // a block that gave up leaves when its copies have arrived
-  if (ctrl.abort_flag && tid == 0)
-    for (int i = max(0, ctrl.asked - S::kSlots); i < ctrl.asked; ++i)
-      for (uint32_t k = 0; k < tc5::kPollLimit && !tc5::mbar_try_wait(full + (uint32_t)(i % S::kSlots) * 8u, (uint32_t)(i / S::kSlots) & 1u); ++k) {}
+  tc5::tc_fence_after();
+  if (ctrl.abort_flag) {
+    // a block that gave up leaves when its copies have arrived and the tensor core is done
+    auto arrived = [](uint32_t bar, uint32_t parity) {
+      for (uint32_t k = 0; k < tc5::kPollLimit && !tc5::mbar_try_wait(bar, parity); ++k) {}
+    };
+    if (tid == 0) {
+      for (int i = max(0, ctrl.asked - kRing); i < ctrl.asked; ++i) arrived(full + (uint32_t)(i % kRing) * 8u, (uint32_t)(i / kRing) & 1u);
+      for (int i = max(0, ctrl.x_asked - S::kGroups); i < ctrl.x_asked; ++i) arrived(xfull + (uint32_t)(i % S::kGroups) * 8u, (uint32_t)(i / S::kGroups) & 1u);
+    }
+    if (warp == S::kWorkers + 1) {
+      tc5::umma_commit(&ctrl.drained);
+      arrived(smem_u32(&ctrl.drained), 0);
+    }
+    __syncthreads();
+  }
+  if (warp == S::kWorkers + 1) tc5::tmem_dealloc(ctrl.tmem_base, S::kTmemCols);
 }
 
-template <typename X>
-cudaError_t launch(Args& p, long long items, cudaStream_t s) {
-  using S = Shape<X>;
-  const rwkvq_lowrank_args& a = p.a;
-  if (!encode(p.A, a.A, true, a.ic, a.rank, a.n_adapters, 16) || !encode(&p.B, a.B, true, a.rank, a.oc, a.n_adapters, 128)) return cudaErrorUnknown;
-  static SmemOptIn opt_in(kCarveOut);
-  cudaError_t e = opt_in((const void*)lowrank_kernel<X>, S::kBytes);
-  if (e != cudaSuccess) return e;
-  // blocks that are there at once, two an SM: clusters as wide as that allows
-  unsigned C = 8;
-  while (C > 1 && items * C > 2ll * sm_count()) C /= 2;
-  // where there are few tiles, several clusters divide a tile's rows of B, and each multiplies A x for itself
-  p.splits = (int)std::max<long long>(1, std::min<long long>({2ll * sm_count() / (items * C), (a.oc + 128ll * C - 1) / (128 * C), 16}));
+// Clusters of C blocks that are on the device at once; asked for once per device (the kernels are alike in this: one block an SM).
+long long clusters_at_once(const void* kernel, unsigned C) {
+  static std::atomic<int> known[kMaxDevices][4];
+  const int dev = current_device(), h = C == 8 ? 3 : C == 4 ? 2 : C == 2 ? 1 : 0;
+  int n = dev >= 0 ? known[dev][h].load(std::memory_order_relaxed) : 0;
+  if (n > 0) return n;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(kAll); cfg.dynamicSmemBytes = S::kBytes; cfg.stream = s;
+  cfg.gridDim = dim3(C); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmemBytes;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) { cudaGetLastError(); return std::max(1u, sm_count() * 3 / 4 / C); }
+  if (dev >= 0) known[dev][h].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+template <typename X, typename W, int NT>
+cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
+  using S = TileShape<X, W, NT>;
+  const rwkvq_lowrank_args& a = p.a;
+  const bool half = a.w_dtype == RWKVQ_F16;
+  const tc5::EncodeTiledFn fn = tc5::encode_tiled();
+  if (!fn || !encode(&p.B, a.B, half, a.rank, a.oc, a.n_adapters, 128)) return cudaErrorUnknown;
+  // Where columns are whole pieces of 64, a box has several of them one behind the other, as many as a slot holds of so many rows; else one.  Boxes for every sixteen of the rank
+  // that an adapter may have.
+  p.whole = a.ic % 64 == 0;
+  const CUtensorMapDataType type = half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  auto map = [&](CUtensorMap* m, const void* at, cuuint64_t rows, cuuint64_t row, cuuint64_t n, cuuint32_t box_rows, cuuint32_t box_pieces) {
+    const cuuint64_t pieces = (cuuint64_t)a.ic / 64, dims4[4] = {64, rows, pieces, n}, strides4[3] = {row * 2, 128, row * 2 * rows};
+    const cuuint64_t dims3[3] = {(cuuint64_t)a.ic, rows, n}, strides3[2] = {row * 2, row * 2 * rows};
+    const cuuint32_t box4[4] = {64, box_rows, box_pieces, 1}, box3[3] = {64, box_rows, 1}, step[4] = {1, 1, 1, 1};
+    return fn(m, type, p.whole ? 4 : 3, const_cast<void*>(at), p.whole ? dims4 : dims3, p.whole ? strides4 : strides3, p.whole ? box4 : box3, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  const int most = (a.rank + 15) / 16;
+  for (int blocks = a.ranks ? 1 : most; blocks <= most; ++blocks)
+    if (!map(&p.A[blocks - 1], a.A, (cuuint64_t)a.rank, (cuuint64_t)a.ic, (cuuint64_t)a.n_adapters, 16u * (cuuint32_t)blocks, (cuuint32_t)pieces_of(blocks))) return cudaErrorUnknown;
+  p.x_by_map = !p.mu && std::is_same<X, W>::value && !(NT == kRows && single_rows(a));
+  if (p.x_by_map) {
+    const cuuint64_t row = (cuuint64_t)(a.tokens > 1 ? a.x_row : a.ic);
+    const cuuint64_t dims[3] = {p.whole ? 64 : (cuuint64_t)a.ic, (cuuint64_t)a.tokens, p.whole ? (cuuint64_t)a.ic / 64 : 1}, strides[2] = {row * 2, p.whole ? 128 : row * 2};
+    const cuuint32_t box[3] = {64, NT, p.whole ? (cuuint32_t)S::kGroup : 1}, step[3] = {1, 1, 1};
+    if (fn(&p.X, type, 3, const_cast<void*>(a.x), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return cudaErrorUnknown;
+  }
+  static SmemOptIn opt_in(kCarveOut);
+  const cudaError_t e = opt_in((const void*)lowrank_tile_kernel<X, W, NT>, kSmemBytes);
+  if (e != cudaSuccess) return e;
+  // One block an SM: clusters as wide as are there at once, then several that divide a tile's rows of B and each multiply A x for themselves.  Wide clusters leave SMs over
+  // (132 of 148 can be in clusters of four, 120 in clusters of eight: what is behind them starts when all is done).
+  unsigned C = 8;
+  while (C > 1 && items > clusters_at_once((const void*)lowrank_tile_kernel<X, W, NT>, C)) C /= 2;
+  p.splits = (int)std::max<long long>(1, std::min<long long>({clusters_at_once((const void*)lowrank_tile_kernel<X, W, NT>, C) / items, (a.oc + 128ll * C - 1) / (128 * C), 16}));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(S::kAll); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, lowrank_kernel<X>, p);
+  return cudaLaunchKernelEx(&cfg, lowrank_tile_kernel<X, W, NT>, p);
 }
-cudaError_t launch(Args& p, cudaStream_t s) {
-  if (tiles_take(p.a.x_dtype, p.a.w_dtype)) return launch_tiles(p, s);
-  const long long items = most_tiles(p.a, kRows);
-  return p.a.x_dtype == RWKVQ_F32 ? launch<float>(p, items, s) : launch<__nv_bfloat16>(p, items, s);
+template <typename X, typename W>
+cudaError_t launch_form(Args& p, cudaStream_t s) {
+  const rwkvq_lowrank_args& a = p.a;
+  // tiles of 64 rows where sequences have half of that and more on average
+  if (!single_rows(a) && a.tokens >= 32ll * a.n_seq) return launch_tile<X, W, 64>(p, most_tiles(a, 64), s);
+  return launch_tile<X, W, kRows>(p, most_tiles(a, kRows), s);
+}
+
+template <typename W>
+cudaError_t launch_x(Args& p, cudaStream_t s) {
+  return p.a.x_dtype == RWKVQ_F32 ? launch_form<float, W>(p, s) : p.a.x_dtype == RWKVQ_F16 ? launch_form<__half, W>(p, s) : launch_form<__nv_bfloat16, W>(p, s);
 }
 
 int bytes_of(int dtype) { return dtype == RWKVQ_F32 ? 4 : dtype == RWKVQ_F16 || dtype == RWKVQ_BF16 ? 2 : 0; }
@@ -382,7 +782,8 @@ rwkvq_status rwkvq_lowrank(const rwkvq_lowrank_args* args, const rwkvq_desc* mu_
   }
   p.status = device_status_ptr();
   if (!p.status) return RWKVQ_ECUDA;
-  return cuda_status(lr::launch(p, static_cast<cudaStream_t>(stream)));
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return cuda_status(a.w_dtype == RWKVQ_F16 ? lr::launch_x<__half>(p, s) : lr::launch_x<__nv_bfloat16>(p, s));
 }
 
 }  // extern "C"

@@ -214,11 +214,18 @@ __device__ __forceinline__ __nv_bfloat16 term(float& x) {
   return __ushort_as_bfloat16((unsigned short)(__float_as_uint(hi) >> 16));
 }
 
-// How x goes into the tensor cores: as it is, or in bf16 terms.
+// How x goes into the tensor cores: as it is, in as many bf16 terms as its bits take, or, beside f16 weights, in f16 terms under a power of two that brings the largest number of
+// a row (of those that a block has) to 2^14: bf16 in one and f32 in two, off by up to 2^-24 of it, or 2^-39 of the row's largest.
 template <typename X, typename W> struct Form {
-  static constexpr bool kHalf = std::is_same<X, __half>::value && std::is_same<W, __half>::value;
-  static constexpr int kX = kHalf || std::is_same<X, __nv_bfloat16>::value ? 1 : std::is_same<X, float>::value ? 3 : 2;
+  static constexpr bool kHalf = std::is_same<W, __half>::value, kScaled = kHalf && !std::is_same<X, __half>::value;
+  static constexpr int kX = std::is_same<X, W>::value ? 1 : kHalf ? (std::is_same<X, float>::value ? 2 : 1) : std::is_same<X, float>::value ? 3 : std::is_same<X, __half>::value ? 2 : 1;
 };
+// The power of two that brings a row's largest finite number, whose bits these are, to 2^14, and the one that takes it back.
+__device__ __forceinline__ void powers_of(int top, float& by, float& back) {
+  const int up = top ? max(min(141 - (top >> 23), 126), -126) : 0;
+  by = __uint_as_float((uint32_t)(127 + up) << 23);
+  back = __uint_as_float((uint32_t)(127 - up) << 23);
+}
 
 // Byte offset of 16 bytes (eight columns) in rows of 128 bytes under the 128-byte swizzle.
 __device__ __forceinline__ uint32_t swizzled(int row, int eight) { return (uint32_t)(row * 128 + ((eight ^ row) & 7) * 16); }
@@ -258,9 +265,10 @@ __device__ __forceinline__ Eights<X> load_eights(const Args& p, const RowOf<X>& 
   col = min(col, p.a.ic - 8);
 #pragma unroll
   for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.x[i] = reinterpret_cast<const uint4*>(r.x + col)[i];
-  if constexpr (kMix)
+  if constexpr (kMix) {
 #pragma unroll
     for (int i = 0; i < (int)sizeof(X) / 2; ++i) e.before[i] = reinterpret_cast<const uint4*>(r.before + col)[i];
+  }
   return e;
 }
 // Their indices of the token-shift vector: four are 4 * mu_bits neighbouring bits from a byte's beginning; behind the indices lies the codebook.
@@ -306,45 +314,64 @@ __device__ __forceinline__ uint32_t cut_off(float2& f) {
 }
 __device__ __forceinline__ float2 mixed(float2 x, float2 y, float2 m) { return make_float2(fmaf(y.x - x.x, m.x, x.x), fmaf(y.y - x.y, m.y, x.y)); }
 
-// x_mix of eight columns, rounded to X, as operands of the tensor cores: F::kX terms, `next` bytes from one to the next; zeros behind the last column.  (What the first terms leave of
-// an infinity is NaN.)
-template <typename X, typename F, bool kMix>
-__device__ __forceinline__ void put_eights(const Eights<X>& e, const float2 (&m)[4], uint8_t* to, uint32_t next) {
+// x_mix of eight columns, rounded to X; zeros behind the last column.
+template <typename X, bool kMix>
+__device__ __forceinline__ void mix_eights(const Eights<X>& e, const float2 (&m)[4], float2 (&f)[4]) {
   auto counts = [](const uint4& w, bool yes) { return make_uint4(yes ? w.x : 0u, yes ? w.y : 0u, yes ? w.z : 0u, yes ? w.w : 0u); };
-  uint32_t out[3][4];
   if constexpr (sizeof(X) == 2) {
     const uint4 x4 = counts(e.x[0], e.there);
-    uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+    const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = pair_of(x[j], X());
     if constexpr (kMix) {
       const uint4 y4 = counts(e.before[0], e.there && e.has_before);
       const uint32_t y[4] = {y4.x, y4.y, y4.z, y4.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = rounded(mixed(pair_of(x[j], X()), pair_of(y[j], X()), m[j]), X());
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      out[0][j] = x[j];
-      if constexpr (F::kX == 2) {
-        float2 f = pair_of(x[j], X());
-        out[0][j] = cut_off(f);
-        out[1][j] = rounded(f, __nv_bfloat16());
-      }
+      for (int j = 0; j < 4; ++j) f[j] = pair_of(rounded(mixed(f[j], pair_of(y[j], X()), m[j]), X()), X());
     }
   } else {
     const uint4 a4 = counts(e.x[0], e.there), b4 = counts(e.x[1], e.there);
-    const uint32_t x[8] = {a4.x, a4.y, a4.z, a4.w, b4.x, b4.y, b4.z, b4.w};
-    uint32_t y[8] = {};
+    f[0] = make_float2(__uint_as_float(a4.x), __uint_as_float(a4.y)); f[1] = make_float2(__uint_as_float(a4.z), __uint_as_float(a4.w));
+    f[2] = make_float2(__uint_as_float(b4.x), __uint_as_float(b4.y)); f[3] = make_float2(__uint_as_float(b4.z), __uint_as_float(b4.w));
     if constexpr (kMix) {
       const uint4 c4 = counts(e.before[0], e.there && e.has_before), d4 = counts(e.before[1], e.there && e.has_before);
-      y[0] = c4.x; y[1] = c4.y; y[2] = c4.z; y[3] = c4.w; y[4] = d4.x; y[5] = d4.y; y[6] = d4.z; y[7] = d4.w;
-    }
+      const float y[8] = {__uint_as_float(c4.x), __uint_as_float(c4.y), __uint_as_float(c4.z), __uint_as_float(c4.w), __uint_as_float(d4.x), __uint_as_float(d4.y), __uint_as_float(d4.z),
+                          __uint_as_float(d4.w)};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float2 f = make_float2(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
-      if constexpr (kMix) f = mixed(f, make_float2(__uint_as_float(y[2 * j]), __uint_as_float(y[2 * j + 1])), m[j]);
-      out[0][j] = cut_off(f);
-      out[1][j] = cut_off(f);
-      out[2][j] = rounded(f, __nv_bfloat16());
+      for (int j = 0; j < 4; ++j) f[j] = mixed(f[j], make_float2(y[2 * j], y[2 * j + 1]), m[j]);
+    }
+  }
+}
+// Bits of the largest finite number among them.
+__device__ __forceinline__ int top_of(const float2 (&f)[4]) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float x = fabsf(f[j].x), y = fabsf(f[j].y);
+    top = fmaxf(top, fmaxf(x < INFINITY ? x : 0.f, y < INFINITY ? y : 0.f));
+  }
+  return __float_as_int(top);
+}
+// x_mix of eight columns, rounded to X, as operands of the tensor cores: F::kX terms, `next` bytes from one to the next; `by`: see Form.  (What the first bf16 terms leave of an
+// infinity is NaN.)
+template <typename X, typename F, bool kMix>
+__device__ __forceinline__ void put_eights(const Eights<X>& e, const float2 (&m)[4], uint8_t* to, uint32_t next, float by) {
+  float2 f[4];
+  mix_eights<X, kMix>(e, m, f);
+  uint32_t out[3][4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (F::kScaled) {
+      f[j].x *= by; f[j].y *= by;
+      out[0][j] = rounded(f[j], __half());
+      const float2 hi = pair_of(out[0][j], __half());
+      if constexpr (F::kX == 2) out[1][j] = rounded(make_float2(fabsf(f[j].x) < INFINITY ? f[j].x - hi.x : 0.f, fabsf(f[j].y) < INFINITY ? f[j].y - hi.y : 0.f), __half());
+    } else if constexpr (F::kX == 1) {
+      out[0][j] = rounded(f[j], X());
+    } else {
+#pragma unroll
+      for (int k = 0; k < F::kX - 1; ++k) out[k][j] = cut_off(f[j]);
+      out[F::kX - 1][j] = rounded(f[j], __nv_bfloat16());
     }
   }
 #pragma unroll
@@ -360,10 +387,6 @@ inline bool encode(CUtensorMap* map, const void* at, bool half, int cols, int ro
   return fn(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(at), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-// Tiles on the tcgen05 tensor cores (lowrank_tile.cu): whether they take operands of these types, and a launch (p complete but for maps and clusters).
-bool tiles_take(int x_dtype, int w_dtype);
-cudaError_t launch_tiles(Args& p, cudaStream_t s);
 
 }  // namespace lr
 }  // namespace rwkvq

@@ -185,6 +185,51 @@ def test_a_row_of_infinities_or_nan_is_its_own():
             assert torch.equal(got[keep], clean[keep]) and not torch.isfinite(got[7]).any()
 
 
+@pytest.mark.parametrize("lens", [[1, 2, 1, 5], [70, 33]])
+@pytest.mark.parametrize("x", TYPES)
+def test_an_infinity_beside_f16_weights(x, lens):
+    """The rows of such inputs are brought to a common size by their largest finite number."""
+    for bad in (math.inf, -math.inf, math.nan):
+        c = Case(15, lens, 712, 40, 16, [0] * len(lens), x, "f16")
+        clean = c.call()
+        c.x[7, 300] = bad
+        got = c.call()
+        keep = [i for i in range(c.T) if i != 7]
+        assert torch.equal(got[keep], clean[keep]) and not torch.isfinite(got[7]).any()
+
+
+@pytest.mark.parametrize("lens", [[1] * 30, [5, 1, 12, 12], [30], [100, 64]])
+@pytest.mark.parametrize("x,mix", [("f32", None), ("f32", "rows"), ("bf16", None), ("bf16", "rows"), ("bf16", "first")])
+def test_rows_of_all_sizes_beside_f16_weights(x, mix, lens):
+    """Rows from 2^-100 to 2^100, some with one number far above the others, some all zero."""
+    c = Case(sum(lens), lens, 1032, 72, 40, [i % 2 for i in range(len(lens))], x, "f16", "f32", mix=mix)
+    c.y.zero_()
+    g = torch.Generator().manual_seed(5)
+    size = torch.pow(2.0, torch.randint(-100, 101, (c.T, 1), generator=g).float()) if mix != "first" else torch.full((c.T, 1), 2.0 ** 90)
+    c.x = (c.x.float() * size).to(c.x.dtype)
+    if c.x_prev is not None:
+        c.x_prev = (c.x_prev.float() * size).to(c.x.dtype)
+    c.x[::3, 700] *= 2.0 ** 20
+    c.x[1::4] = 0
+    if c.x_prev is not None:
+        c.x_prev[1::4] = 0
+    got = c.call().double().cpu()
+    ref, tol = c.expected()
+    # beside f16 weights a number is off by up to 2^-39 of the largest of its row, A x by up to 2^-38 of its own
+    most = c.x.double().abs().amax(1, keepdim=True)
+    if c.mu:
+        prev = c.x_prev.double() if c.x_prev is not None else torch.cat([c.xprev0[:1].double(), c.x[:-1].double()]).abs()
+        most = most + (most + prev.abs().amax(1, keepdim=True)) * float(abs(c.mu.w_hat).max())
+    for a, t0, t1 in zip(c.adapter, c.starts(), c.starts()[1:]):
+        A, Bm, k = c.A[a].double().abs(), c.B[a].double().abs(), float(c.scale[a])
+        h = most[t0:t1] * A.sum(1)
+        tol[t0:t1] += k * ((2.0 ** -39 * h + 2.0 ** -38 * h.amax(1, keepdim=True)) @ Bm.T)
+    assert torch.isfinite(got).all()
+    err = (got - ref).abs()
+    assert (err <= tol).all(), f"max err/tol {(err / tol.clamp(min=1e-300)).max().item()}"
+    assert B.rwkvq_device_status() == 0
+
+
 def test_bad_lists_leave_a_sequence_out():
     good = Case(13, [5, 30, 4], 64, 48, 16, [0, 1, 0])
     want, before = good.call().cpu(), good.y
