@@ -231,16 +231,17 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
     fetch(&p.B);
     if (p.x_by_map) fetch(&p.X);
   }
+  // a cluster is 1, 2, 4 or 8 blocks, and at most 128 blocks divide at most 2^17 tiles of B
+  const int logC = 31 - __clz(C), id = (int)(blockIdx.x >> logC), item = (int)((unsigned)id / (unsigned)p.splits), split = id - item * p.splits;
+  const int pieces = (a.ic + 63) / 64, k0 = pieces * c >> logC, np = (pieces * (c + 1) >> logC) - k0;
+  const unsigned tiles = (unsigned)(a.oc + 127) / 128, parts = (unsigned)(C * p.splits), at = (unsigned)(split * C + c);
+  const int o0 = (int)(tiles * at / parts), o1 = (int)(tiles * (at + 1) / parts);
+  const bool grouped = NT == kRows && single_rows(a);
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (p.mu)
-    for (int i = tid; i < p.mu_entries; i += S::kAll) codebook[i] = p.mu_codebook[i];
-  const int id = (int)(blockIdx.x / C), item = id / p.splits, split = id - item * p.splits;
+  // the codebook is on its way while the rows are looked for, and goes to shared memory when x is asked for
+  const uint32_t entry = p.mu && tid < p.mu_entries ? p.mu_codebook[tid] : 0;
   find_rows<NT>(p, item, t, scratch, share);
   const int n = t.n;
-  const bool grouped = NT == kRows && single_rows(a);
-  const int pieces = (a.ic + 63) / 64, k0 = (int)((long long)pieces * c / C), np = (int)((long long)pieces * (c + 1) / C) - k0;
-  const int tiles = (a.oc + 127) / 128, parts = C * p.splits, at = split * C + c;
-  const int o0 = (int)((long long)tiles * at / parts), o1 = (int)((long long)tiles * (at + 1) / parts);
   const uint32_t ring = smem_u32(smem), xring = smem_u32(xs), full = smem_u32(ctrl.full), empty = smem_u32(ctrl.empty), xfull = smem_u32(ctrl.xfull), xempty = smem_u32(ctrl.xempty);
   bool ok = true;
   auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && tc5::mbar_wait(bar, parity, abortp, p.status); };
@@ -285,6 +286,10 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
     };
     load(0, raw[0], words[0]);
     load(1, raw[1], words[1]);
+    if constexpr (kMix) {
+      if (tid < p.mu_entries) codebook[tid] = entry;
+      asm volatile("bar.sync 1, %0;" ::"n"(S::kWork) : "memory");
+    }
     float by[kN];
     if constexpr (F::kScaled) {          // first the largest number of each row: all groups are read twice but the first two
       int top[kN] = {};
@@ -387,11 +392,12 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
       for (int j = 0; j < gx; ++j) wait(xfull + (uint32_t)j * 8u, 0);
       return;
     }
-    // This warp and those behind it bring nothing to the first meeting of the cluster and do not hold it up: what they wait for below comes behind it.
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    // This warp and those behind it bring nothing to the meetings of the cluster, arrive relaxed (with release it took 1000 cycles) and do not hold them up: what they wait for
+    // below comes behind the first.
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const int total = n_a + (o1 - o0) * wide;
     // Nor does this one hold up the second by waits for slots that B had, which are given back behind that.
-    auto second = [] { asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory"); };
+    auto second = [] { asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.relaxed.aligned;" ::: "memory"); };
     bool met = false;
     const CUtensorMap* const a_map = &p.A[blocks - 1];
     const uint32_t a_bytes = (uint32_t)(a_slot * blocks) * 2048u;
@@ -437,7 +443,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
       tc5::tmem_dealloc(tmem, S::kTmemCols);
       return;
     }
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const uint64_t ring_desc = tc5::smem_desc_sw128(ring), x_desc = tc5::smem_desc_sw128(xring);
     constexpr uint32_t kA = idesc_of(F::kHalf, S::kColsA);
     const uint32_t kB = idesc_of(kHalf, S::kBeside ? NT * (last_term + 1) : NT);
@@ -472,7 +478,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
     if (__all_sync(~0u, ok)) tc5::umma_commit(&ctrl.a_done);
     // the second meeting: A x is there, from all blocks
     __syncwarp();
-    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.relaxed.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     asm volatile("fence.proxy.async;" ::: "memory");
 #pragma unroll 1
     for (int o = 0; o < o1 - o0; ++o) {
@@ -510,7 +516,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
       if (warp == S::kWorkers + 3 && a.x_prev) fetch(a.x_prev, (long long)row_of(r) * a.x_prev_row + k0 * 64, columns, (int)sizeof(X));
       if (warp == S::kWorkers + 2) fetch(a.y, (long long)row_of(r) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
     }
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\nbarrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     if (masks)
 #pragma unroll 1
       for (int o = warp - S::kWorkers - 2; o < o1 - o0; o += 2) {
