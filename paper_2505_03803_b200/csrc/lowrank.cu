@@ -383,11 +383,6 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
       }
     };
     if (p.x_by_map && n > 0) ask_x(min(np, S::kGroup * S::kGroups));        // as much as there is room for, whatever the adapter
-    if (lane == 0) {
-      if (!(grouped && by_groups(a))) find_adapter(p, t);
-      tc5::mbar_arrive(&ctrl.ready);
-    }
-    __syncwarp();
     if (!settle()) {
       for (int j = 0; j < gx; ++j) wait(xfull + (uint32_t)j * 8u, 0);
       return;
@@ -504,6 +499,13 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
       tc5::umma_commit(&ctrl.full_acc[acc]);
     }
   } else if (warp > S::kWorkers + 1) {
+    if (warp == S::kWorkers + 2) {          // the adapter is looked up by a warp that has nothing to do yet
+      if (lane == 0) {
+        if (!(grouped && by_groups(a))) find_adapter(p, t);
+        tc5::mbar_arrive(&ctrl.ready);
+      }
+      __syncwarp();
+    }
     if (!settle()) return;
     // ---- masks, each of two warps for every second tile of B: no more tiles ahead of the products than the ring has slots
     // two warps that have nothing to do yet have y's rows fetched to the second-level cache, which are read when all else is done, and those of x
