@@ -22,7 +22,7 @@ namespace lr {
 
 using tc5::smem_u32;
 
-constexpr int kRing = 7, kSlotBytes = 16 << 10, kMostGroups = 4, kMostAcc = 4;
+constexpr int kMostRing = 11, kSlotBytes = 16 << 10, kMostGroups = 4, kMostAcc = 4;
 constexpr int kSmemBytes = 224 << 10;
 
 // Pieces of 64 columns of A that a slot holds where the rank is up to 16 * blocks.
@@ -45,11 +45,13 @@ struct TileShape {
   // The warps that read an accumulator, sixteen of its rows' columns each: a quarter of 64 rows, or all of sixteen, of every second tile.
   static constexpr int kReaders = NT == 64 ? 16 : 4, kReadCols = 16;
   static_assert(kXBytes >= 6 * kTileBytes, "A x takes x's place");
-  static_assert(1024 + kRing * kSlotBytes + kXBytes + kShare + 1024 <= kSmemBytes, "shared memory");
+  // as many slots as there is room for, beside the codebook and what aligning takes
+  static constexpr int kFree = (kSmemBytes - 2048 - kXBytes - kShare) / kSlotBytes, kRing = kFree < kMostRing ? kFree : kMostRing;
+  static_assert(kRing >= 7, "shared memory");
   static_assert(kShare >= 8 * kMostCounted || NT == 64, "room for counting the rows of adapters");
 };
 struct TileCtrl {
-  uint64_t full[kRing], empty[kRing], masked[kRing + 1], ready, xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
+  uint64_t full[kMostRing], empty[kMostRing], masked[kMostRing + 1], ready, xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
   int abort_flag, asked, x_asked;
   uint32_t tmem_base;
   float back[64];                 // of each row: the power of two that its A x was divided by
@@ -206,7 +208,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
   __shared__ Tile t;
   __shared__ TileCtrl ctrl;
   __shared__ int scratch[2 * kWarps + 2];
-  uint8_t* const xs = smem + kRing * kSlotBytes;                         // [slot][term][row][64 columns], then A x: [term][64 of the rank][row][64], or [64 of the rank][term][row][64]
+  uint8_t* const xs = smem + S::kRing * kSlotBytes;                         // [slot][term][row][64 columns], then A x: [term][64 of the rank][row][64], or [64 of the rank][term][row][64]
   float* const share = reinterpret_cast<float*>(xs + S::kXBytes);        // this block's share of A x: [row][rank]
   uint32_t* const codebook = reinterpret_cast<uint32_t*>(share + S::kShare / 4);
   const rwkvq_lowrank_args& a = p.a;
@@ -217,8 +219,8 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
   asm volatile("griddepcontrol.launch_dependents;");
   if (tid < 64) ctrl.top[tid] = 0;
   if (tid == 0) {
-    for (int i = 0; i < kRing; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], 1); }
-    for (int i = 0; i <= kRing; ++i) tc5::mbar_init(&ctrl.masked[i], 1);
+    for (int i = 0; i < S::kRing; ++i) { tc5::mbar_init(&ctrl.full[i], 1); tc5::mbar_init(&ctrl.empty[i], 1); }
+    for (int i = 0; i <= S::kRing; ++i) tc5::mbar_init(&ctrl.masked[i], 1);
     for (int i = 0; i < S::kGroups; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : S::kWorkers); tc5::mbar_init(&ctrl.xempty[i], 1); }
     for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], S::kReaders); }
     tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.ready, 1); tc5::mbar_init(&ctrl.drained, 1);
@@ -364,7 +366,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
   if (warp == S::kWorkers) {
     // ---- copies
     int i = 0, px = 0, gx = 0;
-    Turn<kRing> slot;
+    Turn<S::kRing> slot;
     Turn<S::kGroups> group;
     auto ask_x = [&](int upto) {
 #pragma unroll 1
@@ -399,7 +401,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
 #pragma unroll 1
     for (; i < n_a; ++i) {
       const uint32_t bar = full + slot.at * 8u, dst = ring + slot.at * kSlotBytes;
-      if (i >= kRing) wait(empty + slot.at * 8u, slot.parity ^ 1u);
+      if (i >= S::kRing) wait(empty + slot.at * 8u, slot.parity ^ 1u);
       if (!__all_sync(~0u, ok)) break;
       const int first = i * a_slot, count = p.whole ? a_slot : min(a_slot, np - first);
       if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[slot.at], p.whole ? a_bytes : (uint32_t)(count * blocks) * 2048u);
@@ -413,9 +415,9 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
     }
 #pragma unroll 1
     for (int tile = o0, k = 0; i < total; ++i) {
-      if (i - kRing >= n_a && !met) { second(); met = true; }
+      if (i - S::kRing >= n_a && !met) { second(); met = true; }
       const uint32_t bar = full + slot.at * 8u;
-      if (i >= kRing) wait(empty + slot.at * 8u, slot.parity ^ 1u);
+      if (i >= S::kRing) wait(empty + slot.at * 8u, slot.parity ^ 1u);
       if (!__all_sync(~0u, ok)) break;
       if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.full[slot.at], kSlotBytes);
       __syncwarp();
@@ -442,7 +444,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
     const uint64_t ring_desc = tc5::smem_desc_sw128(ring), x_desc = tc5::smem_desc_sw128(xring);
     constexpr uint32_t kA = idesc_of(F::kHalf, S::kColsA);
     const uint32_t kB = idesc_of(kHalf, S::kBeside ? NT * (last_term + 1) : NT);
-    Turn<kRing> slot;
+    Turn<S::kRing> slot;
     {
       Turn<S::kGroups> group;
       uint32_t in_group = 0;
@@ -482,7 +484,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
 #pragma unroll 1
       for (int k = 0; k < wide; ++k) {
         if (masks && k + 1 == wide) {
-          wait(smem_u32(&ctrl.masked[o % (kRing + 1)]), (uint32_t)(o / (kRing + 1)) & 1u);
+          wait(smem_u32(&ctrl.masked[o % (S::kRing + 1)]), (uint32_t)(o / (S::kRing + 1)) & 1u);
         } else {
           wait(full + slot.at * 8u, slot.parity);
         }
@@ -499,32 +501,38 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
       tc5::umma_commit(&ctrl.full_acc[acc]);
     }
   } else if (warp > S::kWorkers + 1) {
-    if (warp == S::kWorkers + 2) {          // the adapter is looked up by a warp that has nothing to do yet
+    // One of two warps that have nothing to do yet looks up the adapter, the other has x fetched to the second-level cache, ahead of the weights, behind which each load takes
+    // some 5000 cycles; and y's rows, which are read when all else is done, once A x is computed.
+    auto fetch = [](const void* base, long long at, int elements, int size) {
+      if (elements > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(base) + at * size), "r"(elements * size) : "memory");
+    };
+    if (warp == S::kWorkers + 2) {
       if (lane == 0) {
         if (!(grouped && by_groups(a))) find_adapter(p, t);
         tc5::mbar_arrive(&ctrl.ready);
       }
       __syncwarp();
+    } else {
+      const int columns = min((k0 + np) * 64, a.ic) - k0 * 64;
+      for (int r = lane; r < n; r += 32) {
+        fetch(a.x, (long long)row_of(r) * a.x_row + k0 * 64, columns, (int)sizeof(X));
+        if (a.x_prev) fetch(a.x_prev, (long long)row_of(r) * a.x_prev_row + k0 * 64, columns, (int)sizeof(X));
+      }
     }
     if (!settle()) return;
-    // ---- masks, each of two warps for every second tile of B: no more tiles ahead of the products than the ring has slots
-    // two warps that have nothing to do yet have y's rows fetched to the second-level cache, which are read when all else is done, and those of x
-    auto fetch = [](const void* base, long long at, int elements, int size) {
-      if (elements > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(base) + at * size), "r"(elements * size) : "memory");
-    };
-    for (int r = lane; r < n; r += 32) {
-      const int columns = min((k0 + np) * 64, a.ic) - k0 * 64;
-      if (warp == S::kWorkers + 3) fetch(a.x, (long long)row_of(r) * a.x_row + k0 * 64, columns, (int)sizeof(X));
-      if (warp == S::kWorkers + 3 && a.x_prev) fetch(a.x_prev, (long long)row_of(r) * a.x_prev_row + k0 * 64, columns, (int)sizeof(X));
-      if (warp == S::kWorkers + 2) fetch(a.y, (long long)row_of(r) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
+    if (warp == S::kWorkers + 3) {
+      for (int r = lane; r < n; r += 32) fetch(a.y, (long long)row_of(r) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
+      __syncwarp();
     }
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;\nbarrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;\nbarrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    // ---- masks, each of two warps for every second tile of B: no more tiles ahead of the products than the ring has slots
     if (masks)
 #pragma unroll 1
       for (int o = warp - S::kWorkers - 2; o < o1 - o0; o += 2) {
         const int i = n_a + o * wide + wide - 1, tail = rank - (wide - 1) * 64;
-        uint8_t* const weights = smem + i % kRing * kSlotBytes;
-        wait(full + (uint32_t)(i % kRing) * 8u, (uint32_t)(i / kRing) & 1u);
+        uint8_t* const weights = smem + i % S::kRing * kSlotBytes;
+        wait(full + (uint32_t)(i % S::kRing) * 8u, (uint32_t)(i / S::kRing) & 1u);
         if (!__all_sync(~0u, ok)) break;
         uint4 v[2][4];
 #pragma unroll
@@ -542,7 +550,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) tc5::mbar_arrive(&ctrl.masked[o % (kRing + 1)]);
+        if (lane == 0) tc5::mbar_arrive(&ctrl.masked[o % (S::kRing + 1)]);
       }
   } else {
     if (!p.x_by_map && np > 0 && n > 0) stage();
@@ -661,7 +669,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
       for (uint32_t k = 0; k < tc5::kPollLimit && !tc5::mbar_try_wait(bar, parity); ++k) {}
     };
     if (tid == 0) {
-      for (int i = max(0, ctrl.asked - kRing); i < ctrl.asked; ++i) arrived(full + (uint32_t)(i % kRing) * 8u, (uint32_t)(i / kRing) & 1u);
+      for (int i = max(0, ctrl.asked - S::kRing); i < ctrl.asked; ++i) arrived(full + (uint32_t)(i % S::kRing) * 8u, (uint32_t)(i / S::kRing) & 1u);
       for (int i = max(0, ctrl.x_asked - S::kGroups); i < ctrl.x_asked; ++i) arrived(xfull + (uint32_t)(i % S::kGroups) * 8u, (uint32_t)(i / S::kGroups) & 1u);
     }
     if (warp == S::kWorkers + 1) {
