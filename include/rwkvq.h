@@ -502,6 +502,7 @@ rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace_dev, 
  * Products are exact and summed in fp32, in a fixed order.  bf16 weights: A x goes on in two parts of eight bits where y has 16 bits (off by up to 2^-16 of it), three (all of it)
  * where y has 32.  f16 weights: x of another type is rounded to 24 bits or 2^-39 of the largest of its row, A x to 22 bits or 2^-38 of its largest.  An infinity or NaN in x
  * is seen by its own row alone, where an infinity may come out as NaN; infinite weights may come out as NaN.
+ * Subnormal numbers in a y of 32 bits may be taken for zeros.
  * A sequence whose rows do not exist or that begins in front of any entry of seq_start before its own, whose adapter does not exist, or whose adapter's rank is not in range: it is left out, the others are computed, and
  * rwkvq_device_status reports EINVAL.
  * Pointers (lists, ranks, scale: 4 bytes) and rows 16-byte aligned; y overlaps no input.  Asynchronous on `stream`, no workspace.

@@ -111,90 +111,141 @@ __device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const CUtensorMap*
 __device__ __forceinline__ uint32_t pair_bits(__nv_bfloat16 x, __nv_bfloat16 y) { return (uint32_t)__bfloat16_as_ushort(x) | (uint32_t)__bfloat16_as_ushort(y) << 16; }
 __device__ __forceinline__ uint32_t pair_bits(__half x, __half y) { return (uint32_t)__half_as_ushort(x) | (uint32_t)__half_as_ushort(y) << 16; }
 
-// Four neighbouring numbers of y and as many that are added to them.
-template <typename Y> struct Four { typename std::conditional<sizeof(Y) == 4, uint4, uint2>::type w; };
-template <typename Y>
-__device__ __forceinline__ void add_four(Four<Y>& y, const float4& d) {
-  Y* const v = reinterpret_cast<Y*>(&y.w);
-  v[0] = from_float<Y>(to_float<Y>(v[0]) + d.x); v[1] = from_float<Y>(to_float<Y>(v[1]) + d.y);
-  v[2] = from_float<Y>(to_float<Y>(v[2]) + d.z); v[3] = from_float<Y>(to_float<Y>(v[3]) + d.w);
-}
-// The accumulators of tiles [o0, o1) of B to y, by one of the warps: 32 lanes of a tile, and a quarter of its rows, or all of every second tile's.
-template <typename S, typename Y, bool kScaled>
-__device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, bool grouped, float* share, int last_term, bool& ok) {
-  const rwkvq_lowrank_args& a = p.a;
-  constexpr int kCols = S::kReadCols, kStep = S::kWorkers / S::kReaders;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = warp & 3, quad = lane & 7, r_lane = lane >> 3;
-  const int col0 = kStep == 1 ? (warp >> 2) * kCols : 0, first = kStep == 1 ? 0 : warp >> 2;
-  const int rows = min(n - col0, kCols);             // of this warp, maybe none
-  float* const turn = share + warp * (kMostRank * S::kTileBytes / 128 / S::kWorkers);       // its part of the share's place: 32 columns by kCols rows, or half of them at a time
-  constexpr int kTurn = S::kTileBytes / 128 * kMostRank / S::kWorkers / 32;                 // rows that it holds
-  Y* at[kCols / 4];                                  // rows r_lane, r_lane + 4, ...; those behind the last are read, where there are any at all, as the last
-#pragma unroll
-  for (int i = 0; i < kCols / 4; ++i) {
-    const int r = col0 + max(min(i * 4 + r_lane, rows - 1), -col0);
-    at[i] = static_cast<Y*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row;
+// What a warp has of each accumulator: 32 lanes, neighbouring columns of y, and a quarter of its rows (64), or all of every second tile's (16).
+template <typename S>
+struct Share {
+  static constexpr int kCols = S::kReadCols, kStep = S::kWorkers / S::kReaders;
+  static constexpr int kTurn = S::kTileBytes / 128 * kMostRank / S::kWorkers / 32;          // rows of 32 numbers that its part of the shares' place holds
+  int lane, warp, quarter, col0, first, rows;            // rows: maybe none
+  float* turn;
+  __device__ __forceinline__ Share(int n, float* share) {
+    lane = threadIdx.x & 31; warp = threadIdx.x >> 5; quarter = warp & 3;
+    col0 = kStep == 1 ? (warp >> 2) * kCols : 0; first = kStep == 1 ? 0 : warp >> 2;
+    rows = min(n - col0, kCols);
+    turn = share + warp * (kTurn * 32);
   }
-  // y of the next tiles is on its way while this one's is added to, some 48 to 64 KB an SM (into buffers that take turns, not moved: a move waits for what it moves)
-  constexpr int kDepth = sizeof(Y) == 2 ? 3 : 2;
-  Four<Y> buffers[kDepth][kCols / 4];
-  auto load = [&](int o, Four<Y> (&to)[kCols / 4]) {
-    const int col = min((o0 + o) * 128 + quarter * 32 + quad * 4, a.oc - 4);
-    if (rows > 0 && o < o1 - o0)
-#pragma unroll
-      for (int i = 0; i < kCols / 4; ++i) to[i] = *reinterpret_cast<const Four<Y>*>(at[i] + col);
-  };
-#pragma unroll
-  for (int k = 0; k < kDepth; ++k) load(first + k * kStep, buffers[k]);
-#pragma unroll 1
-  for (int round = first; round < o1 - o0; round += kDepth * kStep)
-#pragma unroll
-  for (int turn_of = 0; turn_of < kDepth; ++turn_of) {
-    const int o = round + turn_of * kStep, acc = o % S::kAcc, col = (o0 + o) * 128 + quarter * 32 + quad * 4;
-    if (o >= o1 - o0) continue;
-    Four<Y> (&y)[kCols / 4] = buffers[turn_of];
+  // The o-th accumulator, added up over its terms, and given back; false where a wait gave up.
+  __device__ __forceinline__ bool take(const Args& p, TileCtrl& ctrl, uint32_t acc0, int o, int last_term, bool& ok, float (&sum)[kCols]) const {
+    const int acc = o % S::kAcc;
     ok = ok && tc5::mbar_wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / S::kAcc) & 1u, &ctrl.abort_flag, p.status);
-    if (!__all_sync(~0u, ok)) return;
+    if (!__all_sync(~0u, ok)) return false;
     tc5::tc_fence_after();
-    float sum[kCols];
     const uint32_t from = acc0 + (uint32_t)(acc * S::kColsB + col0);
-    {
-      uint32_t v[kCols];
-      tmem_ld<kCols>(from, v);
+    uint32_t v[kCols];
+    tmem_ld<kCols>(from, v);
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) sum[j] = __uint_as_float(v[j]);
-      if constexpr (S::kBeside) {
+    for (int j = 0; j < kCols; ++j) sum[j] = __uint_as_float(v[j]);
+    if constexpr (S::kBeside) {
 #pragma unroll 1
-        for (int k = 1; k <= last_term; ++k) {
-          tmem_ld<kCols>(from + (uint32_t)(k * kCols), v);
+      for (int k = 1; k <= last_term; ++k) {
+        tmem_ld<kCols>(from + (uint32_t)(k * kCols), v);
 #pragma unroll
-          for (int j = 0; j < kCols; ++j) sum[j] += __uint_as_float(v[j]);
-        }
+        for (int j = 0; j < kCols; ++j) sum[j] += __uint_as_float(v[j]);
       }
     }
     tc5::tc_fence_before();
     __syncwarp();
     if (lane == 0) tc5::mbar_arrive(&ctrl.empty_acc[acc]);
-    if (rows <= 0) continue;
-    // [row][column], rows of 128 bytes: each lane a column, then each quarter of a warp a row
+    return true;
+  }
+};
+
+// The accumulators of tiles [o0, o1) of B to y of 32 bits: each element is added to once in a call, so that a reduction where y lies is as good as a load, an addition and a store
+// (but for subnormal numbers, which it may take for zeros); 45 us where these took 49 (3001 rows of 4096 columns).
+template <typename S, bool kScaled>
+__device__ __forceinline__ void reduce_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, bool grouped, float* share, int last_term, bool& ok) {
+  const rwkvq_lowrank_args& a = p.a;
+  using H = Share<S>;
+  const H w(n, share);
+#pragma unroll 1
+  for (int o = w.first; o < o1 - o0; o += H::kStep) {
+    float sum[H::kCols];
+    if (!w.take(p, ctrl, acc0, o, last_term, ok, sum)) break;
+    const int col = (o0 + o) * 128 + w.quarter * 32, bytes = min(32, a.oc - col) * 4;
+    if (w.rows <= 0 || bytes <= 0) continue;
 #pragma unroll
-    for (int h = 0; h < kCols / kTurn; ++h) {
-      if (h * kTurn >= rows) continue;
-#pragma unroll
-      for (int j = 0; j < kTurn; ++j) turn[j * 32 + lane] = sum[h * kTurn + j];
+    for (int h = 0; h < H::kCols / H::kTurn; ++h) {
+      if (h * H::kTurn >= w.rows) continue;
+      asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
       __syncwarp();
 #pragma unroll
-      for (int i = 0; i < kTurn / 4; ++i) {
-        const int r = h * kTurn + i * 4 + r_lane;
-        float4 d = *reinterpret_cast<const float4*>(turn + (i * 4 + r_lane) * 32 + quad * 4);
-        if constexpr (kScaled) { const float back = ctrl.back[min(col0 + r, n - 1)]; d.x *= back; d.y *= back; d.z *= back; d.w *= back; }
-        Four<Y>& mine = y[h * kTurn / 4 + i];
-        add_four<Y>(mine, d);
-        if (r < rows && col < a.oc) *reinterpret_cast<Four<Y>*>(at[h * kTurn / 4 + i] + col) = mine;
+      for (int j = 0; j < H::kTurn; ++j) {
+        const float back = kScaled ? ctrl.back[min(w.col0 + h * H::kTurn + j, n - 1)] : 1.f;
+        w.turn[j * 32 + w.lane] = kScaled ? sum[h * H::kTurn + j] * back : sum[h * H::kTurn + j];
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      // a box of sixteen rows, or, where there are fewer or they lie apart, row after row
+      if (p.y_by_map && w.rows == H::kTurn) {
+        asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
+                     " @q cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];\n @q cp.async.bulk.commit_group;\n}"
+                     ::"l"(&p.Y), "r"(col), "r"(t.first + w.col0), "r"(smem_u32(w.turn)) : "memory");
+      } else if (const int r = h * H::kTurn + w.lane; w.lane < H::kTurn && r < w.rows) {
+        float* const to = static_cast<float*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + w.col0 + r) * a.y_row + col;
+        asm volatile("cp.reduce.async.bulk.global.shared::cta.bulk_group.add.f32 [%0], [%1], %2;\ncp.async.bulk.commit_group;"
+                     ::"l"(to), "r"(smem_u32(w.turn + w.lane * 32)), "r"(bytes) : "memory");
+      }
+    }
+  }
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+
+// The same to y of 16 bits, which is rounded once.  A lane of the accumulator is a column; the way to four neighbouring columns a lane is through shared memory, where the shares were
+// (a column a lane, without that, took 32 us where this takes 24: 2048 rows of 4096 columns; what bounds it is the number of accesses).
+template <typename S, typename Y, bool kScaled>
+__device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, bool grouped, float* share, int last_term, bool& ok) {
+  static_assert(sizeof(Y) == 2, "");
+  const rwkvq_lowrank_args& a = p.a;
+  using H = Share<S>;
+  const H w(n, share);
+  const int quad = w.lane & 7, r_lane = w.lane >> 3;
+  Y* at[H::kCols / 4];                                  // rows r_lane, r_lane + 4, ...; those behind the last are read, where there are any at all, as the last
+#pragma unroll
+  for (int i = 0; i < H::kCols / 4; ++i) {
+    const int r = w.col0 + max(min(i * 4 + r_lane, w.rows - 1), -w.col0);
+    at[i] = static_cast<Y*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row;
+  }
+  // y of the next tiles is on its way while this one's is added to, 48 KB an SM (into buffers that take turns, not moved: a move waits for what it moves)
+  constexpr int kDepth = 3;
+  uint2 buffers[kDepth][H::kCols / 4];
+  auto load = [&](int o, uint2 (&to)[H::kCols / 4]) {
+    const int col = min((o0 + o) * 128 + w.quarter * 32 + quad * 4, a.oc - 4);
+    if (w.rows > 0 && o < o1 - o0)
+#pragma unroll
+      for (int i = 0; i < H::kCols / 4; ++i) to[i] = *reinterpret_cast<const uint2*>(at[i] + col);
+  };
+#pragma unroll
+  for (int k = 0; k < kDepth; ++k) load(w.first + k * H::kStep, buffers[k]);
+#pragma unroll 1
+  for (int round = w.first; round < o1 - o0; round += kDepth * H::kStep)
+#pragma unroll
+  for (int turn_of = 0; turn_of < kDepth; ++turn_of) {
+    const int o = round + turn_of * H::kStep, col = (o0 + o) * 128 + w.quarter * 32 + quad * 4;
+    if (o >= o1 - o0) continue;
+    uint2 (&y)[H::kCols / 4] = buffers[turn_of];
+    float sum[H::kCols];
+    if (!w.take(p, ctrl, acc0, o, last_term, ok, sum)) return;
+    if (w.rows <= 0) continue;
+    // [row][column], rows of 128 bytes: each lane a column, then each quarter of a warp a row
+#pragma unroll
+    for (int h = 0; h < H::kCols / H::kTurn; ++h) {
+      if (h * H::kTurn >= w.rows) continue;
+#pragma unroll
+      for (int j = 0; j < H::kTurn; ++j) w.turn[j * 32 + w.lane] = sum[h * H::kTurn + j];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < H::kTurn / 4; ++i) {
+        const int r = h * H::kTurn + i * 4 + r_lane;
+        float4 d = *reinterpret_cast<const float4*>(w.turn + (i * 4 + r_lane) * 32 + quad * 4);
+        if constexpr (kScaled) { const float back = ctrl.back[min(w.col0 + r, n - 1)]; d.x *= back; d.y *= back; d.z *= back; d.w *= back; }
+        uint2& mine = y[h * H::kTurn / 4 + i];
+        const float2 lo = pair_of(mine.x, Y()), hi = pair_of(mine.y, Y());
+        mine = make_uint2(rounded(make_float2(lo.x + d.x, lo.y + d.y), Y()), rounded(make_float2(hi.x + d.z, hi.y + d.w), Y()));
+        if (r < w.rows && col < a.oc) *reinterpret_cast<uint2*>(at[h * H::kTurn / 4 + i] + col) = mine;
       }
       __syncwarp();
     }
-    load(o + kDepth * kStep, y);
+    load(o + kDepth * H::kStep, y);
   }
 }
 
@@ -653,9 +704,8 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
     // the second meeting, behind which no block touches another's memory
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 
-    // ---- y: 32 columns of it for a warp, and half of the tile's rows.  A lane of the accumulator is a column; the way to four neighbouring columns a lane is through
-    // shared memory, where the shares were.
-    if (a.y_dtype == RWKVQ_F32) store_y<S, float, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
+    // ---- y
+    if (a.y_dtype == RWKVQ_F32) reduce_y<S, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
     else if (a.y_dtype == RWKVQ_F16) store_y<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
     else store_y<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
   }
@@ -727,6 +777,15 @@ cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
     if (fn(&p.X, type, 3, const_cast<void*>(a.x), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return cudaErrorUnknown;
+  }
+  p.y_by_map = 0;
+  if (NT == 64 && a.y_dtype == RWKVQ_F32) {
+    const cuuint64_t dims[2] = {(cuuint64_t)a.oc, (cuuint64_t)a.tokens}, strides[1] = {(cuuint64_t)a.y_row * 4};
+    const cuuint32_t box[2] = {32, 16}, step[2] = {1, 1};
+    if (fn(&p.Y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, a.y, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return cudaErrorUnknown;
+    p.y_by_map = 1;
   }
   static SmemOptIn opt_in(kCarveOut);
   const cudaError_t e = opt_in((const void*)lowrank_tile_kernel<X, W, NT>, kSmemBytes);

@@ -26,8 +26,10 @@ struct alignas(64) Args {
   int splits;                    // clusters to a tile
   int* status;
   int x_by_map;                  // x goes to shared memory as it is, through a map
+  int y_by_map;                  // sixteen rows of y, of 32 bits, are added to through a map
   int whole;                     // columns are a multiple of 64: a box holds several pieces of 64 columns
-  CUtensorMap A[8], B, X;        // A: for each sixteen of the rank, as far as it goes, boxes of so many rows; B: 64 columns x 128 rows; X: 64 columns x a tile's rows
+  // A: for each sixteen of the rank, as far as it goes, boxes of so many rows; B: 64 columns x 128 rows; X: 64 columns x a tile's rows; Y: 32 columns x 16 rows
+  CUtensorMap A[8], B, X, Y;
 };
 
 // ---- rows of a tile -----------------------------------------------------------------------------------------
@@ -196,15 +198,6 @@ __device__ __forceinline__ void find_adapter(const Args& p, Tile& t) {
 }
 
 // ---- numbers and operands -----------------------------------------------------------------------------------
-template <typename T> __device__ __forceinline__ float to_float(T x);
-template <> __device__ __forceinline__ float to_float<float>(float x) { return x; }
-template <> __device__ __forceinline__ float to_float<__half>(__half x) { return __half2float(x); }
-template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <typename T> __device__ __forceinline__ T from_float(float x);
-template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
-template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
-template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-
 // The next bf16 term of x, which is left with what the term leaves.  Cut off, not rounded, so that the largest numbers do not become infinite; of an infinity or
 // NaN nothing is left.
 __device__ __forceinline__ __nv_bfloat16 term(float& x) {
