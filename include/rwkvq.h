@@ -562,7 +562,8 @@ rwkvq_status rwkvq_beam_select(const rwkvq_beam_select_args* args, void* workspa
  * A request of which a parent or slot does not exist, or a slot is an earlier entry of the list, too: its states stay as they were, the others are moved,
  * and rwkvq_device_status reports EINVAL.  (ETIMEOUT if a bounded wait ran out.)
  * Parts, their bytes and slot_row are multiples of 16, lists of 4.  Asynchronous on `stream`, no workspace; parts are moved in launches of 128.
- * Errors: EINVAL (parts that overlap, ...), EALIGN, EUNSUPPORTED (more than 64 beams, 2^20 beams in all, RWKVQ_MOST_STATE_PARTS parts, 2^47 bytes), ECUDA.
+ * Errors: EINVAL (parts that overlap, ...), EALIGN, EUNSUPPORTED (more than 64 beams, 2^20 beams in all, 2^20 slots where there is a list of them,
+ * RWKVQ_MOST_STATE_PARTS parts, 2^47 bytes), ECUDA.
  */
 #define RWKVQ_MOST_STATE_PARTS 1024
 typedef struct {

@@ -1,8 +1,11 @@
 // States that follow their beams: state[slot of beam b] = state[slot of b's parent], in place, for every buffer that holds states.
 //
 // Nothing is computed; what has to be read is each slot that some other beam goes on from, once, and what has to be written each slot whose beam changes.
-// A piece of `chunk` bytes of all beams of one request is one thread block's: the sources' pieces are copied to shared memory, all of them, and from
+// A piece of `chunk` bytes of all beams of one request is one warp's, a block of its own: the sources' pieces are copied to shared memory, all of them, and from
 // there to the slots that take them.  Pieces do not meet one another, so nothing is read behind a write of the same call and cycles need no care.
+//
+// HBM bounds it: 215 us, 5.7 TB/s, where four requests of eight beams have 805 MB of states (187 us at the rate of a plain copy).  Blocks take pieces in turn, all of them those of one request before
+// the next one's, as requests differ in how many of their beams move (a range of pieces for each: 225 us).  One request, 17 MB: 7.5 us, of which 3.9 are the bytes'.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -17,7 +20,8 @@ int* device_status_ptr();  // api_misc.cu
 namespace ro {
 
 constexpr int kMostParts = 128, kMostBeams = 64;
-constexpr uint32_t kBuffer = 16 << 10;          // bytes of shared memory for a block's pieces: thirteen blocks an SM
+constexpr uint32_t kBuffer = 16 << 10;          // bytes of shared memory for a block's pieces: thirteen blocks an SM (8 KB and 24 KB: no better; 32 KB: 8.4 where this takes 7.6, one request)
+constexpr int kMostListed = 1 << 20;            // slots, where there is a list of them: a bit each in shared memory
 
 struct Part { uint8_t* base; uint64_t row, bytes; };
 struct Args {
@@ -39,27 +43,30 @@ struct Request {
   int parent[2], slot[2];
   uint64_t sources;
   bool to[2], any;
-  // False (and the status word set) where a parent or slot does not exist or a slot is an earlier entry's, too.
-  __device__ __forceinline__ void take(const Args& a, int r) {
-    const int lane = threadIdx.x & 31, K = a.beams;
-    const long long base = (long long)r * K;
+  // Requests of one block in rising order.  A request moves nothing (and the status word is set) where a parent or slot does not exist or a slot is an earlier entry's, too: `seen` has a
+  // bit for each slot of the entries before `upto`.
+  __device__ __forceinline__ void take(const Args& a, int r, uint32_t* seen, int& upto) {
+    const int lane = threadIdx.x & 31, K = a.beams, base = r * K;
     bool bad = false;
+    if (a.slots)
+      for (; upto < base; upto += 256) {
+        int s[8];
+#pragma unroll
+        for (int h = 0; h < 8; ++h) s[h] = a.slots[min(upto + h * 32 + lane, base - 1)];          // some more than once
+#pragma unroll
+        for (int h = 0; h < 8; ++h)
+          if ((unsigned)s[h] < (unsigned)a.n_slots) atomicOr(seen + (s[h] >> 5), 1u << (s[h] & 31));
+      }
+    upto = base + K;
+    __syncwarp();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int b = lane + 32 * h;
       parent[h] = b < K ? a.parents[base + b] : 0;
-      slot[h] = b < K ? (a.slots ? a.slots[base + b] : (int)(base + b)) : -1;
-      bad |= b < K && ((unsigned)parent[h] >= (unsigned)K || (unsigned)slot[h] >= (unsigned)a.n_slots);
-    }
-    if (a.slots) {
-      for (long long j0 = 0; j0 < base + K; j0 += 32) {
-        const long long j = j0 + lane;
-        const int other = j < base + K ? a.slots[j] : -1;
-        for (int b = 0; b < K; ++b) {
-          const int mine = __shfl_sync(~0u, b < 32 ? slot[0] : slot[1], b & 31);
-          bad |= j < base + b && other == mine;
-        }
-      }
+      slot[h] = b < K ? (a.slots ? a.slots[base + b] : base + b) : -1;
+      const bool there = (unsigned)slot[h] < (unsigned)a.n_slots;
+      bad |= b < K && ((unsigned)parent[h] >= (unsigned)K || !there);
+      if (a.slots && there) bad |= atomicOr(seen + (slot[h] >> 5), 1u << (slot[h] & 31)) >> (slot[h] & 31) & 1;
     }
     bad = __any_sync(~0u, bad);
     if (bad && lane == 0) atomicExch(a.status, (int)RWKVQ_EINVAL);
@@ -87,6 +94,11 @@ __global__ void __launch_bounds__(32) state_reorder_kernel(const __grid_constant
   __syncwarp();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
+  uint32_t* const seen = reinterpret_cast<uint32_t*>(buffer + (size_t)a.chunk * a.beams);
+  if (a.slots)
+    for (int k = lane; k < (a.n_slots + 31) / 32; k += 32) seen[k] = 0;
+  __syncwarp();
+  int upto = 0;
   const long long each = a.first[a.n_parts], all = each * a.requests;
   // One request after the other, by all blocks: requests differ in how many of their beams move.
   long long i = blockIdx.x;
@@ -95,7 +107,7 @@ __global__ void __launch_bounds__(32) state_reorder_kernel(const __grid_constant
   uint32_t parity = 0;
   while (i < all) {
     const int now = (int)(i / each);
-    if (now != r) { r = now; q.take(a, r); }
+    if (now != r) { r = now; q.take(a, r, seen, upto); }
     if (!q.any) { i += ((r + 1ll) * each - i + gridDim.x - 1) / gridDim.x * gridDim.x; continue; }
     const uint32_t c = (uint32_t)(i - r * each);
     int p = 0;
@@ -167,6 +179,7 @@ rwkvq_status rwkvq_state_reorder(const rwkvq_state_part* parts, int n_parts, int
   if (!parts || !parents || n_parts <= 0 || n_slots <= 0 || requests <= 0 || beams <= 0) return RWKVQ_EINVAL;
   if (beams > ro::kMostBeams || n_parts > RWKVQ_MOST_STATE_PARTS || (long long)requests * beams > (1 << 20)) return RWKVQ_EUNSUPPORTED;
   if (!slots && (long long)requests * beams > n_slots) return RWKVQ_EINVAL;
+  if (slots && n_slots > ro::kMostListed) return RWKVQ_EUNSUPPORTED;
   ro::Part all[RWKVQ_MOST_STATE_PARTS];
   const uint32_t chunk = std::min<uint32_t>(ro::kBuffer / (uint32_t)beams / 128 * 128, 8192);
   for (int i = 0; i < n_parts; ++i) {
@@ -181,9 +194,9 @@ rwkvq_status rwkvq_state_reorder(const rwkvq_state_part* parts, int n_parts, int
   a.requests = requests; a.beams = beams; a.n_slots = n_slots; a.chunk = chunk; a.parents = parents; a.slots = slots;
   a.status = device_status_ptr();
   if (!a.status) return RWKVQ_ECUDA;
-  const uint32_t bytes = chunk * (uint32_t)beams;
+  const uint32_t bytes = chunk * (uint32_t)beams + (slots ? ((uint32_t)n_slots + 31) / 32 * 4 : 0);
   static SmemOptIn opt_in(kCarveOut);
-  cudaError_t e = opt_in((const void*)ro::state_reorder_kernel, (int)ro::kBuffer);
+  cudaError_t e = opt_in((const void*)ro::state_reorder_kernel, (int)ro::kBuffer + ro::kMostListed / 8);
   for (int at = 0; e == cudaSuccess && at < n_parts; at += ro::kMostParts) {
     a.n_parts = std::min(n_parts - at, ro::kMostParts);
     a.first[0] = 0;
@@ -191,7 +204,7 @@ rwkvq_status rwkvq_state_reorder(const rwkvq_state_part* parts, int n_parts, int
       a.part[i] = all[at + i];
       a.first[i + 1] = a.first[i] + (uint32_t)((all[at + i].bytes + chunk - 1) / chunk);
     }
-    const long long pieces = (long long)a.first[a.n_parts] * requests, most = (long long)sm_count() * std::min<uint32_t>(32, (224u << 10) / (bytes + 1024));
+    const long long pieces = (long long)a.first[a.n_parts] * requests, most = (long long)sm_count() * std::max<uint32_t>(1, std::min<uint32_t>(32, (224u << 10) / (bytes + 1024)));
     const long long each = (pieces + most - 1) / most;          // as many pieces for every block
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((pieces + each - 1) / each)); cfg.blockDim = dim3(32); cfg.dynamicSmemBytes = bytes; cfg.stream = static_cast<cudaStream_t>(stream);

@@ -314,6 +314,29 @@ def test_bad_entries_leave_a_request_as_it_was():
         run(parents, s, out)
 
 
+@pytest.mark.parametrize("R,K,shape", [(2000, 5, (4,)), (700, 64, (8,)), (40, 33, (2000,)), (16384, 64, (4,))])
+def test_long_lists(R, K, shape):
+    """Slots of an earlier request, far in front, leave a request as it was; all others move."""
+    g = torch.Generator().manual_seed(R)
+    n = R * K + 100
+    slots = torch.randperm(n, generator=g)[:R * K].view(R, K)
+    parents = torch.randint(0, K, (R, K), generator=g)
+    again = torch.randint(1, R, (5,), generator=g).unique().tolist()
+    for r in again:
+        slots[r, r % K] = slots[r // 3, (r * 7) % K]
+    state = torch.randn((n, *shape), generator=g).cuda()
+    if n > 1 << 20:
+        state, slots = state[:1 << 20], slots % (1 << 20)          # some are repeated by that, too
+    want, flat = state.clone(), slots.view(-1)
+    first = torch.full((state.shape[0],), R * K, dtype=torch.int64).scatter_reduce_(0, flat, torch.arange(R * K), "amin")
+    good = (first[flat] == torch.arange(R * K)).view(R, K).all(1)
+    assert not good[again].any() and good.sum() > R // 2
+    want[slots[good].view(-1).cuda()] = state[torch.gather(slots, 1, parents)[good].view(-1).cuda()]
+    B.rwkvq_state_reorder([state], parents.int().cuda(), slots=slots.int().cuda())
+    torch.cuda.synchronize()
+    assert B.rwkvq_device_status() == 1 and torch.equal(state, want)
+
+
 def test_reorder_captured_for_other_parents():
     states = states_of(6, [("f32", (2, 64, 64)), ("f16", (512,))])
     parts = B.make_state_parts(states)

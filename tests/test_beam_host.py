@@ -49,7 +49,7 @@ def reorder(parts, n_slots=4, parents=P, slots=0, requests=1, beams=4, n=None):
 
 @pytest.mark.parametrize("kw,want", [
     (dict(parents=0), EINVAL), (dict(n=0), EINVAL), (dict(n_slots=0), EINVAL), (dict(requests=0), EINVAL), (dict(beams=0), EINVAL), (dict(requests=2), EINVAL), (dict(beams=65, n_slots=65), EUNSUPPORTED),
-    (dict(requests=(1 << 18) + 1, slots=P), EUNSUPPORTED), (dict(parts=[(0, 64, 64)]), EINVAL), (dict(parts=[(P, 64, 0)]), EINVAL), (dict(parts=[(P, 48, 64)]), EINVAL), (dict(parts=[(P + 8, 64, 64)]), EALIGN),
+    (dict(requests=(1 << 18) + 1, slots=P), EUNSUPPORTED), (dict(n_slots=(1 << 20) + 1, slots=P), EUNSUPPORTED), (dict(parts=[(0, 64, 64)]), EINVAL), (dict(parts=[(P, 64, 0)]), EINVAL), (dict(parts=[(P, 48, 64)]), EINVAL), (dict(parts=[(P + 8, 64, 64)]), EALIGN),
     (dict(parts=[(P, 72, 64)]), EALIGN), (dict(parts=[(P, 64, 40)]), EALIGN), (dict(parts=[(P, 1 << 46, 64)]), EUNSUPPORTED), (dict(parts=[(P, 1 << 40, 1 << 40)]), EUNSUPPORTED),
     # the same buffer twice; one that begins in another; layers that lie between one another's slots and overlap; such with another distance
     (dict(parts=[(P, 64, 64), (P, 64, 64)]), EINVAL), (dict(parts=[(P, 64, 64), (P + 240, 64, 64)]), EINVAL), (dict(parts=[(P, 256, 64), (P + 48, 256, 64)]), EINVAL),
