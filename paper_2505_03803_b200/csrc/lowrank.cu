@@ -752,8 +752,16 @@ long long clusters_at_once(const void* kernel, unsigned C) {
   return n;
 }
 
+// One block an SM: clusters as wide as are there at once.  Wide clusters leave SMs over (132 of 148 can be in clusters of four, 120 in clusters of eight: what is behind them starts when
+// all is done).
+unsigned width_of(const void* kernel, long long items) {
+  unsigned C = 8;
+  while (C > 1 && items > clusters_at_once(kernel, C)) C /= 2;
+  return C;
+}
+
 template <typename X, typename W, int NT>
-cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
+cudaError_t launch_tile(Args& p, long long items, unsigned C, cudaStream_t s) {
   using S = TileShape<X, W, NT>;
   const rwkvq_lowrank_args& a = p.a;
   const bool half = a.w_dtype == RWKVQ_F16;
@@ -794,10 +802,7 @@ cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
   static SmemOptIn opt_in(kCarveOut);
   const cudaError_t e = opt_in((const void*)lowrank_tile_kernel<X, W, NT>, kSmemBytes);
   if (e != cudaSuccess) return e;
-  // One block an SM: clusters as wide as are there at once, then several that divide a tile's rows of B and each multiply A x for themselves.  Wide clusters leave SMs over
-  // (132 of 148 can be in clusters of four, 120 in clusters of eight: what is behind them starts when all is done).
-  unsigned C = 8;
-  while (C > 1 && items > clusters_at_once((const void*)lowrank_tile_kernel<X, W, NT>, C)) C /= 2;
+  // where all clusters are as wide as can be and SMs are left, several divide a tile's rows of B and each multiplies A x for itself
   p.splits = (int)std::max<long long>(1, std::min<long long>({clusters_at_once((const void*)lowrank_tile_kernel<X, W, NT>, C) / items, (a.oc + 128ll * C - 1) / (128 * C), 16}));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(S::kAll); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = s;
@@ -812,9 +817,22 @@ cudaError_t launch_tile(Args& p, long long items, cudaStream_t s) {
 template <typename X, typename W>
 cudaError_t launch_form(Args& p, cudaStream_t s) {
   const rwkvq_lowrank_args& a = p.a;
-  // tiles of 64 rows where sequences have half of that and more on average (2048 rows of one: tiles of sixteen took 33 us where 64 took 29; few rows leave most of a wide tile empty)
-  if (!single_rows(a) && a.tokens >= 32ll * a.n_seq) return launch_tile<X, W, 64>(p, most_tiles(a, 64), s);
-  return launch_tile<X, W, kRows>(p, most_tiles(a, kRows), s);
+  if (single_rows(a)) {
+    const long long items = most_tiles(a, kRows);
+    return launch_tile<X, W, kRows>(p, items, width_of((const void*)lowrank_tile_kernel<X, W, kRows>, items), s);
+  }
+  // A tile takes its time by the width of its cluster, and one of 64 rows some 1.4 times that of one of sixteen (4096 x 4096, us, sixteen / 64: prompts of 203 rows 10.0 / 11.4, 448 13.7 / 11.8, 2048
+  // 42 / 23; f16 and rank 128, forty sequences of ten rows 29 / 42, sixty 51 / 40, 96 52 / 73), so that the wider tiles are taken where they leave room for wider clusters, or for fewer rounds.
+  struct Plan { long long items; unsigned C; double cost; };
+  auto plan = [&](const void* kernel, int rows) {
+    const long long items = most_tiles(a, rows), filled = a.tokens / rows;
+    const unsigned C = width_of(kernel, items);
+    const long long tiles = a.seq_start ? std::min<long long>(items, std::max<long long>(a.n_seq, filled + a.n_seq / 2)) : items;          // as many as are to be expected
+    return Plan{items, C, (double)((tiles * C + sm_count() - 1) / sm_count()) / C};
+  };
+  const Plan few = plan((const void*)lowrank_tile_kernel<X, W, kRows>, kRows), many = plan((const void*)lowrank_tile_kernel<X, W, 64>, 64);
+  if (1.4 * many.cost < few.cost) return launch_tile<X, W, 64>(p, many.items, many.C, s);
+  return launch_tile<X, W, kRows>(p, few.items, few.C, s);
 }
 
 template <typename W>

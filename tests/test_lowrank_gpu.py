@@ -96,6 +96,13 @@ def test_types(x, w, y):
     check(Case(1, [5, 1, 40], 200, 136, 24, [1, 0, 2], x, w, y, mix="first"))
 
 
+@pytest.mark.parametrize("mix", [None, "rows", "first"])
+@pytest.mark.parametrize("x,w,y", [(x, w, y) for x in TYPES for w in ("f16", "bf16") for y in TYPES])
+def test_types_of_long_sequences(x, w, y, mix):
+    """Rows enough for the wide tiles, some of them full, others with a row or with most of them."""
+    check(Case(2, [300, 1, 129, 56], 328, 264, 40, [1, 0, 2, -1], x, w, y, mix=mix, pad=3))
+
+
 @pytest.mark.parametrize("ic,oc", [(8, 8), (16, 24), (32, 16), (40, 1000), (264, 8), (512, 4096), (2048, 2048), (4104, 72), (7168, 264), (9000, 40)])
 @pytest.mark.parametrize("rank", [8, 16, 40, 128])
 def test_sizes(ic, oc, rank):
@@ -185,7 +192,7 @@ def test_a_row_of_infinities_or_nan_is_its_own():
             assert torch.equal(got[keep], clean[keep]) and not torch.isfinite(got[7]).any()
 
 
-@pytest.mark.parametrize("lens", [[1, 2, 1, 5], [70, 33]])
+@pytest.mark.parametrize("lens", [[1, 2, 1, 5], [70, 33], [330, 64]])
 @pytest.mark.parametrize("x", TYPES)
 def test_an_infinity_beside_f16_weights(x, lens):
     """The rows of such inputs are brought to a common size by their largest finite number."""
@@ -198,7 +205,7 @@ def test_an_infinity_beside_f16_weights(x, lens):
         assert torch.equal(got[keep], clean[keep]) and not torch.isfinite(got[7]).any()
 
 
-@pytest.mark.parametrize("lens", [[1] * 30, [5, 1, 12, 12], [30], [100, 64]])
+@pytest.mark.parametrize("lens", [[1] * 30, [5, 1, 12, 12], [30], [100, 64], [330, 64]])
 @pytest.mark.parametrize("x,mix", [("f32", None), ("f32", "rows"), ("bf16", None), ("bf16", "rows"), ("bf16", "first")])
 def test_rows_of_all_sizes_beside_f16_weights(x, mix, lens):
     """Rows from 2^-100 to 2^100, some with one number far above the others, some all zero."""
