@@ -160,7 +160,9 @@ __device__ __forceinline__ void find_rows(const Args& p, long long item, Tile& t
       // many rows: an item is a row, which takes the next fifteen of its adapter if it is the first, seventeenth, ... of these
       const int mine = a.adapter[item];
       int before = 0;
-      for (int i = tid; i < item && tid < kThreads; i += kThreads) before += a.adapter[i] == mine;
+      if (tid < kThreads)
+#pragma unroll 8
+        for (int i = tid; i < item; i += kThreads) before += a.adapter[i] == mine;
       for (int o = 16; o > 0; o /= 2) before += __shfl_xor_sync(~0u, before, o);
       if (lane == 0 && warp < kWarps) scratch[warp] = before;
       __syncthreads();
@@ -168,12 +170,18 @@ __device__ __forceinline__ void find_rows(const Args& p, long long item, Tile& t
       for (int w = 0; w < kWarps; ++w) before += scratch[w];
       if (before % kRows == 0 && tid < 32 && mine != -1) {
         int n = 0;
-        for (int i0 = (int)item; i0 < a.n_seq && n < kRows; i0 += 32) {
-          const int i = i0 + tid;
-          const uint32_t same = __ballot_sync(~0u, i < a.n_seq && a.adapter[i] == mine);
-          const int at = n + __popc(same & ((1u << tid) - 1));
-          if ((same >> tid & 1) && at < kRows) t.rows[at] = i;
-          n = min(kRows, n + __popc(same));
+        for (int i0 = (int)item; i0 < a.n_seq && n < kRows; i0 += 256) {
+          int there[8];
+#pragma unroll
+          for (int h = 0; h < 8; ++h) there[h] = a.adapter[min(i0 + h * 32 + tid, a.n_seq - 1)];
+#pragma unroll
+          for (int h = 0; h < 8; ++h) {
+            const int i = i0 + h * 32 + tid;
+            const uint32_t same = __ballot_sync(~0u, i < a.n_seq && there[h] == mine);
+            const int at = n + __popc(same & ((1u << tid) - 1));
+            if ((same >> tid & 1) && at < kRows) t.rows[at] = i;
+            n = min(kRows, n + __popc(same));
+          }
         }
         if (tid == 0) { t.n = n; t.seq = (int)item; }
       }

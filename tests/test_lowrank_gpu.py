@@ -172,6 +172,15 @@ def test_the_shift_is_that_of_the_products():
     assert torch.equal(c.call(listed=False).cpu(), mixed.float())
 
 
+@pytest.mark.parametrize("n,adapters", [(40, 1100), (257, 1), (700, 700), (1500, 40)])
+def test_many_rows_or_many_adapters(n, adapters):
+    g = torch.Generator().manual_seed(n)
+    adapter = (torch.randint(0, adapters, (n,), generator=g) if adapters < n else torch.randperm(adapters, generator=g)[:n]).tolist()
+    adapter[n // 2] = -1
+    c = Case(n, [1] * n, 72, 40, 8, adapter, "bf16", "f16" if n % 2 else "bf16", "f32" if n % 2 else "f16")
+    check(c, listed=False)
+
+
 def test_strided_rows():
     c = Case(11, [70], 136, 72, 16, [0], "bf16", "bf16", "f16", mix="rows")
     wide = lambda t, k: torch.full((t.shape[0], t.shape[1] + k), math.nan, dtype=t.dtype).cuda()
