@@ -10,7 +10,7 @@
 // in two f16 terms under a power of two per row that brings its largest number to 2^14 (off by up to 2^-22 of it, or 2^-38 of the row's largest).
 //
 // Bytes bind the large calls and latency the small ones, and what such a block does besides: one token (2048 x 2048, rank 16) 6.9 us, of which the launch is 2.5; 96 sequences with 64 adapters
-// (4096 x 4096) 19 us, 2.3 TB/s of what it reads; a prompt of 2048 rows 23 us, 2.2 TB/s, floor 7.8.  As many tensor products as there are cost little: the roles are laid out so that copies never wait.  The first
+// (4096 x 4096) 19 us, 2.3 TB/s of what it reads; a prompt of 2048 rows 21 us, 2.5 TB/s, floor 7.8.  As many tensor products as there are cost little: the roles are laid out so that copies never wait.  The first
 // form, on mma.sync with sixteen rows a tile, took 10, 39 and 84 us.
 //
 // A block takes all of an SM's shared memory, so that no other one that wants tensor memory is beside it: tcgen05.alloc has no limit to its wait, and a block
@@ -44,7 +44,7 @@ struct TileShape {
   // read).  Many rows: one product after another into the same accumulator.
   static constexpr bool kBeside = NT == 16;
   static constexpr int kColsA = kBeside ? NT * kTerms : NT, kColsB = kBeside ? NT * 3 : NT;        // of an accumulator
-  static constexpr int kAcc = NT == 64 ? 2 : 4, kTmemCols = 256;
+  static constexpr int kAcc = 4, kTmemCols = NT == 64 ? 512 : 256;
   static_assert(kColsA + kAcc * kColsB <= kTmemCols, "tensor memory");
   // The warps that read an accumulator, sixteen of its rows' columns each: a quarter of 64 rows, or all of sixteen, of every second tile.
   static constexpr int kReaders = NT == 64 ? 16 : 4, kReadCols = 16;
@@ -55,7 +55,7 @@ struct TileShape {
   static_assert(kShare >= 8 * kMostCounted || NT == 64, "room for counting the rows of adapters");
 };
 struct TileCtrl {
-  uint64_t full[kMostRing], empty[kMostRing], masked[kMostRing + 1], ready, xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
+  uint64_t y_full[16], full[kMostRing], empty[kMostRing], masked[kMostRing + 1], ready, xfull[kMostGroups], xempty[kMostGroups], a_done, full_acc[kMostAcc], empty_acc[kMostAcc], drained;
   int abort_flag, asked, x_asked;
   uint32_t tmem_base;
   float back[64];                 // of each row: the power of two that its A x was divided by
@@ -195,7 +195,7 @@ __device__ __forceinline__ void reduce_y(const Args& p, const Tile& t, TileCtrl&
 }
 
 // The same to y of 16 bits, which is rounded once.  A lane of the accumulator is a column; the way to four neighbouring columns a lane is through shared memory, where the shares were
-// (a column a lane, without that, took 32 us where this takes 24: 2048 rows of 4096 columns; what bounds it is the number of accesses).
+// (a column a lane, without that, took 32 us where this took 24 when it served 2048 rows of 4096 columns, too; what bounds it is the number of accesses).
 template <typename S, typename Y, bool kScaled>
 __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, bool grouped, float* share, int last_term, bool& ok) {
   static_assert(sizeof(Y) == 2, "");
@@ -209,7 +209,7 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
     const int r = w.col0 + max(min(i * 4 + r_lane, w.rows - 1), -w.col0);
     at[i] = static_cast<Y*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row;
   }
-  // y of the next tiles is on its way while this one's is added to, 48 KB an SM (into buffers that take turns, not moved: a move waits for what it moves)
+  // y of the next tiles is on its way while this one's is added to (into buffers that take turns, not moved: a move waits for what it moves)
   constexpr int kDepth = 3;
   uint2 buffers[kDepth][H::kCols / 4];
   auto load = [&](int o, uint2 (&to)[H::kCols / 4]) {
@@ -253,6 +253,93 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
   }
 }
 
+// 16 lanes x 16 columns, as a product's sums lie in registers: lane / 4 (and 8 more) by two neighbouring columns for each pair of registers.  Waits for them.
+__device__ __forceinline__ void tmem_ld_pairs(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]) :: "memory");
+}
+// The same for rows that lie one behind the other: y comes to shared memory through a map, sixteen rows at a time for each four warps, where the shares were and behind A x (three or four tiles' worth), and lies in registers
+// as the sums do when it is read transposed; it goes out in rows of 256 bytes.  Eight accesses of a warp to a tile where the way above takes 28
+// (2048 rows, bf16: 20.7 us where that took 22.7).
+template <typename S, typename Y, bool kScaled>
+__device__ __forceinline__ void store_y_rows(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, float* share, bool& ok) {
+  const rwkvq_lowrank_args& a = p.a;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = warp & 3, group = warp >> 2, tiles = o1 - o0;
+  const int rows = min(n - group * 16, 16);              // of this group, maybe none
+  // A x as operands, in two terms, leaves room behind it
+  constexpr int kY = 2 + (S::kXBytes - 4 * S::kTileBytes) / (16 << 10);
+  const uint32_t first = smem_u32(share) - (uint32_t)(kY - 2) * (16u << 10) + (uint32_t)group * 4096u, full = smem_u32(&ctrl.y_full[group * 4]);
+  auto ask = [&](int o) {                                // by one warp of the group
+    const int at = o % kY, row = t.first + group * 16, col = (o0 + o) * 128;
+    const bool second = col + 64 < a.oc;
+    if (lane == 0) tc5::mbar_arrive_expect_tx(&ctrl.y_full[group * 4 + at], second ? 4096u : 2048u);
+    __syncwarp();
+    const uint32_t to = first + (uint32_t)at * (16u << 10), bar = full + (uint32_t)at * 8u;
+    tensor_g2s(to, &p.Y, col, row, 0, bar);
+    if (second) tensor_g2s(to + 2048u, &p.Y, col + 64, row, 0, bar);
+  };
+  auto meet = [&] { asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory"); };
+  int asked = 0;
+  if (quarter == 0 && rows > 0) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    for (; asked < min(tiles, kY); ++asked) ask(asked);
+  }
+  // of the transposed 8 x 8 blocks: rows 0 to 7 and columns 0 to 7, columns 8 to 15, and the same of rows 8 to 15
+  const int m = lane >> 3, token = (m >> 1) * 8 + (lane & 7);
+  float back[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) back[j] = kScaled ? ctrl.back[max(min(group * 16 + (j >> 1) * 8 + (lane & 3) * 2 + (j & 1), n - 1), 0)] : 1.f;
+#pragma unroll 1
+  for (int o = 0; o < tiles; ++o) {
+    const int acc = o % S::kAcc;
+    ok = ok && tc5::mbar_wait(smem_u32(&ctrl.full_acc[acc]), (uint32_t)(o / S::kAcc) & 1u, &ctrl.abort_flag, p.status);
+    ok = __all_sync(~0u, ok);                            // one that gives up goes through all the meetings
+    tc5::tc_fence_after();
+    uint32_t v[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) tmem_ld_pairs(acc0 + (uint32_t)(acc * S::kColsB + group * 16) + ((uint32_t)(h * 16) << 16), v[h]);
+    tc5::tc_fence_before();
+    __syncwarp();
+    if (lane == 0) tc5::mbar_arrive(&ctrl.empty_acc[acc]);
+    if (rows <= 0) continue;
+    ok = ok && tc5::mbar_wait(full + (uint32_t)(o % kY) * 8u, (uint32_t)(o / kY) & 1u, &ctrl.abort_flag, p.status);
+    ok = __all_sync(~0u, ok);
+    const uint32_t tile = first + (uint32_t)(o % kY) * (16u << 10);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t at = tile + (uint32_t)(quarter >> 1) * 2048u + swizzled(token, (quarter & 1) * 4 + h * 2 + (m & 1));
+      uint32_t y[4];
+      asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(at) : "memory");
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float2 f = pair_of(y[j], Y());
+        f.x = fmaf(__uint_as_float(v[h][2 * j]), back[(j >> 1) * 2], f.x);
+        f.y = fmaf(__uint_as_float(v[h][2 * j + 1]), back[(j >> 1) * 2 + 1], f.y);
+        y[j] = rounded(f, Y());
+      }
+      asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+    }
+    meet();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = quarter * 4 + i * 2 + (lane >> 4), eight = lane & 15, col = (o0 + o) * 128 + eight * 8;
+      uint4 w;
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(tile + (uint32_t)(eight >> 3) * 2048u + swizzled(row, eight & 7)) : "memory");
+      if (ok && row < rows && col < a.oc) *reinterpret_cast<uint4*>(static_cast<Y*>(a.y) + (long long)(t.first + group * 16 + row) * a.y_row + col) = w;
+    }
+    meet();
+    if (quarter == 0 && ok && asked < tiles) {
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      ask(asked++);
+    }
+  }
+  // not left before its copies are there
+  if (!ok && quarter == 0)
+    for (int o = max(0, asked - kY); o < asked; ++o)
+      for (uint32_t k = 0; k < tc5::kPollLimit && !tc5::mbar_try_wait(full + (uint32_t)(o % kY) * 8u, (uint32_t)(o / kY) & 1u); ++k) {}
+}
+
 template <typename X, typename W, int NT>
 __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_kernel(const __grid_constant__ Args p) {
   using S = TileShape<X, W, NT>;
@@ -278,6 +365,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
     for (int i = 0; i <= S::kRing; ++i) tc5::mbar_init(&ctrl.masked[i], 1);
     for (int i = 0; i < S::kGroups; ++i) { tc5::mbar_init(&ctrl.xfull[i], p.x_by_map ? 1 : S::kWorkers); tc5::mbar_init(&ctrl.xempty[i], 1); }
     for (int i = 0; i < S::kAcc; ++i) { tc5::mbar_init(&ctrl.full_acc[i], 1); tc5::mbar_init(&ctrl.empty_acc[i], S::kReaders); }
+    for (int i = 0; i < 16; ++i) tc5::mbar_init(&ctrl.y_full[i], 1);
     tc5::mbar_init(&ctrl.a_done, 1); tc5::mbar_init(&ctrl.ready, 1); tc5::mbar_init(&ctrl.drained, 1);
     ctrl.abort_flag = ctrl.asked = ctrl.x_asked = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\nfence.proxy.async.shared::cta;" ::: "memory");
@@ -556,8 +644,8 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
       tc5::umma_commit(&ctrl.full_acc[acc]);
     }
   } else if (warp > S::kWorkers + 1) {
-    // One of two warps that have nothing to do yet looks up the adapter, the other has x fetched to the second-level cache, ahead of the weights, behind which each load takes
-    // some 5000 cycles; and y's rows, which are read when all else is done, once A x is computed.
+    // One of two warps that have nothing to do yet looks up the adapter, the other has x fetched to the second-level cache, ahead of the weights, behind which a load takes
+    // some 5000 cycles, and y's rows, which are read when all else is done; but for those that come through maps of their own (x and y of 2048 rows, bf16: 22.0 us with, 20.7 without).
     auto fetch = [](const void* base, long long at, int elements, int size) {
       if (elements > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const uint8_t*>(base) + at * size), "r"(elements * size) : "memory");
     };
@@ -567,7 +655,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
         tc5::mbar_arrive(&ctrl.ready);
       }
       __syncwarp();
-    } else {
+    } else if (!p.x_by_map) {
       const int columns = min((k0 + np) * 64, a.ic) - k0 * 64;
       for (int r = lane; r < n; r += 32) {
         fetch(a.x, (long long)row_of(r) * a.x_row + k0 * 64, columns, (int)sizeof(X));
@@ -575,7 +663,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
       }
     }
     if (!settle()) return;
-    if (warp == S::kWorkers + 3) {
+    if (warp == S::kWorkers + 3 && (NT == kRows || a.y_dtype == RWKVQ_F32)) {
       for (int r = lane; r < n; r += 32) fetch(a.y, (long long)row_of(r) * a.y_row + o0 * 128, min(o1 * 128, a.oc) - o0 * 128, a.y_dtype == RWKVQ_F32 ? 4 : 2);
       __syncwarp();
     }
@@ -710,8 +798,13 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
 
     // ---- y
     if (a.y_dtype == RWKVQ_F32) reduce_y<S, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
-    else if (a.y_dtype == RWKVQ_F16) store_y<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
-    else store_y<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
+    else if constexpr (NT == 64) {
+      if (a.y_dtype == RWKVQ_F16) store_y_rows<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, share, ok);
+      else store_y_rows<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, share, ok);
+    } else {
+      if (a.y_dtype == RWKVQ_F16) store_y<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
+      else store_y<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
+    }
   }
   if (warp == S::kWorkers || warp > S::kWorkers + 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   tc5::tc_fence_before();
@@ -790,14 +883,14 @@ cudaError_t launch_tile(Args& p, long long items, unsigned C, cudaStream_t s) {
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return cudaErrorUnknown;
   }
-  p.y_by_map = 0;
-  if (NT == 64 && a.y_dtype == RWKVQ_F32) {
-    const cuuint64_t dims[2] = {(cuuint64_t)a.oc, (cuuint64_t)a.tokens}, strides[1] = {(cuuint64_t)a.y_row * 4};
-    const cuuint32_t box[2] = {32, 16}, step[2] = {1, 1};
-    if (fn(&p.Y, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, a.y, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+  p.y_by_map = NT == 64;
+  if (p.y_by_map) {
+    const bool wide = a.y_dtype == RWKVQ_F32;
+    const cuuint64_t dims[3] = {(cuuint64_t)a.oc, (cuuint64_t)a.tokens, 1}, row = (cuuint64_t)a.y_row * (wide ? 4 : 2), strides[2] = {row, row * (cuuint64_t)a.tokens};
+    const cuuint32_t box[3] = {wide ? 32u : 64u, 16, 1}, step[3] = {1, 1, 1};
+    if (fn(&p.Y, wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : a.y_dtype == RWKVQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, wide ? 2 : 3, a.y, dims, strides, box, step,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, wide ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return cudaErrorUnknown;
-    p.y_by_map = 1;
   }
   static SmemOptIn opt_in(kCarveOut);
   const cudaError_t e = opt_in((const void*)lowrank_tile_kernel<X, W, NT>, kSmemBytes);
