@@ -9,7 +9,7 @@
 // A x, in fp32, goes on in bf16 terms (three, all of it, where y has 32 bits; two, the second rounded, where y has 16: off by up to 2^-16 of it), or, where the weights are f16,
 // in two f16 terms under a power of two per row that brings its largest number to 2^14 (off by up to 2^-22 of it, or 2^-38 of the row's largest).
 //
-// Bytes bind the large calls and latency the small ones, and what such a block does besides: one token (2048 x 2048, rank 16) 6.9 us, of which the launch is 2.5; 96 sequences with 64 adapters
+// Bytes bind the large calls and latency the small ones, and what such a block does besides: one token (2048 x 2048, rank 16) 6.8 us, of which the launch is 2.5; 96 sequences with 64 adapters
 // (4096 x 4096) 19 us, 2.3 TB/s of what it reads; a prompt of 2048 rows 21 us, 2.5 TB/s, floor 7.8.  As many tensor products as there are cost little: the roles are laid out so that copies never wait.  The first
 // form, on mma.sync with sixteen rows a tile, took 10, 39 and 84 us.
 //
@@ -915,7 +915,7 @@ cudaError_t launch_form(Args& p, cudaStream_t s) {
     return launch_tile<X, W, kRows>(p, items, width_of((const void*)lowrank_tile_kernel<X, W, kRows>, items), s);
   }
   // A tile takes its time by the width of its cluster, and one of 64 rows some 1.4 times that of one of sixteen (4096 x 4096, us, sixteen / 64: prompts of 203 rows 10.0 / 11.4, 448 13.7 / 11.8, 2048
-  // 42 / 23; f16 and rank 128, forty sequences of ten rows 29 / 42, sixty 51 / 40, 96 52 / 73), so that the wider tiles are taken where they leave room for wider clusters, or for fewer rounds.
+  // 42 / 22.6; f16 and rank 128, forty sequences of ten rows 29 / 42, sixty 51 / 40, 96 52 / 73), so that the wider tiles are taken where they leave room for wider clusters, or for fewer rounds.
   struct Plan { long long items; unsigned C; double cost; };
   auto plan = [&](const void* kernel, int rows) {
     const long long items = most_tiles(a, rows), filled = a.tokens / rows;
