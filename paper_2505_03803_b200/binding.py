@@ -888,6 +888,8 @@ def rwkvq_lowrank(x, A, B, y, adapter, seq_start=None, ranks=None, scale=None, x
     oc = y_shape[1]
     if y_shape[0] != tokens:
         _refuse(where, f"y has to have {tokens} rows")
+    if x_prev is not None and (x_prev.dtype is not dtype or x_prev.shape != x_shape):
+        _refuse(where, f"x_prev has to be {list(x_shape)} of {dtype}")
     rows = []
     for z in (x, y) if x_prev is None else (x, y, x_prev):
         if z.get_device() != here:
@@ -911,8 +913,6 @@ def rwkvq_lowrank(x, A, B, y, adapter, seq_start=None, ranks=None, scale=None, x
         _check_list(where, ranks, n_adapters, "ranks", here, t.int32)
     if scale is not None:
         _check_list(where, scale, n_adapters, "scale", here, t.float32)
-    if x_prev is not None and (x_prev.dtype is not dtype or x_prev.shape != x_shape):
-        _refuse(where, f"x_prev has to be {list(x_shape)} of {dtype}")
     if xprev0 is not None:
         _check_list(where, xprev0, n_seq * ic, "xprev0", here, dtype)
     if (mu_image is None) != (mu_desc is None) or (mu_image is None and not (x_prev is None and xprev0 is None)):

@@ -337,3 +337,13 @@ def test_behind_32_bits():
     want = c.call(listed=False)
     big.copy_(c.x)
     assert torch.equal(c.call(listed=False, x=big), want)
+
+
+def test_tensors_of_other_shapes_are_refused():
+    c = Case(16, [4], 64, 48, 16, [0], mix="rows")
+    cuda = lambda t: t.cuda()
+    for over in (dict(x_prev=cuda(c.x_prev)[:3]), dict(x_prev=cuda(c.x_prev).unsqueeze(0)), dict(x_prev=cuda(c.x_prev).float()), dict(A=cuda(c.A)[:, :8]), dict(A=cuda(c.A).transpose(0, 1)),
+                 dict(B=cuda(c.B)[:1]), dict(B=cuda(c.B).float()), dict(y=cuda(c.y)[:3]), dict(y=cuda(c.y).t()), dict(x=cuda(c.x).t().contiguous().t()), dict(adapter=torch.zeros(1, dtype=torch.int64, device="cuda")),
+                 dict(scale=torch.ones(1, device="cuda")), dict(ranks=torch.ones(c.n, device="cuda")), dict(mu_image=None), dict(x=cuda(c.x).double()), dict(adapter=torch.zeros(1, dtype=torch.int32))):
+        with pytest.raises((ValueError, B.RwkvqError)):
+            c.call(listed=False, **over)
