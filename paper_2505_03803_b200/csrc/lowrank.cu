@@ -6,8 +6,8 @@
 // shared memory in their order: one launch, no workspace.  Weights come through tensor maps into a ring of seven slots, B's under the meeting of the blocks; x through a map, too, or,
 // where it has to be mixed with the row before or taken apart (see Form), by the warps that read the accumulators later.
 //
-// A x, in fp32, goes on in bf16 terms (three, all of it, where y has 32 bits; two, the second rounded, where y has 16: off by up to 2^-16 of it), or, where the weights are f16,
-// in two f16 terms under a power of two per row that brings its largest number to 2^14 (off by up to 2^-22 of it, or 2^-38 of the row's largest).
+// A x, in fp32, goes on in three bf16 terms, which are all of it, or, where the weights are f16, in two f16 terms under a power of two per row that brings its largest number to
+// 2^14 (off by up to 2^-22 of it, or 2^-38 of the row's largest).
 //
 // Bytes bind the large calls and latency the small ones, and what such a block does besides: one token (2048 x 2048, rank 16) 6.8 us, of which the launch is 2.5; 96 sequences with 64 adapters
 // (4096 x 4096) 19 us, 2.3 TB/s of what it reads; a prompt of 2048 rows 21 us, 2.5 TB/s, floor 7.8.  As many tensor products as there are cost little: the roles are laid out so that copies never wait.  The first
@@ -259,16 +259,16 @@ __device__ __forceinline__ void tmem_ld_pairs(uint32_t taddr, uint32_t (&r)[8]) 
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
   asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]) :: "memory");
 }
-// The same for rows that lie one behind the other: y comes to shared memory through a map, sixteen rows at a time for each four warps, where the shares were and behind A x (three or four tiles' worth), and lies in registers
+// The same for rows that lie one behind the other: y comes to shared memory through a map, sixteen rows at a time for each four warps, where the shares were and behind A x (two to four tiles' worth), and lies in registers
 // as the sums do when it is read transposed; it goes out in rows of 256 bytes.  Eight accesses of a warp to a tile where the way above takes 28
-// (2048 rows, bf16: 20.7 us where that took 22.7).
-template <typename S, typename Y, bool kScaled>
+// (2048 rows, bf16: 20.7 us where that took 22.7, A x in two terms; in all three it takes 21.1).
+template <typename S, typename Y, bool kScaled, int kTerms>
 __device__ __forceinline__ void store_y_rows(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, float* share, bool& ok) {
   const rwkvq_lowrank_args& a = p.a;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = warp & 3, group = warp >> 2, tiles = o1 - o0;
   const int rows = min(n - group * 16, 16);              // of this group, maybe none
-  // A x as operands, in two terms, leaves room behind it
-  constexpr int kY = 2 + (S::kXBytes - 4 * S::kTileBytes) / (16 << 10);
+  // A x as operands, of up to 128 numbers a row, leaves room behind it
+  constexpr int kY = 2 + (S::kXBytes - 2 * kTerms * S::kTileBytes) / (16 << 10);
   const uint32_t first = smem_u32(share) - (uint32_t)(kY - 2) * (16u << 10) + (uint32_t)group * 4096u, full = smem_u32(&ctrl.y_full[group * 4]);
   auto ask = [&](int o) {                                // by one warp of the group
     const int at = o % kY, row = t.first + group * 16, col = (o0 + o) * 128;
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
   // What depends on the adapter, which one thread looks up while x is on its way; false where there is none: the same for all blocks of the cluster.
   int rank = 0, blocks = 0, wide = 0, a_slot = 1, n_a = 0;
   bool masks = false;
-  const int last_term = kHalf ? 1 : a.y_dtype == RWKVQ_F32 ? 2 : 1;
+  constexpr int last_term = kHalf ? 1 : 2;
   auto settle = [&] {
     wait(smem_u32(&ctrl.ready), 0);
     if (t.n == 0) return false;
@@ -773,7 +773,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
           for (int k = 0; k < 3; ++k) {
             __nv_bfloat16 b[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = k == 1 && last_term == 1 ? __float2bfloat16_rn(h[j]) : term(h[j]);
+            for (int j = 0; j < 4; ++j) b[j] = term(h[j]);
             terms[k] = make_uint2(pair_bits(b[0], b[1]), pair_bits(b[2], b[3]));
           }
         }
@@ -783,7 +783,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
             uint8_t* const there_to = cluster.map_shared_rank(to, k);
             *reinterpret_cast<uint2*>(there_to) = terms[0];
             *reinterpret_cast<uint2*>(there_to + next) = terms[1];
-            if (!kHalf && last_term == 2) *reinterpret_cast<uint2*>(there_to + 2 * next) = terms[2];
+            if (!kHalf) *reinterpret_cast<uint2*>(there_to + 2 * next) = terms[2];
             if (kHalf && r4 == 0) *cluster.map_shared_rank(&ctrl.back[row], k) = back;
           }
       }
@@ -799,8 +799,8 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
     // ---- y
     if (a.y_dtype == RWKVQ_F32) reduce_y<S, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
     else if constexpr (NT == 64) {
-      if (a.y_dtype == RWKVQ_F16) store_y_rows<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, share, ok);
-      else store_y_rows<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, share, ok);
+      if (a.y_dtype == RWKVQ_F16) store_y_rows<S, __half, kHalf, last_term + 1>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, share, ok);
+      else store_y_rows<S, __nv_bfloat16, kHalf, last_term + 1>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, share, ok);
     } else {
       if (a.y_dtype == RWKVQ_F16) store_y<S, __half, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
       else store_y<S, __nv_bfloat16, kHalf>(p, t, ctrl, lanes + S::kColsA, o0, o1, n, grouped, share, last_term, ok);
