@@ -398,7 +398,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
   constexpr int last_term = kHalf ? 1 : 2;
   auto settle = [&] {
     wait(smem_u32(&ctrl.ready), 0);
-    if (t.n == 0) return false;
+    if (!t.counts) return false;
     rank = t.rank; blocks = (rank + 15) / 16; wide = (rank + 63) / 64;
     a_slot = pieces_of(blocks); n_a = (np + a_slot - 1) / a_slot;          // pieces of A in a slot, and slots
     // What lies behind the adapter's rank may be anything: in B's last sixteen columns it is masked, unless these end the rows, where a box has zeros.
@@ -651,7 +651,7 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
     };
     if (warp == S::kWorkers + 2) {
       if (lane == 0) {
-        if (!(grouped && by_groups(a))) find_adapter(p, t);
+        find_adapter(p, t);
         tc5::mbar_arrive(&ctrl.ready);
       }
       __syncwarp();

@@ -38,6 +38,7 @@ struct Tile {
   int first, n, seq, start;     // of others: row `first` on, of the sequence that begins at `start`
   int adapter, rank;
   float scale;
+  int counts;                   // has an adapter of a rank above 0: written, by one thread, only when all of the block may have read n
 };
 
 // The tile that is the item-th among all tiles of kTile rows of the sequences in seq_start; t.n stays 0 where there is none.  A sequence counts whose rows exist and that
@@ -102,13 +103,13 @@ inline long long most_tiles(const rwkvq_lowrank_args& a, int rows) {
   return a.seq_start ? std::min<long long>(a.tokens, whole + a.n_seq) : !single_rows(a) ? whole : by_groups(a) ? std::min<long long>(a.n_seq, a.n_adapters + whole) : (long long)a.n_seq;
 }
 
-// The rows of a tile of up to kTile; of single rows that share an adapter (then t.n is final, and adapter, rank and scale are known, too) or of a sequence.  All threads.
+// The rows of a tile of up to kTile; of single rows that share an adapter (then adapter, rank and scale are known, too) or of a sequence.  All threads; t.n stays as it is behind this.
 // scratch: 2 * kWarps + 2 numbers; memory: 8 * kMostCounted bytes.
 template <int kTile>
 __device__ __forceinline__ void find_rows(const Args& p, long long item, Tile& t, int* scratch, void* memory) {
   const rwkvq_lowrank_args& a = p.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (tid == 0) { t.n = 0; t.adapter = -1; }
+  if (tid == 0) { t.n = t.counts = 0; t.adapter = -1; }
   if (!single_rows(a)) {
     if (a.seq_start) {
       __syncthreads();
@@ -190,9 +191,10 @@ __device__ __forceinline__ void find_rows(const Args& p, long long item, Tile& t
   __syncthreads();
 }
 
-// Adapter, rank and scale of a tile whose rows are known, by one thread; t.n is 0 where it has none.
+// Adapter, rank and scale of a tile whose rows are known, and whether they count, by one thread.  The others may be reading t.n, each for itself: it is not touched.
 __device__ __forceinline__ void find_adapter(const Args& p, Tile& t) {
   const rwkvq_lowrank_args& a = p.a;
+  t.counts = t.n > 0 && t.adapter >= 0;
   if (t.n == 0 || t.adapter >= 0) return;
   const int mine = a.adapter[t.seq], at = min(max(mine, 0), a.n_adapters - 1);
   // both loads at once, from where something is
@@ -200,9 +202,8 @@ __device__ __forceinline__ void find_adapter(const Args& p, Tile& t) {
   const float scale_there = *(a.scale ? a.scale + at : reinterpret_cast<const float*>(a.adapter));
   const int rank = a.ranks ? rank_there : a.rank;
   const bool bad = mine < -1 || mine >= a.n_adapters || (mine >= 0 && (rank < 0 || rank > a.rank));
-  if (!bad && mine >= 0 && rank > 0) { t.adapter = mine; t.rank = rank; t.scale = a.scale ? scale_there : 1.f; }
+  if (!bad && mine >= 0 && rank > 0) { t.adapter = mine; t.rank = rank; t.scale = a.scale ? scale_there : 1.f; t.counts = 1; }
   if (bad) atomicExch(p.status, (int)RWKVQ_EINVAL);
-  if (bad || t.adapter < 0) t.n = 0;
 }
 
 // ---- numbers and operands -----------------------------------------------------------------------------------
