@@ -828,29 +828,47 @@ __global__ void __launch_bounds__((TileShape<X, W, NT>::kAll), 1) lowrank_tile_k
   if (warp == S::kWorkers + 1) tc5::tmem_dealloc(ctrl.tmem_base, S::kTmemCols);
 }
 
-// Clusters of C blocks that are on the device at once; asked for once per device (the kernels are alike in this: one block an SM).
-long long clusters_at_once(const void* kernel, unsigned C) {
-  static std::atomic<int> known[kMaxDevices][4];
+template <typename X, typename W, int NT>
+cudaError_t opt_in_tile() {
+  static SmemOptIn opt_in(kCarveOut);
+  return opt_in((const void*)lowrank_tile_kernel<X, W, NT>, kSmemBytes);
+}
+
+// Clusters of C blocks that are on the device at once; asked for once per device and kernel.  What is asked for is answered with none as long as the kernel may not have its shared
+// memory, so that is seen to first: how a call is cut, and with that the order of its sums, depends on the call and the device alone, not on the calls before.
+template <typename X, typename W, int NT>
+cudaError_t clusters_at_once(unsigned C, long long* n) {
+  static std::atomic<int> known[kMaxDevices][4];          // and one more: 0 is not known
   const int dev = current_device(), h = C == 8 ? 3 : C == 4 ? 2 : C == 2 ? 1 : 0;
-  int n = dev >= 0 ? known[dev][h].load(std::memory_order_relaxed) : 0;
-  if (n > 0) return n;
+  int got = dev >= 0 ? known[dev][h].load(std::memory_order_relaxed) : 0;
+  if (got > 0) { *n = got - 1; return cudaSuccess; }
+  cudaError_t e = opt_in_tile<X, W, NT>();
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(C); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.gridDim = dim3(C); cfg.blockDim = dim3(TileShape<X, W, NT>::kAll); cfg.dynamicSmemBytes = kSmemBytes;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) { cudaGetLastError(); return std::max(1u, sm_count() * 3 / 4 / C); }
-  if (dev >= 0) known[dev][h].store(n, std::memory_order_relaxed);
-  return n;
+  e = cudaOccupancyMaxActiveClusters(&got, (const void*)lowrank_tile_kernel<X, W, NT>, &cfg);
+  if (e != cudaSuccess) { cudaGetLastError(); return e; }
+  got = std::max(got, 0);
+  if (dev >= 0) known[dev][h].store(got + 1, std::memory_order_relaxed);
+  *n = got;
+  return cudaSuccess;
 }
 
 // One block an SM: clusters as wide as are there at once.  Wide clusters leave SMs over (132 of 148 can be in clusters of four, 120 in clusters of eight: what is behind them starts when
 // all is done).
-unsigned width_of(const void* kernel, long long items) {
-  unsigned C = 8;
-  while (C > 1 && items > clusters_at_once(kernel, C)) C /= 2;
-  return C;
+template <typename X, typename W, int NT>
+cudaError_t width_of(long long items, unsigned* C) {
+  for (*C = 8; *C > 1; *C /= 2) {
+    long long at_once = 0;
+    const cudaError_t e = clusters_at_once<X, W, NT>(*C, &at_once);
+    if (e != cudaSuccess) return e;
+    if (items <= at_once) break;
+  }
+  return cudaSuccess;
 }
 
 template <typename X, typename W, int NT>
@@ -892,11 +910,12 @@ cudaError_t launch_tile(Args& p, long long items, unsigned C, cudaStream_t s) {
            CU_TENSOR_MAP_INTERLEAVE_NONE, wide ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return cudaErrorUnknown;
   }
-  static SmemOptIn opt_in(kCarveOut);
-  const cudaError_t e = opt_in((const void*)lowrank_tile_kernel<X, W, NT>, kSmemBytes);
+  long long at_once = 0;
+  cudaError_t e = opt_in_tile<X, W, NT>();
+  if (e == cudaSuccess) e = clusters_at_once<X, W, NT>(C, &at_once);
   if (e != cudaSuccess) return e;
   // where all clusters are as wide as can be and SMs are left, several divide a tile's rows of B and each multiplies A x for itself
-  p.splits = (int)std::max<long long>(1, std::min<long long>({clusters_at_once((const void*)lowrank_tile_kernel<X, W, NT>, C) / items, (a.oc + 128ll * C - 1) / (128 * C), 16}));
+  p.splits = (int)std::max<long long>(1, std::min<long long>({at_once / items, (a.oc + 128ll * C - 1) / (128 * C), 16}));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(items * C * p.splits)); cfg.blockDim = dim3(S::kAll); cfg.dynamicSmemBytes = kSmemBytes; cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -912,18 +931,24 @@ cudaError_t launch_form(Args& p, cudaStream_t s) {
   const rwkvq_lowrank_args& a = p.a;
   if (single_rows(a)) {
     const long long items = most_tiles(a, kRows);
-    return launch_tile<X, W, kRows>(p, items, width_of((const void*)lowrank_tile_kernel<X, W, kRows>, items), s);
+    unsigned C = 1;
+    const cudaError_t e = width_of<X, W, kRows>(items, &C);
+    return e != cudaSuccess ? e : launch_tile<X, W, kRows>(p, items, C, s);
   }
   // A tile takes its time by the width of its cluster, and one of 64 rows some 1.4 times that of one of sixteen (4096 x 4096, us, sixteen / 64: prompts of 203 rows 10.0 / 11.4, 448 13.7 / 11.8, 2048
   // 42 / 22.6; f16 and rank 128, forty sequences of ten rows 29 / 42, sixty 51 / 40, 96 52 / 73), so that the wider tiles are taken where they leave room for wider clusters, or for fewer rounds.
   struct Plan { long long items; unsigned C; double cost; };
-  auto plan = [&](const void* kernel, int rows) {
+  cudaError_t e = cudaSuccess;
+  auto plan = [&](auto of_rows) {
+    constexpr int rows = decltype(of_rows)::value;
     const long long items = most_tiles(a, rows), filled = a.tokens / rows;
-    const unsigned C = width_of(kernel, items);
+    unsigned C = 1;
+    if (e == cudaSuccess) e = width_of<X, W, rows>(items, &C);
     const long long tiles = a.seq_start ? std::min<long long>(items, std::max<long long>(a.n_seq, filled + a.n_seq / 2)) : items;          // as many as are to be expected
     return Plan{items, C, (double)((tiles * C + sm_count() - 1) / sm_count()) / C};
   };
-  const Plan few = plan((const void*)lowrank_tile_kernel<X, W, kRows>, kRows), many = plan((const void*)lowrank_tile_kernel<X, W, 64>, 64);
+  const Plan few = plan(std::integral_constant<int, kRows>()), many = plan(std::integral_constant<int, 64>());
+  if (e != cudaSuccess) return e;
   if (1.4 * many.cost < few.cost) return launch_tile<X, W, 64>(p, many.items, many.C, s);
   return launch_tile<X, W, kRows>(p, few.items, few.C, s);
 }
