@@ -415,12 +415,14 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
     }
   }
   __syncthreads();
-  // As in a piece: a warp's q-th best are passed by q candidates, those of all full warps by enough.  By the total rounded to fp32, which keeps the order.
+  // As in a piece: a warp's q-th best are passed by q candidates, those of all full warps by enough.  By the total rounded to fp32, which keeps the order; a total that fp32 has no
+  // room for (a score and a mask of the type's lowest value) is a candidate all the same, above none at all.
+  auto coarse = [](const Candidate& y) { return max(order_of((float)value_of(y.total)), 1u); };
   Candidate x[kHeld];
   uint32_t order[kHeld], top = 0, bound = 0;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
-    order[i] = c0 + i * step < all && candidate(held_k[i], held[i], x[i]) ? order_of((float)value_of(x[i].total)) : 0u;
+    order[i] = c0 + i * step < all && candidate(held_k[i], held[i], x[i]) ? coarse(x[i]) : 0u;
     top = max(top, order[i]);
   }
 #pragma unroll 1
@@ -428,7 +430,7 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
     Candidate y;
     int k;
     const uint2 b = fetch(c, k);
-    if (candidate(k, b, y)) top = max(top, order_of((float)value_of(y.total)));
+    if (candidate(k, b, y)) top = max(top, coarse(y));
   }
   const int q = (P + full - 1) / full;
   if (q <= 32 && all >= 32) {
@@ -450,7 +452,7 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
     Candidate y;
     int k;
     const uint2 b = fetch(c, k);
-    if (candidate(k, b, y) && order_of((float)value_of(y.total)) >= bound) keep(y);
+    if (candidate(k, b, y) && coarse(y) >= bound) keep(y);
   }
   __syncthreads();
   int n = count;
