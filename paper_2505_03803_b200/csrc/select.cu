@@ -348,8 +348,8 @@ __device__ __forceinline__ bool above(const Candidate& x, const Candidate& y) { 
 __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
   constexpr int kHeld = 2;                         // candidates that a thread keeps; those behind them are made anew where they are needed
   __shared__ double offset[kMostBeams], most[kMostBeams];      // score - log(sum) and m, of which a logit's total is offset + (logit - m); of a beam that ended, its score
-  __shared__ int kind[kMostBeams];                 // 0: no candidates, 1: of its logits, 2: ended, 3: of its logits, the largest of which is +inf
-  __shared__ int alive[kMostBeams], n_alive;       // beams of kind 1 to 3
+  __shared__ int kind[kMostBeams];                 // 0: no candidates, 1: of its logits, 2: ended; not written again, as it is read while sums and maxima are still joined
+  __shared__ int alive[kMostBeams], n_alive;       // beams of kind 1 and 2
   __shared__ Candidate list[kList], warp_best[kWarps];
   __shared__ uint32_t warp_low[kWarps];
   __shared__ int count;
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
       const int k = lane + 32 * h;
       const float score = k < K ? a.scores[r0 + k] : INFINITY;
       kinds[h] = !(score > -INFINITY && score < INFINITY) ? 0 : a.finished && a.finished[r0 + k] ? 2 : 1;
-      if (k < K) { kind[k] = kinds[h]; offset[k] = (double)score; }
+      if (k < K) { kind[k] = kinds[h]; offset[k] = (double)score; most[k] = 0.0; }
     }
     const uint32_t bx = __ballot_sync(~0u, kinds[0]), by = __ballot_sync(~0u, kinds[1]), low = (1u << lane) - 1;
     if (kinds[0]) alive[__popc(bx & low)] = lane;
@@ -386,8 +386,9 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
       return b.y == 0;
     }
     const float v = __uint_as_float(b.x);
-    x.total = order_of(kind[k] == 3 ? offset[k] : offset[k] + ((double)v - most[k])); x.place = place_of(k, v, b.y);
-    return kind[k] == 3 ? v == INFINITY : v > -INFINITY;
+    const bool infinite = most[k] == INFINITY;          // the logits of +inf share the probability
+    x.total = order_of(infinite ? offset[k] : offset[k] + ((double)v - most[k])); x.place = place_of(k, v, b.y);
+    return infinite ? v == INFINITY : v > -INFINITY;
   };
   asm volatile("griddepcontrol.wait;" ::: "memory");
   uint2 held[kHeld];
@@ -411,7 +412,6 @@ __global__ void __launch_bounds__(kThreads) beam_merge_kernel(const Args a) {
     if (lane == 0 && some) {
       offset[k] -= log(S);
       most[k] = (double)M;
-      if (M == INFINITY) kind[k] = 3;
     }
   }
   __syncthreads();
