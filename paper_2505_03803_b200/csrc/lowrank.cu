@@ -3,7 +3,7 @@
 //
 // The rows are the 16- to 64-column operand and the weights the 128-row one: A x is one accumulator of 128 (of the rank) by the tile's rows, B (A x) one for each 128 rows
 // of B, whose lanes are neighbouring columns of y.  A cluster of blocks divides the columns of A and the rows of B; A x is summed over the blocks through distributed
-// shared memory in their order: one launch, no workspace.  Weights come through tensor maps into a ring of seven slots, B's under the meeting of the blocks; x through a map, too, or,
+// shared memory in their order: one launch, no workspace.  Weights come through tensor maps into a ring of seven to eleven slots, B's under the meeting of the blocks; x through a map, too, or,
 // where it has to be mixed with the row before or taken apart (see Form), by the warps that read the accumulators later.
 //
 // A x, in fp32, goes on in three bf16 terms, which are all of it, or, where the weights are f16, in two f16 terms under a power of two per row that brings its largest number to
@@ -88,23 +88,17 @@ __device__ __forceinline__ void umma(uint32_t tmem_d, uint64_t adesc, uint64_t b
 // 32 lanes x kCols columns; see tc5::tmem_ld32_issue.  Waits for them.
 template <int kCols>
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[kCols]) {
-  if constexpr (kCols == 32) {
-    tc5::tmem_ld32_issue(taddr, r);
-    tc5::tmem_ld_wait(r);
+  static_assert(kCols == 8 || kCols == 16, "");
+  if constexpr (kCols == 16) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+                   "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                 "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
   } else {
-    static_assert(kCols == 8 || kCols == 16, "");
-    if constexpr (kCols == 16) {
-      asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
-                     "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
-      asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
-                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
-      return;
-    } else {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
     asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]) :: "memory");
-    }
   }
 }
 __device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, int v, uint32_t bar) {
@@ -194,19 +188,19 @@ __device__ __forceinline__ void reduce_y(const Args& p, const Tile& t, TileCtrl&
   asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
-// The same to y of 16 bits, which is rounded once.  A lane of the accumulator is a column; the way to four neighbouring columns a lane is through shared memory, where the shares were
+// The same to y of 16 bits, which is rounded once, for tiles of sixteen rows.  A lane of the accumulator is a column; the way to four neighbouring columns a lane is through shared memory, where the shares were
 // (a column a lane, without that, took 32 us where this took 24 when it served 2048 rows of 4096 columns, too; what bounds it is the number of accesses).
 template <typename S, typename Y, bool kScaled>
 __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& ctrl, uint32_t acc0, int o0, int o1, int n, bool grouped, float* share, int last_term, bool& ok) {
-  static_assert(sizeof(Y) == 2, "");
+  static_assert(sizeof(Y) == 2 && S::kBeside, "");
   const rwkvq_lowrank_args& a = p.a;
   using H = Share<S>;
   const H w(n, share);
   const int quad = w.lane & 7, r_lane = w.lane >> 3;
-  Y* at[H::kCols / 4];                                  // rows r_lane, r_lane + 4, ...; those behind the last are read, where there are any at all, as the last
+  Y* at[H::kCols / 4];                                  // rows r_lane, r_lane + 4, ...; those behind the last are read as the last
 #pragma unroll
   for (int i = 0; i < H::kCols / 4; ++i) {
-    const int r = w.col0 + max(min(i * 4 + r_lane, w.rows - 1), -w.col0);
+    const int r = min(i * 4 + r_lane, w.rows - 1);
     at[i] = static_cast<Y*>(a.y) + (long long)(grouped ? t.rows[r] : t.first + r) * a.y_row;
   }
   // y of the next tiles is on its way while this one's is added to (into buffers that take turns, not moved: a move waits for what it moves)
@@ -214,7 +208,7 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
   uint2 buffers[kDepth][H::kCols / 4];
   auto load = [&](int o, uint2 (&to)[H::kCols / 4]) {
     const int col = min((o0 + o) * 128 + w.quarter * 32 + quad * 4, a.oc - 4);
-    if (w.rows > 0 && o < o1 - o0)
+    if (o < o1 - o0)
 #pragma unroll
       for (int i = 0; i < H::kCols / 4; ++i) to[i] = *reinterpret_cast<const uint2*>(at[i] + col);
   };
@@ -229,7 +223,6 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
     uint2 (&y)[H::kCols / 4] = buffers[turn_of];
     float sum[H::kCols];
     if (!w.take(p, ctrl, acc0, o, last_term, ok, sum)) return;
-    if (w.rows <= 0) continue;
     // [row][column], rows of 128 bytes: each lane a column, then each quarter of a warp a row
 #pragma unroll
     for (int h = 0; h < H::kCols / H::kTurn; ++h) {
@@ -241,7 +234,7 @@ __device__ __forceinline__ void store_y(const Args& p, const Tile& t, TileCtrl& 
       for (int i = 0; i < H::kTurn / 4; ++i) {
         const int r = h * H::kTurn + i * 4 + r_lane;
         float4 d = *reinterpret_cast<const float4*>(w.turn + (i * 4 + r_lane) * 32 + quad * 4);
-        if constexpr (kScaled) { const float back = ctrl.back[min(w.col0 + r, n - 1)]; d.x *= back; d.y *= back; d.z *= back; d.w *= back; }
+        if constexpr (kScaled) { const float back = ctrl.back[min(r, n - 1)]; d.x *= back; d.y *= back; d.z *= back; d.w *= back; }
         uint2& mine = y[h * H::kTurn / 4 + i];
         const float2 lo = pair_of(mine.x, Y()), hi = pair_of(mine.y, Y());
         mine = make_uint2(rounded(make_float2(lo.x + d.x, lo.y + d.y), Y()), rounded(make_float2(hi.x + d.z, hi.y + d.w), Y()));
