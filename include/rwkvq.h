@@ -499,7 +499,8 @@ rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace_dev, 
  *      captured call serves other batches.
  *  mu_desc, mu_image (both or neither): the token shift of the products, x_mix = x + (x_prev - x) (.) mu_hat, rounded to x_dtype as theirs is.  x_prev[tokens][ic] (x_prev_row
  *      elements from row to row, as in rwkvq_gemv), or NULL: the row before in the sequence, and in front of its first xprev0[n_seq][ic] (NULL: zeros; as in rwkvq_gemm_prefill).
- * Products are exact and summed in fp32, in a fixed order.  bf16 weights: all of A x goes on, in three parts of eight bits.  f16 weights: x of another type is rounded to 24 bits or 2^-39 of the largest of its row, A x to 22 bits or 2^-38 of its largest.  An infinity or NaN in x
+ * Products are exact and summed in fp32, in a fixed order, by tensor cores, which may cut off up to 2^-23 of what they add to where an fp32 addition rounds by 2^-24 (4096 columns: off by some
+ * 2e-6 of the largest, an fp32 product by 1e-6).  bf16 weights: all of A x goes on, in three parts of eight bits.  f16 weights: x of another type is rounded to 24 bits or 2^-39 of the largest of its row, A x to 22 bits or 2^-38 of its largest.  An infinity or NaN in x
  * is seen by its own row alone, where an infinity may come out as NaN; infinite weights may come out as NaN.
  * Subnormal numbers in a y of 32 bits may be taken for zeros.
  * A sequence whose rows do not exist or that begins in front of any entry of seq_start before its own, whose adapter does not exist, or whose adapter's rank is not in range: it is left out, the others are computed, and
@@ -532,7 +533,8 @@ rwkvq_status rwkvq_lowrank(const rwkvq_lowrank_args* args, const rwkvq_desc* mu_
  *  finished: [requests][beams] bytes, or NULL: a beam that has ended (not 0) has one candidate, token eos with its score unchanged, and its logits do not count.
  *  next_scores, parents, tokens: [requests][picks]: the totals (fp32), their beams and tokens.  finished_out: [requests][picks] bytes, or NULL: whether the parent had ended or the token is eos.
  *      next_scores, finished_out and scores, finished are different buffers.
- * Maxima and sums of a thread are fp32, of a row and the totals fp64: they are compared before they are rounded (and where they are equal, within a beam the logits).
+ * Maxima and sums of a thread are fp32, of a row and the totals fp64: they are compared before they are rounded (and where they are equal, within a beam the logits).  The logarithm
+ * of a beam is off by up to 2^-15, some 1e-6 as a rule: beams that lie nearer to one another may change places; those with equal logits and scores are equal, and go by their numbers.
  * workspace_dev: rwkvq_beam_select_workspace_bytes() bytes (enough for fewer requests, beams, tokens and picks, too), 16-byte aligned, contents irrelevant, not shared by calls in flight at the same time.
  * logits aligned to their type, scores and outputs to 4 bytes.  Asynchronous on `stream`.  rwkvq_state_reorder moves the states as `parents` says.
  * Errors: EINVAL (picks above beams * vocab, eos outside the vocabulary with `finished` or `finished_out`, ...), EALIGN, EUNSUPPORTED (more than 64 beams or picks, 2^24 tokens,

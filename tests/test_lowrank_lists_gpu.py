@@ -31,3 +31,30 @@ def test_tiles_without_an_adapter(x, w, mix, lens):
     assert B.rwkvq_device_status() == 0 and all(torch.equal(y, want) for y in ys)
     none = torch.full((n,), -1, dtype=torch.int32, device="cuda")
     assert torch.equal(c.call(adapter=none).cpu(), c.y) and B.rwkvq_device_status() == 0
+
+
+@pytest.mark.parametrize("lens", [[5, 30, 4], [500, 3000, 400]])
+def test_rows_of_bad_lists(lens):
+    """Which rows a list that does not rise, or leaves the rows there are, computes and which it leaves, each of them."""
+    c = Case(13, lens, 64, 48, 16, [0, 1, 0])
+    want, before = c.call().cpu(), c.y
+    n0, n1, T = lens[0], lens[0] + lens[1], sum(lens)
+    for starts, ranges in (([0, n0, n1, T + 1], [(0, n1)]),                    # the last ends behind the rows
+                           ([0, n0, n0 - 2, T], [(0, n0)]),                    # one ends before it begins, the next begins in front of an earlier entry
+                           ([-1, n0, n1, T], [(n0, T)]),
+                           ([0, n0, n1, 2 ** 31 - 1], [(0, n1)]),
+                           ([0, n1, n0, T], [(0, n1)]),                        # the second is [n1, n0), the third lies inside the first
+                           ([n0, n1, n1, n1 - 1], [])):
+        got = c.call(seq_start=torch.tensor(starts, dtype=torch.int32, device="cuda")).cpu()
+        assert B.rwkvq_device_status() == 1
+        if starts[0] > 0:          # the first is [n0, n1) with the adapter of the first, the second is empty, the third ends before it begins
+            assert torch.equal(got[:n0], before[:n0]) and torch.equal(got[n1:], before[n1:]) and not torch.equal(got[n0:n1], before[n0:n1])
+            continue
+        if starts[1] == n1:        # the first takes the second's rows, too, with its own adapter
+            assert torch.equal(got[:n0], want[:n0]) and torch.equal(got[n1:], before[n1:]) and not torch.equal(got[n0:n1], before[n0:n1])
+            continue
+        keep = torch.ones(T, dtype=torch.bool)
+        for a, b in ranges:
+            assert torch.equal(got[a:b], want[a:b])
+            keep[a:b] = False
+        assert torch.equal(got[keep], before[keep])
