@@ -500,7 +500,7 @@ rwkvq_status rwkvq_linattn(const rwkvq_linattn_args* args, void* workspace_dev, 
  *  mu_desc, mu_image (both or neither): the token shift of the products, x_mix = x + (x_prev - x) (.) mu_hat, rounded to x_dtype as theirs is.  x_prev[tokens][ic] (x_prev_row
  *      elements from row to row, as in rwkvq_gemv), or NULL: the row before in the sequence, and in front of its first xprev0[n_seq][ic] (NULL: zeros; as in rwkvq_gemm_prefill).
  * Products are exact and summed in fp32, in a fixed order, by tensor cores, which may cut off up to 2^-23 of what they add to where an fp32 addition rounds by 2^-24 (4096 columns: off by some
- * 2e-6 of the largest, an fp32 product by 1e-6).  bf16 weights: all of A x goes on, in three parts of eight bits.  f16 weights: x of another type is rounded to 24 bits or 2^-39 of the largest of its row, A x to 22 bits or 2^-38 of its largest.  An infinity or NaN in x
+ * 1.3e-6 of the largest output, an fp32 product by 1.0e-6).  bf16 weights: all of A x goes on, in three parts of eight bits.  f16 weights: x of another type is rounded to 24 bits or 2^-39 of the largest of its row, A x to 22 bits or 2^-38 of its largest.  An infinity or NaN in x
  * is seen by its own row alone, where an infinity may come out as NaN; infinite weights may come out as NaN.
  * Subnormal numbers in a y of 32 bits may be taken for zeros.
  * A sequence whose rows do not exist or that begins in front of any entry of seq_start before its own, whose adapter does not exist, or whose adapter's rank is not in range: it is left out, the others are computed, and

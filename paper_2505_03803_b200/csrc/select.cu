@@ -9,7 +9,7 @@
 // ones, q = ceil(picks / 8), is passed by q elements in each of the block's eight warps (or as many as a short row has elements for), so that what is below the least of these cannot be among the best:
 // a few dozen elements of the tile are left, and ranked by counting.  From the second tile on the last best element is the bound, and hardly any tile has one above it.
 //
-// 256 rows of 65536 bf16 logits and sixteen picks take 24 us (1.3 TB/s; 9.3 M warp instructions, 57 % of the issue slots, no unit full: the rest is waiting, at the ends of pieces above all), four rows 6.2, of which
+// 256 rows of 65536 bf16 logits and sixteen picks take 24 us (1.3 TB/s; 9.3 M warp instructions, 58 % of the issue slots, no unit full: the rest is waiting, at the ends of pieces above all), four rows 6.2, of which
 // two launches are 3.  First 71 and 14: packed
 // conversions and maxima, four blocks an SM for three, candidates ranked by four threads each.
 #include <cuda_runtime.h>
