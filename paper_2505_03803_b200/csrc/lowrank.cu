@@ -970,7 +970,7 @@ rwkvq_status rwkvq_lowrank(const rwkvq_lowrank_args* args, const rwkvq_desc* mu_
   if (a.tokens < 0 || a.n_seq <= 0 || a.ic <= 0 || a.oc <= 0 || a.rank <= 0 || a.n_adapters <= 0) return RWKVQ_EINVAL;
   if (!a.A || !a.B || !a.adapter || (a.tokens > 0 && (!a.x || !a.y))) return RWKVQ_EINVAL;
   if (!a.seq_start && a.n_seq != 1 && a.n_seq != a.tokens) return RWKVQ_EINVAL;
-  if ((mu_image && !mu_desc) || ((a.x_prev || a.xprev0) && !mu_image) || (a.x_prev && a.xprev0)) return RWKVQ_EINVAL;
+  if (!mu_image != !mu_desc || ((a.x_prev || a.xprev0) && !mu_image) || (a.x_prev && a.xprev0)) return RWKVQ_EINVAL;
   if (a.rank > lr::kMostRank || a.n_seq > 65535 || a.tokens > (1 << 24) || a.ic > (1 << 24) || a.oc > (1 << 24)) return RWKVQ_EUNSUPPORTED;
   if (a.ic % 8 || a.oc % 8 || a.rank % 8) return RWKVQ_ESHAPE;
   if (mu_image) {
